@@ -14,6 +14,14 @@
  *   qlin_linear_fused          NVFP4 GEMM whose epilogue also re-quantizes the
  *                              bf16 output to NVFP4 for the next layer
  *
+ * and adds what stands around those linears in a transformer block:
+ *
+ *   qlin_rmsnorm[_fp8/_nvfp4]  residual addition and root-mean-square norm, its
+ *                              output quantized for the next linear
+ *   qlin_linear_nvfp4 / _fp8   linears with bias, activation and residual in the
+ *     / _bf16 / _fp16          epilogue, from one token up
+ *   qlin_rope                  rotary positions on q and k
+ *
  * Formats (the paper names them and cites their definitions; it fixes no block
  * size or rounding rule, so the readings taken here are stated per call):
  *   - E4M3: FP8 with exponent bias 7, max 448, NaN = S.1111.111, no infinity
@@ -291,6 +299,190 @@ qlin_status qlin_gemm_fp16(const void *a_fp16, int64_t lda, const void *w_fp16, 
 qlin_status qlin_linear_dynamic(const qlin_nvfp4_t *A, const qlin_nvfp4_t *W, void *y_bf16,
                                 qlin_nvfp4_t *y_q, void *workspace, size_t ws_bytes,
                                 void *stream);
+
+/* ------------------------------------------------------------------------
+ * Around the linears of a transformer block.  16-bit data of the calls below is
+ * bf16 or fp16.
+ */
+typedef enum { QLIN_BF16 = 1, QLIN_FP16 = 2 } qlin_float16;
+
+/*
+ * Root-mean-square norm with the residual's addition.  Per row, in fp32:
+ *   s = x + residual (x without one);   sum = s rounded to 16 bits;
+ *   n = (s * (1 / sqrt(mean(s^2) + eps))) * weight.
+ * n is computed from s itself, not from the rounded sum, and is rounded once, to
+ * the output's format.  A row whose squares overflow fp32 is normalised through
+ * scaled squares; a row with an infinity or a NaN becomes NaN.
+ *  x:        16-bit [M, K], rows x_stride elements apart (a multiple of 8, >= K).
+ *  residual: the same with residual_stride, or NULL.
+ *  sum:      receives x + residual (rows sum_stride apart), or NULL.  May be x or
+ *            residual itself (same pointer and stride).  NULL without a residual.
+ *  weight:   16-bit [K], or NULL for ones.
+ *  eps:      finite, > 0.
+ *  dtype:    QLIN_BF16 or QLIN_FP16, of x, residual, sum, weight and a 16-bit y.
+ * Pointers are 16-byte aligned; K % 64 == 0.
+ */
+typedef struct {
+  const void *x;
+  const void *residual;
+  void *sum;
+  const void *weight;
+  int64_t x_stride, residual_stride, sum_stride;
+  int64_t M, K;
+  float eps;
+  int32_t dtype;
+} qlin_rmsnorm_t;
+
+/* y = n in 16 bits, [M, K] with rows K apart.  y may be x itself where x's rows
+ * are K apart.  Errors: INVALID_ARG, MISALIGNED, UNSUPPORTED, CUDA. */
+qlin_status qlin_rmsnorm(const qlin_rmsnorm_t *args, void *y, void *stream);
+
+/*
+ * n as the FP8 input of a linear:
+ *   out->per_channel != 0, static_scale NULL: one scale per row (token),
+ *     scale[m] = max_k |n| / 448 (1 for an all-zero row), found in the same launch;
+ *   out->per_channel == 0: static_scale is the device S_dec; scale[0] receives it.
+ *   code = E4M3(n * S_enc), S_enc = 1 / S_dec (FLT_MAX if that overflows).
+ * Errors: INVALID_ARG, MISALIGNED, UNSUPPORTED, CUDA.
+ */
+qlin_status qlin_rmsnorm_fp8(const qlin_rmsnorm_t *args, const float *static_scale,
+                             qlin_fp8_t *out, void *stream);
+
+/* n as the NVFP4 input of a linear with the static tensor scale *static_scale:
+ * the blocks of qlin_quantize_act_nvfp4, taken from n in fp32.
+ * Errors: INVALID_ARG, MISALIGNED, UNSUPPORTED, CUDA. */
+qlin_status qlin_rmsnorm_nvfp4(const qlin_rmsnorm_t *args, const float *static_scale,
+                               qlin_nvfp4_t *out, void *stream);
+
+/* Activations of the linears below.  GELU_TANH is
+ * 0.5 v (1 + tanh(sqrt(2/pi) (v + 0.044715 v^3))), GELU 0.5 v erfc(-v / sqrt 2),
+ * SILU v / (1 + exp(-v)). */
+typedef enum {
+  QLIN_ACT_NONE = 0,
+  QLIN_ACT_RELU = 1,
+  QLIN_ACT_SILU = 2,
+  QLIN_ACT_GELU_TANH = 3,
+  QLIN_ACT_GELU = 4
+} qlin_activation;
+
+/*
+ * What a linear's epilogue does with its fp32 products before the one rounding to
+ * the 16-bit output:
+ *   y = round16( act( products + bias[n] ) + residual[m, n] ).
+ *  bias:     16-bit [N] of the output's type, 16-byte aligned, or NULL.
+ *  residual: 16-bit [M, N] of the output's type, rows residual_stride elements
+ *            apart (a multiple of 8, >= N), 16-byte aligned, or NULL.  May be y
+ *            itself (residual_stride == N); otherwise it must not overlap y.
+ */
+typedef struct {
+  const void *bias;
+  const void *residual;
+  int64_t residual_stride;
+  int32_t act;
+} qlin_epilogue_t;
+
+/*
+ * qlin_linear_fused with the epilogue above in place of the plain rounding
+ * (epilogue NULL: none of it): y_bf16, next_scale, y_q and rq_col0 as there.
+ * Errors: INVALID_ARG, MISALIGNED, UNSUPPORTED, CUDA.
+ */
+qlin_status qlin_linear_nvfp4(const qlin_nvfp4_t *A, const qlin_nvfp4_t *W,
+                              const qlin_epilogue_t *epilogue, void *y_bf16,
+                              const float *next_scale, qlin_nvfp4_t *y_q, int64_t rq_col0,
+                              void *stream);
+
+/*
+ * The FP8 linear with that epilogue; the products are
+ *   (S_A[m] * S_W[n]) * sum_k e4m3(a) * e4m3(w),
+ * with one scale for A (per_channel == 0) or one per row (per_channel != 0, as
+ * qlin_rmsnorm_fp8 writes them).  next_scale NULL: no re-quantization (then y_bf16
+ * must be non-NULL); else as in qlin_linear_fused_fp8.
+ * Errors: INVALID_ARG, MISALIGNED, UNSUPPORTED, CUDA.
+ */
+qlin_status qlin_linear_fp8(const qlin_fp8_t *A, const qlin_fp8_t *W,
+                            const qlin_epilogue_t *epilogue, void *y_bf16,
+                            const float *next_scale, qlin_fp8_t *y_q, int64_t rq_col0,
+                            void *stream);
+
+/* qlin_gemm_bf16 / qlin_gemm_fp16 with that epilogue. */
+qlin_status qlin_linear_bf16(const void *a_bf16, int64_t lda, const void *w_bf16, int64_t M,
+                             int64_t N, int64_t K, const qlin_epilogue_t *epilogue,
+                             void *y_bf16, void *stream);
+qlin_status qlin_linear_fp16(const void *a_fp16, int64_t lda, const void *w_fp16, int64_t M,
+                             int64_t N, int64_t K, const qlin_epilogue_t *epilogue,
+                             void *y_fp16, void *stream);
+
+/*
+ * Rotary positions.  Pair i of a head's first rot_dim elements turns by the angle
+ * positions[t, axis of i] * f_i:
+ *   (a, b) -> magnitude * (a cos - b sin, a sin + b cos)
+ * (inverse: by the negative angle, which is the gradient of the forward rotation).
+ * Elements past rot_dim are copied.  fp32 arithmetic, one rounding.
+ *  x, y:      16-bit [tokens, heads, head_dim], head_dim contiguous, any strides (in
+ *             elements) of tokens and heads; y may be x itself with the same
+ *             strides, else the two must not overlap.  2-byte aligned; 16-byte
+ *             aligned rows of multiples of 8 elements take 16-byte accesses.
+ *  positions: int32 or int64 (position_bits) [tokens, axes] with strides in
+ *             elements; any values, negative ones too.
+ *  turns:     device uint64 [rot_dim / 2]: each pair's turns per position, f_i /
+ *             (2 pi), in units of 2^-64 turn.  position * turns modulo 2^64 is the
+ *             angle modulo whole turns without rounding, so that angles stay exact
+ *             at any position.
+ *  axis_pairs: how many pairs follow each of the `axes` (1 to 4) positions of a
+ *             token, in order; they add up to rot_dim / 2.
+ *  layout:    QLIN_ROPE_INTERLEAVED pairs elements (2i, 2i + 1), QLIN_ROPE_HALF
+ *             (i, i + rot_dim / 2).
+ * tokens, heads >= 1; rot_dim even, 2 <= rot_dim <= head_dim <= 1024.
+ * Errors: INVALID_ARG, MISALIGNED, UNSUPPORTED, CUDA.
+ */
+typedef enum { QLIN_ROPE_INTERLEAVED = 0, QLIN_ROPE_HALF = 1 } qlin_rope_layout;
+
+typedef struct {
+  const void *x;
+  void *y;
+  int64_t x_token_stride, x_head_stride;
+  int64_t y_token_stride, y_head_stride;
+  int64_t tokens, heads;
+  const void *positions;
+  int64_t position_token_stride, position_axis_stride;
+  const uint64_t *turns;
+  float magnitude;
+  int32_t head_dim, rot_dim;
+  int32_t position_bits;
+  int32_t axes;
+  int32_t axis_pairs[4];
+  int32_t layout;
+  int32_t inverse;
+  int32_t dtype;
+} qlin_rope_t;
+
+qlin_status qlin_rope(const qlin_rope_t *args, void *stream);
+
+/*
+ * Fills turns (HOST memory, rot_dim / 2 entries) for f_i = base^(-2i / rot_dim)
+ * scaled for contexts longer than `trained_length`, and *magnitude:
+ *   QLIN_ROPE_NONE    f_i;                             magnitude 1
+ *   QLIN_ROPE_LINEAR  f_i / factor;                    magnitude 1
+ *   QLIN_ROPE_NTK     base * factor^(rot_dim / (rot_dim - 2)) in place of base
+ *                     (f_i / factor where rot_dim is 2); magnitude 1
+ *   QLIN_ROPE_YARN    (Peng et al. 2023) f_i where a pair turns more than beta_fast
+ *                     times over trained_length, f_i / factor where less than
+ *                     beta_slow times, a linear ramp in i between (from
+ *                     floor(i_fast) to ceil(i_slow), inside [0, rot_dim - 1]);
+ *                     magnitude 0.1 ln(factor) + 1
+ * Host arithmetic in 64 bits.  base > 1; factor >= 1 (ignored by NONE); for YARN
+ * trained_length > 0 and beta_fast > beta_slow > 0.  Errors: INVALID_ARG.
+ */
+typedef enum {
+  QLIN_ROPE_NONE = 0,
+  QLIN_ROPE_LINEAR = 1,
+  QLIN_ROPE_NTK = 2,
+  QLIN_ROPE_YARN = 3
+} qlin_rope_scaling;
+
+qlin_status qlin_rope_turns(int32_t rot_dim, double base, int32_t scaling, double factor,
+                            double trained_length, double beta_fast, double beta_slow,
+                            uint64_t *turns, float *magnitude);
 
 /*
  * Waits for `stream`, then returns and clears the device status word:

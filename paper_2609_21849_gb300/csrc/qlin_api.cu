@@ -1,6 +1,7 @@
 // The C ABI of libqlin (declared in include/qlin.h): argument validation on
 // the host, then launches on the caller's stream.  No call allocates memory.
 #include <atomic>
+#include <cmath>
 #include <cstdio>
 #include <cstring>
 #include <mutex>
@@ -231,10 +232,27 @@ qlin_status qlin_quantize_weight(const void* w_bf16, int64_t N, int64_t K, qlin_
   return QLIN_OK;
 }
 
+// Bias, activation and residual of a linear into its GEMM's arguments (M, N set).
+static qlin_status set_epilogue(GemmArgs& a, const qlin_epilogue_t* ep) {
+  if (ep == nullptr) return QLIN_OK;
+  if (ep->act < QLIN_ACT_NONE || ep->act > QLIN_ACT_GELU) return QLIN_ERR_INVALID_ARG;
+  if (ep->residual != nullptr && ep->residual_stride < a.N) return QLIN_ERR_INVALID_ARG;
+  if (!aligned(ep->bias, 16) || !aligned(ep->residual, 16) ||
+      (ep->residual != nullptr && ep->residual_stride % 8 != 0))
+    return QLIN_ERR_MISALIGNED;
+  a.bias = ep->bias;
+  a.residual = ep->residual;
+  a.residual_stride = ep->residual_stride;
+  a.act = ep->act;
+  a.epilogue = a.epilogue || a.bias != nullptr || a.residual != nullptr || a.act != QLIN_ACT_NONE;
+  return QLIN_OK;
+}
+
 static qlin_status gemm_common(bool fp4, const void* Aany, const void* Wany, void* y,
                                const float* next_scale, qlin_nvfp4_t* y_q, int64_t rq_col0,
                                void* stream, unsigned* y_amax = nullptr,
-                               qlin_fp8_t* y_q8 = nullptr, float* y_sdec = nullptr) {
+                               qlin_fp8_t* y_q8 = nullptr, float* y_sdec = nullptr,
+                               const qlin_epilogue_t* ep = nullptr, bool rows_ok = false) {
   GemmArgs a{};
   a.y_amax = y_amax;
   a.y_departures = y_amax != nullptr ? y_amax + 1 : nullptr;
@@ -261,7 +279,9 @@ static qlin_status gemm_common(bool fp4, const void* Aany, const void* Wany, voi
     if (A == nullptr || W == nullptr) return QLIN_ERR_INVALID_ARG;
     QLIN_TRY(check_fp8(A, A->rows, A->K));
     QLIN_TRY(check_fp8(W, W->rows, A->K));
-    if (A->per_channel) return QLIN_ERR_INVALID_ARG;
+    if (A->per_channel && !rows_ok) return QLIN_ERR_INVALID_ARG;
+    a.a_per_row = A->per_channel != 0;
+    a.epilogue = a.a_per_row;
     a.a_codes = A->codes;
     a.w_codes = W->codes;
     a.sdec_a = A->scale;
@@ -275,6 +295,7 @@ static qlin_status gemm_common(bool fp4, const void* Aany, const void* Wany, voi
   if (a.M > (int64_t)1 << 31 || a.N > (int64_t)1 << 31) return QLIN_ERR_UNSUPPORTED;
   if (y != nullptr && !aligned(y, 16)) return QLIN_ERR_MISALIGNED;
   a.y = y;
+  QLIN_TRY(set_epilogue(a, ep));
   if (next_scale != nullptr) {
     // the re-quantized operand: NVFP4 after an NVFP4 GEMM, FP8 after an FP8 one
     const int64_t rq_cols = fp4 ? (y_q ? y_q->K : 0) : (y_q8 ? y_q8->K : 0);
@@ -328,7 +349,8 @@ qlin_status qlin_linear_fused(const qlin_nvfp4_t* A, const qlin_nvfp4_t* W, void
 
 // The unquantized 16-bit linear (bf16 or fp16 operands and output).
 static qlin_status gemm16(const void* a16, int64_t lda, const void* w16, int64_t M, int64_t N,
-                          int64_t K, void* y16, void* stream, bool fp16) {
+                          int64_t K, void* y16, void* stream, bool fp16,
+                          const qlin_epilogue_t* ep = nullptr) {
   if (a16 == nullptr || w16 == nullptr || y16 == nullptr) return QLIN_ERR_INVALID_ARG;
   if (M < 1 || K < 64 || K % 64 != 0 || N < 64 || N % 64 != 0 || lda < K)
     return QLIN_ERR_INVALID_ARG;
@@ -345,6 +367,7 @@ static qlin_status gemm16(const void* a16, int64_t lda, const void* w16, int64_t
   a.M = M;
   a.N = N;
   a.K = K;
+  QLIN_TRY(set_epilogue(a, ep));
   unsigned* status;
   Device dev;
   QLIN_TRY(device_state(&status, &dev));
@@ -390,6 +413,159 @@ qlin_status qlin_linear_fused_fp8(const qlin_fp8_t* A, const qlin_fp8_t* W, void
                                   void* stream) {
   if (next_scale == nullptr) return QLIN_ERR_INVALID_ARG;
   return gemm_common(false, A, W, y_bf16, next_scale, nullptr, rq_col0, stream, nullptr, y_q);
+}
+
+qlin_status qlin_linear_nvfp4(const qlin_nvfp4_t* A, const qlin_nvfp4_t* W,
+                              const qlin_epilogue_t* epilogue, void* y_bf16,
+                              const float* next_scale, qlin_nvfp4_t* y_q, int64_t rq_col0,
+                              void* stream) {
+  return gemm_common(true, A, W, y_bf16, next_scale, y_q, rq_col0, stream, nullptr, nullptr,
+                     nullptr, epilogue);
+}
+
+qlin_status qlin_linear_fp8(const qlin_fp8_t* A, const qlin_fp8_t* W,
+                            const qlin_epilogue_t* epilogue, void* y_bf16,
+                            const float* next_scale, qlin_fp8_t* y_q, int64_t rq_col0,
+                            void* stream) {
+  return gemm_common(false, A, W, y_bf16, next_scale, nullptr, rq_col0, stream, nullptr, y_q,
+                     nullptr, epilogue, true);
+}
+
+qlin_status qlin_linear_bf16(const void* a_bf16, int64_t lda, const void* w_bf16, int64_t M,
+                             int64_t N, int64_t K, const qlin_epilogue_t* epilogue,
+                             void* y_bf16, void* stream) {
+  return gemm16(a_bf16, lda, w_bf16, M, N, K, y_bf16, stream, false, epilogue);
+}
+
+qlin_status qlin_linear_fp16(const void* a_fp16, int64_t lda, const void* w_fp16, int64_t M,
+                             int64_t N, int64_t K, const qlin_epilogue_t* epilogue,
+                             void* y_fp16, void* stream) {
+  return gemm16(a_fp16, lda, w_fp16, M, N, K, y_fp16, stream, true, epilogue);
+}
+
+static qlin_status check_rmsnorm(const qlin_rmsnorm_t* a) {
+  if (a == nullptr || a->x == nullptr || !shape_ok(a->M, a->K)) return QLIN_ERR_INVALID_ARG;
+  if (a->dtype != QLIN_BF16 && a->dtype != QLIN_FP16) return QLIN_ERR_INVALID_ARG;
+  if (!(a->eps > 0.0f) || !std::isfinite(a->eps)) return QLIN_ERR_INVALID_ARG;
+  if (a->sum != nullptr && a->residual == nullptr) return QLIN_ERR_INVALID_ARG;
+  if (a->x_stride < a->K || (a->residual != nullptr && a->residual_stride < a->K) ||
+      (a->sum != nullptr && a->sum_stride < a->K))
+    return QLIN_ERR_INVALID_ARG;
+  if (a->M > INT32_MAX || a->K > INT32_MAX) return QLIN_ERR_UNSUPPORTED;
+  if (!aligned(a->x, 16) || !aligned(a->residual, 16) || !aligned(a->sum, 16) ||
+      !aligned(a->weight, 16) || a->x_stride % 8 != 0 ||
+      (a->residual != nullptr && a->residual_stride % 8 != 0) ||
+      (a->sum != nullptr && a->sum_stride % 8 != 0))
+    return QLIN_ERR_MISALIGNED;
+  return QLIN_OK;
+}
+
+static qlin_status rmsnorm(const qlin_rmsnorm_t* args, void* y16, const float* static_scale,
+                           const qlin_fp8_t* fp8, const qlin_nvfp4_t* nvfp4, void* stream) {
+  unsigned* status;
+  Device dev;
+  QLIN_TRY(device_state(&status, &dev));
+  QLIN_CUDA(launch_rmsnorm(*args, y16, static_scale, fp8, nvfp4, static_cast<cudaStream_t>(stream)));
+  return QLIN_OK;
+}
+
+qlin_status qlin_rmsnorm(const qlin_rmsnorm_t* args, void* y, void* stream) {
+  QLIN_TRY(check_rmsnorm(args));
+  if (y == nullptr) return QLIN_ERR_INVALID_ARG;
+  if (!aligned(y, 16)) return QLIN_ERR_MISALIGNED;
+  return rmsnorm(args, y, nullptr, nullptr, nullptr, stream);
+}
+
+qlin_status qlin_rmsnorm_fp8(const qlin_rmsnorm_t* args, const float* static_scale,
+                             qlin_fp8_t* out, void* stream) {
+  QLIN_TRY(check_rmsnorm(args));
+  QLIN_TRY(check_fp8(out, args->M, args->K));
+  if ((static_scale == nullptr) != (out->per_channel != 0)) return QLIN_ERR_INVALID_ARG;
+  if (!aligned(static_scale, 4)) return QLIN_ERR_MISALIGNED;
+  return rmsnorm(args, nullptr, static_scale, out, nullptr, stream);
+}
+
+qlin_status qlin_rmsnorm_nvfp4(const qlin_rmsnorm_t* args, const float* static_scale,
+                               qlin_nvfp4_t* out, void* stream) {
+  QLIN_TRY(check_rmsnorm(args));
+  QLIN_TRY(check_nvfp4(out, args->M, args->K));
+  if (static_scale == nullptr) return QLIN_ERR_INVALID_ARG;
+  if (!aligned(static_scale, 4)) return QLIN_ERR_MISALIGNED;
+  return rmsnorm(args, nullptr, static_scale, nullptr, out, stream);
+}
+
+qlin_status qlin_rope(const qlin_rope_t* a, void* stream) {
+  if (a == nullptr || a->x == nullptr || a->y == nullptr || a->positions == nullptr ||
+      a->turns == nullptr)
+    return QLIN_ERR_INVALID_ARG;
+  if (a->tokens < 1 || a->heads < 1 || a->rot_dim < 2 || a->rot_dim % 2 != 0 ||
+      a->rot_dim > a->head_dim || a->axes < 1 || a->axes > 4)
+    return QLIN_ERR_INVALID_ARG;
+  if ((a->position_bits != 32 && a->position_bits != 64) ||
+      (a->layout != QLIN_ROPE_INTERLEAVED && a->layout != QLIN_ROPE_HALF) ||
+      (a->dtype != QLIN_BF16 && a->dtype != QLIN_FP16))
+    return QLIN_ERR_INVALID_ARG;
+  int64_t pairs = 0;
+  for (int i = 0; i < a->axes; ++i) {
+    if (a->axis_pairs[i] < 0) return QLIN_ERR_INVALID_ARG;
+    pairs += a->axis_pairs[i];
+  }
+  if (pairs != a->rot_dim / 2) return QLIN_ERR_INVALID_ARG;
+  if (a->x == a->y &&
+      (a->x_token_stride != a->y_token_stride || a->x_head_stride != a->y_head_stride))
+    return QLIN_ERR_INVALID_ARG;
+  // heads * head_dim is indexed in 32 bits
+  if (a->head_dim > 1024 || a->tokens > INT32_MAX || a->heads > INT32_MAX / 1024)
+    return QLIN_ERR_UNSUPPORTED;
+  if (!aligned(a->x, 2) || !aligned(a->y, 2) || !aligned(a->turns, 8) ||
+      !aligned(a->positions, a->position_bits / 8))
+    return QLIN_ERR_MISALIGNED;
+  unsigned* status;
+  Device dev;
+  QLIN_TRY(device_state(&status, &dev));
+  QLIN_CUDA(launch_rope(*a, static_cast<cudaStream_t>(stream)));
+  return QLIN_OK;
+}
+
+qlin_status qlin_rope_turns(int32_t rot_dim, double base, int32_t scaling, double factor,
+                            double trained_length, double beta_fast, double beta_slow,
+                            uint64_t* turns, float* magnitude) {
+  if (turns == nullptr || magnitude == nullptr || rot_dim < 2 || rot_dim % 2 != 0)
+    return QLIN_ERR_INVALID_ARG;
+  if (!std::isfinite(base) || !(base > 1.0) || scaling < QLIN_ROPE_NONE || scaling > QLIN_ROPE_YARN)
+    return QLIN_ERR_INVALID_ARG;
+  if (scaling == QLIN_ROPE_NONE) factor = 1.0;
+  if (!std::isfinite(factor) || !(factor >= 1.0)) return QLIN_ERR_INVALID_ARG;
+  const double kTwoPi = 6.283185307179586476925;
+  const double R = rot_dim;
+  double low = 0.0, high = 0.0;   // YARN: the ramp's first and last pair
+  if (scaling == QLIN_ROPE_YARN) {
+    if (!std::isfinite(trained_length) || !(trained_length > 0.0) || !(beta_slow > 0.0) ||
+        !std::isfinite(beta_fast) || !(beta_fast > beta_slow))
+      return QLIN_ERR_INVALID_ARG;
+    // the pair that turns `beta` times over the trained length
+    auto pair_of = [&](double beta) {
+      return R * std::log(trained_length / (beta * kTwoPi)) / (2.0 * std::log(base));
+    };
+    low = std::max(std::floor(pair_of(beta_fast)), 0.0);
+    high = std::min(std::ceil(pair_of(beta_slow)), R - 1.0);
+  }
+  double b = base;
+  if (scaling == QLIN_ROPE_NTK && rot_dim > 2) {
+    b = base * std::pow(factor, R / (R - 2.0));
+    if (!std::isfinite(b)) return QLIN_ERR_INVALID_ARG;
+  }
+  for (int i = 0; i < rot_dim / 2; ++i) {
+    double f = std::pow(b, -2.0 * i / R);
+    if (scaling == QLIN_ROPE_LINEAR || (scaling == QLIN_ROPE_NTK && rot_dim == 2)) f /= factor;
+    if (scaling == QLIN_ROPE_YARN) {
+      const double ramp = std::min(std::max((i - low) / std::max(high - low, 1e-3), 0.0), 1.0);
+      f = f * (1.0 - ramp) + f / factor * ramp;
+    }
+    turns[i] = (uint64_t)std::nearbyint(std::ldexp(f / kTwoPi, 64));   // f <= 1: below 2^62
+  }
+  *magnitude = scaling == QLIN_ROPE_YARN ? (float)(0.1 * std::log(factor) + 1.0) : 1.0f;
+  return QLIN_OK;
 }
 
 qlin_status qlin_sync_status(void* stream) {

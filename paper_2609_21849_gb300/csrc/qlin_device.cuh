@@ -640,6 +640,43 @@ __device__ __forceinline__ void mul2_rn(float& a, float& b, float s) {
       : "f"(a), "f"(b), "f"(s));
 }
 
+// ---------------------------------------------------------- activations ---
+
+// v / (1 + exp(-u)): SiLU (u = v) and the tanh form of GELU (0.5 (1 + tanh z) is
+// 1 / (1 + exp(-2 z))).  The quotient is 0 where the exponential overflows.
+__device__ __forceinline__ float times_sigmoid(float v, float u) {
+  return __fdividef(v, 1.0f + __expf(-u));
+}
+
+// act (qlin_activation) of every value; the same act in all threads of a warp.
+template <int N>
+__device__ __forceinline__ void activate(float (&v)[N], int act) {
+  switch (act) {
+    case 1:
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] = v[i] < 0.0f ? 0.0f : v[i];   // (a NaN stays)
+      break;
+    case 2:
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] = times_sigmoid(v[i], v[i]);
+      break;
+    case 3:
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        // 2 sqrt(2 / pi) (v + 0.044715 v^3)
+        const float u = v[i] * __fmaf_rn(0.07135481283f, v[i] * v[i], 1.595769122f);
+        v[i] = times_sigmoid(v[i], u);
+      }
+      break;
+    case 4:
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] = 0.5f * v[i] * erfcf(-0.70710678f * v[i]);
+      break;
+    default:
+      break;
+  }
+}
+
 // Byte offset of block scale (row r, scale column c) in the 128x4-atom layout
 // of an operand with K elements per row.
 __host__ __device__ __forceinline__ int64_t scale_offset(int64_t r, int64_t c, int64_t K) {

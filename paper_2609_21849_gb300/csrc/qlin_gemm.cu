@@ -141,6 +141,12 @@ struct KParams {
   int rq_v8;          // the re-quantized codes are 32-byte aligned: one 32-byte store per group
   unsigned* err;
   uint64_t timeout_ns;
+  // kEpi: act(products + bias) + residual
+  const uint16_t* bias;
+  const uint16_t* residual;
+  int64_t residual_stride;
+  int act;
+  int a_per_row;
 };
 
 // Coordinates of cluster tile ct, its M tile group and its N tile: M fastest
@@ -203,9 +209,61 @@ __device__ __forceinline__ void st_global_v4_hint(void* p, uint32_t a, uint32_t 
                : "memory");
 }
 
+// ------------------------------------------------- bias, activation, residual ---
+
+__device__ __forceinline__ void unpack16x2(uint32_t w, bool fp16, float& lo, float& hi) {
+  if (fp16) {
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
+    lo = f.x;
+    hi = f.y;
+  } else {
+    lo = bf16_lo(w);
+    hi = bf16_hi(w);
+  }
+}
+
+// v[i] += 32 16-bit values at p (16-byte aligned).
+template <bool kMaybeFp16>
+__device__ __forceinline__ void add32(float (&v)[32], const uint16_t* p, bool fp16) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const uint4 w = ld_global_v4(p + 8 * k);
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float lo, hi;
+      unpack16x2(u[i], kMaybeFp16 && fp16, lo, hi);
+      v[8 * k + 2 * i] = __fadd_rn(v[8 * k + 2 * i], lo);
+      v[8 * k + 2 * i + 1] = __fadd_rn(v[8 * k + 2 * i + 1], hi);
+    }
+  }
+}
+
+// FP8: v[i] *= S_A * S_W[n0 + i]
+__device__ __forceinline__ void scale_columns(float (&v)[32], const KParams& p, float s_a,
+                                              int64_t n0) {
+  const float one = p.w_per_channel ? 0.0f : __ldg(p.sdec_w);
+#pragma unroll
+  for (int i = 0; i < 32; ++i)
+    v[i] = __fmul_rn(v[i], __fmul_rn(s_a, p.w_per_channel ? __ldg(p.sdec_w + n0 + i) : one));
+}
+
+// act(v + bias) + residual of 32 columns of one row.
+template <bool kMaybeFp16>
+__device__ __forceinline__ void finish32(float (&v)[32], const KParams& p, int64_t row,
+                                         int64_t n0) {
+  const bool fp16 = p.fp16 != 0;
+  if (p.bias != nullptr) add32<kMaybeFp16>(v, p.bias + n0, fp16);
+  activate(v, p.act);
+  if (p.residual != nullptr && row < p.M)
+    add32<kMaybeFp16>(v, p.residual + row * p.residual_stride + n0, fp16);
+}
+
 // kBf16 (with !kFp4): bf16 operands on the FP8 skeleton (the same 128-byte
 // rows, 32 bytes of K per MMA), no scales.
-template <bool kFp4, int kBN, bool kPair, bool kRequant, bool kBf16 = false>
+// kEpi: the epilogue of qlin_linear_*: bias, activation and residual before the
+// 16-bit rounding, FP8 row scales of A.
+template <bool kFp4, int kBN, bool kPair, bool kRequant, bool kBf16 = false, bool kEpi = false>
 __global__ void __launch_bounds__(Cfg<kFp4, kBN, kPair>::kThreads, 1)
     gemm_kernel(const __grid_constant__ CUtensorMap tmap_a,
                 const __grid_constant__ CUtensorMap tmap_b,
@@ -739,7 +797,7 @@ __global__ void __launch_bounds__(Cfg<kFp4, kBN, kPair>::kThreads, 1)
     const int e = warp - C::kEpiWarp0;
     const int quarter = warp & 3;   // the TMEM lane quarter this warp may access
     const int half = e >> 2;
-    const float sdec_a = kBf16 ? 1.0f : *p.sdec_a;
+    const float sdec_a = kBf16 || (kEpi && p.a_per_row) ? 1.0f : *p.sdec_a;
     const float alpha = kFp4 ? __fmul_rn(sdec_a, *p.sdec_w) : kBf16 ? 1.0f : 0.0f;
     float s_enc_next = 0.0f;
     __shared__ float r_table[kFp4 && kRequant ? 256 : 1];
@@ -779,6 +837,10 @@ __global__ void __launch_bounds__(Cfg<kFp4, kBN, kPair>::kThreads, 1)
       // chunk c (32 columns) of this thread starts at column ccol(c)
       const int64_t col0 = (int64_t)nb * kBN + half * kCols;
       auto ccol = [&](int c) -> int64_t { return col0 + c * 32; };
+      const float row_scale = !kEpi || kFp4 || kBf16 ? 1.0f
+                              : !p.a_per_row         ? sdec_a
+                              : row < p.M            ? __ldg(p.sdec_a + row)
+                                                     : 0.0f;
       uint32_t packed[kCols / 2];
       const uint32_t taddr =
           tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(acc * kBN + half * kCols);
@@ -813,6 +875,26 @@ __global__ void __launch_bounds__(Cfg<kFp4, kBN, kPair>::kThreads, 1)
 #pragma unroll
         for (int b = 0; b < kBatch; ++b) {
           const int c = cb + b;
+          if constexpr (kEpi) {
+            float v[32];
+            const int64_t n0 = ccol(c);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[b][i]);
+            if (n0 < p.N) {
+              if (kFp4) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) v[i] = __fmul_rn(v[i], alpha);
+              } else if (!kBf16) {
+                scale_columns(v, p, row_scale, n0);
+              }
+              finish32<kBf16>(v, p, row, n0);
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              packed[c * 16 + i] = kBf16 && p.fp16 ? pack_f16x2(v[2 * i], v[2 * i + 1])
+                                                   : pack_bf16x2(v[2 * i], v[2 * i + 1]);
+            continue;
+          }
           float a[32];
           if (kFp4 || kBf16) {
 #pragma unroll
@@ -1115,7 +1197,7 @@ CUresult encode_scales(CUtensorMap* map, const void* base, uint64_t rows, uint64
                    CU_TENSOR_MAP_SWIZZLE_NONE);
 }
 
-template <bool kFp4, int kBN, bool kPair, bool kRequant, bool kBf16 = false>
+template <bool kFp4, int kBN, bool kPair, bool kRequant, bool kBf16 = false, bool kEpi = false>
 cudaError_t launch_cfg(const GemmArgs& a, cudaStream_t s, Device dev, unsigned* err,
                        uint64_t timeout_ns) {
   using C = Cfg<kFp4, kBN, kPair>;
@@ -1159,7 +1241,12 @@ cudaError_t launch_cfg(const GemmArgs& a, cudaStream_t s, Device dev, unsigned* 
   p.rq_v8 = (reinterpret_cast<uintptr_t>(a.rq_codes) & 31u) == 0 ? 1 : 0;
   p.err = err;
   p.timeout_ns = timeout_ns;
-  auto kern = gemm_kernel<kFp4, kBN, kPair, kRequant, kBf16>;
+  p.bias = static_cast<const uint16_t*>(a.bias);
+  p.residual = static_cast<const uint16_t*>(a.residual);
+  p.residual_stride = a.residual_stride;
+  p.act = a.act;
+  p.a_per_row = a.a_per_row ? 1 : 0;
+  auto kern = gemm_kernel<kFp4, kBN, kPair, kRequant, kBf16, kEpi>;
 
   cudaLaunchConfig_t cfg{};
   cudaLaunchAttribute attr[2];
@@ -1208,19 +1295,19 @@ Tile tile_of(const GemmArgs& a, int num_sms) {
                      a.M, a.N, a.K, num_sms);
 }
 
-template <bool kFp4>
+template <bool kFp4, bool kEpi>
 cudaError_t dispatch_bn(const GemmArgs& a, cudaStream_t s, Device dev, unsigned* err,
                         uint64_t timeout_ns) {
   const bool requant = a.next_scale != nullptr;
   switch (tile_of(a, dev.num_sms)) {
     case Tile::kPair:
-      return requant ? launch_cfg<kFp4, 256, true, true>(a, s, dev, err, timeout_ns)
-                     : launch_cfg<kFp4, 256, true, false>(a, s, dev, err, timeout_ns);
+      return requant ? launch_cfg<kFp4, 256, true, true, false, kEpi>(a, s, dev, err, timeout_ns)
+                     : launch_cfg<kFp4, 256, true, false, false, kEpi>(a, s, dev, err, timeout_ns);
     case Tile::kSingle:
-      return requant ? launch_cfg<kFp4, 128, false, true>(a, s, dev, err, timeout_ns)
-                     : launch_cfg<kFp4, 128, false, false>(a, s, dev, err, timeout_ns);
+      return requant ? launch_cfg<kFp4, 128, false, true, false, kEpi>(a, s, dev, err, timeout_ns)
+                     : launch_cfg<kFp4, 128, false, false, false, kEpi>(a, s, dev, err, timeout_ns);
     default:
-      return launch_cfg<kFp4, 64, false, false>(a, s, dev, err, timeout_ns);
+      return launch_cfg<kFp4, 64, false, false, false, kEpi>(a, s, dev, err, timeout_ns);
   }
 }
 
@@ -1245,12 +1332,18 @@ CUresult encode_tensor_map_out_bf16(CUtensorMap* map, void* base, uint64_t cols,
 cudaError_t launch_gemm(const GemmArgs& a, cudaStream_t s, Device dev, unsigned* err,
                         uint64_t timeout_ns) {
   if (a.bf16) {
-    return tile_of(a, dev.num_sms) == Tile::kPair
-               ? launch_cfg<false, 256, true, false, true>(a, s, dev, err, timeout_ns)
-               : launch_cfg<false, 128, false, false, true>(a, s, dev, err, timeout_ns);
+    const bool pair = tile_of(a, dev.num_sms) == Tile::kPair;
+    if (a.epilogue)
+      return pair ? launch_cfg<false, 256, true, false, true, true>(a, s, dev, err, timeout_ns)
+                  : launch_cfg<false, 128, false, false, true, true>(a, s, dev, err, timeout_ns);
+    return pair ? launch_cfg<false, 256, true, false, true>(a, s, dev, err, timeout_ns)
+                : launch_cfg<false, 128, false, false, true>(a, s, dev, err, timeout_ns);
   }
-  return a.fp4 ? dispatch_bn<true>(a, s, dev, err, timeout_ns)
-               : dispatch_bn<false>(a, s, dev, err, timeout_ns);
+  if (a.epilogue)
+    return a.fp4 ? dispatch_bn<true, true>(a, s, dev, err, timeout_ns)
+                 : dispatch_bn<false, true>(a, s, dev, err, timeout_ns);
+  return a.fp4 ? dispatch_bn<true, false>(a, s, dev, err, timeout_ns)
+               : dispatch_bn<false, false>(a, s, dev, err, timeout_ns);
 }
 
 cudaError_t launch_wait_selftest(uint64_t timeout_ns, cudaStream_t s, unsigned* err) {

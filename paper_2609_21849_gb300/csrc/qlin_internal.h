@@ -19,6 +19,23 @@ struct Device {
   int num_sms;
 };
 
+// Launch with programmatic stream serialization (see grid_dep_wait).
+template <typename... Params, typename... Args>
+cudaError_t launch_pdl(void (*kern)(Params...), unsigned grid, int block, int smem, cudaStream_t s,
+                       Args... args) {
+  cudaLaunchConfig_t cfg{};
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.gridDim = dim3(grid, 1, 1);
+  cfg.blockDim = dim3((unsigned)block, 1, 1);
+  cfg.dynamicSmemBytes = (size_t)smem;
+  cfg.stream = s;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kern, args...);
+}
+
 // ---- quantizers (qlin_quant.cu) ----
 // err / timeout_ns: device status word and limit of the bounded waits.
 cudaError_t launch_quant_nvfp4(const void* x, int64_t M, int64_t K, const float* scale_src,
@@ -54,6 +71,13 @@ cudaError_t take_grid_counts(unsigned (&counts)[3]);
 cudaError_t launch_quant_fp8_rows(const void* w, int64_t N, int64_t K, const qlin_fp8_t& out,
                                   cudaStream_t s, Device dev);
 
+// ---- norm (qlin_norm.cu): one of y16, fp8 and nvfp4 is the output ----
+cudaError_t launch_rmsnorm(const qlin_rmsnorm_t& a, void* y16, const float* static_scale,
+                           const qlin_fp8_t* fp8, const qlin_nvfp4_t* nvfp4, cudaStream_t s);
+
+// ---- rotary positions (qlin_rope.cu) ----
+cudaError_t launch_rope(const qlin_rope_t& a, cudaStream_t s);
+
 // ---- GEMMs (qlin_gemm.cu) ----
 struct GemmArgs {
   bool fp4;                 // NVFP4 (true) or FP8
@@ -81,6 +105,13 @@ struct GemmArgs {
   unsigned* y_amax;
   unsigned* y_departures;
   float* y_sdec;
+  // optional epilogue of a linear: act(products + bias) + residual
+  bool epilogue;            // any of these, or a_per_row
+  const void* bias;         // 16-bit [N] or null
+  const void* residual;     // 16-bit [M, N] or null, rows residual_stride elements apart
+  int64_t residual_stride;
+  int act;                  // qlin_activation
+  bool a_per_row;           // FP8: sdec_a has M entries
 };
 cudaError_t launch_gemm(const GemmArgs& a, cudaStream_t s, Device dev, unsigned* err,
                         uint64_t timeout_ns);

@@ -1141,23 +1141,6 @@ const Setup& setup(Device dev, int threads, int smem) {
   });
 }
 
-// Launch with programmatic stream serialization (see grid_dep_wait).
-template <typename... Params, typename... Args>
-cudaError_t launch_pdl(void (*kern)(Params...), int grid, int block, int smem, cudaStream_t s,
-                       Args... args) {
-  cudaLaunchConfig_t cfg{};
-  cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.gridDim = dim3((unsigned)grid, 1, 1);
-  cfg.blockDim = dim3((unsigned)block, 1, 1);
-  cfg.dynamicSmemBytes = (size_t)smem;
-  cfg.stream = s;
-  cfg.attrs = at;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kern, args...);
-}
-
 int stream_grid(uint64_t n_chunks, int num_sms) {
   const uint64_t tiles = (n_chunks + kTileChunks - 1) / kTileChunks;
   return (int)std::max<uint64_t>(1, std::min<uint64_t>(tiles, (uint64_t)num_sms * kBlocksPerSm));

@@ -19,6 +19,10 @@ LIB_PATH = os.path.join(_HERE, "_lib", "libqlin.so")
 
 QLIN_FMT_NVFP4 = 1
 QLIN_FMT_FP8 = 2
+QLIN_BF16, QLIN_FP16 = 1, 2
+QLIN_ACT_NONE, QLIN_ACT_RELU, QLIN_ACT_SILU, QLIN_ACT_GELU_TANH, QLIN_ACT_GELU = range(5)
+QLIN_ROPE_INTERLEAVED, QLIN_ROPE_HALF = 0, 1
+QLIN_ROPE_NONE, QLIN_ROPE_LINEAR, QLIN_ROPE_NTK, QLIN_ROPE_YARN = range(4)
 STATUS = {0: "QLIN_OK", 1: "QLIN_ERR_INVALID_ARG", 2: "QLIN_ERR_UNSUPPORTED",
           3: "QLIN_ERR_MISALIGNED", 4: "QLIN_ERR_CUDA", 5: "QLIN_ERR_TIMEOUT",
           6: "QLIN_ERR_WORKSPACE"}
@@ -28,6 +32,9 @@ EXPORTS = ("qlin_nvfp4_scale_bytes", "qlin_workspace_size", "qlin_quantize_act_n
            "qlin_quantize_act_fp8", "qlin_quantize_weight", "qlin_gemm_nvfp4", "qlin_gemm_fp8",
            "qlin_linear_fused", "qlin_linear_fused_fp8", "qlin_linear_dynamic", "qlin_gemm_bf16",
            "qlin_gemm_fp16", "qlin_quantize_act_nvfp4_noalloc",
+           "qlin_rmsnorm", "qlin_rmsnorm_fp8", "qlin_rmsnorm_nvfp4",
+           "qlin_linear_nvfp4", "qlin_linear_fp8", "qlin_linear_bf16", "qlin_linear_fp16",
+           "qlin_rope", "qlin_rope_turns",
            "qlin_sync_status", "qlin_selftest_bounded_wait",
            "qlin_set_wait_timeout_ns", "qlin_status_str", "qlin_last_error")
 
@@ -50,6 +57,29 @@ class FP8Desc(ctypes.Structure):
                 ("per_channel", ctypes.c_int32)]
 
 
+class RMSNormDesc(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("x", "residual", "sum", "weight")]
+                + [(n, ctypes.c_int64) for n in ("x_stride", "residual_stride", "sum_stride", "M", "K")]
+                + [("eps", ctypes.c_float), ("dtype", ctypes.c_int32)])
+
+
+class EpilogueDesc(ctypes.Structure):
+    _fields_ = [("bias", ctypes.c_void_p), ("residual", ctypes.c_void_p),
+                ("residual_stride", ctypes.c_int64), ("act", ctypes.c_int32)]
+
+
+class RopeDesc(ctypes.Structure):
+    _fields_ = ([("x", ctypes.c_void_p), ("y", ctypes.c_void_p)]
+                + [(n, ctypes.c_int64) for n in ("x_token_stride", "x_head_stride", "y_token_stride",
+                                                 "y_head_stride", "tokens", "heads")]
+                + [("positions", ctypes.c_void_p), ("position_token_stride", ctypes.c_int64),
+                   ("position_axis_stride", ctypes.c_int64), ("turns", ctypes.c_void_p),
+                   ("magnitude", ctypes.c_float)]
+                + [(n, ctypes.c_int32) for n in ("head_dim", "rot_dim", "position_bits", "axes")]
+                + [("axis_pairs", ctypes.c_int32 * 4)]
+                + [(n, ctypes.c_int32) for n in ("layout", "inverse", "dtype")])
+
+
 # The descriptors as packed bytes, the form the calls below hand over: the
 # struct's layout, built in a third of the time of a ctypes Structure and its
 # reference (0.2 against 0.6 us; a call's host time is a few microseconds).
@@ -57,6 +87,12 @@ _pack_nvfp4 = struct.Struct("=QQQqq").pack
 _pack_fp8 = struct.Struct("=QQqqi4x").pack
 assert struct.calcsize("=QQQqq") == ctypes.sizeof(NVFP4Desc)
 assert struct.calcsize("=QQqqi4x") == ctypes.sizeof(FP8Desc)
+_pack_rmsnorm = struct.Struct("=QQQQqqqqqfi").pack
+_pack_epilogue = struct.Struct("=QQqi4x").pack
+_pack_rope = struct.Struct("=QQqqqqqqQqqQf11i").pack
+assert struct.calcsize("=QQQQqqqqqfi") == ctypes.sizeof(RMSNormDesc)
+assert struct.calcsize("=QQqi4x") == ctypes.sizeof(EpilogueDesc)
+assert struct.calcsize("=QQqqqqqqQqqQf11i") == ctypes.sizeof(RopeDesc)
 
 _lock = threading.Lock()
 _lib = None
@@ -95,6 +131,20 @@ def load_library(path: str = LIB_PATH):
             "qlin_linear_dynamic": (ctypes.c_int, [ctypes.POINTER(NVFP4Desc), ctypes.POINTER(NVFP4Desc), p,
                                                    ctypes.POINTER(NVFP4Desc), p, sz, p]),
             "qlin_quantize_act_nvfp4_noalloc": (ctypes.c_int, [p, i64, i64, ctypes.POINTER(NVFP4Desc), p]),
+            "qlin_rmsnorm": (ctypes.c_int, [ctypes.POINTER(RMSNormDesc), p, p]),
+            "qlin_rmsnorm_fp8": (ctypes.c_int, [ctypes.POINTER(RMSNormDesc), p, ctypes.POINTER(FP8Desc), p]),
+            "qlin_rmsnorm_nvfp4": (ctypes.c_int, [ctypes.POINTER(RMSNormDesc), p, ctypes.POINTER(NVFP4Desc), p]),
+            "qlin_linear_nvfp4": (ctypes.c_int, [ctypes.POINTER(NVFP4Desc), ctypes.POINTER(NVFP4Desc),
+                                                 ctypes.POINTER(EpilogueDesc), p, p,
+                                                 ctypes.POINTER(NVFP4Desc), i64, p]),
+            "qlin_linear_fp8": (ctypes.c_int, [ctypes.POINTER(FP8Desc), ctypes.POINTER(FP8Desc),
+                                               ctypes.POINTER(EpilogueDesc), p, p,
+                                               ctypes.POINTER(FP8Desc), i64, p]),
+            "qlin_linear_bf16": (ctypes.c_int, [p, i64, p, i64, i64, i64, ctypes.POINTER(EpilogueDesc), p, p]),
+            "qlin_linear_fp16": (ctypes.c_int, [p, i64, p, i64, i64, i64, ctypes.POINTER(EpilogueDesc), p, p]),
+            "qlin_rope": (ctypes.c_int, [ctypes.POINTER(RopeDesc), p]),
+            "qlin_rope_turns": (ctypes.c_int, [ctypes.c_int32, ctypes.c_double, ctypes.c_int32]
+                                + [ctypes.c_double] * 4 + [p, ctypes.POINTER(ctypes.c_float)]),
             "qlin_sync_status": (ctypes.c_int, [p]),
             "qlin_selftest_bounded_wait": (ctypes.c_int, [ctypes.c_uint64, p]),
             "qlin_set_wait_timeout_ns": (None, [ctypes.c_uint64]),
@@ -117,6 +167,14 @@ def load_library(path: str = LIB_PATH):
             "qlin_linear_fused_fp8": [d, d, p, p, d, i64, p],
             "qlin_linear_dynamic": [d, d, p, d, p, sz, p],
             "qlin_quantize_act_nvfp4_noalloc": [p, i64, i64, d, p],
+            "qlin_rmsnorm": [d, p, p],
+            "qlin_rmsnorm_fp8": [d, p, d, p],
+            "qlin_rmsnorm_nvfp4": [d, p, d, p],
+            "qlin_linear_nvfp4": [d, d, d, p, p, d, i64, p],
+            "qlin_linear_fp8": [d, d, d, p, p, d, i64, p],
+            "qlin_linear_bf16": [p, i64, p, i64, i64, i64, d, p, p],
+            "qlin_linear_fp16": [p, i64, p, i64, i64, i64, d, p, p],
+            "qlin_rope": [d, p],
         }
         lib.packed = types.SimpleNamespace()
         for name, args in packed.items():
@@ -394,6 +452,261 @@ def qlin_linear_dynamic(A: NVFP4Tensor, W: NVFP4Tensor, y: torch.Tensor | None =
         _nvfp4(A), _nvfp4(W), _ptr(y), _nvfp4(y_q), _ptr(workspace),
         workspace.numel(), _stream(stream)), "qlin_linear_dynamic")
     return y, y_q
+
+
+# ------------------------------------- around the linears of a block ---
+
+_FLOAT16 = {torch.bfloat16: QLIN_BF16, torch.float16: QLIN_FP16}
+
+
+def _empty(shape, dtype, device, stream):
+    """An output of a call on `stream`: allocated in that stream's order, so that
+    memory that the current stream still uses is not handed out for it."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _rows16(t, name, dtype, M, K, device):
+    """The row stride of a 16-bit [M, K] matrix whose columns are adjacent."""
+    if (t.dtype != dtype or t.dim() != 2 or t.shape[0] != M or t.shape[1] != K or t.device != device
+            or (t.stride(1) != 1 and K > 1)):
+        raise ValueError(f"{name}: expected a {dtype} [{M}, {K}] tensor on {device} with unit column stride")
+    return t.stride(0) if M > 1 else K
+
+
+def _vector16(t, name, dtype, n, device):
+    if t.dtype != dtype or t.dim() != 1 or t.shape[0] != n or t.device != device or (t.stride(0) != 1 and n > 1):
+        raise ValueError(f"{name}: expected a contiguous {dtype} [{n}] tensor on {device}")
+    return t.data_ptr()
+
+
+def _rmsnorm_args(x, weight, residual, eps, sum_out, stream):
+    """(packed arguments, M, K, sum) of a norm call; sum is allocated where a
+    residual comes without one."""
+    dt = _FLOAT16.get(x.dtype)
+    if dt is None or x.dim() != 2 or not x.is_cuda:
+        raise ValueError("x: expected a 2-D bf16 or fp16 CUDA tensor")
+    M, K = x.shape
+    dtype, dev = x.dtype, x.device
+    xs, rs, ss, rp, sp = _rows16(x, "x", dtype, M, K, dev), 0, 0, 0, 0
+    if residual is not None:
+        rs, rp = _rows16(residual, "residual", dtype, M, K, dev), residual.data_ptr()
+        if sum_out is None:
+            sum_out = _empty((M, K), dtype, dev, stream)
+        ss, sp = _rows16(sum_out, "sum_out", dtype, M, K, dev), sum_out.data_ptr()
+    elif sum_out is not None:
+        raise ValueError("sum_out without a residual")
+    wp = 0 if weight is None else _vector16(weight, "weight", dtype, K, dev)
+    return _pack_rmsnorm(x.data_ptr(), rp, sp, wp, xs, rs, ss, M, K, eps, dt), M, K, sum_out
+
+
+def qlin_rmsnorm(x: torch.Tensor, weight: torch.Tensor | None = None,
+                 residual: torch.Tensor | None = None, eps: float = 1e-6,
+                 sum_out: torch.Tensor | None = None, y: torch.Tensor | None = None, stream=None):
+    """(norm of x + residual in x's type, x + residual).  x, residual and sum_out are
+    [M, K] with any row stride that is a multiple of 8; sum_out may be x or residual.
+    Without a residual the second is None."""
+    args, M, K, sum_out = _rmsnorm_args(x, weight, residual, eps, sum_out, stream)
+    if y is None:
+        y = _empty((M, K), x.dtype, x.device, stream)
+    elif y.dtype != x.dtype or y.shape != x.shape or not y.is_contiguous() or y.device != x.device:
+        raise ValueError(f"y: expected a contiguous {x.dtype} [{M}, {K}] tensor on {x.device}")
+    _check(_library().packed.qlin_rmsnorm(args, y.data_ptr(), _stream(stream)), "qlin_rmsnorm")
+    return y, sum_out
+
+
+def qlin_rmsnorm_fp8(x: torch.Tensor, weight: torch.Tensor | None = None,
+                     residual: torch.Tensor | None = None, eps: float = 1e-6,
+                     sum_out: torch.Tensor | None = None, static_scale: torch.Tensor | None = None,
+                     out: FP8Tensor | None = None, stream=None):
+    """The norm as an FP8 operand: one scale per row, found here, or the static
+    tensor scale.  Returns (operand, x + residual) as qlin_rmsnorm does."""
+    args, M, K, sum_out = _rmsnorm_args(x, weight, residual, eps, sum_out, stream)
+    if out is None:
+        rows = static_scale is None
+        out = FP8Tensor(_empty((M, K), torch.uint8, x.device, stream),
+                        _empty(M if rows else 1, torch.float32, x.device, stream), M, K, 1 if rows else 0)
+    _check(_library().packed.qlin_rmsnorm_fp8(args, _ptr(static_scale), _fp8(out), _stream(stream)),
+           "qlin_rmsnorm_fp8")
+    return out, sum_out
+
+
+def qlin_rmsnorm_nvfp4(x: torch.Tensor, static_scale: torch.Tensor, weight: torch.Tensor | None = None,
+                       residual: torch.Tensor | None = None, eps: float = 1e-6,
+                       sum_out: torch.Tensor | None = None, out: NVFP4Tensor | None = None, stream=None):
+    """The norm as an NVFP4 operand with the static tensor scale.  Returns
+    (operand, x + residual) as qlin_rmsnorm does."""
+    args, M, K, sum_out = _rmsnorm_args(x, weight, residual, eps, sum_out, stream)
+    if out is None:
+        nb = qlin_nvfp4_scale_bytes(M, K)
+        if nb == 0:
+            raise ValueError(f"invalid NVFP4 shape [{M}, {K}]")
+        out = NVFP4Tensor(_empty((M, K // 2), torch.uint8, x.device, stream),
+                          _empty(nb, torch.uint8, x.device, stream),
+                          _empty(1, torch.float32, x.device, stream), M, K)
+    _check(_library().packed.qlin_rmsnorm_nvfp4(args, _ptr(static_scale), _nvfp4(out), _stream(stream)),
+           "qlin_rmsnorm_nvfp4")
+    return out, sum_out
+
+
+def _epilogue(bias, act, residual, dtype, M, N, device):
+    """The packed epilogue of a linear with an [M, N] output."""
+    bp = 0 if bias is None else _vector16(bias, "bias", dtype, N, device)
+    if residual is None:
+        return _pack_epilogue(bp, 0, 0, act)
+    return _pack_epilogue(bp, residual.data_ptr(), _rows16(residual, "residual", dtype, M, N, device), act)
+
+
+def _linear_quantized(name, pack, A, W, bias, act, residual, y, next_scale, y_q, rq_col0, device, stream):
+    M, N = A.rows, W.rows
+    if (y_q is None) != (next_scale is None):
+        raise ValueError("next_scale and y_q come together")
+    if y is None:
+        if y_q is None:
+            y = _empty((M, N), torch.bfloat16, device, stream)
+    elif y.dtype != torch.bfloat16 or y.shape != (M, N) or not y.is_contiguous() or y.device != device:
+        raise ValueError(f"y: expected a contiguous bf16 [{M}, {N}] tensor on {device}")
+    ep = _epilogue(bias, act, residual, torch.bfloat16, M, N, device)
+    _check(getattr(_library().packed, name)(
+        pack(A), pack(W), ep, _ptr(y), _ptr(next_scale), None if y_q is None else pack(y_q), rq_col0,
+        _stream(stream)), name)
+    return y, y_q
+
+
+def qlin_linear_nvfp4(A: NVFP4Tensor, W: NVFP4Tensor, bias: torch.Tensor | None = None,
+                      act: int = QLIN_ACT_NONE, residual: torch.Tensor | None = None,
+                      y: torch.Tensor | None = None, next_scale: torch.Tensor | None = None,
+                      y_q: NVFP4Tensor | None = None, rq_col0: int = 0, stream=None):
+    """y = act(A W^T + bias) + residual (bf16, one rounding) and, with next_scale and
+    y_q, the next layer's NVFP4 input from columns [rq_col0, rq_col0 + y_q.K) of y.
+    Returns (y, y_q); y None is allocated, or not written where y_q is given.
+    residual may be y."""
+    return _linear_quantized("qlin_linear_nvfp4", _nvfp4, A, W, bias, act, residual, y, next_scale, y_q,
+                             rq_col0, A.codes.device, stream)
+
+
+def qlin_linear_fp8(A: FP8Tensor, W: FP8Tensor, bias: torch.Tensor | None = None,
+                    act: int = QLIN_ACT_NONE, residual: torch.Tensor | None = None,
+                    y: torch.Tensor | None = None, next_scale: torch.Tensor | None = None,
+                    y_q: FP8Tensor | None = None, rq_col0: int = 0, stream=None):
+    """As qlin_linear_nvfp4 with FP8 operands; A has one scale or one per row."""
+    return _linear_quantized("qlin_linear_fp8", _fp8, A, W, bias, act, residual, y, next_scale, y_q,
+                             rq_col0, A.codes.device, stream)
+
+
+def _linear16(name, dtype, a, w, bias, act, residual, y, stream):
+    if a.dtype != dtype or a.dim() != 2 or not a.is_cuda:
+        raise ValueError(f"a: expected a 2-D {dtype} CUDA tensor")
+    if w.dtype != dtype or w.dim() != 2 or w.shape[1] != a.shape[1] or not w.is_contiguous() or w.device != a.device:
+        raise ValueError(f"w: expected a contiguous {dtype} [N, {a.shape[1]}] tensor on {a.device}")
+    (M, K), N, dev = a.shape, w.shape[0], a.device
+    lda = _rows16(a, "a", dtype, M, K, dev)
+    if y is None:
+        y = _empty((M, N), dtype, dev, stream)
+    elif y.dtype != dtype or y.shape != (M, N) or not y.is_contiguous() or y.device != dev:
+        raise ValueError(f"y: expected a contiguous {dtype} [{M}, {N}] tensor on {dev}")
+    ep = _epilogue(bias, act, residual, dtype, M, N, dev)
+    _check(getattr(_library().packed, name)(a.data_ptr(), lda, w.data_ptr(), M, N, K, ep, y.data_ptr(),
+                                            _stream(stream)), name)
+    return y
+
+
+def qlin_linear_bf16(a: torch.Tensor, w: torch.Tensor, bias: torch.Tensor | None = None,
+                     act: int = QLIN_ACT_NONE, residual: torch.Tensor | None = None,
+                     y: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """y = act(a w^T + bias) + residual for bf16 a [M, K] (rows may be strided) and
+    w [N, K], one rounding to bf16.  residual may be y."""
+    return _linear16("qlin_linear_bf16", torch.bfloat16, a, w, bias, act, residual, y, stream)
+
+
+def qlin_linear_fp16(a: torch.Tensor, w: torch.Tensor, bias: torch.Tensor | None = None,
+                     act: int = QLIN_ACT_NONE, residual: torch.Tensor | None = None,
+                     y: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """As qlin_linear_bf16 in fp16."""
+    return _linear16("qlin_linear_fp16", torch.float16, a, w, bias, act, residual, y, stream)
+
+
+_LAYOUTS = {"interleaved": QLIN_ROPE_INTERLEAVED, "half": QLIN_ROPE_HALF}
+_SCALINGS = {"none": QLIN_ROPE_NONE, "linear": QLIN_ROPE_LINEAR, "ntk": QLIN_ROPE_NTK, "yarn": QLIN_ROPE_YARN}
+
+
+@dataclass
+class RopePlan:
+    """What the rotation needs beside positions: each pair's turns per position in
+    units of 2^-64 turn, the layout ("interleaved" or "half"), the magnitude, and how
+    many pairs follow each position axis."""
+    turns: torch.Tensor          # int64 (the bits of uint64) [rot_dim / 2]
+    layout: str
+    magnitude: float
+    axis_pairs: tuple
+
+    @property
+    def rot_dim(self) -> int:
+        return 2 * self.turns.numel()
+
+
+def qlin_rope_turns(rot_dim: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0,
+                    trained_length: float = 4096.0, beta_fast: float = 32.0, beta_slow: float = 1.0):
+    """(turns as a host int64 tensor with uint64's bits, magnitude) of one axis."""
+    if scaling not in _SCALINGS:
+        raise ValueError(f"scaling: one of {sorted(_SCALINGS)}")
+    turns = torch.empty(max(rot_dim // 2, 0), dtype=torch.int64)
+    mag = ctypes.c_float()
+    _check(_library().qlin_rope_turns(rot_dim, base, _SCALINGS[scaling], factor, trained_length, beta_fast,
+                                      beta_slow, turns.data_ptr(), ctypes.byref(mag)), "qlin_rope_turns")
+    return turns, mag.value
+
+
+def rope_plan(rot_dims, base: float = 10000.0, layout: str = "half", scaling: str = "none",
+              factor: float = 1.0, trained_length: float = 4096.0, beta_fast: float = 32.0,
+              beta_slow: float = 1.0, device="cuda") -> RopePlan:
+    """A plan for heads whose first sum(rot_dims) elements turn; rot_dims is the
+    rotated width, or one width per position axis (each with its own frequencies)."""
+    if layout not in _LAYOUTS:
+        raise ValueError(f"layout: one of {sorted(_LAYOUTS)}")
+    dims = (rot_dims,) if isinstance(rot_dims, int) else tuple(rot_dims)
+    if not 1 <= len(dims) <= 4:
+        raise ValueError("one to four position axes")
+    parts = [qlin_rope_turns(d, base, scaling, factor, trained_length, beta_fast, beta_slow) for d in dims]
+    return RopePlan(torch.cat([t for t, _ in parts]).to(device), layout, parts[0][1],
+                    tuple(d // 2 for d in dims))
+
+
+def qlin_rope(x: torch.Tensor, positions: torch.Tensor, plan: RopePlan, out: torch.Tensor | None = None,
+              inverse: bool = False, stream=None) -> torch.Tensor:
+    """x [tokens, heads, head_dim] (any strides of tokens and heads, e.g. the q and k
+    columns of a QKV output) with its rotary positions applied, or taken back
+    (inverse: also the gradient).  positions: int32 or int64 [tokens], or [tokens,
+    axes] for a plan of several axes.  out may be x."""
+    dt = _FLOAT16.get(x.dtype)
+    if dt is None or x.dim() != 3 or not x.is_cuda or (x.stride(2) != 1 and x.shape[2] > 1):
+        raise ValueError("x: expected a bf16 or fp16 [tokens, heads, head_dim] CUDA tensor with contiguous heads")
+    T, H, D = x.shape
+    axes = len(plan.axis_pairs)
+    if (positions.dtype not in (torch.int32, torch.int64) or positions.device != x.device
+            or positions.shape != ((T, axes) if positions.dim() == 2 else (T,))
+            or (positions.dim() == 1 and axes != 1)):
+        raise ValueError(f"positions: expected int32 or int64 [{T}, {axes}] on {x.device}")
+    turns = plan.turns
+    if turns.dtype != torch.int64 or turns.dim() != 1 or not turns.is_contiguous() or turns.device != x.device:
+        raise ValueError(f"plan.turns: expected a contiguous int64 vector on {x.device}")
+    if not 1 <= axes <= 4 or plan.layout not in _LAYOUTS:
+        raise ValueError("plan: one to four axes, layout 'interleaved' or 'half'")
+    if out is None:
+        out = _empty((T, H, D), x.dtype, x.device, stream)
+    elif out.dtype != x.dtype or out.shape != x.shape or out.device != x.device or (out.stride(2) != 1 and D > 1):
+        raise ValueError(f"out: expected a {x.dtype} {list(x.shape)} tensor on {x.device} with contiguous heads")
+    pairs = plan.axis_pairs + (0,) * (4 - axes)
+    _check(_library().packed.qlin_rope(_pack_rope(
+        x.data_ptr(), out.data_ptr(), x.stride(0), x.stride(1), out.stride(0), out.stride(1), T, H,
+        positions.data_ptr(), positions.stride(0), positions.stride(1) if positions.dim() == 2 else 0,
+        turns.data_ptr(), plan.magnitude, D, 2 * turns.numel(), 64 if positions.dtype == torch.int64 else 32,
+        axes, *pairs, _LAYOUTS[plan.layout], 1 if inverse else 0, dt), _stream(stream)), "qlin_rope")
+    return out
 
 
 def qlin_sync_status(stream=None) -> int:
