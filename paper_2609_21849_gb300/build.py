@@ -15,7 +15,8 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB_DIR = os.path.join(HERE, "_lib")
 LIB = os.path.join(LIB_DIR, "libqlin.so")
-SOURCES = ["qlin_api.cu", "qlin_quant.cu", "qlin_gemm.cu", "qlin_norm.cu", "qlin_rope.cu"]
+SOURCES = ["qlin_api.cu", "qlin_quant.cu", "qlin_gemm.cu", "qlin_few.cu", "qlin_norm.cu",
+           "qlin_rope.cu"]
 # the rate probes of the measurement harness and the probes of the quantizers'
 # grid-wide wait: a library of its own
 PROBE_LIB = os.path.join(LIB_DIR, "libqlin_probe.so")

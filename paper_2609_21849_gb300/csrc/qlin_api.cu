@@ -248,11 +248,18 @@ static qlin_status set_epilogue(GemmArgs& a, const qlin_epilogue_t* ep) {
   return QLIN_OK;
 }
 
+// The plain GEMMs always take the tensor-core tiles, so that their sums keep their
+// order; the linears take the few-token kernel where it applies.
+static cudaError_t launch_linear(const GemmArgs& a, cudaStream_t s, Device dev, unsigned* status) {
+  if (a.few_ok && a.M <= kFewTokens) return launch_few(a, s);
+  return launch_gemm(a, s, dev, status, timeout());
+}
+
 static qlin_status gemm_common(bool fp4, const void* Aany, const void* Wany, void* y,
                                const float* next_scale, qlin_nvfp4_t* y_q, int64_t rq_col0,
                                void* stream, unsigned* y_amax = nullptr,
                                qlin_fp8_t* y_q8 = nullptr, float* y_sdec = nullptr,
-                               const qlin_epilogue_t* ep = nullptr, bool rows_ok = false) {
+                               const qlin_epilogue_t* ep = nullptr, bool linear = false) {
   GemmArgs a{};
   a.y_amax = y_amax;
   a.y_departures = y_amax != nullptr ? y_amax + 1 : nullptr;
@@ -279,7 +286,7 @@ static qlin_status gemm_common(bool fp4, const void* Aany, const void* Wany, voi
     if (A == nullptr || W == nullptr) return QLIN_ERR_INVALID_ARG;
     QLIN_TRY(check_fp8(A, A->rows, A->K));
     QLIN_TRY(check_fp8(W, W->rows, A->K));
-    if (A->per_channel && !rows_ok) return QLIN_ERR_INVALID_ARG;
+    if (A->per_channel && !linear) return QLIN_ERR_INVALID_ARG;
     a.a_per_row = A->per_channel != 0;
     a.epilogue = a.a_per_row;
     a.a_codes = A->codes;
@@ -296,6 +303,7 @@ static qlin_status gemm_common(bool fp4, const void* Aany, const void* Wany, voi
   if (y != nullptr && !aligned(y, 16)) return QLIN_ERR_MISALIGNED;
   a.y = y;
   QLIN_TRY(set_epilogue(a, ep));
+  a.few_ok = linear;
   if (next_scale != nullptr) {
     // the re-quantized operand: NVFP4 after an NVFP4 GEMM, FP8 after an FP8 one
     const int64_t rq_cols = fp4 ? (y_q ? y_q->K : 0) : (y_q8 ? y_q8->K : 0);
@@ -324,8 +332,7 @@ static qlin_status gemm_common(bool fp4, const void* Aany, const void* Wany, voi
   unsigned* status;
   Device dev;
   QLIN_TRY(device_state(&status, &dev));
-  cudaError_t e = launch_gemm(a, static_cast<cudaStream_t>(stream), dev, status,
-                              g_timeout_ns.load(std::memory_order_relaxed));
+  cudaError_t e = launch_linear(a, static_cast<cudaStream_t>(stream), dev, status);
   if (e != cudaSuccess) return cuda_fail(e);
   return QLIN_OK;
 }
@@ -350,7 +357,7 @@ qlin_status qlin_linear_fused(const qlin_nvfp4_t* A, const qlin_nvfp4_t* W, void
 // The unquantized 16-bit linear (bf16 or fp16 operands and output).
 static qlin_status gemm16(const void* a16, int64_t lda, const void* w16, int64_t M, int64_t N,
                           int64_t K, void* y16, void* stream, bool fp16,
-                          const qlin_epilogue_t* ep = nullptr) {
+                          const qlin_epilogue_t* ep = nullptr, bool linear = false) {
   if (a16 == nullptr || w16 == nullptr || y16 == nullptr) return QLIN_ERR_INVALID_ARG;
   if (M < 1 || K < 64 || K % 64 != 0 || N < 64 || N % 64 != 0 || lda < K)
     return QLIN_ERR_INVALID_ARG;
@@ -368,10 +375,11 @@ static qlin_status gemm16(const void* a16, int64_t lda, const void* w16, int64_t
   a.N = N;
   a.K = K;
   QLIN_TRY(set_epilogue(a, ep));
+  a.few_ok = linear;
   unsigned* status;
   Device dev;
   QLIN_TRY(device_state(&status, &dev));
-  cudaError_t e = launch_gemm(a, static_cast<cudaStream_t>(stream), dev, status, timeout());
+  cudaError_t e = launch_linear(a, static_cast<cudaStream_t>(stream), dev, status);
   if (e != cudaSuccess) return cuda_fail(e);
   return QLIN_OK;
 }
@@ -420,7 +428,7 @@ qlin_status qlin_linear_nvfp4(const qlin_nvfp4_t* A, const qlin_nvfp4_t* W,
                               const float* next_scale, qlin_nvfp4_t* y_q, int64_t rq_col0,
                               void* stream) {
   return gemm_common(true, A, W, y_bf16, next_scale, y_q, rq_col0, stream, nullptr, nullptr,
-                     nullptr, epilogue);
+                     nullptr, epilogue, true);
 }
 
 qlin_status qlin_linear_fp8(const qlin_fp8_t* A, const qlin_fp8_t* W,
@@ -434,13 +442,13 @@ qlin_status qlin_linear_fp8(const qlin_fp8_t* A, const qlin_fp8_t* W,
 qlin_status qlin_linear_bf16(const void* a_bf16, int64_t lda, const void* w_bf16, int64_t M,
                              int64_t N, int64_t K, const qlin_epilogue_t* epilogue,
                              void* y_bf16, void* stream) {
-  return gemm16(a_bf16, lda, w_bf16, M, N, K, y_bf16, stream, false, epilogue);
+  return gemm16(a_bf16, lda, w_bf16, M, N, K, y_bf16, stream, false, epilogue, true);
 }
 
 qlin_status qlin_linear_fp16(const void* a_fp16, int64_t lda, const void* w_fp16, int64_t M,
                              int64_t N, int64_t K, const qlin_epilogue_t* epilogue,
                              void* y_fp16, void* stream) {
-  return gemm16(a_fp16, lda, w_fp16, M, N, K, y_fp16, stream, true, epilogue);
+  return gemm16(a_fp16, lda, w_fp16, M, N, K, y_fp16, stream, true, epilogue, true);
 }
 
 static qlin_status check_rmsnorm(const qlin_rmsnorm_t* a) {

@@ -112,9 +112,13 @@ struct GemmArgs {
   int64_t residual_stride;
   int act;                  // qlin_activation
   bool a_per_row;           // FP8: sdec_a has M entries
+  bool few_ok;              // a call that may take the few-token kernel
 };
 cudaError_t launch_gemm(const GemmArgs& a, cudaStream_t s, Device dev, unsigned* err,
                         uint64_t timeout_ns);
+// The same for at most kFewTokens rows of A (qlin_few.cu; no output amax).
+constexpr int kFewTokens = 16;
+cudaError_t launch_few(const GemmArgs& a, cudaStream_t s);
 cudaError_t launch_wait_selftest(uint64_t timeout_ns, cudaStream_t s, unsigned* err);
 
 // Resolves cuTensorMapEncodeTiled through the runtime (no libcuda link).
