@@ -473,7 +473,7 @@ static qlin_status rmsnorm(const qlin_rmsnorm_t* args, void* y16, const float* s
   unsigned* status;
   Device dev;
   QLIN_TRY(device_state(&status, &dev));
-  QLIN_CUDA(launch_rmsnorm(*args, y16, static_scale, fp8, nvfp4, static_cast<cudaStream_t>(stream)));
+  QLIN_CUDA(launch_rmsnorm(*args, y16, static_scale, fp8, nvfp4, static_cast<cudaStream_t>(stream), dev));
   return QLIN_OK;
 }
 

@@ -211,8 +211,9 @@ __device__ __forceinline__ void st_global_v4_hint(void* p, uint32_t a, uint32_t 
 
 // ------------------------------------------------- bias, activation, residual ---
 
-__device__ __forceinline__ void unpack16x2(uint32_t w, bool fp16, float& lo, float& hi) {
-  if (fp16) {
+template <bool kF16>
+__device__ __forceinline__ void unpack16x2(uint32_t w, float& lo, float& hi) {
+  if constexpr (kF16) {
     const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
     lo = f.x;
     hi = f.y;
@@ -223,8 +224,8 @@ __device__ __forceinline__ void unpack16x2(uint32_t w, bool fp16, float& lo, flo
 }
 
 // v[i] += 32 16-bit values at p (16-byte aligned).
-template <bool kMaybeFp16>
-__device__ __forceinline__ void add32(float (&v)[32], const uint16_t* p, bool fp16) {
+template <bool kF16>
+__device__ __forceinline__ void add32(float (&v)[32], const uint16_t* p) {
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
     const uint4 w = ld_global_v4(p + 8 * k);
@@ -232,7 +233,7 @@ __device__ __forceinline__ void add32(float (&v)[32], const uint16_t* p, bool fp
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       float lo, hi;
-      unpack16x2(u[i], kMaybeFp16 && fp16, lo, hi);
+      unpack16x2<kF16>(u[i], lo, hi);
       v[8 * k + 2 * i] = __fadd_rn(v[8 * k + 2 * i], lo);
       v[8 * k + 2 * i + 1] = __fadd_rn(v[8 * k + 2 * i + 1], hi);
     }
@@ -249,14 +250,13 @@ __device__ __forceinline__ void scale_columns(float (&v)[32], const KParams& p, 
 }
 
 // act(v + bias) + residual of 32 columns of one row.
-template <bool kMaybeFp16>
+template <bool kF16>
 __device__ __forceinline__ void finish32(float (&v)[32], const KParams& p, int64_t row,
                                          int64_t n0) {
-  const bool fp16 = p.fp16 != 0;
-  if (p.bias != nullptr) add32<kMaybeFp16>(v, p.bias + n0, fp16);
+  if (p.bias != nullptr) add32<kF16>(v, p.bias + n0);
   activate(v, p.act);
   if (p.residual != nullptr && row < p.M)
-    add32<kMaybeFp16>(v, p.residual + row * p.residual_stride + n0, fp16);
+    add32<kF16>(v, p.residual + row * p.residual_stride + n0);
 }
 
 // kBf16 (with !kFp4): bf16 operands on the FP8 skeleton (the same 128-byte
@@ -887,12 +887,18 @@ __global__ void __launch_bounds__(Cfg<kFp4, kBN, kPair>::kThreads, 1)
               } else if (!kBf16) {
                 scale_columns(v, p, row_scale, n0);
               }
-              finish32<kBf16>(v, p, row, n0);
+              if (kBf16 && p.fp16)
+                finish32<true>(v, p, row, n0);
+              else
+                finish32<false>(v, p, row, n0);
             }
+            if (kBf16 && p.fp16) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-              packed[c * 16 + i] = kBf16 && p.fp16 ? pack_f16x2(v[2 * i], v[2 * i + 1])
-                                                   : pack_bf16x2(v[2 * i], v[2 * i + 1]);
+              for (int i = 0; i < 16; ++i) packed[c * 16 + i] = pack_f16x2(v[2 * i], v[2 * i + 1]);
+            } else {
+#pragma unroll
+              for (int i = 0; i < 16; ++i) packed[c * 16 + i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
+            }
             continue;
           }
           float a[32];

@@ -73,7 +73,8 @@ cudaError_t launch_quant_fp8_rows(const void* w, int64_t N, int64_t K, const qli
 
 // ---- norm (qlin_norm.cu): one of y16, fp8 and nvfp4 is the output ----
 cudaError_t launch_rmsnorm(const qlin_rmsnorm_t& a, void* y16, const float* static_scale,
-                           const qlin_fp8_t* fp8, const qlin_nvfp4_t* nvfp4, cudaStream_t s);
+                           const qlin_fp8_t* fp8, const qlin_nvfp4_t* nvfp4, cudaStream_t s,
+                           Device dev);
 
 // ---- rotary positions (qlin_rope.cu) ----
 cudaError_t launch_rope(const qlin_rope_t& a, cudaStream_t s);

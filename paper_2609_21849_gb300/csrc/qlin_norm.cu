@@ -1,14 +1,23 @@
 // Residual addition and root-mean-square norm, written as the 16-bit, FP8 or NVFP4
 // input of the next linear:
 //   s = x + residual,  n = s * (1 / sqrt(mean(s^2) + eps)) * weight.
-// A unit is 16 elements of a row: one NVFP4 block, 16 bytes of FP8 codes.
+// A row is an array of 16-byte chunks (8 elements); neighbouring threads take
+// neighbouring chunks.  Two of them hold one NVFP4 block (K % 64 == 0: both inside).
+//
+// Bound by HBM: 2 bytes read (4 with a residual, 2 more for the sum) and 0.5625 to 2
+// written per element.  A row stays in registers between its reduction and its output,
+// so everything is read once: 4608 x 3072 bf16 with residual to FP8 rows 16.5 us, 99 MB
+// at 90% of the measured copy rate; the same kernel with three reads per row took 28.
+// Below that it is instructions: at 18432 x 3072 fp16 a run-time choice of the 16-bit
+// type, bounds tests and tests for weight and residual in every chunk cost as many as
+// the arithmetic (42 us; the type and the residual as template parameters, ones for a
+// missing weight and a path without bounds tests: 29.5).  Copies ahead through shared
+// memory (cp.async, three rows in flight per CTA) measured slower, 42.
 #include "qlin_internal.h"
 
 namespace qlin {
 
 namespace {
-
-constexpr int kThreads = 256;
 
 enum class NormOut { k16, kFp8Rows, kFp8, kNvfp4 };
 
@@ -18,9 +27,8 @@ struct NormParams {
   uint8_t* sum;
   const uint8_t* weight;
   int64_t x_row, residual_row, sum_row;   // bytes
-  int64_t K;
-  float eps;
-  int fp16;
+  int64_t M, K;
+  float one_over_K, eps;
   const float* static_scale;
   float* scale;        // FP8 / NVFP4: receives the static scale, or a scale per row
   uint8_t* y;          // 16-bit values or codes
@@ -41,175 +49,413 @@ __device__ __forceinline__ uint4 ldg128(const void* p) {
                : "l"(p));
   return v;
 }
-
-__device__ __forceinline__ void unpack2(uint32_t w, bool fp16, float& lo, float& hi) {
-  if (fp16) {
-    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
-    lo = f.x;
-    hi = f.y;
-  } else {
-    lo = bf16_lo(w);
-    hi = bf16_hi(w);
-  }
-}
-
-__device__ __forceinline__ void load16(const uint8_t* p, bool fp16, float (&f)[16]) {
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const uint4 v = ldg128(p + 16 * h);
-    unpack2(v.x, fp16, f[8 * h], f[8 * h + 1]);
-    unpack2(v.y, fp16, f[8 * h + 2], f[8 * h + 3]);
-    unpack2(v.z, fp16, f[8 * h + 4], f[8 * h + 5]);
-    unpack2(v.w, fp16, f[8 * h + 6], f[8 * h + 7]);
-  }
-}
-
-__device__ __forceinline__ void store16(uint8_t* p, bool fp16, const float (&f)[16]) {
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    uint32_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float lo = f[8 * h + 2 * i], hi = f[8 * h + 2 * i + 1];
-      w[i] = fp16 ? pack_f16x2(lo, hi) : pack_bf16x2(lo, hi);
-    }
-    *reinterpret_cast<uint4*>(p + 16 * h) = make_uint4(w[0], w[1], w[2], w[3]);
-  }
-}
-
-__device__ __forceinline__ float block_reduce(float v, bool maximum, float* red) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    const float u = __shfl_xor_sync(0xFFFFFFFFu, v, o);
-    v = maximum ? max_nan(v, u) : v + u;
-  }
-  __syncthreads();   // red's last readers are done
-  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
-  __syncthreads();
-  v = red[0];
-#pragma unroll
-  for (int w = 1; w < kThreads / 32; ++w) v = maximum ? max_nan(v, red[w]) : v + red[w];
+// (x and residual are read once)
+__device__ __forceinline__ uint4 ldg128_once(const void* p) {
+  uint4 v;
+  asm volatile("ld.global.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+               : "l"(p));
   return v;
 }
 
-// 1 / sqrt(ss / K + eps); a row whose squares overflowed takes them of s * 2^-80
+// Two packed fp32 operations per instruction, each rounded once.
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 r;
+  asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\t"
+      "mul.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
+      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return r;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 r;
+  asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\t"
+      "add.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
+      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return r;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 r;
+  asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\t"
+      "fma.rn.f32x2 x, x, y, z;\n\tmov.b64 {%0, %1}, x;\n\t}"
+      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return r;
+}
+
+// kF16: fp16 data, else bf16 (as a run-time choice both conversions were computed and
+// one selected: a third of all instructions).
+template <bool kF16>
+__device__ __forceinline__ float2 unpack2(uint32_t w) {
+  if constexpr (kF16)
+    return __half22float2(*reinterpret_cast<const __half2*>(&w));
+  else
+    return make_float2(bf16_lo(w), bf16_hi(w));
+}
+
+template <bool kF16>
+__device__ __forceinline__ void unpack8(uint4 v, float2 (&f)[4]) {
+  f[0] = unpack2<kF16>(v.x);
+  f[1] = unpack2<kF16>(v.y);
+  f[2] = unpack2<kF16>(v.z);
+  f[3] = unpack2<kF16>(v.w);
+}
+
+template <bool kF16>
+__device__ __forceinline__ uint4 pack8(const float2 (&f)[4]) {
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = kF16 ? pack_f16x2(f[i].x, f[i].y) : pack_bf16x2(f[i].x, f[i].y);
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+__device__ __forceinline__ float abs_max8(float m, const float2 (&f)[4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) m = max_nan(m, max_nan(fabsf(f[i].x), fabsf(f[i].y)));
+  return m;
+}
+
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+  return v;
+}
+__device__ __forceinline__ float warp_max(float v) {
+  float r;
+  asm("redux.sync.max.NaN.f32 %0, %1, 0xFFFFFFFF;" : "=f"(r) : "f"(v));
+  return r;
+}
+
+// The sum of a and the maximum of m over the threads of a row (a warp, or the CTA;
+// red: an entry per warp, not written again before another barrier).
+template <bool kWarpRow, bool kMax>
+__device__ __forceinline__ float2 row_reduce(float a, float m, float2* red) {
+  a = warp_sum(a);
+  if (kMax) m = warp_max(m);
+  if constexpr (!kWarpRow) {
+    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = make_float2(a, m);
+    __syncthreads();
+    const int warps = (int)(blockDim.x >> 5);
+    a = red[0].x;
+    m = red[0].y;
+    for (int w = 1; w < warps; ++w) {
+      const float2 v = red[w];
+      a += v.x;
+      if (kMax) m = max_nan(m, v.y);
+    }
+  }
+  return make_float2(a, m);
+}
+
+// 1 / sqrt(ss / K + eps); a row whose squares overflow takes them of s * 2^-80
 // instead (2^-80 times the largest sum of two 16-bit values squares to 2^98).
 constexpr float kDown = 0x1p-80f;
-__device__ __forceinline__ float inverse_rms(float ss, float K, float eps) {
-  return __frsqrt_rn(__fadd_rn(__fdiv_rn(ss, K), eps));
+__device__ __forceinline__ float inverse_rms(float ss, float one_over_K, float eps) {
+  return rsqrtf(__fmaf_rn(ss, one_over_K, eps));
 }
 
-// The 16 codes of one unit.
-template <NormOut kOut>
-__device__ __forceinline__ void write_unit(const NormParams& p, int64_t row, int u,
-                                           const float (&n)[16], float s_enc) {
+// The output of a chunk: 16-bit values, FP8 codes of n * s_enc, or half an NVFP4 block
+// (the neighbouring lane has the other half; whole warps call).  y: the chunk's place in
+// the output, c its number in the row.
+template <NormOut kOut, bool kF16>
+__device__ __forceinline__ void write_chunk(const NormParams& p, uint8_t* y, int64_t row, int c, bool own,
+                                            float2 (&n)[4], float s_enc) {
   if constexpr (kOut == NormOut::k16) {
-    store16(p.y + (row * p.K + 16 * u) * 2, p.fp16 != 0, n);
+    if (own) *reinterpret_cast<uint4*>(y) = pack8<kF16>(n);
   } else if constexpr (kOut == NormOut::kNvfp4) {
-    float amax = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) amax = max_nan(amax, fabsf(n[i]));
+    float amax = abs_max8(0.0f, n);
+    amax = max_nan(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 1));
     const uint32_t sb = e4m3_code_div6(__fmul_rn(amax, s_enc));
     const float r_b = sb == 0u ? 0.0f : __fdiv_rn(s_enc, e4m3_value(sb));
-    uint32_t w[2];
+    float f[8];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      float f[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) f[i] = __fmul_rn(n[8 * h + i], r_b);
-      w[h] = e2m1x8(f);
+    for (int i = 0; i < 4; ++i) {
+      const float2 q = mul2(n[i], make_float2(r_b, r_b));
+      f[2 * i] = q.x;
+      f[2 * i + 1] = q.y;
     }
-    *reinterpret_cast<uint2*>(p.y + row * (p.K / 2) + 8 * u) = make_uint2(w[0], w[1]);
-    p.block_scales[scale_offset(row, u, p.K)] = (uint8_t)sb;
+    if (own) *reinterpret_cast<uint32_t*>(y) = e2m1x8(f);
+    if (own && (c & 1) == 0) p.block_scales[scale_offset(row, c / 2, p.K)] = (uint8_t)sb;
   } else {
-    uint32_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      w[i] = e4m3x4(__fmul_rn(n[4 * i], s_enc), __fmul_rn(n[4 * i + 1], s_enc),
-                    __fmul_rn(n[4 * i + 2], s_enc), __fmul_rn(n[4 * i + 3], s_enc));
-    *reinterpret_cast<uint4*>(p.y + row * p.K + 16 * u) = make_uint4(w[0], w[1], w[2], w[3]);
+    if (own)
+      *reinterpret_cast<uint2*>(y) =
+          make_uint2(e4m3x4(n[0].x, n[0].y, n[1].x, n[1].y), e4m3x4(n[2].x, n[2].y, n[3].x, n[3].y));
   }
 }
-
-// One CTA per row, which it reads once per pass (sum of squares; FP8 rows: the
-// maximum; output).  sum is written in the last pass, by the thread that reads the
-// same elements, so that it may be x or residual.
+// Bytes of a chunk's output.
 template <NormOut kOut>
-__global__ void __launch_bounds__(kThreads) rmsnorm_kernel(const NormParams p) {
-  __shared__ float red[kThreads / 32];
-  const int64_t row = blockIdx.x;
-  const bool fp16 = p.fp16 != 0;
-  const int units = (int)(p.K / 16);
-  const uint8_t* const x = p.x + row * p.x_row;
-  const uint8_t* const r = p.residual == nullptr ? nullptr : p.residual + row * p.residual_row;
+constexpr int kOutChunk = kOut == NormOut::k16 ? 16 : kOut == NormOut::kNvfp4 ? 4 : 8;
+
+// s of one chunk from x and the residual, its squares added to ss.
+template <bool kF16, bool kResidual>
+__device__ __forceinline__ void add_chunk(uint4 x, uint4 r, float2 (&s)[4], float2& ss) {
+  unpack8<kF16>(x, s);
+  if (kResidual) {
+    float2 f[4];
+    unpack8<kF16>(r, f);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s[i] = add2(s[i], f[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) ss = fma2(s[i], s[i], ss);
+}
+
+// s * pre * weight of one chunk.
+template <bool kF16>
+__device__ __forceinline__ void weigh(float2 (&s)[4], float pre, const uint4& w) {
+  float2 f[4];
+  unpack8<kF16>(w, f);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) s[i] = mul2(mul2(s[i], make_float2(pre, pre)), f[i]);
+}
+
+// A weight of ones (without one).
+template <bool kF16>
+__device__ __forceinline__ uint4 ones() {
+  const uint32_t w = kF16 ? 0x3C003C00u : 0x3F803F80u;
+  return make_uint4(w, w, w, w);
+}
+
+// A row from registers: chunks tid, tid + T, ... of thread tid of the row's T.  kFull:
+// every thread has kChunks of them.  With t = s * weight, FP8 rows take max |t| in the
+// same reduction as the squares: max |n| is max |t| / rms, and the codes are
+// t * (448 / max |t|).
+template <NormOut kOut, bool kF16, bool kResidual, int kChunks, bool kWarpRow, bool kFull>
+__device__ __forceinline__ void held_row(const NormParams& p, int64_t row, int tid, int T, int chunks,
+                                         float2* red) {
+  auto in = [&](int i) { return kFull || tid + i * T < chunks; };
+  uint4 vx[kChunks], vr[kChunks], vw[kChunks];
+  {
+    const uint8_t* const x = p.x + row * p.x_row + 16 * tid;
+    const uint8_t* const r = kResidual ? p.residual + row * p.residual_row + 16 * tid : nullptr;
+    const uint8_t* const w = p.weight + 16 * tid;
+#pragma unroll
+    for (int i = 0; i < kChunks; ++i) {
+      if (!in(i)) continue;
+      vx[i] = ldg128_once(x + 16 * i * T);
+      if (kResidual) vr[i] = ldg128_once(r + 16 * i * T);
+    }
+    if (p.weight != nullptr) {
+#pragma unroll
+      for (int i = 0; i < kChunks; ++i)
+        if (in(i)) vw[i] = ldg128(w + 16 * i * T);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kChunks; ++i) vw[i] = ones<kF16>();
+    }
+  }
+  float s_dec = 1.0f, f = 1.0f;
+  if constexpr (kOut == NormOut::kFp8 || kOut == NormOut::kNvfp4) {
+    s_dec = *p.static_scale;
+    if (row == 0 && tid == 0 && p.scale != p.static_scale) *p.scale = s_dec;
+    f = encode_scale(s_dec);
+  }
+  float2 s[kChunks][4], ss = make_float2(0.0f, 0.0f);
+#pragma unroll
+  for (int i = 0; i < kChunks; ++i) {
+    if (in(i)) {
+      add_chunk<kF16, kResidual>(vx[i], vr[i], s[i], ss);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) s[i][k] = make_float2(0.0f, 0.0f);
+      vw[i] = ones<kF16>();
+    }
+  }
+  if (kResidual && p.sum != nullptr) {
+    uint8_t* const sum = p.sum + row * p.sum_row + 16 * tid;
+#pragma unroll
+    for (int i = 0; i < kChunks; ++i)
+      if (in(i)) *reinterpret_cast<uint4*>(sum + 16 * i * T) = pack8<kF16>(s[i]);
+  }
+  // max |s * pre * weight|
+  auto peak = [&](float pre) {
+    float m = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kChunks; ++i) {
+      float2 t[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) t[k] = s[i][k];
+      weigh<kF16>(t, pre, vw[i]);
+      m = abs_max8(m, t);
+    }
+    return m;
+  };
+  float m = 0.0f;
+  if (kOut == NormOut::kFp8Rows) m = peak(1.0f);
+  const float2 tot = row_reduce<kWarpRow, kOut == NormOut::kFp8Rows>(ss.x + ss.y, m, red);
+  float inv;
+  if (tot.x <= FLT_MAX) {
+    inv = inverse_rms(tot.x, p.one_over_K, p.eps);
+  } else {               // squares overflowed, or an infinity or a NaN
+    float2 s2 = make_float2(0.0f, 0.0f);
+#pragma unroll
+    for (int i = 0; i < kChunks; ++i)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float2 v = mul2(s[i][k], make_float2(kDown, kDown));
+        s2 = fma2(v, v, s2);
+      }
+    inv = inverse_rms(row_reduce<kWarpRow, false>(s2.x + s2.y, 0.0f, red + 32).x, p.one_over_K, 0.0f) * kDown;
+  }
+  // n's factors of s: pre * weight * f, in one product with pre where none of them, nor
+  // s * pre, can overflow (|s * inv| <= sqrt(K))
+  float pre = inv;
+  bool one = kOut == NormOut::k16 || kOut == NormOut::kNvfp4;
+  if constexpr (kOut == NormOut::kFp8Rows) {
+    one = tot.x <= FLT_MAX && tot.y >= 0x1p-50f && tot.y <= FLT_MAX;
+    if (one) {
+      pre = __fdividef(448.0f, tot.y);
+      s_dec = __fmul_rn(__fmul_rn(tot.y, inv), 1.0f / 448.0f);
+    } else {
+      m = row_reduce<kWarpRow, true>(0.0f, peak(inv), red + 64).y;
+      s_dec = m == 0.0f ? 1.0f : __fdiv_rn(m, 448.0f);
+      f = encode_scale(s_dec);
+    }
+    if (tid == 0) p.scale[row] = s_dec;
+  } else if constexpr (kOut == NormOut::kFp8) {
+    one = f >= 0x1p-64f && f <= 0x1p64f && inv >= 0x1p-60f;
+    if (one) pre = __fmul_rn(inv, f);
+  }
+#pragma unroll
+  for (int i = 0; i < kChunks; ++i) weigh<kF16>(s[i], pre, vw[i]);
+  if (!one) {
+#pragma unroll
+    for (int i = 0; i < kChunks; ++i)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) s[i][k] = mul2(s[i][k], make_float2(f, f));
+  }
+  uint8_t* const y = p.y + (row * (p.K / 8) + tid) * kOutChunk<kOut>;
+#pragma unroll
+  for (int i = 0; i < kChunks; ++i)
+    write_chunk<kOut, kF16>(p, y + i * T * kOutChunk<kOut>, row, tid + i * T, in(i), s[i], f);
+}
+
+// A row per CTA, or per warp, held in registers in fp32 between its reduction and its
+// output: x and the residual are read once.  (Four chunks: 80 registers, so that two
+// CTAs of a 12288-element row fit an SM; 2048 such rows 37.0 us with 82, now 28.3.)
+template <NormOut kOut, bool kF16, bool kResidual, int kChunks, bool kWarpRow>
+__global__ void __launch_bounds__(kWarpRow ? 256 : kChunks == 2 ? 1024 : 768)
+    rmsnorm_held_kernel(const NormParams p) {
+  __shared__ float2 red[kWarpRow ? 1 : 3 * 32];
+  const int tid = kWarpRow ? threadIdx.x & 31 : threadIdx.x;
+  const int T = kWarpRow ? 32 : (int)blockDim.x;
+  const int64_t row = kWarpRow ? (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5) : blockIdx.x;
+  const int chunks = (int)(p.K / 8);
   grid_dep_wait();
   grid_dep_launch();
-  auto load_s = [&](int u, float (&s)[16]) {
-    load16(x + 32 * (int64_t)u, fp16, s);
-    if (r != nullptr) {
-      float f[16];
-      load16(r + 32 * (int64_t)u, fp16, f);
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] = __fadd_rn(s[i], f[i]);
-    }
+  if (row >= p.M) return;   // (whole warps)
+  if (chunks == kChunks * T)
+    held_row<kOut, kF16, kResidual, kChunks, kWarpRow, true>(p, row, tid, T, chunks, red);
+  else
+    held_row<kOut, kF16, kResidual, kChunks, kWarpRow, false>(p, row, tid, T, chunks, red);
+}
+
+// Rows beyond the registers of a CTA: one CTA per row, which it reads once per pass
+// (sum of squares; FP8 rows: the maximum; output).  The sum is written in the last
+// pass, by the thread that reads the same elements, so that it may be x or residual.
+constexpr int kLongThreads = 512;
+
+template <NormOut kOut, bool kF16, bool kResidual>
+__global__ void __launch_bounds__(kLongThreads) rmsnorm_long_kernel(const NormParams p) {
+  __shared__ float2 red[3 * 32];
+  const int64_t row = blockIdx.x;
+  const int chunks = (int)(p.K / 8);
+  const uint8_t* const x = p.x + row * p.x_row;
+  const uint8_t* const r = p.residual + row * p.residual_row;
+  grid_dep_wait();
+  grid_dep_launch();
+  auto load = [&](int c, float2 (&s)[4], float2& ss) {
+    const uint4 a = ldg128(x + 16 * (int64_t)c);
+    add_chunk<kF16, kResidual>(a, kResidual ? ldg128(r + 16 * (int64_t)c) : a, s, ss);
   };
-  auto load_n = [&](const float (&s)[16], int u, float inv, float (&n)[16]) {
-    float w[16];
-    if (p.weight != nullptr) load16(p.weight + 32 * (int64_t)u, fp16, w);
+  auto load_w = [&](int c) { return p.weight != nullptr ? ldg128(p.weight + 16 * (int64_t)c) : ones<kF16>(); };
+  float2 s[4], ss = make_float2(0.0f, 0.0f), unused = ss;
+  float inv;
+  for (int c = threadIdx.x; c < chunks; c += kLongThreads) load(c, s, ss);
+  const float tot = row_reduce<false, false>(ss.x + ss.y, 0.0f, red).x;
+  if (tot <= FLT_MAX) {
+    inv = inverse_rms(tot, p.one_over_K, p.eps);
+  } else {
+    ss = make_float2(0.0f, 0.0f);
+    for (int c = threadIdx.x; c < chunks; c += kLongThreads) {
+      load(c, s, unused);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      n[i] = __fmul_rn(s[i], inv);
-      if (p.weight != nullptr) n[i] = __fmul_rn(n[i], w[i]);
-    }
-  };
-  auto squares = [&](float pre) {
-    float ss = 0.0f, s[16];
-    for (int u = threadIdx.x; u < units; u += kThreads) {
-      load_s(u, s);
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float v = s[i] * pre;
-        ss = __fmaf_rn(v, v, ss);
+      for (int k = 0; k < 4; ++k) {
+        const float2 v = mul2(s[k], make_float2(kDown, kDown));
+        ss = fma2(v, v, ss);
       }
     }
-    return block_reduce(ss, false, red);
-  };
-  float ss = squares(1.0f), inv;
-  if (ss <= FLT_MAX)
-    inv = inverse_rms(ss, (float)p.K, p.eps);
-  else
-    inv = inverse_rms(squares(kDown), (float)p.K, 0.0f) * kDown;
-  float s_enc = 0.0f;
+    inv = inverse_rms(row_reduce<false, false>(ss.x + ss.y, 0.0f, red + 32).x, p.one_over_K, 0.0f) * kDown;
+  }
+  float f = 1.0f;
   if constexpr (kOut == NormOut::kFp8Rows) {
-    float amax = 0.0f, s[16], n[16];
-    for (int u = threadIdx.x; u < units; u += kThreads) {
-      load_s(u, s);
-      load_n(s, u, inv, n);
-#pragma unroll
-      for (int i = 0; i < 16; ++i) amax = max_nan(amax, fabsf(n[i]));
+    float m = 0.0f;
+    for (int c = threadIdx.x; c < chunks; c += kLongThreads) {
+      load(c, s, unused);
+      weigh<kF16>(s, inv, load_w(c));
+      m = abs_max8(m, s);
     }
-    amax = block_reduce(amax, true, red);
-    const float s_dec = amax == 0.0f ? 1.0f : __fdiv_rn(amax, 448.0f);
+    m = row_reduce<false, true>(0.0f, m, red + 64).y;
+    const float s_dec = m == 0.0f ? 1.0f : __fdiv_rn(m, 448.0f);
     if (threadIdx.x == 0) p.scale[row] = s_dec;
-    s_enc = encode_scale(s_dec);
+    f = encode_scale(s_dec);
   } else if constexpr (kOut != NormOut::k16) {
     const float s_dec = *p.static_scale;
     if (row == 0 && threadIdx.x == 0 && p.scale != p.static_scale) *p.scale = s_dec;
-    s_enc = encode_scale(s_dec);
+    f = encode_scale(s_dec);
   }
-  for (int u = threadIdx.x; u < units; u += kThreads) {
-    float s[16], n[16];
-    load_s(u, s);
-    load_n(s, u, inv, n);
-    if (p.sum != nullptr) store16(p.sum + row * p.sum_row + 32 * (int64_t)u, fp16, s);
-    write_unit<kOut>(p, row, u, n, s_enc);
+  for (int c0 = 0; c0 < chunks; c0 += kLongThreads) {
+    const int c = c0 + (int)threadIdx.x;
+    const bool own = c < chunks;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) s[k] = make_float2(0.0f, 0.0f);
+    if (own) {
+      load(c, s, unused);
+      if (kResidual && p.sum != nullptr)
+        *reinterpret_cast<uint4*>(p.sum + row * p.sum_row + 16 * (int64_t)c) = pack8<kF16>(s);
+      weigh<kF16>(s, inv, load_w(c));
+      if (kOut == NormOut::kFp8Rows || kOut == NormOut::kFp8) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) s[k] = mul2(s[k], make_float2(f, f));
+      }
+    }
+    write_chunk<kOut, kF16>(p, p.y + (row * (p.K / 8) + c) * kOutChunk<kOut>, row, c, own, s, f);
   }
+}
+
+template <NormOut kOut, bool kF16, bool kResidual>
+cudaError_t launch_out(const NormParams& p, int num_sms, cudaStream_t s) {
+  const int64_t chunks = p.K / 8;
+  if (chunks <= 128) {
+    const unsigned grid = (unsigned)((p.M + 7) / 8);
+    return chunks <= 32   ? launch_pdl(rmsnorm_held_kernel<kOut, kF16, kResidual, 1, true>, grid, 256, 0, s, p)
+           : chunks <= 64 ? launch_pdl(rmsnorm_held_kernel<kOut, kF16, kResidual, 2, true>, grid, 256, 0, s, p)
+                          : launch_pdl(rmsnorm_held_kernel<kOut, kF16, kResidual, 4, true>, grid, 256, 0, s, p);
+  }
+  // Four chunks per thread halve a row's share of the reduction (18432 x 3072 fp16 to
+  // static FP8 31.0 us, with two 36.2); two leave fewer threads idle where four do not
+  // divide the row (4608 x 2560 to FP8 rows 14.5 against 16.3) and have the shorter
+  // chain where rows are few (512 x 2560 3.4 against 4.0).
+  if (chunks > 2048)
+    return launch_pdl(rmsnorm_long_kernel<kOut, kF16, kResidual>, (unsigned)p.M, kLongThreads, 0, s, p);
+  if (chunks % 128 == 0 && p.M >= 4 * num_sms)
+    return launch_pdl(rmsnorm_held_kernel<kOut, kF16, kResidual, 4, false>, (unsigned)p.M,
+                      (int)(chunks / 4), 0, s, p);
+  const int threads = (int)((chunks + 63) / 64) * 32;
+  return launch_pdl(rmsnorm_held_kernel<kOut, kF16, kResidual, 2, false>, (unsigned)p.M, threads, 0, s, p);
+}
+
+template <NormOut kOut>
+cudaError_t launch_types(const NormParams& p, int dtype, int num_sms, cudaStream_t s) {
+  if (dtype == QLIN_FP16)
+    return p.residual != nullptr ? launch_out<kOut, true, true>(p, num_sms, s)
+                                 : launch_out<kOut, true, false>(p, num_sms, s);
+  return p.residual != nullptr ? launch_out<kOut, false, true>(p, num_sms, s)
+                               : launch_out<kOut, false, false>(p, num_sms, s);
 }
 
 }  // namespace
 
 cudaError_t launch_rmsnorm(const qlin_rmsnorm_t& a, void* y16, const float* static_scale,
-                           const qlin_fp8_t* fp8, const qlin_nvfp4_t* nvfp4, cudaStream_t s) {
+                           const qlin_fp8_t* fp8, const qlin_nvfp4_t* nvfp4, cudaStream_t s, Device dev) {
   NormParams p{};
   p.x = static_cast<const uint8_t*>(a.x);
   p.residual = static_cast<const uint8_t*>(a.residual);
@@ -218,23 +464,24 @@ cudaError_t launch_rmsnorm(const qlin_rmsnorm_t& a, void* y16, const float* stat
   p.x_row = a.x_stride * 2;
   p.residual_row = a.residual_stride * 2;
   p.sum_row = a.sum_stride * 2;
+  p.M = a.M;
   p.K = a.K;
+  p.one_over_K = 1.0f / (float)a.K;
   p.eps = a.eps;
-  p.fp16 = a.dtype == QLIN_FP16 ? 1 : 0;
   p.static_scale = static_scale;
   p.y = static_cast<uint8_t*>(y16);
-  auto kern = rmsnorm_kernel<NormOut::k16>;
   if (fp8 != nullptr) {
     p.y = fp8->codes;
     p.scale = fp8->scale;
-    kern = fp8->per_channel ? rmsnorm_kernel<NormOut::kFp8Rows> : rmsnorm_kernel<NormOut::kFp8>;
-  } else if (nvfp4 != nullptr) {
+    return fp8->per_channel ? launch_types<NormOut::kFp8Rows>(p, a.dtype, dev.num_sms, s) : launch_types<NormOut::kFp8>(p, a.dtype, dev.num_sms, s);
+  }
+  if (nvfp4 != nullptr) {
     p.y = nvfp4->codes;
     p.scale = nvfp4->tensor_scale;
     p.block_scales = nvfp4->scales;
-    kern = rmsnorm_kernel<NormOut::kNvfp4>;
+    return launch_types<NormOut::kNvfp4>(p, a.dtype, dev.num_sms, s);
   }
-  return launch_pdl(kern, (unsigned)a.M, kThreads, 0, s, p);
+  return launch_types<NormOut::k16>(p, a.dtype, dev.num_sms, s);
 }
 
 }  // namespace qlin
