@@ -531,7 +531,7 @@ qlin_status qlin_rope(const qlin_rope_t* a, void* stream) {
   unsigned* status;
   Device dev;
   QLIN_TRY(device_state(&status, &dev));
-  QLIN_CUDA(launch_rope(*a, static_cast<cudaStream_t>(stream)));
+  QLIN_CUDA(launch_rope(*a, dev.num_sms, static_cast<cudaStream_t>(stream)));
   return QLIN_OK;
 }
 

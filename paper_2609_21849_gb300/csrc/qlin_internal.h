@@ -21,13 +21,13 @@ struct Device {
 
 // Launch with programmatic stream serialization (see grid_dep_wait).
 template <typename... Params, typename... Args>
-cudaError_t launch_pdl(void (*kern)(Params...), unsigned grid, int block, int smem, cudaStream_t s,
+cudaError_t launch_pdl(void (*kern)(Params...), dim3 grid, int block, int smem, cudaStream_t s,
                        Args... args) {
   cudaLaunchConfig_t cfg{};
   cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.gridDim = dim3(grid, 1, 1);
+  cfg.gridDim = grid;
   cfg.blockDim = dim3((unsigned)block, 1, 1);
   cfg.dynamicSmemBytes = (size_t)smem;
   cfg.stream = s;
@@ -77,7 +77,7 @@ cudaError_t launch_rmsnorm(const qlin_rmsnorm_t& a, void* y16, const float* stat
                            Device dev);
 
 // ---- rotary positions (qlin_rope.cu) ----
-cudaError_t launch_rope(const qlin_rope_t& a, cudaStream_t s);
+cudaError_t launch_rope(const qlin_rope_t& a, int num_sms, cudaStream_t s);
 
 // ---- GEMMs (qlin_gemm.cu) ----
 struct GemmArgs {

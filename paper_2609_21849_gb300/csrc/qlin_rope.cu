@@ -3,6 +3,8 @@
 // turns modulo 2^64 is the angle without whole turns, exact for every position; its
 // top 32 bits give the angle to 2^-32 turn.  (In fp32 the product alone is off by
 // 0.03 radians at position 10^6.)
+#include <type_traits>
+
 #include "qlin_internal.h"
 
 namespace qlin {
@@ -78,11 +80,36 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(const RopeParams p) {
 }
 
 // ---- 16-byte accesses ----
-// An item is eight pairs of one head (16 elements: two chunks of 8, eight pairs
-// apart in the half layout, adjacent in the interleaved one), or a chunk past
-// rot_dim.  A CTA takes whole tokens; each thread issues the loads of its first items
-// before the rotations are computed, which overlap them.
-constexpr int kItems = 2;
+// A lane takes 16 elements of a head in two chunks of 8: eight pairs (the chunks half a
+// rotation apart in the half layout, adjacent in the interleaved one), or elements past
+// rot_dim (the last lane of a head perhaps one chunk of them; none in place).
+// A warp works alone, on some heads of one token or, where heads are few, on several
+// tokens: a lane keeps its place in the head, so its eight rotations stay in registers
+// for all of its heads, and nothing waits for another warp.  The loads of its first
+// heads are issued before the rotations are computed.
+//
+// Bound by HBM (2 bytes in, 2 out per element; positions and turns are small): 4608 x
+// 48 x 128 with strided rows 20.2 us interleaved, 19.8 in halves, 84-86% of the measured
+// copy rate; 9216 x 48 x 128 of which 64 turn 35.4 us, 96%.  A CTA per token with the
+// rotations behind a barrier took 24.8 us, scalar accesses 57.  Where the lanes of a
+// head do not divide a warp some idle (192 of 192: 24 of 32 lanes, 70%).  One token
+// takes 1.7 us, a launch and one chain of loads.
+// kItems heads of a lane are in flight at once (4, where work is plenty).
+constexpr int kMostItems = 4;
+constexpr int kVecWarps = 4;
+
+// 32 bytes (32-byte aligned).
+__device__ __forceinline__ void ldg256(const uint16_t* p, uint4 (&v)[2]) {
+  asm volatile("ld.global.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(v[0].x), "=r"(v[0].y), "=r"(v[0].z), "=r"(v[0].w), "=r"(v[1].x), "=r"(v[1].y),
+                 "=r"(v[1].z), "=r"(v[1].w)
+               : "l"(p));
+}
+__device__ __forceinline__ void stg256(uint16_t* p, uint4 a, uint4 b) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(a.x),
+               "r"(a.y), "r"(a.z), "r"(a.w), "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w)
+               : "memory");
+}
 
 __device__ __forceinline__ uint4 ldg128(const uint16_t* p) {
   uint4 v;
@@ -93,113 +120,159 @@ __device__ __forceinline__ uint4 ldg128(const uint16_t* p) {
 }
 
 template <bool kF16>
-__device__ __forceinline__ void unpack8(const uint4 v, float (&f)[8]) {
-  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+__device__ __forceinline__ float2 unpack2(uint32_t w) {
+  if constexpr (kF16)
+    return __half22float2(*reinterpret_cast<const __half2*>(&w));
+  else
+    return make_float2(bf16_lo(w), bf16_hi(w));
+}
+template <bool kF16>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  return kF16 ? pack_f16x2(lo, hi) : pack_bf16x2(lo, hi);
+}
+
+// The eight pairs (a[i], b[i]) of two chunks: element i of each (kHalf), or elements
+// 2 i and 2 i + 1 of both in a row.
+template <bool kF16, bool kHalf>
+__device__ __forceinline__ void unpack_pairs(const uint4 (&v)[2], float (&a)[8], float (&b)[8]) {
+  const uint32_t w[8] = {v[0].x, v[0].y, v[0].z, v[0].w, v[1].x, v[1].y, v[1].z, v[1].w};
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if constexpr (kF16) {
-      const float2 h = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
-      f[2 * i] = h.x;
-      f[2 * i + 1] = h.y;
+  for (int i = 0; i < 8; ++i) {
+    const float2 f = unpack2<kF16>(w[i]);
+    if (!kHalf) {
+      a[i] = f.x;
+      b[i] = f.y;
     } else {
-      f[2 * i] = bf16_lo(w[i]);
-      f[2 * i + 1] = bf16_hi(w[i]);
+      float* const d = i < 4 ? a : b;
+      d[2 * (i & 3)] = f.x;
+      d[2 * (i & 3) + 1] = f.y;
     }
   }
 }
-
-template <bool kF16>
-__device__ __forceinline__ uint4 pack8(const float (&f)[8]) {
-  uint32_t w[4];
+template <bool kF16, bool kHalf>
+__device__ __forceinline__ void pack_pairs(const float (&a)[8], const float (&b)[8], uint4 (&v)[2]) {
+  uint32_t w[8];
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    w[i] = kF16 ? pack_f16x2(f[2 * i], f[2 * i + 1]) : pack_bf16x2(f[2 * i], f[2 * i + 1]);
-  return make_uint4(w[0], w[1], w[2], w[3]);
+  for (int i = 0; i < 8; ++i) {
+    const float* const d = i < 4 ? a : b;
+    w[i] = kHalf ? pack2<kF16>(d[2 * (i & 3)], d[2 * (i & 3) + 1]) : pack2<kF16>(a[i], b[i]);
+  }
+  v[0] = make_uint4(w[0], w[1], w[2], w[3]);
+  v[1] = make_uint4(w[4], w[5], w[6], w[7]);
 }
 
-// (a, b) of a pair turned by r = (cos, sin).
-__device__ __forceinline__ void turn(float& a, float& b, float c, float s) {
-  const float x = a;
-  a = __fsub_rn(__fmul_rn(x, c), __fmul_rn(b, s));
-  b = __fadd_rn(__fmul_rn(x, s), __fmul_rn(b, c));
+// Two pairs turned by packed arithmetic: (a, b) -> (a c - b s, b c + a s); ns = -s.
+__device__ __forceinline__ void turn2(float (&a)[8], float (&b)[8], int i, float2 c, float2 s, float2 ns) {
+  asm("{\n\t.reg .b64 a, b, c, s, n, x, y;\n\t"
+      "mov.b64 a, {%0, %1};\n\tmov.b64 b, {%2, %3};\n\tmov.b64 c, {%4, %5};\n\t"
+      "mov.b64 s, {%6, %7};\n\tmov.b64 n, {%8, %9};\n\t"
+      "mul.rn.f32x2 x, b, n;\n\tmul.rn.f32x2 y, b, c;\n\t"
+      "fma.rn.f32x2 x, a, c, x;\n\tfma.rn.f32x2 y, a, s, y;\n\t"
+      "mov.b64 {%0, %1}, x;\n\tmov.b64 {%2, %3}, y;\n\t}"
+      : "+f"(a[i]), "+f"(a[i + 1]), "+f"(b[i]), "+f"(b[i + 1])
+      : "f"(c.x), "f"(c.y), "f"(s.x), "f"(s.y), "f"(ns.x), "f"(ns.y));
 }
 
-// The threads of a CTA are a multiple of the items of a head, so that a thread keeps
-// its place in the head and steps through heads.  kOneToken: a CTA has one token.
-template <bool kF16, bool kHalf, bool kOneToken>
-__global__ void __launch_bounds__(512) rope_vec_kernel(const RopeParams p, int tokens_per_cta,
-                                                       int64_t tokens) {
-  extern __shared__ float2 rot[];   // [tokens_per_cta][pairs]
-  const int64_t token0 = (int64_t)blockIdx.x * tokens_per_cta;
-  const int here = kOneToken ? 1 : (int)min((int64_t)tokens_per_cta, tokens - token0);
-  const int eights = p.pairs / 8, per_head = eights + (p.head_dim - 2 * p.pairs) / 8;
-  const int heads = here * p.heads;
-  const int first = (int)threadIdx.x / per_head, at = (int)threadIdx.x - first * per_head;
-  const int step = (int)blockDim.x / per_head;
-  const bool turns = at < eights;
-  const int off0 = turns ? (kHalf ? 8 : 16) * at : 8 * at + p.pairs;
-  const int off1 = kHalf ? 8 * at + p.pairs : 16 * at + 8;
+// The split of the work: units (warps) of `tokens` tokens or of `heads` heads of one.
+// The CTAs' y counts the groups of heads.
+struct RopeUnits {
+  int64_t count;
+  int per_head, slots;    // lanes of a head; heads that a warp takes at a time
+  int tokens, heads;
+  // n / d of the small n here is n * ceil(2^20 / d) >> 20 (n d < 2^20)
+  uint32_t by_per_head, by_heads, by_pairs;
+  int wide;               // rows start on 32-byte boundaries: a lane's adjacent chunks in one access
+};
+
+template <bool kF16, bool kHalf, int kItems>
+__global__ void __launch_bounds__(kVecWarps * 32) rope_vec_kernel(const RopeParams p, const RopeUnits u,
+                                                                  int64_t tokens) {
+  extern __shared__ float2 rot_all[];   // per warp [tokens][pairs]
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int64_t unit = (int64_t)blockIdx.x * kVecWarps + warp;
   grid_dep_wait();
   grid_dep_launch();
-  bool have_rot = false;
-  for (int h0 = first; h0 < heads || !have_rot; h0 += kItems * step) {
-    uint4 v[kItems][2];
-    int64_t yo[kItems];
-    int tok[kItems];
+  if (unit >= u.count) return;   // (whole warps)
+  const int group = (int)blockIdx.y;
+  const int64_t token0 = unit * u.tokens;
+  const int here = (int)min((int64_t)u.tokens, tokens - token0);
+  const int eights = p.pairs / 8;
+  auto div20 = [](int n, uint32_t by) { return (int)(((uint32_t)n * by) >> 20); };
+  const int slot = div20(lane, u.by_per_head), at = lane - slot * u.per_head;
+  // the lane's token, and its heads: first, then every slots-th
+  const int tok = u.tokens == 1 ? 0 : div20(slot, u.by_heads);
+  int head = u.tokens == 1 ? group * u.heads + slot : slot - tok * p.heads;
+  const int head_end = slot >= u.slots || tok >= here ? 0
+                       : u.tokens == 1                ? min(p.heads, (group + 1) * u.heads)
+                                                      : head + 1;
+  const bool turns = at < eights;
+  const int off0 = (kHalf && turns ? 8 : 16) * at;   // (2 pairs = 16 eights precede the rest)
+  const int off1 = kHalf && turns ? off0 + p.pairs : off0 + 8;
+  const bool second = off1 < p.head_dim;
+  const bool wide = u.wide && second && (!kHalf || !turns);
+  const uint16_t* x = p.x + (token0 + tok) * p.x_token + head * p.x_head;
+  uint16_t* y = p.y + (token0 + tok) * p.y_token + head * p.y_head;
+  const int64_t x_step = u.slots * p.x_head, y_step = u.slots * p.y_head;
+  uint4 v[kItems][2];
+  auto load = [&] {
 #pragma unroll
     for (int k = 0; k < kItems; ++k) {
-      const int q = h0 + k * step;
-      if (q >= heads) continue;
-      tok[k] = kOneToken ? 0 : q / p.heads;
-      const int head = q - tok[k] * p.heads;
-      const uint16_t* const xp = p.x + (token0 + tok[k]) * p.x_token + head * p.x_head;
-      yo[k] = (token0 + tok[k]) * p.y_token + head * p.y_head;
-      v[k][0] = ldg128(xp + off0);
-      if (turns) v[k][1] = ldg128(xp + off1);
-    }
-    if (!have_rot) {
-      for (int j = threadIdx.x; j < here * p.pairs; j += blockDim.x) {
-        const int t = kOneToken ? 0 : j / p.pairs;
-        rot[j] = rotation(p, token0 + t, j - t * p.pairs);
+      if (head + k * u.slots >= head_end) continue;
+      if (wide) {
+        ldg256(x + off0, v[k]);
+      } else {
+        v[k][0] = ldg128(x + off0);
+        if (second) v[k][1] = ldg128(x + off1);
       }
-      __syncthreads();
-      have_rot = true;
+      x += x_step;
     }
+  };
+  load();
+  float2* const rot = rot_all + warp * u.tokens * p.pairs;
+#pragma unroll 2
+  for (int j = lane; j < here * p.pairs; j += 32) {
+    const int t = u.tokens == 1 ? 0 : div20(j, u.by_pairs);
+    rot[j] = rotation(p, token0 + t, j - t * p.pairs);
+  }
+  __syncwarp();
+  float2 c[4], sn[4], ns[4];   // of pairs 2 j and 2 j + 1
+  if (head < head_end && turns) {
+    const float4* const src = reinterpret_cast<const float4*>(rot + tok * p.pairs + 8 * at);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float4 r = src[j];
+      c[j] = make_float2(r.x, r.z);
+      sn[j] = make_float2(r.y, r.w);
+      ns[j] = make_float2(-r.y, -r.w);
+    }
+  }
+  while (head < head_end) {
 #pragma unroll
     for (int k = 0; k < kItems; ++k) {
-      if (h0 + k * step >= heads) continue;
-      uint16_t* const yp = p.y + yo[k];
-      if (!turns) {
-        *reinterpret_cast<uint4*>(yp + off0) = v[k][0];
-        continue;
-      }
-      const float4* const r = reinterpret_cast<const float4*>(rot + tok[k] * p.pairs + 8 * at);
-      float a[8], b[8];
-      unpack8<kF16>(v[k][0], a);
-      unpack8<kF16>(v[k][1], b);
+      if (head + k * u.slots >= head_end) continue;
+      if (turns) {
+        float a[8], b[8];
+        unpack_pairs<kF16, kHalf>(v[k], a, b);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {   // two pairs
-        const float4 c = r[j];
-        if (kHalf) {
-          turn(a[2 * j], b[2 * j], c.x, c.y);
-          turn(a[2 * j + 1], b[2 * j + 1], c.z, c.w);
-        } else if (j < 2) {
-          turn(a[4 * j], a[4 * j + 1], c.x, c.y);
-          turn(a[4 * j + 2], a[4 * j + 3], c.z, c.w);
-        } else {
-          turn(b[4 * j - 8], b[4 * j - 7], c.x, c.y);
-          turn(b[4 * j - 6], b[4 * j - 5], c.z, c.w);
-        }
+        for (int j = 0; j < 4; ++j) turn2(a, b, 2 * j, c[j], sn[j], ns[j]);
+        pack_pairs<kF16, kHalf>(a, b, v[k]);
       }
-      *reinterpret_cast<uint4*>(yp + off0) = pack8<kF16>(a);
-      *reinterpret_cast<uint4*>(yp + off1) = pack8<kF16>(b);
+      if (wide) {
+        stg256(y + off0, v[k][0], v[k][1]);
+      } else {
+        *reinterpret_cast<uint4*>(y + off0) = v[k][0];
+        if (second) *reinterpret_cast<uint4*>(y + off1) = v[k][1];
+      }
+      y += y_step;
     }
+    head += kItems * u.slots;
+    load();
   }
 }
 
 }  // namespace
 
-cudaError_t launch_rope(const qlin_rope_t& a, cudaStream_t s) {
+cudaError_t launch_rope(const qlin_rope_t& a, int num_sms, cudaStream_t s) {
   RopeParams p{};
   p.x = static_cast<const uint16_t*>(a.x);
   p.y = static_cast<uint16_t*>(a.y);
@@ -225,30 +298,47 @@ cudaError_t launch_rope(const qlin_rope_t& a, cudaStream_t s) {
   p.inverse = a.inverse ? 1 : 0;
   p.fp16 = a.dtype == QLIN_FP16 ? 1 : 0;
   // 16-byte accesses: every row starts on a 16-byte boundary, and chunks of eight
-  // elements divide the pairs, the halves and what follows them
-  const bool vec = p.pairs % 8 == 0 && p.head_dim % 8 == 0 &&
+  // elements divide the pairs, the halves and what follows them, a warp's lanes hold a head
+  const int per_head = p.pairs / 8 + (p.x == p.y ? 0 : (p.head_dim - 2 * p.pairs + 15) / 16);
+  const bool vec = p.pairs % 8 == 0 && per_head <= 32 && p.head_dim % 8 == 0 &&
                    ((reinterpret_cast<uintptr_t>(p.x) | reinterpret_cast<uintptr_t>(p.y)) & 15u) == 0 &&
                    ((p.x_token | p.x_head | p.y_token | p.y_head) & 7) == 0;
   if (vec) {
-    const int per_head = p.pairs / 8 + (p.head_dim - 2 * p.pairs) / 8;
-    const int64_t per_token = (int64_t)p.heads * per_head;
-    const int most = 8192 / (p.pairs * (int)sizeof(float2));
-    const int per_cta = (int)std::max<int64_t>(1, std::min<int64_t>({(int64_t)most, 256 / per_token, a.tokens}));
-    // threads: whole heads, kItems of them per thread and round, at most 512 threads
-    const int64_t heads = per_cta * p.heads;
-    const int64_t fit = 512 / per_head;   // per_head <= 128
-    const int64_t rounds = (heads + fit * kItems - 1) / (fit * kItems);
-    const int threads = (int)((heads + rounds * kItems - 1) / (rounds * kItems)) * per_head;
-    const unsigned grid = (unsigned)((a.tokens + per_cta - 1) / per_cta);
-    const int smem = per_cta * p.pairs * (int)sizeof(float2);
-    using Kernel = void (*)(RopeParams, int, int64_t);
-    static constexpr Kernel kKernels[2][2][2] = {
-        {{rope_vec_kernel<false, false, false>, rope_vec_kernel<false, false, true>},
-         {rope_vec_kernel<false, true, false>, rope_vec_kernel<false, true, true>}},
-        {{rope_vec_kernel<true, false, false>, rope_vec_kernel<true, false, true>},
-         {rope_vec_kernel<true, true, false>, rope_vec_kernel<true, true, true>}}};
-    const Kernel kern = kKernels[p.fp16][p.half][per_cta == 1];
-    return launch_pdl(kern, grid, threads, smem, s, p, per_cta, a.tokens);
+    RopeUnits u{};
+    u.per_head = per_head;
+    u.slots = 32 / u.per_head;
+    u.tokens = std::max(1, u.slots / p.heads);
+    const int steps = (p.heads + u.slots - 1) / u.slots;
+    // up to four of them per warp, as far as 16 warps per SM are left
+    const int64_t fill = (a.tokens + u.tokens - 1) / u.tokens * steps / (16 * num_sms);
+    const int most = (int)std::max<int64_t>(1, std::min<int64_t>(fill, kMostItems));
+    const int groups = std::min((steps + most - 1) / most, 65535);
+    const int per_warp = (steps + groups - 1) / groups;
+    u.heads = per_warp * u.slots;
+    u.count = (a.tokens + u.tokens - 1) / u.tokens;
+    auto by = [](int d) { return (uint32_t)(((1 << 20) + d - 1) / d); };
+    u.by_per_head = by(u.per_head);
+    u.by_heads = u.tokens > 1 ? by(p.heads) : 0;
+    u.by_pairs = by(p.pairs);
+    u.wide = ((reinterpret_cast<uintptr_t>(p.x) | reinterpret_cast<uintptr_t>(p.y)) & 31u) == 0 &&
+                     ((p.x_token | p.x_head | p.y_token | p.y_head) & 15) == 0
+                 ? 1
+                 : 0;
+    const unsigned grid = (unsigned)((u.count + kVecWarps - 1) / kVecWarps);
+    const int smem = kVecWarps * u.tokens * p.pairs * (int)sizeof(float2);
+    auto launch = [&](auto kern) {
+      return launch_pdl(kern, dim3(grid, (unsigned)groups), kVecWarps * 32, smem, s, p, u, a.tokens);
+    };
+    auto with_items = [&](auto f16, auto half) {
+      constexpr bool kF16 = decltype(f16)::value, kHalf = decltype(half)::value;
+      return per_warp == 1   ? launch(rope_vec_kernel<kF16, kHalf, 1>)
+             : per_warp == 2 ? launch(rope_vec_kernel<kF16, kHalf, 2>)
+                             : launch(rope_vec_kernel<kF16, kHalf, 4>);
+    };
+    using T = std::true_type;
+    using F = std::false_type;
+    return p.fp16 ? (p.half ? with_items(T{}, T{}) : with_items(T{}, F{}))
+                  : (p.half ? with_items(F{}, T{}) : with_items(F{}, F{}));
   }
   return launch_pdl(rope_kernel, (unsigned)a.tokens, kThreads, 0, s, p);
 }
