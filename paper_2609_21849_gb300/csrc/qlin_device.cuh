@@ -640,37 +640,100 @@ __device__ __forceinline__ void mul2_rn(float& a, float& b, float s) {
       : "f"(a), "f"(b), "f"(s));
 }
 
+// Two packed fp32 operations per instruction, each rounded once.
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 r;
+  asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\t"
+      "mul.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
+      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return r;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 r;
+  asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\t"
+      "add.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
+      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return r;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 r;
+  asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\t"
+      "fma.rn.f32x2 x, x, y, z;\n\tmov.b64 {%0, %1}, x;\n\t}"
+      : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return r;
+}
+
 // ---------------------------------------------------------- activations ---
 
-// v / (1 + exp(-u)): SiLU (u = v) and the tanh form of GELU (0.5 (1 + tanh z) is
-// 1 / (1 + exp(-2 z))).  The quotient is 0 where the exponential overflows.
-__device__ __forceinline__ float times_sigmoid(float v, float u) {
-  return __fdividef(v, 1.0f + __expf(-u));
+// 2^x and 1 / x to two units in the last place, subnormals as zero.
+__device__ __forceinline__ float exp2_fast(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ float rcp_fast(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+
+__device__ __forceinline__ float2 splat(float v) { return make_float2(v, v); }
+
+// v / (1 + 2^e) of two values: v times a logistic function.  0 where 2^e overflows.
+__device__ __forceinline__ float2 over_one_plus_exp2(float2 v, float2 e) {
+  const float2 d = add2(make_float2(exp2_fast(e.x), exp2_fast(e.y)), splat(1.0f));
+  return mul2(v, make_float2(rcp_fast(d.x), rcp_fast(d.y)));
+}
+
+// SiLU: v / (1 + exp(-v)).
+__device__ __forceinline__ float2 silu2(float2 v) {
+  return over_one_plus_exp2(v, mul2(v, splat(-1.442695041f)));   // -log2(e)
+}
+
+// 0.5 v (1 + tanh(z)) = v / (1 + exp(-2 z)), z = sqrt(2 / pi) (v + 0.044715 v^3): the
+// exponent in powers of two is v (c1 + c3 v^2).
+__device__ __forceinline__ float2 gelu_tanh2(float2 v) {
+  const float2 q = fma2(mul2(v, v), splat(-0.1029432397f), splat(-2.302208198f));
+  return over_one_plus_exp2(v, mul2(v, q));
+}
+
+// 0.5 v erfc(-v / sqrt 2) with erfc(z) = (a1 t + ... + a5 t^5) exp(-z^2), t = 1 / (1 +
+// 0.3275911 z) for z >= 0 (Abramowitz and Stegun 7.1.26: erf to 1.5e-7), the
+// coefficients halved.
+__device__ __forceinline__ float2 gelu2(float2 v) {
+  const float2 z = mul2(make_float2(fabsf(v.x), fabsf(v.y)), splat(0.7071067812f));
+  const float2 d = fma2(z, splat(0.3275911f), splat(1.0f));
+  const float2 t = make_float2(rcp_fast(d.x), rcp_fast(d.y));
+  float2 h = fma2(t, splat(0.5307027145f), splat(-0.7265760135f));
+  h = fma2(t, h, splat(0.7107068705f));
+  h = fma2(t, h, splat(-0.142248368f));
+  h = fma2(t, h, splat(0.127414796f));
+  const float2 e = mul2(mul2(z, z), splat(-1.442695041f));
+  h = mul2(mul2(h, t), make_float2(exp2_fast(e.x), exp2_fast(e.y)));
+  const float2 g = make_float2(v.x >= 0.0f ? 1.0f - h.x : h.x, v.y >= 0.0f ? 1.0f - h.y : h.y);
+  return mul2(v, g);
 }
 
 // act (qlin_activation) of every value; the same act in all threads of a warp.
 template <int N>
-__device__ __forceinline__ void activate(float (&v)[N], int act) {
+__device__ __forceinline__ void activate(float2 (&v)[N], int act) {
   switch (act) {
     case 1:
 #pragma unroll
-      for (int i = 0; i < N; ++i) v[i] = v[i] < 0.0f ? 0.0f : v[i];   // (a NaN stays)
+      for (int i = 0; i < N; ++i)   // (a NaN stays)
+        v[i] = make_float2(v[i].x < 0.0f ? 0.0f : v[i].x, v[i].y < 0.0f ? 0.0f : v[i].y);
       break;
     case 2:
 #pragma unroll
-      for (int i = 0; i < N; ++i) v[i] = times_sigmoid(v[i], v[i]);
+      for (int i = 0; i < N; ++i) v[i] = silu2(v[i]);
       break;
     case 3:
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        // 2 sqrt(2 / pi) (v + 0.044715 v^3)
-        const float u = v[i] * __fmaf_rn(0.07135481283f, v[i] * v[i], 1.595769122f);
-        v[i] = times_sigmoid(v[i], u);
-      }
+      for (int i = 0; i < N; ++i) v[i] = gelu_tanh2(v[i]);
       break;
     case 4:
 #pragma unroll
-      for (int i = 0; i < N; ++i) v[i] = 0.5f * v[i] * erfcf(-0.70710678f * v[i]);
+      for (int i = 0; i < N; ++i) v[i] = gelu2(v[i]);
       break;
     default:
       break;

@@ -216,9 +216,9 @@ __global__ void __launch_bounds__(kWarps * 32) few_kernel(const FewParams p) {
       else if constexpr (kKind == Kind::kFp8)
         v = __fmul_rn(v, __fmul_rn(p.sdec_a[p.a_per_row ? m : 0], p.sdec_w[p.w_per_channel ? n : 0]));
       if (p.bias != nullptr) v = __fadd_rn(v, load16f(p.bias + n, kF16));
-      float one[1] = {v};
+      float2 one[1] = {make_float2(v, v)};
       activate(one, p.act);
-      v = one[0];
+      v = one[0].x;
       if (p.residual != nullptr) v = __fadd_rn(v, load16f(p.residual + m * p.residual_stride + n, kF16));
     }
     const uint32_t bits = (kF16 ? pack_f16x2(v, 0.0f) : pack_bf16x2(v, 0.0f)) & 0xFFFFu;

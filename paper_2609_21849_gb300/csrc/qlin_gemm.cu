@@ -212,51 +212,47 @@ __device__ __forceinline__ void st_global_v4_hint(void* p, uint32_t a, uint32_t 
 // ------------------------------------------------- bias, activation, residual ---
 
 template <bool kF16>
-__device__ __forceinline__ void unpack16x2(uint32_t w, float& lo, float& hi) {
-  if constexpr (kF16) {
-    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
-    lo = f.x;
-    hi = f.y;
-  } else {
-    lo = bf16_lo(w);
-    hi = bf16_hi(w);
-  }
+__device__ __forceinline__ float2 unpack16x2(uint32_t w) {
+  if constexpr (kF16)
+    return __half22float2(*reinterpret_cast<const __half2*>(&w));
+  else
+    return make_float2(bf16_lo(w), bf16_hi(w));
 }
 
-// v[i] += 32 16-bit values at p (16-byte aligned).
-template <bool kF16>
-__device__ __forceinline__ void add32(float (&v)[32], const uint16_t* p) {
+// act(v * scale + bias) + residual of 32 columns of one row, as 16-bit pairs.  scale is
+// s_row (NVFP4), s_row * S_W[n] (FP8) or 1.
+template <bool kFp4, bool kBf16, bool kF16>
+__device__ __forceinline__ void finish32(float2 (&v)[16], const KParams& p, float s_row, int64_t row,
+                                         int64_t n0, uint32_t* packed) {
+  const float2 s2 = splat(s_row);
+  if (!kFp4 && !kBf16 && p.w_per_channel) {
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const uint4 w = ld_global_v4(p + 8 * k);
-    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      float lo, hi;
-      unpack16x2<kF16>(u[i], lo, hi);
-      v[8 * k + 2 * i] = __fadd_rn(v[8 * k + 2 * i], lo);
-      v[8 * k + 2 * i + 1] = __fadd_rn(v[8 * k + 2 * i + 1], hi);
+    for (int k = 0; k < 8; ++k) {
+      const float4 sw = __ldg(reinterpret_cast<const float4*>(p.sdec_w + n0) + k);
+      v[2 * k] = mul2(v[2 * k], mul2(s2, make_float2(sw.x, sw.y)));
+      v[2 * k + 1] = mul2(v[2 * k + 1], mul2(s2, make_float2(sw.z, sw.w)));
     }
-  }
-}
-
-// FP8: v[i] *= S_A * S_W[n0 + i]
-__device__ __forceinline__ void scale_columns(float (&v)[32], const KParams& p, float s_a,
-                                              int64_t n0) {
-  const float one = p.w_per_channel ? 0.0f : __ldg(p.sdec_w);
+  } else if (!kBf16) {
+    const float2 s = kFp4 ? s2 : mul2(s2, splat(__ldg(p.sdec_w)));
 #pragma unroll
-  for (int i = 0; i < 32; ++i)
-    v[i] = __fmul_rn(v[i], __fmul_rn(s_a, p.w_per_channel ? __ldg(p.sdec_w + n0 + i) : one));
-}
-
-// act(v + bias) + residual of 32 columns of one row.
-template <bool kF16>
-__device__ __forceinline__ void finish32(float (&v)[32], const KParams& p, int64_t row,
-                                         int64_t n0) {
-  if (p.bias != nullptr) add32<kF16>(v, p.bias + n0);
+    for (int i = 0; i < 16; ++i) v[i] = mul2(v[i], s);
+  }
+  auto add = [&](const uint16_t* src) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const uint4 w = ld_global_v4(src + 8 * k);
+      v[4 * k] = add2(v[4 * k], unpack16x2<kF16>(w.x));
+      v[4 * k + 1] = add2(v[4 * k + 1], unpack16x2<kF16>(w.y));
+      v[4 * k + 2] = add2(v[4 * k + 2], unpack16x2<kF16>(w.z));
+      v[4 * k + 3] = add2(v[4 * k + 3], unpack16x2<kF16>(w.w));
+    }
+  };
+  if (p.bias != nullptr) add(p.bias + n0);
   activate(v, p.act);
-  if (p.residual != nullptr && row < p.M)
-    add32<kF16>(v, p.residual + row * p.residual_stride + n0);
+  if (p.residual != nullptr && row < p.M) add(p.residual + row * p.residual_stride + n0);
+#pragma unroll
+  for (int i = 0; i < 16; ++i)
+    packed[i] = kF16 ? pack_f16x2(v[i].x, v[i].y) : pack_bf16x2(v[i].x, v[i].y);
 }
 
 // kBf16 (with !kFp4): bf16 operands on the FP8 skeleton (the same 128-byte
@@ -837,10 +833,11 @@ __global__ void __launch_bounds__(Cfg<kFp4, kBN, kPair>::kThreads, 1)
       // chunk c (32 columns) of this thread starts at column ccol(c)
       const int64_t col0 = (int64_t)nb * kBN + half * kCols;
       auto ccol = [&](int c) -> int64_t { return col0 + c * 32; };
-      const float row_scale = !kEpi || kFp4 || kBf16 ? 1.0f
-                              : !p.a_per_row         ? sdec_a
-                              : row < p.M            ? __ldg(p.sdec_a + row)
-                                                     : 0.0f;
+      const float row_scale = !kEpi || kBf16 ? 1.0f
+                              : kFp4         ? alpha
+                              : !p.a_per_row ? sdec_a
+                              : row < p.M    ? __ldg(p.sdec_a + row)
+                                             : 0.0f;
       uint32_t packed[kCols / 2];
       const uint32_t taddr =
           tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(acc * kBN + half * kCols);
@@ -876,28 +873,16 @@ __global__ void __launch_bounds__(Cfg<kFp4, kBN, kPair>::kThreads, 1)
         for (int b = 0; b < kBatch; ++b) {
           const int c = cb + b;
           if constexpr (kEpi) {
-            float v[32];
+            float2 v[16];
             const int64_t n0 = ccol(c);
 #pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[b][i]);
+            for (int i = 0; i < 16; ++i)
+              v[i] = make_float2(__uint_as_float(r[b][2 * i]), __uint_as_float(r[b][2 * i + 1]));
             if (n0 < p.N) {
-              if (kFp4) {
-#pragma unroll
-                for (int i = 0; i < 32; ++i) v[i] = __fmul_rn(v[i], alpha);
-              } else if (!kBf16) {
-                scale_columns(v, p, row_scale, n0);
-              }
               if (kBf16 && p.fp16)
-                finish32<true>(v, p, row, n0);
+                finish32<kFp4, kBf16, true>(v, p, row_scale, row, n0, packed + c * 16);
               else
-                finish32<false>(v, p, row, n0);
-            }
-            if (kBf16 && p.fp16) {
-#pragma unroll
-              for (int i = 0; i < 16; ++i) packed[c * 16 + i] = pack_f16x2(v[2 * i], v[2 * i + 1]);
-            } else {
-#pragma unroll
-              for (int i = 0; i < 16; ++i) packed[c * 16 + i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
+                finish32<kFp4, kBf16, false>(v, p, row_scale, row, n0, packed + c * 16);
             }
             continue;
           }
