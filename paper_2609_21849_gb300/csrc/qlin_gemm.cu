@@ -56,7 +56,10 @@ constexpr int pow2_at_least(int x) {
 
 // kPair: a CTA pair runs one tcgen05 MMA of M = 256 (cta_group::2); each CTA
 // holds its own 128 rows of A and its own half of the W tile.
-template <bool kFp4, int kBN, bool kPair = false>
+// kHold: the epilogue's warps hold a whole accumulator in registers (setmaxnreg), so
+// that the one accumulator of an NVFP4 pair goes back to the MMAs before the
+// activations: two warpgroups of roles, then two of epilogue.
+template <bool kFp4, int kBN, bool kPair = false, bool kHold = false>
 struct Cfg {
   // warps: 0 producer, 1 MMA, NVFP4: four scale warps, pairs: the scale
   // producer, then the epilogue (an epilogue or scale warp w reaches TMEM
@@ -65,7 +68,8 @@ struct Cfg {
   static constexpr int kSfWarps = kFp4 ? 4 : 0;
   static constexpr bool kSfCopy = kFp4 && kPair;   // scales by TMA and tcgen05.cp
   static constexpr int kSfProducer = kSfCopy ? 2 + kSfWarps : -1;
-  static constexpr int kEpiWarp0 = 2 + kSfWarps + (kSfCopy ? 1 : 0);
+  static constexpr int kRoleWarps = 2 + kSfWarps + (kSfCopy ? 1 : 0);
+  static constexpr int kEpiWarp0 = kHold ? 8 : kRoleWarps;
   static constexpr int kEpiWarps = 8;
   static constexpr int kThreads = (kEpiWarp0 + kEpiWarps) * 32;
   // Row boxes per operand tile and stage: copies of separate boxes overlap
@@ -118,6 +122,9 @@ struct Cfg {
   static_assert(kTmemCols <= 512, "TMEM budget");
   static_assert(kSmemBytes <= 232448, "shared memory budget");
   static_assert(kStages >= 2, "pipeline depth");
+  // (512 threads at 128 registers; the shares add up to all 65,536)
+  static constexpr int kRoleRegs = 56, kHoldRegs = 200;
+  static_assert(!kHold || (kThreads == 512 && 256 * (kRoleRegs + kHoldRegs) == 65536), "registers");
 };
 
 struct KParams {
@@ -147,6 +154,7 @@ struct KParams {
   int64_t residual_stride;
   int act;
   int a_per_row;
+  int r_v8;           // residual rows start on 32-byte boundaries
 };
 
 // Coordinates of cluster tile ct, its M tile group and its N tile: M fastest
@@ -219,11 +227,32 @@ __device__ __forceinline__ float2 unpack16x2(uint32_t w) {
     return make_float2(bf16_lo(w), bf16_hi(w));
 }
 
+// 32 columns (64 bytes) of a residual's row.
+__device__ __forceinline__ void load_residual(uint32_t (&r)[16], const uint16_t* p, bool aligned32) {
+  if (aligned32) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                   : "=r"(r[8 * h]), "=r"(r[8 * h + 1]), "=r"(r[8 * h + 2]), "=r"(r[8 * h + 3]),
+                     "=r"(r[8 * h + 4]), "=r"(r[8 * h + 5]), "=r"(r[8 * h + 6]), "=r"(r[8 * h + 7])
+                   : "l"(p + 16 * h));
+  } else {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const uint4 w = ld_global_v4(p + 8 * k);
+      r[4 * k] = w.x;
+      r[4 * k + 1] = w.y;
+      r[4 * k + 2] = w.z;
+      r[4 * k + 3] = w.w;
+    }
+  }
+}
+
 // act(v * scale + bias) + residual of 32 columns of one row, as 16-bit pairs.  scale is
 // s_row (NVFP4), s_row * S_W[n] (FP8) or 1.
 template <bool kFp4, bool kBf16, bool kF16>
-__device__ __forceinline__ void finish32(float2 (&v)[16], const KParams& p, float s_row, int64_t row,
-                                         int64_t n0, uint32_t* packed) {
+__device__ __forceinline__ void finish32(float2 (&v)[16], const KParams& p, float s_row,
+                                         int64_t n0, const uint32_t (&res)[16], uint32_t* packed) {
   const float2 s2 = splat(s_row);
   if (!kFp4 && !kBf16 && p.w_per_channel) {
 #pragma unroll
@@ -237,19 +266,21 @@ __device__ __forceinline__ void finish32(float2 (&v)[16], const KParams& p, floa
 #pragma unroll
     for (int i = 0; i < 16; ++i) v[i] = mul2(v[i], s);
   }
-  auto add = [&](const uint16_t* src) {
+  if (p.bias != nullptr) {
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      const uint4 w = ld_global_v4(src + 8 * k);
+      const uint4 w = __ldg(reinterpret_cast<const uint4*>(p.bias + n0) + k);
       v[4 * k] = add2(v[4 * k], unpack16x2<kF16>(w.x));
       v[4 * k + 1] = add2(v[4 * k + 1], unpack16x2<kF16>(w.y));
       v[4 * k + 2] = add2(v[4 * k + 2], unpack16x2<kF16>(w.z));
       v[4 * k + 3] = add2(v[4 * k + 3], unpack16x2<kF16>(w.w));
     }
-  };
-  if (p.bias != nullptr) add(p.bias + n0);
+  }
   activate(v, p.act);
-  if (p.residual != nullptr && row < p.M) add(p.residual + row * p.residual_stride + n0);
+  if (p.residual != nullptr) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = add2(v[i], unpack16x2<kF16>(res[i]));
+  }
 #pragma unroll
   for (int i = 0; i < 16; ++i)
     packed[i] = kF16 ? pack_f16x2(v[i].x, v[i].y) : pack_bf16x2(v[i].x, v[i].y);
@@ -260,13 +291,14 @@ __device__ __forceinline__ void finish32(float2 (&v)[16], const KParams& p, floa
 // kEpi: the epilogue of qlin_linear_*: bias, activation and residual before the
 // 16-bit rounding, FP8 row scales of A.
 template <bool kFp4, int kBN, bool kPair, bool kRequant, bool kBf16 = false, bool kEpi = false>
-__global__ void __launch_bounds__(Cfg<kFp4, kBN, kPair>::kThreads, 1)
+__global__ void __launch_bounds__(Cfg<kFp4, kBN, kPair, kEpi && kFp4 && kPair>::kThreads, 1)
     gemm_kernel(const __grid_constant__ CUtensorMap tmap_a,
                 const __grid_constant__ CUtensorMap tmap_b,
                 const __grid_constant__ CUtensorMap tmap_sfa,
                 const __grid_constant__ CUtensorMap tmap_sfb,
                 const __grid_constant__ CUtensorMap tmap_y, const KParams p) {
-  using C = Cfg<kFp4, kBN, kPair>;
+  constexpr bool kHold = kEpi && kFp4 && kPair;
+  using C = Cfg<kFp4, kBN, kPair, kHold>;
   constexpr int kCM = kPair ? 2 : 1;          // CTAs per cluster (M tiles per cluster tile)
   constexpr uint16_t kMask = (uint16_t)((1u << kCM) - 1u);
   extern __shared__ uint8_t smem_raw[];
@@ -360,6 +392,7 @@ __global__ void __launch_bounds__(Cfg<kFp4, kBN, kPair>::kThreads, 1)
   // the prologue above overlaps the previous kernel; global data only below
   grid_dep_wait();
 
+  auto run_role = [&] {
   if (warp == 0) {
     // ------------------------------------------------------ TMA producer ---
     // One elected lane issues a stage's A and W boxes (kSplit row boxes each).
@@ -632,7 +665,7 @@ __global__ void __launch_bounds__(Cfg<kFp4, kBN, kPair>::kThreads, 1)
         mbar_drain(&sf_full[slot], phase, p.timeout_ns, p.err);
       }
     }
-  } else if (C::kSfCopy && warp < C::kEpiWarp0) {
+  } else if (C::kSfCopy && warp < C::kRoleWarps) {
     // ------------------------------------- NVFP4 scale copies (pairs) ---
     // Block scales move shared -> TMEM beside the MMA stream, the stages in
     // turn to the four scale warps: a tcgen05.cp occupies its issuing thread
@@ -699,7 +732,7 @@ __global__ void __launch_bounds__(Cfg<kFp4, kBN, kPair>::kThreads, 1)
         mbar_drain(&sf_done[sw], 0, p.timeout_ns, p.err);
       }
     }
-  } else if (warp < C::kEpiWarp0) {
+  } else if (warp < C::kRoleWarps) {
     // ------------------------------ NVFP4 scale warps (single-CTA tiles) ---
     // Block scales go from global memory through registers into TMEM
     // (tcgen05.st): lane l of the warp of each lane quarter takes the 16 bytes
@@ -786,7 +819,9 @@ __global__ void __launch_bounds__(Cfg<kFp4, kBN, kPair>::kThreads, 1)
         load_next(v1);
       }
     }
-  } else {
+  }
+  };
+  auto run_epilogue = [&] {
     // --------------------------------------------------------- epilogue ---
     constexpr int kCols = kBN / (C::kEpiWarps / 4);  // columns per thread
     constexpr int kChunks = kCols / 32;
@@ -826,165 +861,87 @@ __global__ void __launch_bounds__(Cfg<kFp4, kBN, kPair>::kThreads, 1)
         if (lane < kCols / 32 && cl < p.N)
           asm volatile("prefetch.global.L1 [%0];" ::"l"(p.sdec_w + cl));
       }
-      if (!mbar_wait(&tmem_full[acc], acc_phase, ctl)) break;
-      tc_fence_after();
       const int mb = mg * kCM + rank;
       const int64_t row = (int64_t)mb * kBM + quarter * 32 + lane;
       // chunk c (32 columns) of this thread starts at column ccol(c)
       const int64_t col0 = (int64_t)nb * kBN + half * kCols;
       auto ccol = [&](int c) -> int64_t { return col0 + c * 32; };
+      // kEpi: the residual is loaded a chunk ahead of its use, the first one while the
+      // accumulator is still being computed
+      uint32_t res[kEpi ? 16 : 1];
+      const bool has_res = kEpi && p.residual != nullptr && row < p.M;
+      const uint16_t* const res_row = has_res ? p.residual + row * p.residual_stride : nullptr;
+      if constexpr (kEpi) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) res[i] = 0u;
+        if (has_res && ccol(0) < p.N) load_residual(res, res_row + ccol(0), p.r_v8 != 0);
+      }
+      if (!mbar_wait(&tmem_full[acc], acc_phase, ctl)) break;
+      tc_fence_after();
       const float row_scale = !kEpi || kBf16 ? 1.0f
                               : kFp4         ? alpha
                               : !p.a_per_row ? sdec_a
                               : row < p.M    ? __ldg(p.sdec_a + row)
                                              : 0.0f;
-      uint32_t packed[kCols / 2];
       const uint32_t taddr =
           tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(acc * kBN + half * kCols);
-      // Accumulator columns in batches of tcgen05.ld per wait; TMEM goes back
-      // to the MMA issuer right after the last batch has landed in registers.
-      // (Sixteen epilogue warps of 64 columns each, so one batch, measured
-      // 1-2% slower: 56.1 against 54.8 us on 4608 x 12288 x 3072 NVFP4.)
-      constexpr int kBatch = kChunks < 2 ? kChunks : 2;
-      static_assert(kChunks % kBatch == 0, "TMEM is released after the last batch");
-#pragma unroll
-      for (int cb = 0; cb < kChunks; cb += kBatch) {
-        uint32_t r[kBatch][32];
-#pragma unroll
-        for (int b = 0; b < kBatch; ++b) tmem_ld32(taddr + (cb + b) * 32, r[b]);
-        tmem_ld_wait();
-        if (cb + kBatch == kChunks) {
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) {
-            if (kPair && rank == 1)
-              mbar_arrive_cluster(mapa_shared(&tmem_empty[acc], 0));   // the leader owns the MMA
-            else
-              mbar_arrive(&tmem_empty[acc]);
-          }
-          if (C::kNumAcc == 2) {
-            acc ^= 1;
-            if (acc == 0) acc_phase ^= 1u;
-          } else {
-            acc_phase ^= 1u;
-          }
+      // TMEM goes back to the MMA issuer
+      auto release = [&] {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          if (kPair && rank == 1)
+            mbar_arrive_cluster(mapa_shared(&tmem_empty[acc], 0));   // the leader owns the MMA
+          else
+            mbar_arrive(&tmem_empty[acc]);
         }
+        if (C::kNumAcc == 2) {
+          acc ^= 1;
+          if (acc == 0) acc_phase ^= 1u;
+        } else {
+          acc_phase ^= 1u;
+        }
+      };
+      // 16-bit output of chunk c from its packed pairs
+      const bool keep = !kEpi && p.y_amax != nullptr;
+      const uint64_t pol = C::kDirectStore && keep ? policy_evict_last() : 0ull;
+      auto store_y = [&](int c, const uint32_t* pk) {
+        if constexpr (C::kDirectStore) {
+          // straight from registers: the thread's row, 64 bytes; N % 64 == 0, so a
+          // chunk is wholly inside or outside the matrix.  With an output amax (the
+          // dynamic chain), y is read back right after this kernel by the quantizer:
+          // keep it in L2 if it can.
+          if (p.y == nullptr || row >= p.M || ccol(c) >= p.N) return;
+          uint32_t* const dst = reinterpret_cast<uint32_t*>(p.y + row * p.N + ccol(c));
+          if (p.y_v8) {
+            if (keep) {
+              st_global_v8_hint(dst, pk, pol);
+              st_global_v8_hint(dst + 8, pk + 8, pol);
+            } else {
+              st_global_v8(dst, pk);
+              st_global_v8(dst + 8, pk + 8);
+            }
+          } else {
 #pragma unroll
-        for (int b = 0; b < kBatch; ++b) {
-          const int c = cb + b;
-          if constexpr (kEpi) {
-            float2 v[16];
-            const int64_t n0 = ccol(c);
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-              v[i] = make_float2(__uint_as_float(r[b][2 * i]), __uint_as_float(r[b][2 * i + 1]));
-            if (n0 < p.N) {
-              if (kBf16 && p.fp16)
-                finish32<kFp4, kBf16, true>(v, p, row_scale, row, n0, packed + c * 16);
+            for (int k = 0; k < 4; ++k) {
+              if (keep)
+                st_global_v4_hint(dst + 4 * k, pk[4 * k], pk[4 * k + 1], pk[4 * k + 2], pk[4 * k + 3],
+                                  pol);
               else
-                finish32<kFp4, kBf16, false>(v, p, row_scale, row, n0, packed + c * 16);
-            }
-            continue;
-          }
-          float a[32];
-          if (kFp4 || kBf16) {
-#pragma unroll
-            for (int i = 0; i < 32; ++i) a[i] = alpha;
-          } else {
-            const int64_t n0 = ccol(c);
-            if (p.w_per_channel && n0 < p.N) {
-              const float4* sw = reinterpret_cast<const float4*>(p.sdec_w + n0);
-#pragma unroll
-              for (int i = 0; i < 8; ++i) {
-                const float4 v = __ldg(sw + i);
-                a[4 * i] = __fmul_rn(sdec_a, v.x);
-                a[4 * i + 1] = __fmul_rn(sdec_a, v.y);
-                a[4 * i + 2] = __fmul_rn(sdec_a, v.z);
-                a[4 * i + 3] = __fmul_rn(sdec_a, v.w);
-              }
-            } else {
-              const float a0 = p.w_per_channel ? 0.0f : __fmul_rn(sdec_a, *p.sdec_w);
-#pragma unroll
-              for (int i = 0; i < 32; ++i) a[i] = a0;
+                st_global_v4(dst + 4 * k, pk[4 * k], pk[4 * k + 1], pk[4 * k + 2], pk[4 * k + 3]);
             }
           }
-          if (kBf16 && p.fp16) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-              packed[c * 16 + i] = pack_f16x2(__uint_as_float(r[b][2 * i]),
-                                              __uint_as_float(r[b][2 * i + 1]));
-          } else {
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-              packed[c * 16 + i] =
-                  pack_bf16x2(__fmul_rn(__uint_as_float(r[b][2 * i]), a[2 * i]),
-                              __fmul_rn(__uint_as_float(r[b][2 * i + 1]), a[2 * i + 1]));
-          }
-        }
-      }
-
-      if (p.y_amax != nullptr) {
-        // the output's tensor amax (for a dynamic scale of the next layer's
-        // input): max over this thread's bf16 values, then the warp, then
-        // one atomic per warp.  Rows past M and columns past N hold zeros
-        // (zero-filled operands), which leave the maximum unchanged.
-        uint32_t m = 0;
-#pragma unroll
-        for (int i = 0; i < kCols / 2; ++i) m = __vmaxu2(m, packed[i] & 0x7FFF7FFFu);
-        m = max(m & 0xFFFFu, m >> 16);
-        m = __reduce_max_sync(0xFFFFFFFFu, m);
-        if (lane == 0 && m != 0u) atomicMax(p.y_amax, m << 16);
-      }
-      if constexpr (C::kDirectStore) {
-        // 16-bit output straight from registers: the thread's row, 32
-        // columns (64 bytes) per chunk; N % 64 == 0, so a chunk is wholly
-        // inside or outside the matrix
-        if (p.y != nullptr && row < p.M) {
-          uint16_t* const yrow = p.y + row * p.N;
-          // With an output amax (the dynamic chain), y is read back right
-          // after this kernel by the quantizer: keep it in L2 if it can.
-          const bool keep = p.y_amax != nullptr;
-          const uint64_t pol = keep ? policy_evict_last() : 0ull;
-#pragma unroll
-          for (int c = 0; c < kChunks; ++c) {
-            if (ccol(c) >= p.N) continue;
-            uint32_t* const dst = reinterpret_cast<uint32_t*>(yrow + ccol(c));
-            if (p.y_v8) {
-              if (keep) {
-                st_global_v8_hint(dst, &packed[c * 16], pol);
-                st_global_v8_hint(dst + 8, &packed[c * 16 + 8], pol);
-              } else {
-                st_global_v8(dst, &packed[c * 16]);
-                st_global_v8(dst + 8, &packed[c * 16 + 8]);
-              }
-            } else {
-#pragma unroll
-              for (int k = 0; k < 4; ++k) {
-                if (keep)
-                  st_global_v4_hint(dst + 4 * k, packed[c * 16 + 4 * k], packed[c * 16 + 4 * k + 1],
-                                    packed[c * 16 + 4 * k + 2], packed[c * 16 + 4 * k + 3], pol);
-                else
-                  st_global_v4(dst + 4 * k, packed[c * 16 + 4 * k], packed[c * 16 + 4 * k + 1],
-                               packed[c * 16 + 4 * k + 2], packed[c * 16 + 4 * k + 3]);
-              }
-            }
-          }
-        }
-      } else if (p.y != nullptr) {
-        // bf16 output: each 32 x 32 box goes through a 64-byte-swizzled
-        // staging buffer and one TMA store (rows >= M, cols >= N are clipped).
-        uint8_t* const out_buf = out_stage + e * 4096;   // this warp's two staging boxes
-#pragma unroll
-        for (int c = 0; c < kChunks; ++c) {
-          uint8_t* const bufp = out_buf + (c & 1) * 2048;
+        } else if (p.y != nullptr) {
+          // each 32 x 32 box goes through a 64-byte-swizzled staging buffer and one
+          // TMA store (rows >= M, cols >= N are clipped)
+          uint8_t* const bufp = out_stage + e * 4096 + (c & 1) * 2048;   // of this warp's two
           const uint32_t buf = smem_u32(bufp);
           if (lane == 0) bulk_wait_group_read<1>();   // this buffer's last store has read it
           __syncwarp();
 #pragma unroll
           for (int k = 0; k < 4; ++k)
-            st_shared_v4(buf + lane * 64 + ((k ^ ((lane >> 1) & 3)) << 4), packed[c * 16 + 4 * k],
-                         packed[c * 16 + 4 * k + 1], packed[c * 16 + 4 * k + 2],
-                         packed[c * 16 + 4 * k + 3]);
+            st_shared_v4(buf + lane * 64 + ((k ^ ((lane >> 1) & 3)) << 4), pk[4 * k], pk[4 * k + 1],
+                         pk[4 * k + 2], pk[4 * k + 3]);
           fence_proxy_async_smem();
           __syncwarp();
           if (lane == 0) {
@@ -992,79 +949,182 @@ __global__ void __launch_bounds__(Cfg<kFp4, kBN, kPair>::kThreads, 1)
             bulk_commit_group();
           }
         }
-      }
-      if (row < p.M) {
-        if (kRequant && !kFp4) {
-          // FP8 re-quantization with the static next-layer scale: E4M3 of
-          // bf16(y) * S_enc per element, 64 columns per group
+      };
+      // The re-quantized columns of chunks 2 g and 2 g + 1 (64 columns)
+      auto requant = [&](int g, const uint32_t* pk64) {
+        const int64_t c64 = ccol(2 * g);
+        if (row >= p.M || c64 < p.rq_col0 || c64 + 64 > p.rq_col0 + p.rq_cols || c64 >= p.N) return;
+        if constexpr (kRequant && !kFp4) {
+          // FP8 with the static next-layer scale: E4M3 of bf16(y) * S_enc
+          uint8_t* cp = p.rq_codes + row * p.rq_cols + (c64 - p.rq_col0);
 #pragma unroll
-          for (int g = 0; g < kCols / 64; ++g) {
-            const int64_t c64 = ccol(2 * g);   // chunks 2g, 2g + 1: 64 contiguous columns
-            if (c64 < p.rq_col0 || c64 + 64 > p.rq_col0 + p.rq_cols || c64 >= p.N) continue;
-            uint8_t* cp = p.rq_codes + row * p.rq_cols + (c64 - p.rq_col0);
+          for (int q2 = 0; q2 < 2; ++q2) {   // 32 columns per 32-byte store (or two 16-byte)
+            uint32_t w8[8];
 #pragma unroll
-            for (int q2 = 0; q2 < 2; ++q2) {   // 32 columns per 32-byte store (or two 16-byte)
-              uint32_t w8[8];
+            for (int h = 0; h < 2; ++h) {
+              const uint32_t* pk = pk64 + (2 * q2 + h) * 8;
 #pragma unroll
-              for (int h = 0; h < 2; ++h) {
-                const uint32_t* pk = packed + g * 32 + (2 * q2 + h) * 8;
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                  w8[4 * h + i] = e4m3x4(__fmul_rn(bf16_lo(pk[2 * i]), s_enc_next),
-                                         __fmul_rn(bf16_hi(pk[2 * i]), s_enc_next),
-                                         __fmul_rn(bf16_lo(pk[2 * i + 1]), s_enc_next),
-                                         __fmul_rn(bf16_hi(pk[2 * i + 1]), s_enc_next));
-              }
-              if (p.rq_v8) {
-                st_global_v8(cp + 32 * q2, w8);
-              } else {
-                st_global_v4(cp + 32 * q2, w8[0], w8[1], w8[2], w8[3]);
-                st_global_v4(cp + 32 * q2 + 16, w8[4], w8[5], w8[6], w8[7]);
-              }
+              for (int i = 0; i < 4; ++i)
+                w8[4 * h + i] = e4m3x4(__fmul_rn(bf16_lo(pk[2 * i]), s_enc_next),
+                                       __fmul_rn(bf16_hi(pk[2 * i]), s_enc_next),
+                                       __fmul_rn(bf16_lo(pk[2 * i + 1]), s_enc_next),
+                                       __fmul_rn(bf16_hi(pk[2 * i + 1]), s_enc_next));
+            }
+            if (p.rq_v8) {
+              st_global_v8(cp + 32 * q2, w8);
+            } else {
+              st_global_v4(cp + 32 * q2, w8[0], w8[1], w8[2], w8[3]);
+              st_global_v4(cp + 32 * q2 + 16, w8[4], w8[5], w8[6], w8[7]);
             }
           }
         }
-        if (kRequant && kFp4) {
+        if constexpr (kRequant && kFp4) {
+          const int64_t lc = c64 - p.rq_col0;
+          uint32_t words[8];
+          uint32_t sw = 0;
 #pragma unroll
-          for (int g = 0; g < kCols / 64; ++g) {
-            const int64_t c64 = ccol(2 * g);   // chunks 2g, 2g + 1: 64 contiguous columns
-            if (c64 < p.rq_col0 || c64 + 64 > p.rq_col0 + p.rq_cols || c64 >= p.N) continue;
-            const int64_t lc = c64 - p.rq_col0;
-            uint32_t words[8];
-            uint32_t sw = 0;
+          for (int b = 0; b < 4; ++b) {
+            const uint32_t* pk = pk64 + b * 8;  // 16 bf16 of this block
+            uint32_t m = 0;
 #pragma unroll
-            for (int b = 0; b < 4; ++b) {
-              const uint32_t* pk = packed + g * 32 + b * 8;  // 16 bf16 of this block
-              uint32_t m = 0;
+            for (int i = 0; i < 8; ++i) m = __vmaxu2(m, pk[i] & 0x7FFF7FFFu);
+            m = max(m & 0xFFFFu, m >> 16);
+            const uint32_t sb = e4m3_code_div6(__fmul_rn(__uint_as_float(m << 16), s_enc_next));
+            const float r_b = r_table[sb];
+            sw |= sb << (8 * b);
 #pragma unroll
-              for (int i = 0; i < 8; ++i) m = __vmaxu2(m, pk[i] & 0x7FFF7FFFu);
-              m = max(m & 0xFFFFu, m >> 16);
-              const uint32_t sb = e4m3_code_div6(__fmul_rn(__uint_as_float(m << 16), s_enc_next));
-              const float r_b = r_table[sb];
-              sw |= sb << (8 * b);
+            for (int h8 = 0; h8 < 2; ++h8) {
+              float f[8];
 #pragma unroll
-              for (int h8 = 0; h8 < 2; ++h8) {
-                float f[8];
+              for (int i = 0; i < 4; ++i) {
+                f[2 * i] = bf16_lo(pk[h8 * 4 + i]);
+                f[2 * i + 1] = bf16_hi(pk[h8 * 4 + i]);
+                mul2_rn(f[2 * i], f[2 * i + 1], r_b);
+              }
+              words[b * 2 + h8] = e2m1x8(f);
+            }
+          }
+          uint8_t* cp = p.rq_codes + row * (p.rq_cols / 2) + lc / 2;
+          // the group's 32 bytes of codes: one store where aligned (each
+          // store instruction of the epilogue slows the mainloop beside it)
+          if (p.rq_v8) {
+            st_global_v8(cp, words);
+          } else {
+            st_global_v4(cp, words[0], words[1], words[2], words[3]);
+            st_global_v4(cp + 16, words[4], words[5], words[6], words[7]);
+          }
+          *reinterpret_cast<uint32_t*>(p.rq_scales + scale_offset(row, lc / 16, p.rq_cols)) = sw;
+        }
+      };
+      if constexpr (kEpi) {
+        // kHold: all columns into registers, then TMEM is free; else 64 at a time.
+        constexpr int kBatch = kHold || kChunks < 2 ? kChunks : 2;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                  f[2 * i] = bf16_lo(pk[h8 * 4 + i]);
-                  f[2 * i + 1] = bf16_hi(pk[h8 * 4 + i]);
-                  mul2_rn(f[2 * i], f[2 * i + 1], r_b);
+        for (int cb = 0; cb < kChunks; cb += kBatch) {
+          uint32_t r[kBatch][32];
+#pragma unroll
+          for (int b = 0; b < kBatch; ++b) tmem_ld32(taddr + (cb + b) * 32, r[b]);
+          tmem_ld_wait();
+#pragma unroll
+          for (int b = 0; b < kBatch; ++b)
+#pragma unroll
+            for (int i = 0; i < 32; ++i) asm volatile("" : "+r"(r[b][i]));   // read after the wait
+          if (cb + kBatch == kChunks) release();
+          uint32_t packed[32];   // of the chunk and, where it is odd, the one before
+#pragma unroll
+          for (int b = 0; b < kBatch; ++b) {
+            const int c = cb + b;
+            const int64_t n0 = ccol(c);
+            uint32_t cur[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) cur[i] = res[i];
+            if (c + 1 < kChunks && has_res && ccol(c + 1) < p.N)
+              load_residual(res, res_row + ccol(c + 1), p.r_v8 != 0);
+            uint32_t* const pk = packed + (b & 1) * 16;
+            if (n0 >= p.N) continue;   // (an even chunk and the next one are both in or out)
+            float2 v[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              v[i] = make_float2(__uint_as_float(r[b][2 * i]), __uint_as_float(r[b][2 * i + 1]));
+            if (kBf16 && p.fp16)
+              finish32<kFp4, kBf16, true>(v, p, row_scale, n0, cur, pk);
+            else
+              finish32<kFp4, kBf16, false>(v, p, row_scale, n0, cur, pk);
+            store_y(c, pk);
+            if (kRequant && (b & 1) == 1) requant(c / 2, packed);
+          }
+        }
+      } else {
+        uint32_t packed[kCols / 2];
+        // Accumulator columns in batches of tcgen05.ld per wait; TMEM goes back
+        // to the MMA issuer right after the last batch has landed in registers.
+        // (Sixteen epilogue warps of 64 columns each, so one batch, measured
+        // 1-2% slower: 56.1 against 54.8 us on 4608 x 12288 x 3072 NVFP4.)
+        constexpr int kBatch = kChunks < 2 ? kChunks : 2;
+        static_assert(kChunks % kBatch == 0, "TMEM is released after the last batch");
+#pragma unroll
+        for (int cb = 0; cb < kChunks; cb += kBatch) {
+          uint32_t r[kBatch][32];
+#pragma unroll
+          for (int b = 0; b < kBatch; ++b) tmem_ld32(taddr + (cb + b) * 32, r[b]);
+          tmem_ld_wait();
+          if (cb + kBatch == kChunks) release();
+#pragma unroll
+          for (int b = 0; b < kBatch; ++b) {
+            const int c = cb + b;
+            float a[32];
+            if (kFp4 || kBf16) {
+#pragma unroll
+              for (int i = 0; i < 32; ++i) a[i] = alpha;
+            } else {
+              const int64_t n0 = ccol(c);
+              if (p.w_per_channel && n0 < p.N) {
+                const float4* sw = reinterpret_cast<const float4*>(p.sdec_w + n0);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                  const float4 v = __ldg(sw + i);
+                  a[4 * i] = __fmul_rn(sdec_a, v.x);
+                  a[4 * i + 1] = __fmul_rn(sdec_a, v.y);
+                  a[4 * i + 2] = __fmul_rn(sdec_a, v.z);
+                  a[4 * i + 3] = __fmul_rn(sdec_a, v.w);
                 }
-                words[b * 2 + h8] = e2m1x8(f);
+              } else {
+                const float a0 = p.w_per_channel ? 0.0f : __fmul_rn(sdec_a, *p.sdec_w);
+#pragma unroll
+                for (int i = 0; i < 32; ++i) a[i] = a0;
               }
             }
-            uint8_t* cp = p.rq_codes + row * (p.rq_cols / 2) + lc / 2;
-            // the group's 32 bytes of codes: one store where aligned (each
-            // store instruction of the epilogue slows the mainloop beside it)
-            if (p.rq_v8) {
-              st_global_v8(cp, words);
+            if (kBf16 && p.fp16) {
+#pragma unroll
+              for (int i = 0; i < 16; ++i)
+                packed[c * 16 + i] = pack_f16x2(__uint_as_float(r[b][2 * i]),
+                                                __uint_as_float(r[b][2 * i + 1]));
             } else {
-              st_global_v4(cp, words[0], words[1], words[2], words[3]);
-              st_global_v4(cp + 16, words[4], words[5], words[6], words[7]);
+#pragma unroll
+              for (int i = 0; i < 16; ++i)
+                packed[c * 16 + i] =
+                    pack_bf16x2(__fmul_rn(__uint_as_float(r[b][2 * i]), a[2 * i]),
+                                __fmul_rn(__uint_as_float(r[b][2 * i + 1]), a[2 * i + 1]));
             }
-            *reinterpret_cast<uint32_t*>(p.rq_scales + scale_offset(row, lc / 16, p.rq_cols)) = sw;
           }
+        }
+        if (p.y_amax != nullptr) {
+          // the output's tensor amax (for a dynamic scale of the next layer's
+          // input): max over this thread's bf16 values, then the warp, then
+          // one atomic per warp.  Rows past M and columns past N hold zeros
+          // (zero-filled operands), which leave the maximum unchanged.
+          uint32_t m = 0;
+#pragma unroll
+          for (int i = 0; i < kCols / 2; ++i) m = __vmaxu2(m, packed[i] & 0x7FFF7FFFu);
+          m = max(m & 0xFFFFu, m >> 16);
+          m = __reduce_max_sync(0xFFFFFFFFu, m);
+          if (lane == 0 && m != 0u) atomicMax(p.y_amax, m << 16);
+        }
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) store_y(c, packed + c * 16);
+        if constexpr (kRequant) {
+#pragma unroll
+          for (int g = 0; g < kCols / 64; ++g) requant(g, packed + g * 32);
         }
       }
     }
@@ -1091,6 +1151,14 @@ __global__ void __launch_bounds__(Cfg<kFp4, kBN, kPair>::kThreads, 1)
         }
       }
     }
+  };
+  // (kHold: each warpgroup executes one setmaxnreg, at the head of all it does after)
+  if (warp >= C::kEpiWarp0) {
+    if constexpr (kHold) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::kHoldRegs));
+    run_epilogue();
+  } else {
+    if constexpr (kHold) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kRoleRegs));
+    run_role();
   }
 
   // No CTA of the cluster may exit while a peer can still multicast into it
@@ -1191,7 +1259,7 @@ CUresult encode_scales(CUtensorMap* map, const void* base, uint64_t rows, uint64
 template <bool kFp4, int kBN, bool kPair, bool kRequant, bool kBf16 = false, bool kEpi = false>
 cudaError_t launch_cfg(const GemmArgs& a, cudaStream_t s, Device dev, unsigned* err,
                        uint64_t timeout_ns) {
-  using C = Cfg<kFp4, kBN, kPair>;
+  using C = Cfg<kFp4, kBN, kPair, kEpi && kFp4 && kPair>;
   constexpr int kCM = kPair ? 2 : 1;
   const uint64_t k_bytes = kFp4 ? (uint64_t)a.K / 2 : kBf16 ? (uint64_t)a.K * 2 : (uint64_t)a.K;
   CUtensorMap ta, tb, tsa, tsb, ty;
@@ -1237,6 +1305,7 @@ cudaError_t launch_cfg(const GemmArgs& a, cudaStream_t s, Device dev, unsigned* 
   p.residual_stride = a.residual_stride;
   p.act = a.act;
   p.a_per_row = a.a_per_row ? 1 : 0;
+  p.r_v8 = ((reinterpret_cast<uintptr_t>(a.residual) | (uintptr_t)(a.residual_stride * 2)) & 31u) == 0 ? 1 : 0;
   auto kern = gemm_kernel<kFp4, kBN, kPair, kRequant, kBf16, kEpi>;
 
   cudaLaunchConfig_t cfg{};
