@@ -248,36 +248,34 @@ __device__ __forceinline__ void load_residual(uint32_t (&r)[16], const uint16_t*
   }
 }
 
-// act(v * scale + bias) + residual of 32 columns of one row, as 16-bit pairs.  scale is
-// s_row (NVFP4), s_row * S_W[n] (FP8) or 1.
-template <bool kFp4, bool kBf16, bool kF16>
-__device__ __forceinline__ void finish32(float2 (&v)[16], const KParams& p, float s_row,
-                                         int64_t n0, const uint32_t (&res)[16], uint32_t* packed) {
+// Values of 32 columns that the lanes of a warp hold one each, for every lane's row:
+// columns 2 i and 2 i + 1.
+__device__ __forceinline__ float2 column_pair(float held, int i) {
+  return make_float2(__shfl_sync(0xFFFFFFFFu, held, 2 * i), __shfl_sync(0xFFFFFFFFu, held, 2 * i + 1));
+}
+
+// act(v * scale + bias) + residual of 32 columns of one row, as 16-bit pairs.  The scale
+// is s_row (NVFP4), s_row * S_W[n] (FP8) or 1; lane i holds the bias and S_W of column
+// i.  (Loads of them at the same address in all lanes cost 11 of 38 us at 4608 x 12288 x
+// 256 NVFP4, where the epilogue is the bound.)
+template <bool kFp4, bool kBf16, bool kF16, bool kRes>
+__device__ __forceinline__ void finish32(float2 (&v)[16], const KParams& p, float s_row, float bias,
+                                         float s_w, const uint32_t (&res)[16], uint32_t* packed) {
   const float2 s2 = splat(s_row);
   if (!kFp4 && !kBf16 && p.w_per_channel) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const float4 sw = __ldg(reinterpret_cast<const float4*>(p.sdec_w + n0) + k);
-      v[2 * k] = mul2(v[2 * k], mul2(s2, make_float2(sw.x, sw.y)));
-      v[2 * k + 1] = mul2(v[2 * k + 1], mul2(s2, make_float2(sw.z, sw.w)));
-    }
+    for (int i = 0; i < 16; ++i) v[i] = mul2(v[i], mul2(s2, column_pair(s_w, i)));
   } else if (!kBf16) {
-    const float2 s = kFp4 ? s2 : mul2(s2, splat(__ldg(p.sdec_w)));
+    const float2 s = kFp4 ? s2 : mul2(s2, splat(s_w));
 #pragma unroll
     for (int i = 0; i < 16; ++i) v[i] = mul2(v[i], s);
   }
   if (p.bias != nullptr) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const uint4 w = __ldg(reinterpret_cast<const uint4*>(p.bias + n0) + k);
-      v[4 * k] = add2(v[4 * k], unpack16x2<kF16>(w.x));
-      v[4 * k + 1] = add2(v[4 * k + 1], unpack16x2<kF16>(w.y));
-      v[4 * k + 2] = add2(v[4 * k + 2], unpack16x2<kF16>(w.z));
-      v[4 * k + 3] = add2(v[4 * k + 3], unpack16x2<kF16>(w.w));
-    }
+    for (int i = 0; i < 16; ++i) v[i] = add2(v[i], column_pair(bias, i));
   }
   activate(v, p.act);
-  if (p.residual != nullptr) {
+  if (kRes) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) v[i] = add2(v[i], unpack16x2<kF16>(res[i]));
   }
@@ -288,15 +286,16 @@ __device__ __forceinline__ void finish32(float2 (&v)[16], const KParams& p, floa
 
 // kBf16 (with !kFp4): bf16 operands on the FP8 skeleton (the same 128-byte
 // rows, 32 bytes of K per MMA), no scales.
-// kEpi: the epilogue of qlin_linear_*: bias, activation and residual before the
-// 16-bit rounding, FP8 row scales of A.
-template <bool kFp4, int kBN, bool kPair, bool kRequant, bool kBf16 = false, bool kEpi = false>
-__global__ void __launch_bounds__(Cfg<kFp4, kBN, kPair, kEpi && kFp4 && kPair>::kThreads, 1)
+// kLin: the epilogue of qlin_linear_*: bias and activation before the 16-bit rounding,
+// FP8 row scales of A; kLin == 2 adds a residual.
+template <bool kFp4, int kBN, bool kPair, bool kRequant, bool kBf16 = false, int kLin = 0>
+__global__ void __launch_bounds__(Cfg<kFp4, kBN, kPair, kLin != 0 && kFp4 && kPair>::kThreads, 1)
     gemm_kernel(const __grid_constant__ CUtensorMap tmap_a,
                 const __grid_constant__ CUtensorMap tmap_b,
                 const __grid_constant__ CUtensorMap tmap_sfa,
                 const __grid_constant__ CUtensorMap tmap_sfb,
                 const __grid_constant__ CUtensorMap tmap_y, const KParams p) {
+  constexpr bool kEpi = kLin != 0, kRes = kLin == 2;
   constexpr bool kHold = kEpi && kFp4 && kPair;
   using C = Cfg<kFp4, kBN, kPair, kHold>;
   constexpr int kCM = kPair ? 2 : 1;          // CTAs per cluster (M tiles per cluster tile)
@@ -866,15 +865,47 @@ __global__ void __launch_bounds__(Cfg<kFp4, kBN, kPair, kEpi && kFp4 && kPair>::
       // chunk c (32 columns) of this thread starts at column ccol(c)
       const int64_t col0 = (int64_t)nb * kBN + half * kCols;
       auto ccol = [&](int c) -> int64_t { return col0 + c * 32; };
-      // kEpi: the residual is loaded a chunk ahead of its use, the first one while the
-      // accumulator is still being computed
-      uint32_t res[kEpi ? 16 : 1];
-      const bool has_res = kEpi && p.residual != nullptr && row < p.M;
-      const uint16_t* const res_row = has_res ? p.residual + row * p.residual_stride : nullptr;
+      // kEpi, while the accumulator is still being computed: lane i's bias and S_W of
+      // column i of every chunk; the residual's first group (two chunks) into registers
+      // (each later one is loaded as the one before is used), and the next tile's rows
+      // of it into L2
+      float bias[kEpi ? kChunks : 1], s_w[kEpi ? kChunks : 1];
+      uint32_t res[kRes ? 2 : 1][16];
+      const uint16_t* const res_row = kRes && row < p.M ? p.residual + row * p.residual_stride : nullptr;
+      auto load_res = [&](int b, int c) {
+        if (kRes && res_row != nullptr && c < kChunks && ccol(c) < p.N)
+          load_residual(res[b], res_row + ccol(c), p.r_v8 != 0);
+      };
       if constexpr (kEpi) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) res[i] = 0u;
-        if (has_res && ccol(0) < p.N) load_residual(res, res_row + ccol(0), p.r_v8 != 0);
+        for (int c = 0; c < kChunks; ++c) {
+          const int64_t n = ccol(c) + lane;
+          bias[c] = s_w[c] = 0.0f;
+          if (ccol(c) >= p.N) continue;
+          if (p.bias != nullptr) {
+            const uint32_t w = __ldg(reinterpret_cast<const unsigned short*>(p.bias) + n);
+            bias[c] = kBf16 && p.fp16 ? __half2float(__ushort_as_half((unsigned short)w)) : bf16_lo(w);
+          }
+          if (!kFp4 && !kBf16) s_w[c] = __ldg(p.sdec_w + (p.w_per_channel ? n : 0));
+        }
+      }
+      if constexpr (kRes) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) res[b][i] = 0u;
+          load_res(b, b);
+        }
+        if (ct + ncl < num_ctiles) {
+          int mg2, nb2;
+          tile_coords(ct + ncl, groups_m, &mg2, &nb2);
+          const int64_t r2 = (int64_t)(mg2 * kCM + rank) * kBM + quarter * 32 + lane;
+          const int64_t c2 = (int64_t)nb2 * kBN + half * kCols;
+#pragma unroll
+          for (int k = 0; k < (kCols + 63) / 64; ++k)
+            if (r2 < p.M && c2 + 64 * k < p.N)
+              asm volatile("prefetch.global.L2 [%0];" ::"l"(p.residual + r2 * p.residual_stride + c2 + 64 * k));
+        }
       }
       if (!mbar_wait(&tmem_full[acc], acc_phase, ctl)) break;
       tc_fence_after();
@@ -1017,41 +1048,56 @@ __global__ void __launch_bounds__(Cfg<kFp4, kBN, kPair, kEpi && kFp4 && kPair>::
         }
       };
       if constexpr (kEpi) {
-        // kHold: all columns into registers, then TMEM is free; else 64 at a time.
-        constexpr int kBatch = kHold || kChunks < 2 ? kChunks : 2;
+        // Groups of two chunks in a rolled loop: unrolled over the tile, the activations'
+        // code outgrew the instruction caches.  kHold: all columns into registers, then
+        // TMEM is free; each group then moves down.
+        constexpr int kGroup = kChunks < 2 ? 1 : 2;
+        constexpr int kRaw = kHold ? kChunks : kGroup;
+        uint32_t r[kRaw][32];
+        auto load_raw = [&](int c0) {
 #pragma unroll
-        for (int cb = 0; cb < kChunks; cb += kBatch) {
-          uint32_t r[kBatch][32];
-#pragma unroll
-          for (int b = 0; b < kBatch; ++b) tmem_ld32(taddr + (cb + b) * 32, r[b]);
+          for (int b = 0; b < kRaw; ++b) tmem_ld32(taddr + (uint32_t)(c0 + b) * 32, r[b]);
           tmem_ld_wait();
 #pragma unroll
-          for (int b = 0; b < kBatch; ++b)
+          for (int b = 0; b < kRaw; ++b)
 #pragma unroll
             for (int i = 0; i < 32; ++i) asm volatile("" : "+r"(r[b][i]));   // read after the wait
-          if (cb + kBatch == kChunks) release();
-          uint32_t packed[32];   // of the chunk and, where it is odd, the one before
+        };
+        if constexpr (kHold) {
+          load_raw(0);
+          release();
+        }
+#pragma unroll 1
+        for (int c0 = 0; c0 < kChunks; c0 += kGroup) {
+          if constexpr (!kHold) {
+            load_raw(c0);
+            if (c0 + kGroup == kChunks) release();
+          }
+          if (ccol(c0) < p.N) {   // (N % 64 == 0: a group is wholly inside or outside)
+            uint32_t packed[kGroup * 16];
 #pragma unroll
-          for (int b = 0; b < kBatch; ++b) {
-            const int c = cb + b;
-            const int64_t n0 = ccol(c);
-            uint32_t cur[16];
+            for (int b = 0; b < kGroup; ++b) {
+              float2 v[16];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) cur[i] = res[i];
-            if (c + 1 < kChunks && has_res && ccol(c + 1) < p.N)
-              load_residual(res, res_row + ccol(c + 1), p.r_v8 != 0);
-            uint32_t* const pk = packed + (b & 1) * 16;
-            if (n0 >= p.N) continue;   // (an even chunk and the next one are both in or out)
-            float2 v[16];
+              for (int i = 0; i < 16; ++i)
+                v[i] = make_float2(__uint_as_float(r[b][2 * i]), __uint_as_float(r[b][2 * i + 1]));
+              if (kBf16 && p.fp16)
+                finish32<kFp4, kBf16, true, kRes>(v, p, row_scale, bias[b], s_w[b], res[kRes ? b : 0], packed + b * 16);
+              else
+                finish32<kFp4, kBf16, false, kRes>(v, p, row_scale, bias[b], s_w[b], res[kRes ? b : 0], packed + b * 16);
+              load_res(b, c0 + kGroup + b);
+              store_y(c0 + b, packed + b * 16);
+            }
+            if constexpr (kRequant) requant(c0 / 2, packed);
+          }
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-              v[i] = make_float2(__uint_as_float(r[b][2 * i]), __uint_as_float(r[b][2 * i + 1]));
-            if (kBf16 && p.fp16)
-              finish32<kFp4, kBf16, true>(v, p, row_scale, n0, cur, pk);
-            else
-              finish32<kFp4, kBf16, false>(v, p, row_scale, n0, cur, pk);
-            store_y(c, pk);
-            if (kRequant && (b & 1) == 1) requant(c / 2, packed);
+          for (int c = 0; c + kGroup < kChunks; ++c) {   // the next group moves to the front
+            bias[c] = bias[c + kGroup];
+            s_w[c] = s_w[c + kGroup];
+            if constexpr (kHold) {
+#pragma unroll
+              for (int i = 0; i < 32; ++i) r[c][i] = r[c + kGroup][i];
+            }
           }
         }
       } else {
@@ -1256,10 +1302,10 @@ CUresult encode_scales(CUtensorMap* map, const void* base, uint64_t rows, uint64
                    CU_TENSOR_MAP_SWIZZLE_NONE);
 }
 
-template <bool kFp4, int kBN, bool kPair, bool kRequant, bool kBf16 = false, bool kEpi = false>
+template <bool kFp4, int kBN, bool kPair, bool kRequant, bool kBf16 = false, int kLin = 0>
 cudaError_t launch_cfg(const GemmArgs& a, cudaStream_t s, Device dev, unsigned* err,
                        uint64_t timeout_ns) {
-  using C = Cfg<kFp4, kBN, kPair, kEpi && kFp4 && kPair>;
+  using C = Cfg<kFp4, kBN, kPair, kLin != 0 && kFp4 && kPair>;
   constexpr int kCM = kPair ? 2 : 1;
   const uint64_t k_bytes = kFp4 ? (uint64_t)a.K / 2 : kBf16 ? (uint64_t)a.K * 2 : (uint64_t)a.K;
   CUtensorMap ta, tb, tsa, tsb, ty;
@@ -1306,7 +1352,7 @@ cudaError_t launch_cfg(const GemmArgs& a, cudaStream_t s, Device dev, unsigned* 
   p.act = a.act;
   p.a_per_row = a.a_per_row ? 1 : 0;
   p.r_v8 = ((reinterpret_cast<uintptr_t>(a.residual) | (uintptr_t)(a.residual_stride * 2)) & 31u) == 0 ? 1 : 0;
-  auto kern = gemm_kernel<kFp4, kBN, kPair, kRequant, kBf16, kEpi>;
+  auto kern = gemm_kernel<kFp4, kBN, kPair, kRequant, kBf16, kLin>;
 
   cudaLaunchConfig_t cfg{};
   cudaLaunchAttribute attr[2];
@@ -1355,19 +1401,19 @@ Tile tile_of(const GemmArgs& a, int num_sms) {
                      a.M, a.N, a.K, num_sms);
 }
 
-template <bool kFp4, bool kEpi>
+template <bool kFp4, int kLin>
 cudaError_t dispatch_bn(const GemmArgs& a, cudaStream_t s, Device dev, unsigned* err,
                         uint64_t timeout_ns) {
   const bool requant = a.next_scale != nullptr;
   switch (tile_of(a, dev.num_sms)) {
     case Tile::kPair:
-      return requant ? launch_cfg<kFp4, 256, true, true, false, kEpi>(a, s, dev, err, timeout_ns)
-                     : launch_cfg<kFp4, 256, true, false, false, kEpi>(a, s, dev, err, timeout_ns);
+      return requant ? launch_cfg<kFp4, 256, true, true, false, kLin>(a, s, dev, err, timeout_ns)
+                     : launch_cfg<kFp4, 256, true, false, false, kLin>(a, s, dev, err, timeout_ns);
     case Tile::kSingle:
-      return requant ? launch_cfg<kFp4, 128, false, true, false, kEpi>(a, s, dev, err, timeout_ns)
-                     : launch_cfg<kFp4, 128, false, false, false, kEpi>(a, s, dev, err, timeout_ns);
+      return requant ? launch_cfg<kFp4, 128, false, true, false, kLin>(a, s, dev, err, timeout_ns)
+                     : launch_cfg<kFp4, 128, false, false, false, kLin>(a, s, dev, err, timeout_ns);
     default:
-      return launch_cfg<kFp4, 64, false, false, false, kEpi>(a, s, dev, err, timeout_ns);
+      return launch_cfg<kFp4, 64, false, false, false, kLin>(a, s, dev, err, timeout_ns);
   }
 }
 
@@ -1393,17 +1439,23 @@ cudaError_t launch_gemm(const GemmArgs& a, cudaStream_t s, Device dev, unsigned*
                         uint64_t timeout_ns) {
   if (a.bf16) {
     const bool pair = tile_of(a, dev.num_sms) == Tile::kPair;
+    if (a.residual != nullptr)
+      return pair ? launch_cfg<false, 256, true, false, true, 2>(a, s, dev, err, timeout_ns)
+                  : launch_cfg<false, 128, false, false, true, 2>(a, s, dev, err, timeout_ns);
     if (a.epilogue)
-      return pair ? launch_cfg<false, 256, true, false, true, true>(a, s, dev, err, timeout_ns)
-                  : launch_cfg<false, 128, false, false, true, true>(a, s, dev, err, timeout_ns);
+      return pair ? launch_cfg<false, 256, true, false, true, 1>(a, s, dev, err, timeout_ns)
+                  : launch_cfg<false, 128, false, false, true, 1>(a, s, dev, err, timeout_ns);
     return pair ? launch_cfg<false, 256, true, false, true>(a, s, dev, err, timeout_ns)
                 : launch_cfg<false, 128, false, false, true>(a, s, dev, err, timeout_ns);
   }
+  if (a.residual != nullptr)
+    return a.fp4 ? dispatch_bn<true, 2>(a, s, dev, err, timeout_ns)
+                 : dispatch_bn<false, 2>(a, s, dev, err, timeout_ns);
   if (a.epilogue)
-    return a.fp4 ? dispatch_bn<true, true>(a, s, dev, err, timeout_ns)
-                 : dispatch_bn<false, true>(a, s, dev, err, timeout_ns);
-  return a.fp4 ? dispatch_bn<true, false>(a, s, dev, err, timeout_ns)
-               : dispatch_bn<false, false>(a, s, dev, err, timeout_ns);
+    return a.fp4 ? dispatch_bn<true, 1>(a, s, dev, err, timeout_ns)
+                 : dispatch_bn<false, 1>(a, s, dev, err, timeout_ns);
+  return a.fp4 ? dispatch_bn<true, 0>(a, s, dev, err, timeout_ns)
+               : dispatch_bn<false, 0>(a, s, dev, err, timeout_ns);
 }
 
 cudaError_t launch_wait_selftest(uint64_t timeout_ns, cudaStream_t s, unsigned* err) {
