@@ -58,7 +58,8 @@ constexpr int pow2_at_least(int x) {
 // holds its own 128 rows of A and its own half of the W tile.
 // kHold: the epilogue's warps hold a whole accumulator in registers (setmaxnreg), so
 // that the one accumulator of an NVFP4 pair goes back to the MMAs before the
-// activations: two warpgroups of roles, then two of epilogue.
+// activations, and the other kinds have room for a tile's residual: whole warpgroups of
+// roles, then two of epilogue.
 template <bool kFp4, int kBN, bool kPair = false, bool kHold = false>
 struct Cfg {
   // warps: 0 producer, 1 MMA, NVFP4: four scale warps, pairs: the scale
@@ -69,7 +70,7 @@ struct Cfg {
   static constexpr bool kSfCopy = kFp4 && kPair;   // scales by TMA and tcgen05.cp
   static constexpr int kSfProducer = kSfCopy ? 2 + kSfWarps : -1;
   static constexpr int kRoleWarps = 2 + kSfWarps + (kSfCopy ? 1 : 0);
-  static constexpr int kEpiWarp0 = kHold ? 8 : kRoleWarps;
+  static constexpr int kEpiWarp0 = kHold ? (kRoleWarps + 3) / 4 * 4 : kRoleWarps;
   static constexpr int kEpiWarps = 8;
   static constexpr int kThreads = (kEpiWarp0 + kEpiWarps) * 32;
   // Row boxes per operand tile and stage: copies of separate boxes overlap
@@ -122,9 +123,13 @@ struct Cfg {
   static_assert(kTmemCols <= 512, "TMEM budget");
   static_assert(kSmemBytes <= 232448, "shared memory budget");
   static_assert(kStages >= 2, "pipeline depth");
-  // (512 threads at 128 registers; the shares add up to all 65,536)
-  static constexpr int kRoleRegs = 56, kHoldRegs = 200;
-  static_assert(!kHold || (kThreads == 512 && 256 * (kRoleRegs + kHoldRegs) == 65536), "registers");
+  // Registers of the roles' warpgroups and of the two that hold accumulators; the
+  // shares add up to what the launch gives (512 threads 128 each, 384 threads 168).
+  static constexpr int kRoleRegs = 56, kHoldRegs = kFp4 ? 200 : 224;
+  static_assert(!kHold || kEpiWarp0 * 32 * kRoleRegs + kEpiWarps * 32 * kHoldRegs <=
+                              kThreads * (kThreads == 512 ? 128 : 168),
+                "registers");
+  static_assert(!kHold || kThreads == 512 || kThreads == 384, "whole warpgroups");
 };
 
 struct KParams {
@@ -232,7 +237,7 @@ __device__ __forceinline__ void load_residual(uint32_t (&r)[16], const uint16_t*
   if (aligned32) {
 #pragma unroll
     for (int h = 0; h < 2; ++h)
-      asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+      asm volatile("ld.global.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
                    : "=r"(r[8 * h]), "=r"(r[8 * h + 1]), "=r"(r[8 * h + 2]), "=r"(r[8 * h + 3]),
                      "=r"(r[8 * h + 4]), "=r"(r[8 * h + 5]), "=r"(r[8 * h + 6]), "=r"(r[8 * h + 7])
                    : "l"(p + 16 * h));
@@ -289,14 +294,14 @@ __device__ __forceinline__ void finish32(float2 (&v)[16], const KParams& p, floa
 // kLin: the epilogue of qlin_linear_*: bias and activation before the 16-bit rounding,
 // FP8 row scales of A; kLin == 2 adds a residual.
 template <bool kFp4, int kBN, bool kPair, bool kRequant, bool kBf16 = false, int kLin = 0>
-__global__ void __launch_bounds__(Cfg<kFp4, kBN, kPair, kLin != 0 && kFp4 && kPair>::kThreads, 1)
+__global__ void __launch_bounds__(Cfg<kFp4, kBN, kPair, kLin != 0 && kPair>::kThreads, 1)
     gemm_kernel(const __grid_constant__ CUtensorMap tmap_a,
                 const __grid_constant__ CUtensorMap tmap_b,
                 const __grid_constant__ CUtensorMap tmap_sfa,
                 const __grid_constant__ CUtensorMap tmap_sfb,
                 const __grid_constant__ CUtensorMap tmap_y, const KParams p) {
   constexpr bool kEpi = kLin != 0, kRes = kLin == 2;
-  constexpr bool kHold = kEpi && kFp4 && kPair;
+  constexpr bool kHold = kEpi && kPair;
   using C = Cfg<kFp4, kBN, kPair, kHold>;
   constexpr int kCM = kPair ? 2 : 1;          // CTAs per cluster (M tiles per cluster tile)
   constexpr uint16_t kMask = (uint16_t)((1u << kCM) - 1u);
@@ -866,11 +871,12 @@ __global__ void __launch_bounds__(Cfg<kFp4, kBN, kPair, kLin != 0 && kFp4 && kPa
       const int64_t col0 = (int64_t)nb * kBN + half * kCols;
       auto ccol = [&](int c) -> int64_t { return col0 + c * 32; };
       // kEpi, while the accumulator is still being computed: lane i's bias and S_W of
-      // column i of every chunk; the residual's first group (two chunks) into registers
-      // (each later one is loaded as the one before is used), and the next tile's rows
-      // of it into L2
+      // column i of every chunk; the residual into registers (all of it where they
+      // suffice, else two chunks, the others loaded as these are used), and the next
+      // tile's rows of it into L2
       float bias[kEpi ? kChunks : 1], s_w[kEpi ? kChunks : 1];
-      uint32_t res[kRes ? 2 : 1][16];
+      constexpr int kResHeld = !kRes ? 1 : kHold && !kFp4 ? kChunks : 2;
+      uint32_t res[kResHeld][16];
       const uint16_t* const res_row = kRes && row < p.M ? p.residual + row * p.residual_stride : nullptr;
       auto load_res = [&](int b, int c) {
         if (kRes && res_row != nullptr && c < kChunks && ccol(c) < p.N)
@@ -891,7 +897,7 @@ __global__ void __launch_bounds__(Cfg<kFp4, kBN, kPair, kLin != 0 && kFp4 && kPa
       }
       if constexpr (kRes) {
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
+        for (int b = 0; b < kResHeld; ++b) {
 #pragma unroll
           for (int i = 0; i < 16; ++i) res[b][i] = 0u;
           load_res(b, b);
@@ -1085,7 +1091,7 @@ __global__ void __launch_bounds__(Cfg<kFp4, kBN, kPair, kLin != 0 && kFp4 && kPa
                 finish32<kFp4, kBf16, true, kRes>(v, p, row_scale, bias[b], s_w[b], res[kRes ? b : 0], packed + b * 16);
               else
                 finish32<kFp4, kBf16, false, kRes>(v, p, row_scale, bias[b], s_w[b], res[kRes ? b : 0], packed + b * 16);
-              load_res(b, c0 + kGroup + b);
+              if (kResHeld == 2) load_res(b, c0 + kGroup + b);
               store_y(c0 + b, packed + b * 16);
             }
             if constexpr (kRequant) requant(c0 / 2, packed);
@@ -1097,6 +1103,10 @@ __global__ void __launch_bounds__(Cfg<kFp4, kBN, kPair, kLin != 0 && kFp4 && kPa
             if constexpr (kHold) {
 #pragma unroll
               for (int i = 0; i < 32; ++i) r[c][i] = r[c + kGroup][i];
+            }
+            if constexpr (kResHeld > 2) {
+#pragma unroll
+              for (int i = 0; i < 16; ++i) res[c][i] = res[c + kGroup][i];
             }
           }
         }
@@ -1305,7 +1315,7 @@ CUresult encode_scales(CUtensorMap* map, const void* base, uint64_t rows, uint64
 template <bool kFp4, int kBN, bool kPair, bool kRequant, bool kBf16 = false, int kLin = 0>
 cudaError_t launch_cfg(const GemmArgs& a, cudaStream_t s, Device dev, unsigned* err,
                        uint64_t timeout_ns) {
-  using C = Cfg<kFp4, kBN, kPair, kLin != 0 && kFp4 && kPair>;
+  using C = Cfg<kFp4, kBN, kPair, kLin != 0 && kPair>;
   constexpr int kCM = kPair ? 2 : 1;
   const uint64_t k_bytes = kFp4 ? (uint64_t)a.K / 2 : kBf16 ? (uint64_t)a.K * 2 : (uint64_t)a.K;
   CUtensorMap ta, tb, tsa, tsb, ty;
