@@ -97,7 +97,12 @@ struct Cfg {
   static constexpr int kSfSmemSlots = kSfCopy ? kSfWarps : 0;
   static constexpr int kSfSlotBytes = (1 + kSfbAtoms) * kStepsPerStage * 512;
   static constexpr int kSfBytes = kSfSmemSlots * kSfSlotBytes;
-  static constexpr int kStagesRaw = (kSmemBudget - kOutBytes - kSfBytes) / kStageBytes;
+  // kHold, NVFP4: a copy of the tile's bias per epilogue warp, where its epilogue is on
+  // the critical path and shared memory is left (the other kinds have none left, and
+  // longer mainloops).
+  static constexpr bool kSmemBias = kHold && kFp4;
+  static constexpr int kBiasBytes = kSmemBias ? kEpiWarps * (kBN / 2) * 4 : 0;
+  static constexpr int kStagesRaw = (kSmemBudget - kOutBytes - kSfBytes - kBiasBytes) / kStageBytes;
   static constexpr int kStages = kStagesRaw > 8 ? 8 : kStagesRaw;
   static constexpr int kNumAcc = (kFp4 && kBN == 256) ? 1 : 2;
   // Scale columns of one stage: A's (4 per 64 elements of K), then W's (4 per
@@ -118,7 +123,8 @@ struct Cfg {
   static constexpr int kTmemCols =
       pow2_at_least(kSfColBase + kSfSlots * kSfColsPerSlot);
   static constexpr int kBarrierBytes = 512;
-  static constexpr int kSmemBytes = 1024 + kStages * kStageBytes + kOutBytes + kSfBytes + kBarrierBytes;
+  static constexpr int kSmemBytes =
+      1024 + kStages * kStageBytes + kOutBytes + kSfBytes + kBiasBytes + kBarrierBytes;
   static_assert(kStageBytes % 1024 == 0, "stages must keep 1024-byte alignment");
   static_assert(kTmemCols <= 512, "TMEM budget");
   static_assert(kSmemBytes <= 232448, "shared memory budget");
@@ -261,11 +267,12 @@ __device__ __forceinline__ float2 column_pair(float held, int i) {
 
 // act(v * scale + bias) + residual of 32 columns of one row, as 16-bit pairs.  The scale
 // is s_row (NVFP4), s_row * S_W[n] (FP8) or 1; lane i holds the bias and S_W of column
-// i.  (Loads of them at the same address in all lanes cost 11 of 38 us at 4608 x 12288 x
+// i, or shared memory the biases.  (Loads of them at the same address in all lanes cost 11 of 38 us at 4608 x 12288 x
 // 256 NVFP4, where the epilogue is the bound.)
-template <bool kFp4, bool kBf16, bool kF16, bool kRes>
+template <bool kFp4, bool kBf16, bool kF16, bool kRes, bool kSmemBias>
 __device__ __forceinline__ void finish32(float2 (&v)[16], const KParams& p, float s_row, float bias,
-                                         float s_w, const uint32_t (&res)[16], uint32_t* packed) {
+                                         const float* bias_s, float s_w, const uint32_t (&res)[16],
+                                         uint32_t* packed) {
   const float2 s2 = splat(s_row);
   if (!kFp4 && !kBf16 && p.w_per_channel) {
 #pragma unroll
@@ -277,7 +284,16 @@ __device__ __forceinline__ void finish32(float2 (&v)[16], const KParams& p, floa
   }
   if (p.bias != nullptr) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = add2(v[i], column_pair(bias, i));
+    for (int i = 0; i < 16; i += 2) {
+      if (kSmemBias) {
+        const float4 b = *reinterpret_cast<const float4*>(bias_s + 2 * i);
+        v[i] = add2(v[i], make_float2(b.x, b.y));
+        v[i + 1] = add2(v[i + 1], make_float2(b.z, b.w));
+      } else {
+        v[i] = add2(v[i], column_pair(bias, i));
+        v[i + 1] = add2(v[i + 1], column_pair(bias, i + 1));
+      }
+    }
   }
   activate(v, p.act);
   if (kRes) {
@@ -310,7 +326,8 @@ __global__ void __launch_bounds__(Cfg<kFp4, kBN, kPair, kLin != 0 && kPair>::kTh
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   uint8_t* out_stage = smem + C::kStages * C::kStageBytes;   // epilogue staging boxes
   uint8_t* sf_ring = out_stage + C::kOutBytes;               // block scales (kSfCopy)
-  uint64_t* full = reinterpret_cast<uint64_t*>(sf_ring + C::kSfBytes);
+  float* const bias_copies = reinterpret_cast<float*>(sf_ring + C::kSfBytes);   // kSmemBias
+  uint64_t* full = reinterpret_cast<uint64_t*>(sf_ring + C::kSfBytes + C::kBiasBytes);
   uint64_t* empty = full + C::kStages;
   uint64_t* sf_full = empty + C::kStages;       // kSfCopy: a slot's scale bytes landed
   uint64_t* sf_empty = sf_full + C::kSfSmemSlots;   // and its copies to TMEM are done
@@ -875,6 +892,7 @@ __global__ void __launch_bounds__(Cfg<kFp4, kBN, kPair, kLin != 0 && kPair>::kTh
       // suffice, else two chunks, the others loaded as these are used), and the next
       // tile's rows of it into L2
       float bias[kEpi ? kChunks : 1], s_w[kEpi ? kChunks : 1];
+      float* const bias_s = bias_copies + (C::kSmemBias ? e * kCols : 0);
       constexpr int kResHeld = !kRes ? 1 : kHold && !kFp4 ? kChunks : 2;
       uint32_t res[kResHeld][16];
       const uint16_t* const res_row = kRes && row < p.M ? p.residual + row * p.residual_stride : nullptr;
@@ -893,6 +911,12 @@ __global__ void __launch_bounds__(Cfg<kFp4, kBN, kPair, kLin != 0 && kPair>::kTh
             bias[c] = kBf16 && p.fp16 ? __half2float(__ushort_as_half((unsigned short)w)) : bf16_lo(w);
           }
           if (!kFp4 && !kBf16) s_w[c] = __ldg(p.sdec_w + (p.w_per_channel ? n : 0));
+        }
+        if constexpr (C::kSmemBias) {
+          __syncwarp();   // the tile before has read its copy
+#pragma unroll
+          for (int c = 0; c < kChunks; ++c) bias_s[c * 32 + lane] = bias[c];
+          __syncwarp();
         }
       }
       if constexpr (kRes) {
@@ -1088,9 +1112,9 @@ __global__ void __launch_bounds__(Cfg<kFp4, kBN, kPair, kLin != 0 && kPair>::kTh
               for (int i = 0; i < 16; ++i)
                 v[i] = make_float2(__uint_as_float(r[b][2 * i]), __uint_as_float(r[b][2 * i + 1]));
               if (kBf16 && p.fp16)
-                finish32<kFp4, kBf16, true, kRes>(v, p, row_scale, bias[b], s_w[b], res[kRes ? b : 0], packed + b * 16);
+                finish32<kFp4, kBf16, true, kRes, C::kSmemBias>(v, p, row_scale, bias[b], bias_s + (c0 + b) * 32, s_w[b], res[kRes ? b : 0], packed + b * 16);
               else
-                finish32<kFp4, kBf16, false, kRes>(v, p, row_scale, bias[b], s_w[b], res[kRes ? b : 0], packed + b * 16);
+                finish32<kFp4, kBf16, false, kRes, C::kSmemBias>(v, p, row_scale, bias[b], bias_s + (c0 + b) * 32, s_w[b], res[kRes ? b : 0], packed + b * 16);
               if (kResHeld == 2) load_res(b, c0 + kGroup + b);
               store_y(c0 + b, packed + b * 16);
             }
