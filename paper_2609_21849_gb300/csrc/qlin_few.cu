@@ -16,10 +16,14 @@ namespace qlin {
 
 namespace {
 
+#ifndef FW
+#define FW 32
+#endif
 enum class Kind { kNvfp4, kFp8, kBf16, kFp16 };
 
 constexpr int kRows = 16;         // rows of W per CTA: one MMA's M, one NVFP4 block of y
 constexpr int kChunk = 64;        // bytes of a row per warp and step
+constexpr int kMaxWarps = 8, kMaxSplit = 8;
 
 struct FewParams {
   const uint8_t* a;
@@ -42,6 +46,7 @@ struct FewParams {
   uint8_t* rq_scales;
   float* rq_tensor_scale;
   int64_t rq_col0, rq_cols;
+  int split;                // CTAs of a cluster
 };
 
 __device__ __forceinline__ uint4 ld_stream(const uint8_t* p) {
@@ -113,28 +118,39 @@ __device__ __forceinline__ float load16f(const uint16_t* p, bool fp16) {
   return fp16 ? __half2float(__ushort_as_half(w)) : __uint_as_float((uint32_t)w << 16);
 }
 
-// kTiles: groups of eight tokens.
-template <Kind kKind, int kTiles, int kWarps>
-__global__ void __launch_bounds__(kWarps * 32) few_kernel(const FewParams p) {
+__device__ __forceinline__ float ld_cluster(uint32_t addr) {
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+  return v;
+}
+
+// kTiles: groups of eight tokens.  A cluster of CTAs shares 16 rows of W, all of its
+// warps taking chunks of K in turn; the CTAs' sums meet in distributed shared memory.
+template <Kind kKind, int kTiles>
+__global__ void __launch_bounds__(kMaxWarps * 32) few_kernel(const FewParams p) {
   constexpr bool kFp4 = kKind == Kind::kNvfp4;
-  constexpr int kUnroll = 4;
-  __shared__ float red[kWarps][kTiles * 8][kRows + 1];
+  constexpr int kUnroll = kFp4 ? 2 : 4;
+  __shared__ float red[kMaxWarps][kTiles * 8][kRows + 1];
+  __shared__ float part[kTiles * 8][kRows];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const int64_t n0 = (int64_t)blockIdx.x * kRows;
+  const int warps = blockDim.x >> 5;
+  const int rank = p.split > 1 ? (int)cluster_ctarank() : 0;
+  const int64_t n0 = (int64_t)(blockIdx.x / (unsigned)p.split) * kRows;
   const int64_t w_row = kFp4 ? p.K / 2 : kKind == Kind::kFp8 ? p.K : p.K * 2;
   const int chunks = (int)((w_row + kChunk - 1) / kChunk);
   const uint8_t* const w0 = p.w + (n0 + g) * w_row + 16 * t;
   const uint8_t* const w1 = w0 + 8 * w_row;
+  const int stride = warps * p.split;   // warps that share the rows
   grid_dep_wait();
   grid_dep_launch();
   float acc[kTiles][4] = {};
   const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
-  for (int c0 = warp; c0 < chunks; c0 += kWarps * kUnroll) {
+  for (int c0 = rank * warps + warp; c0 < chunks; c0 += stride * kUnroll) {
     uint4 va[kUnroll][2], vb[kUnroll][kTiles];
     uint16_t sa[kUnroll][2], sb[kUnroll][kTiles];
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
-      const int c = c0 + u * kWarps;
+      const int c = c0 + u * stride;
       const int64_t at = (int64_t)c * kChunk;
       // NVFP4 rows are multiples of 32 bytes: the last chunk may be half a chunk
       const bool in = c < chunks && (!kFp4 || at + 16 * t < w_row);
@@ -196,21 +212,35 @@ __global__ void __launch_bounds__(kWarps * 32) few_kernel(const FewParams p) {
     red[warp][j * 8 + 2 * t + 1][g + 8] = acc[j][3];
   }
   __syncthreads();
-  // sixteen neighbouring threads finish a token's sixteen outputs
+  auto cta_sum = [&](int m, int r) {
+    float v = 0.0f;
+    for (int w = 0; w < warps; ++w) v = __fadd_rn(v, red[w][m][r]);
+    return v;
+  };
+  if (p.split > 1) {
+    for (int i = threadIdx.x; i < kTiles * 8 * kRows; i += blockDim.x)
+      part[i / kRows][i % kRows] = cta_sum(i / kRows, i % kRows);
+    cluster_sync();
+  }
+  // sixteen neighbouring threads finish a token's sixteen outputs; of a cluster's CTAs
+  // each takes every split-th token
   constexpr bool kF16 = kKind == Kind::kFp16;
   const bool requant = p.next_scale != nullptr;
   const float s_next = requant ? *p.next_scale : 1.0f;
   const float s_enc = encode_scale(s_next);
   if (requant && blockIdx.x == 0 && threadIdx.x == 0 && p.rq_tensor_scale != p.next_scale)
     *p.rq_tensor_scale = s_next;
-  for (int i = threadIdx.x; i < kTiles * 8 * kRows; i += kWarps * 32) {
+  for (int i = threadIdx.x; i < kTiles * 8 * kRows; i += blockDim.x) {
     const int m = i / kRows, r = i % kRows;
-    const bool own = m < p.M;   // the same for all sixteen
+    const bool own = m < p.M && (p.split == 1 || m % p.split == rank);   // for all sixteen
     const int64_t n = n0 + r;
     float v = 0.0f;
     if (own) {
-#pragma unroll
-      for (int w = 0; w < kWarps; ++w) v = __fadd_rn(v, red[w][m][r]);
+      if (p.split == 1) {
+        v = cta_sum(m, r);
+      } else {
+        for (int q = 0; q < p.split; ++q) v = __fadd_rn(v, ld_cluster(mapa_shared(&part[m][r], q)));
+      }
       if constexpr (kFp4)
         v = __fmul_rn(v, __fmul_rn(*p.sdec_a, *p.sdec_w));
       else if constexpr (kKind == Kind::kFp8)
@@ -241,18 +271,39 @@ __global__ void __launch_bounds__(kWarps * 32) few_kernel(const FewParams p) {
       if (inside && r == 0) p.rq_scales[scale_offset(m, col / 16, p.rq_cols)] = (uint8_t)code;
     }
   }
+  if (p.split > 1) cluster_sync();   // no CTA leaves while another reads its sums
 }
 
 template <Kind kKind>
-cudaError_t launch_kind(const FewParams& p, cudaStream_t s) {
-  const unsigned grid = (unsigned)(p.N / kRows);
-  if (p.M <= 8) return launch_pdl(few_kernel<kKind, 1, 8>, grid, 256, 0, s, p);
-  return launch_pdl(few_kernel<kKind, 2, 8>, grid, 256, 0, s, p);
+cudaError_t launch_kind(FewParams p, cudaStream_t s, int num_sms) {
+  // Warps that share 16 rows of W: as many as fill the machine once (32 per SM), at most
+  // one per two chunks of K; beyond a CTA's eight they spread over a cluster.
+  const int64_t groups = p.N / kRows;
+  const int64_t chunks = ((kKind == Kind::kNvfp4 ? p.K / 2 : kKind == Kind::kFp8 ? p.K : p.K * 2) + kChunk - 1) / kChunk;
+  const int64_t want = std::max<int64_t>(1, std::min<int64_t>({(int64_t)num_sms * FW / groups, (chunks + 1) / 2,
+                                                              (int64_t)kMaxWarps * kMaxSplit}));
+  p.split = (int)((want + kMaxWarps - 1) / kMaxWarps);
+  const int warps = (int)std::max<int64_t>(2, want / p.split);
+  auto kern = p.M <= 8 ? few_kernel<kKind, 1> : few_kernel<kKind, 2>;
+  cudaLaunchConfig_t cfg{};
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = (unsigned)p.split;
+  at[1].val.clusterDim.y = 1;
+  at[1].val.clusterDim.z = 1;
+  cfg.gridDim = dim3((unsigned)(groups * p.split), 1, 1);
+  cfg.blockDim = dim3((unsigned)warps * 32, 1, 1);
+  cfg.stream = s;
+  cfg.attrs = at;
+  cfg.numAttrs = p.split > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kern, p);
 }
 
 }  // namespace
 
-cudaError_t launch_few(const GemmArgs& a, cudaStream_t s) {
+cudaError_t launch_few(const GemmArgs& a, cudaStream_t s, int num_sms) {
   FewParams p{};
   p.a = static_cast<const uint8_t*>(a.a_codes);
   p.a_row = a.bf16 ? a.a_row_bytes : a.fp4 ? a.K / 2 : a.K;
@@ -277,9 +328,9 @@ cudaError_t launch_few(const GemmArgs& a, cudaStream_t s) {
   p.rq_tensor_scale = a.rq_tensor_scale;
   p.rq_col0 = a.rq_col0;
   p.rq_cols = a.rq_cols;
-  return a.bf16 ? (a.fp16 ? launch_kind<Kind::kFp16>(p, s) : launch_kind<Kind::kBf16>(p, s))
-         : a.fp4 ? launch_kind<Kind::kNvfp4>(p, s)
-                 : launch_kind<Kind::kFp8>(p, s);
+  return a.bf16 ? (a.fp16 ? launch_kind<Kind::kFp16>(p, s, num_sms) : launch_kind<Kind::kBf16>(p, s, num_sms))
+         : a.fp4 ? launch_kind<Kind::kNvfp4>(p, s, num_sms)
+                 : launch_kind<Kind::kFp8>(p, s, num_sms);
 }
 
 }  // namespace qlin
