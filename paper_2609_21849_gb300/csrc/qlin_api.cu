@@ -251,7 +251,7 @@ static qlin_status set_epilogue(GemmArgs& a, const qlin_epilogue_t* ep) {
 // The plain GEMMs always take the tensor-core tiles, so that their sums keep their
 // order; the linears take the few-token kernel where it applies.
 static cudaError_t launch_linear(const GemmArgs& a, cudaStream_t s, Device dev, unsigned* status) {
-  if (a.few_ok && a.M <= kFewTokens) return launch_few(a, s, dev.num_sms);
+  if (a.few_ok && a.M <= kFewTokens) return launch_few(a, s, dev);
   return launch_gemm(a, s, dev, status, timeout());
 }
 

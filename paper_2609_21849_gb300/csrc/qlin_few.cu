@@ -16,14 +16,11 @@ namespace qlin {
 
 namespace {
 
-#ifndef FW
-#define FW 32
-#endif
 enum class Kind { kNvfp4, kFp8, kBf16, kFp16 };
 
-constexpr int kRows = 16;         // rows of W per CTA: one MMA's M, one NVFP4 block of y
+constexpr int kBlock = 16;        // rows of W per MMA, and of an NVFP4 block of y
 constexpr int kChunk = 64;        // bytes of a row per warp and step
-constexpr int kMaxWarps = 8, kMaxSplit = 8;
+constexpr int kMinWarps = 4, kMaxWarps = 8, kMaxSplit = 8;   // (a thread has kTiles outputs at most)
 
 struct FewParams {
   const uint8_t* a;
@@ -69,12 +66,7 @@ __device__ __forceinline__ uint4 ld_keep(const uint8_t* p) {
 template <Kind kKind>
 __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2,
                                     uint32_t a3, uint32_t b0, uint32_t b1) {
-  if constexpr (kKind == Kind::kFp8)
-    asm("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32"
-        " {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-  else if constexpr (kKind == Kind::kBf16)
+  if constexpr (kKind == Kind::kBf16)
     asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32"
         " {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
@@ -104,6 +96,15 @@ __device__ __forceinline__ void e2m1x8_scaled(uint32_t w, __half2 s, uint32_t (&
   }
 }
 
+// FP8: four E4M3 codes as fp16, exactly.  (sm_103a has no E4M3 mma.sync of its own: the
+// instruction becomes these conversions, repeated for every product.)
+__device__ __forceinline__ void e4m3x4_half(uint32_t w, uint32_t& lo, uint32_t& hi) {
+  asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\t"
+      "cvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}"
+      : "=r"(lo), "=r"(hi)
+      : "r"(w));
+}
+
 // Two adjacent E4M3 scales as two pairs of equal halves.
 __device__ __forceinline__ void scale_pairs(uint16_t s2, __half2 (&s)[2]) {
   uint32_t h;
@@ -124,12 +125,17 @@ __device__ __forceinline__ float ld_cluster(uint32_t addr) {
   return v;
 }
 
-// kTiles: groups of eight tokens.  A cluster of CTAs shares 16 rows of W, all of its
-// warps taking chunks of K in turn; the CTAs' sums meet in distributed shared memory.
-template <Kind kKind, int kTiles>
+// Chunks in flight per warp.
+template <Kind kKind, int kTiles, int kRowTiles>
+constexpr int kUnrollOf = kRowTiles == 2 ? 2 : kKind == Kind::kNvfp4 ? 2 : 4;
+
+// kTiles: groups of eight tokens; kRowTiles: of sixteen rows of W.  A cluster of CTAs shares the rows of W, all of
+// its warps taking chunks of K in turn; the CTAs' sums meet in distributed shared memory.
+template <Kind kKind, int kTiles, int kRowTiles>
 __global__ void __launch_bounds__(kMaxWarps * 32) few_kernel(const FewParams p) {
   constexpr bool kFp4 = kKind == Kind::kNvfp4;
-  constexpr int kUnroll = kFp4 ? 2 : 4;
+  constexpr int kRows = kBlock * kRowTiles, kOuts = kTiles * kRowTiles;
+  constexpr int kUnroll = kUnrollOf<kKind, kTiles, kRowTiles>;
   __shared__ float red[kMaxWarps][kTiles * 8][kRows + 1];
   __shared__ float part[kTiles * 8][kRows];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
@@ -138,79 +144,159 @@ __global__ void __launch_bounds__(kMaxWarps * 32) few_kernel(const FewParams p) 
   const int64_t n0 = (int64_t)(blockIdx.x / (unsigned)p.split) * kRows;
   const int64_t w_row = kFp4 ? p.K / 2 : kKind == Kind::kFp8 ? p.K : p.K * 2;
   const int chunks = (int)((w_row + kChunk - 1) / kChunk);
-  const uint8_t* const w0 = p.w + (n0 + g) * w_row + 16 * t;
-  const uint8_t* const w1 = w0 + 8 * w_row;
   const int stride = warps * p.split;   // warps that share the rows
+  // the warp's first chunks of W into L2 while the previous kernel still runs (a hint
+  // that returns no data, so that it may be issued before the wait)
+  for (int u = 0; u < kUnroll; ++u) {
+    const int c = rank * warps + warp + u * stride;
+    if (t < 2 * kRowTiles && c < chunks)
+      asm volatile("prefetch.global.L2 [%0];" ::"l"(p.w + (n0 + g + 8 * t) * w_row + (int64_t)c * kChunk));
+  }
   grid_dep_wait();
   grid_dep_launch();
-  float acc[kTiles][4] = {};
-  const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
-  for (int c0 = rank * warps + warp; c0 < chunks; c0 += stride * kUnroll) {
-    uint4 va[kUnroll][2], vb[kUnroll][kTiles];
-    uint16_t sa[kUnroll][2], sb[kUnroll][kTiles];
+  // what this thread's outputs need beside the sums: loaded now, used after them
+  // (loaded there, they cost a chain of two loads at the end)
+  constexpr bool kF16 = kKind == Kind::kFp16;
+  const bool requant = kKind != Kind::kBf16 && !kF16 && p.next_scale != nullptr;
+  float o_scale[kOuts], o_bias[kOuts], o_res[kOuts];
+  bool o_own[kOuts];   // (the same for the sixteen threads of a token)
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      const int c = c0 + u * stride;
-      const int64_t at = (int64_t)c * kChunk;
-      // NVFP4 rows are multiples of 32 bytes: the last chunk may be half a chunk
-      const bool in = c < chunks && (!kFp4 || at + 16 * t < w_row);
-      va[u][0] = in ? ld_stream(w0 + at) : zero;
-      va[u][1] = in ? ld_stream(w1 + at) : zero;
-      const int64_t blk = (int64_t)c * 8 + 2 * t;   // NVFP4: first block of the 16 bytes
+  for (int k = 0; k < kOuts; ++k) {
+    const int i = threadIdx.x + k * blockDim.x, m = i / kRows;
+    const int64_t n = n0 + i % kRows;
+    // of a cluster's CTAs each takes every split-th token
+    const bool own = i < kTiles * 8 * kRows && m < p.M && (p.split == 1 || m % p.split == rank);
+    o_own[k] = own;
+    o_scale[k] = 1.0f;
+    o_bias[k] = o_res[k] = 0.0f;
+    if (!own) continue;
+    if constexpr (kFp4)
+      o_scale[k] = __fmul_rn(*p.sdec_a, *p.sdec_w);
+    else if constexpr (kKind == Kind::kFp8)
+      o_scale[k] = __fmul_rn(p.sdec_a[p.a_per_row ? m : 0], p.sdec_w[p.w_per_channel ? n : 0]);
+    if (p.bias != nullptr) o_bias[k] = load16f(p.bias + n, kF16);
+    if (p.residual != nullptr) o_res[k] = load16f(p.residual + m * p.residual_stride + n, kF16);
+  }
+  const float s_next = requant ? *p.next_scale : 1.0f;
+
+  // Chunks through a ring of registers: each is loaded kUnroll chunks ahead of its use.
+  // The pointers run along the warp's chunks; a token past M reads the first one's row
+  // (its column of the sums is not used).
+  float acc[kRowTiles][kTiles][4] = {};
+  uint4 va[kUnroll][kRowTiles][2], vb[kUnroll][kTiles];
+  uint16_t sa[kUnroll][kRowTiles][2], sb[kUnroll][kTiles];
+  const int first = rank * warps + warp;
+  int left = (chunks - first + stride - 1) / stride;   // chunks to load
+  int tail = kFp4 ? (int)(w_row - (int64_t)first * kChunk) - 16 * t : 0;   // bytes of the row from here
+  const uint8_t* w = p.w + (n0 + g) * w_row + 16 * t + (int64_t)first * kChunk;
+  const uint8_t *a[kTiles], *fa[kTiles], *fw[kRowTiles][2];
+#pragma unroll
+  for (int j = 0; j < kTiles; ++j) {
+    const int m = j * 8 + g < p.M ? j * 8 + g : 0;
+    a[j] = p.a + m * p.a_row + 16 * t + (int64_t)first * kChunk;
+    // the scales of blocks 8 c + 2 t and the next: 1024 bytes per chunk of 128 elements
+    fa[j] = kFp4 ? p.sfa + scale_offset(m, 8 * (int64_t)first + 2 * t, p.K) : nullptr;
+  }
+#pragma unroll
+  for (int h = 0; h < 2 * kRowTiles; ++h)
+    fw[h / 2][h % 2] = kFp4 ? p.sfb + scale_offset(n0 + g + 8 * h, 8 * (int64_t)first + 2 * t, p.K) : nullptr;
+  const int step = stride * kChunk, fstep = stride * 1024;
+  auto load = [&](int u) {
+    // NVFP4 rows are multiples of 32 bytes: the last chunk may be half a chunk
+    const bool in = left > 0 && (!kFp4 || tail > 0);
+#pragma unroll
+    for (int h = 0; h < 2 * kRowTiles; ++h) {
+      va[u][h / 2][h % 2] = make_uint4(0u, 0u, 0u, 0u);
+      if (in) va[u][h / 2][h % 2] = ld_stream(w + 8 * h * w_row);
       if (kFp4) {
-        sa[u][0] = in ? *reinterpret_cast<const uint16_t*>(p.sfb + scale_offset(n0 + g, blk, p.K)) : 0;
-        sa[u][1] = in ? *reinterpret_cast<const uint16_t*>(p.sfb + scale_offset(n0 + g + 8, blk, p.K)) : 0;
-      }
-#pragma unroll
-      for (int j = 0; j < kTiles; ++j) {
-        const int m = j * 8 + g;
-        const bool tok = in && m < p.M;
-        vb[u][j] = tok ? ld_keep(p.a + m * p.a_row + at + 16 * t) : zero;
-        if (kFp4)
-          sb[u][j] = tok ? *reinterpret_cast<const uint16_t*>(p.sfa + scale_offset(m, blk, p.K)) : 0;
+        sa[u][h / 2][h % 2] = 0;
+        if (in) sa[u][h / 2][h % 2] = *reinterpret_cast<const uint16_t*>(fw[h / 2][h % 2]);
+        fw[h / 2][h % 2] += fstep;
       }
     }
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      if constexpr (kFp4) {
-        __half2 s0[2], s1[2], st[kTiles][2];
-        scale_pairs(sa[u][0], s0);
-        scale_pairs(sa[u][1], s1);
+    for (int j = 0; j < kTiles; ++j) {
+      vb[u][j] = make_uint4(0u, 0u, 0u, 0u);
+      if (in) vb[u][j] = ld_keep(a[j]);
+      a[j] += step;
+      if (kFp4) {
+        sb[u][j] = 0;
+        if (in) sb[u][j] = *reinterpret_cast<const uint16_t*>(fa[j]);
+        fa[j] += fstep;
+      }
+    }
+    w += step;
+    tail -= step;
+    --left;
+  };
+  auto multiply = [&](int u) {
+    if constexpr (kFp4) {
+      __half2 sw[kRowTiles][2][2], st[kTiles][2];
 #pragma unroll
-        for (int j = 0; j < kTiles; ++j) scale_pairs(sb[u][j], st[j]);
-        const uint32_t a0[4] = {va[u][0].x, va[u][0].y, va[u][0].z, va[u][0].w};
-        const uint32_t a1[4] = {va[u][1].x, va[u][1].y, va[u][1].z, va[u][1].w};
+      for (int h = 0; h < 2 * kRowTiles; ++h) scale_pairs(sa[u][h / 2][h % 2], sw[h / 2][h % 2]);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {   // eight elements of K per lane
+      for (int j = 0; j < kTiles; ++j) scale_pairs(sb[u][j], st[j]);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {   // eight elements of K per lane
+        auto word = [&](const uint4& v) { return q == 0 ? v.x : q == 1 ? v.y : q == 2 ? v.z : v.w; };
+        uint32_t hb[kTiles][4];
+#pragma unroll
+        for (int j = 0; j < kTiles; ++j) e2m1x8_scaled(word(vb[u][j]), st[j][q >> 1], hb[j]);
+#pragma unroll
+        for (int i = 0; i < kRowTiles; ++i) {
           uint32_t h0[4], h1[4];
-          e2m1x8_scaled(a0[q], s0[q >> 1], h0);
-          e2m1x8_scaled(a1[q], s1[q >> 1], h1);
+          e2m1x8_scaled(word(va[u][i][0]), sw[i][0][q >> 1], h0);
+          e2m1x8_scaled(word(va[u][i][1]), sw[i][1][q >> 1], h1);
 #pragma unroll
           for (int j = 0; j < kTiles; ++j) {
-            const uint32_t b[4] = {vb[u][j].x, vb[u][j].y, vb[u][j].z, vb[u][j].w};
-            uint32_t hb[4];
-            e2m1x8_scaled(b[q], st[j][q >> 1], hb);
-            mma<kKind>(acc[j], h0[0], h1[0], h0[1], h1[1], hb[0], hb[1]);
-            mma<kKind>(acc[j], h0[2], h1[2], h0[3], h1[3], hb[2], hb[3]);
+            mma<kKind>(acc[i][j], h0[0], h1[0], h0[1], h1[1], hb[j][0], hb[j][1]);
+            mma<kKind>(acc[i][j], h0[2], h1[2], h0[3], h1[3], hb[j][2], hb[j][3]);
           }
         }
-      } else {
+      }
+    } else if constexpr (kKind == Kind::kFp8) {
 #pragma unroll
-        for (int j = 0; j < kTiles; ++j) {
-          mma<kKind>(acc[j], va[u][0].x, va[u][1].x, va[u][0].y, va[u][1].y, vb[u][j].x, vb[u][j].y);
-          mma<kKind>(acc[j], va[u][0].z, va[u][1].z, va[u][0].w, va[u][1].w, vb[u][j].z, vb[u][j].w);
+      for (int q = 0; q < 4; ++q) {   // four elements of K per lane
+        auto word = [&](const uint4& v) { return q == 0 ? v.x : q == 1 ? v.y : q == 2 ? v.z : v.w; };
+        uint32_t hb[kTiles][2];
+#pragma unroll
+        for (int j = 0; j < kTiles; ++j) e4m3x4_half(word(vb[u][j]), hb[j][0], hb[j][1]);
+#pragma unroll
+        for (int i = 0; i < kRowTiles; ++i) {
+          uint32_t h0[2], h1[2];
+          e4m3x4_half(word(va[u][i][0]), h0[0], h0[1]);
+          e4m3x4_half(word(va[u][i][1]), h1[0], h1[1]);
+#pragma unroll
+          for (int j = 0; j < kTiles; ++j) mma<kKind>(acc[i][j], h0[0], h1[0], h0[1], h1[1], hb[j][0], hb[j][1]);
         }
       }
+    } else {
+#pragma unroll
+      for (int i = 0; i < kRowTiles; ++i)
+#pragma unroll
+        for (int j = 0; j < kTiles; ++j) {
+          const uint4 &x = va[u][i][0], &y = va[u][i][1], &b = vb[u][j];
+          mma<kKind>(acc[i][j], x.x, y.x, x.y, y.y, b.x, b.y);
+          mma<kKind>(acc[i][j], x.z, y.z, x.w, y.w, b.z, b.w);
+        }
+    }
+  };
+#pragma unroll
+  for (int u = 0; u < kUnroll; ++u) load(u);
+  for (int done = left + kUnroll; done > 0; done -= kUnroll) {
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      multiply(u);   // (zeros past the last chunk)
+      load(u);
     }
   }
   // the warps' sums, in order
 #pragma unroll
-  for (int j = 0; j < kTiles; ++j) {
-    red[warp][j * 8 + 2 * t][g] = acc[j][0];
-    red[warp][j * 8 + 2 * t + 1][g] = acc[j][1];
-    red[warp][j * 8 + 2 * t][g + 8] = acc[j][2];
-    red[warp][j * 8 + 2 * t + 1][g + 8] = acc[j][3];
-  }
+  for (int i = 0; i < kRowTiles; ++i)
+#pragma unroll
+    for (int j = 0; j < kTiles; ++j)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) red[warp][j * 8 + 2 * t + (k & 1)][i * kBlock + g + 8 * (k >> 1)] = acc[i][j][k];
   __syncthreads();
   auto cta_sum = [&](int m, int r) {
     float v = 0.0f;
@@ -222,17 +308,16 @@ __global__ void __launch_bounds__(kMaxWarps * 32) few_kernel(const FewParams p) 
       part[i / kRows][i % kRows] = cta_sum(i / kRows, i % kRows);
     cluster_sync();
   }
-  // sixteen neighbouring threads finish a token's sixteen outputs; of a cluster's CTAs
-  // each takes every split-th token
-  constexpr bool kF16 = kKind == Kind::kFp16;
-  const bool requant = p.next_scale != nullptr;
-  const float s_next = requant ? *p.next_scale : 1.0f;
+  // sixteen neighbouring threads finish a token's sixteen outputs
   const float s_enc = encode_scale(s_next);
   if (requant && blockIdx.x == 0 && threadIdx.x == 0 && p.rq_tensor_scale != p.next_scale)
     *p.rq_tensor_scale = s_next;
-  for (int i = threadIdx.x; i < kTiles * 8 * kRows; i += blockDim.x) {
+#pragma unroll
+  for (int k = 0; k < kOuts; ++k) {
+    const int i = threadIdx.x + k * blockDim.x;
+    if (i >= kTiles * 8 * kRows) break;   // (whole warps)
     const int m = i / kRows, r = i % kRows;
-    const bool own = m < p.M && (p.split == 1 || m % p.split == rank);   // for all sixteen
+    const bool own = o_own[k];
     const int64_t n = n0 + r;
     float v = 0.0f;
     if (own) {
@@ -241,21 +326,17 @@ __global__ void __launch_bounds__(kMaxWarps * 32) few_kernel(const FewParams p) 
       } else {
         for (int q = 0; q < p.split; ++q) v = __fadd_rn(v, ld_cluster(mapa_shared(&part[m][r], q)));
       }
-      if constexpr (kFp4)
-        v = __fmul_rn(v, __fmul_rn(*p.sdec_a, *p.sdec_w));
-      else if constexpr (kKind == Kind::kFp8)
-        v = __fmul_rn(v, __fmul_rn(p.sdec_a[p.a_per_row ? m : 0], p.sdec_w[p.w_per_channel ? n : 0]));
-      if (p.bias != nullptr) v = __fadd_rn(v, load16f(p.bias + n, kF16));
+      v = __fadd_rn(__fmul_rn(v, o_scale[k]), o_bias[k]);
       float2 one[1] = {make_float2(v, v)};
       activate(one, p.act);
-      v = one[0].x;
-      if (p.residual != nullptr) v = __fadd_rn(v, load16f(p.residual + m * p.residual_stride + n, kF16));
+      v = __fadd_rn(one[0].x, o_res[k]);
     }
     const uint32_t bits = (kF16 ? pack_f16x2(v, 0.0f) : pack_bf16x2(v, 0.0f)) & 0xFFFFu;
     if (own && p.y != nullptr) p.y[m * p.N + n] = (uint16_t)bits;
-    if (kF16 || kKind == Kind::kBf16 || !requant) continue;
+    if (!requant) continue;
     const int64_t col = n - p.rq_col0;
-    const bool inside = own && n0 >= p.rq_col0 && n0 + kRows <= p.rq_col0 + p.rq_cols;
+    const int64_t b0 = n - r % kBlock;   // of the sixteen
+    const bool inside = own && b0 >= p.rq_col0 && b0 + kBlock <= p.rq_col0 + p.rq_cols;
     const float y16 = __uint_as_float(bits << 16);
     if constexpr (kKind == Kind::kFp8) {
       if (inside) p.rq_codes[m * p.rq_cols + col] = (uint8_t)e4m3_code(__fmul_rn(y16, s_enc));
@@ -268,23 +349,62 @@ __global__ void __launch_bounds__(kMaxWarps * 32) few_kernel(const FewParams p) 
       const float q = __fmul_rn(y16, r_b), q1 = __shfl_down_sync(0xFFFFFFFFu, q, 1);
       const float f[8] = {q, q1, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
       if (inside && (r & 1) == 0) p.rq_codes[m * (p.rq_cols / 2) + col / 2] = (uint8_t)e2m1x8(f);
-      if (inside && r == 0) p.rq_scales[scale_offset(m, col / 16, p.rq_cols)] = (uint8_t)code;
+      if (inside && r % kBlock == 0) p.rq_scales[scale_offset(m, col / 16, p.rq_cols)] = (uint8_t)code;
     }
   }
   if (p.split > 1) cluster_sync();   // no CTA leaves while another reads its sums
 }
 
-template <Kind kKind>
-cudaError_t launch_kind(FewParams p, cudaStream_t s, int num_sms) {
-  // Warps that share 16 rows of W: as many as fill the machine once (32 per SM), at most
-  // one per two chunks of K; beyond a CTA's eight they spread over a cluster.
-  const int64_t groups = p.N / kRows;
-  const int64_t chunks = ((kKind == Kind::kNvfp4 ? p.K / 2 : kKind == Kind::kFp8 ? p.K : p.K * 2) + kChunk - 1) / kChunk;
-  const int64_t want = std::max<int64_t>(1, std::min<int64_t>({(int64_t)num_sms * FW / groups, (chunks + 1) / 2,
-                                                              (int64_t)kMaxWarps * kMaxSplit}));
-  p.split = (int)((want + kMaxWarps - 1) / kMaxWarps);
-  const int warps = (int)std::max<int64_t>(2, want / p.split);
-  auto kern = p.M <= 8 ? few_kernel<kKind, 1> : few_kernel<kKind, 2>;
+// How a launch splits its work: row tiles per CTA, warps per CTA, CTAs per cluster.
+struct Split {
+  int row_tiles, warps, ctas;
+};
+
+// One wave: CTAs have a fixed cost (16 x 12288 x 3072 NVFP4 with 768 CTAs on 760 places
+// 12.0 us, with 384 of twice the rows 10.0), so the warps that share rows are as many as
+// stay resident together (`resident` warps per SM of each row tiling), at most one per
+// four chunks of K.  A cluster's barriers cost about a microsecond: they pay where they
+// give sixteen warps or more (FP8 8 x 3072 x 12288 10.5 -> 9.8 us with two CTAs of eight,
+// fp16 2 x 1024 x 2560 4.65 -> 4.1; bf16 16 x 3072 x 3072 7.05 -> 8.3).
+Split choose_split(int64_t N, int64_t chunks, const int (&resident)[2], int num_sms) {
+  const int most = (int)std::max<int64_t>(kMinWarps, std::min<int64_t>((chunks + 3) / 4, kMaxWarps * kMaxSplit));
+  Split best{1, kMinWarps, 1};
+  for (int rt = 1; rt <= 2; ++rt) {
+    const int64_t groups = N / (kBlock * rt);
+    bool fits = false;
+    for (int ctas = 1; ctas <= kMaxSplit; ++ctas)
+      for (int w = kMinWarps; w <= kMaxWarps; ++w) {
+        if (w * ctas > most || groups * ctas > (int64_t)num_sms * (resident[rt - 1] / w)) continue;
+        if (ctas > 1 && w * ctas < 16) continue;
+        if (!fits || w * ctas > best.warps * best.ctas) best = {rt, w, ctas};
+        fits = true;
+      }
+    if (fits) return best;
+  }
+  return {2, kMinWarps, 1};
+}
+
+template <Kind kKind, int kTiles>
+cudaError_t launch_tiles(FewParams p, cudaStream_t s, Device dev) {
+  static constexpr void (*kKernels[2])(FewParams) = {few_kernel<kKind, kTiles, 1>, few_kernel<kKind, kTiles, 2>};
+  struct Setup {
+    cudaError_t err;
+    int resident[2];
+  };
+  static PerDevice<Setup> per_device;
+  const Setup& setup = per_device.get(dev.index, [&] {
+    Setup t{cudaSuccess, {0, 0}};
+    for (int i = 0; i < 2 && t.err == cudaSuccess; ++i) {
+      int blocks = 0;
+      t.err = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&blocks, kKernels[i], kMinWarps * 32, 0);
+      t.resident[i] = blocks * kMinWarps;
+    }
+    return t;
+  });
+  if (setup.err != cudaSuccess) return setup.err;
+  const int64_t row = kKind == Kind::kNvfp4 ? p.K / 2 : kKind == Kind::kFp8 ? p.K : p.K * 2;
+  const Split split = choose_split(p.N, (row + kChunk - 1) / kChunk, setup.resident, dev.num_sms);
+  p.split = split.ctas;
   cudaLaunchConfig_t cfg{};
   cudaLaunchAttribute at[2];
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -293,17 +413,22 @@ cudaError_t launch_kind(FewParams p, cudaStream_t s, int num_sms) {
   at[1].val.clusterDim.x = (unsigned)p.split;
   at[1].val.clusterDim.y = 1;
   at[1].val.clusterDim.z = 1;
-  cfg.gridDim = dim3((unsigned)(groups * p.split), 1, 1);
-  cfg.blockDim = dim3((unsigned)warps * 32, 1, 1);
+  cfg.gridDim = dim3((unsigned)(p.N / (kBlock * split.row_tiles) * p.split), 1, 1);
+  cfg.blockDim = dim3((unsigned)split.warps * 32, 1, 1);
   cfg.stream = s;
   cfg.attrs = at;
   cfg.numAttrs = p.split > 1 ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, kern, p);
+  return cudaLaunchKernelEx(&cfg, kKernels[split.row_tiles - 1], p);
+}
+
+template <Kind kKind>
+cudaError_t launch_kind(const FewParams& p, cudaStream_t s, Device dev) {
+  return p.M <= 8 ? launch_tiles<kKind, 1>(p, s, dev) : launch_tiles<kKind, 2>(p, s, dev);
 }
 
 }  // namespace
 
-cudaError_t launch_few(const GemmArgs& a, cudaStream_t s, int num_sms) {
+cudaError_t launch_few(const GemmArgs& a, cudaStream_t s, Device dev) {
   FewParams p{};
   p.a = static_cast<const uint8_t*>(a.a_codes);
   p.a_row = a.bf16 ? a.a_row_bytes : a.fp4 ? a.K / 2 : a.K;
@@ -328,9 +453,9 @@ cudaError_t launch_few(const GemmArgs& a, cudaStream_t s, int num_sms) {
   p.rq_tensor_scale = a.rq_tensor_scale;
   p.rq_col0 = a.rq_col0;
   p.rq_cols = a.rq_cols;
-  return a.bf16 ? (a.fp16 ? launch_kind<Kind::kFp16>(p, s, num_sms) : launch_kind<Kind::kBf16>(p, s, num_sms))
-         : a.fp4 ? launch_kind<Kind::kNvfp4>(p, s, num_sms)
-                 : launch_kind<Kind::kFp8>(p, s, num_sms);
+  return a.bf16 ? (a.fp16 ? launch_kind<Kind::kFp16>(p, s, dev) : launch_kind<Kind::kBf16>(p, s, dev))
+         : a.fp4 ? launch_kind<Kind::kNvfp4>(p, s, dev)
+                 : launch_kind<Kind::kFp8>(p, s, dev);
 }
 
 }  // namespace qlin

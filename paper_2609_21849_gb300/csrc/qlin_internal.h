@@ -119,7 +119,7 @@ cudaError_t launch_gemm(const GemmArgs& a, cudaStream_t s, Device dev, unsigned*
                         uint64_t timeout_ns);
 // The same for at most kFewTokens rows of A (qlin_few.cu; no output amax).
 constexpr int kFewTokens = 16;
-cudaError_t launch_few(const GemmArgs& a, cudaStream_t s, int num_sms);
+cudaError_t launch_few(const GemmArgs& a, cudaStream_t s, Device dev);
 cudaError_t launch_wait_selftest(uint64_t timeout_ns, cudaStream_t s, unsigned* err);
 
 // Resolves cuTensorMapEncodeTiled through the runtime (no libcuda link).
