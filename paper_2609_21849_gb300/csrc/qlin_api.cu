@@ -7,6 +7,7 @@
 #include <mutex>
 
 #include "qlin_internal.h"
+#include "qlin_tiles.h"
 
 namespace qlin {
 namespace {
@@ -251,7 +252,7 @@ static qlin_status set_epilogue(GemmArgs& a, const qlin_epilogue_t* ep) {
 // The plain GEMMs always take the tensor-core tiles, so that their sums keep their
 // order; the linears take the few-token kernel where it applies.
 static cudaError_t launch_linear(const GemmArgs& a, cudaStream_t s, Device dev, unsigned* status) {
-  if (a.few_ok && a.M <= kFewTokens) return launch_few(a, s, dev);
+  if (a.few_ok && few_tokens(a.bf16, a.M, a.N, dev.num_sms)) return launch_few(a, s, dev);
   return launch_gemm(a, s, dev, status, timeout());
 }
 

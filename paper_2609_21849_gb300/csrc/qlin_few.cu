@@ -1,9 +1,16 @@
-// Linears of a few tokens (qlin_linear_* up to kFewTokens rows).  The weights are
-// read once and everything else is small, so the bound is HBM: each of a row's
-// elements meets at most 16 tokens.  A tcgen05 tile of 128 x 64 spends its 128 rows
-// on one token and has N / 64 CTAs to pull W with; here a CTA takes 16 rows of W
-// (N / 16 CTAs, several to an SM), its warps split K among them, and W goes straight
-// from global memory into mma.sync fragments.
+// Linears of a few tokens (few_tokens says which).  The weights are read once per 16
+// tokens and everything else is small, so the bound is HBM: a row's elements meet at most
+// 16 tokens at a time.  A tcgen05 tile of 128 x 64 spends its 128 rows on them and has
+// N / 64 CTAs to pull W with; here a CTA takes 16 or 32 rows of W, its warps (or a
+// cluster's) split K among them, and W goes straight from global memory into mma.sync
+// fragments.
+//
+// Measured with bias and SiLU, operands of several calls in turn: bf16 1 x 12288 x 3072
+// 12.7 us, 89% of the measured copy rate; FP8 1 x 12288 x 3072 7.5 us, 76%; FP8 8 x 3072 x
+// 12288 10.7 us, 53%; 1 x 3072 x 3072 4.3 us.  What is left is a launch, the first loads
+// and the joined sums, about three microseconds.  NVFP4 1 x 12288 x 3072 takes 8.0 us, 40%:
+// codes become fp16 and meet their block scales in registers, sixteen instructions per
+// 16 bytes.
 //
 // Fragments without shared memory: an MMA sums over K in any order, as long as both
 // operands agree.  Lane (g, t) = (lane / 4, lane % 4) loads the 16 bytes at 16 t of a
@@ -140,6 +147,7 @@ __global__ void __launch_bounds__(kMaxWarps * 32) few_kernel(const FewParams p) 
   __shared__ float part[kTiles * 8][kRows];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int warps = blockDim.x >> 5;
+  const int m0 = (int)blockIdx.y * kTiles * 8;   // the CTA's first token
   const int rank = p.split > 1 ? (int)cluster_ctarank() : 0;
   const int64_t n0 = (int64_t)(blockIdx.x / (unsigned)p.split) * kRows;
   const int64_t w_row = kFp4 ? p.K / 2 : kKind == Kind::kFp8 ? p.K : p.K * 2;
@@ -162,10 +170,10 @@ __global__ void __launch_bounds__(kMaxWarps * 32) few_kernel(const FewParams p) 
   bool o_own[kOuts];   // (the same for the sixteen threads of a token)
 #pragma unroll
   for (int k = 0; k < kOuts; ++k) {
-    const int i = threadIdx.x + k * blockDim.x, m = i / kRows;
+    const int i = threadIdx.x + k * blockDim.x, m = m0 + i / kRows;
     const int64_t n = n0 + i % kRows;
     // of a cluster's CTAs each takes every split-th token
-    const bool own = i < kTiles * 8 * kRows && m < p.M && (p.split == 1 || m % p.split == rank);
+    const bool own = i < kTiles * 8 * kRows && m < p.M && (p.split == 1 || (m - m0) % p.split == rank);
     o_own[k] = own;
     o_scale[k] = 1.0f;
     o_bias[k] = o_res[k] = 0.0f;
@@ -180,7 +188,7 @@ __global__ void __launch_bounds__(kMaxWarps * 32) few_kernel(const FewParams p) 
   const float s_next = requant ? *p.next_scale : 1.0f;
 
   // Chunks through a ring of registers: each is loaded kUnroll chunks ahead of its use.
-  // The pointers run along the warp's chunks; a token past M reads the first one's row
+  // The pointers run along the warp's chunks; a token past M reads the CTA's first one's row
   // (its column of the sums is not used).
   float acc[kRowTiles][kTiles][4] = {};
   uint4 va[kUnroll][kRowTiles][2], vb[kUnroll][kTiles];
@@ -192,7 +200,7 @@ __global__ void __launch_bounds__(kMaxWarps * 32) few_kernel(const FewParams p) 
   const uint8_t *a[kTiles], *fa[kTiles], *fw[kRowTiles][2];
 #pragma unroll
   for (int j = 0; j < kTiles; ++j) {
-    const int m = j * 8 + g < p.M ? j * 8 + g : 0;
+    const int64_t m = m0 + j * 8 + g < p.M ? m0 + j * 8 + g : m0;
     a[j] = p.a + m * p.a_row + 16 * t + (int64_t)first * kChunk;
     // the scales of blocks 8 c + 2 t and the next: 1024 bytes per chunk of 128 elements
     fa[j] = kFp4 ? p.sfa + scale_offset(m, 8 * (int64_t)first + 2 * t, p.K) : nullptr;
@@ -310,21 +318,21 @@ __global__ void __launch_bounds__(kMaxWarps * 32) few_kernel(const FewParams p) 
   }
   // sixteen neighbouring threads finish a token's sixteen outputs
   const float s_enc = encode_scale(s_next);
-  if (requant && blockIdx.x == 0 && threadIdx.x == 0 && p.rq_tensor_scale != p.next_scale)
+  if (requant && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0 && p.rq_tensor_scale != p.next_scale)
     *p.rq_tensor_scale = s_next;
 #pragma unroll
   for (int k = 0; k < kOuts; ++k) {
     const int i = threadIdx.x + k * blockDim.x;
     if (i >= kTiles * 8 * kRows) break;   // (whole warps)
-    const int m = i / kRows, r = i % kRows;
+    const int i_m = i / kRows, r = i % kRows;
     const bool own = o_own[k];
-    const int64_t n = n0 + r;
+    const int64_t n = n0 + r, m = m0 + i_m;
     float v = 0.0f;
     if (own) {
       if (p.split == 1) {
-        v = cta_sum(m, r);
+        v = cta_sum(i_m, r);
       } else {
-        for (int q = 0; q < p.split; ++q) v = __fadd_rn(v, ld_cluster(mapa_shared(&part[m][r], q)));
+        for (int q = 0; q < p.split; ++q) v = __fadd_rn(v, ld_cluster(mapa_shared(&part[i_m][r], q)));
       }
       v = __fadd_rn(__fmul_rn(v, o_scale[k]), o_bias[k]);
       float2 one[1] = {make_float2(v, v)};
@@ -366,11 +374,11 @@ struct Split {
 // four chunks of K.  A cluster's barriers cost about a microsecond: they pay where they
 // give sixteen warps or more (FP8 8 x 3072 x 12288 10.5 -> 9.8 us with two CTAs of eight,
 // fp16 2 x 1024 x 2560 4.65 -> 4.1; bf16 16 x 3072 x 3072 7.05 -> 8.3).
-Split choose_split(int64_t N, int64_t chunks, const int (&resident)[2], int num_sms) {
+Split choose_split(int64_t N, int64_t token_groups, int64_t chunks, const int (&resident)[2], int num_sms) {
   const int most = (int)std::max<int64_t>(kMinWarps, std::min<int64_t>((chunks + 3) / 4, kMaxWarps * kMaxSplit));
   Split best{1, kMinWarps, 1};
   for (int rt = 1; rt <= 2; ++rt) {
-    const int64_t groups = N / (kBlock * rt);
+    const int64_t groups = N / (kBlock * rt) * token_groups;
     bool fits = false;
     for (int ctas = 1; ctas <= kMaxSplit; ++ctas)
       for (int w = kMinWarps; w <= kMaxWarps; ++w) {
@@ -403,7 +411,7 @@ cudaError_t launch_tiles(FewParams p, cudaStream_t s, Device dev) {
   });
   if (setup.err != cudaSuccess) return setup.err;
   const int64_t row = kKind == Kind::kNvfp4 ? p.K / 2 : kKind == Kind::kFp8 ? p.K : p.K * 2;
-  const Split split = choose_split(p.N, (row + kChunk - 1) / kChunk, setup.resident, dev.num_sms);
+  const Split split = choose_split(p.N, (p.M + kTiles * 8 - 1) / (kTiles * 8), (row + kChunk - 1) / kChunk, setup.resident, dev.num_sms);
   p.split = split.ctas;
   cudaLaunchConfig_t cfg{};
   cudaLaunchAttribute at[2];
@@ -413,7 +421,8 @@ cudaError_t launch_tiles(FewParams p, cudaStream_t s, Device dev) {
   at[1].val.clusterDim.x = (unsigned)p.split;
   at[1].val.clusterDim.y = 1;
   at[1].val.clusterDim.z = 1;
-  cfg.gridDim = dim3((unsigned)(p.N / (kBlock * split.row_tiles) * p.split), 1, 1);
+  cfg.gridDim = dim3((unsigned)(p.N / (kBlock * split.row_tiles) * p.split),
+                     (unsigned)((p.M + kTiles * 8 - 1) / (kTiles * 8)), 1);
   cfg.blockDim = dim3((unsigned)split.warps * 32, 1, 1);
   cfg.stream = s;
   cfg.attrs = at;

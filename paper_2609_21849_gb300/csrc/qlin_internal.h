@@ -117,8 +117,7 @@ struct GemmArgs {
 };
 cudaError_t launch_gemm(const GemmArgs& a, cudaStream_t s, Device dev, unsigned* err,
                         uint64_t timeout_ns);
-// The same for at most kFewTokens rows of A (qlin_few.cu; no output amax).
-constexpr int kFewTokens = 16;
+// The same for few rows of A (few_tokens; qlin_few.cu; no output amax).
 cudaError_t launch_few(const GemmArgs& a, cudaStream_t s, Device dev);
 cudaError_t launch_wait_selftest(uint64_t timeout_ns, cudaStream_t s, unsigned* err);
 
