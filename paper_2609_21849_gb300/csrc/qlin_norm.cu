@@ -126,7 +126,7 @@ __device__ __forceinline__ float2 row_reduce(float a, float m, float2* red) {
 // instead (2^-80 times the largest sum of two 16-bit values squares to 2^98).
 constexpr float kDown = 0x1p-80f;
 __device__ __forceinline__ float inverse_rms(float ss, float one_over_K, float eps) {
-  return rsqrtf(__fmaf_rn(ss, one_over_K, eps));
+  return __frsqrt_rn(__fmaf_rn(ss, one_over_K, eps));
 }
 
 // The output of a chunk: 16-bit values, FP8 codes of n * s_enc, or half an NVFP4 block

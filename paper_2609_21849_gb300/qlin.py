@@ -470,33 +470,49 @@ def _empty(shape, dtype, device, stream):
         return torch.empty(shape, dtype=dtype, device=device)
 
 
-def _rows16(t, name, dtype, M, K, device):
-    """The row stride of a 16-bit [M, K] matrix whose columns are adjacent."""
-    if (t.dtype != dtype or t.dim() != 2 or t.shape[0] != M or t.shape[1] != K or t.device != device
-            or (t.stride(1) != 1 and K > 1)):
-        raise ValueError(f"{name}: expected a {dtype} [{M}, {K}] tensor on {device} with unit column stride")
-    return t.stride(0) if M > 1 else K
+# The checks below read each attribute of a tensor once and compare device indices, not
+# device objects: a call's host time is a few microseconds.
+
+def _rows16(t, name, dtype, M, K, dev):
+    """The row stride of a 16-bit [M, K] matrix on device `dev` with adjacent columns."""
+    if t.dtype is dtype and t.get_device() == dev:
+        shape = t.shape
+        if len(shape) == 2 and shape[0] == M and shape[1] == K:
+            s0, s1 = t.stride()
+            if s1 == 1 or K <= 1:
+                return s0 if M > 1 else K
+    raise ValueError(f"{name}: expected a {dtype} [{M}, {K}] tensor on cuda:{dev} with unit column stride")
 
 
-def _vector16(t, name, dtype, n, device):
-    if t.dtype != dtype or t.dim() != 1 or t.shape[0] != n or t.device != device or (t.stride(0) != 1 and n > 1):
-        raise ValueError(f"{name}: expected a contiguous {dtype} [{n}] tensor on {device}")
+def _vector16(t, name, dtype, n, dev):
+    shape = t.shape
+    if (t.dtype is not dtype or len(shape) != 1 or shape[0] != n or t.get_device() != dev
+            or not t.is_contiguous()):
+        raise ValueError(f"{name}: expected a contiguous {dtype} [{n}] tensor on cuda:{dev}")
+    return t.data_ptr()
+
+
+def _dense16(t, name, dtype, M, N, dev):
+    shape = t.shape
+    if (t.dtype is not dtype or len(shape) != 2 or shape[0] != M or shape[1] != N or t.get_device() != dev
+            or not t.is_contiguous()):
+        raise ValueError(f"{name}: expected a contiguous {dtype} [{M}, {N}] tensor on cuda:{dev}")
     return t.data_ptr()
 
 
 def _rmsnorm_args(x, weight, residual, eps, sum_out, stream):
     """(packed arguments, M, K, sum) of a norm call; sum is allocated where a
     residual comes without one."""
-    dt = _FLOAT16.get(x.dtype)
-    if dt is None or x.dim() != 2 or not x.is_cuda:
+    dtype, dev, shape = x.dtype, x.get_device(), x.shape
+    dt = _FLOAT16.get(dtype)
+    if dt is None or len(shape) != 2 or dev < 0:
         raise ValueError("x: expected a 2-D bf16 or fp16 CUDA tensor")
-    M, K = x.shape
-    dtype, dev = x.dtype, x.device
+    M, K = shape
     xs, rs, ss, rp, sp = _rows16(x, "x", dtype, M, K, dev), 0, 0, 0, 0
     if residual is not None:
         rs, rp = _rows16(residual, "residual", dtype, M, K, dev), residual.data_ptr()
         if sum_out is None:
-            sum_out = _empty((M, K), dtype, dev, stream)
+            sum_out = _empty((M, K), dtype, x.device, stream)
         ss, sp = _rows16(sum_out, "sum_out", dtype, M, K, dev), sum_out.data_ptr()
     elif sum_out is not None:
         raise ValueError("sum_out without a residual")
@@ -513,9 +529,8 @@ def qlin_rmsnorm(x: torch.Tensor, weight: torch.Tensor | None = None,
     args, M, K, sum_out = _rmsnorm_args(x, weight, residual, eps, sum_out, stream)
     if y is None:
         y = _empty((M, K), x.dtype, x.device, stream)
-    elif y.dtype != x.dtype or y.shape != x.shape or not y.is_contiguous() or y.device != x.device:
-        raise ValueError(f"y: expected a contiguous {x.dtype} [{M}, {K}] tensor on {x.device}")
-    _check(_library().packed.qlin_rmsnorm(args, y.data_ptr(), _stream(stream)), "qlin_rmsnorm")
+    _check(_library().packed.qlin_rmsnorm(args, _dense16(y, "y", x.dtype, M, K, x.get_device()),
+                                          _stream(stream)), "qlin_rmsnorm")
     return y, sum_out
 
 
@@ -553,26 +568,27 @@ def qlin_rmsnorm_nvfp4(x: torch.Tensor, static_scale: torch.Tensor, weight: torc
     return out, sum_out
 
 
-def _epilogue(bias, act, residual, dtype, M, N, device):
-    """The packed epilogue of a linear with an [M, N] output."""
-    bp = 0 if bias is None else _vector16(bias, "bias", dtype, N, device)
+def _epilogue(bias, act, residual, dtype, M, N, dev):
+    """The packed epilogue of a linear with an [M, N] output; None where it is empty."""
     if residual is None:
-        return _pack_epilogue(bp, 0, 0, act)
-    return _pack_epilogue(bp, residual.data_ptr(), _rows16(residual, "residual", dtype, M, N, device), act)
+        if bias is None and act == QLIN_ACT_NONE:
+            return None
+        return _pack_epilogue(0 if bias is None else _vector16(bias, "bias", dtype, N, dev), 0, 0, act)
+    return _pack_epilogue(0 if bias is None else _vector16(bias, "bias", dtype, N, dev), residual.data_ptr(),
+                          _rows16(residual, "residual", dtype, M, N, dev), act)
 
 
-def _linear_quantized(name, pack, A, W, bias, act, residual, y, next_scale, y_q, rq_col0, device, stream):
-    M, N = A.rows, W.rows
+def _linear_quantized(name, pack, A, W, bias, act, residual, y, next_scale, y_q, rq_col0, stream):
+    M, N, codes = A.rows, W.rows, A.codes
+    dev = codes.get_device()
     if (y_q is None) != (next_scale is None):
         raise ValueError("next_scale and y_q come together")
-    if y is None:
-        if y_q is None:
-            y = _empty((M, N), torch.bfloat16, device, stream)
-    elif y.dtype != torch.bfloat16 or y.shape != (M, N) or not y.is_contiguous() or y.device != device:
-        raise ValueError(f"y: expected a contiguous bf16 [{M}, {N}] tensor on {device}")
-    ep = _epilogue(bias, act, residual, torch.bfloat16, M, N, device)
+    if y is None and y_q is None:
+        y = _empty((M, N), torch.bfloat16, codes.device, stream)
+    yp = None if y is None else _dense16(y, "y", torch.bfloat16, M, N, dev)
+    ep = _epilogue(bias, act, residual, torch.bfloat16, M, N, dev)
     _check(getattr(_library().packed, name)(
-        pack(A), pack(W), ep, _ptr(y), _ptr(next_scale), None if y_q is None else pack(y_q), rq_col0,
+        pack(A), pack(W), ep, yp, _ptr(next_scale), None if y_q is None else pack(y_q), rq_col0,
         _stream(stream)), name)
     return y, y_q
 
@@ -586,7 +602,7 @@ def qlin_linear_nvfp4(A: NVFP4Tensor, W: NVFP4Tensor, bias: torch.Tensor | None 
     Returns (y, y_q); y None is allocated, or not written where y_q is given.
     residual may be y."""
     return _linear_quantized("qlin_linear_nvfp4", _nvfp4, A, W, bias, act, residual, y, next_scale, y_q,
-                             rq_col0, A.codes.device, stream)
+                             rq_col0, stream)
 
 
 def qlin_linear_fp8(A: FP8Tensor, W: FP8Tensor, bias: torch.Tensor | None = None,
@@ -595,23 +611,22 @@ def qlin_linear_fp8(A: FP8Tensor, W: FP8Tensor, bias: torch.Tensor | None = None
                     y_q: FP8Tensor | None = None, rq_col0: int = 0, stream=None):
     """As qlin_linear_nvfp4 with FP8 operands; A has one scale or one per row."""
     return _linear_quantized("qlin_linear_fp8", _fp8, A, W, bias, act, residual, y, next_scale, y_q,
-                             rq_col0, A.codes.device, stream)
+                             rq_col0, stream)
 
 
 def _linear16(name, dtype, a, w, bias, act, residual, y, stream):
-    if a.dtype != dtype or a.dim() != 2 or not a.is_cuda:
+    dev, shape = a.get_device(), a.shape
+    if a.dtype is not dtype or len(shape) != 2 or dev < 0:
         raise ValueError(f"a: expected a 2-D {dtype} CUDA tensor")
-    if w.dtype != dtype or w.dim() != 2 or w.shape[1] != a.shape[1] or not w.is_contiguous() or w.device != a.device:
-        raise ValueError(f"w: expected a contiguous {dtype} [N, {a.shape[1]}] tensor on {a.device}")
-    (M, K), N, dev = a.shape, w.shape[0], a.device
+    M, K = shape
+    N = w.shape[0]
+    wp = _dense16(w, "w", dtype, N, K, dev)
     lda = _rows16(a, "a", dtype, M, K, dev)
     if y is None:
-        y = _empty((M, N), dtype, dev, stream)
-    elif y.dtype != dtype or y.shape != (M, N) or not y.is_contiguous() or y.device != dev:
-        raise ValueError(f"y: expected a contiguous {dtype} [{M}, {N}] tensor on {dev}")
-    ep = _epilogue(bias, act, residual, dtype, M, N, dev)
-    _check(getattr(_library().packed, name)(a.data_ptr(), lda, w.data_ptr(), M, N, K, ep, y.data_ptr(),
-                                            _stream(stream)), name)
+        y = _empty((M, N), dtype, a.device, stream)
+    _check(getattr(_library().packed, name)(a.data_ptr(), lda, wp, M, N, K,
+                                            _epilogue(bias, act, residual, dtype, M, N, dev),
+                                            _dense16(y, "y", dtype, M, N, dev), _stream(stream)), name)
     return y
 
 
@@ -682,30 +697,32 @@ def qlin_rope(x: torch.Tensor, positions: torch.Tensor, plan: RopePlan, out: tor
     columns of a QKV output) with its rotary positions applied, or taken back
     (inverse: also the gradient).  positions: int32 or int64 [tokens], or [tokens,
     axes] for a plan of several axes.  out may be x."""
-    dt = _FLOAT16.get(x.dtype)
-    if dt is None or x.dim() != 3 or not x.is_cuda or (x.stride(2) != 1 and x.shape[2] > 1):
+    dtype, dev, shape = x.dtype, x.get_device(), x.shape
+    dt = _FLOAT16.get(dtype)
+    xs = x.stride()
+    if dt is None or len(shape) != 3 or dev < 0 or (xs[2] != 1 and shape[2] > 1):
         raise ValueError("x: expected a bf16 or fp16 [tokens, heads, head_dim] CUDA tensor with contiguous heads")
-    T, H, D = x.shape
-    axes = len(plan.axis_pairs)
-    if (positions.dtype not in (torch.int32, torch.int64) or positions.device != x.device
-            or positions.shape != ((T, axes) if positions.dim() == 2 else (T,))
-            or (positions.dim() == 1 and axes != 1)):
-        raise ValueError(f"positions: expected int32 or int64 [{T}, {axes}] on {x.device}")
-    turns = plan.turns
-    if turns.dtype != torch.int64 or turns.dim() != 1 or not turns.is_contiguous() or turns.device != x.device:
-        raise ValueError(f"plan.turns: expected a contiguous int64 vector on {x.device}")
-    if not 1 <= axes <= 4 or plan.layout not in _LAYOUTS:
+    T, H, D = shape
+    pairs, turns, layout = plan.axis_pairs, plan.turns, _LAYOUTS.get(plan.layout)
+    axes = len(pairs)
+    ps, pdt, pst = positions.shape, positions.dtype, positions.stride()
+    if ((pdt is not torch.int32 and pdt is not torch.int64) or positions.get_device() != dev
+            or not (ps == (T, axes) or (axes == 1 and ps == (T,)))):
+        raise ValueError(f"positions: expected int32 or int64 [{T}, {axes}] on cuda:{dev}")
+    if turns.dtype is not torch.int64 or turns.dim() != 1 or not turns.is_contiguous() or turns.get_device() != dev:
+        raise ValueError(f"plan.turns: expected a contiguous int64 vector on cuda:{dev}")
+    if not 1 <= axes <= 4 or layout is None:
         raise ValueError("plan: one to four axes, layout 'interleaved' or 'half'")
     if out is None:
-        out = _empty((T, H, D), x.dtype, x.device, stream)
-    elif out.dtype != x.dtype or out.shape != x.shape or out.device != x.device or (out.stride(2) != 1 and D > 1):
-        raise ValueError(f"out: expected a {x.dtype} {list(x.shape)} tensor on {x.device} with contiguous heads")
-    pairs = plan.axis_pairs + (0,) * (4 - axes)
+        out = _empty((T, H, D), dtype, x.device, stream)
+    os_ = out.stride()
+    if out.dtype is not dtype or out.shape != shape or out.get_device() != dev or (os_[2] != 1 and D > 1):
+        raise ValueError(f"out: expected a {dtype} {list(shape)} tensor on cuda:{dev} with contiguous heads")
     _check(_library().packed.qlin_rope(_pack_rope(
-        x.data_ptr(), out.data_ptr(), x.stride(0), x.stride(1), out.stride(0), out.stride(1), T, H,
-        positions.data_ptr(), positions.stride(0), positions.stride(1) if positions.dim() == 2 else 0,
-        turns.data_ptr(), plan.magnitude, D, 2 * turns.numel(), 64 if positions.dtype == torch.int64 else 32,
-        axes, *pairs, _LAYOUTS[plan.layout], 1 if inverse else 0, dt), _stream(stream)), "qlin_rope")
+        x.data_ptr(), out.data_ptr(), xs[0], xs[1], os_[0], os_[1], T, H,
+        positions.data_ptr(), pst[0], pst[1] if len(pst) == 2 else 0,
+        turns.data_ptr(), plan.magnitude, D, 2 * turns.numel(), 64 if pdt is torch.int64 else 32,
+        axes, *pairs, *(0,) * (4 - axes), layout, 1 if inverse else 0, dt), _stream(stream)), "qlin_rope")
     return out
 
 
