@@ -1429,9 +1429,11 @@ cudaError_t launch_cfg(const GemmArgs& a, cudaStream_t s, Device dev, unsigned* 
 
 Tile tile_of(const GemmArgs& a, int num_sms) {
   return choose_tile(a.fp4 ? GemmKind::kNvfp4 : a.bf16 ? GemmKind::k16 : GemmKind::kFp8,
-                     a.next_scale != nullptr ? Epilogue::kRequant
-                     : a.y_amax != nullptr   ? Epilogue::kAmax
-                                             : Epilogue::kPlain,
+                     a.epilogue              ? (a.next_scale != nullptr ? Epilogue::kLinearRequant
+                                                                        : Epilogue::kLinear)
+                     : a.next_scale != nullptr ? Epilogue::kRequant
+                     : a.y_amax != nullptr     ? Epilogue::kAmax
+                                               : Epilogue::kPlain,
                      a.M, a.N, a.K, num_sms);
 }
 

@@ -14,8 +14,8 @@ constexpr int kStageRowBytes = 128; // bytes of K per pipeline stage and row
 enum class Tile { kPair, kSingle, kNarrow };   // 256 x 256, 128 x 128, 128 x 64
 enum class GemmKind { kNvfp4, kFp8, k16 };     // k16: bf16 / fp16 operands
 
-// What the epilogue does beside writing y.
-enum class Epilogue { kPlain, kRequant, kAmax };
+// What the epilogue does beside writing y (kLinear: bias, activation and residual).
+enum class Epilogue { kPlain, kRequant, kAmax, kLinear, kLinearRequant };
 
 // Time of a launch in a tile configuration, in microseconds: a launch, then
 // waves of tiles that each cost a start and end and their K stages.  Fitted
@@ -23,9 +23,10 @@ enum class Epilogue { kPlain, kRequant, kAmax };
 // in L2; rms error 5-9%).
 struct TileCost {
   double launch, wave, stage;
-  double us(int64_t tiles, int64_t slots, int64_t stages, double wave_extra) const {
-    return launch +
-           (double)((tiles + slots - 1) / slots) * (wave + wave_extra + (double)stages * stage);
+  double us(int64_t tiles, int64_t slots, int64_t stages, double wave_extra,
+            double wave_least = 0.0) const {
+    return launch + (double)((tiles + slots - 1) / slots) *
+                        std::max(wave + wave_extra + (double)stages * stage, wave_least);
   }
 };
 
@@ -49,7 +50,9 @@ inline Tile choose_tile(GemmKind kind, Epilogue epi, int64_t M, int64_t N, int64
   const bool fp4 = kind == GemmKind::kNvfp4;
   // the fused re-quantization's 64-column groups need 128-column tiles, and no
   // 16-bit kernel has narrow ones
-  const bool narrow_ok = epi != Epilogue::kRequant && kind != GemmKind::k16;
+  const bool linear = epi == Epilogue::kLinear || epi == Epilogue::kLinearRequant;
+  const bool narrow_ok =
+      epi != Epilogue::kRequant && epi != Epilogue::kLinearRequant && kind != GemmKind::k16;
   const TileCost* cost = kCosts[(int)kind];
   const int64_t k_bytes = fp4 ? K / 2 : kind == GemmKind::k16 ? K * 2 : K;
   const int64_t stages = (k_bytes + kStageRowBytes - 1) / kStageRowBytes;
@@ -60,9 +63,14 @@ inline Tile choose_tile(GemmKind kind, Epilogue epi, int64_t M, int64_t N, int64
   // short K chains took single tiles where pairs are faster (NVFP4 9216 x 3072 x 64:
   // 33.0 us, single tiles 37.6).
   const double wave_extra = epi == Epilogue::kAmax ? 0.2 : 0.0;
-  double us[3] = {cost[0].us((tiles_m + 1) / 2 * n256, num_sms / 2, stages, 0.0),
-                  cost[1].us(tiles_m * n128, num_sms, stages, wave_extra),
-                  cost[2].us(tiles_m * ((N + 63) / 64), num_sms, stages, wave_extra)};
+  // With bias, activation and residual a wave takes at least its epilogue, and a pair
+  // tile, with twice the columns per thread, ends later: bf16 1500 x 6144 x 512 with GELU
+  // 15.7 us in pairs, 13.1 in single tiles; FP8 2048 x 2048 x 2048 11.9 and 10.8; NVFP4
+  // 2048 x 2048 x 2048 8.6 and 9.2.
+  double us[3] = {cost[0].us((tiles_m + 1) / 2 * n256, num_sms / 2, stages, 0.0, linear ? 4.0 : 0.0),
+                  cost[1].us(tiles_m * n128, num_sms, stages, wave_extra, linear ? 2.1 : 0.0),
+                  cost[2].us(tiles_m * ((N + 63) / 64), num_sms, stages, wave_extra, linear ? 1.2 : 0.0)};
+  if (linear) us[0] += fp4 ? 1.0 : 1.5;
   // a pair tile's re-quantizing epilogue ends about this much later
   if (epi == Epilogue::kRequant) us[0] += fp4 ? 1.0 : 0.6;
   if (epi == Epilogue::kAmax) us[0] += 1.0;
