@@ -56,12 +56,16 @@ constexpr int pow2_at_least(int x) {
 
 // kPair: a CTA pair runs one tcgen05 MMA of M = 256 (cta_group::2); each CTA
 // holds its own 128 rows of A and its own half of the W tile.
-// kHold: the epilogue's warps hold a whole accumulator in registers (setmaxnreg), so
-// that the one accumulator of an NVFP4 pair goes back to the MMAs before the
-// activations, and the other kinds have room for a tile's residual: whole warpgroups of
-// roles, then two of epilogue.
-template <bool kFp4, int kBN, bool kPair = false, bool kHold = false>
+// kLin: the epilogue of qlin_linear_* (2: with a residual).  Its pair tiles hold a whole
+// accumulator in the epilogue warps' registers (setmaxnreg), so that the one accumulator
+// of an NVFP4 pair goes back to the MMAs before the activations, and the other kinds have
+// room for a tile's residual: whole warpgroups of roles, then those of the epilogue.
+// NVFP4 without a residual has sixteen epilogue warps of 64 columns, whose exponentials
+// hide one another's latency better (4608 x 12288 x 3072 with tanh GELU, re-quantized,
+// 62.6 -> 54.9 us); with one, there are too few registers (73 -> 82).
+template <bool kFp4, int kBN, bool kPair = false, int kLin = 0>
 struct Cfg {
+  static constexpr bool kHold = kLin != 0 && kPair;
   // warps: 0 producer, 1 MMA, NVFP4: four scale warps, pairs: the scale
   // producer, then the epilogue (an epilogue or scale warp w reaches TMEM
   // lanes 32 (w % 4) and up, so any four or eight consecutive warps cover
@@ -71,7 +75,7 @@ struct Cfg {
   static constexpr int kSfProducer = kSfCopy ? 2 + kSfWarps : -1;
   static constexpr int kRoleWarps = 2 + kSfWarps + (kSfCopy ? 1 : 0);
   static constexpr int kEpiWarp0 = kHold ? (kRoleWarps + 3) / 4 * 4 : kRoleWarps;
-  static constexpr int kEpiWarps = 8;
+  static constexpr int kEpiWarps = kHold && kFp4 && kLin == 1 ? 16 : 8;
   static constexpr int kThreads = (kEpiWarp0 + kEpiWarps) * 32;
   // Row boxes per operand tile and stage: copies of separate boxes overlap
   // (pairs, 4608 x 12288 x 3072 NVFP4: one box 58.1, two 56.0, four 54.8 us).
@@ -101,7 +105,7 @@ struct Cfg {
   // the critical path and shared memory is left (the other kinds have none left, and
   // longer mainloops).
   static constexpr bool kSmemBias = kHold && kFp4;
-  static constexpr int kBiasBytes = kSmemBias ? kEpiWarps * (kBN / 2) * 4 : 0;
+  static constexpr int kBiasBytes = kSmemBias ? kEpiWarps * (kBN / (kEpiWarps / 4)) * 4 : 0;
   static constexpr int kStagesRaw = (kSmemBudget - kOutBytes - kSfBytes - kBiasBytes) / kStageBytes;
   static constexpr int kStages = kStagesRaw > 8 ? 8 : kStagesRaw;
   static constexpr int kNumAcc = (kFp4 && kBN == 256) ? 1 : 2;
@@ -129,13 +133,14 @@ struct Cfg {
   static_assert(kTmemCols <= 512, "TMEM budget");
   static_assert(kSmemBytes <= 232448, "shared memory budget");
   static_assert(kStages >= 2, "pipeline depth");
-  // Registers of the roles' warpgroups and of the two that hold accumulators; the
-  // shares add up to what the launch gives (512 threads 128 each, 384 threads 168).
-  static constexpr int kRoleRegs = 56, kHoldRegs = kFp4 ? 200 : 224;
-  static_assert(!kHold || kEpiWarp0 * 32 * kRoleRegs + kEpiWarps * 32 * kHoldRegs <=
-                              kThreads * (kThreads == 512 ? 128 : 168),
+  // Registers of the roles' warpgroups and of those that hold accumulators; the shares
+  // add up to what the launch gives.
+  static constexpr int kRoleRegs = kThreads == 768 ? 32 : 56;
+  static constexpr int kHoldRegs = kThreads == 768 ? 104 : kThreads == 512 ? 200 : 224;
+  static constexpr int kLaunchRegs = kThreads == 768 ? 80 : kThreads == 512 ? 128 : 168;
+  static_assert(!kHold || kEpiWarp0 * 32 * kRoleRegs + kEpiWarps * 32 * kHoldRegs <= kThreads * kLaunchRegs,
                 "registers");
-  static_assert(!kHold || kThreads == 512 || kThreads == 384, "whole warpgroups");
+  static_assert(!kHold || kThreads == 768 || kThreads == 512 || kThreads == 384, "whole warpgroups");
 };
 
 struct KParams {
@@ -310,15 +315,15 @@ __device__ __forceinline__ void finish32(float2 (&v)[16], const KParams& p, floa
 // kLin: the epilogue of qlin_linear_*: bias and activation before the 16-bit rounding,
 // FP8 row scales of A; kLin == 2 adds a residual.
 template <bool kFp4, int kBN, bool kPair, bool kRequant, bool kBf16 = false, int kLin = 0>
-__global__ void __launch_bounds__(Cfg<kFp4, kBN, kPair, kLin != 0 && kPair>::kThreads, 1)
+__global__ void __launch_bounds__(Cfg<kFp4, kBN, kPair, kLin>::kThreads, 1)
     gemm_kernel(const __grid_constant__ CUtensorMap tmap_a,
                 const __grid_constant__ CUtensorMap tmap_b,
                 const __grid_constant__ CUtensorMap tmap_sfa,
                 const __grid_constant__ CUtensorMap tmap_sfb,
                 const __grid_constant__ CUtensorMap tmap_y, const KParams p) {
   constexpr bool kEpi = kLin != 0, kRes = kLin == 2;
-  constexpr bool kHold = kEpi && kPair;
-  using C = Cfg<kFp4, kBN, kPair, kHold>;
+  using C = Cfg<kFp4, kBN, kPair, kLin>;
+  constexpr bool kHold = C::kHold;
   constexpr int kCM = kPair ? 2 : 1;          // CTAs per cluster (M tiles per cluster tile)
   constexpr uint16_t kMask = (uint16_t)((1u << kCM) - 1u);
   extern __shared__ uint8_t smem_raw[];
@@ -862,8 +867,8 @@ __global__ void __launch_bounds__(Cfg<kFp4, kBN, kPair, kLin != 0 && kPair>::kTh
         // r_b = S_enc / s_b of every E4M3 code, by the division that
         // defines it (one table look-up instead of a division per block:
         // 59.8 -> 59.3 us at 4608 x 12288 x 3072)
-        const uint32_t c = threadIdx.x - C::kEpiWarp0 * 32;
-        static_assert(C::kEpiWarps * 32 == 256, "one entry per epilogue thread");
+        const uint32_t c = (threadIdx.x - C::kEpiWarp0 * 32) & 255u;
+        static_assert(C::kEpiWarps * 32 >= 256, "an entry per epilogue thread");
         r_table[c] = c == 0u ? 0.0f : __fdiv_rn(s_enc_next, e4m3_value(c));
         asm volatile("bar.sync 1, %0;" ::"n"(C::kEpiWarps * 32) : "memory");
       }
@@ -1339,7 +1344,7 @@ CUresult encode_scales(CUtensorMap* map, const void* base, uint64_t rows, uint64
 template <bool kFp4, int kBN, bool kPair, bool kRequant, bool kBf16 = false, int kLin = 0>
 cudaError_t launch_cfg(const GemmArgs& a, cudaStream_t s, Device dev, unsigned* err,
                        uint64_t timeout_ns) {
-  using C = Cfg<kFp4, kBN, kPair, kLin != 0 && kPair>;
+  using C = Cfg<kFp4, kBN, kPair, kLin>;
   constexpr int kCM = kPair ? 2 : 1;
   const uint64_t k_bytes = kFp4 ? (uint64_t)a.K / 2 : kBf16 ? (uint64_t)a.K * 2 : (uint64_t)a.K;
   CUtensorMap ta, tb, tsa, tsb, ty;
