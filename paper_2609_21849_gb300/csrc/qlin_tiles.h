@@ -84,14 +84,14 @@ inline Tile choose_tile(GemmKind kind, Epilogue epi, int64_t M, int64_t N, int64
 
 // Whether a linear takes the few-token kernel, which reads W once per 16 tokens, rather
 // than the tiles above: always up to 16 tokens, beyond that as long as its groups of 16
-// rows of W and 16 tokens are at most 2.5 per SM (16-bit operands 5).  Both timed at 9
+// rows of W and 16 tokens are at most 2.6 per SM (16-bit operands 5.2).  Both timed at 9
 // weights (N 64-12288, K 512-12288), M 16-128, in us (few / tiles): NVFP4 N = K = 3072
 // M = 32 6.9 / 8.1, M = 48 8.6 / 8.2; FP8 M = 32 7.9 / 7.9, M = 48 8.9 / 7.9; bf16 M = 64
 // 13.1 / 13.7, M = 96 24.8 / 13.8; bf16 N = 64, K = 12288 M = 128 6.1 / 36; at 16 tokens
 // NVFP4 N = 12288 10.4 / 10.2, all others faster here.
 inline bool few_tokens(bool float16, int64_t M, int64_t N, int num_sms) {
   if (M <= 16) return true;
-  return M <= 128 && 2 * (N / 16) * ((M + 15) / 16) <= (int64_t)(float16 ? 10 : 5) * num_sms;
+  return M <= 128 && 10 * (N / 16) * ((M + 15) / 16) <= (int64_t)(float16 ? 52 : 26) * num_sms;
 }
 
 }  // namespace qlin

@@ -11,6 +11,10 @@ Cases (seeded synthetic inputs, shapes of the paper's workloads):
   fused_nvfp4      the same with the fused NVFP4 re-quantization
   gemm_fp8         FP8 GEMM 4608 x 3072 x 3072
   small_nvfp4      NVFP4 GEMM 512 x 2560 x 1024 (translator shape)
+  norm_fp8_rows    residual addition and norm of [4608, 3072] to FP8 rows
+  rope_qk          rotary positions of 4608 x 48 heads of 128 inside a QKV output
+  linear_up        NVFP4 linear 4608 x 12288 x 3072, bias, tanh GELU, re-quantized
+  linear_one       bf16 linear 1 x 12288 x 3072, bias and SiLU
 Prints the mean device time per launch (CUDA events, not for use under a
 profiler).
 """
@@ -63,6 +67,29 @@ def make_case(name: str):
         W = qlin.qlin_quantize_weight(_dev(w1), qlin.QLIN_FMT_NVFP4)
         y = torch.empty((A.rows, W.rows), dtype=torch.bfloat16, device="cuda")
         return lambda: qlin.qlin_gemm_nvfp4(A, W, y)
+    if name == "norm_fp8_rows":
+        x, r = _dev(synthetic.act_normal(2, 4608, 3072)), _dev(synthetic.act_normal(3, 4608, 3072))
+        out, t = qlin.alloc_fp8(4608, 3072, True), torch.empty_like(x)
+        w = torch.ones(3072, dtype=torch.bfloat16, device="cuda")
+        return lambda: qlin.qlin_rmsnorm_fp8(x, w, r, 1e-6, t, out=out)
+    if name == "rope_qk":
+        x = torch.randn(4608, 72 * 128, device="cuda").bfloat16().view(4608, 72, 128)[:, :48]
+        pos = torch.randint(0, 64, (4608, 3), device="cuda", dtype=torch.int32)
+        plan = qlin.rope_plan((16, 56, 56), layout="interleaved")
+        y = torch.empty(4608, 48, 128, dtype=torch.bfloat16, device="cuda")
+        return lambda: qlin.qlin_rope(x, pos, plan, y)
+    if name == "linear_up":
+        xb, wb = synthetic.nvfp4_mlp_up()
+        A = qlin.qlin_quantize_act_nvfp4(_dev(xb))
+        W = qlin.qlin_quantize_weight(_dev(wb), qlin.QLIN_FMT_NVFP4)
+        b = torch.zeros(W.rows, dtype=torch.bfloat16, device="cuda")
+        yq, sc = qlin.alloc_nvfp4(A.rows, W.rows), torch.tensor([np.float32(0.002)], device="cuda")
+        return lambda: qlin.qlin_linear_nvfp4(A, W, b, qlin.QLIN_ACT_GELU_TANH, None, None, sc, yq)
+    if name == "linear_one":
+        x = torch.randn(1, 3072, device="cuda").bfloat16()
+        w, b = torch.randn(12288, 3072, device="cuda").bfloat16(), torch.zeros(12288, dtype=torch.bfloat16, device="cuda")
+        y = torch.empty(1, 12288, dtype=torch.bfloat16, device="cuda")
+        return lambda: qlin.qlin_linear_bf16(x, w, b, qlin.QLIN_ACT_SILU, None, y)
     raise SystemExit(f"unknown case {name}")
 
 
