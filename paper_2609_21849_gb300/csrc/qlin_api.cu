@@ -252,7 +252,9 @@ static qlin_status set_epilogue(GemmArgs& a, const qlin_epilogue_t* ep) {
 // The plain GEMMs always take the tensor-core tiles, so that their sums keep their
 // order; the linears take the few-token kernel where it applies.
 static cudaError_t launch_linear(const GemmArgs& a, cudaStream_t s, Device dev, unsigned* status) {
-  if (a.few_ok && few_tokens(a.bf16, a.M, a.N, dev.num_sms)) return launch_few(a, s, dev);
+  // (the few-token kernel counts a row's bytes in 32 bits)
+  if (a.few_ok && few_tokens(a.bf16, a.M, a.N, dev.num_sms) && a.K <= (int64_t)1 << 28)
+    return launch_few(a, s, dev);
   return launch_gemm(a, s, dev, status, timeout());
 }
 

@@ -168,6 +168,17 @@ def test_requantized_output(M, N, K, fmt):
         assert y2 is None and torch.equal(q2.codes, q.codes)
 
 
+@pytest.mark.parametrize("M", [3, 300, 2048])
+def test_fp8_weight_with_one_scale(M):
+    # W with a tensor scale, A with one scale and with one per row
+    N, K = 4096 if M == 2048 else 320, 512
+    for fmt in ("fp8", "fp8_rows"):
+        a, w, bias, res, _ = _operands(fmt, M, N, K, 31)
+        one = qlin.qlin_quantize_act_fp8(torch.randn(N, K, device="cuda").bfloat16())
+        y, _ = qlin.qlin_linear_fp8(a, one, bias, qlin.QLIN_ACT_GELU, res)
+        _check(y, a, one, bias, qlin.QLIN_ACT_GELU, res, (fmt, M))
+
+
 @pytest.mark.parametrize("M", [1, 5, 200, 2048])
 @pytest.mark.parametrize("act", ACTS)
 def test_large_and_special_values(M, act):
