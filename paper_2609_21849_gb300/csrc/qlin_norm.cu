@@ -408,14 +408,15 @@ cudaError_t launch_out(const NormParams& p, int num_sms, cudaStream_t s) {
                           : launch_pdl(rmsnorm_held_kernel<kOut, kF16, kResidual, 4, true>, grid, 256, 0, s, p);
   }
   // Four chunks per thread halve a row's share of the reduction (18432 x 3072 fp16 to
-  // static FP8 31.0 us, with two 36.2); two leave fewer threads idle where four do not
-  // divide the row (4608 x 2560 to FP8 rows 14.5 against 16.3) and have the shorter
-  // chain where rows are few (512 x 2560 3.4 against 4.0).
+  // static FP8 31.0 us, with two 36.2; 2255 x 6208 to FP8 rows 18.2 and 20.8); two leave
+  // fewer threads idle in short rows that four do not divide (5468 x 2560 to static FP8
+  // 10.8 against 11.4) and have the shorter chain where rows are few (300 x 6208 4.1
+  // against 4.5), up to where their CTAs fill an SM (300 x 9216 6.3 against 4.9).
   if (chunks > 2048)
     return launch_pdl(rmsnorm_long_kernel<kOut, kF16, kResidual>, (unsigned)p.M, kLongThreads, 0, s, p);
-  if (chunks % 128 == 0 && p.M >= 4 * num_sms)
+  if (chunks > 1024 || (p.M >= 4 * num_sms && (chunks % 128 == 0 || chunks >= 384)))
     return launch_pdl(rmsnorm_held_kernel<kOut, kF16, kResidual, 4, false>, (unsigned)p.M,
-                      (int)(chunks / 4), 0, s, p);
+                      (int)((chunks + 127) / 128) * 32, 0, s, p);
   const int threads = (int)((chunks + 63) / 64) * 32;
   return launch_pdl(rmsnorm_held_kernel<kOut, kF16, kResidual, 2, false>, (unsigned)p.M, threads, 0, s, p);
 }
