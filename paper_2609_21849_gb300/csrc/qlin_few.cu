@@ -126,10 +126,8 @@ __device__ __forceinline__ float load16f(const uint16_t* p, bool fp16) {
   return fp16 ? __half2float(__ushort_as_half(w)) : __uint_as_float((uint32_t)w << 16);
 }
 
-__device__ __forceinline__ float ld_cluster(uint32_t addr) {
-  float v;
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
-  return v;
+__device__ __forceinline__ void st_cluster(uint32_t addr, float v) {
+  asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
 }
 
 // Chunks in flight per warp.
@@ -144,7 +142,7 @@ __global__ void __launch_bounds__(kMaxWarps * 32) few_kernel(const FewParams p) 
   constexpr int kRows = kBlock * kRowTiles, kOuts = kTiles * kRowTiles;
   constexpr int kUnroll = kUnrollOf<kKind, kTiles, kRowTiles>;
   __shared__ float red[kMaxWarps][kTiles * 8][kRows + 1];
-  __shared__ float part[kTiles * 8][kRows];
+  __shared__ float part[kMaxSplit][kTiles * 8][kRows];   // the cluster's sums of this CTA's tokens
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int warps = blockDim.x >> 5;
   const int m0 = (int)blockIdx.y * kTiles * 8;   // the CTA's first token
@@ -153,6 +151,8 @@ __global__ void __launch_bounds__(kMaxWarps * 32) few_kernel(const FewParams p) 
   const int64_t w_row = kFp4 ? p.K / 2 : kKind == Kind::kFp8 ? p.K : p.K * 2;
   const int chunks = (int)((w_row + kChunk - 1) / kChunk);
   const int stride = warps * p.split;   // warps that share the rows
+  // every CTA of the cluster runs before one writes into another's shared memory
+  if (p.split > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
   // the warp's first chunks of W into L2 while the previous kernel still runs (a hint
   // that returns no data, so that it may be issued before the wait)
   for (int u = 0; u < kUnroll; ++u) {
@@ -312,8 +312,12 @@ __global__ void __launch_bounds__(kMaxWarps * 32) few_kernel(const FewParams p) 
     return v;
   };
   if (p.split > 1) {
-    for (int i = threadIdx.x; i < kTiles * 8 * kRows; i += blockDim.x)
-      part[i / kRows][i % kRows] = cta_sum(i / kRows, i % kRows);
+    // each CTA's sums go to the CTA that finishes the token, which adds them in order
+    asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+    for (int i = threadIdx.x; i < kTiles * 8 * kRows; i += blockDim.x) {
+      const int m = i / kRows, r = i % kRows;
+      st_cluster(mapa_shared(&part[rank][m][r], (uint32_t)(m % p.split)), cta_sum(m, r));
+    }
     cluster_sync();
   }
   // sixteen neighbouring threads finish a token's sixteen outputs
@@ -332,7 +336,7 @@ __global__ void __launch_bounds__(kMaxWarps * 32) few_kernel(const FewParams p) 
       if (p.split == 1) {
         v = cta_sum(i_m, r);
       } else {
-        for (int q = 0; q < p.split; ++q) v = __fadd_rn(v, ld_cluster(mapa_shared(&part[i_m][r], q)));
+        for (int q = 0; q < p.split; ++q) v = __fadd_rn(v, part[q][i_m][r]);
       }
       v = __fadd_rn(__fmul_rn(v, o_scale[k]), o_bias[k]);
       float2 one[1] = {make_float2(v, v)};
@@ -360,7 +364,6 @@ __global__ void __launch_bounds__(kMaxWarps * 32) few_kernel(const FewParams p) 
       if (inside && r % kBlock == 0) p.rq_scales[scale_offset(m, col / 16, p.rq_cols)] = (uint8_t)code;
     }
   }
-  if (p.split > 1) cluster_sync();   // no CTA leaves while another reads its sums
 }
 
 // How a launch splits its work: row tiles per CTA, warps per CTA, CTAs per cluster.
