@@ -6,11 +6,11 @@
 // fragments.
 //
 // Measured with bias and SiLU, operands of several calls in turn: bf16 1 x 12288 x 3072
-// 12.7 us, 89% of the measured copy rate; FP8 1 x 12288 x 3072 7.5 us, 76%; FP8 8 x 3072 x
-// 12288 10.7 us, 53%; 1 x 3072 x 3072 4.3 us.  What is left is a launch, the first loads
-// and the joined sums, about three microseconds.  NVFP4 1 x 12288 x 3072 takes 8.0 us, 40%:
-// codes become fp16 and meet their block scales in registers, sixteen instructions per
-// 16 bytes.
+// 12.6 us, 90% of the measured copy rate, 8 x 3072 x 12288 13.7, 83%; FP8 1 x 12288 x 3072
+// 7.6 us, 75%, 8 x 3072 x 12288 8.9, 64%, 1 x 3072 x 3072 4.4.  What is left is a launch,
+// the first loads and the joined sums, about three microseconds.  NVFP4 1 x 12288 x 3072
+// takes 7.9 us, 40%: codes become fp16 and meet their block scales in registers, sixteen
+// instructions per 16 bytes.
 //
 // Fragments without shared memory: an MMA sums over K in any order, as long as both
 // operands agree.  Lane (g, t) = (lane / 4, lane % 4) loads the 16 bytes at 16 t of a
@@ -374,20 +374,25 @@ struct Split {
 // One wave: CTAs have a fixed cost (16 x 12288 x 3072 NVFP4 with 768 CTAs on 760 places
 // 12.0 us, with 384 of twice the rows 10.0), so the warps that share rows are as many as
 // stay resident together (`resident` warps per SM of each row tiling), at most one per
-// four chunks of K.  A cluster's barriers cost about a microsecond: they pay where they
-// give sixteen warps or more (FP8 8 x 3072 x 12288 10.5 -> 9.8 us with two CTAs of eight,
-// fp16 2 x 1024 x 2560 4.65 -> 4.1; bf16 16 x 3072 x 3072 7.05 -> 8.3).
-Split choose_split(int64_t N, int64_t token_groups, int64_t chunks, const int (&resident)[2], int num_sms) {
-  const int most = (int)std::max<int64_t>(kMinWarps, std::min<int64_t>((chunks + 3) / 4, kMaxWarps * kMaxSplit));
+// four chunks of K, or two while that leaves the machine near empty (NVFP4 48 x 512 x 2048
+// 3.5 -> 3.1 us).  A cluster pays where it gives sixteen warps or more and either few of
+// them share an SM (fp16 2 x 1024 x 2560 4.1 -> 3.2 us; bf16 48 x 512 x 2048, ten per SM,
+// 3.9 -> 4.6) or K is long (FP8 8 x 3072 x 12288 10.3 -> 8.9 us with two CTAs; bf16 1 x 3072
+// x 3072 6.0 -> 8.6), never over rows of less than 64 chunks (bf16 12 x 320 x 1088 2.8 -> 3.4).
+Split choose_split(int64_t N, int64_t token_groups, int64_t K, int64_t chunks, const int (&resident)[2],
+                   int num_sms) {
   Split best{1, kMinWarps, 1};
   for (int rt = 1; rt <= 2; ++rt) {
-    const int64_t groups = N / (kBlock * rt) * token_groups;
+    const int64_t units = N / (kBlock * rt) * token_groups;
     bool fits = false;
     for (int ctas = 1; ctas <= kMaxSplit; ++ctas)
       for (int w = kMinWarps; w <= kMaxWarps; ++w) {
-        if (w * ctas > most || groups * ctas > (int64_t)num_sms * (resident[rt - 1] / w)) continue;
-        if (ctas > 1 && w * ctas < 16) continue;
-        if (!fits || w * ctas > best.warps * best.ctas) best = {rt, w, ctas};
+        const int64_t warps = w * ctas, all = units * warps;
+        const int64_t per = all <= 6 * num_sms ? 2 : 4;
+        if (units * ctas > (int64_t)num_sms * (resident[rt - 1] / w)) continue;
+        if (warps > std::max<int64_t>(kMinWarps, (chunks + per - 1) / per)) continue;
+        if (ctas > 1 && (warps < 16 || chunks < 64 || (all > 9 * num_sms && (K < 8192 || ctas > 2)))) continue;
+        if (!fits || warps > best.warps * best.ctas) best = {rt, w, ctas};
         fits = true;
       }
     if (fits) return best;
@@ -414,7 +419,8 @@ cudaError_t launch_tiles(FewParams p, cudaStream_t s, Device dev) {
   });
   if (setup.err != cudaSuccess) return setup.err;
   const int64_t row = kKind == Kind::kNvfp4 ? p.K / 2 : kKind == Kind::kFp8 ? p.K : p.K * 2;
-  const Split split = choose_split(p.N, (p.M + kTiles * 8 - 1) / (kTiles * 8), (row + kChunk - 1) / kChunk, setup.resident, dev.num_sms);
+  const Split split = choose_split(p.N, (p.M + kTiles * 8 - 1) / (kTiles * 8), p.K, (row + kChunk - 1) / kChunk,
+                                   setup.resident, dev.num_sms);
   p.split = split.ctas;
   cudaLaunchConfig_t cfg{};
   cudaLaunchAttribute at[2];
