@@ -101,10 +101,10 @@ struct Cfg {
   static constexpr int kSfSmemSlots = kSfCopy ? kSfWarps : 0;
   static constexpr int kSfSlotBytes = (1 + kSfbAtoms) * kStepsPerStage * 512;
   static constexpr int kSfBytes = kSfSmemSlots * kSfSlotBytes;
-  // kHold, NVFP4: a copy of the tile's bias per epilogue warp, where its epilogue is on
-  // the critical path and shared memory is left (the other kinds have none left, and
-  // longer mainloops).
-  static constexpr bool kSmemBias = kHold && kFp4;
+  // kLin: a copy of the tile's bias per epilogue warp (instead of a shuffle per column:
+  // 1333 x 2112 x 1088 with GELU, FP8 9.86 -> 9.42 us, bf16 11.35 -> 11.0).  Pairs of the
+  // other kinds than NVFP4 have no shared memory left for it, and longer mainloops.
+  static constexpr bool kSmemBias = kLin != 0 && (kFp4 || !kPair);
   static constexpr int kBiasBytes = kSmemBias ? kEpiWarps * (kBN / (kEpiWarps / 4)) * 4 : 0;
   static constexpr int kStagesRaw = (kSmemBudget - kOutBytes - kSfBytes - kBiasBytes) / kStageBytes;
   static constexpr int kStages = kStagesRaw > 8 ? 8 : kStagesRaw;
@@ -272,8 +272,8 @@ __device__ __forceinline__ float2 column_pair(float held, int i) {
 
 // act(v * scale + bias) + residual of 32 columns of one row, as 16-bit pairs.  The scale
 // is s_row (NVFP4), s_row * S_W[n] (FP8) or 1; lane i holds the bias and S_W of column
-// i, or shared memory the biases.  (Loads of them at the same address in all lanes cost 11 of 38 us at 4608 x 12288 x
-// 256 NVFP4, where the epilogue is the bound.)
+// i, or shared memory the biases.  (Loads of them at the same address in all lanes cost
+// 11 of 38 us at 4608 x 12288 x 256 NVFP4, where the epilogue is the bound.)
 template <bool kFp4, bool kBf16, bool kF16, bool kRes, bool kSmemBias>
 __device__ __forceinline__ void finish32(float2 (&v)[16], const KParams& p, float s_row, float bias,
                                          const float* bias_s, float s_w, const uint32_t (&res)[16],
