@@ -253,7 +253,8 @@ static qlin_status set_epilogue(GemmArgs& a, const qlin_epilogue_t* ep) {
 // order; the linears take the few-token kernel where it applies.
 static cudaError_t launch_linear(const GemmArgs& a, cudaStream_t s, Device dev, unsigned* status) {
   // (the few-token kernel counts a row's bytes in 32 bits)
-  if (a.few_ok && few_tokens(a.bf16, a.M, a.N, dev.num_sms) && a.K <= (int64_t)1 << 28)
+  if (a.few_ok && a.K <= (int64_t)1 << 28 &&
+      few_tokens(a.bf16, a.M, a.N, a.bf16 ? 2 * a.K : a.fp4 ? a.K / 2 : a.K, dev.num_sms))
     return launch_few(a, s, dev);
   return launch_gemm(a, s, dev, status, timeout());
 }

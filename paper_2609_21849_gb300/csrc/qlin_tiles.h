@@ -83,15 +83,20 @@ inline Tile choose_tile(GemmKind kind, Epilogue epi, int64_t M, int64_t N, int64
 }
 
 // Whether a linear takes the few-token kernel, which reads W once per 16 tokens, rather
-// than the tiles above: always up to 16 tokens, beyond that as long as its groups of 16
-// rows of W and 16 tokens are at most 2.6 per SM (16-bit operands 5.2).  Both timed at 9
-// weights (N 64-12288, K 512-12288), M 16-128, in us (few / tiles): NVFP4 N = K = 3072
-// M = 32 6.9 / 8.1, M = 48 8.6 / 8.2; FP8 M = 32 7.9 / 7.9, M = 48 8.9 / 7.9; bf16 M = 64
-// 13.1 / 13.7, M = 96 24.8 / 13.8; bf16 N = 64, K = 12288 M = 128 6.1 / 36; at 16 tokens
-// NVFP4 N = 12288 10.4 / 10.2, all others faster here.
-inline bool few_tokens(bool float16, int64_t M, int64_t N, int num_sms) {
+// than the tiles above: always up to 16 tokens, beyond that as long as its units, 16 rows
+// of W and 16 tokens, are at most 5.2 per SM with 16-bit operands, 2.6 with others (1.9
+// over rows of W shorter than 2048 bytes, from 33 tokens).  Few / tiles, timed over N
+// 64-12288, K 512-12288 and M 16-1600, in us: bf16 128 x 768 x 12288 16.6 / 45.4 (4.9
+// units per SM), 552 x 64 x 12288 10.9 / 42.8 (0.9), 1600 x 128 x 768 6.1 / 6.2 (5.3), 352
+// x 768 x 6144 42 / 24 (6.9); FP8 960 x 64 x 6144 8.4 / 12.1 (1.6), 32 x 3072 x 3072 7.9 /
+// 7.9 (2.5), 48 x 2048 x 768 4.7 / 4.1 (2.5), 352 x 320 x 12288 18.2 / 19.8 (2.9); NVFP4
+// 552 x 128 x 768 3.3 / 3.9 (1.8), 32 x 3072 x 3072 6.9 / 8.1 (2.5), 1600 x 64 x 2560 6.6 /
+// 5.7 and x 12288 18.0 / 21.1 (2.6); at 16 tokens NVFP4 N = 12288 9.9 / 10.2.
+inline bool few_tokens(bool float16, int64_t M, int64_t N, int64_t row_bytes, int num_sms) {
   if (M <= 16) return true;
-  return M <= 128 && 10 * (N / 16) * ((M + 15) / 16) <= (int64_t)(float16 ? 52 : 26) * num_sms;
+  const int limit = float16 ? 52 : M <= 32 || row_bytes >= 2048 ? 26 : 19;
+  // (M < 2^31 and N / 16 < 2^59: beyond a limit that large grids exceed anyway)
+  return N / 16 <= limit * (int64_t)num_sms && 10 * (N / 16) * ((M + 15) / 16) <= limit * (int64_t)num_sms;
 }
 
 }  // namespace qlin

@@ -91,7 +91,7 @@ def _check(y, a, w, bias, act, residual, what):
 # one token and a few; partial tiles; long and short K; each tile configuration
 SHAPES = [(1, 64, 64), (1, 1024, 2560), (2, 192, 3136), (5, 576, 1088), (8, 3072, 512), (9, 64, 12288), (16, 320, 192),
           (17, 2112, 320), (33, 1024, 4160), (77, 320, 192), (129, 576, 1088), (300, 128, 512), (1300, 3648, 320),
-          (2048, 4096, 1088)]
+          (2048, 4096, 1088), (552, 64, 4160), (1000, 576, 1088), (1040, 128, 320), (1500, 64, 1088)]
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
@@ -105,7 +105,7 @@ def test_shapes(M, N, K, fmt):
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
-@pytest.mark.parametrize("M", [1, 6, 200, 2048])
+@pytest.mark.parametrize("M", [1, 6, 200, 1000, 2048])
 def test_parts(M, fmt):
     N, K = (4096, 192) if M == 2048 else (448, 1088)
     a, w, bias, res, dt = _operands(fmt, M, N, K, 17 + M)
@@ -115,7 +115,7 @@ def test_parts(M, fmt):
 
 
 @pytest.mark.parametrize("fmt", ["nvfp4", "fp8", "bf16", "fp16"])
-@pytest.mark.parametrize("M", [300, 2048])
+@pytest.mark.parametrize("M", [900, 2048])
 def test_without_an_epilogue_as_the_plain_gemm(M, fmt):
     # at these sizes the same kernel runs: bit for bit
     N, K = (4096, 1088) if M == 2048 else (320, 1088)
@@ -125,7 +125,7 @@ def test_without_an_epilogue_as_the_plain_gemm(M, fmt):
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
-@pytest.mark.parametrize("M", [1, 7, 100, 2048])
+@pytest.mark.parametrize("M", [1, 7, 100, 1000, 2048])
 def test_residual_in_place_and_strided(M, fmt):
     N, K = 4096 if M == 2048 else 320, 512
     a, w, bias, res, dt = _operands(fmt, M, N, K, 23)
@@ -143,7 +143,7 @@ def test_residual_in_place_and_strided(M, fmt):
 
 
 @pytest.mark.parametrize("M,N,K", [(1, 64, 64), (3, 320, 1088), (16, 1024, 512), (40, 576, 320), (333, 512, 1088),
-                                   (2048, 4096, 320)])
+                                   (2048, 4096, 320), (700, 64, 2112)])
 @pytest.mark.parametrize("fmt", ["nvfp4", "fp8", "fp8_rows"])
 def test_requantized_output(M, N, K, fmt):
     a, w, bias, res, _ = _operands(fmt, M, N, K, M + N)
@@ -179,7 +179,7 @@ def test_fp8_weight_with_one_scale(M):
         _check(y, a, one, bias, qlin.QLIN_ACT_GELU, res, (fmt, M))
 
 
-@pytest.mark.parametrize("M", [1, 5, 200, 2048])
+@pytest.mark.parametrize("M", [1, 5, 200, 1700, 2048])
 @pytest.mark.parametrize("act", ACTS)
 def test_large_and_special_values(M, act):
     # Products far out in both tails, and infinities and NaN in bias and residual,
