@@ -81,19 +81,22 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(const RopeParams p) {
 
 // ---- 16-byte accesses ----
 // A lane takes 16 elements of a head in two chunks of 8: eight pairs (the chunks half a
-// rotation apart in the half layout, adjacent in the interleaved one), or elements past
-// rot_dim (the last lane of a head perhaps one chunk of them; none in place).
+// rotation apart in the half layout, adjacent in the interleaved one; the last lane of
+// the pairs perhaps fewer), or elements past rot_dim (the last lane of a head perhaps one
+// chunk of them; none in place).
 // A warp works alone, on some heads of one token or, where heads are few, on several
 // tokens: a lane keeps its place in the head, so its eight rotations stay in registers
 // for all of its heads, and nothing waits for another warp.  The loads of its first
 // heads are issued before the rotations are computed.
 //
 // Bound by HBM (2 bytes in, 2 out per element; positions and turns are small): 4608 x
-// 48 x 128 with strided rows 20.2 us interleaved, 19.8 in halves, 84-86% of the measured
+// 48 x 128 with strided rows 20.0 us interleaved, 20.1 in halves, 84-85% of the measured
 // copy rate; 9216 x 48 x 128 of which 64 turn 35.4 us, 96%.  A CTA per token with the
 // rotations behind a barrier took 24.8 us, scalar accesses 57.  Where the lanes of a
-// head do not divide a warp some idle (192 of 192: 24 of 32 lanes, 70%).  One token
-// takes 1.7 us, a launch and one chain of loads.
+// head do not divide a warp some idle (192 of 192: 24 of 32 lanes, 70%), and where the
+// pairs do not fill their last lane; 9079 x 25 x 80 of which 40 turn 17.4 us interleaved,
+// 19.3 in halves (element by element 57).  One token takes 1.9 us, a launch and one chain
+// of loads.
 // kItems heads of a lane are in flight at once (4, where work is plenty).
 constexpr int kMostItems = 4;
 constexpr int kVecWarps = 4;
@@ -117,6 +120,18 @@ __device__ __forceinline__ uint4 ldg128(const uint16_t* p) {
                : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
                : "l"(p));
   return v;
+}
+
+// Four or eight elements from an eight-byte boundary.
+__device__ __forceinline__ void ldg_fours(const uint16_t* p, int n, uint4& v) {
+  const uint2 a = *reinterpret_cast<const uint2*>(p);
+  uint2 b = make_uint2(0u, 0u);
+  if (n > 4) b = *reinterpret_cast<const uint2*>(p + 4);
+  v = make_uint4(a.x, a.y, b.x, b.y);
+}
+__device__ __forceinline__ void stg_fours(uint16_t* p, int n, uint4 v) {
+  *reinterpret_cast<uint2*>(p) = make_uint2(v.x, v.y);
+  if (n > 4) *reinterpret_cast<uint2*>(p + 4) = make_uint2(v.z, v.w);
 }
 
 template <bool kF16>
@@ -149,13 +164,17 @@ __device__ __forceinline__ void unpack_pairs(const uint4 (&v)[2], float (&a)[8],
     }
   }
 }
+// The interleaved elements past `turned` (even) pairs stay as they came.
 template <bool kF16, bool kHalf>
-__device__ __forceinline__ void pack_pairs(const float (&a)[8], const float (&b)[8], uint4 (&v)[2]) {
-  uint32_t w[8];
+__device__ __forceinline__ void pack_pairs(const float (&a)[8], const float (&b)[8], int turned, uint4 (&v)[2]) {
+  uint32_t w[8] = {v[0].x, v[0].y, v[0].z, v[0].w, v[1].x, v[1].y, v[1].z, v[1].w};
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const float* const d = i < 4 ? a : b;
-    w[i] = kHalf ? pack2<kF16>(d[2 * (i & 3)], d[2 * (i & 3) + 1]) : pack2<kF16>(a[i], b[i]);
+    if (kHalf)
+      w[i] = pack2<kF16>(d[2 * (i & 3)], d[2 * (i & 3) + 1]);
+    else if ((i & ~1) < turned)
+      w[i] = pack2<kF16>(a[i], b[i]);
   }
   v[0] = make_uint4(w[0], w[1], w[2], w[3]);
   v[1] = make_uint4(w[4], w[5], w[6], w[7]);
@@ -184,7 +203,9 @@ struct RopeUnits {
   int wide;               // rows start on 32-byte boundaries: a lane's adjacent chunks in one access
 };
 
-template <bool kF16, bool kHalf, int kItems>
+// kFours: halves that are no multiple of eight take eight-byte accesses, the last lane one
+// per half.  (An instance of its own: the branch cost the others 6%.)
+template <bool kF16, bool kHalf, bool kFours, int kItems>
 __global__ void __launch_bounds__(kVecWarps * 32) rope_vec_kernel(const RopeParams p, const RopeUnits u,
                                                                   int64_t tokens) {
   extern __shared__ float2 rot_all[];   // per warp [tokens][pairs]
@@ -196,7 +217,7 @@ __global__ void __launch_bounds__(kVecWarps * 32) rope_vec_kernel(const RopePara
   const int group = (int)blockIdx.y;
   const int64_t token0 = unit * u.tokens;
   const int here = (int)min((int64_t)u.tokens, tokens - token0);
-  const int eights = p.pairs / 8;
+  const int eights = (kFours || !kHalf ? p.pairs + 7 : p.pairs) / 8;
   auto div20 = [](int n, uint32_t by) { return (int)(((uint32_t)n * by) >> 20); };
   const int slot = div20(lane, u.by_per_head), at = lane - slot * u.per_head;
   // the lane's token, and its heads: first, then every slots-th
@@ -205,11 +226,15 @@ __global__ void __launch_bounds__(kVecWarps * 32) rope_vec_kernel(const RopePara
   const int head_end = slot >= u.slots || tok >= here ? 0
                        : u.tokens == 1                ? min(p.heads, (group + 1) * u.heads)
                                                       : head + 1;
-  const bool turns = at < eights;
-  const int off0 = (kHalf && turns ? 8 : 16) * at;   // (2 pairs = 16 eights precede the rest)
+  constexpr bool kPart = kFours || !kHalf;
+  const int turned = kPart ? min(8, p.pairs - 8 * at) : 8;   // pairs of a lane that turns
+  const bool turns = kPart ? turned > 0 : at < eights;
+  // (2 pairs precede the rest: 16 eights, or less)
+  const int off0 = kHalf && turns ? 8 * at : kFours ? 2 * p.pairs + 16 * (at - eights) : 16 * at;
   const int off1 = kHalf && turns ? off0 + p.pairs : off0 + 8;
   const bool second = off1 < p.head_dim;
   const bool wide = u.wide && second && (!kHalf || !turns);
+  const bool fours = kFours && turns;
   const uint16_t* x = p.x + (token0 + tok) * p.x_token + head * p.x_head;
   uint16_t* y = p.y + (token0 + tok) * p.y_token + head * p.y_head;
   const int64_t x_step = u.slots * p.x_head, y_step = u.slots * p.y_head;
@@ -220,6 +245,9 @@ __global__ void __launch_bounds__(kVecWarps * 32) rope_vec_kernel(const RopePara
       if (head + k * u.slots >= head_end) continue;
       if (wide) {
         ldg256(x + off0, v[k]);
+      } else if (fours) {
+        ldg_fours(x + off0, turned, v[k][0]);
+        ldg_fours(x + off1, turned, v[k][1]);
       } else {
         v[k][0] = ldg128(x + off0);
         if (second) v[k][1] = ldg128(x + off1);
@@ -240,7 +268,7 @@ __global__ void __launch_bounds__(kVecWarps * 32) rope_vec_kernel(const RopePara
     const float4* const src = reinterpret_cast<const float4*>(rot + tok * p.pairs + 8 * at);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const float4 r = src[j];
+      const float4 r = !kPart || 2 * j < turned ? src[j] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
       c[j] = make_float2(r.x, r.z);
       sn[j] = make_float2(r.y, r.w);
       ns[j] = make_float2(-r.y, -r.w);
@@ -255,10 +283,13 @@ __global__ void __launch_bounds__(kVecWarps * 32) rope_vec_kernel(const RopePara
         unpack_pairs<kF16, kHalf>(v[k], a, b);
 #pragma unroll
         for (int j = 0; j < 4; ++j) turn2(a, b, 2 * j, c[j], sn[j], ns[j]);
-        pack_pairs<kF16, kHalf>(a, b, v[k]);
+        pack_pairs<kF16, kHalf>(a, b, turned, v[k]);
       }
       if (wide) {
         stg256(y + off0, v[k][0], v[k][1]);
+      } else if (fours) {
+        stg_fours(y + off0, turned, v[k][0]);
+        stg_fours(y + off1, turned, v[k][1]);
       } else {
         *reinterpret_cast<uint4*>(y + off0) = v[k][0];
         if (second) *reinterpret_cast<uint4*>(y + off1) = v[k][1];
@@ -297,10 +328,13 @@ cudaError_t launch_rope(const qlin_rope_t& a, int num_sms, cudaStream_t s) {
   p.half = a.layout == QLIN_ROPE_HALF ? 1 : 0;
   p.inverse = a.inverse ? 1 : 0;
   p.fp16 = a.dtype == QLIN_FP16 ? 1 : 0;
-  // 16-byte accesses: every row starts on a 16-byte boundary, and chunks of eight
-  // elements divide the pairs, the halves and what follows them, a warp's lanes hold a head
-  const int per_head = p.pairs / 8 + (p.x == p.y ? 0 : (p.head_dim - 2 * p.pairs + 15) / 16);
-  const bool vec = p.pairs % 8 == 0 && per_head <= 32 && p.head_dim % 8 == 0 &&
+  // 16-byte accesses: every row starts on a 16-byte boundary, chunks of eight elements
+  // divide the head, an access never divides a pair (in halves, eight bytes at least
+  // where their length is no multiple of eight), a warp's lanes hold a head
+  const int eights = (p.pairs + 7) / 8;
+  const int past = p.head_dim - (p.half ? 2 * p.pairs : std::min(16 * eights, p.head_dim));
+  const int per_head = eights + (p.x == p.y ? 0 : (past + 15) / 16);
+  const bool vec = p.pairs % (p.half ? 4 : 2) == 0 && per_head <= 32 && p.head_dim % 8 == 0 &&
                    ((reinterpret_cast<uintptr_t>(p.x) | reinterpret_cast<uintptr_t>(p.y)) & 15u) == 0 &&
                    ((p.x_token | p.x_head | p.y_token | p.y_head) & 7) == 0;
   if (vec) {
@@ -321,7 +355,7 @@ cudaError_t launch_rope(const qlin_rope_t& a, int num_sms, cudaStream_t s) {
     u.by_heads = u.tokens > 1 ? by(p.heads) : 0;
     u.by_pairs = by(p.pairs);
     u.wide = ((reinterpret_cast<uintptr_t>(p.x) | reinterpret_cast<uintptr_t>(p.y)) & 31u) == 0 &&
-                     ((p.x_token | p.x_head | p.y_token | p.y_head) & 15) == 0
+                     ((p.x_token | p.x_head | p.y_token | p.y_head) & 15) == 0 && (!p.half || p.pairs % 8 == 0)
                  ? 1
                  : 0;
     const unsigned grid = (unsigned)((u.count + kVecWarps - 1) / kVecWarps);
@@ -329,16 +363,20 @@ cudaError_t launch_rope(const qlin_rope_t& a, int num_sms, cudaStream_t s) {
     auto launch = [&](auto kern) {
       return launch_pdl(kern, dim3(grid, (unsigned)groups), kVecWarps * 32, smem, s, p, u, a.tokens);
     };
-    auto with_items = [&](auto f16, auto half) {
-      constexpr bool kF16 = decltype(f16)::value, kHalf = decltype(half)::value;
-      return per_warp == 1   ? launch(rope_vec_kernel<kF16, kHalf, 1>)
-             : per_warp == 2 ? launch(rope_vec_kernel<kF16, kHalf, 2>)
-                             : launch(rope_vec_kernel<kF16, kHalf, 4>);
-    };
     using T = std::true_type;
     using F = std::false_type;
-    return p.fp16 ? (p.half ? with_items(T{}, T{}) : with_items(T{}, F{}))
-                  : (p.half ? with_items(F{}, T{}) : with_items(F{}, F{}));
+    auto with_items = [&](auto f16, auto half, auto fours) {
+      constexpr bool kF16 = decltype(f16)::value, kHalf = decltype(half)::value, kFours = decltype(fours)::value;
+      return per_warp == 1   ? launch(rope_vec_kernel<kF16, kHalf, kFours, 1>)
+             : per_warp == 2 ? launch(rope_vec_kernel<kF16, kHalf, kFours, 2>)
+                             : launch(rope_vec_kernel<kF16, kHalf, kFours, 4>);
+    };
+    auto with_layout = [&](auto f16) {
+      return !p.half            ? with_items(f16, F{}, F{})
+             : p.pairs % 8 != 0 ? with_items(f16, T{}, T{})
+                                : with_items(f16, T{}, F{});
+    };
+    return p.fp16 ? with_layout(T{}) : with_layout(F{});
   }
   return launch_pdl(rope_kernel, (unsigned)a.tokens, kThreads, 0, s, p);
 }

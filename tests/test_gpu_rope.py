@@ -165,6 +165,25 @@ def test_inverse_is_the_gradient(layout):
         assert (got - want).abs().max() <= 2.0**-9 * (2 * g.abs().max().item() * 1.3)
 
 
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("D,R", [(80, 40), (80, 20), (72, 72), (24, 12), (96, 24), (88, 4), (40, 36), (88, 88), (200, 88)])
+def test_rotations_of_any_width_beside_elements_that_pass(D, R, layout):
+    # whatever is past the rotation, NaN among it, stays bit for bit
+    for T, H in ((70, 1), (33, 6)):
+        x = _x(T, H, D, torch.bfloat16, D + R)
+        x.view(torch.int16)[..., R:] = torch.randint(-2**15, 2**15, (T, H, D - R), device="cuda").to(torch.int16)
+        pos = torch.randint(0, 5000, (T,), device="cuda")
+        plan = qlin.rope_plan(R, layout=layout)
+        y = qlin.qlin_rope(x, pos, plan)
+        _check(y[..., :R].contiguous(), x[..., :R].contiguous(), pos, plan)
+        assert torch.equal(y.view(torch.int16)[..., R:], x.view(torch.int16)[..., R:])
+        place = x.clone()
+        qlin.qlin_rope(place, pos, plan, place)
+        assert torch.equal(place.view(torch.int16), y.view(torch.int16))
+        odd = torch.zeros(T, H, D + 8, dtype=x.dtype, device="cuda")[..., :D].copy_(x)   # rows 16 bytes apart
+        assert torch.equal(qlin.qlin_rope(odd, pos, plan).view(torch.int16), y.view(torch.int16))
+
+
 def test_refusals_of_tensors():
     x = _x(4, 2, 64, torch.bfloat16)
     pos = torch.arange(4, device="cuda")
