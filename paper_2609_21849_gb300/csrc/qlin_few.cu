@@ -378,9 +378,11 @@ struct Split {
 // 3.5 -> 3.1 us).  A cluster pays where it gives sixteen warps or more and either few of
 // them share an SM (fp16 2 x 1024 x 2560 4.1 -> 3.2 us; bf16 48 x 512 x 2048, ten per SM,
 // 3.9 -> 4.6) or K is long (FP8 8 x 3072 x 12288 10.3 -> 8.9 us with two CTAs; bf16 1 x 3072
-// x 3072 6.0 -> 8.6), never over rows of less than 64 chunks (bf16 12 x 320 x 1088 2.8 -> 3.4).
-Split choose_split(int64_t N, int64_t token_groups, int64_t K, int64_t chunks, const int (&resident)[2],
-                   int num_sms) {
+// x 3072 6.0 -> 8.6), never over short rows (bf16 10 x 320 x 1280 2.9 -> 3.3 us, 4 x 1024 x
+// 1984 3.7 -> 3.1; an NVFP4 chunk takes longer: 10 x 320 x 4352 4.3 -> 4.4, x 5120 4.5 -> 3.8).
+Split choose_split(Kind kind, int64_t N, int64_t token_groups, int64_t K, int64_t chunks,
+                   const int (&resident)[2], int num_sms) {
+  const int64_t least = kind == Kind::kNvfp4 ? 40 : 60;
   Split best{1, kMinWarps, 1};
   for (int rt = 1; rt <= 2; ++rt) {
     const int64_t units = N / (kBlock * rt) * token_groups;
@@ -391,7 +393,7 @@ Split choose_split(int64_t N, int64_t token_groups, int64_t K, int64_t chunks, c
         const int64_t per = all <= 6 * num_sms ? 2 : 4;
         if (units * ctas > (int64_t)num_sms * (resident[rt - 1] / w)) continue;
         if (warps > std::max<int64_t>(kMinWarps, (chunks + per - 1) / per)) continue;
-        if (ctas > 1 && (warps < 16 || chunks < 64 || (all > 9 * num_sms && (K < 8192 || ctas > 2)))) continue;
+        if (ctas > 1 && (warps < 16 || chunks < least || (all > 9 * num_sms && (K < 8192 || ctas > 2)))) continue;
         if (!fits || warps > best.warps * best.ctas) best = {rt, w, ctas};
         fits = true;
       }
@@ -419,7 +421,7 @@ cudaError_t launch_tiles(FewParams p, cudaStream_t s, Device dev) {
   });
   if (setup.err != cudaSuccess) return setup.err;
   const int64_t row = kKind == Kind::kNvfp4 ? p.K / 2 : kKind == Kind::kFp8 ? p.K : p.K * 2;
-  const Split split = choose_split(p.N, (p.M + kTiles * 8 - 1) / (kTiles * 8), p.K, (row + kChunk - 1) / kChunk,
+  const Split split = choose_split(kKind, p.N, (p.M + kTiles * 8 - 1) / (kTiles * 8), p.K, (row + kChunk - 1) / kChunk,
                                    setup.resident, dev.num_sms);
   p.split = split.ctas;
   cudaLaunchConfig_t cfg{};
