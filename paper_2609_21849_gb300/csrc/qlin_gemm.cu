@@ -104,7 +104,7 @@ struct Cfg {
   // kLin: a copy of the tile's bias per epilogue warp (instead of a shuffle per column:
   // 1333 x 2112 x 1088 with GELU, FP8 9.86 -> 9.42 us, bf16 11.35 -> 11.0).  Pairs of the
   // other kinds than NVFP4 have no shared memory left for it, and longer mainloops.
-  static constexpr bool kSmemBias = kLin != 0 && (kFp4 || !kPair);
+  static constexpr bool kSmemBias = kLin != 0 && kLin != 3 && (kFp4 || !kPair);
   static constexpr int kBiasBytes = kSmemBias ? kEpiWarps * (kBN / (kEpiWarps / 4)) * 4 : 0;
   static constexpr int kStagesRaw = (kSmemBudget - kOutBytes - kSfBytes - kBiasBytes) / kStageBytes;
   static constexpr int kStages = kStagesRaw > 8 ? 8 : kStagesRaw;
@@ -171,6 +171,7 @@ struct KParams {
   int act;
   int a_per_row;
   int r_v8;           // residual rows start on 32-byte boundaries
+  int split;          // kLin == 3: CTAs that share a tile's K (2, 4 or 8)
 };
 
 // Coordinates of cluster tile ct, its M tile group and its N tile: M fastest
@@ -313,7 +314,8 @@ __device__ __forceinline__ void finish32(float2 (&v)[16], const KParams& p, floa
 // kBf16 (with !kFp4): bf16 operands on the FP8 skeleton (the same 128-byte
 // rows, 32 bytes of K per MMA), no scales.
 // kLin: the epilogue of qlin_linear_*: bias and activation before the 16-bit rounding,
-// FP8 row scales of A; kLin == 2 adds a residual.
+// FP8 row scales of A; kLin == 2 adds a residual; kLin == 3 (single-CTA tiles, a residual
+// or none) shares a tile's K among the CTAs of a cluster.
 template <bool kFp4, int kBN, bool kPair, bool kRequant, bool kBf16 = false, int kLin = 0>
 __global__ void __launch_bounds__(Cfg<kFp4, kBN, kPair, kLin>::kThreads, 1)
     gemm_kernel(const __grid_constant__ CUtensorMap tmap_a,
@@ -321,7 +323,8 @@ __global__ void __launch_bounds__(Cfg<kFp4, kBN, kPair, kLin>::kThreads, 1)
                 const __grid_constant__ CUtensorMap tmap_sfa,
                 const __grid_constant__ CUtensorMap tmap_sfb,
                 const __grid_constant__ CUtensorMap tmap_y, const KParams p) {
-  constexpr bool kEpi = kLin != 0, kRes = kLin == 2;
+  constexpr bool kEpi = kLin != 0, kRes = kLin == 2, kSplitK = kLin == 3;
+  static_assert(!kSplitK || (!kPair && !kRequant), "split tiles");
   using C = Cfg<kFp4, kBN, kPair, kLin>;
   constexpr bool kHold = C::kHold;
   constexpr int kCM = kPair ? 2 : 1;          // CTAs per cluster (M tiles per cluster tile)
@@ -391,11 +394,16 @@ __global__ void __launch_bounds__(Cfg<kFp4, kBN, kPair, kLin>::kThreads, 1)
   const int tiles_n = (int)((p.N + kBN - 1) / kBN);
   const int groups_m = (tiles_m + kCM - 1) / kCM;
   const int num_ctiles = groups_m * tiles_n;
-  const int cid = (int)blockIdx.x / kCM;
-  const int ncl = (int)gridDim.x / kCM;
+  const int splits = kSplitK ? p.split : 1;
+  const int krank = kSplitK ? __shfl_sync(0xFFFFFFFFu, (int)cluster_ctarank(), 0) : 0;
+  const int cid = (int)blockIdx.x / (kCM * splits);
+  const int ncl = (int)gridDim.x / (kCM * splits);
   const int64_t k_bytes = kFp4 ? p.K / 2 : kBf16 ? p.K * 2 : p.K;
   const int num_kb = (int)((k_bytes + kRowBytes - 1) / kRowBytes);
   const int k_steps = (int)(k_bytes / 32);
+  // stages of this CTA: all, or its share of them (at least one: split <= num_kb)
+  const int kb0 = kSplitK ? krank * num_kb / splits : 0;
+  const int kb1 = kSplitK ? (krank + 1) * num_kb / splits : num_kb;
 
   // The first W boxes into L2 while the previous kernel still runs: a prefetch
   // is a hint that returns no data, so it is correct even if that kernel
@@ -409,8 +417,8 @@ __global__ void __launch_bounds__(Cfg<kFp4, kBN, kPair, kLin>::kThreads, 1)
     tile_coords(cid, groups_m, &mg, &nb);
     constexpr int kWRows = kBN / kCM / C::kSplit;
     const int w_row = nb * kBN + rank * (kBN / kCM);
-    const int boxes = mg == 0 ? min(num_kb, C::kStages) : 0;
-    for (int kb = 0; kb < boxes; ++kb)
+    const int boxes = mg == 0 ? min(kb1 - kb0, C::kStages) : 0;
+    for (int kb = kb0; kb < kb0 + boxes; ++kb)
 #pragma unroll
       for (int b = 0; b < C::kSplit; ++b)
         l2_prefetch_4d(&tmap_b, kb * kRowBytes, w_row + b * kWRows);
@@ -443,7 +451,7 @@ __global__ void __launch_bounds__(Cfg<kFp4, kBN, kPair, kLin>::kThreads, 1)
       // 3072 GEMMs took 117 us at the 99th percentile, now 64; on one stream both
       // measure the same, since a CTA fills its SM.)
       if (ct + ncl >= num_ctiles) grid_dep_launch();
-      for (int kb = 0; kb < num_kb; ++kb) {
+      for (int kb = kb0; kb < kb1; ++kb) {
         if (!mbar_wait_warp(&empty[stage], phase ^ 1u, ctl)) {
           ok = false;
           break;
@@ -513,7 +521,7 @@ __global__ void __launch_bounds__(Cfg<kFp4, kBN, kPair, kLin>::kThreads, 1)
         if (!wait_ready(stage, phase)) break;
         tc_fence_after();
         const uint32_t d_tmem = tmem_base + (uint32_t)(acc * kBN);
-        for (int kb = 0; kb < num_kb; ++kb) {
+        for (int kb = kb0; kb < kb1; ++kb) {
           const uint32_t sA = smem_u32(smem + stage * C::kStageBytes);
           const uint32_t sB = sA + C::kABytes;
           const int nsteps = min(kStepsPerStage, k_steps - kb * kStepsPerStage);
@@ -524,7 +532,7 @@ __global__ void __launch_bounds__(Cfg<kFp4, kBN, kPair, kLin>::kThreads, 1)
           const uint32_t sfa0 =
               tmem_base + (uint32_t)(C::kSfColBase + slot * C::kSfColsPerSlot);
           const uint32_t sfb0 = sfa0 + (uint32_t)(kStepsPerStage * C::kSfaCols) + sfb_off;
-          const uint32_t acc0 = kb > 0 ? 1u : 0u;
+          const uint32_t acc0 = kb > kb0 ? 1u : 0u;
           auto issue = [&](int j, uint32_t accumulate) {
             const uint64_t adesc = adesc0 + (uint64_t)(2 * j);
             const uint64_t bdesc = bdesc0 + (uint64_t)(2 * j);
@@ -588,7 +596,7 @@ __global__ void __launch_bounds__(Cfg<kFp4, kBN, kPair, kLin>::kThreads, 1)
                 issue(2, 1u);
               }
             }
-            if (kb + 1 < num_kb) {
+            if (kb + 1 < kb1) {
               const bool wrap = stage + 1 == C::kStages;
               next_ready = __all_sync(0xFFFFFFFFu,
                                       mbar_test_wait(smem_u32(&full[wrap ? 0 : stage + 1]),
@@ -609,7 +617,7 @@ __global__ void __launch_bounds__(Cfg<kFp4, kBN, kPair, kLin>::kThreads, 1)
           if (++slot == C::kSfSlots) slot = 0;
           // the tile's next stage: one barrier test per stage (the scale
           // warps arrive on the same barrier as the operands)
-          if (kb + 1 < num_kb) {
+          if (kb + 1 < kb1) {
             if (!next_ready && !wait_ready(stage, phase)) {
               ok = false;
               break;
@@ -773,11 +781,11 @@ __global__ void __launch_bounds__(Cfg<kFp4, kBN, kPair, kLin>::kThreads, 1)
       const int64_t k64 = p.K >> 6;                 // atoms of a 128-row block
       // position of the next load: tile, stage and this lane's bytes of the
       // tile's two atom rows (they exist: tiles start inside M and N)
-      int lct = cid, lkb = 0;
+      int lct = cid, lkb = kb0;
       const uint8_t *arow = nullptr, *wrow = nullptr;
       auto load_next = [&](uint32_t (&v)[32]) {
         if (lct >= num_ctiles) return;
-        if (lkb == 0) {
+        if (lkb == kb0) {
           int mg, nb;
           tile_coords(lct, groups_m, &mg, &nb);
           arow = p.sfa + mg * k64 * 512 + lane * 16;
@@ -792,8 +800,8 @@ __global__ void __launch_bounds__(Cfg<kFp4, kBN, kPair, kLin>::kThreads, 1)
           v[4 * j] = a.x; v[4 * j + 1] = a.y; v[4 * j + 2] = a.z; v[4 * j + 3] = a.w;
           v[16 + 4 * j] = w.x; v[17 + 4 * j] = w.y; v[18 + 4 * j] = w.z; v[19 + 4 * j] = w.w;
         }
-        if (++lkb == num_kb) {
-          lkb = 0;
+        if (++lkb == kb1) {
+          lkb = kb0;
           lct += ncl;
         }
       };
@@ -826,7 +834,7 @@ __global__ void __launch_bounds__(Cfg<kFp4, kBN, kPair, kLin>::kThreads, 1)
         if (lane == 0) mbar_arrive(&full[stage]);
         if (++stage == C::kStages) stage = 0;
       };
-      const int64_t total = (int64_t)((num_ctiles - cid + ncl - 1) / ncl) * num_kb;
+      const int64_t total = (int64_t)((num_ctiles - cid + ncl - 1) / ncl) * (kb1 - kb0);
       uint32_t v0[32], v1[32];
       load_next(v0);
       load_next(v1);
@@ -1237,13 +1245,115 @@ __global__ void __launch_bounds__(Cfg<kFp4, kBN, kPair, kLin>::kThreads, 1)
       }
     }
   };
+  // kSplitK: one tile per cluster.  Each CTA reads its sums out of TMEM and sends every box
+  // of 32 x 32 to the CTA that finishes it (which adds them in the order of K), through the
+  // shared memory of its pipeline stages, free once all CTAs' products are done.
+  auto run_split_epilogue = [&] {
+    constexpr int kChunks = kBN / 64, kBoxes = kBN / 8;   // of 32 columns per warp; boxes
+    static_assert(C::kStages * C::kStageBytes >= kBoxes * 4096, "the boxes of split CTAs");
+    const int e = warp - C::kEpiWarp0, quarter = warp & 3, half = e >> 2;
+    const int boxes = kBoxes / splits, box = krank * boxes + e;   // box = chunk * 4 + quarter
+    int mg, nb;
+    tile_coords(cid, groups_m, &mg, &nb);
+    const int64_t n0 = (int64_t)nb * kBN + (box >> 2) * 32;
+    const int64_t row = (int64_t)mg * kBM + (box & 3) * 32 + lane;
+    const bool own = e < boxes && n0 < p.N;
+    float bias = 0.0f, s_w = 0.0f, row_scale = 1.0f;
+    uint32_t res[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) res[i] = 0x80008000u;   // -0: leaves any sum as it is
+    if (own) {
+      if (p.bias != nullptr) {
+        const uint32_t w = __ldg(reinterpret_cast<const unsigned short*>(p.bias) + n0 + lane);
+        bias = kBf16 && p.fp16 ? __half2float(__ushort_as_half((unsigned short)w)) : bf16_lo(w);
+      }
+      if (p.residual != nullptr && row < p.M) load_residual(res, p.residual + row * p.residual_stride + n0, p.r_v8 != 0);
+      if (kFp4) row_scale = __fmul_rn(*p.sdec_a, *p.sdec_w);
+      if (!kFp4 && !kBf16) {
+        s_w = __ldg(p.sdec_w + (p.w_per_channel ? n0 + lane : 0));
+        row_scale = !p.a_per_row ? *p.sdec_a : row < p.M ? __ldg(p.sdec_a + row) : 0.0f;
+      }
+    }
+    const bool ok = __all_sync(0xFFFFFFFFu, mbar_wait(&tmem_full[0], 0, ctl));
+    uint32_t r[kChunks][32];
+    if (ok) {
+      tc_fence_after();
+#pragma unroll
+      for (int c = 0; c < kChunks; ++c)
+        tmem_ld32(tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(half * (kBN / 2) + c * 32), r[c]);
+      tmem_ld_wait();
+#pragma unroll
+      for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+        for (int i = 0; i < 32; ++i) asm volatile("" : "+r"(r[c][i]));   // read after the wait
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&tmem_empty[0]);
+    }
+    __syncwarp();
+    cluster_sync();
+    if (ok) {
+#pragma unroll
+      for (int c = 0; c < kChunks; ++c) {
+        const int b = (half * kChunks + c) * 4 + quarter;
+        const uint32_t dst = mapa_shared(smem + ((b % boxes) * splits + krank) * 4096 + lane * 16, (uint32_t)(b / boxes));
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + (uint32_t)k * 512u),
+                       "r"(r[c][4 * k]), "r"(r[c][4 * k + 1]), "r"(r[c][4 * k + 2]), "r"(r[c][4 * k + 3])
+                       : "memory");
+      }
+    }
+    __syncwarp();
+    cluster_sync();
+    if (ok && own) {
+      float2 v[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) v[i] = make_float2(0.0f, 0.0f);
+      const float4* src = reinterpret_cast<const float4*>(smem + e * splits * 4096) + lane;
+      for (int t = 0; t < splits; ++t, src += 256) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const float4 q = src[k * 32];
+          v[2 * k] = add2(v[2 * k], make_float2(q.x, q.y));
+          v[2 * k + 1] = add2(v[2 * k + 1], make_float2(q.z, q.w));
+        }
+      }
+      uint32_t packed[16];
+      if (kBf16 && p.fp16)
+        finish32<kFp4, kBf16, true, true, false>(v, p, row_scale, bias, nullptr, s_w, res, packed);
+      else
+        finish32<kFp4, kBf16, false, true, false>(v, p, row_scale, bias, nullptr, s_w, res, packed);
+      uint8_t* const bufp = out_stage + e * 4096;
+      const uint32_t buf = smem_u32(bufp);
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        st_shared_v4(buf + lane * 64 + ((k ^ ((lane >> 1) & 3)) << 4), packed[4 * k], packed[4 * k + 1],
+                     packed[4 * k + 2], packed[4 * k + 3]);
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) {
+        tma_store_2d(&tmap_y, bufp, (int32_t)n0, (int32_t)(row - lane));
+        bulk_commit_group();
+        bulk_wait_group_read<0>();
+      }
+    }
+  };
   // (kHold: each warpgroup executes one setmaxnreg, at the head of all it does after)
   if (warp >= C::kEpiWarp0) {
     if constexpr (kHold) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::kHoldRegs));
-    run_epilogue();
+    if constexpr (kSplitK)
+      run_split_epilogue();
+    else
+      run_epilogue();
   } else {
     if constexpr (kHold) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kRoleRegs));
     run_role();
+    if constexpr (kSplitK) {   // the epilogue's two cluster barriers
+      __syncwarp();
+      cluster_sync();
+      cluster_sync();
+    }
   }
 
   // No CTA of the cluster may exit while a peer can still multicast into it
@@ -1341,6 +1451,16 @@ CUresult encode_scales(CUtensorMap* map, const void* base, uint64_t rows, uint64
                    CU_TENSOR_MAP_SWIZZLE_NONE);
 }
 
+Tile tile_of(const GemmArgs& a, int num_sms) {
+  return choose_tile(a.fp4 ? GemmKind::kNvfp4 : a.bf16 ? GemmKind::k16 : GemmKind::kFp8,
+                     a.epilogue              ? (a.next_scale != nullptr ? Epilogue::kLinearRequant
+                                                                        : Epilogue::kLinear)
+                     : a.next_scale != nullptr ? Epilogue::kRequant
+                     : a.y_amax != nullptr     ? Epilogue::kAmax
+                                               : Epilogue::kPlain,
+                     a.M, a.N, a.K, num_sms);
+}
+
 template <bool kFp4, int kBN, bool kPair, bool kRequant, bool kBf16 = false, int kLin = 0>
 cudaError_t launch_cfg(const GemmArgs& a, cudaStream_t s, Device dev, unsigned* err,
                        uint64_t timeout_ns) {
@@ -1391,6 +1511,7 @@ cudaError_t launch_cfg(const GemmArgs& a, cudaStream_t s, Device dev, unsigned* 
   p.act = a.act;
   p.a_per_row = a.a_per_row ? 1 : 0;
   p.r_v8 = ((reinterpret_cast<uintptr_t>(a.residual) | (uintptr_t)(a.residual_stride * 2)) & 31u) == 0 ? 1 : 0;
+  p.split = a.split;
   auto kern = gemm_kernel<kFp4, kBN, kPair, kRequant, kBf16, kLin>;
 
   cudaLaunchConfig_t cfg{};
@@ -1428,18 +1549,12 @@ cudaError_t launch_cfg(const GemmArgs& a, cudaStream_t s, Device dev, unsigned* 
   const int64_t ctiles = ((tiles_m + kCM - 1) / kCM) * ((a.N + kBN - 1) / kBN);
   const int clusters = (int)std::min<int64_t>(ctiles, std::min(setup.max_clusters, dev.num_sms / kCM));
   cfg.gridDim = dim3((unsigned)(clusters * kCM), 1, 1);
+  if (kLin == 3) {   // a cluster per tile
+    cfg.gridDim.x = (unsigned)(ctiles * a.split);
+    attr[0].val.clusterDim.x = (unsigned)a.split;
+  }
   cfg.numAttrs = 2;
   return cudaLaunchKernelEx(&cfg, kern, ta, tb, tsa, tsb, ty, p);
-}
-
-Tile tile_of(const GemmArgs& a, int num_sms) {
-  return choose_tile(a.fp4 ? GemmKind::kNvfp4 : a.bf16 ? GemmKind::k16 : GemmKind::kFp8,
-                     a.epilogue              ? (a.next_scale != nullptr ? Epilogue::kLinearRequant
-                                                                        : Epilogue::kLinear)
-                     : a.next_scale != nullptr ? Epilogue::kRequant
-                     : a.y_amax != nullptr     ? Epilogue::kAmax
-                                               : Epilogue::kPlain,
-                     a.M, a.N, a.K, num_sms);
 }
 
 template <bool kFp4, int kLin>
@@ -1478,6 +1593,10 @@ CUresult encode_tensor_map_out_bf16(CUtensorMap* map, void* base, uint64_t cols,
 
 cudaError_t launch_gemm(const GemmArgs& a, cudaStream_t s, Device dev, unsigned* err,
                         uint64_t timeout_ns) {
+  if (a.split > 1)
+    return a.bf16  ? launch_cfg<false, 128, false, false, true, 3>(a, s, dev, err, timeout_ns)
+           : a.fp4 ? launch_cfg<true, 128, false, false, false, 3>(a, s, dev, err, timeout_ns)
+                   : launch_cfg<false, 128, false, false, false, 3>(a, s, dev, err, timeout_ns);
   if (a.bf16) {
     const bool pair = tile_of(a, dev.num_sms) == Tile::kPair;
     if (a.residual != nullptr)

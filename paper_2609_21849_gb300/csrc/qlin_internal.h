@@ -113,7 +113,8 @@ struct GemmArgs {
   int64_t residual_stride;
   int act;                  // qlin_activation
   bool a_per_row;           // FP8: sdec_a has M entries
-  bool few_ok;              // a call that may take the few-token kernel
+  bool few_ok;              // a call that may take the few-token kernel or a split K
+  int split;                // CTAs that share a tile's K (0, 1: none)
 };
 cudaError_t launch_gemm(const GemmArgs& a, cudaStream_t s, Device dev, unsigned* err,
                         uint64_t timeout_ns);

@@ -17,6 +17,10 @@ enum class GemmKind { kNvfp4, kFp8, k16 };     // k16: bf16 / fp16 operands
 // What the epilogue does beside writing y (kLinear: bias, activation and residual).
 enum class Epilogue { kPlain, kRequant, kAmax, kLinear, kLinearRequant };
 
+inline int64_t k_row_bytes(GemmKind kind, int64_t K) {
+  return kind == GemmKind::kNvfp4 ? K / 2 : kind == GemmKind::k16 ? K * 2 : K;
+}
+
 // Time of a launch in a tile configuration, in microseconds: a launch, then
 // waves of tiles that each cost a start and end and their K stages.  Fitted
 // to graph-replayed launches over M 16-4608, N 256-6144, K 256-3072 (operands
@@ -54,8 +58,7 @@ inline Tile choose_tile(GemmKind kind, Epilogue epi, int64_t M, int64_t N, int64
   const bool narrow_ok =
       epi != Epilogue::kRequant && epi != Epilogue::kLinearRequant && kind != GemmKind::k16;
   const TileCost* cost = kCosts[(int)kind];
-  const int64_t k_bytes = fp4 ? K / 2 : kind == GemmKind::k16 ? K * 2 : K;
-  const int64_t stages = (k_bytes + kStageRowBytes - 1) / kStageRowBytes;
+  const int64_t stages = (k_row_bytes(kind, K) + kStageRowBytes - 1) / kStageRowBytes;
   const int64_t tiles_m = (M + kTileM - 1) / kTileM;
   const int64_t n128 = (N + 127) / 128, n256 = (N + 255) / 256;
   // An output amax costs single-CTA tiles more per wave (its reductions, and y
@@ -82,6 +85,27 @@ inline Tile choose_tile(GemmKind kind, Epilogue epi, int64_t M, int64_t N, int64
   return static_cast<Tile>(pick);
 }
 
+// CTAs of a cluster that share a tile's K, for 128 x 128 tiles too few to fill the machine.
+// Sending the sums and joining them costs 1.5-3 us, so K has to be long, longer where there
+// is room for two CTAs only or, with two more barriers' worth of skew, for eight.  (M x N x K
+// in us with one, two and four CTAs: NVFP4 552 x 832 x 2048 6.5, 7.3, 7.5; x 3072 8.2, 8.2,
+// 8.0; x 12288 20.8, 14.7, 11.6; FP8 x 3072 8.1, 8.5, 8.2; x 12288 20.2, 15.1, 12.1; bf16 x
+// 1024 7.9, 7.5, 7.7; x 12288 43.2, 23.9, 17.0.  With four and eight: 352 x 320 x 12288 NVFP4
+// 10.4, 8.9; FP8 10.5, 9.3; bf16 352 x 640 x 2048 7.7, 8.0.)  A cluster of eight needs eight
+// SMs of one GPC: fifteen run at once on 152 SMs, with sixteen tiles some wait (bf16 500 x
+// 512 x 2048 14.3 us, with four CTAs 7.8).
+inline int choose_split_k(GemmKind kind, int64_t M, int64_t N, int64_t K, int num_sms) {
+  static const int kLeast[3][3] = {{16, 12, 24}, {44, 24, 48}, {20, 16, 44}};   // stages; 2, 4, 8 CTAs
+  const int64_t stages = (k_row_bytes(kind, K) + kStageRowBytes - 1) / kStageRowBytes;
+  const int64_t tiles_m = (M + kTileM - 1) / kTileM, tiles_n = (N + 127) / 128;
+  if (tiles_m > num_sms || tiles_n > num_sms) return 1;
+  const int64_t tiles = tiles_m * tiles_n;
+  const int* least = kLeast[(int)kind];
+  if (10 * 8 * tiles <= 8 * (int64_t)num_sms && stages >= least[2]) return 8;
+  if (4 * tiles <= num_sms && stages >= least[1]) return 4;
+  return 2 * tiles <= num_sms && stages >= least[0] ? 2 : 1;
+}
+
 // Whether a linear takes the few-token kernel, which reads W once per 16 tokens, rather
 // than the tiles above: always up to 16 tokens, beyond that as long as its units, 16 rows
 // of W and 16 tokens, are at most 5.2 per SM with 16-bit operands, 2.6 with others (1.9
@@ -97,6 +121,19 @@ inline bool few_tokens(bool float16, int64_t M, int64_t N, int64_t row_bytes, in
   const int limit = float16 ? 52 : M <= 32 || row_bytes >= 2048 ? 26 : 19;
   // (M < 2^31 and N / 16 < 2^59: beyond a limit that large grids exceed anyway)
   return N / 16 <= limit * (int64_t)num_sms && 10 * (N / 16) * ((M + 15) / 16) <= limit * (int64_t)num_sms;
+}
+
+// Whether tiles with a split K take a linear that few_tokens would give to the few-token
+// kernel: from 65 tokens, once the few-token kernel's units have much of W to read (units
+// per SM times kilobytes of a row).  Few / split, in us: bf16 552 x 64 x 4096 7.2 / 8.1 (7),
+// 176 x 768 x 2560 9.2 / 8.1 (18), 176 x 320 x 12288 16.7 / 11.2 (35), 48 x 768 x 12288 10.9
+// / 11.9; FP8 960 x 64 x 4096 6.9 / 7.5 (6.5), 128 x 768 x 4096 8.8 / 7.1 (10); NVFP4 552 x
+// 128 x 4096 5.7 / 6.4 (3.7), 352 x 128 x 12288 11.7 / 8.1 (7).
+inline bool split_over_few(GemmKind kind, int64_t M, int64_t N, int64_t K, int num_sms) {
+  const double units = (double)(N / 16) * (double)((M + 15) / 16) / num_sms;
+  const double least = kind == GemmKind::kNvfp4 ? 4.5 : kind == GemmKind::kFp8 ? 8.0 : 12.0;
+  return M > 64 && units * ((double)k_row_bytes(kind, K) / 1024) >= least &&
+         choose_split_k(kind, M, N, K, num_sms) > 1;
 }
 
 }  // namespace qlin

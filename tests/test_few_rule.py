@@ -39,3 +39,51 @@ def test_rule(tmp_path):
     text = "".join("%d %d %d %d 152\n" % c for c, _ in cases)
     out = subprocess.run([str(tmp_path / "main")], input=text, capture_output=True, text=True, check=True)
     assert [int(v) for v in out.stdout.split()] == [w for _, w in cases]
+
+
+SPLIT = r"""
+#include <cstdio>
+#include "qlin_tiles.h"
+int main() {
+  int kind, sms; long long m, n, k;
+  while (std::scanf("%d %lld %lld %lld %d", &kind, &m, &n, &k, &sms) == 5)
+    std::printf("%d %d\n", qlin::choose_split_k((qlin::GemmKind)kind, m, n, k, sms),
+                (int)qlin::split_over_few((qlin::GemmKind)kind, m, n, k, sms));
+}
+"""
+
+
+def test_split_rule(tmp_path):
+    cxx = shutil.which("g++")
+    if cxx is None:
+        pytest.skip("no C++ compiler")
+    (tmp_path / "split.cpp").write_text(SPLIT)
+    csrc = os.path.join(ROOT, "paper_2609_21849_gb300", "csrc")
+    subprocess.run([cxx, "-std=c++17", "-I" + csrc, str(tmp_path / "split.cpp"), "-o", str(tmp_path / "split")],
+                   check=True)
+
+    def rule(kind, m, n, k):
+        out = subprocess.run([str(tmp_path / "split")], input="%d %d %d %d 152\n" % (kind, m, n, k), capture_output=True,
+                             text=True, check=True).stdout.split()
+        return int(out[0]), int(out[1])
+
+    nvfp4, fp8, f16 = 0, 1, 2
+    assert rule(nvfp4, 552, 832, 3072)[0] == 4 and rule(nvfp4, 552, 832, 2816)[0] == 1     # 12 stages, 11
+    assert rule(fp8, 552, 832, 3072)[0] == 4 and rule(fp8, 552, 832, 2944)[0] == 1
+    assert rule(f16, 552, 832, 1024)[0] == 4 and rule(f16, 552, 832, 960)[0] == 1
+    assert rule(f16, 300, 3072, 1024)[0] == 1 and rule(f16, 300, 3072, 1280)[0] == 2       # 72 tiles
+    assert rule(f16, 300, 3328, 12288)[0] == 1                                             # 78
+    assert rule(f16, 352, 640, 4096)[0] == 8 and rule(f16, 512, 512, 4096)[0] == 4         # 15 tiles, 16
+    assert rule(f16, 2**31 - 1, 2**40, 12288)[0] == 1
+    # against the few-token kernel: more than 64 tokens, much of W to read
+    assert rule(f16, 552, 64, 4096)[1] == 0 and rule(f16, 176, 768, 2560)[1] == 1
+    assert rule(f16, 64, 768, 12288)[1] == 0 and rule(f16, 65, 768, 12288)[1] == 1
+    assert rule(nvfp4, 552, 128, 4096)[1] == 0 and rule(nvfp4, 352, 128, 12288)[1] == 1
+    # every split leaves each CTA a stage
+    for kind in (nvfp4, fp8, f16):
+        for m in (17, 129, 500, 2000):
+            for n in (64, 320, 1024, 3072):
+                for k in range(64, 6145, 320):
+                    s = rule(kind, m, n, k)[0]
+                    row = k // 2 if kind == nvfp4 else 2 * k if kind == f16 else k
+                    assert s == 1 or s <= (row + 127) // 128

@@ -91,7 +91,8 @@ def _check(y, a, w, bias, act, residual, what):
 # one token and a few; partial tiles; long and short K; each tile configuration
 SHAPES = [(1, 64, 64), (1, 1024, 2560), (2, 192, 3136), (5, 576, 1088), (8, 3072, 512), (9, 64, 12288), (16, 320, 192),
           (17, 2112, 320), (33, 1024, 4160), (77, 320, 192), (129, 576, 1088), (300, 128, 512), (1300, 3648, 320),
-          (2048, 4096, 1088), (552, 64, 4160), (1000, 576, 1088), (1040, 128, 320), (1500, 64, 1088)]
+          (2048, 4096, 1088), (552, 64, 4160), (1000, 576, 1088), (1040, 128, 320), (1500, 64, 1088),
+          (300, 1024, 4160), (352, 320, 12288), (555, 832, 6208), (300, 3136, 6080)]
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
@@ -118,7 +119,7 @@ def test_parts(M, fmt):
 @pytest.mark.parametrize("M", [900, 2048])
 def test_without_an_epilogue_as_the_plain_gemm(M, fmt):
     # at these sizes the same kernel runs: bit for bit
-    N, K = (4096, 1088) if M == 2048 else (320, 1088)
+    N, K = (4096, 1088) if M == 2048 else (320, 960)
     a, w, _, _, _ = _operands(fmt, M, N, K, 3)
     plain = getattr(qlin, "qlin_gemm_" + fmt)(a, w)
     assert torch.equal(_call(fmt, a, w), plain)
@@ -224,6 +225,39 @@ def test_repeated_and_on_another_stream(fmt):
         g.replay()
         torch.cuda.synchronize()
         assert torch.equal(y, y0) and qlin.qlin_sync_status() == 0
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("M,N,K", [(352, 640, 12288), (555, 832, 6208), (129, 3136, 6080)])
+def test_tiles_that_share_k(M, N, K, fmt):
+    # eight, four and two CTAs per tile; rows and columns past the edges
+    a, w, bias, res, dt = _operands(fmt, M, N, K, K)
+    for b, act, r in ((None, qlin.QLIN_ACT_NONE, None), (bias, qlin.QLIN_ACT_NONE, None), (None, qlin.QLIN_ACT_NONE, res),
+                      (bias, qlin.QLIN_ACT_GELU, res)):
+        y = _call(fmt, a, w, b, act, r)
+        _check(y, a, w, b, act, r, (fmt, M, N, K, b is None, r is None))
+    # a residual in place and strided, an output that is only 16-byte aligned, other streams
+    place = res.clone()
+    _call(fmt, a, w, bias, qlin.QLIN_ACT_GELU, place, place)
+    assert torch.equal(place, y)
+    wide = torch.zeros(M, N + 24, dtype=dt, device="cuda")
+    wide[:, 8:8 + N] = res
+    flat = torch.full((M * N + 16,), 5.0, dtype=dt, device="cuda")
+    _call(fmt, a, w, bias, qlin.QLIN_ACT_GELU, wide[:, 8:8 + N], flat[8:8 + M * N].view(M, N))
+    assert torch.equal(flat[8:8 + M * N].view(M, N), y) and (flat[:8] == 5).all() and (flat[-8:] == 5).all()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    ys = [_call(fmt, a, w, bias, qlin.QLIN_ACT_GELU, res, stream=side) for _ in range(20)]
+    side.synchronize()
+    assert all(torch.equal(v, y) for v in ys)
+    # special values stay in their rows and columns
+    bias[3], bias[N - 1] = float("inf"), float("nan")
+    r2 = res.clone()
+    r2[M - 1, 20] = float("-inf")
+    y2 = _call(fmt, a, w, bias, qlin.QLIN_ACT_GELU, r2)
+    assert (y2[:, 3] == float("inf")).all() and y2[:, N - 1].isnan().all() and y2[M - 1, 20] == float("-inf")
+    y2[:, 3], y2[:, N - 1], y2[M - 1, 20] = y[:, 3], y[:, N - 1], y[M - 1, 20]
+    assert torch.equal(y2, y) and qlin.qlin_sync_status() == 0
 
 
 def test_refusals_of_tensors():
