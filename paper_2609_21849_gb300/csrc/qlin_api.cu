@@ -250,17 +250,15 @@ static qlin_status set_epilogue(GemmArgs& a, const qlin_epilogue_t* ep) {
 }
 
 // The plain GEMMs always take whole tensor-core tiles, so that their sums keep their
-// order; the linears take the few-token kernel or tiles with a split K where those apply
-// (no split with a re-quantized output, whose groups of columns are wider than its boxes).
+// order; the linears take the few-token kernel or tiles with a split K where those apply.
 static cudaError_t launch_linear(GemmArgs& a, cudaStream_t s, Device dev, unsigned* status) {
   const GemmKind kind = a.fp4 ? GemmKind::kNvfp4 : a.bf16 ? GemmKind::k16 : GemmKind::kFp8;
-  const bool can_split = a.few_ok && a.next_scale == nullptr;
   // (the few-token kernel counts a row's bytes in 32 bits)
   if (a.few_ok && a.K <= (int64_t)1 << 28 &&
       few_tokens(a.bf16, a.M, a.N, k_row_bytes(kind, a.K), dev.num_sms) &&
-      !(can_split && split_over_few(kind, a.M, a.N, a.K, dev.num_sms)))
+      !split_over_few(kind, a.M, a.N, a.K, dev.num_sms))
     return launch_few(a, s, dev);
-  a.split = can_split ? choose_split_k(kind, a.M, a.N, a.K, dev.num_sms) : 1;
+  a.split = a.few_ok ? choose_split_k(kind, a.M, a.N, a.K, dev.num_sms) : 1;
   return launch_gemm(a, s, dev, status, timeout());
 }
 

@@ -324,7 +324,7 @@ __global__ void __launch_bounds__(Cfg<kFp4, kBN, kPair, kLin>::kThreads, 1)
                 const __grid_constant__ CUtensorMap tmap_sfb,
                 const __grid_constant__ CUtensorMap tmap_y, const KParams p) {
   constexpr bool kEpi = kLin != 0, kRes = kLin == 2, kSplitK = kLin == 3;
-  static_assert(!kSplitK || (!kPair && !kRequant), "split tiles");
+  static_assert(!kSplitK || (!kPair && !kRequant), "split tiles (their own epilogue also re-quantizes)");
   using C = Cfg<kFp4, kBN, kPair, kLin>;
   constexpr bool kHold = C::kHold;
   constexpr int kCM = kPair ? 2 : 1;          // CTAs per cluster (M tiles per cluster tile)
@@ -1258,7 +1258,12 @@ __global__ void __launch_bounds__(Cfg<kFp4, kBN, kPair, kLin>::kThreads, 1)
     const int64_t n0 = (int64_t)nb * kBN + (box >> 2) * 32;
     const int64_t row = (int64_t)mg * kBM + (box & 3) * 32 + lane;
     const bool own = e < boxes && n0 < p.N;
-    float bias = 0.0f, s_w = 0.0f, row_scale = 1.0f;
+    float bias = 0.0f, s_w = 0.0f, row_scale = 1.0f, s_enc_next = 0.0f;
+    if (!kBf16 && p.next_scale != nullptr) {
+      const float s_next = *p.next_scale;
+      s_enc_next = encode_scale(s_next);
+      if (blockIdx.x == 0 && e == 0 && lane == 0 && p.rq_tensor_scale != p.next_scale) *p.rq_tensor_scale = s_next;
+    }
     uint32_t res[16];
 #pragma unroll
     for (int i = 0; i < 16; ++i) res[i] = 0x80008000u;   // -0: leaves any sum as it is
@@ -1324,19 +1329,61 @@ __global__ void __launch_bounds__(Cfg<kFp4, kBN, kPair, kLin>::kThreads, 1)
         finish32<kFp4, kBf16, true, true, false>(v, p, row_scale, bias, nullptr, s_w, res, packed);
       else
         finish32<kFp4, kBf16, false, true, false>(v, p, row_scale, bias, nullptr, s_w, res, packed);
-      uint8_t* const bufp = out_stage + e * 4096;
-      const uint32_t buf = smem_u32(bufp);
+      if (p.y != nullptr) {
+        uint8_t* const bufp = out_stage + e * 4096;
+        const uint32_t buf = smem_u32(bufp);
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
-        st_shared_v4(buf + lane * 64 + ((k ^ ((lane >> 1) & 3)) << 4), packed[4 * k], packed[4 * k + 1],
-                     packed[4 * k + 2], packed[4 * k + 3]);
-      fence_proxy_async_smem();
-      __syncwarp();
-      if (lane == 0) {
-        tma_store_2d(&tmap_y, bufp, (int32_t)n0, (int32_t)(row - lane));
-        bulk_commit_group();
-        bulk_wait_group_read<0>();
+        for (int k = 0; k < 4; ++k)
+          st_shared_v4(buf + lane * 64 + ((k ^ ((lane >> 1) & 3)) << 4), packed[4 * k], packed[4 * k + 1],
+                       packed[4 * k + 2], packed[4 * k + 3]);
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+          tma_store_2d(&tmap_y, bufp, (int32_t)n0, (int32_t)(row - lane));
+          bulk_commit_group();
+        }
       }
+      // the re-quantized columns: 32 codes, or two blocks (windows are multiples of 64)
+      if (!kBf16 && p.next_scale != nullptr && row < p.M && n0 >= p.rq_col0 && n0 < p.rq_col0 + p.rq_cols) {
+        const int64_t lc = n0 - p.rq_col0;
+        uint32_t words[8];
+        if constexpr (!kFp4) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            words[i] = e4m3x4(__fmul_rn(bf16_lo(packed[2 * i]), s_enc_next), __fmul_rn(bf16_hi(packed[2 * i]), s_enc_next),
+                              __fmul_rn(bf16_lo(packed[2 * i + 1]), s_enc_next),
+                              __fmul_rn(bf16_hi(packed[2 * i + 1]), s_enc_next));
+          uint8_t* const cp = p.rq_codes + row * p.rq_cols + lc;
+          st_global_v4(cp, words[0], words[1], words[2], words[3]);
+          st_global_v4(cp + 16, words[4], words[5], words[6], words[7]);
+        } else {
+          uint32_t scales = 0;
+#pragma unroll
+          for (int b = 0; b < 2; ++b) {
+            uint32_t m = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) m = __vmaxu2(m, packed[8 * b + i] & 0x7FFF7FFFu);
+            m = max(m & 0xFFFFu, m >> 16);
+            const uint32_t sb = e4m3_code_div6(__fmul_rn(__uint_as_float(m << 16), s_enc_next));
+            const float r_b = sb == 0u ? 0.0f : __fdiv_rn(s_enc_next, e4m3_value(sb));
+            scales |= sb << (8 * b);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              float f[8];
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                f[2 * i] = bf16_lo(packed[8 * b + 4 * h + i]);
+                f[2 * i + 1] = bf16_hi(packed[8 * b + 4 * h + i]);
+                mul2_rn(f[2 * i], f[2 * i + 1], r_b);
+              }
+              words[2 * b + h] = e2m1x8(f);
+            }
+          }
+          st_global_v4(p.rq_codes + row * (p.rq_cols / 2) + lc / 2, words[0], words[1], words[2], words[3]);
+          *reinterpret_cast<uint16_t*>(p.rq_scales + scale_offset(row, lc / 16, p.rq_cols)) = (uint16_t)scales;
+        }
+      }
+      if (lane == 0) bulk_wait_group_read<0>();
     }
   };
   // (kHold: each warpgroup executes one setmaxnreg, at the head of all it does after)

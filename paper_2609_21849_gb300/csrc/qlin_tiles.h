@@ -91,11 +91,12 @@ inline Tile choose_tile(GemmKind kind, Epilogue epi, int64_t M, int64_t N, int64
 // in us with one, two and four CTAs: NVFP4 552 x 832 x 2048 6.5, 7.3, 7.5; x 3072 8.2, 8.2,
 // 8.0; x 12288 20.8, 14.7, 11.6; FP8 x 3072 8.1, 8.5, 8.2; x 12288 20.2, 15.1, 12.1; bf16 x
 // 1024 7.9, 7.5, 7.7; x 12288 43.2, 23.9, 17.0.  With four and eight: 352 x 320 x 12288 NVFP4
-// 10.4, 8.9; FP8 10.5, 9.3; bf16 352 x 640 x 2048 7.7, 8.0.)  A cluster of eight needs eight
+// 10.4, 8.9; FP8 10.5, 9.3; bf16 352 x 640 x 2048 7.7, 8.0.  All with W from HBM; from L2 a
+// single CTA gains more, NVFP4 555 x 832 x 4096 7.6 against 8.2.)  A cluster of eight needs eight
 // SMs of one GPC: fifteen run at once on 152 SMs, with sixteen tiles some wait (bf16 500 x
 // 512 x 2048 14.3 us, with four CTAs 7.8).
 inline int choose_split_k(GemmKind kind, int64_t M, int64_t N, int64_t K, int num_sms) {
-  static const int kLeast[3][3] = {{16, 12, 24}, {44, 24, 48}, {20, 16, 44}};   // stages; 2, 4, 8 CTAs
+  static const int kLeast[3][3] = {{20, 16, 24}, {48, 32, 48}, {24, 20, 44}};   // stages; 2, 4, 8 CTAs
   const int64_t stages = (k_row_bytes(kind, K) + kStageRowBytes - 1) / kStageRowBytes;
   const int64_t tiles_m = (M + kTileM - 1) / kTileM, tiles_n = (N + 127) / 128;
   if (tiles_m > num_sms || tiles_n > num_sms) return 1;

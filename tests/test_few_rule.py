@@ -68,10 +68,10 @@ def test_split_rule(tmp_path):
         return int(out[0]), int(out[1])
 
     nvfp4, fp8, f16 = 0, 1, 2
-    assert rule(nvfp4, 552, 832, 3072)[0] == 4 and rule(nvfp4, 552, 832, 2816)[0] == 1     # 12 stages, 11
-    assert rule(fp8, 552, 832, 3072)[0] == 4 and rule(fp8, 552, 832, 2944)[0] == 1
-    assert rule(f16, 552, 832, 1024)[0] == 4 and rule(f16, 552, 832, 960)[0] == 1
-    assert rule(f16, 300, 3072, 1024)[0] == 1 and rule(f16, 300, 3072, 1280)[0] == 2       # 72 tiles
+    assert rule(nvfp4, 552, 832, 4096)[0] == 4 and rule(nvfp4, 552, 832, 3840)[0] == 1     # 16 stages, 15
+    assert rule(fp8, 552, 832, 4096)[0] == 4 and rule(fp8, 552, 832, 3968)[0] == 1
+    assert rule(f16, 552, 832, 1280)[0] == 4 and rule(f16, 552, 832, 1216)[0] == 1
+    assert rule(f16, 300, 3072, 1472)[0] == 1 and rule(f16, 300, 3072, 1536)[0] == 2       # 72 tiles
     assert rule(f16, 300, 3328, 12288)[0] == 1                                             # 78
     assert rule(f16, 352, 640, 4096)[0] == 8 and rule(f16, 512, 512, 4096)[0] == 4         # 15 tiles, 16
     assert rule(f16, 2**31 - 1, 2**40, 12288)[0] == 1

@@ -144,7 +144,8 @@ def test_residual_in_place_and_strided(M, fmt):
 
 
 @pytest.mark.parametrize("M,N,K", [(1, 64, 64), (3, 320, 1088), (16, 1024, 512), (40, 576, 320), (333, 512, 1088),
-                                   (2048, 4096, 320), (700, 64, 2112)])
+                                   (2048, 4096, 320), (700, 64, 2112),
+                                   (352, 640, 12288), (555, 832, 6208), (129, 3136, 6080)])
 @pytest.mark.parametrize("fmt", ["nvfp4", "fp8", "fp8_rows"])
 def test_requantized_output(M, N, K, fmt):
     a, w, bias, res, _ = _operands(fmt, M, N, K, M + N)
