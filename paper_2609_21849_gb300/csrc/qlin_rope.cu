@@ -95,7 +95,7 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(const RopeParams p) {
 // rotations behind a barrier took 24.8 us, scalar accesses 57.  Where the lanes of a
 // head do not divide a warp some idle (192 of 192: 24 of 32 lanes, 70%), and where the
 // pairs do not fill their last lane; 9079 x 25 x 80 of which 40 turn 17.4 us interleaved,
-// 19.3 in halves (element by element 57).  One token takes 1.9 us, a launch and one chain
+// 19.3 in halves (element by element 57).  One token takes 1.8 us, a launch and one chain
 // of loads.
 // kItems heads of a lane are in flight at once (4, where work is plenty).
 constexpr int kMostItems = 4;
@@ -343,9 +343,12 @@ cudaError_t launch_rope(const qlin_rope_t& a, int num_sms, cudaStream_t s) {
     u.slots = 32 / u.per_head;
     u.tokens = std::max(1, u.slots / p.heads);
     const int steps = (p.heads + u.slots - 1) / u.slots;
-    // up to four of them per warp, as far as 16 warps per SM are left
+    // Two of them per warp (T x H x D in halves, us with one and two: 1 x 64 x 128 2.1, 1.8;
+    // 206 x 35 x 256 5.3, 3.9; with two and four: 2048 x 32 x 128 8.0, 9.1), four where
+    // warps are plenty even so (4608 x 24 x 192 20.2, 18.3), three rather than two and
+    // one (5674 x 9 x 128 8.8, 8.4).
     const int64_t fill = (a.tokens + u.tokens - 1) / u.tokens * steps / (16 * num_sms);
-    const int most = (int)std::max<int64_t>(1, std::min<int64_t>(fill, kMostItems));
+    const int most = fill >= 16 ? kMostItems : fill >= 4 && steps == 3 ? 3 : 2;
     const int groups = std::min((steps + most - 1) / most, 65535);
     const int per_warp = (steps + groups - 1) / groups;
     u.heads = per_warp * u.slots;
