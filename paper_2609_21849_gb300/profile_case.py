@@ -15,6 +15,7 @@ Cases (seeded synthetic inputs, shapes of the paper's workloads):
   rope_qk          rotary positions of 4608 x 48 heads of 128 inside a QKV output
   linear_up        NVFP4 linear 4608 x 12288 x 3072, bias, tanh GELU, re-quantized
   linear_one       bf16 linear 1 x 12288 x 3072, bias and SiLU
+  linear_split     bf16 linear 552 x 832 x 12288 (tiles that share K), bias and SiLU
 Prints the mean device time per launch (CUDA events, not for use under a
 profiler).
 """
@@ -85,10 +86,11 @@ def make_case(name: str):
         b = torch.zeros(W.rows, dtype=torch.bfloat16, device="cuda")
         yq, sc = qlin.alloc_nvfp4(A.rows, W.rows), torch.tensor([np.float32(0.002)], device="cuda")
         return lambda: qlin.qlin_linear_nvfp4(A, W, b, qlin.QLIN_ACT_GELU_TANH, None, None, sc, yq)
-    if name == "linear_one":
-        x = torch.randn(1, 3072, device="cuda").bfloat16()
-        w, b = torch.randn(12288, 3072, device="cuda").bfloat16(), torch.zeros(12288, dtype=torch.bfloat16, device="cuda")
-        y = torch.empty(1, 12288, dtype=torch.bfloat16, device="cuda")
+    if name in ("linear_one", "linear_split"):
+        M, N, K = (1, 12288, 3072) if name == "linear_one" else (552, 832, 12288)
+        x = torch.randn(M, K, device="cuda").bfloat16()
+        w, b = torch.randn(N, K, device="cuda").bfloat16(), torch.zeros(N, dtype=torch.bfloat16, device="cuda")
+        y = torch.empty(M, N, dtype=torch.bfloat16, device="cuda")
         return lambda: qlin.qlin_linear_bf16(x, w, b, qlin.QLIN_ACT_SILU, None, y)
     raise SystemExit(f"unknown case {name}")
 
