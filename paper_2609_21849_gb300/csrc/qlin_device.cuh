@@ -563,6 +563,19 @@ __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
   return r;
 }
 
+// The same with negative values rounded to zero (a NaN stays).
+__device__ __forceinline__ uint32_t pack_bf16x2_relu(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.relu.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+
+__device__ __forceinline__ uint32_t pack_f16x2_relu(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.relu.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 
@@ -721,7 +734,7 @@ __device__ __forceinline__ void activate(float2 (&v)[N], int act) {
     case 1:
 #pragma unroll
       for (int i = 0; i < N; ++i)   // (a NaN stays)
-        v[i] = make_float2(v[i].x < 0.0f ? 0.0f : v[i].x, v[i].y < 0.0f ? 0.0f : v[i].y);
+        asm("max.NaN.f32 %0, %0, 0f00000000;\n\tmax.NaN.f32 %1, %1, 0f00000000;" : "+f"(v[i].x), "+f"(v[i].y));
       break;
     case 2:
 #pragma unroll
