@@ -912,7 +912,7 @@ __global__ void __launch_bounds__(Cfg<kFp4, kBN, kPair, kLin>::kThreads, 1)
       // tile's rows of it into L2
       float bias[kEpi ? kChunks : 1], s_w[kEpi ? kChunks : 1];
       float* const bias_s = bias_copies + (C::kSmemBias ? e * kCols : 0);
-      constexpr int kResHeld = !kRes ? 1 : kHold && !kFp4 ? kChunks : 2;
+      constexpr int kResHeld = !kRes ? 1 : kHold && !kFp4 ? kChunks : kChunks % 2 != 0 ? 1 : 2;
       uint32_t res[kResHeld][16];
       const uint16_t* const res_row = kRes && row < p.M ? p.residual + row * p.residual_stride : nullptr;
       auto load_res = [&](int b, int c) {
@@ -1100,7 +1100,7 @@ __global__ void __launch_bounds__(Cfg<kFp4, kBN, kPair, kLin>::kThreads, 1)
         // Groups of two chunks in a rolled loop: unrolled over the tile, the activations'
         // code outgrew the instruction caches.  kHold: all columns into registers, then
         // TMEM is free; each group then moves down.
-        constexpr int kGroup = kChunks < 2 ? 1 : 2;
+        constexpr int kGroup = kChunks % 2 != 0 ? 1 : 2;
         constexpr int kRaw = kHold ? kChunks : kGroup;
         uint32_t r[kRaw][32];
         auto load_raw = [&](int c0) {
@@ -1134,7 +1134,7 @@ __global__ void __launch_bounds__(Cfg<kFp4, kBN, kPair, kLin>::kThreads, 1)
                 finish32<kFp4, kBf16, true, kRes, C::kSmemBias>(v, p, row_scale, bias[b], bias_s + (c0 + b) * 32, s_w[b], res[kRes ? b : 0], packed + b * 16);
               else
                 finish32<kFp4, kBf16, false, kRes, C::kSmemBias>(v, p, row_scale, bias[b], bias_s + (c0 + b) * 32, s_w[b], res[kRes ? b : 0], packed + b * 16);
-              if (kResHeld == 2) load_res(b, c0 + kGroup + b);
+              if (kResHeld == kGroup) load_res(b, c0 + kGroup + b);
               store_y(c0 + b, packed + b * 16);
             }
             if constexpr (kRequant) requant(c0 / 2, packed);
@@ -1651,7 +1651,11 @@ cudaError_t launch_gemm(const GemmArgs& a, cudaStream_t s, Device dev, unsigned*
            : a.fp4 ? launch_cfg<true, 128, false, false, false, 3>(a, s, dev, err, timeout_ns)
                    : launch_cfg<false, 128, false, false, false, 3>(a, s, dev, err, timeout_ns);
   if (a.bf16) {
-    const bool pair = tile_of(a, dev.num_sms) == Tile::kPair;
+    const Tile tile = tile_of(a, dev.num_sms);
+    const bool pair = tile == Tile::kPair;
+    if (tile == Tile::kWide)
+      return a.residual != nullptr ? launch_cfg<false, 192, false, false, true, 2>(a, s, dev, err, timeout_ns)
+                                   : launch_cfg<false, 192, false, false, true, 1>(a, s, dev, err, timeout_ns);
     if (a.residual != nullptr)
       return pair ? launch_cfg<false, 256, true, false, true, 2>(a, s, dev, err, timeout_ns)
                   : launch_cfg<false, 128, false, false, true, 2>(a, s, dev, err, timeout_ns);

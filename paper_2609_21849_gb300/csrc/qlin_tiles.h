@@ -11,7 +11,7 @@ namespace qlin {
 constexpr int kTileM = 128;         // rows of a CTA's tile (a pair tile: 256)
 constexpr int kStageRowBytes = 128; // bytes of K per pipeline stage and row
 
-enum class Tile { kPair, kSingle, kNarrow };   // 256 x 256, 128 x 128, 128 x 64
+enum class Tile { kPair, kSingle, kNarrow, kWide };   // 256 x 256, 128 x 128, x 64, x 192
 enum class GemmKind { kNvfp4, kFp8, k16 };     // k16: bf16 / fp16 operands
 
 // What the epilogue does beside writing y (kLinear: bias, activation and residual).
@@ -70,17 +70,23 @@ inline Tile choose_tile(GemmKind kind, Epilogue epi, int64_t M, int64_t N, int64
   // tile, with twice the columns per thread, ends later: bf16 1500 x 6144 x 512 with GELU
   // 15.7 us in pairs, 13.1 in single tiles; FP8 2048 x 2048 x 2048 11.9 and 10.8; NVFP4
   // 2048 x 2048 x 2048 8.6 and 9.2.
-  double us[3] = {cost[0].us((tiles_m + 1) / 2 * n256, num_sms / 2, stages, 0.0, linear ? 4.0 : 0.0),
+  // 128 x 192 tiles for the 16-bit linears, where they need a wave less (with GELU and
+  // residual, W from HBM: 1333 x 2112 x 1088 12.8 -> 11.6 us, x 256 8.9 -> 7.5; 2000 x 5120
+  // x 1088 26.4, in pairs 28.3, -> 24.2).
+  static const TileCost kWide{2.6, 0.8, 0.275};
+  const bool wide_ok = epi == Epilogue::kLinear && kind == GemmKind::k16;
+  double us[4] = {cost[0].us((tiles_m + 1) / 2 * n256, num_sms / 2, stages, 0.0, linear ? 4.0 : 0.0),
                   cost[1].us(tiles_m * n128, num_sms, stages, wave_extra, linear ? 2.1 : 0.0),
-                  cost[2].us(tiles_m * ((N + 63) / 64), num_sms, stages, wave_extra, linear ? 1.2 : 0.0)};
+                  cost[2].us(tiles_m * ((N + 63) / 64), num_sms, stages, wave_extra, linear ? 1.2 : 0.0),
+                  kWide.us(tiles_m * ((N + 191) / 192), num_sms, stages, wave_extra, 3.1)};
   if (linear) us[0] += fp4 ? 1.0 : 1.5;
   // a pair tile's re-quantizing epilogue ends about this much later
   if (epi == Epilogue::kRequant) us[0] += fp4 ? 1.0 : 0.6;
   if (epi == Epilogue::kAmax) us[0] += 1.0;
   int pick = tiles_m * n256 >= num_sms ? 0 : narrow_ok && 2 * tiles_m * n128 <= num_sms ? 2 : 1;
   int best = pick;
-  for (int t = 0; t < (narrow_ok ? 3 : 2); ++t)
-    if (us[t] < us[best]) best = t;
+  for (int t = 0; t < 4; ++t)
+    if (us[t] < us[best] && (t < 2 || (t == 2 ? narrow_ok : wide_ok))) best = t;
   if (us[best] < 0.9 * us[pick]) pick = best;
   return static_cast<Tile>(pick);
 }

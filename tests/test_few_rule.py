@@ -87,3 +87,34 @@ def test_split_rule(tmp_path):
                     s = rule(kind, m, n, k)[0]
                     row = k // 2 if kind == nvfp4 else 2 * k if kind == f16 else k
                     assert s == 1 or s <= (row + 127) // 128
+
+
+WIDE = r"""
+#include <cstdio>
+#include "qlin_tiles.h"
+int main() {
+  int kind, epi; long long m, n, k;
+  while (std::scanf("%d %d %lld %lld %lld", &kind, &epi, &m, &n, &k) == 5)
+    std::printf("%d\n", (int)qlin::choose_tile((qlin::GemmKind)kind, (qlin::Epilogue)epi, m, n, k, 152));
+}
+"""
+
+
+def test_wide_tiles(tmp_path):
+    # 128 x 192 for 16-bit linears alone, where they save a wave
+    cxx = shutil.which("g++")
+    if cxx is None:
+        pytest.skip("no C++ compiler")
+    (tmp_path / "wide.cpp").write_text(WIDE)
+    csrc = os.path.join(ROOT, "paper_2609_21849_gb300", "csrc")
+    subprocess.run([cxx, "-std=c++17", "-I" + csrc, str(tmp_path / "wide.cpp"), "-o", str(tmp_path / "wide")], check=True)
+    f16, linear = 2, 3
+    cases = [((f16, linear, 1333, 2112, 1088), 3), ((f16, linear, 1333, 2112, 256), 3),
+             ((f16, linear, 2000, 5120, 1088), 3), ((f16, linear, 2048, 2048, 1088), 1),
+             ((f16, linear, 512, 3072, 1088), 1), ((f16, linear, 4608, 12288, 3072), 0)]
+    every = [(kind, epi, m, n, k) for kind in (0, 1, 2) for epi in (0, 1, 2, 3, 4) if (kind, epi) != (f16, linear)
+             for m, n in ((1333, 2112), (2000, 5120), (4608, 1024)) for k in (256, 1088, 3072)]
+    text = "".join("%d %d %d %d %d\n" % c for c in [c for c, _ in cases] + every)
+    out = [int(v) for v in subprocess.run([str(tmp_path / "wide")], input=text, capture_output=True, text=True,
+                                          check=True).stdout.split()]
+    assert out[:len(cases)] == [w for _, w in cases] and 3 not in out[len(cases):]

@@ -92,7 +92,8 @@ def _check(y, a, w, bias, act, residual, what):
 SHAPES = [(1, 64, 64), (1, 1024, 2560), (2, 192, 3136), (5, 576, 1088), (8, 3072, 512), (9, 64, 12288), (16, 320, 192),
           (17, 2112, 320), (33, 1024, 4160), (77, 320, 192), (129, 576, 1088), (300, 128, 512), (1300, 3648, 320),
           (2048, 4096, 1088), (552, 64, 4160), (1000, 576, 1088), (1040, 128, 320), (1500, 64, 1088),
-          (300, 1024, 4160), (352, 320, 12288), (555, 832, 6208), (300, 3136, 6080)]
+          (300, 1024, 4160), (352, 320, 12288), (555, 832, 6208), (300, 3136, 6080),
+          (1333, 2112, 320), (900, 2560, 1088)]
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
@@ -106,9 +107,9 @@ def test_shapes(M, N, K, fmt):
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
-@pytest.mark.parametrize("M", [1, 6, 200, 1000, 2048])
+@pytest.mark.parametrize("M", [1, 6, 200, 1000, 1333, 2048])
 def test_parts(M, fmt):
-    N, K = (4096, 192) if M == 2048 else (448, 1088)
+    N, K = (4096, 192) if M == 2048 else (2112, 192) if M == 1333 else (448, 1088)
     a, w, bias, res, dt = _operands(fmt, M, N, K, 17 + M)
     for act in ACTS:
         for b, r in ((bias, None), (None, res), (None, None)):
@@ -126,9 +127,9 @@ def test_without_an_epilogue_as_the_plain_gemm(M, fmt):
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
-@pytest.mark.parametrize("M", [1, 7, 100, 1000, 2048])
+@pytest.mark.parametrize("M", [1, 7, 100, 1000, 1333, 2048])
 def test_residual_in_place_and_strided(M, fmt):
-    N, K = 4096 if M == 2048 else 320, 512
+    N, K = 4096 if M == 2048 else 2112 if M == 1333 else 320, 512
     a, w, bias, res, dt = _operands(fmt, M, N, K, 23)
     y0 = _call(fmt, a, w, bias, qlin.QLIN_ACT_SILU, res)
     y1 = res.clone()
