@@ -279,7 +279,7 @@ __device__ __forceinline__ void held_row(const NormParams& p, int64_t row, int t
   if constexpr (kOut == NormOut::kFp8Rows) {
     one = tot.x <= FLT_MAX && tot.y >= 0x1p-50f && tot.y <= FLT_MAX;
     if (one) {
-      pre = __fdividef(448.0f, tot.y);
+      pre = __fdiv_rn(448.0f, tot.y);   // (exact ties stay ties, and any finite maximum)
       s_dec = __fmul_rn(__fmul_rn(tot.y, inv), 1.0f / 448.0f);
     } else {
       m = row_reduce<kWarpRow, true>(0.0f, peak(inv), red + 64).y;

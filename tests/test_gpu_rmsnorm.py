@@ -162,6 +162,22 @@ def test_extreme_rows(K):
     assert (y == 0).all() and (t == 0).all()
 
 
+@pytest.mark.parametrize("K", [64, 1088, 3072, 20480])
+def test_row_scales_of_weighted_rows_near_the_largest_number(K):
+    # max |x weight| beyond 2^126, and rows whose codes are exact
+    x = torch.full((3, K), 1e17, dtype=torch.bfloat16, device="cuda")
+    x[:, ::3] *= -0.5
+    w = torch.full((K,), 1.5e21, dtype=torch.bfloat16, device="cuda")
+    q, _ = qlin.qlin_rmsnorm_fp8(x, w)
+    _, n = _exact(x, None, w, 1e-6)
+    S = n.abs().amax(1) / 448
+    assert ((q.scale.double() - S).abs() <= 2 * REL * S).all()
+    _check_fp8(q.codes, n / q.scale.double()[:, None], K)
+    v = torch.arange(-14, 15, device="cuda").float()[torch.arange(3 * K, device="cuda") % 29].view(3, K).to(torch.bfloat16)
+    q, _ = qlin.qlin_rmsnorm_fp8(v)
+    assert torch.equal(q.codes.view(torch.float8_e4m3fn).float(), v.float() * 32)
+
+
 def test_repeated_and_on_another_stream():
     x, r, w = _inputs(513, 2560, torch.bfloat16, 4)
     q0, t0 = qlin.qlin_rmsnorm_fp8(x, w, r)
