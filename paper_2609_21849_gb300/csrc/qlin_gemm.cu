@@ -889,6 +889,7 @@ __global__ void __launch_bounds__(Cfg<kFp4, kBN, kPair, kLin>::kThreads, 1)
     }
     int acc = 0;
     uint32_t acc_phase = 0;
+    StagingBoxes boxes;
     for (int ct = cid; ct < num_ctiles; ct += ncl) {
       int mg, nb;
       tile_coords(ct, groups_m, &mg, &nb);
@@ -1014,9 +1015,9 @@ __global__ void __launch_bounds__(Cfg<kFp4, kBN, kPair, kLin>::kThreads, 1)
         } else if (p.y != nullptr) {
           // each 32 x 32 box goes through a 64-byte-swizzled staging buffer and one
           // TMA store (rows >= M, cols >= N are clipped)
-          uint8_t* const bufp = out_stage + e * 4096 + (c & 1) * 2048;   // of this warp's two
+          uint8_t* const bufp = out_stage + e * 4096 + boxes.take() * 2048;   // of this warp's two
           const uint32_t buf = smem_u32(bufp);
-          if (lane == 0) bulk_wait_group_read<1>();   // this buffer's last store has read it
+          if (lane == 0) bulk_wait_group_read<1>();   // all but the other box's store have read theirs
           __syncwarp();
 #pragma unroll
           for (int k = 0; k < 4; ++k)

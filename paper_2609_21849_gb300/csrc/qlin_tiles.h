@@ -11,6 +11,23 @@ namespace qlin {
 constexpr int kTileM = 128;         // rows of a CTA's tile (a pair tile: 256)
 constexpr int kStageRowBytes = 128; // bytes of K per pipeline stage and row
 
+// The staging box (of a warp's two) that its next TMA store of y takes.  The warp waits
+// until at most one of its stores still reads shared memory, so a store may never take
+// the box of the store before it: the boxes alternate over the stores that are issued,
+// across tiles.  (Not over a tile's chunks of columns: with an odd number of them, or some
+// past N, a tile began in the box that the last one had ended in.)
+struct StagingBoxes {
+  int next = 0;
+#ifdef __CUDACC__
+  __host__ __device__
+#endif
+  int take() {
+    const int box = next;
+    next ^= 1;
+    return box;
+  }
+};
+
 enum class Tile { kPair, kSingle, kNarrow, kWide };   // 256 x 256, 128 x 128, x 64, x 192
 enum class GemmKind { kNvfp4, kFp8, k16 };     // k16: bf16 / fp16 operands
 
