@@ -1211,11 +1211,16 @@ __global__ void __launch_bounds__(Cfg<kFp4, kBN, kPair, kLin>::kThreads, 1)
         if (p.y_amax != nullptr) {
           // the output's tensor amax (for a dynamic scale of the next layer's
           // input): max over this thread's bf16 values, then the warp, then
-          // one atomic per warp.  Rows past M and columns past N hold zeros
-          // (zero-filled operands), which leave the maximum unchanged.
+          // one atomic per warp.  Rows past M and columns past N are left out:
+          // their codes are zero-filled, but not their block scales, and a
+          // padding byte that is a NaN makes a NaN of the zero.
           uint32_t m = 0;
 #pragma unroll
-          for (int i = 0; i < kCols / 2; ++i) m = __vmaxu2(m, packed[i] & 0x7FFF7FFFu);
+          for (int c = 0; c < kChunks; ++c) {
+            if (row >= p.M || ccol(c) >= p.N) continue;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) m = __vmaxu2(m, packed[c * 16 + i] & 0x7FFF7FFFu);
+          }
           m = max(m & 0xFFFFu, m >> 16);
           m = __reduce_max_sync(0xFFFFFFFFu, m);
           if (lane == 0 && m != 0u) atomicMax(p.y_amax, m << 16);

@@ -459,15 +459,15 @@ def qlin_linear_dynamic(A: NVFP4Tensor, W: NVFP4Tensor, y: torch.Tensor | None =
 _FLOAT16 = {torch.bfloat16: QLIN_BF16, torch.float16: QLIN_FP16}
 
 
-def _empty(shape, dtype, device, stream):
+def _empty(shape, dtype, device, stream, make=torch.empty):
     """An output of a call on `stream`: allocated in that stream's order, so that
     memory that the current stream still uses is not handed out for it."""
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+        return make(shape, dtype=dtype, device=device)
     if isinstance(stream, int):
         stream = torch.cuda.ExternalStream(stream, device=device)
     with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=device)
+        return make(shape, dtype=dtype, device=device)
 
 
 # The checks below read each attribute of a tensor once and compare device indices, not
@@ -561,7 +561,7 @@ def qlin_rmsnorm_nvfp4(x: torch.Tensor, static_scale: torch.Tensor, weight: torc
         if nb == 0:
             raise ValueError(f"invalid NVFP4 shape [{M}, {K}]")
         out = NVFP4Tensor(_empty((M, K // 2), torch.uint8, x.device, stream),
-                          _empty(nb, torch.uint8, x.device, stream),
+                          _empty(nb, torch.uint8, x.device, stream, torch.zeros),   # (padding too, as alloc_nvfp4)
                           _empty(1, torch.float32, x.device, stream), M, K)
     _check(_library().packed.qlin_rmsnorm_nvfp4(args, _ptr(static_scale), _nvfp4(out), _stream(stream)),
            "qlin_rmsnorm_nvfp4")
