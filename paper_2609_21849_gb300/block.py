@@ -45,7 +45,7 @@ class Block:
     W: dict = field(default_factory=dict)          # qkv, out, up, down
     bias: dict = field(default_factory=dict)
     scale: dict = field(default_factory=dict)      # static scales: v, u; NVFP4 also a, c
-    q: dict = field(default_factory=dict)          # quantized a, v, c, u
+    q: dict = field(default_factory=dict)          # quantized a, v, o, c, u
     qkv: torch.Tensor | None = None
     o: torch.Tensor | None = None
     x1: torch.Tensor | None = None
@@ -76,14 +76,14 @@ class Block:
 
     def finish(self, x: torch.Tensor, attended: torch.Tensor | None = None, stream=None) -> torch.Tensor:
         """The rest of the block on x, the block's input, and attention's output
-        [M, hidden] bf16 (None: the values stand in)."""
-        v = self.q["v"]
+        [M, hidden] bf16 (None: the values that project() left stand in)."""
+        o = self.q["v"] if attended is None else self.q["o"]
         if attended is not None:
             if self.fmt == "fp8":
-                qlin.qlin_quantize_act_fp8(attended, None, v, self.workspace, stream)
+                qlin.qlin_quantize_act_fp8(attended, None, o, self.workspace, stream)
             else:
-                qlin.qlin_quantize_act_nvfp4(attended, None, v, self.workspace, stream)
-        self._linear(v, "out", y=self.o, stream=stream)
+                qlin.qlin_quantize_act_nvfp4(attended, None, o, self.workspace, stream)
+        self._linear(o, "out", y=self.o, stream=stream)
         self._norm(self.o, self.norm2, "c", residual=x, sum_out=self.x1, stream=stream)
         self._linear(self.q["c"], "up", act=qlin.QLIN_ACT_GELU_TANH, next_scale=self.scale["u"], y_q=self.q["u"],
                      stream=stream)
@@ -148,10 +148,12 @@ def build_block(fmt: str, M: int, hidden: int = synthetic.HIDDEN, heads: int = 2
     for n in shapes:
         b.W[n] = qlin.qlin_quantize_weight(weights[n], code, workspace=b.workspace)
         b.bias[n] = weights[n + ".bias"]
-    for n, width in (("a", hidden), ("v", hidden), ("c", hidden), ("u", mlp)):
+    # (o has a scale of its own in every call, a and c one per row in FP8)
+    for n, width in (("a", hidden), ("v", hidden), ("o", hidden), ("c", hidden), ("u", mlp)):
         b.q[n] = (qlin.alloc_fp8(M, width, n in "ac", device) if fmt == "fp8"
                   else qlin.alloc_nvfp4(M, width, device))
-        b.scale[n] = torch.ones(1, dtype=torch.float32, device=device)
+        if n != "o":
+            b.scale[n] = torch.ones(1, dtype=torch.float32, device=device)
     empty = lambda w: torch.empty((M, w), dtype=torch.bfloat16, device=device)  # noqa: E731
     b.qkv, b.o, b.x1, b.y = empty(3 * hidden), empty(hidden), empty(hidden), empty(hidden)
     torch.cuda.synchronize()
