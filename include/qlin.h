@@ -356,7 +356,8 @@ qlin_status qlin_rmsnorm_nvfp4(const qlin_rmsnorm_t *args, const float *static_s
 
 /* Activations of the linears below.  GELU_TANH is
  * 0.5 v (1 + tanh(sqrt(2/pi) (v + 0.044715 v^3))), GELU 0.5 v erfc(-v / sqrt 2),
- * SILU v / (1 + exp(-v)). */
+ * SILU v / (1 + exp(-v)), each to 2^-13 of its value before the rounding to 16 bits.
+ * Values below 2^-119 may come as zero. */
 typedef enum {
   QLIN_ACT_NONE = 0,
   QLIN_ACT_RELU = 1,
