@@ -339,10 +339,18 @@ qlin_status qlin_rmsnorm(const qlin_rmsnorm_t *args, void *y, void *stream);
 
 /*
  * n as the FP8 input of a linear:
- *   out->per_channel != 0, static_scale NULL: one scale per row (token),
- *     scale[m] = max_k |n| / 448 (1 for an all-zero row), found in the same launch;
+ *   out->per_channel != 0, static_scale NULL: one scale per row (token), scale[m] =
+ *     max_k |n| / 448 (1 for an all-zero row), found in the same launch;
  *   out->per_channel == 0: static_scale is the device S_dec; scale[0] receives it.
- *   code = E4M3(n * S_enc), S_enc = 1 / S_dec (FLT_MAX if that overflows).
+ * The codes are n / S_dec with the factors of s taken together, in fp32 with one
+ * rounding per operation and r = 1 / sqrt(mean(s^2) + eps):
+ *   a scale per row: code = E4M3((s * (448 / t)) * weight), t = max_k |s * weight|;
+ *     scale[m] = (t * r) * (1 / 448);
+ *   static: code = E4M3((s * (r * S_enc)) * weight), S_enc = 1 / S_dec (FLT_MAX if that
+ *     overflows).
+ * Where a factor could overflow (t < 2^-50 or infinite, or squares that overflow; static:
+ * S_enc outside [2^-64, 2^64] or r < 2^-60) it is code = E4M3(n * S_enc), with scale[m] =
+ * max_k |n| / 448.
  * Errors: INVALID_ARG, MISALIGNED, UNSUPPORTED, CUDA.
  */
 qlin_status qlin_rmsnorm_fp8(const qlin_rmsnorm_t *args, const float *static_scale,

@@ -191,10 +191,26 @@ __device__ __forceinline__ uint4 ones() {
   return make_uint4(w, w, w, w);
 }
 
+// The factor of s in FP8 codes, (s * pre) * weight: 448 / max |s * weight| for a scale per
+// row (tot: the row's sum of squares and that maximum, found in one reduction, since
+// max |n| is the maximum / rms), inv * f for a static one.  False where a factor or a
+// product with it could overflow (|s * inv| <= sqrt(K)); codes are then n * f, n = (s *
+// inv) * weight, with f of max |n|.
+template <NormOut kOut>
+__device__ __forceinline__ bool fp8_factor(float2 tot, float inv, float f, float& pre, float& s_dec) {
+  if constexpr (kOut == NormOut::kFp8Rows) {
+    if (!(tot.x <= FLT_MAX && tot.y >= 0x1p-50f && tot.y <= FLT_MAX)) return false;
+    pre = __fdiv_rn(448.0f, tot.y);   // (exact ties stay ties, and any finite maximum)
+    s_dec = __fmul_rn(__fmul_rn(tot.y, inv), 1.0f / 448.0f);
+  } else {
+    if (!(f >= 0x1p-64f && f <= 0x1p64f && inv >= 0x1p-60f)) return false;
+    pre = __fmul_rn(inv, f);
+  }
+  return true;
+}
+
 // A row from registers: chunks tid, tid + T, ... of thread tid of the row's T.  kFull:
-// every thread has kChunks of them.  With t = s * weight, FP8 rows take max |t| in the
-// same reduction as the squares: max |n| is max |t| / rms, and the codes are
-// t * (448 / max |t|).
+// every thread has kChunks of them.
 template <NormOut kOut, bool kF16, bool kResidual, int kChunks, bool kWarpRow, bool kFull>
 __device__ __forceinline__ void held_row(const NormParams& p, int64_t row, int tid, int T, int chunks,
                                          float2* red) {
@@ -272,24 +288,18 @@ __device__ __forceinline__ void held_row(const NormParams& p, int64_t row, int t
       }
     inv = inverse_rms(row_reduce<kWarpRow, false>(s2.x + s2.y, 0.0f, red + 32).x, p.one_over_K, 0.0f) * kDown;
   }
-  // n's factors of s: pre * weight * f, in one product with pre where none of them, nor
-  // s * pre, can overflow (|s * inv| <= sqrt(K))
   float pre = inv;
-  bool one = kOut == NormOut::k16 || kOut == NormOut::kNvfp4;
-  if constexpr (kOut == NormOut::kFp8Rows) {
-    one = tot.x <= FLT_MAX && tot.y >= 0x1p-50f && tot.y <= FLT_MAX;
-    if (one) {
-      pre = __fdiv_rn(448.0f, tot.y);   // (exact ties stay ties, and any finite maximum)
-      s_dec = __fmul_rn(__fmul_rn(tot.y, inv), 1.0f / 448.0f);
-    } else {
-      m = row_reduce<kWarpRow, true>(0.0f, peak(inv), red + 64).y;
-      s_dec = m == 0.0f ? 1.0f : __fdiv_rn(m, 448.0f);
-      f = encode_scale(s_dec);
+  bool one = true;
+  if constexpr (kOut == NormOut::kFp8Rows || kOut == NormOut::kFp8) {
+    one = fp8_factor<kOut>(tot, inv, f, pre, s_dec);
+    if (kOut == NormOut::kFp8Rows) {
+      if (!one) {
+        m = row_reduce<kWarpRow, true>(0.0f, peak(inv), red + 64).y;
+        s_dec = m == 0.0f ? 1.0f : __fdiv_rn(m, 448.0f);
+        f = encode_scale(s_dec);
+      }
+      if (tid == 0) p.scale[row] = s_dec;
     }
-    if (tid == 0) p.scale[row] = s_dec;
-  } else if constexpr (kOut == NormOut::kFp8) {
-    one = f >= 0x1p-64f && f <= 0x1p64f && inv >= 0x1p-60f;
-    if (one) pre = __fmul_rn(inv, f);
   }
 #pragma unroll
   for (int i = 0; i < kChunks; ++i) weigh<kF16>(s[i], pre, vw[i]);
@@ -326,7 +336,7 @@ __global__ void __launch_bounds__(kWarpRow ? 256 : kChunks == 2 ? 1024 : 768)
 }
 
 // Rows beyond the registers of a CTA: one CTA per row, which it reads once per pass
-// (sum of squares; FP8 rows: the maximum; output).  The sum is written in the last
+// (squares and maximum; output), by the same formulas.  The sum is written in the last
 // pass, by the thread that reads the same elements, so that it may be x or residual.
 constexpr int kLongThreads = 512;
 
@@ -345,11 +355,20 @@ __global__ void __launch_bounds__(kLongThreads) rmsnorm_long_kernel(const NormPa
   };
   auto load_w = [&](int c) { return p.weight != nullptr ? ldg128(p.weight + 16 * (int64_t)c) : ones<kF16>(); };
   float2 s[4], ss = make_float2(0.0f, 0.0f), unused = ss;
+  // max |s * pre * weight| of chunk c's s
+  auto peak = [&](float m, int c, float pre) {
+    weigh<kF16>(s, pre, load_w(c));
+    return abs_max8(m, s);
+  };
+  float m = 0.0f;
+  for (int c = threadIdx.x; c < chunks; c += kLongThreads) {
+    load(c, s, ss);
+    if (kOut == NormOut::kFp8Rows) m = peak(m, c, 1.0f);
+  }
+  const float2 tot = row_reduce<false, kOut == NormOut::kFp8Rows>(ss.x + ss.y, m, red);
   float inv;
-  for (int c = threadIdx.x; c < chunks; c += kLongThreads) load(c, s, ss);
-  const float tot = row_reduce<false, false>(ss.x + ss.y, 0.0f, red).x;
-  if (tot <= FLT_MAX) {
-    inv = inverse_rms(tot, p.one_over_K, p.eps);
+  if (tot.x <= FLT_MAX) {
+    inv = inverse_rms(tot.x, p.one_over_K, p.eps);
   } else {
     ss = make_float2(0.0f, 0.0f);
     for (int c = threadIdx.x; c < chunks; c += kLongThreads) {
@@ -362,22 +381,28 @@ __global__ void __launch_bounds__(kLongThreads) rmsnorm_long_kernel(const NormPa
     }
     inv = inverse_rms(row_reduce<false, false>(ss.x + ss.y, 0.0f, red + 32).x, p.one_over_K, 0.0f) * kDown;
   }
-  float f = 1.0f;
-  if constexpr (kOut == NormOut::kFp8Rows) {
-    float m = 0.0f;
-    for (int c = threadIdx.x; c < chunks; c += kLongThreads) {
-      load(c, s, unused);
-      weigh<kF16>(s, inv, load_w(c));
-      m = abs_max8(m, s);
-    }
-    m = row_reduce<false, true>(0.0f, m, red + 64).y;
-    const float s_dec = m == 0.0f ? 1.0f : __fdiv_rn(m, 448.0f);
-    if (threadIdx.x == 0) p.scale[row] = s_dec;
-    f = encode_scale(s_dec);
-  } else if constexpr (kOut != NormOut::k16) {
-    const float s_dec = *p.static_scale;
+  float f = 1.0f, s_dec = 1.0f, pre = inv;
+  if constexpr (kOut == NormOut::kFp8 || kOut == NormOut::kNvfp4) {
+    s_dec = *p.static_scale;
     if (row == 0 && threadIdx.x == 0 && p.scale != p.static_scale) *p.scale = s_dec;
     f = encode_scale(s_dec);
+  }
+  bool one = true;
+  if constexpr (kOut == NormOut::kFp8Rows || kOut == NormOut::kFp8) {
+    one = fp8_factor<kOut>(tot, inv, f, pre, s_dec);
+    if (kOut == NormOut::kFp8Rows) {
+      if (!one) {
+        m = 0.0f;
+        for (int c = threadIdx.x; c < chunks; c += kLongThreads) {
+          load(c, s, unused);
+          m = peak(m, c, inv);
+        }
+        m = row_reduce<false, true>(0.0f, m, red + 64).y;
+        s_dec = m == 0.0f ? 1.0f : __fdiv_rn(m, 448.0f);
+        f = encode_scale(s_dec);
+      }
+      if (threadIdx.x == 0) p.scale[row] = s_dec;
+    }
   }
   for (int c0 = 0; c0 < chunks; c0 += kLongThreads) {
     const int c = c0 + (int)threadIdx.x;
@@ -388,8 +413,8 @@ __global__ void __launch_bounds__(kLongThreads) rmsnorm_long_kernel(const NormPa
       load(c, s, unused);
       if (kResidual && p.sum != nullptr)
         *reinterpret_cast<uint4*>(p.sum + row * p.sum_row + 16 * (int64_t)c) = pack8<kF16>(s);
-      weigh<kF16>(s, inv, load_w(c));
-      if (kOut == NormOut::kFp8Rows || kOut == NormOut::kFp8) {
+      weigh<kF16>(s, pre, load_w(c));
+      if (!one) {
 #pragma unroll
         for (int k = 0; k < 4; ++k) s[k] = mul2(s[k], make_float2(f, f));
       }
