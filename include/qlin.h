@@ -312,7 +312,10 @@ typedef enum { QLIN_BF16 = 1, QLIN_FP16 = 2 } qlin_float16;
  *   n = (s * (1 / sqrt(mean(s^2) + eps))) * weight.
  * n is computed from s itself, not from the rounded sum, and is rounded once, to
  * the output's format.  A row whose squares overflow fp32 is normalised through
- * scaled squares; a row with an infinity or a NaN becomes NaN.
+ * scaled squares.  A NaN makes a NaN of every n of its row.  With an infinity (one that
+ * x + residual overflows to, too) the quotient is 0: n is NaN where s is infinite and 0
+ * elsewhere.  In FP8 and NVFP4 such a NaN is the code or the block scale of NaN; a scale
+ * per row is then NaN with all of the row's codes.
  *  x:        16-bit [M, K], rows x_stride elements apart (a multiple of 8, >= K).
  *  residual: the same with residual_stride, or NULL.
  *  sum:      receives x + residual (rows sum_stride apart), or NULL.  May be x or

@@ -122,8 +122,9 @@ __device__ __forceinline__ float2 row_reduce(float a, float m, float2* red) {
   return make_float2(a, m);
 }
 
-// 1 / sqrt(ss / K + eps); a row whose squares overflow takes them of s * 2^-80
-// instead (2^-80 times the largest sum of two 16-bit values squares to 2^98).
+// 1 / sqrt(ss / K + eps); a row whose squares overflow takes them of s * 2^-80 instead
+// (squares below 2^96, K < 2^31 of them).  With an infinity among s the result is 0: n is
+// NaN there and 0 elsewhere.
 constexpr float kDown = 0x1p-80f;
 __device__ __forceinline__ float inverse_rms(float ss, float one_over_K, float eps) {
   return __frsqrt_rn(__fmaf_rn(ss, one_over_K, eps));
