@@ -385,6 +385,9 @@ typedef enum {
  *  residual: 16-bit [M, N] of the output's type, rows residual_stride elements
  *            apart (a multiple of 8, >= N), 16-byte aligned, or NULL.  May be y
  *            itself (residual_stride == N); otherwise it must not overlap y.
+ * The order in which products are added follows M, N and K (few tokens, tiles, tiles
+ * that share K), so the last bits of a token's outputs may change with the number of
+ * tokens in the call; equal calls give equal bits.
  */
 typedef struct {
   const void *bias;
