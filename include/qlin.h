@@ -336,8 +336,8 @@ typedef struct {
   int32_t dtype;
 } qlin_rmsnorm_t;
 
-/* y = n in 16 bits, [M, K] with rows K apart.  y may be x itself where x's rows
- * are K apart.  Errors: INVALID_ARG, MISALIGNED, UNSUPPORTED, CUDA. */
+/* y = n in 16 bits, [M, K] with rows K apart.  y may be x or residual itself where
+ * their rows are K apart, not sum.  Errors: INVALID_ARG, MISALIGNED, UNSUPPORTED, CUDA. */
 qlin_status qlin_rmsnorm(const qlin_rmsnorm_t *args, void *y, void *stream);
 
 /*
@@ -434,8 +434,9 @@ qlin_status qlin_linear_fp16(const void *a_fp16, int64_t lda, const void *w_fp16
  * (inverse: by the negative angle, which is the gradient of the forward rotation).
  * Elements past rot_dim are copied.  fp32 arithmetic, one rounding.
  *  x, y:      16-bit [tokens, heads, head_dim], head_dim contiguous, any strides (in
- *             elements) of tokens and heads; y may be x itself with the same
- *             strides, else the two must not overlap.  2-byte aligned; 16-byte
+ *             elements) of tokens and heads, in y head_dim or more (also negative
+ *             ones); y may be x itself with the same strides, else the two must
+ *             not overlap.  2-byte aligned; 16-byte
  *             aligned rows of multiples of 8 elements take 16-byte accesses.
  *  positions: int32 or int64 (position_bits) [tokens, axes] with strides in
  *             elements; any values, negative ones too.

@@ -241,6 +241,9 @@ static qlin_status set_epilogue(GemmArgs& a, const qlin_epilogue_t* ep) {
   if (!aligned(ep->bias, 16) || !aligned(ep->residual, 16) ||
       (ep->residual != nullptr && ep->residual_stride % 8 != 0))
     return QLIN_ERR_MISALIGNED;
+  // (in place: a thread reads what it writes, at the same address)
+  if (ep->residual != nullptr && ep->residual == a.y && ep->residual_stride != a.N && a.M > 1)
+    return QLIN_ERR_INVALID_ARG;
   a.bias = ep->bias;
   a.residual = ep->residual;
   a.residual_stride = ep->residual_stride;
@@ -472,6 +475,11 @@ static qlin_status check_rmsnorm(const qlin_rmsnorm_t* a) {
       (a->residual != nullptr && a->residual_stride % 8 != 0) ||
       (a->sum != nullptr && a->sum_stride % 8 != 0))
     return QLIN_ERR_MISALIGNED;
+  // in place only with equal strides
+  if (a->sum != nullptr && a->M > 1 &&
+      ((a->sum == a->x && a->sum_stride != a->x_stride) ||
+       (a->sum == a->residual && a->sum_stride != a->residual_stride)))
+    return QLIN_ERR_INVALID_ARG;
   return QLIN_OK;
 }
 
@@ -488,6 +496,9 @@ qlin_status qlin_rmsnorm(const qlin_rmsnorm_t* args, void* y, void* stream) {
   QLIN_TRY(check_rmsnorm(args));
   if (y == nullptr) return QLIN_ERR_INVALID_ARG;
   if (!aligned(y, 16)) return QLIN_ERR_MISALIGNED;
+  if (y == args->sum || (args->M > 1 && ((y == args->x && args->x_stride != args->K) ||
+                                         (y == args->residual && args->residual_stride != args->K))))
+    return QLIN_ERR_INVALID_ARG;
   return rmsnorm(args, y, nullptr, nullptr, nullptr, stream);
 }
 
@@ -535,6 +546,11 @@ qlin_status qlin_rope(const qlin_rope_t* a, void* stream) {
   if (!aligned(a->x, 2) || !aligned(a->y, 2) || !aligned(a->turns, 8) ||
       !aligned(a->positions, a->position_bits / 8))
     return QLIN_ERR_MISALIGNED;
+  // heads of y that lie over one another (an expanded tensor, say)
+  auto apart = [&](int64_t n, int64_t stride) {
+    return n == 1 || stride >= a->head_dim || stride <= -(int64_t)a->head_dim;
+  };
+  if (!apart(a->tokens, a->y_token_stride) || !apart(a->heads, a->y_head_stride)) return QLIN_ERR_INVALID_ARG;
   unsigned* status;
   Device dev;
   QLIN_TRY(device_state(&status, &dev));
