@@ -47,8 +47,8 @@
  *     device status word that qlin_sync_status() returns and clears.
  *   - Shapes: K must be a positive multiple of 64; N a positive multiple of
  *     64; M >= 1 (any value: partial tiles are masked).
- *   - Alignment: every code, scale and bf16 buffer 16-byte aligned; fp32
- *     scalars 4-byte aligned.
+ *   - Alignment: every code, block-scale and bf16 buffer 16-byte aligned; fp32
+ *     scalars and FP8 row scales 4-byte aligned.
  */
 #ifndef QLIN_H
 #define QLIN_H

@@ -298,7 +298,8 @@ static qlin_status gemm_common(bool fp4, const void* Aany, const void* Wany, voi
     QLIN_TRY(check_fp8(W, W->rows, A->K));
     if (A->per_channel && !linear) return QLIN_ERR_INVALID_ARG;
     a.a_per_row = A->per_channel != 0;
-    a.epilogue = a.a_per_row;
+    // (the plain epilogue reads W's row scales 16 bytes at a time)
+    a.epilogue = a.a_per_row || (W->per_channel && !aligned(W->scale, 16));
     a.a_codes = A->codes;
     a.w_codes = W->codes;
     a.sdec_a = A->scale;

@@ -900,7 +900,7 @@ __global__ void __launch_bounds__(Cfg<kFp4, kBN, kPair, kLin>::kThreads, 1)
         // than L2 -- the last tile's epilogue is on the kernel's critical path
         const int64_t cl = (int64_t)nb * kBN + half * kCols + 32 * lane;
         if (lane < kCols / 32 && cl < p.N)
-          asm volatile("prefetch.global.L1 [%0];" ::"l"(p.sdec_w + cl));
+          asm volatile("prefetch.global.L1 [%0];" ::"l"(reinterpret_cast<uintptr_t>(p.sdec_w + cl) & ~(uintptr_t)15));
       }
       const int mb = mg * kCM + rank;
       const int64_t row = (int64_t)mb * kBM + quarter * 32 + lane;
@@ -1179,6 +1179,7 @@ __global__ void __launch_bounds__(Cfg<kFp4, kBN, kPair, kLin>::kThreads, 1)
             } else {
               const int64_t n0 = ccol(c);
               if (p.w_per_channel && n0 < p.N) {
+                // (16-byte aligned: other scales come with the linears' epilogue)
                 const float4* sw = reinterpret_cast<const float4*>(p.sdec_w + n0);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {

@@ -107,7 +107,7 @@ struct GemmArgs {
   unsigned* y_departures;
   float* y_sdec;
   // optional epilogue of a linear: act(products + bias) + residual
-  bool epilogue;            // any of these, or a_per_row
+  bool epilogue;            // any of these, a_per_row, or FP8 row scales of W off 16-byte boundaries
   const void* bias;         // 16-bit [N] or null
   const void* residual;     // 16-bit [M, N] or null, rows residual_stride elements apart
   int64_t residual_stride;
