@@ -500,6 +500,42 @@ def _dense16(t, name, dtype, M, N, dev):
     return t.data_ptr()
 
 
+def _scalar32(t, name, dev):
+    """The address of a scale on device `dev` (an int is one already)."""
+    if t is None or type(t) is int:
+        return t
+    p = t.data_ptr()
+    if t.dtype is not torch.float32 or t.get_device() != dev or not p:
+        raise ValueError(f"{name}: expected a float32 tensor on cuda:{dev}")
+    return p
+
+
+def _fp8_on(q, name, dev) -> bytes:
+    """The packed descriptor of an FP8 operand, one of ours on device `dev`."""
+    if type(q) is not FP8Tensor:
+        return _descriptor(q, FP8Desc)
+    codes, scale = q.codes, q.scale
+    if codes.get_device() != dev or scale.get_device() != dev:
+        raise ValueError(f"{name}: expected an operand on cuda:{dev}")
+    try:
+        return _pack_fp8(codes.data_ptr(), scale.data_ptr(), q.rows, q.K, q.per_channel)
+    except struct.error:   # no integer, or out of range: as the structure takes it
+        return bytes(q.desc())
+
+
+def _nvfp4_on(q, name, dev) -> bytes:
+    """The same of an NVFP4 operand."""
+    if type(q) is not NVFP4Tensor:
+        return _descriptor(q, NVFP4Desc)
+    codes, scales, scale = q.codes, q.scales, q.tensor_scale
+    if codes.get_device() != dev or scales.get_device() != dev or scale.get_device() != dev:
+        raise ValueError(f"{name}: expected an operand on cuda:{dev}")
+    try:
+        return _pack_nvfp4(codes.data_ptr(), scales.data_ptr(), scale.data_ptr(), q.rows, q.K)
+    except struct.error:
+        return bytes(q.desc())
+
+
 def _rmsnorm_args(x, weight, residual, eps, sum_out, stream):
     """(packed arguments, M, K, sum) of a norm call; sum is allocated where a
     residual comes without one."""
@@ -545,7 +581,9 @@ def qlin_rmsnorm_fp8(x: torch.Tensor, weight: torch.Tensor | None = None,
         rows = static_scale is None
         out = FP8Tensor(_empty((M, K), torch.uint8, x.device, stream),
                         _empty(M if rows else 1, torch.float32, x.device, stream), M, K, 1 if rows else 0)
-    _check(_library().packed.qlin_rmsnorm_fp8(args, _ptr(static_scale), _fp8(out), _stream(stream)),
+    dev = x.get_device()
+    _check(_library().packed.qlin_rmsnorm_fp8(args, _scalar32(static_scale, "static_scale", dev),
+                                              _fp8_on(out, "out", dev), _stream(stream)),
            "qlin_rmsnorm_fp8")
     return out, sum_out
 
@@ -563,7 +601,9 @@ def qlin_rmsnorm_nvfp4(x: torch.Tensor, static_scale: torch.Tensor, weight: torc
         out = NVFP4Tensor(_empty((M, K // 2), torch.uint8, x.device, stream),
                           _empty(nb, torch.uint8, x.device, stream, torch.zeros),   # (padding too, as alloc_nvfp4)
                           _empty(1, torch.float32, x.device, stream), M, K)
-    _check(_library().packed.qlin_rmsnorm_nvfp4(args, _ptr(static_scale), _nvfp4(out), _stream(stream)),
+    dev = x.get_device()
+    _check(_library().packed.qlin_rmsnorm_nvfp4(args, _scalar32(static_scale, "static_scale", dev),
+                                                _nvfp4_on(out, "out", dev), _stream(stream)),
            "qlin_rmsnorm_nvfp4")
     return out, sum_out
 
@@ -581,6 +621,8 @@ def _epilogue(bias, act, residual, dtype, M, N, dev):
 def _linear_quantized(name, pack, A, W, bias, act, residual, y, next_scale, y_q, rq_col0, stream):
     M, N, codes = A.rows, W.rows, A.codes
     dev = codes.get_device()
+    if dev < 0:
+        raise ValueError("A: expected a CUDA operand")
     if (y_q is None) != (next_scale is None):
         raise ValueError("next_scale and y_q come together")
     if y is None and y_q is None:
@@ -588,8 +630,8 @@ def _linear_quantized(name, pack, A, W, bias, act, residual, y, next_scale, y_q,
     yp = None if y is None else _dense16(y, "y", torch.bfloat16, M, N, dev)
     ep = _epilogue(bias, act, residual, torch.bfloat16, M, N, dev)
     _check(getattr(_library().packed, name)(
-        pack(A), pack(W), ep, yp, _ptr(next_scale), None if y_q is None else pack(y_q), rq_col0,
-        _stream(stream)), name)
+        pack(A, "A", dev), pack(W, "W", dev), ep, yp, _scalar32(next_scale, "next_scale", dev),
+        None if y_q is None else pack(y_q, "y_q", dev), rq_col0, _stream(stream)), name)
     return y, y_q
 
 
@@ -601,7 +643,7 @@ def qlin_linear_nvfp4(A: NVFP4Tensor, W: NVFP4Tensor, bias: torch.Tensor | None 
     y_q, the next layer's NVFP4 input from columns [rq_col0, rq_col0 + y_q.K) of y.
     Returns (y, y_q); y None is allocated, or not written where y_q is given.
     residual may be y."""
-    return _linear_quantized("qlin_linear_nvfp4", _nvfp4, A, W, bias, act, residual, y, next_scale, y_q,
+    return _linear_quantized("qlin_linear_nvfp4", _nvfp4_on, A, W, bias, act, residual, y, next_scale, y_q,
                              rq_col0, stream)
 
 
@@ -610,7 +652,7 @@ def qlin_linear_fp8(A: FP8Tensor, W: FP8Tensor, bias: torch.Tensor | None = None
                     y: torch.Tensor | None = None, next_scale: torch.Tensor | None = None,
                     y_q: FP8Tensor | None = None, rq_col0: int = 0, stream=None):
     """As qlin_linear_nvfp4 with FP8 operands; A has one scale or one per row."""
-    return _linear_quantized("qlin_linear_fp8", _fp8, A, W, bias, act, residual, y, next_scale, y_q,
+    return _linear_quantized("qlin_linear_fp8", _fp8_on, A, W, bias, act, residual, y, next_scale, y_q,
                              rq_col0, stream)
 
 
