@@ -74,8 +74,9 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(const RopeParams p) {
     const int da = p.half ? i : 2 * i, db = p.half ? i + p.pairs : 2 * i + 1;
     const float a = load16(x + da, fp16), b = load16(x + db, fp16);
     const float2 r = rot[i];
-    y[da] = pack16(__fsub_rn(__fmul_rn(a, r.x), __fmul_rn(b, r.y)), fp16);
-    y[db] = pack16(__fadd_rn(__fmul_rn(a, r.y), __fmul_rn(b, r.x)), fp16);
+    // (rounded as turn2 below: a value's bits do not depend on where its row starts)
+    y[da] = pack16(__fmaf_rn(a, r.x, __fmul_rn(b, -r.y)), fp16);
+    y[db] = pack16(__fmaf_rn(a, r.y, __fmul_rn(b, r.x)), fp16);
   }
 }
 
