@@ -324,6 +324,8 @@ typedef enum { QLIN_BF16 = 1, QLIN_FP16 = 2 } qlin_float16;
  *  eps:      finite, > 0.
  *  dtype:    QLIN_BF16 or QLIN_FP16, of x, residual, sum, weight and a 16-bit y.
  * Pointers are 16-byte aligned; K % 64 == 0.
+ * The squares' order follows K and how many rows there are, so the last bits of a row may
+ * change with the number of rows in the call; equal calls give equal bits.
  */
 typedef struct {
   const void *x;
