@@ -22,6 +22,13 @@
  *     / _bf16 / _fp16          epilogue, from one token up
  *   qlin_rope                  rotary positions on q and k
  *
+ * and the rest of a serving step:
+ *
+ *   qlin_quantize_fp8_block    FP8 operands with a scale for each block of 128
+ *   qlin_linear_fp8_block      the linear of such operands
+ *   qlin_cache_append          new keys and values into a paged cache, rotated on the way
+ *   qlin_cache_attention       attention of new tokens (one, a run, a drafted tree) over it
+ *
  * Formats (the paper names them and cites their definitions; it fixes no block
  * size or rounding rule, so the readings taken here are stated per call):
  *   - E4M3: FP8 with exponent bias 7, max 448, NaN = S.1111.111, no infinity
@@ -502,9 +509,182 @@ qlin_status qlin_rope_turns(int32_t rot_dim, double base, int32_t scaling, doubl
                             double trained_length, double beta_fast, double beta_slow,
                             uint64_t *turns, float *magnitude);
 
+/* ------------------------------------------------------------------------
+ * A serving step: block-scaled FP8 linears, a paged cache and the attention over it.
+ */
+
+/*
+ * FP8 (E4M3) operand [rows, K] with a scale for each block of block_rows rows and 128
+ * elements of K (the last block of K may have 64, the last of the rows fewer).
+ *  codes:  rows x K bytes, row stride K, 16-byte aligned.
+ *  scales: fp32 decode scales, [ceil(K / 128), ceil(rows / block_rows)]: those of one block
+ *          of K are adjacent.  4-byte aligned.
+ *  block_rows: 1 (activations) or 128 (weights).
+ */
+typedef struct {
+  uint8_t *codes;
+  float *scales;
+  int64_t rows;
+  int64_t K;
+  int32_t block_rows;
+} qlin_fp8_block_t;
+
+/* Number of scales of such an operand; 0 for invalid shapes. */
+size_t qlin_fp8_block_scales(int64_t rows, int64_t K, int32_t block_rows);
+
+/*
+ * Quantizes x to a block-scaled operand.  Per block, each fp32 op rounded once:
+ *   S = max |x| / 448 (1 for a block of zeros); code = E4M3(x * S_enc), S_enc = 1 / S
+ *   (FLT_MAX if that overflows).
+ * A NaN makes its block's scale and codes NaN; with an infinity the scale is infinite, its
+ * codes are NaN and the block's others zero.
+ *  x:   16-bit [rows, K] (dtype), rows x_stride elements apart (a multiple of 8, >= K),
+ *       16-byte aligned.
+ *  out: rows, K and block_rows set.
+ * Errors: INVALID_ARG, MISALIGNED, UNSUPPORTED, CUDA.
+ */
+qlin_status qlin_quantize_fp8_block(const void *x, int32_t dtype, int64_t x_stride,
+                                    const qlin_fp8_block_t *out, void *stream);
+
+/*
+ * The linear of block-scaled operands, A with block_rows 1 and W with block_rows 128:
+ *   y = bf16( act( sum_b (S_A[m, b] S_W[n / 128, b]) sum_{k in block b} a w + bias[n] )
+ *             + residual[m, n] ),
+ * products and sums in fp32, y [M, N] rows N apart; epilogue as for the other linears (NULL:
+ * none of it).  Any M from one token.
+ * Errors: INVALID_ARG, MISALIGNED, UNSUPPORTED, CUDA.
+ */
+qlin_status qlin_linear_fp8_block(const qlin_fp8_block_t *A, const qlin_fp8_block_t *W,
+                                  const qlin_epilogue_t *epilogue, void *y_bf16, void *stream);
+
+typedef enum { QLIN_CACHE_BF16 = 1, QLIN_CACHE_FP16 = 2, QLIN_CACHE_E4M3 = 3 } qlin_cache_format;
+
+/*
+ * Keys and values in pages, and the step's sequences.  Token i of sequence b (cached tokens
+ * first, then the step's new ones) lies in page page_table[b, i / page_size], slot i %
+ * page_size.
+ *  k, v:       [pages, page_size, heads, head_dim] of the format, head_dim contiguous, other
+ *              strides in elements, zero or more; pages may hold up to any number of bytes.
+ *  page_table: int32 [sequences, table_width], rows table_stride apart.  Entries that a
+ *              sequence's tokens do not reach are not read.
+ *  cached:     int32 [sequences], tokens in the cache before this step.
+ *  q_start:    int32 [sequences + 1], not decreasing: sequence b's new tokens are
+ *              q_start[b] .. q_start[b + 1] - 1 of the call's.  Tokens of the call before the
+ *              first or behind the last (a padded batch) are not touched; a sequence may have
+ *              none.
+ *  k_scale, v_scale: E4M3 only, device fp32 decode scales: value = code * scale.
+ * All of this is device data that the host does not see: what it gets wrong (a page that is
+ * none of `pages`, a token past the table, counts that are negative or decrease) reads and
+ * writes nothing and is reported by qlin_sync_status as QLIN_ERR_INVALID_ARG; such keys are
+ * not seen, such tokens not written.
+ * heads, pages, page_size, table_width, sequences >= 1; head_dim <= 256.
+ */
+typedef struct {
+  void *k;
+  void *v;
+  int64_t k_page_stride, k_slot_stride, k_head_stride;
+  int64_t v_page_stride, v_slot_stride, v_head_stride;
+  const int32_t *page_table;
+  int64_t table_stride;
+  const int32_t *cached;
+  const int32_t *q_start;
+  const float *k_scale;
+  const float *v_scale;
+  int32_t sequences, pages, page_size, table_width;
+  int32_t heads, head_dim;
+  int32_t format;
+} qlin_cache_t;
+
+/*
+ * Writes the new tokens' keys and values to their slots, k with its rotary positions, and q
+ * (optional) rotated to q_out.  fp32 arithmetic, one rounding; E4M3: code = E4M3(value *
+ * S_enc), S_enc = 1 / scale (FLT_MAX if that overflows).
+ *  k, v:  16-bit (dtype) [tokens, heads, head_dim], head_dim contiguous, any strides of
+ *         tokens and heads in elements.  q, q_out: [tokens, q_heads, head_dim] likewise (in
+ *         q_out, head_dim or more, also negative); q_out may be q itself with the same
+ *         strides, else the two must not overlap.  q NULL: none.
+ *         2-byte aligned; 16-byte aligned rows and pairs in fours take wide accesses.
+ *  positions, turns, magnitude, rot_dim, axes, axis_pairs, layout: as in qlin_rope.
+ *         positions NULL: a token's number in its sequence (one axis).  turns NULL: nothing
+ *         turns.
+ * A 16-bit cache has the type of k and v.  Two tokens that share a slot (a page that two
+ * sequences list for new tokens) leave either's values there.
+ * Errors: INVALID_ARG, MISALIGNED, UNSUPPORTED, CUDA.
+ */
+typedef struct {
+  const void *k;
+  const void *v;
+  const void *q;
+  void *q_out;
+  int64_t k_token_stride, k_head_stride;
+  int64_t v_token_stride, v_head_stride;
+  int64_t q_token_stride, q_head_stride;
+  int64_t q_out_token_stride, q_out_head_stride;
+  int64_t tokens;
+  const void *positions;
+  int64_t position_token_stride, position_axis_stride;
+  const uint64_t *turns;
+  float magnitude;
+  int32_t q_heads;
+  int32_t rot_dim;
+  int32_t position_bits;
+  int32_t axes;
+  int32_t axis_pairs[4];
+  int32_t layout;
+  int32_t dtype;
+} qlin_cache_append_t;
+
+qlin_status qlin_cache_append(const qlin_cache_t *cache, const qlin_cache_append_t *args,
+                              void *stream);
+
+/*
+ * Attention of the new tokens over their sequence's cached + new keys (the new ones appended
+ * before):
+ *   out = softmax(scale q k^T, masked) v;   lse = ln sum exp(scale q k^T)  (optional)
+ * Query head h reads KV head h / (q_heads / heads).  Every new token sees all cached ones;
+ * of the new ones, mask bit i of token t's words (bit i % 64 of word i / 64) says whether t
+ * sees new token i, itself among them; bits past the words are 0.  mask NULL: those up to
+ * itself.  A row that sees nothing gives zeros and lse -infinity.  NaN and infinities in
+ * keys and values that a row does not see do not reach it.  Scores, running maximum and sum
+ * and the products' sums in fp32; probabilities are rounded to 16 bits for the product with v.
+ *  q, out: 16-bit (dtype) [tokens, q_heads, head_dim], head_dim contiguous, strides in
+ *          elements, multiples of 8, 16-byte aligned; out may be q with the same strides, else
+ *          the two must not overlap.  Rows of tokens of no sequence are left as they were.
+ *  lse:    fp32 [tokens, q_heads] or NULL.
+ *  mask:   uint64 [tokens, mask_words], rows mask_stride words apart, or NULL.
+ *  scale:  normal and > 0.
+ *  workspace: device memory of >= qlin_cache_attention_workspace_size() bytes, 16-byte
+ *          aligned, its first 4096 bytes zero before the first use; every call leaves them
+ *          zero.  Calls whose work overlaps on the GPU must not share one.
+ * A 16-bit cache has the type of q.  head_dim: a multiple of 16.  Cache rows 16-byte aligned.
+ * Sums are joined in the order of the keys, split by all sequences' lengths: equal calls give
+ * equal bits, other batches may change the last ones.
+ * Errors: INVALID_ARG, MISALIGNED, UNSUPPORTED, WORKSPACE, CUDA.
+ */
+typedef struct {
+  const void *q;
+  void *out;
+  float *lse;
+  const uint64_t *mask;
+  int64_t q_token_stride, q_head_stride;
+  int64_t out_token_stride, out_head_stride;
+  int64_t mask_stride;
+  int64_t tokens;
+  float scale;
+  int32_t q_heads;
+  int32_t mask_words;
+  int32_t dtype;
+} qlin_cache_attention_t;
+
+size_t qlin_cache_attention_workspace_size(void);
+
+qlin_status qlin_cache_attention(const qlin_cache_t *cache, const qlin_cache_attention_t *args,
+                                 void *workspace, size_t ws_bytes, void *stream);
+
 /*
  * Waits for `stream`, then returns and clears the device status word:
  * QLIN_ERR_TIMEOUT if a kernel's bounded wait expired since the last call,
+ * QLIN_ERR_INVALID_ARG if a cache call found page tables or counts that are wrong,
  * QLIN_ERR_CUDA if the stream reports an error, else QLIN_OK.
  */
 qlin_status qlin_sync_status(void *stream);

@@ -6,6 +6,7 @@
 #include <cstring>
 #include <mutex>
 
+#include "qlin_attention.h"
 #include "qlin_internal.h"
 #include "qlin_tiles.h"
 
@@ -233,6 +234,14 @@ qlin_status qlin_quantize_weight(const void* w_bf16, int64_t N, int64_t K, qlin_
   return QLIN_OK;
 }
 
+static qlin_status check_fp8_block(const qlin_fp8_block_t* t, int32_t block_rows) {
+  if (t == nullptr || t->codes == nullptr || t->scales == nullptr || !shape_ok(t->rows, t->K) ||
+      t->block_rows != block_rows)
+    return QLIN_ERR_INVALID_ARG;
+  if (!aligned(t->codes, 16) || !aligned(t->scales, 4)) return QLIN_ERR_MISALIGNED;
+  return QLIN_OK;
+}
+
 // Bias, activation and residual of a linear into its GEMM's arguments (M, N set).
 static qlin_status set_epilogue(GemmArgs& a, const qlin_epilogue_t* ep) {
   if (ep == nullptr) return QLIN_OK;
@@ -450,6 +459,35 @@ qlin_status qlin_linear_fp8(const qlin_fp8_t* A, const qlin_fp8_t* W,
                      nullptr, epilogue, true);
 }
 
+qlin_status qlin_linear_fp8_block(const qlin_fp8_block_t* A, const qlin_fp8_block_t* W,
+                                  const qlin_epilogue_t* epilogue, void* y_bf16, void* stream) {
+  QLIN_TRY(check_fp8_block(A, 1));
+  QLIN_TRY(check_fp8_block(W, 128));
+  if (y_bf16 == nullptr || A->K != W->K || W->rows % 64 != 0) return QLIN_ERR_INVALID_ARG;
+  if (A->rows > (int64_t)1 << 31 || W->rows > (int64_t)1 << 31 || A->K > INT32_MAX) return QLIN_ERR_UNSUPPORTED;
+  if (!aligned(y_bf16, 16)) return QLIN_ERR_MISALIGNED;
+  GemmArgs a{};
+  a.blocks = true;
+  a.a_codes = A->codes;
+  a.w_codes = W->codes;
+  a.sdec_a = A->scales;
+  a.sdec_w = W->scales;
+  a.M = A->rows;
+  a.N = W->rows;
+  a.K = A->K;
+  a.y = y_bf16;
+  QLIN_TRY(set_epilogue(a, epilogue));
+  unsigned* status;
+  Device dev;
+  QLIN_TRY(device_state(&status, &dev));
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (a.K <= (int64_t)1 << 28 && few_tokens(false, a.M, a.N, a.K, dev.num_sms))
+    QLIN_CUDA(launch_few(a, s, dev));
+  else
+    QLIN_CUDA(launch_gemm_block(a, s, dev, status, timeout()));
+  return QLIN_OK;
+}
+
 qlin_status qlin_linear_bf16(const void* a_bf16, int64_t lda, const void* w_bf16, int64_t M,
                              int64_t N, int64_t K, const qlin_epilogue_t* epilogue,
                              void* y_bf16, void* stream) {
@@ -559,6 +597,135 @@ qlin_status qlin_rope(const qlin_rope_t* a, void* stream) {
   return QLIN_OK;
 }
 
+size_t qlin_fp8_block_scales(int64_t rows, int64_t K, int32_t block_rows) {
+  if (!shape_ok(rows, K) || (block_rows != 1 && block_rows != 128)) return 0;
+  return (size_t)((K + 127) / 128) * (size_t)((rows + block_rows - 1) / block_rows);
+}
+
+qlin_status qlin_quantize_fp8_block(const void* x, int32_t dtype, int64_t x_stride,
+                                    const qlin_fp8_block_t* out, void* stream) {
+  if (x == nullptr || out == nullptr || (dtype != QLIN_BF16 && dtype != QLIN_FP16)) return QLIN_ERR_INVALID_ARG;
+  if (out->block_rows != 1 && out->block_rows != 128) return QLIN_ERR_INVALID_ARG;
+  QLIN_TRY(check_fp8_block(out, out->block_rows));
+  if (x_stride < out->K) return QLIN_ERR_INVALID_ARG;
+  if (!aligned(x, 16) || x_stride % 8 != 0) return QLIN_ERR_MISALIGNED;
+  // (CTAs are counted in 31 bits: at least 2^36 elements)
+  if (out->rows > INT32_MAX || out->K > INT32_MAX || qlin_fp8_block_scales(out->rows, out->K, out->block_rows) > INT32_MAX)
+    return QLIN_ERR_UNSUPPORTED;
+  unsigned* status;
+  Device dev;
+  QLIN_TRY(device_state(&status, &dev));
+  QLIN_CUDA(launch_quant_fp8_block(x, x_stride, dtype == QLIN_FP16, *out, static_cast<cudaStream_t>(stream)));
+  return QLIN_OK;
+}
+
+static qlin_status check_cache(const qlin_cache_t* c) {
+  if (c == nullptr || c->k == nullptr || c->v == nullptr || c->page_table == nullptr || c->cached == nullptr ||
+      c->q_start == nullptr)
+    return QLIN_ERR_INVALID_ARG;
+  if (c->sequences < 1 || c->pages < 1 || c->page_size < 1 || c->table_width < 1 || c->heads < 1 ||
+      c->head_dim < 1 || c->format < QLIN_CACHE_BF16 || c->format > QLIN_CACHE_E4M3)
+    return QLIN_ERR_INVALID_ARG;
+  if (c->format == QLIN_CACHE_E4M3 && (c->k_scale == nullptr || c->v_scale == nullptr)) return QLIN_ERR_INVALID_ARG;
+  if (c->k_page_stride < 0 || c->k_slot_stride < 0 || c->k_head_stride < 0 || c->v_page_stride < 0 ||
+      c->v_slot_stride < 0 || c->v_head_stride < 0 || (c->sequences > 1 && c->table_stride < c->table_width))
+    return QLIN_ERR_INVALID_ARG;
+  if (c->head_dim > 256 || c->heads > 65536 || c->sequences > 1 << 24) return QLIN_ERR_UNSUPPORTED;
+  if (!aligned(c->page_table, 4) || !aligned(c->cached, 4) || !aligned(c->q_start, 4) || !aligned(c->k_scale, 4) ||
+      !aligned(c->v_scale, 4))
+    return QLIN_ERR_MISALIGNED;
+  return QLIN_OK;
+}
+
+qlin_status qlin_cache_append(const qlin_cache_t* c, const qlin_cache_append_t* a, void* stream) {
+  QLIN_TRY(check_cache(c));
+  if (a == nullptr || a->k == nullptr || a->v == nullptr || a->tokens < 1 ||
+      (a->dtype != QLIN_BF16 && a->dtype != QLIN_FP16))
+    return QLIN_ERR_INVALID_ARG;
+  if (a->q != nullptr && (a->q_out == nullptr || a->q_heads < 1)) return QLIN_ERR_INVALID_ARG;
+  // cache rows of new tokens must not lie over one another
+  auto rows_apart = [&](int64_t page, int64_t slot, int64_t head) {
+    return (c->pages == 1 || page >= c->head_dim) && (c->page_size == 1 || slot >= c->head_dim) &&
+           (c->heads == 1 || head >= c->head_dim);
+  };
+  if (!rows_apart(c->k_page_stride, c->k_slot_stride, c->k_head_stride) ||
+      !rows_apart(c->v_page_stride, c->v_slot_stride, c->v_head_stride))
+    return QLIN_ERR_INVALID_ARG;
+  if (c->format != QLIN_CACHE_E4M3 && c->format != a->dtype) return QLIN_ERR_UNSUPPORTED;
+  if (a->turns != nullptr) {
+    if (a->rot_dim < 2 || a->rot_dim % 2 != 0 || a->rot_dim > c->head_dim || a->axes < 1 || a->axes > 4 ||
+        (a->layout != QLIN_ROPE_INTERLEAVED && a->layout != QLIN_ROPE_HALF) ||
+        (a->positions != nullptr && a->position_bits != 32 && a->position_bits != 64) ||
+        (a->positions == nullptr && a->axes != 1))
+      return QLIN_ERR_INVALID_ARG;
+    int64_t pairs = 0;
+    for (int i = 0; i < a->axes; ++i) {
+      if (a->axis_pairs[i] < 0) return QLIN_ERR_INVALID_ARG;
+      pairs += a->axis_pairs[i];
+    }
+    if (pairs != a->rot_dim / 2) return QLIN_ERR_INVALID_ARG;
+    if (!aligned(a->turns, 8) || (a->positions != nullptr && !aligned(a->positions, a->position_bits / 8)))
+      return QLIN_ERR_MISALIGNED;
+  }
+  if (a->q != nullptr) {
+    if (a->q == a->q_out &&
+        (a->q_token_stride != a->q_out_token_stride || a->q_head_stride != a->q_out_head_stride))
+      return QLIN_ERR_INVALID_ARG;
+    auto apart = [&](int64_t n, int64_t stride) {
+      return n == 1 || stride >= c->head_dim || stride <= -(int64_t)c->head_dim;
+    };
+    if (!apart(a->tokens, a->q_out_token_stride) || !apart(a->q_heads, a->q_out_head_stride))
+      return QLIN_ERR_INVALID_ARG;
+    if (!aligned(a->q, 2) || !aligned(a->q_out, 2)) return QLIN_ERR_MISALIGNED;
+  }
+  if (a->tokens > 1 << 28 || (a->q != nullptr && a->q_heads > 65536)) return QLIN_ERR_UNSUPPORTED;
+  if (!aligned(a->k, 2) || !aligned(a->v, 2) ||
+      (c->format != QLIN_CACHE_E4M3 && (!aligned(c->k, 2) || !aligned(c->v, 2))))
+    return QLIN_ERR_MISALIGNED;
+  unsigned* status;
+  Device dev;
+  QLIN_TRY(device_state(&status, &dev));
+  QLIN_CUDA(launch_cache_append(*c, *a, static_cast<cudaStream_t>(stream), dev, status));
+  return QLIN_OK;
+}
+
+size_t qlin_cache_attention_workspace_size(void) { return (size_t)kWorkspaceBytes; }
+
+qlin_status qlin_cache_attention(const qlin_cache_t* c, const qlin_cache_attention_t* a, void* workspace,
+                                 size_t ws_bytes, void* stream) {
+  QLIN_TRY(check_cache(c));
+  if (a == nullptr || a->q == nullptr || a->out == nullptr || a->tokens < 1 || a->q_heads < 1 ||
+      (a->dtype != QLIN_BF16 && a->dtype != QLIN_FP16) || a->q_heads % c->heads != 0)
+    return QLIN_ERR_INVALID_ARG;
+  if (!std::isnormal(a->scale) || !(a->scale > 0.0f)) return QLIN_ERR_INVALID_ARG;
+  if (a->mask != nullptr && (a->mask_words < 1 || (a->tokens > 1 && a->mask_stride < 0))) return QLIN_ERR_INVALID_ARG;
+  if (a->q == a->out &&
+      (a->q_token_stride != a->out_token_stride || a->q_head_stride != a->out_head_stride))
+    return QLIN_ERR_INVALID_ARG;
+  auto apart = [&](int64_t n, int64_t stride) {
+    return n == 1 || stride >= c->head_dim || stride <= -(int64_t)c->head_dim;
+  };
+  if (!apart(a->tokens, a->out_token_stride) || !apart(a->q_heads, a->out_head_stride)) return QLIN_ERR_INVALID_ARG;
+  if (c->head_dim % 16 != 0 || (c->format != QLIN_CACHE_E4M3 && c->format != a->dtype)) return QLIN_ERR_UNSUPPORTED;
+  // (rows, and the tiles of a call, are counted in 31 and 43 bits)
+  if (a->tokens > 1 << 24 || a->q_heads > 65536) return QLIN_ERR_UNSUPPORTED;
+  const int64_t per16 = c->format == QLIN_CACHE_E4M3 ? 16 : 8;
+  const int64_t strides = c->k_page_stride | c->k_slot_stride | c->k_head_stride | c->v_page_stride |
+                          c->v_slot_stride | c->v_head_stride;
+  if (!aligned(c->k, 16) || !aligned(c->v, 16) || strides % per16 != 0 || !aligned(a->q, 16) ||
+      !aligned(a->out, 16) ||
+      ((a->q_token_stride | a->q_head_stride | a->out_token_stride | a->out_head_stride) & 7) != 0 ||
+      !aligned(a->lse, 4) || !aligned(a->mask, 8))
+    return QLIN_ERR_MISALIGNED;
+  if (workspace == nullptr || ws_bytes < qlin_cache_attention_workspace_size()) return QLIN_ERR_WORKSPACE;
+  if (!aligned(workspace, 16)) return QLIN_ERR_MISALIGNED;
+  unsigned* status;
+  Device dev;
+  QLIN_TRY(device_state(&status, &dev));
+  QLIN_CUDA(launch_cache_attention(*c, *a, workspace, static_cast<cudaStream_t>(stream), dev, status));
+  return QLIN_OK;
+}
+
 qlin_status qlin_rope_turns(int32_t rot_dim, double base, int32_t scaling, double factor,
                             double trained_length, double beta_fast, double beta_slow,
                             uint64_t* turns, float* magnitude) {
@@ -611,7 +778,7 @@ qlin_status qlin_sync_status(void* stream) {
   if (word != 0) {
     const unsigned zero = 0;
     QLIN_CUDA(cudaMemcpy(status, &zero, sizeof zero, cudaMemcpyHostToDevice));
-    return word == kErrTimeout ? QLIN_ERR_TIMEOUT : QLIN_ERR_CUDA;
+    return word == kErrTimeout ? QLIN_ERR_TIMEOUT : word == kErrInvalid ? QLIN_ERR_INVALID_ARG : QLIN_ERR_CUDA;
   }
   return QLIN_OK;
 }

@@ -1,0 +1,718 @@
+// Attention of new tokens over a paged cache: out = softmax(scale q k^T, masked) v in one
+// pass over the keys with the running maximum and sum of each row.
+//
+// The rows of a KV head's group (its query heads times the sequence's new tokens) share its
+// keys, so that these are read once for up to 16 or 32 rows; few rows leave HBM as the bound.
+// Work is counted in tiles of keys of one (sequence, KV head, rows) item, and the CTAs get
+// equal runs of tiles whatever the sequences' lengths.  A run that ends inside an item
+// leaves its sums in the workspace, and the last CTA of the item to arrive joins them in the
+// order of the keys: the same bits whichever CTA that is.
+//
+// A CTA has four warps that work alone: each takes a quarter of a tile's keys through a ring
+// of its own of cp.async copies, a page's rows wherever the table says.  Scores by mma.sync
+// with the rows as M: Q's fragments stay in registers, K's come as 16-byte pieces in K order
+// 8 t (an MMA sums in any order as long as both operands agree), V's through transposing
+// ldmatrix.  The warps' sums meet once an item.
+//   E4M3: codes become fp16, exactly.  Q is brought into fp16 by a power of two per row
+// (bf16 exponents exceed fp16's; elements 2^-14 below the row's largest lose bits that are
+// below 2^-25 of it), and P is fp16.
+//   P is rounded to the values' 16-bit type for the second product, the row's sum is taken
+// before that rounding: errors of half a step of P, independent from key to key, average out.
+#include <type_traits>
+
+#include "qlin_attention.h"
+
+namespace qlin {
+
+namespace {
+
+constexpr int kWarps = 4;
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool in) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(in ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_async_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
+__device__ __forceinline__ uint4 lds128(uint32_t a) {
+  uint4 v;
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
+  return v;
+}
+
+__device__ __forceinline__ void ldmatrix_trans(uint32_t a, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(a));
+}
+
+// c += A B, 16 x 8 x 16; a0, a2 of row g, a1, a3 of row g + 8.
+template <bool kF16>
+__device__ __forceinline__ void mma16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                      uint32_t b1) {
+  if constexpr (kF16)
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, "
+        "%2, %3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+  else
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, "
+        "%2, %3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// Two E4M3 codes as two halves, exactly.
+__device__ __forceinline__ uint32_t e4m3x2_half2(uint32_t codes) {
+  uint32_t h;
+  const uint16_t c = (uint16_t)codes;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(c));
+  return h;
+}
+
+template <CacheKind kKind, int kD, int kM>
+struct AttnCfg {
+  static constexpr int kEs = kKind == CacheKind::kE4m3 ? 1 : 2;
+  static constexpr int kRows = 16 * kM;
+  static constexpr int kKeys = kEs == 1 ? 32 : 16 * kM;    // of a warp and tile
+  static constexpr int kTile = kWarps * kKeys;
+  static constexpr int kRow = kD * kEs;                    // bytes
+  static constexpr int kPieces = kRow / 16;
+  // rows of whole 128-byte lines: 16-byte pieces permuted by the row; else a stride that
+  // spreads the rows over the banks (64 modulo 128 for K's reads, 16 for ldmatrix)
+  static constexpr bool kSwizzle = kRow % 128 == 0;
+  static constexpr int kKStride = kRow;
+  static constexpr int kVStride = kSwizzle ? kRow : kRow + 16;
+  static constexpr int kKBytes = kKeys * kKStride, kVBytes = kKeys * kVStride;
+  static constexpr int kSlot = kKBytes + kVBytes;          // one warp's part of a stage
+  static constexpr int kStageBytes = kWarps * kSlot;
+  static constexpr int kMergeBytes = kRows * kD * 4;       // one warp's sums
+  static constexpr bool kOwnMerge = kMergeBytes > kSlot;   // else in the stage just used
+  static constexpr int kExtra = kOwnMerge ? kWarps * kMergeBytes : 0;
+  static constexpr int kStagesTwo = (112 * 1024 - kExtra) / kStageBytes, kStagesOne = (224 * 1024 - kExtra) / kStageBytes;
+  static constexpr int kStages = kStagesTwo >= 3 ? (kStagesTwo > 4 ? 4 : kStagesTwo) : kStagesOne > 4 ? 4 : kStagesOne;
+  static constexpr int kSmem = kStages * kStageBytes + kExtra;
+  static constexpr int kCtas = 2 * (kSmem + 2048) <= 227 * 1024 ? 2 : 1;   // of an SM
+  static_assert(kStages >= 2, "shared memory");
+  static_assert(kRow % 64 == 0, "K is read in 64-byte chunks");
+};
+
+// A place in the work: tile `tile` of the item (b, h, rt).
+struct Cursor {
+  CacheSeq s;
+  int b, h, rt, tile, tiles, row_tiles;
+};
+
+template <int kRows, int kTile>
+__device__ __forceinline__ CacheSeq read_seq(const AttnParams& p, int b) {
+  return cache_seq(p.q_start[b], p.q_start[b + 1], p.cached[b], p.tokens, p.page_size, p.table_width);
+}
+
+template <int kRows, int kTile>
+__device__ __forceinline__ void open_seq(const AttnParams& p, Cursor& c) {
+  c.s = read_seq<kRows, kTile>(p, c.b);
+  c.tiles = (int)((c.s.keys + kTile - 1) / kTile);
+  c.row_tiles = (int)(((int64_t)c.s.fresh * p.group + kRows - 1) / kRows);
+}
+
+// The next tile; past the last sequence the cursor stays at its end.
+template <int kRows, int kTile>
+__device__ __forceinline__ void advance(const AttnParams& p, Cursor& c) {
+  if (++c.tile < c.tiles) return;
+  c.tile = 0;
+  if (++c.rt < c.row_tiles) return;
+  c.rt = 0;
+  if (++c.h < p.heads) return;
+  c.h = 0;
+  while (++c.b < p.sequences) {
+    open_seq<kRows, kTile>(p, c);
+    if (c.s.fresh > 0 && c.s.keys > 0) return;
+  }
+}
+
+template <int kRows, int kTile>
+__device__ __forceinline__ int64_t seq_units(const AttnParams& p, const CacheSeq& s) {
+  return ((int64_t)s.fresh * p.group + kRows - 1) / kRows * p.heads * ((s.keys + kTile - 1) / kTile);
+}
+
+// The CTA's run of tiles and the cursor at its begin; the same in all threads.
+struct Run {
+  int64_t total, begin, end;
+  int ctas;
+};
+
+template <int kRows, int kTile, int kThreads>
+__device__ __forceinline__ Run find_run(const AttnParams& p, Cursor& c) {
+  __shared__ int64_t warp_sum[kThreads / 32];
+  __shared__ int64_t found_at;
+  __shared__ int found_b;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  Run r{0, 0, 0, 1};
+  int64_t mine = 0, first = 0;
+  bool bad = false;
+  for (int b = threadIdx.x; b < p.sequences; b += kThreads) {
+    const CacheSeq s = read_seq<kRows, kTile>(p, b);
+    bad |= s.bad;
+    const int64_t u = seq_units<kRows, kTile>(p, s);
+    if (b < kThreads) first = u;
+    mine += u;
+  }
+  if (bad && blockIdx.x == 0) atomicExch(p.err, kErrInvalid);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xFFFFFFFFu, mine, o);
+  if (lane == 0) warp_sum[warp] = mine;
+  __syncthreads();
+  for (int w = 0; w < kThreads / 32; ++w) r.total += warp_sum[w];
+  if (r.total == 0) return r;
+  r.ctas = (int)split_ctas(r.total, gridDim.x, p.least);
+  if ((int)blockIdx.x >= r.ctas) return r;
+  r.begin = split_begin(blockIdx.x, r.total, r.ctas);
+  r.end = split_begin(blockIdx.x + 1, r.total, r.ctas);
+  int64_t run = 0;
+  for (int b0 = 0; b0 < p.sequences; b0 += kThreads) {
+    const int b = b0 + threadIdx.x;
+    int64_t u = first;
+    if (b0 > 0) u = b < p.sequences ? seq_units<kRows, kTile>(p, read_seq<kRows, kTile>(p, b)) : 0;
+    int64_t incl = u;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t n = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+      if (lane >= o) incl += n;
+    }
+    __syncthreads();   // warp_sum's last readers
+    if (lane == 31) warp_sum[warp] = incl;
+    __syncthreads();
+    int64_t base = run;
+    for (int w = 0; w < kThreads / 32; ++w) {
+      if (w < warp) base += warp_sum[w];
+      run += warp_sum[w];
+    }
+    if (base + incl - u <= r.begin && r.begin < base + incl) {
+      found_b = b;
+      found_at = base + incl - u;
+    }
+    if (run > r.begin) break;
+  }
+  __syncthreads();
+  c.b = found_b;
+  open_seq<kRows, kTile>(p, c);
+  int64_t at = r.begin - found_at;
+  c.tile = (int)(at % c.tiles);
+  at /= c.tiles;
+  c.rt = (int)(at % c.row_tiles);
+  c.h = (int)(at / c.row_tiles);
+  return r;
+}
+
+// Whether new token t of a sequence (number `token` of the call) sees new token i.
+__device__ __forceinline__ bool sees(const AttnParams& p, int64_t token, int t, int64_t i) {
+  if (p.mask == nullptr) return i <= t;
+  const int64_t w = i >> 6;
+  return w < p.mask_words && ((p.mask[token * p.mask_token + w] >> (i & 63)) & 1u) != 0u;
+}
+
+__device__ __forceinline__ void store_out4(const AttnParams& p, int64_t token, int head, int d, float4 v) {
+  uint16_t* const y = p.out + token * p.out_token + head * p.out_head + d;
+  const uint2 w = p.fp16 ? make_uint2(pack_f16x2(v.x, v.y), pack_f16x2(v.z, v.w))
+                         : make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
+  *reinterpret_cast<uint2*>(y) = w;
+}
+
+__device__ __forceinline__ float log_sum(float m, float l) {   // m in powers of two
+  return l > 0.0f || l != l ? fmaf(m, 0.693147181f, logf(l)) : -INFINITY;
+}
+
+// The rows of an item whose parts CTAs first..last left in the workspace, joined in order.
+template <int kRows, int kD, int kThreads>
+__device__ __forceinline__ void join_parts(const AttnParams& p, const Cursor& c, int first, int last, float v_scale) {
+  const int rows = (int)min((int64_t)kRows, (int64_t)c.s.fresh * p.group - (int64_t)c.rt * kRows);
+  for (int i = threadIdx.x; i < rows * (p.head_dim / 4); i += kThreads) {
+    const int row = i / (p.head_dim / 4), d = i % (p.head_dim / 4) * 4;
+    float m = -INFINITY;
+    for (int q = first; q <= last; ++q) {
+      const int64_t at = (int64_t)(2 * q + (q == first ? 1 : 0)) * kRows + row;
+      m = fmaxf(m, __ldcg(&p.part_ml[at]).x);
+    }
+    const float ms = m == -INFINITY ? 0.0f : m;
+    float l = 0.0f;
+    float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (int q = first; q <= last; ++q) {
+      const int64_t at = (int64_t)(2 * q + (q == first ? 1 : 0)) * kRows + row;
+      const float2 ml = __ldcg(&p.part_ml[at]);
+      const float4 v = __ldcg(reinterpret_cast<const float4*>(p.part + at * kD + d));
+      const float f = exp2_fast(ml.x - ms);
+      l = fmaf(ml.y, f, l);
+      o = make_float4(fmaf(v.x, f, o.x), fmaf(v.y, f, o.y), fmaf(v.z, f, o.z), fmaf(v.w, f, o.w));
+    }
+    const int64_t r = (int64_t)c.rt * kRows + row;
+    const int64_t token = c.s.first + r / p.group;
+    const int head = c.h * p.group + (int)(r % p.group);
+    const float inv = l == 0.0f ? 0.0f : v_scale / l;
+    store_out4(p, token, head, d, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
+    if (p.lse != nullptr && d == 0) p.lse[token * p.lse_token + head] = log_sum(m, l);
+  }
+}
+
+template <CacheKind kKind, int kD, int kM>
+__global__ void __launch_bounds__(kWarps * 32, (AttnCfg<kKind, kD, kM>::kCtas)) attn_kernel(const AttnParams p) {
+  using C = AttnCfg<kKind, kD, kM>;
+  constexpr bool kFp8 = kKind == CacheKind::kE4m3, kF16 = kKind != CacheKind::kBf16;
+  constexpr int kKeys = C::kKeys, kNT = kKeys / 8, kDT = kD / 8, kRows = C::kRows;
+  constexpr int kThreads = kWarps * 32;
+  constexpr int kQWords = kD / 8;          // 32-bit words of a lane's share of a row
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ unsigned ok_bits[kWarps][C::kStages];
+  __shared__ float2 warp_ml[kWarps][kRows];
+  __shared__ unsigned last_flag;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+
+  grid_dep_wait();
+  grid_dep_launch();
+  Cursor cur;
+  const Run run = find_run<kRows, C::kTile, kThreads>(p, cur);
+  if (run.begin >= run.end) return;
+  float k_scale = 1.0f, v_scale = 1.0f;
+  if (kFp8) {
+    k_scale = *p.k_scale;
+    v_scale = *p.v_scale;
+  }
+
+  // ---- loads: lane r < kKeys finds the page of the warp's key r, one tile ahead ----
+  Cursor ahead = cur;
+  int64_t left = run.end - run.begin;   // tiles to fetch
+  int page = -1, page_slot = 0, fetch_h = 0;
+  bool key_in = false;
+  auto fetch = [&] {
+    key_in = false;
+    page = -1;
+    if (left <= 0) return;
+    const int64_t key = (int64_t)ahead.tile * C::kTile + warp * kKeys + lane;
+    int index;
+    fetch_h = ahead.h;
+    if (lane < kKeys && key < ahead.s.keys && cache_place(key, p.page_size, p.table_width, &index, &page_slot)) {
+      page = p.table[ahead.b * p.table_stride + index];
+      key_in = true;
+    }
+    --left;
+    if (left > 0) advance<kRows, C::kTile>(p, ahead);
+  };
+  auto issue = [&](int stage) {
+    const bool ok = key_in && page >= 0 && page < p.pages;
+    if (key_in && !ok) atomicExch(p.err, kErrInvalid);   // the keys of a bad page are not seen
+    const unsigned bits = __ballot_sync(0xFFFFFFFFu, ok);
+    if (lane == 0) ok_bits[warp][stage] = bits;
+    if (bits != 0u) {
+      const int64_t ko = ok ? page * p.k_page + page_slot * p.k_slot + fetch_h * p.k_head : 0;
+      const int64_t vo = ok ? page * p.v_page + page_slot * p.v_slot + fetch_h * p.v_head : 0;
+      const uint32_t kbase = smem_u32(smem + stage * C::kStageBytes + warp * C::kSlot), vbase = kbase + C::kKBytes;
+#pragma unroll
+      for (int i = 0; i < kKeys * C::kPieces / 32; ++i) {
+        const int at = i * 32 + lane, row = at / C::kPieces, piece = at % C::kPieces;
+        const int64_t kr = __shfl_sync(0xFFFFFFFFu, ko, row), vr = __shfl_sync(0xFFFFFFFFu, vo, row);
+        const bool in = ((bits >> row) & 1u) != 0u && piece * 16 < p.head_dim * C::kEs;
+        const int kp = C::kSwizzle ? piece ^ ((row & 1) * 4) : piece, vp = C::kSwizzle ? piece ^ (row & 7) : piece;
+        const int o = in ? piece * 16 : 0;
+        cp_async16(kbase + row * C::kKStride + kp * 16, p.k + kr + o, in);
+        cp_async16(vbase + row * C::kVStride + vp * 16, p.v + vr + o, in);
+      }
+    }
+    cp_async_commit();
+  };
+
+  // ---- one item's state ----
+  uint32_t qf[kM][2][kQWords];
+  float o[kM][kDT][4], m[kM][2], l[kM][2], mult[kM][2];
+  auto begin_item = [&] {
+#pragma unroll
+    for (int i = 0; i < kM; ++i)
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        const int64_t row = (int64_t)cur.rt * kRows + i * 16 + r * 8 + g;
+        const bool in = row < (int64_t)cur.s.fresh * p.group;
+        const uint16_t* const q = p.q + (in ? (cur.s.first + row / p.group) * p.q_token +
+                                                  (cur.h * p.group + row % p.group) * p.q_head
+                                            : 0);
+        m[i][r] = -INFINITY;
+        l[i][r] = 0.0f;
+        mult[i][r] = p.scale_log2;
+        constexpr int kLane = kFp8 ? 16 : 8;   // adjacent elements of a lane
+#pragma unroll
+        for (int c = 0; c < kD / (4 * kLane); ++c)
+#pragma unroll
+          for (int h = 0; h < kLane / 8; ++h) {
+            const int d = c * 4 * kLane + t * kLane + h * 8;
+            uint4 w = make_uint4(0u, 0u, 0u, 0u);
+            if (in && d < p.head_dim) w = *reinterpret_cast<const uint4*>(q + d);
+            uint32_t* const f = &qf[i][r][(c * (kLane / 8) + h) * 4];
+            f[0] = w.x;
+            f[1] = w.y;
+            f[2] = w.z;
+            f[3] = w.w;
+          }
+        if constexpr (kFp8) {
+          // the row's power of two: its largest |q| into [1, 2) (a zero, infinite or NaN row as it is)
+          uint32_t top = 0u;
+#pragma unroll
+          for (int k = 0; k < kQWords; ++k) top = __vmaxu2(top, qf[i][r][k] & 0x7FFF7FFFu);
+          top = max(top & 0xFFFFu, top >> 16);
+          top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+          top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+          const float big = p.fp16 ? __half2float(__ushort_as_half((unsigned short)top))
+                                   : __uint_as_float(top << 16);
+          int e = (int)(__float_as_uint(big) >> 23);   // biased
+          e = e == 0 || e == 255 ? 127 : min(e, 252);
+          const float down = __uint_as_float((uint32_t)(254 - e) << 23);
+          mult[i][r] = fminf(fmaxf(p.scale_log2 * __uint_as_float((uint32_t)e << 23) * k_scale, FLT_MIN), FLT_MAX);
+#pragma unroll
+          for (int k = 0; k < kQWords; ++k) {
+            const uint32_t w = qf[i][r][k];
+            const float2 v = p.fp16 ? __half22float2(*reinterpret_cast<const __half2*>(&w))
+                                    : make_float2(bf16_lo(w), bf16_hi(w));
+            qf[i][r][k] = pack_f16x2(v.x * down, v.y * down);
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < kDT; ++j) o[i][j][2 * r] = o[i][j][2 * r + 1] = 0.0f;
+      }
+  };
+
+  // Element d of the output that word k (0, 1) of accumulator tile j holds in this lane.
+  auto column = [&](int j, int k) {
+    return kFp8 ? (j >> 1) * 16 + 4 * t + 2 * k + (j & 1) : j * 8 + 2 * t + k;
+  };
+
+  auto compute = [&](int stage) {
+    const unsigned bits = ok_bits[warp][stage];
+    if (bits == 0u) return;
+    const uint32_t kbase = smem_u32(smem + stage * C::kStageBytes + warp * C::kSlot), vbase = kbase + C::kKBytes;
+    float s[kM][kNT][4];
+#pragma unroll
+    for (int j = 0; j < kNT; ++j) {
+#pragma unroll
+      for (int i = 0; i < kM; ++i) s[i][j][0] = s[i][j][1] = s[i][j][2] = s[i][j][3] = 0.0f;
+      const int row = 8 * j + g;
+#pragma unroll
+      for (int c = 0; c < C::kRow / 64; ++c) {
+        const int piece = 4 * c + t;
+        const uint4 w = lds128(kbase + row * C::kKStride + (C::kSwizzle ? piece ^ ((row & 1) * 4) : piece) * 16);
+        if constexpr (kFp8) {
+          const uint32_t words[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const uint32_t b0 = e4m3x2_half2(words[q]), b1 = e4m3x2_half2(words[q] >> 16);
+#pragma unroll
+            for (int i = 0; i < kM; ++i)
+              mma16<true>(s[i][j], qf[i][0][8 * c + 2 * q], qf[i][1][8 * c + 2 * q], qf[i][0][8 * c + 2 * q + 1],
+                          qf[i][1][8 * c + 2 * q + 1], b0, b1);
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < kM; ++i) {
+            const uint32_t *q0 = &qf[i][0][4 * c], *q1 = &qf[i][1][4 * c];
+            mma16<kF16>(s[i][j], q0[0], q1[0], q0[1], q1[1], w.x, w.y);
+            mma16<kF16>(s[i][j], q0[2], q1[2], q0[3], q1[3], w.z, w.w);
+          }
+        }
+      }
+    }
+    const int64_t key0 = (int64_t)cur.tile * C::kTile + warp * kKeys;
+    const bool tail = key0 + kKeys > cur.s.cached;   // new tokens among the keys
+    if (tail || bits != (kKeys == 32 ? 0xFFFFFFFFu : (1u << kKeys) - 1u)) {
+#pragma unroll
+      for (int i = 0; i < kM; ++i)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          const int64_t row = (int64_t)cur.rt * kRows + i * 16 + r * 8 + g;
+          const bool in = row < (int64_t)cur.s.fresh * p.group;
+          const int tok = in ? (int)(row / p.group) : 0;
+#pragma unroll
+          for (int j = 0; j < kNT; ++j)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              const int key = 8 * j + 2 * t + k;
+              const int64_t i_new = key0 + key - cur.s.cached;
+              const bool seen = ((bits >> key) & 1u) != 0u && (i_new < 0 || sees(p, cur.s.first + tok, tok, i_new));
+              if (!seen) s[i][j][2 * r + k] = -INFINITY;
+            }
+        }
+    }
+    bool moved = false;
+    float keep[kM][2];
+#pragma unroll
+    for (int i = 0; i < kM; ++i)
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        float mx = fmaxf(s[i][0][2 * r], s[i][0][2 * r + 1]);
+#pragma unroll
+        for (int j = 1; j < kNT; ++j) mx = fmaxf(mx, fmaxf(s[i][j][2 * r], s[i][j][2 * r + 1]));
+        mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 1));
+        mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 2));
+        const float now = fmaxf(m[i][r], mx * mult[i][r]);
+        const float base = now == -INFINITY ? 0.0f : now;   // (nothing seen yet)
+        keep[i][r] = exp2_fast(m[i][r] - base);
+        moved |= now != m[i][r];
+        m[i][r] = now;
+        float sum = 0.0f;
+#pragma unroll
+        for (int j = 0; j < kNT; ++j)
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const float e = exp2_fast(fmaf(s[i][j][2 * r + k], mult[i][r], -base));
+            s[i][j][2 * r + k] = e;
+            sum += e;
+          }
+        l[i][r] = fmaf(l[i][r], keep[i][r], sum);
+      }
+    if (__any_sync(0xFFFFFFFFu, moved)) {
+#pragma unroll
+      for (int i = 0; i < kM; ++i)
+#pragma unroll
+        for (int j = 0; j < kDT; ++j) {
+          o[i][j][0] *= keep[i][0];
+          o[i][j][1] *= keep[i][0];
+          o[i][j][2] *= keep[i][1];
+          o[i][j][3] *= keep[i][1];
+        }
+    }
+    // A value that is not finite must not reach rows that do not see its key, and in a
+    // product 0 times it would: such a tile (of new tokens; all others are seen by every
+    // row) is added up key by key.
+    if (tail) {
+      bool odd = false;
+      for (int at = lane; at < kKeys * C::kPieces; at += 32) {
+        const uint4 w = lds128(vbase + at / C::kPieces * C::kVStride + at % C::kPieces * 16);
+        const uint32_t words[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          if (kFp8)
+            odd |= __vcmpeq4(words[q] & 0x7F7F7F7Fu, 0x7F7F7F7Fu) != 0u;
+          else
+            odd |= __vcmpgeu2(words[q] & 0x7FFF7FFFu, kF16 ? 0x7C007C00u : 0x7F807F80u) != 0u;
+        }
+      }
+      if (__any_sync(0xFFFFFFFFu, odd)) {
+        // in K's place, or where that is too small in the warp's place for its sums
+        constexpr bool kFits = kRows * 4 <= C::kRow;
+        static_assert(kFits || C::kOwnMerge, "room for the probabilities");
+        float* const probs = reinterpret_cast<float*>(
+            kFits ? smem + stage * C::kStageBytes + warp * C::kSlot
+                  : smem + C::kStages * C::kStageBytes + warp * C::kMergeBytes);
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < kM; ++i)
+#pragma unroll
+          for (int j = 0; j < kNT; ++j)
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              probs[(i * 16 + (k >> 1) * 8 + g) * kKeys + 8 * j + 2 * t + (k & 1)] = s[i][j][k];
+        __syncwarp();
+        const uint8_t* const vs = smem + stage * C::kStageBytes + warp * C::kSlot + C::kKBytes;
+        for (int key = 0; key < kKeys; ++key) {
+#pragma unroll
+          for (int j = 0; j < kDT; ++j)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              const int at = column(j, k) * C::kEs, piece = at / 16;
+              const uint8_t* const a = vs + key * C::kVStride + (C::kSwizzle ? piece ^ (key & 7) : piece) * 16 + at % 16;
+              float v;
+              if (kFp8)
+                v = e4m3_value(*a);
+              else if (kF16)
+                v = __half2float(*reinterpret_cast<const __half*>(a));
+              else
+                v = __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t*>(a) << 16);
+#pragma unroll
+              for (int i = 0; i < kM; ++i)
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                  const float pr = probs[(i * 16 + r * 8 + g) * kKeys + key];
+                  if (pr != 0.0f) o[i][j][2 * r + k] = fmaf(pr, v, o[i][j][2 * r + k]);
+                }
+            }
+        }
+        __syncwarp();
+        return;
+      }
+    }
+#pragma unroll
+    for (int c = 0; c < kKeys / 16; ++c) {
+      uint32_t a[kM][4];
+#pragma unroll
+      for (int i = 0; i < kM; ++i)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float lo = s[i][2 * c + (k >> 1)][2 * (k & 1)], hi = s[i][2 * c + (k >> 1)][2 * (k & 1) + 1];
+          a[i][k] = kF16 ? pack_f16x2(lo, hi) : pack_bf16x2(lo, hi);
+        }
+      // lane -> row of one of four 8 x 16-byte matrices: keys 0-7, 8-15 of one piece, then of the next
+      const int key = c * 16 + ((lane >> 3) & 1) * 8 + (lane & 7);
+#pragma unroll
+      for (int j = 0; j < C::kPieces / 2; ++j) {
+        const int piece = 2 * j + (lane >> 4);
+        uint32_t r[4];
+        ldmatrix_trans(vbase + key * C::kVStride + (C::kSwizzle ? piece ^ (key & 7) : piece) * 16, r);
+        if constexpr (kFp8) {
+          // a 16-bit unit is two adjacent elements of one key: even and odd ones apart
+#pragma unroll
+          for (int q = 0; q < 2; ++q) {
+            const uint32_t w0 = __byte_perm(r[2 * q], 0u, 0x3120), w1 = __byte_perm(r[2 * q + 1], 0u, 0x3120);
+            const uint32_t e0 = e4m3x2_half2(w0), e1 = e4m3x2_half2(w1);
+            const uint32_t d0 = e4m3x2_half2(w0 >> 16), d1 = e4m3x2_half2(w1 >> 16);
+#pragma unroll
+            for (int i = 0; i < kM; ++i) {
+              mma16<true>(o[i][4 * j + 2 * q], a[i][0], a[i][1], a[i][2], a[i][3], e0, e1);
+              mma16<true>(o[i][4 * j + 2 * q + 1], a[i][0], a[i][1], a[i][2], a[i][3], d0, d1);
+            }
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < kM; ++i) {
+            mma16<kF16>(o[i][2 * j], a[i][0], a[i][1], a[i][2], a[i][3], r[0], r[1]);
+            mma16<kF16>(o[i][2 * j + 1], a[i][0], a[i][1], a[i][2], a[i][3], r[2], r[3]);
+          }
+        }
+      }
+    }
+  };
+
+  // The end of an item, or of the CTA's run inside one: the warps' sums meet in shared
+  // memory (the stage just used is free until the next tile's turn).
+  auto end_item = [&](int stage, int64_t unit) {
+    float* const own = reinterpret_cast<float*>(
+        C::kOwnMerge ? smem + C::kStages * C::kStageBytes + warp * C::kMergeBytes
+                     : smem + stage * C::kStageBytes + warp * C::kSlot);
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < kM; ++i)
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        float sum = l[i][r];
+        sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 1);
+        sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 2);
+        const int row = i * 16 + r * 8 + g;
+        if (t == 0) warp_ml[warp][row] = make_float2(m[i][r], sum);
+#pragma unroll
+        for (int j = 0; j < kDT; ++j)
+#pragma unroll
+          for (int k = 0; k < 2; ++k) own[row * kD + column(j, k)] = o[i][j][2 * r + k];
+      }
+    __syncthreads();
+    const int64_t item0 = unit - cur.tile, item1 = item0 + cur.tiles - 1;   // the item's first and last unit
+    const bool whole = item0 >= run.begin && item1 < run.end;
+    const int rows = (int)min((int64_t)kRows, (int64_t)cur.s.fresh * p.group - (int64_t)cur.rt * kRows);
+    const int64_t part_row = (int64_t)(2 * blockIdx.x + (item0 < run.begin ? 0 : 1)) * kRows;
+    const uint8_t* const sums = C::kOwnMerge ? smem + C::kStages * C::kStageBytes : smem + stage * C::kStageBytes;
+    constexpr int kStep = C::kOwnMerge ? C::kMergeBytes : C::kSlot;
+    for (int i = threadIdx.x; i < rows * (p.head_dim / 4); i += kThreads) {
+      const int row = i / (p.head_dim / 4), d = i % (p.head_dim / 4) * 4;
+      float top = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) top = fmaxf(top, warp_ml[w][row].x);
+      const float base = top == -INFINITY ? 0.0f : top;
+      float sum = 0.0f;
+      float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        const float2 ml = warp_ml[w][row];
+        const float f = exp2_fast(ml.x - base);
+        const float4 x = *reinterpret_cast<const float4*>(sums + w * kStep + (row * kD + d) * 4);
+        sum = fmaf(ml.y, f, sum);
+        v = make_float4(fmaf(x.x, f, v.x), fmaf(x.y, f, v.y), fmaf(x.z, f, v.z), fmaf(x.w, f, v.w));
+      }
+      if (whole) {
+        const int64_t r = (int64_t)cur.rt * kRows + row;
+        const int64_t token = cur.s.first + r / p.group;
+        const int head = cur.h * p.group + (int)(r % p.group);
+        const float inv = sum == 0.0f ? 0.0f : v_scale / sum;
+        store_out4(p, token, head, d, make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv));
+        if (p.lse != nullptr && d == 0) p.lse[token * p.lse_token + head] = log_sum(top, sum);
+      } else {
+        if (d == 0) p.part_ml[part_row + row] = make_float2(top, sum);
+        *reinterpret_cast<float4*>(p.part + (part_row + row) * kD + d) = v;
+      }
+    }
+    if (!whole) {
+      const int first = (int)split_owner(item0, run.total, run.ctas), last = (int)split_owner(item1, run.total, run.ctas);
+      __threadfence();
+      __syncthreads();
+      if (threadIdx.x == 0) {
+        const bool all = atomicAdd(&p.counts[first], 1u) == (unsigned)(last - first);
+        if (all) p.counts[first] = 0u;   // as it was before the call
+        __threadfence();
+        last_flag = all ? 1u : 0u;
+      }
+      __syncthreads();
+      if (last_flag != 0u) join_parts<kRows, kD, kThreads>(p, cur, first, last, v_scale);
+    }
+    __syncthreads();
+  };
+
+  fetch();
+#pragma unroll
+  for (int s = 0; s < C::kStages - 1; ++s) {
+    issue(s);
+    fetch();
+  }
+  bool fresh_item = true;
+  int stage = 0;
+  for (int64_t unit = run.begin; unit < run.end; ++unit) {
+    if (fresh_item) begin_item();
+    cp_async_wait<C::kStages - 2>();
+    __syncwarp();
+    issue(stage == 0 ? C::kStages - 1 : stage - 1);
+    fetch();
+    compute(stage);
+    const bool done = cur.tile + 1 == cur.tiles;
+    if (done || unit + 1 == run.end) end_item(stage, unit);
+    fresh_item = done;
+    if (unit + 1 < run.end) advance<kRows, C::kTile>(p, cur);
+    if (++stage == C::kStages) stage = 0;
+    __syncwarp();
+  }
+  cp_async_wait<0>();
+}
+
+template <CacheKind kKind, int kD, int kM>
+cudaError_t launch_attn(AttnParams p, cudaStream_t s, Device dev) {
+  using C = AttnCfg<kKind, kD, kM>;
+  struct Setup {
+    cudaError_t err;
+    int ctas;
+  };
+  static PerDevice<Setup> per_device;
+  const Setup& setup = per_device.get(dev.index, [&] {
+    Setup t{cudaFuncSetAttribute(attn_kernel<kKind, kD, kM>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem), 0};
+    if (t.err == cudaSuccess)
+      t.err = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&t.ctas, attn_kernel<kKind, kD, kM>, kWarps * 32, C::kSmem);
+    if (t.err == cudaSuccess && t.ctas < 1) t.err = cudaErrorInvalidConfiguration;
+    return t;
+  });
+  if (setup.err != cudaSuccess) return setup.err;
+  // two unfinished items per CTA in the workspace, behind the counts
+  constexpr int64_t kPart = 2 * C::kRows * ((int64_t)kD * 4 + 8);
+  const int64_t most = std::min<int64_t>(kMostCtas, (kWorkspaceBytes - kCountBytes) / kPart);
+  const int ctas = (int)std::min<int64_t>((int64_t)setup.ctas * dev.num_sms, most);
+  p.part_ml = reinterpret_cast<float2*>(reinterpret_cast<uint8_t*>(p.counts) + kCountBytes);
+  p.part = reinterpret_cast<float*>(p.part_ml + (int64_t)2 * C::kRows * ctas);
+  p.least = std::max(1, 256 / C::kTile);
+  return launch_pdl(attn_kernel<kKind, kD, kM>, dim3((unsigned)ctas), kWarps * 32, C::kSmem, s, p);
+}
+
+// Rows per sequence and KV head, on average, say whether 32 rows share a read of the keys.
+template <CacheKind kKind>
+cudaError_t launch_attn_kind(const AttnParams& p, cudaStream_t s, Device dev) {
+  const bool more = p.tokens * p.group > (int64_t)16 * p.sequences;
+  if (p.head_dim <= 64) return more ? launch_attn<kKind, 64, 2>(p, s, dev) : launch_attn<kKind, 64, 1>(p, s, dev);
+  if constexpr (kKind != CacheKind::kE4m3)
+    if (p.head_dim <= 96) return more ? launch_attn<kKind, 96, 2>(p, s, dev) : launch_attn<kKind, 96, 1>(p, s, dev);
+  if (p.head_dim <= 128) return more ? launch_attn<kKind, 128, 2>(p, s, dev) : launch_attn<kKind, 128, 1>(p, s, dev);
+  if (p.head_dim <= 192) return launch_attn<kKind, 192, 1>(p, s, dev);
+  return launch_attn<kKind, 256, 1>(p, s, dev);
+}
+
+}  // namespace
+
+}  // namespace qlin

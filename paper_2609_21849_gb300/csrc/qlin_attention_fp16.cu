@@ -1,0 +1,11 @@
+// Attention over a paged cache of fp16 keys and values (a translation unit per type, so that
+// they compile side by side).
+#include "qlin_attention.cuh"
+
+namespace qlin {
+
+cudaError_t launch_attention_fp16(const AttnParams& p, cudaStream_t s, Device dev) {
+  return launch_attn_kind<CacheKind::kFp16>(p, s, dev);
+}
+
+}  // namespace qlin

@@ -1,0 +1,64 @@
+// The paged cache's index arithmetic and the attention's split of its work: host and
+// device code without CUDA headers, so that a CPU test can run it.
+#pragma once
+
+#include <stdint.h>
+
+#ifdef __CUDACC__
+#define QLIN_HD __host__ __device__ __forceinline__
+#else
+#define QLIN_HD inline
+#endif
+
+namespace qlin {
+
+// Where the cache of one sequence holds its token `at`: its page's number in the table
+// row, and the slot in that page.  False past the table's row.
+QLIN_HD bool cache_place(int64_t at, int page_size, int table_width, int* index, int* slot) {
+  if (at < 0 || at >= (int64_t)page_size * table_width) return false;
+  *index = (int)(at / page_size);   // (the product fits 62 bits, the quotient 31)
+  *slot = (int)(at - (int64_t)*index * page_size);
+  return true;
+}
+
+// One sequence's share of a call, from device data that may be wrong: counts outside the
+// call or the table come as an empty sequence, or its keys cut at the table's end.
+struct CacheSeq {
+  int64_t first;    // its first new token
+  int64_t cached;   // tokens before these
+  int64_t keys;     // cached + fresh, at most what the table can hold
+  int fresh;        // new tokens
+  bool bad;
+};
+
+QLIN_HD CacheSeq cache_seq(int64_t start, int64_t end, int64_t cached, int64_t tokens, int page_size,
+                           int table_width) {
+  CacheSeq s{start, cached, 0, 0, false};
+  const int64_t room = (int64_t)page_size * table_width;
+  if (start < 0 || end < start || end > tokens || cached < 0) {
+    s.bad = true;
+    return s;
+  }
+  s.fresh = (int)(end - start);
+  s.keys = cached + s.fresh;
+  if (s.keys > room) {
+    s.bad = s.fresh > 0;
+    s.keys = room;
+  }
+  return s;
+}
+
+// An even split of `total` units among `ctas`: CTA c takes [begin(c), begin(c + 1)).
+// (total below 2^43, ctas below 2^20)
+QLIN_HD int64_t split_begin(int64_t c, int64_t total, int64_t ctas) { return c * total / ctas; }
+
+// The CTA that takes unit t.
+QLIN_HD int64_t split_owner(int64_t t, int64_t total, int64_t ctas) { return ((t + 1) * ctas - 1) / total; }
+
+// How many of `ctas` work where each should have `least` units.
+QLIN_HD int64_t split_ctas(int64_t total, int64_t ctas, int64_t least) {
+  const int64_t want = (total + least - 1) / least;
+  return want < 1 ? 1 : want < ctas ? want : ctas;
+}
+
+}  // namespace qlin

@@ -15,6 +15,7 @@
 namespace qlin {
 
 // Device status word values (mirrors qlin_status).
+constexpr unsigned kErrInvalid = 1u;
 constexpr unsigned kErrTimeout = 5u;
 
 // ------------------------------------------------------------------ misc ---
@@ -674,6 +675,16 @@ __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
       "fma.rn.f32x2 x, x, y, z;\n\tmov.b64 {%0, %1}, x;\n\t}"
       : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
   return r;
+}
+
+// (cos, sin) of position * turns, turns in units of 2^-64 turn: the product modulo 2^64 is
+// the angle without whole turns, its top 32 bits a signed fraction of a turn, which is
+// twice as many half turns.
+__device__ __forceinline__ float2 turn_by(int64_t position, uint64_t turns) {
+  const uint64_t t = (uint64_t)position * turns;
+  float s, c;
+  sincospif((float)(int32_t)(uint32_t)(t >> 32) * 0x1p-31f, &s, &c);
+  return make_float2(c, s);
 }
 
 // ---------------------------------------------------------- activations ---

@@ -23,7 +23,7 @@ namespace qlin {
 
 namespace {
 
-enum class Kind { kNvfp4, kFp8, kBf16, kFp16 };
+enum class Kind { kNvfp4, kFp8, kBf16, kFp16, kFp8Block };
 
 constexpr int kBlock = 16;        // rows of W per MMA, and of an NVFP4 block of y
 constexpr int kChunk = 64;        // bytes of a row per warp and step
@@ -35,8 +35,8 @@ struct FewParams {
   const uint8_t* w;
   const uint8_t* sfa;       // NVFP4 block scales
   const uint8_t* sfb;
-  const float* sdec_a;
-  const float* sdec_w;
+  const float* sdec_a;      // FP8 block: [K blocks, M]
+  const float* sdec_w;      // and [K blocks, ceil(N / 128)]
   int a_per_row, w_per_channel;
   const uint16_t* bias;
   const uint16_t* residual;
@@ -138,7 +138,7 @@ constexpr int kUnrollOf = kRowTiles == 2 ? 2 : kKind == Kind::kNvfp4 ? 2 : 4;
 // its warps taking chunks of K in turn; the CTAs' sums meet in distributed shared memory.
 template <Kind kKind, int kTiles, int kRowTiles>
 __global__ void __launch_bounds__(kMaxWarps * 32) few_kernel(const FewParams p) {
-  constexpr bool kFp4 = kKind == Kind::kNvfp4;
+  constexpr bool kFp4 = kKind == Kind::kNvfp4, kBlocks = kKind == Kind::kFp8Block;
   constexpr int kRows = kBlock * kRowTiles, kOuts = kTiles * kRowTiles;
   constexpr int kUnroll = kUnrollOf<kKind, kTiles, kRowTiles>;
   __shared__ float red[kMaxWarps][kTiles * 8][kRows + 1];
@@ -148,7 +148,7 @@ __global__ void __launch_bounds__(kMaxWarps * 32) few_kernel(const FewParams p) 
   const int m0 = (int)blockIdx.y * kTiles * 8;   // the CTA's first token
   const int rank = p.split > 1 ? (int)cluster_ctarank() : 0;
   const int64_t n0 = (int64_t)(blockIdx.x / (unsigned)p.split) * kRows;
-  const int64_t w_row = kFp4 ? p.K / 2 : kKind == Kind::kFp8 ? p.K : p.K * 2;
+  const int64_t w_row = kFp4 ? p.K / 2 : kKind == Kind::kFp8 || kBlocks ? p.K : p.K * 2;
   const int chunks = (int)((w_row + kChunk - 1) / kChunk);
   const int stride = warps * p.split;   // warps that share the rows
   // every CTA of the cluster runs before one writes into another's shared memory
@@ -165,7 +165,7 @@ __global__ void __launch_bounds__(kMaxWarps * 32) few_kernel(const FewParams p) 
   // what this thread's outputs need beside the sums: loaded now, used after them
   // (loaded there, they cost a chain of two loads at the end)
   constexpr bool kF16 = kKind == Kind::kFp16;
-  const bool requant = kKind != Kind::kBf16 && !kF16 && p.next_scale != nullptr;
+  const bool requant = kKind != Kind::kBf16 && !kF16 && !kBlocks && p.next_scale != nullptr;
   float o_scale[kOuts], o_bias[kOuts], o_res[kOuts];
   bool o_own[kOuts];   // (the same for the sixteen threads of a token)
 #pragma unroll
@@ -193,6 +193,9 @@ __global__ void __launch_bounds__(kMaxWarps * 32) few_kernel(const FewParams p) 
   float acc[kRowTiles][kTiles][4] = {};
   uint4 va[kUnroll][kRowTiles][2], vb[kUnroll][kTiles];
   uint16_t sa[kUnroll][kRowTiles][2], sb[kUnroll][kTiles];
+  // FP8 block: a chunk's scale of these rows of W, and of the lane's tokens 2 t and 2 t + 1 of each tile
+  float block_w[kUnroll], block_a[kUnroll][kTiles][2];
+  const int64_t w_blocks = (p.N + 127) / 128;
   const int first = rank * warps + warp;
   int left = (chunks - first + stride - 1) / stride;   // chunks to load
   int tail = kFp4 ? (int)(w_row - (int64_t)first * kChunk) - 16 * t : 0;   // bytes of the row from here
@@ -209,6 +212,7 @@ __global__ void __launch_bounds__(kMaxWarps * 32) few_kernel(const FewParams p) 
   for (int h = 0; h < 2 * kRowTiles; ++h)
     fw[h / 2][h % 2] = kFp4 ? p.sfb + scale_offset(n0 + g + 8 * h, 8 * (int64_t)first + 2 * t, p.K) : nullptr;
   const int step = stride * kChunk, fstep = stride * 1024;
+  int chunk = first;
   auto load = [&](int u) {
     // NVFP4 rows are multiples of 32 bytes: the last chunk may be half a chunk
     const bool in = left > 0 && (!kFp4 || tail > 0);
@@ -232,6 +236,18 @@ __global__ void __launch_bounds__(kMaxWarps * 32) few_kernel(const FewParams p) 
         if (in) sb[u][j] = *reinterpret_cast<const uint16_t*>(fa[j]);
         fa[j] += fstep;
       }
+    }
+    if constexpr (kBlocks) {
+      const int64_t kb = chunk >> 1;   // two chunks to a block of 128
+      block_w[u] = in ? __ldg(p.sdec_w + kb * w_blocks + (n0 >> 7)) : 0.0f;
+#pragma unroll
+      for (int j = 0; j < kTiles; ++j)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const int64_t m = m0 + j * 8 + 2 * t + k;
+          block_a[u][j][k] = in && m < p.M ? __ldg(p.sdec_a + kb * p.M + m) : 0.0f;
+        }
+      chunk += stride;
     }
     w += step;
     tail -= step;
@@ -262,20 +278,35 @@ __global__ void __launch_bounds__(kMaxWarps * 32) few_kernel(const FewParams p) 
           }
         }
       }
-    } else if constexpr (kKind == Kind::kFp8) {
+    } else if constexpr (kKind == Kind::kFp8 || kBlocks) {
+      auto products = [&](float (&sum)[kRowTiles][kTiles][4]) {
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {   // four elements of K per lane
-        auto word = [&](const uint4& v) { return q == 0 ? v.x : q == 1 ? v.y : q == 2 ? v.z : v.w; };
-        uint32_t hb[kTiles][2];
+        for (int q = 0; q < 4; ++q) {   // four elements of K per lane
+          auto word = [&](const uint4& v) { return q == 0 ? v.x : q == 1 ? v.y : q == 2 ? v.z : v.w; };
+          uint32_t hb[kTiles][2];
 #pragma unroll
-        for (int j = 0; j < kTiles; ++j) e4m3x4_half(word(vb[u][j]), hb[j][0], hb[j][1]);
+          for (int j = 0; j < kTiles; ++j) e4m3x4_half(word(vb[u][j]), hb[j][0], hb[j][1]);
 #pragma unroll
-        for (int i = 0; i < kRowTiles; ++i) {
-          uint32_t h0[2], h1[2];
-          e4m3x4_half(word(va[u][i][0]), h0[0], h0[1]);
-          e4m3x4_half(word(va[u][i][1]), h1[0], h1[1]);
+          for (int i = 0; i < kRowTiles; ++i) {
+            uint32_t h0[2], h1[2];
+            e4m3x4_half(word(va[u][i][0]), h0[0], h0[1]);
+            e4m3x4_half(word(va[u][i][1]), h1[0], h1[1]);
 #pragma unroll
-          for (int j = 0; j < kTiles; ++j) mma<kKind>(acc[i][j], h0[0], h1[0], h0[1], h1[1], hb[j][0], hb[j][1]);
+            for (int j = 0; j < kTiles; ++j) mma<kKind>(sum[i][j], h0[0], h1[0], h0[1], h1[1], hb[j][0], hb[j][1]);
+          }
+        }
+      };
+      if constexpr (!kBlocks) products(acc);
+      if constexpr (kBlocks) {   // the chunk's products apart: their scales differ from the next one's
+        float part[kRowTiles][kTiles][4] = {};
+        products(part);
+#pragma unroll
+        for (int j = 0; j < kTiles; ++j) {
+          const float s[2] = {__fmul_rn(block_a[u][j][0], block_w[u]), __fmul_rn(block_a[u][j][1], block_w[u])};
+#pragma unroll
+          for (int i = 0; i < kRowTiles; ++i)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) acc[i][j][k] = __fmaf_rn(part[i][j][k], s[k & 1], acc[i][j][k]);
         }
       }
     } else {
@@ -420,7 +451,7 @@ cudaError_t launch_tiles(FewParams p, cudaStream_t s, Device dev) {
     return t;
   });
   if (setup.err != cudaSuccess) return setup.err;
-  const int64_t row = kKind == Kind::kNvfp4 ? p.K / 2 : kKind == Kind::kFp8 ? p.K : p.K * 2;
+  const int64_t row = kKind == Kind::kNvfp4 ? p.K / 2 : kKind == Kind::kFp8 || kKind == Kind::kFp8Block ? p.K : p.K * 2;
   const Split split = choose_split(kKind, p.N, (p.M + kTiles * 8 - 1) / (kTiles * 8), p.K, (row + kChunk - 1) / kChunk,
                                    setup.resident, dev.num_sms);
   p.split = split.ctas;
@@ -474,6 +505,7 @@ cudaError_t launch_few(const GemmArgs& a, cudaStream_t s, Device dev) {
   p.rq_col0 = a.rq_col0;
   p.rq_cols = a.rq_cols;
   return a.bf16 ? (a.fp16 ? launch_kind<Kind::kFp16>(p, s, dev) : launch_kind<Kind::kBf16>(p, s, dev))
+         : a.blocks ? launch_kind<Kind::kFp8Block>(p, s, dev)
          : a.fp4 ? launch_kind<Kind::kNvfp4>(p, s, dev)
                  : launch_kind<Kind::kFp8>(p, s, dev);
 }

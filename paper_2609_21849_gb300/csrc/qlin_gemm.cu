@@ -1651,6 +1651,11 @@ CUresult encode_tensor_map_out_bf16(CUtensorMap* map, void* base, uint64_t cols,
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
 }
 
+CUresult encode_tensor_map_codes(CUtensorMap* map, const void* base, uint64_t k_bytes, uint64_t rows,
+                                 uint32_t box_rows) {
+  return encode_codes(map, base, k_bytes, rows, box_rows);
+}
+
 cudaError_t launch_gemm(const GemmArgs& a, cudaStream_t s, Device dev, unsigned* err,
                         uint64_t timeout_ns) {
   if (a.split > 1)

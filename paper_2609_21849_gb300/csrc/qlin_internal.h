@@ -79,10 +79,21 @@ cudaError_t launch_rmsnorm(const qlin_rmsnorm_t& a, void* y16, const float* stat
 // ---- rotary positions (qlin_rope.cu) ----
 cudaError_t launch_rope(const qlin_rope_t& a, int num_sms, cudaStream_t s);
 
+// ---- block-scaled FP8 quantizer (qlin_quant_block.cu) ----
+cudaError_t launch_quant_fp8_block(const void* x, int64_t x_stride, bool fp16, const qlin_fp8_block_t& out,
+                                   cudaStream_t s);
+
+// ---- paged cache (qlin_append.cu, qlin_attention*.cu); err: device status word ----
+cudaError_t launch_cache_append(const qlin_cache_t& c, const qlin_cache_append_t& a, cudaStream_t s, Device dev,
+                                unsigned* err);
+cudaError_t launch_cache_attention(const qlin_cache_t& c, const qlin_cache_attention_t& a, void* workspace,
+                                   cudaStream_t s, Device dev, unsigned* err);
+
 // ---- GEMMs (qlin_gemm.cu) ----
 struct GemmArgs {
   bool fp4;                 // NVFP4 (true) or FP8
   bool bf16;                // 16-bit float operands (fp4 false), no scales
+  bool blocks;              // FP8 with sdec_a [K blocks, M] and sdec_w [K blocks, N blocks]
   bool fp16;                // with bf16: the operands and y are fp16, not bf16
   const void* a_codes;      // [M, K/2] or [M, K] bytes, or bf16 [M, K]
   int64_t a_row_bytes;      // row stride of A in bytes (0: packed rows)
@@ -120,10 +131,16 @@ cudaError_t launch_gemm(const GemmArgs& a, cudaStream_t s, Device dev, unsigned*
                         uint64_t timeout_ns);
 // The same for few rows of A (few_tokens; qlin_few.cu; no output amax).
 cudaError_t launch_few(const GemmArgs& a, cudaStream_t s, Device dev);
+// FP8 with block scales (qlin_gemm_block.cu).
+cudaError_t launch_gemm_block(const GemmArgs& a, cudaStream_t s, Device dev, unsigned* err, uint64_t timeout_ns);
 cudaError_t launch_wait_selftest(uint64_t timeout_ns, cudaStream_t s, unsigned* err);
 
 // Resolves cuTensorMapEncodeTiled through the runtime (no libcuda link).
 CUresult encode_tensor_map_out_bf16(CUtensorMap* map, void* base, uint64_t cols, uint64_t rows,
                                     bool fp16 = false);
+
+// FP8 codes [rows, k_bytes]: 128-byte x box_rows boxes, 128-byte swizzle.
+CUresult encode_tensor_map_codes(CUtensorMap* map, const void* base, uint64_t k_bytes, uint64_t rows,
+                                 uint32_t box_rows);
 
 }  // namespace qlin

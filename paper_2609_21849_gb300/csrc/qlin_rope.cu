@@ -43,12 +43,8 @@ __device__ __forceinline__ float2 rotation(const RopeParams& p, int64_t token, i
   const int64_t at = token * p.pos_token + axis * p.pos_axis;
   const int64_t pos = p.pos64 ? static_cast<const int64_t*>(p.positions)[at]
                               : (int64_t)static_cast<const int32_t*>(p.positions)[at];
-  const uint64_t t = (uint64_t)pos * p.turns[i];
-  // a signed 32-bit fraction of a turn is twice as many half turns
-  float s, c;
-  sincospif((float)(int32_t)(uint32_t)(t >> 32) * 0x1p-31f, &s, &c);
-  if (p.inverse) s = -s;
-  return make_float2(c * p.magnitude, s * p.magnitude);
+  const float2 r = turn_by(pos, p.turns[i]);
+  return make_float2(r.x * p.magnitude, (p.inverse ? -r.y : r.y) * p.magnitude);
 }
 
 // One CTA per token: the rotations of its pairs once, then the heads.

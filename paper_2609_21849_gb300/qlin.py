@@ -23,6 +23,7 @@ QLIN_BF16, QLIN_FP16 = 1, 2
 QLIN_ACT_NONE, QLIN_ACT_RELU, QLIN_ACT_SILU, QLIN_ACT_GELU_TANH, QLIN_ACT_GELU = range(5)
 QLIN_ROPE_INTERLEAVED, QLIN_ROPE_HALF = 0, 1
 QLIN_ROPE_NONE, QLIN_ROPE_LINEAR, QLIN_ROPE_NTK, QLIN_ROPE_YARN = range(4)
+QLIN_CACHE_BF16, QLIN_CACHE_FP16, QLIN_CACHE_E4M3 = 1, 2, 3
 STATUS = {0: "QLIN_OK", 1: "QLIN_ERR_INVALID_ARG", 2: "QLIN_ERR_UNSUPPORTED",
           3: "QLIN_ERR_MISALIGNED", 4: "QLIN_ERR_CUDA", 5: "QLIN_ERR_TIMEOUT",
           6: "QLIN_ERR_WORKSPACE"}
@@ -35,6 +36,8 @@ EXPORTS = ("qlin_nvfp4_scale_bytes", "qlin_workspace_size", "qlin_quantize_act_n
            "qlin_rmsnorm", "qlin_rmsnorm_fp8", "qlin_rmsnorm_nvfp4",
            "qlin_linear_nvfp4", "qlin_linear_fp8", "qlin_linear_bf16", "qlin_linear_fp16",
            "qlin_rope", "qlin_rope_turns",
+           "qlin_fp8_block_scales", "qlin_quantize_fp8_block", "qlin_linear_fp8_block",
+           "qlin_cache_append", "qlin_cache_attention", "qlin_cache_attention_workspace_size",
            "qlin_sync_status", "qlin_selftest_bounded_wait",
            "qlin_set_wait_timeout_ns", "qlin_status_str", "qlin_last_error")
 
@@ -80,6 +83,41 @@ class RopeDesc(ctypes.Structure):
                 + [(n, ctypes.c_int32) for n in ("layout", "inverse", "dtype")])
 
 
+class FP8BlockDesc(ctypes.Structure):
+    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("rows", ctypes.c_int64),
+                ("K", ctypes.c_int64), ("block_rows", ctypes.c_int32)]
+
+
+class CacheDesc(ctypes.Structure):
+    _fields_ = ([("k", ctypes.c_void_p), ("v", ctypes.c_void_p)]
+                + [(n, ctypes.c_int64) for n in ("k_page_stride", "k_slot_stride", "k_head_stride", "v_page_stride",
+                                                 "v_slot_stride", "v_head_stride")]
+                + [("page_table", ctypes.c_void_p), ("table_stride", ctypes.c_int64)]
+                + [(n, ctypes.c_void_p) for n in ("cached", "q_start", "k_scale", "v_scale")]
+                + [(n, ctypes.c_int32) for n in ("sequences", "pages", "page_size", "table_width", "heads",
+                                                 "head_dim", "format")])
+
+
+class CacheAppendDesc(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("k", "v", "q", "q_out")]
+                + [(n, ctypes.c_int64) for n in ("k_token_stride", "k_head_stride", "v_token_stride",
+                                                 "v_head_stride", "q_token_stride", "q_head_stride",
+                                                 "q_out_token_stride", "q_out_head_stride", "tokens")]
+                + [("positions", ctypes.c_void_p), ("position_token_stride", ctypes.c_int64),
+                   ("position_axis_stride", ctypes.c_int64), ("turns", ctypes.c_void_p),
+                   ("magnitude", ctypes.c_float)]
+                + [(n, ctypes.c_int32) for n in ("q_heads", "rot_dim", "position_bits", "axes")]
+                + [("axis_pairs", ctypes.c_int32 * 4)] + [(n, ctypes.c_int32) for n in ("layout", "dtype")])
+
+
+class CacheAttentionDesc(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("q", "out", "lse", "mask")]
+                + [(n, ctypes.c_int64) for n in ("q_token_stride", "q_head_stride", "out_token_stride",
+                                                 "out_head_stride", "mask_stride", "tokens")]
+                + [("scale", ctypes.c_float)]
+                + [(n, ctypes.c_int32) for n in ("q_heads", "mask_words", "dtype")])
+
+
 # The descriptors as packed bytes, the form the calls below hand over: the
 # struct's layout, built in a third of the time of a ctypes Structure and its
 # reference (0.2 against 0.6 us; a call's host time is a few microseconds).
@@ -90,6 +128,14 @@ assert struct.calcsize("=QQqqi4x") == ctypes.sizeof(FP8Desc)
 _pack_rmsnorm = struct.Struct("=QQQQqqqqqfi").pack
 _pack_epilogue = struct.Struct("=QQqi4x").pack
 _pack_rope = struct.Struct("=QQqqqqqqQqqQf11i").pack
+_pack_fp8_block = struct.Struct("=QQqqi4x").pack
+_pack_cache = struct.Struct("=QQ6qQqQQQQ7i4x").pack
+_pack_append = struct.Struct("=QQQQ9qQqqQf10i4x").pack
+_pack_attention = struct.Struct("=QQQQ6qf3i").pack
+assert struct.calcsize("=QQqqi4x") == ctypes.sizeof(FP8BlockDesc)
+assert struct.calcsize("=QQ6qQqQQQQ7i4x") == ctypes.sizeof(CacheDesc)
+assert struct.calcsize("=QQQQ9qQqqQf10i4x") == ctypes.sizeof(CacheAppendDesc)
+assert struct.calcsize("=QQQQ6qf3i") == ctypes.sizeof(CacheAttentionDesc)
 assert struct.calcsize("=QQQQqqqqqfi") == ctypes.sizeof(RMSNormDesc)
 assert struct.calcsize("=QQqi4x") == ctypes.sizeof(EpilogueDesc)
 assert struct.calcsize("=QQqqqqqqQqqQf11i") == ctypes.sizeof(RopeDesc)
@@ -145,6 +191,14 @@ def load_library(path: str = LIB_PATH):
             "qlin_rope": (ctypes.c_int, [ctypes.POINTER(RopeDesc), p]),
             "qlin_rope_turns": (ctypes.c_int, [ctypes.c_int32, ctypes.c_double, ctypes.c_int32]
                                 + [ctypes.c_double] * 4 + [p, ctypes.POINTER(ctypes.c_float)]),
+            "qlin_fp8_block_scales": (sz, [i64, i64, ctypes.c_int32]),
+            "qlin_quantize_fp8_block": (ctypes.c_int, [p, ctypes.c_int32, i64, ctypes.POINTER(FP8BlockDesc), p]),
+            "qlin_linear_fp8_block": (ctypes.c_int, [ctypes.POINTER(FP8BlockDesc), ctypes.POINTER(FP8BlockDesc),
+                                                     ctypes.POINTER(EpilogueDesc), p, p]),
+            "qlin_cache_append": (ctypes.c_int, [ctypes.POINTER(CacheDesc), ctypes.POINTER(CacheAppendDesc), p]),
+            "qlin_cache_attention": (ctypes.c_int, [ctypes.POINTER(CacheDesc), ctypes.POINTER(CacheAttentionDesc),
+                                                    p, sz, p]),
+            "qlin_cache_attention_workspace_size": (sz, []),
             "qlin_sync_status": (ctypes.c_int, [p]),
             "qlin_selftest_bounded_wait": (ctypes.c_int, [ctypes.c_uint64, p]),
             "qlin_set_wait_timeout_ns": (None, [ctypes.c_uint64]),
@@ -175,6 +229,10 @@ def load_library(path: str = LIB_PATH):
             "qlin_linear_bf16": [p, i64, p, i64, i64, i64, d, p, p],
             "qlin_linear_fp16": [p, i64, p, i64, i64, i64, d, p, p],
             "qlin_rope": [d, p],
+            "qlin_quantize_fp8_block": [p, ctypes.c_int32, i64, d, p],
+            "qlin_linear_fp8_block": [d, d, d, p, p],
+            "qlin_cache_append": [d, d, p],
+            "qlin_cache_attention": [d, d, p, sz, p],
         }
         lib.packed = types.SimpleNamespace()
         for name, args in packed.items():
@@ -765,6 +823,242 @@ def qlin_rope(x: torch.Tensor, positions: torch.Tensor, plan: RopePlan, out: tor
         positions.data_ptr(), pst[0], pst[1] if len(pst) == 2 else 0,
         turns.data_ptr(), plan.magnitude, D, 2 * turns.numel(), 64 if pdt is torch.int64 else 32,
         axes, *pairs, *(0,) * (4 - axes), layout, 1 if inverse else 0, dt), _stream(stream)), "qlin_rope")
+    return out
+
+
+# ------------------------------------------------------ a serving step ---
+
+@dataclass
+class FP8BlockTensor:
+    """FP8 operand [rows, K] with a scale for each block of block_rows rows (1: activations,
+    128: weights) and 128 elements of K."""
+    codes: torch.Tensor          # uint8 [rows, K]
+    scales: torch.Tensor         # float32 [ceil(K / 128), ceil(rows / block_rows)]
+    rows: int
+    K: int
+    block_rows: int
+
+    def desc(self) -> FP8BlockDesc:
+        return FP8BlockDesc(self.codes.data_ptr(), self.scales.data_ptr(), self.rows, self.K, self.block_rows)
+
+
+def qlin_fp8_block_scales(rows: int, K: int, block_rows: int) -> int:
+    return _library().qlin_fp8_block_scales(rows, K, block_rows)
+
+
+def alloc_fp8_block(rows: int, K: int, block_rows: int = 1, device="cuda", stream=None) -> FP8BlockTensor:
+    if qlin_fp8_block_scales(rows, K, block_rows) == 0:
+        raise ValueError(f"invalid block-scaled FP8 shape [{rows}, {K}], block_rows {block_rows}")
+    return FP8BlockTensor(_empty((rows, K), torch.uint8, device, stream),
+                          _empty(((K + 127) // 128, -(-rows // block_rows)), torch.float32, device, stream),
+                          rows, K, block_rows)
+
+
+def _fp8_block_on(q, name, dev) -> bytes:
+    """The packed descriptor of a block-scaled FP8 operand whose tensors hold what it says,
+    on device `dev`."""
+    codes, scales, rows, K, br = q.codes, q.scales, q.rows, q.K, q.block_rows
+    ss = scales.shape
+    if (codes.dtype is not torch.uint8 or codes.shape != (rows, K) or codes.get_device() != dev
+            or not codes.is_contiguous()):
+        raise ValueError(f"{name}.codes: expected a contiguous uint8 [{rows}, {K}] tensor on cuda:{dev}")
+    if (br != 1 and br != 128) or (scales.dtype is not torch.float32 or len(ss) != 2 or ss[0] != (K + 127) // 128
+                                   or ss[1] != -(-rows // br) or scales.get_device() != dev
+                                   or not scales.is_contiguous()):
+        raise ValueError(f"{name}.scales: expected a contiguous float32 [ceil(K / 128), ceil(rows / block_rows)] "
+                         f"tensor on cuda:{dev}, block_rows 1 or 128")
+    return _pack_fp8_block(codes.data_ptr(), scales.data_ptr(), rows, K, br)
+
+
+def qlin_quantize_fp8_block(x: torch.Tensor, block_rows: int = 1, out: FP8BlockTensor | None = None,
+                            stream=None) -> FP8BlockTensor:
+    """x [rows, K] (bf16 or fp16, rows any multiple of 8 elements apart) as a block-scaled
+    FP8 operand; block_rows as in ``out`` where that is given."""
+    dtype, dev, shape = x.dtype, x.get_device(), x.shape
+    dt = _FLOAT16.get(dtype)
+    if dt is None or len(shape) != 2 or dev < 0:
+        raise ValueError("x: expected a 2-D bf16 or fp16 CUDA tensor")
+    rows, K = shape
+    stride = _rows16(x, "x", dtype, rows, K, dev)
+    if out is None:
+        out = alloc_fp8_block(rows, K, block_rows, x.device, stream)
+    elif out.rows != rows or out.K != K:
+        raise ValueError(f"out: expected an operand [{rows}, {K}]")
+    _check(_library().packed.qlin_quantize_fp8_block(x.data_ptr(), dt, stride, _fp8_block_on(out, "out", dev),
+                                                     _stream(stream)), "qlin_quantize_fp8_block")
+    return out
+
+
+def qlin_linear_fp8_block(A: FP8BlockTensor, W: FP8BlockTensor, bias: torch.Tensor | None = None,
+                          act: int = QLIN_ACT_NONE, residual: torch.Tensor | None = None,
+                          y: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """y = act(A W^T + bias) + residual (bf16, one rounding) of block-scaled FP8 operands, A
+    with block_rows 1 and W with 128.  residual may be y."""
+    M, N, codes = A.rows, W.rows, A.codes
+    dev = codes.get_device()
+    if dev < 0:
+        raise ValueError("A: expected a CUDA operand")
+    ad, wd = _fp8_block_on(A, "A", dev), _fp8_block_on(W, "W", dev)
+    if y is None:
+        y = _empty((M, N), torch.bfloat16, codes.device, stream)
+    yp = _dense16(y, "y", torch.bfloat16, M, N, dev)
+    _check(_library().packed.qlin_linear_fp8_block(ad, wd, _epilogue(bias, act, residual, torch.bfloat16, M, N, dev),
+                                                   yp, _stream(stream)), "qlin_linear_fp8_block")
+    return y
+
+
+_CACHE_FORMATS = {torch.bfloat16: QLIN_CACHE_BF16, torch.float16: QLIN_CACHE_FP16,
+                  torch.float8_e4m3fn: QLIN_CACHE_E4M3}
+
+
+@dataclass
+class PagedCache:
+    """Keys and values in pages, and a step's sequences: token i of sequence b, cached ones
+    first, lies in page page_table[b, i // page_size], slot i % page_size; its new tokens are
+    q_start[b] .. q_start[b + 1] - 1 of the call's."""
+    k: torch.Tensor              # bf16, fp16 or float8_e4m3fn [pages, page_size, heads, head_dim]
+    v: torch.Tensor
+    page_table: torch.Tensor     # int32 [sequences, table_width]
+    cached: torch.Tensor         # int32 [sequences]
+    q_start: torch.Tensor        # int32 [sequences + 1]
+    k_scale: torch.Tensor | None = None   # float32 [1], float8_e4m3fn only
+    v_scale: torch.Tensor | None = None
+
+
+def _cache_on(c, dev):
+    """(the packed descriptor of a cache on device `dev`, heads, head_dim)."""
+    k, v, table, cached, q_start = c.k, c.v, c.page_table, c.cached, c.q_start
+    shape, fmt = k.shape, _CACHE_FORMATS.get(k.dtype)
+    ks, vs = k.stride(), v.stride()
+    if (fmt is None or len(shape) != 4 or v.dtype is not k.dtype or v.shape != shape or k.get_device() != dev
+            or v.get_device() != dev or (shape[3] > 1 and (ks[3] != 1 or vs[3] != 1))):
+        raise ValueError("cache: expected k and v bf16, fp16 or float8_e4m3fn [pages, page_size, heads, head_dim] "
+                         f"on cuda:{dev} with contiguous heads")
+    B, i32 = cached.numel(), torch.int32
+    if cached.dtype is not i32 or cached.dim() != 1 or cached.get_device() != dev or not cached.is_contiguous():
+        raise ValueError(f"cache.cached: expected a contiguous int32 vector on cuda:{dev}")
+    if (q_start.dtype is not i32 or q_start.dim() != 1 or q_start.numel() != B + 1 or q_start.get_device() != dev
+            or not q_start.is_contiguous()):
+        raise ValueError(f"cache.q_start: expected a contiguous int32 [{B + 1}] tensor on cuda:{dev}")
+    ts = table.shape
+    if (table.dtype is not i32 or len(ts) != 2 or ts[0] != B or table.get_device() != dev
+            or (table.stride(1) != 1 and ts[1] > 1)):
+        raise ValueError(f"cache.page_table: expected an int32 [{B}, table_width] tensor on cuda:{dev} with "
+                         "contiguous rows")
+    if fmt == QLIN_CACHE_E4M3:
+        if c.k_scale is None or c.v_scale is None:
+            raise ValueError("cache: an FP8 cache needs k_scale and v_scale")
+        sk, sv = _scalar32(c.k_scale, "cache.k_scale", dev), _scalar32(c.v_scale, "cache.v_scale", dev)
+    else:
+        sk = sv = 0
+    desc = _pack_cache(k.data_ptr(), v.data_ptr(), ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], table.data_ptr(),
+                       table.stride(0) if B > 1 else ts[1], cached.data_ptr(), q_start.data_ptr(), sk, sv, B,
+                       shape[0], shape[1], ts[1], shape[2], shape[3], fmt)
+    return desc, shape[2], shape[3]
+
+
+def _heads16(t, name, dtype, T, H, D, dev):
+    """The strides of a 16-bit [tokens, heads, head_dim] tensor with contiguous heads."""
+    s = t.stride()
+    if t.dtype is not dtype or t.shape != (T, H, D) or t.get_device() != dev or (s[2] != 1 and D > 1):
+        raise ValueError(f"{name}: expected a {dtype} [{T}, {H}, {D}] tensor on cuda:{dev} with contiguous heads")
+    return s[0], s[1]
+
+
+def qlin_cache_append(cache: PagedCache, k: torch.Tensor, v: torch.Tensor, plan: RopePlan | None = None,
+                      positions: torch.Tensor | None = None, q: torch.Tensor | None = None,
+                      q_out: torch.Tensor | None = None, stream=None):
+    """Writes the step's keys (rotated) and values to their slots in the cache and returns q
+    rotated (in q_out, allocated where it is None; None without q).  k, v [tokens, heads,
+    head_dim] and q [tokens, q_heads, head_dim] may be views of a QKV output.  positions: int32
+    or int64 [tokens] or [tokens, axes]; None: each token's number in its sequence.  plan None:
+    nothing turns.  q_out may be q."""
+    dtype, dev, shape = k.dtype, k.get_device(), k.shape
+    dt = _FLOAT16.get(dtype)
+    if dt is None or len(shape) != 3 or dev < 0:
+        raise ValueError("k: expected a bf16 or fp16 [tokens, heads, head_dim] CUDA tensor")
+    desc, H, D = _cache_on(cache, dev)
+    T = shape[0]
+    ks, vs = _heads16(k, "k", dtype, T, H, D, dev), _heads16(v, "v", dtype, T, H, D, dev)
+    qp, qop, Hq, qs, qos = 0, 0, 0, (0, 0), (0, 0)
+    if q is not None:
+        if q.dim() != 3:
+            raise ValueError("q: expected a [tokens, q_heads, head_dim] tensor")
+        Hq = q.shape[1]
+        qs, qp = _heads16(q, "q", dtype, T, Hq, D, dev), q.data_ptr()
+        if q_out is None:
+            q_out = _empty((T, Hq, D), dtype, q.device, stream)
+        qos, qop = _heads16(q_out, "q_out", dtype, T, Hq, D, dev), q_out.data_ptr()
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    pp, pst, bits, tp, mag, R, pairs, layout = 0, (0, 0), 32, 0, 1.0, 0, (), 0
+    if plan is None:
+        if positions is not None:
+            raise ValueError("positions without a plan")
+    else:
+        turns, pairs, layout = plan.turns, plan.axis_pairs, _LAYOUTS.get(plan.layout)
+        if turns.dtype is not torch.int64 or turns.dim() != 1 or not turns.is_contiguous() or turns.get_device() != dev:
+            raise ValueError(f"plan.turns: expected a contiguous int64 vector on cuda:{dev}")
+        if not 1 <= len(pairs) <= 4 or layout is None:
+            raise ValueError("plan: one to four axes, layout 'interleaved' or 'half'")
+        tp, mag, R = turns.data_ptr(), plan.magnitude, 2 * turns.numel()
+        if positions is not None:
+            pdt, ps = positions.dtype, positions.shape
+            if ((pdt is not torch.int32 and pdt is not torch.int64) or positions.get_device() != dev
+                    or not (ps == (T, len(pairs)) or (len(pairs) == 1 and ps == (T,)))):
+                raise ValueError(f"positions: expected int32 or int64 [{T}, {len(pairs)}] on cuda:{dev}")
+            st = positions.stride()
+            pp, pst, bits = positions.data_ptr(), (st[0], st[1] if len(st) == 2 else 0), 64 if pdt is torch.int64 else 32
+    _check(_library().packed.qlin_cache_append(desc, _pack_append(
+        k.data_ptr(), v.data_ptr(), qp, qop, *ks, *vs, *qs, *qos, T, pp, *pst, tp, mag, Hq, R, bits, len(pairs),
+        *pairs, *(0,) * (4 - len(pairs)), layout, dt), _stream(stream)), "qlin_cache_append")
+    return q_out
+
+
+def qlin_cache_attention_workspace_size() -> int:
+    return _library().qlin_cache_attention_workspace_size()
+
+
+def alloc_cache_attention_workspace(device="cuda") -> torch.Tensor:
+    return torch.zeros(qlin_cache_attention_workspace_size(), dtype=torch.uint8, device=device)
+
+
+def qlin_cache_attention(cache: PagedCache, q: torch.Tensor, scale: float, mask: torch.Tensor | None = None,
+                         out: torch.Tensor | None = None, lse: torch.Tensor | None = None,
+                         workspace: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """Attention of the step's tokens q [tokens, q_heads, head_dim] over their sequences' keys
+    in the cache (the new ones appended before).  mask: int64 words (uint64's bits) [tokens,
+    words], bit i of a token's row saying whether it sees its sequence's new token i; None:
+    those up to itself.  lse: float32 [tokens, q_heads], written where it is given.  out may
+    be q.  Calls that overlap on the GPU must not share a workspace."""
+    dtype, dev, shape = q.dtype, q.get_device(), q.shape
+    dt = _FLOAT16.get(dtype)
+    if dt is None or len(shape) != 3 or dev < 0:
+        raise ValueError("q: expected a bf16 or fp16 [tokens, q_heads, head_dim] CUDA tensor")
+    desc, H, D = _cache_on(cache, dev)
+    T, Hq = shape[0], shape[1]
+    qs = _heads16(q, "q", dtype, T, Hq, D, dev)
+    if out is None:
+        out = _empty((T, Hq, D), dtype, q.device, stream)
+    os_ = _heads16(out, "out", dtype, T, Hq, D, dev)
+    mp, ms, words, lp = 0, 0, 0, 0
+    if mask is not None:
+        if (mask.dtype is not torch.int64 or mask.dim() != 2 or mask.shape[0] != T or mask.get_device() != dev
+                or (mask.stride(1) != 1 and mask.shape[1] > 1)):
+            raise ValueError(f"mask: expected an int64 [{T}, words] tensor on cuda:{dev} with contiguous rows")
+        mp, ms, words = mask.data_ptr(), mask.stride(0), mask.shape[1]
+    if lse is not None:
+        if (lse.dtype is not torch.float32 or lse.shape != (T, Hq) or lse.get_device() != dev
+                or not lse.is_contiguous()):
+            raise ValueError(f"lse: expected a contiguous float32 [{T}, {Hq}] tensor on cuda:{dev}")
+        lp = lse.data_ptr()
+    if workspace is None:
+        workspace = _empty(qlin_cache_attention_workspace_size(), torch.uint8, q.device, stream, torch.zeros)
+    elif workspace.get_device() != dev or not workspace.is_contiguous():
+        raise ValueError(f"workspace: expected a contiguous tensor on cuda:{dev}")
+    _check(_library().packed.qlin_cache_attention(desc, _pack_attention(
+        q.data_ptr(), out.data_ptr(), lp, mp, *qs, *os_, ms, T, scale, Hq, words, dt), workspace.data_ptr(),
+        workspace.numel() * workspace.element_size(), _stream(stream)), "qlin_cache_attention")
     return out
 
 
