@@ -17,7 +17,7 @@ LIB_DIR = os.path.join(HERE, "_lib")
 LIB = os.path.join(LIB_DIR, "libqlin.so")
 SOURCES = ["qlin_api.cu", "qlin_quant.cu", "qlin_gemm.cu", "qlin_few.cu", "qlin_norm.cu",
            "qlin_rope.cu", "qlin_quant_block.cu", "qlin_gemm_block.cu",
-           "qlin_append.cu", "qlin_attention.cu", "qlin_attention_bf16.cu",
+           "qlin_append.cu", "qlin_attention.cu", "qlin_attention_tiles.cu", "qlin_attention_bf16.cu",
            "qlin_attention_fp16.cu", "qlin_attention_e4m3.cu"]
 # the rate probes of the measurement harness and the probes of the quantizers'
 # grid-wide wait: a library of its own

@@ -722,7 +722,7 @@ qlin_status qlin_cache_attention(const qlin_cache_t* c, const qlin_cache_attenti
   unsigned* status;
   Device dev;
   QLIN_TRY(device_state(&status, &dev));
-  QLIN_CUDA(launch_cache_attention(*c, *a, workspace, static_cast<cudaStream_t>(stream), dev, status));
+  QLIN_CUDA(launch_cache_attention(*c, *a, workspace, static_cast<cudaStream_t>(stream), dev, status, timeout()));
   return QLIN_OK;
 }
 

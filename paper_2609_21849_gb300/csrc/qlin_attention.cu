@@ -4,7 +4,7 @@
 namespace qlin {
 
 cudaError_t launch_cache_attention(const qlin_cache_t& c, const qlin_cache_attention_t& a, void* workspace,
-                                   cudaStream_t s, Device dev, unsigned* err) {
+                                   cudaStream_t s, Device dev, unsigned* err, uint64_t timeout_ns) {
   const int es = c.format == QLIN_CACHE_E4M3 ? 1 : 2;
   AttnParams p{};
   p.q = static_cast<const uint16_t*>(a.q);
@@ -44,6 +44,9 @@ cudaError_t launch_cache_attention(const qlin_cache_t& c, const qlin_cache_atten
   p.fp16 = a.dtype == QLIN_FP16 ? 1 : 0;
   p.counts = static_cast<unsigned*>(workspace);
   p.err = err;
+  // more rows per sequence and KV head, on average, than the mma.sync kernel shares a read among
+  if (c.format != QLIN_CACHE_E4M3 && p.tokens * p.group > (int64_t)32 * p.sequences && attention_tiles_fit(p))
+    return launch_attention_tiles(p, c.format == QLIN_CACHE_FP16, timeout_ns, s, dev);
   return c.format == QLIN_CACHE_E4M3   ? launch_attention_e4m3(p, s, dev)
          : c.format == QLIN_CACHE_FP16 ? launch_attention_fp16(p, s, dev)
                                        : launch_attention_bf16(p, s, dev);

@@ -1,0 +1,170 @@
+// What the attention kernels share: the split of the work among CTAs, masks, and the join of
+// what CTAs leave unfinished.
+#pragma once
+
+#include "qlin_attention.h"
+
+namespace qlin {
+
+namespace {
+
+// A place in the work: tile `tile` of the item (b, h, rt).
+struct Cursor {
+  CacheSeq s;
+  int b, h, rt, tile, tiles, row_tiles;
+};
+
+template <int kRows, int kTile>
+__device__ __forceinline__ CacheSeq read_seq(const AttnParams& p, int b) {
+  return cache_seq(p.q_start[b], p.q_start[b + 1], p.cached[b], p.tokens, p.page_size, p.table_width);
+}
+
+template <int kRows, int kTile>
+__device__ __forceinline__ void open_seq(const AttnParams& p, Cursor& c) {
+  c.s = read_seq<kRows, kTile>(p, c.b);
+  c.tiles = (int)((c.s.keys + kTile - 1) / kTile);
+  c.row_tiles = (int)(((int64_t)c.s.fresh * p.group + kRows - 1) / kRows);
+}
+
+// The next tile; past the last sequence the cursor stays at its end.
+template <int kRows, int kTile>
+__device__ __forceinline__ void advance(const AttnParams& p, Cursor& c) {
+  if (++c.tile < c.tiles) return;
+  c.tile = 0;
+  if (++c.rt < c.row_tiles) return;
+  c.rt = 0;
+  if (++c.h < p.heads) return;
+  c.h = 0;
+  while (++c.b < p.sequences) {
+    open_seq<kRows, kTile>(p, c);
+    if (c.s.fresh > 0 && c.s.keys > 0) return;
+  }
+}
+
+template <int kRows, int kTile>
+__device__ __forceinline__ int64_t seq_units(const AttnParams& p, const CacheSeq& s) {
+  return ((int64_t)s.fresh * p.group + kRows - 1) / kRows * p.heads * ((s.keys + kTile - 1) / kTile);
+}
+
+// The CTA's run of tiles and the cursor at its begin; the same in all threads.
+struct Run {
+  int64_t total, begin, end;
+  int ctas;
+};
+
+template <int kRows, int kTile, int kThreads>
+__device__ __forceinline__ Run find_run(const AttnParams& p, Cursor& c) {
+  __shared__ int64_t warp_sum[kThreads / 32];
+  __shared__ int64_t found_at;
+  __shared__ int found_b;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  Run r{0, 0, 0, 1};
+  int64_t mine = 0, first = 0;
+  bool bad = false;
+  for (int b = threadIdx.x; b < p.sequences; b += kThreads) {
+    const CacheSeq s = read_seq<kRows, kTile>(p, b);
+    bad |= s.bad;
+    const int64_t u = seq_units<kRows, kTile>(p, s);
+    if (b < kThreads) first = u;
+    mine += u;
+  }
+  if (bad && blockIdx.x == 0) atomicExch(p.err, kErrInvalid);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xFFFFFFFFu, mine, o);
+  if (lane == 0) warp_sum[warp] = mine;
+  __syncthreads();
+  for (int w = 0; w < kThreads / 32; ++w) r.total += warp_sum[w];
+  if (r.total == 0) return r;
+  r.ctas = (int)split_ctas(r.total, gridDim.x, p.least);
+  if ((int)blockIdx.x >= r.ctas) return r;
+  r.begin = split_begin(blockIdx.x, r.total, r.ctas);
+  r.end = split_begin(blockIdx.x + 1, r.total, r.ctas);
+  int64_t run = 0;
+  for (int b0 = 0; b0 < p.sequences; b0 += kThreads) {
+    const int b = b0 + threadIdx.x;
+    int64_t u = first;
+    if (b0 > 0) u = b < p.sequences ? seq_units<kRows, kTile>(p, read_seq<kRows, kTile>(p, b)) : 0;
+    int64_t incl = u;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t n = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+      if (lane >= o) incl += n;
+    }
+    __syncthreads();   // warp_sum's last readers
+    if (lane == 31) warp_sum[warp] = incl;
+    __syncthreads();
+    int64_t base = run;
+    for (int w = 0; w < kThreads / 32; ++w) {
+      if (w < warp) base += warp_sum[w];
+      run += warp_sum[w];
+    }
+    if (base + incl - u <= r.begin && r.begin < base + incl) {
+      found_b = b;
+      found_at = base + incl - u;
+    }
+    if (run > r.begin) break;
+  }
+  __syncthreads();
+  c.b = found_b;
+  open_seq<kRows, kTile>(p, c);
+  int64_t at = r.begin - found_at;
+  c.tile = (int)(at % c.tiles);
+  at /= c.tiles;
+  c.rt = (int)(at % c.row_tiles);
+  c.h = (int)(at / c.row_tiles);
+  return r;
+}
+
+// Whether new token t of a sequence (number `token` of the call) sees new token i.
+__device__ __forceinline__ bool sees(const AttnParams& p, int64_t token, int t, int64_t i) {
+  if (p.mask == nullptr) return i <= t;
+  const int64_t w = i >> 6;
+  return w < p.mask_words && ((p.mask[token * p.mask_token + w] >> (i & 63)) & 1u) != 0u;
+}
+
+__device__ __forceinline__ void store_out4(const AttnParams& p, int64_t token, int head, int d, float4 v) {
+  uint16_t* const y = p.out + token * p.out_token + head * p.out_head + d;
+  const uint2 w = p.fp16 ? make_uint2(pack_f16x2(v.x, v.y), pack_f16x2(v.z, v.w))
+                         : make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
+  *reinterpret_cast<uint2*>(y) = w;
+}
+
+__device__ __forceinline__ float log_sum(float m, float l) {   // m in powers of two
+  return l > 0.0f || l != l ? fmaf(m, 0.693147181f, logf(l)) : -INFINITY;
+}
+
+// The rows of an item whose parts CTAs first..last left in the workspace, joined in order.
+template <int kRows, int kD, int kThreads>
+__device__ __forceinline__ void join_parts(const AttnParams& p, const Cursor& c, int first, int last, float v_scale,
+                                           int thread) {
+  const int rows = (int)min((int64_t)kRows, (int64_t)c.s.fresh * p.group - (int64_t)c.rt * kRows);
+  for (int i = thread; i < rows * (p.head_dim / 4); i += kThreads) {
+    const int row = i / (p.head_dim / 4), d = i % (p.head_dim / 4) * 4;
+    float m = -INFINITY;
+    for (int q = first; q <= last; ++q) {
+      const int64_t at = (int64_t)(2 * q + (q == first ? 1 : 0)) * kRows + row;
+      m = fmaxf(m, __ldcg(&p.part_ml[at]).x);
+    }
+    const float ms = m == -INFINITY ? 0.0f : m;
+    float l = 0.0f;
+    float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (int q = first; q <= last; ++q) {
+      const int64_t at = (int64_t)(2 * q + (q == first ? 1 : 0)) * kRows + row;
+      const float2 ml = __ldcg(&p.part_ml[at]);
+      const float4 v = __ldcg(reinterpret_cast<const float4*>(p.part + at * kD + d));
+      const float f = exp2_fast(ml.x - ms);
+      l = fmaf(ml.y, f, l);
+      o = make_float4(fmaf(v.x, f, o.x), fmaf(v.y, f, o.y), fmaf(v.z, f, o.z), fmaf(v.w, f, o.w));
+    }
+    const int64_t r = (int64_t)c.rt * kRows + row;
+    const int64_t token = c.s.first + r / p.group;
+    const int head = c.h * p.group + (int)(r % p.group);
+    const float inv = l == 0.0f ? 0.0f : v_scale / l;
+    store_out4(p, token, head, d, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
+    if (p.lse != nullptr && d == 0) p.lse[token * p.lse_token + head] = log_sum(m, l);
+  }
+}
+
+}  // namespace
+
+}  // namespace qlin

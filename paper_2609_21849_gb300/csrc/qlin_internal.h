@@ -87,7 +87,7 @@ cudaError_t launch_quant_fp8_block(const void* x, int64_t x_stride, bool fp16, c
 cudaError_t launch_cache_append(const qlin_cache_t& c, const qlin_cache_append_t& a, cudaStream_t s, Device dev,
                                 unsigned* err);
 cudaError_t launch_cache_attention(const qlin_cache_t& c, const qlin_cache_attention_t& a, void* workspace,
-                                   cudaStream_t s, Device dev, unsigned* err);
+                                   cudaStream_t s, Device dev, unsigned* err, uint64_t timeout_ns);
 
 // ---- GEMMs (qlin_gemm.cu) ----
 struct GemmArgs {
@@ -139,6 +139,9 @@ cudaError_t launch_wait_selftest(uint64_t timeout_ns, cudaStream_t s, unsigned* 
 CUresult encode_tensor_map_out_bf16(CUtensorMap* map, void* base, uint64_t cols, uint64_t rows,
                                     bool fp16 = false);
 
+// 16-bit elements, four dimensions (innermost first, strides of the others in bytes), 128-byte swizzle.
+CUresult encode_tensor_map_4d16(CUtensorMap* map, const void* base, bool fp16, const uint64_t (&dims)[4],
+                                const uint64_t (&strides)[3], const uint32_t (&box)[4]);
 // FP8 codes [rows, k_bytes]: 128-byte x box_rows boxes, 128-byte swizzle.
 CUresult encode_tensor_map_codes(CUtensorMap* map, const void* base, uint64_t k_bytes, uint64_t rows,
                                  uint32_t box_rows);
