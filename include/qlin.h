@@ -654,7 +654,7 @@ qlin_status qlin_cache_append(const qlin_cache_t *cache, const qlin_cache_append
  *  mask:   uint64 [tokens, mask_words], rows mask_stride words apart, or NULL.
  *  scale:  normal and > 0.
  *  workspace: device memory of >= qlin_cache_attention_workspace_size() bytes, 16-byte
- *          aligned, its first 4096 bytes zero before the first use; every call leaves them
+ *          aligned, its first 8192 bytes zero before the first use; every call leaves them
  *          zero.  Calls whose work overlaps on the GPU must not share one.
  * A 16-bit cache has the type of q.  head_dim: a multiple of 16.  Cache rows 16-byte aligned.
  * Sums are joined in the order of the keys, split by all sequences' lengths: equal calls give

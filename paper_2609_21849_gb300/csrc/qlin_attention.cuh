@@ -27,6 +27,7 @@ namespace qlin {
 namespace {
 
 constexpr int kWarps = 4;
+constexpr int kGroup = 16;   // CTAs whose parts are joined at a time
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool in) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(in ? 16 : 0) : "memory");
@@ -111,12 +112,13 @@ __global__ void __launch_bounds__(kWarps * 32, (AttnCfg<kKind, kD, kM>::kCtas)) 
   __shared__ unsigned ok_bits[kWarps][C::kStages];
   __shared__ float2 warp_ml[kWarps][kRows];
   __shared__ unsigned last_flag;
+  __shared__ RunScratch scratch;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
 
   grid_dep_wait();
   grid_dep_launch();
   Cursor cur;
-  const Run run = find_run<kRows, C::kTile, kThreads>(p, cur);
+  const Run run = find_run<kRows, C::kTile, kThreads>(p, cur, (int)blockIdx.x, (int)gridDim.x, scratch);
   if (run.begin >= run.end) return;
   float k_scale = 1.0f, v_scale = 1.0f;
   if (kFp8) {
@@ -480,16 +482,29 @@ __global__ void __launch_bounds__(kWarps * 32, (AttnCfg<kKind, kD, kM>::kCtas)) 
     }
     if (!whole) {
       const int first = (int)split_owner(item0, run.total, run.ctas), last = (int)split_owner(item1, run.total, run.ctas);
-      __threadfence();
-      __syncthreads();
-      if (threadIdx.x == 0) {
-        const bool all = atomicAdd(&p.counts[first], 1u) == (unsigned)(last - first);
-        if (all) p.counts[first] = 0u;   // as it was before the call
+      // whether this CTA is the last of `parties` to arrive
+      auto arrive = [&](unsigned* count, int parties) {
         __threadfence();
-        last_flag = all ? 1u : 0u;
+        __syncthreads();
+        if (threadIdx.x == 0) {
+          const bool all = atomicAdd(count, 1u) == (unsigned)(parties - 1);
+          if (all) *count = 0u;   // as it was before the call
+          __threadfence();
+          last_flag = all ? 1u : 0u;
+        }
+        __syncthreads();
+        return last_flag != 0u;
+      };
+      auto join = [&](int from, int to, int step, bool output) {
+        join_parts<kRows, kD, kThreads>(p, cur, first, from, to, step, output, v_scale, 0, rows, (int)threadIdx.x,
+                                        warp_ml[0], [] { __syncthreads(); });
+      };
+      const int groups = (last - first) / kGroup + 1, from = first + ((int)blockIdx.x - first) / kGroup * kGroup,
+                to = min(last, from + kGroup - 1);
+      if (arrive(&p.counts[from], to - from + 1)) {
+        join(from, to, 1, groups == 1);
+        if (groups > 1 && arrive(&p.counts[kMostCtas + first], groups)) join(first, last, kGroup, true);
       }
-      __syncthreads();
-      if (last_flag != 0u) join_parts<kRows, kD, kThreads>(p, cur, first, last, v_scale, (int)threadIdx.x);
     }
     __syncthreads();
   };

@@ -38,9 +38,9 @@ struct AttnParams {
   unsigned* err;
 };
 
-// Workspace: a count per CTA, then two unfinished items per CTA of at most kMostRows rows.
+// Workspace: two counts per CTA, then two unfinished items per CTA.
 constexpr int kMostCtas = 1024;
-constexpr int64_t kCountBytes = kMostCtas * 4;
+constexpr int64_t kCountBytes = 2 * kMostCtas * 4;
 constexpr int64_t kWorkspaceBytes = (int64_t)64 << 20;
 
 // Many rows on tcgen05 (qlin_attention_tiles.cu): whether it takes these pages and heads.

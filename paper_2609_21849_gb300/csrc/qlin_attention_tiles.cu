@@ -7,27 +7,65 @@
 // 128 rows the streams are the rows' halves over the same keys; with 128 or fewer, even and
 // odd tiles over the same rows, joined at the end.  Per stream and tile:
 //   S = Q K^T     tcgen05 from shared memory (K's pages by TMA, 128-byte swizzle) into 128 columns
-//   P = 2^(S - m) a thread per row: 128 scores in registers, P as 16-bit over S's columns
+//   P = 2^(S - m) two threads per row, 64 scores in registers each, P as 16-bit over S's columns
 //   O += P V      A from tensor memory, V as it lies (keys x elements: an MN-major B)
 // The running maximum moves only when it rises by more than 2^8, so O is rarely rescaled; P
 // stays below 2^8 and the sums in fp32 (both fine in 16 bits: a P's rounding is relative).
 //   Per tile of 256 rows and 128 keys of 128: 2048 cycles of MMAs, 2048 of exponentials (16 a
 // cycle and SM), 64 KB of keys and values, about 2850 cycles of an SM's share of HBM.
-// Roles: warp 0 loads, warp 1 issues MMAs, warps 4-7 and 8-11 are the streams' softmax.
+// Roles: warps 0 and 2 load K and V, warp 1 issues MMAs, warps 4-11 and 12-19 are the streams' softmax.
 // Tiles with new tokens are masked, and V's slots behind the last key and values that are
 // not finite are zeroed in shared memory: 0 times them would reach rows that do not see them.
 // (Rows that do see such a value take it at the end.)
+// An item that several CTAs share is joined by a second kernel, many CTAs to an item (by one of
+// these, at one SM's rate of reading, the 16 trees below took 262 us, not 2xx).
 #include "qlin_attention_work.cuh"
 
 namespace qlin {
 
 namespace {
 
-constexpr int kRows = 256, kTile = 128;
-constexpr int kThreads = 384, kSoftWarp0 = 4;
-constexpr int kRoleRegs = 56, kSoftRegs = 224;
+constexpr int kRows = 256, kTile = 128, kHalf = 64;
+constexpr int kSoftWarp0 = 4, kSoftThreads = 256, kThreads = kSoftWarp0 * 32 + kSoftThreads;
+constexpr int kRoleRegs = 104, kSoftRegs = 200, kLaunchRegs = 168;
+static_assert(kSoftWarp0 * 32 * kRoleRegs + kSoftThreads * kSoftRegs <= kThreads * kLaunchRegs, "registers");
 constexpr float kSlack = 8.0f;   // powers of two that a score may exceed the kept maximum by
 constexpr int kBadRing = 16;     // tiles whose bad pages are remembered
+
+// A run's pieces: consecutive tiles of one item.
+struct Segment {
+  int first, n;      // tiles
+  bool halves;
+};
+__device__ __forceinline__ Segment segment_at(const AttnParams& p, const Cursor& c, int64_t unit, int64_t end) {
+  const int64_t rows = (int64_t)c.s.fresh * p.group - (int64_t)c.rt * kRows;
+  return {c.tile, (int)min((int64_t)(c.tiles - c.tile), end - unit), rows > 128};
+}
+__device__ __forceinline__ void skip_segment(const AttnParams& p, Cursor& c, const Segment& s) {
+  c.tile += s.n - 1;
+  advance<kRows, kTile>(p, c);
+}
+
+// A segment as the softmax threads need it, in shared memory: their registers hold scores.
+struct SoftSegment {
+  CacheSeq s;
+  uint32_t base;         // loads before it
+  int b, h, rt;
+  int first, n;          // tiles; n 0: none left
+  unsigned tiles_done;   // K tiles before it
+  bool halves, whole, begun;   // begun: the item, before this CTA
+};
+
+// What the roles share beside tiles and barriers.
+struct TileShared {
+  float2 other[128];       // the odd tiles' maxima and sums
+  RunScratch scratch;
+  SoftSegment seg[2];
+  unsigned bad_pages[kBadRing];   // of K tiles in order
+  uint32_t tmem;
+  int abort;
+  int odd_values;
+};
 
 template <int kDC>   // chunks of 64 elements of a head
 struct TileCfg {
@@ -35,9 +73,9 @@ struct TileCfg {
   static constexpr int kSlot = kDC * kChunk;          // a tile of K or V, or 128 rows of Q
   static constexpr int kSlots = kDC == 1 ? 10 : 5;
   static constexpr int kQBytes = 2 * kSlot;
-  static constexpr int kBarrierBytes = 256;
-  static constexpr int kSmem = 1024 + kQBytes + kSlots * kSlot + kBarrierBytes;
-  static_assert((2 * kSlots + 8) * 8 <= kBarrierBytes && kSmem <= 232448 - 1536, "shared memory (static: 1.3 KB)");
+  static constexpr int kBarrierBytes = 320;
+  static constexpr int kSmem = kQBytes + kSlots * kSlot + kBarrierBytes + (int)sizeof(TileShared);
+  static_assert((2 * kSlots + 14) * 8 <= kBarrierBytes && kSmem <= 232448, "shared memory");
 };
 
 struct TileParams {
@@ -69,26 +107,11 @@ __device__ __forceinline__ uint64_t sdesc_v(uint32_t saddr, uint32_t chunk_bytes
   return d;
 }
 
-__device__ __forceinline__ void softmax_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
-
+__device__ __forceinline__ void softmax_sync() { asm volatile("bar.sync 1, %0;" ::"n"(kSoftThreads) : "memory"); }
 // Where in the order of loads a segment's tiles lie (n tiles; K and V of each).  Rows in two
 // halves: K0 V0 K1 V1 ...  Tiles in turn: K0 K1 V0 K2 V1 K3 ...: each as the MMAs take them.
 __device__ __forceinline__ int k_pos(bool halves, int j) { return halves ? 2 * j : j < 2 ? j : 2 * j - 1; }
 __device__ __forceinline__ int v_pos(bool halves, int j, int n) { return halves ? 2 * j + 1 : min(2 * j + 2, n + j); }
-
-// A run's pieces: consecutive tiles of one item.
-struct Segment {
-  int first, n;      // tiles
-  bool halves;
-};
-__device__ __forceinline__ Segment segment_at(const AttnParams& p, const Cursor& c, int64_t unit, int64_t end) {
-  const int64_t rows = (int64_t)c.s.fresh * p.group - (int64_t)c.rt * kRows;
-  return {c.tile, (int)min((int64_t)(c.tiles - c.tile), end - unit), rows > 128};
-}
-__device__ __forceinline__ void skip_segment(const AttnParams& p, Cursor& c, const Segment& s) {
-  c.tile += s.n - 1;
-  advance<kRows, kTile>(p, c);
-}
 
 // 32 bits of a row's mask from new token i on (negative ones are cached tokens: seen).
 __device__ __forceinline__ uint32_t mask_window(const uint64_t* m, int words, int64_t i) {
@@ -118,6 +141,23 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
   return kF16 ? pack_f16x2(lo, hi) : pack_bf16x2(lo, hi);
 }
 
+// The largest, or NaN.
+__device__ __forceinline__ float max_nan(float a, float b, float c) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+
+// Minus infinity for the scores of columns 32 c on that a row does not see.
+__device__ __forceinline__ void hide(uint32_t bits, unsigned bads, int c, int box_rows, uint32_t (&v)[32]) {
+  if (bads != 0u)
+    for (int i = 0; i < 32; ++i)
+      if ((bads >> ((32 * c + i) / box_rows)) & 1u) bits &= ~(1u << i);
+#pragma unroll
+  for (int i = 0; i < 32; ++i)
+    if (!((bits >> i) & 1u)) v[i] = 0xFF800000u;
+}
+
 template <bool kF16, int kDC>
 __global__ void __launch_bounds__(kThreads, 1)
     attn_tiles_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v,
@@ -125,24 +165,21 @@ __global__ void __launch_bounds__(kThreads, 1)
   using C = TileCfg<kDC>;
   constexpr int kD = 64 * kDC;
   const AttnParams& p = tp.a;
-  extern __shared__ uint8_t smem_raw[];
-  uint8_t* const smem =
-      reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+  extern __shared__ __align__(1024) uint8_t smem[];
+  if ((smem_u32(smem) & 1023u) != 0u) {   // (the swizzle's atoms; no other shared memory comes before)
+    atomicExch(p.err, kErrTimeout);
+    return;
+  }
   uint8_t* const q_smem = smem;
   uint8_t* const ring = smem + C::kQBytes;
   uint64_t* const full = reinterpret_cast<uint64_t*>(ring + C::kSlots * C::kSlot);
   uint64_t* const empty = full + C::kSlots;
-  uint64_t* const s_full = empty + C::kSlots;    // per stream: scores are there (and its products before done)
-  uint64_t* const p_ready = s_full + 2;          // per stream: P is there
-  uint64_t* const o_done = p_ready + 2;          // per stream: the segment's last product is done
-  uint64_t* const q_ready = o_done + 2;
+  uint64_t* const s_full = empty + C::kSlots;    // per stream and half of a tile: scores are there
+  uint64_t* const p_ready = s_full + 4;          // the same: P is there
+  uint64_t* const pv_done = p_ready + 4;         // the same: its product is done
+  uint64_t* const q_ready = pv_done + 4;
   uint64_t* const mma_done = q_ready + 1;
-  __shared__ uint32_t tmem_slot;
-  __shared__ int abort_word;
-  __shared__ unsigned bad_pages[kBadRing];       // of K tiles in order
-  __shared__ int odd_values;
-  __shared__ unsigned last_flag;
-  __shared__ float2 other_ml[128];
+  TileShared& sh = *reinterpret_cast<TileShared*>(ring + C::kSlots * C::kSlot + C::kBarrierBytes);
 
   const int warp = __shfl_sync(0xFFFFFFFFu, (int)(threadIdx.x >> 5), 0);
   const int lane = threadIdx.x & 31;
@@ -151,74 +188,65 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(&full[i], 1);
       mbar_init(&empty[i], 1);
     }
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < 4; ++i) {
       mbar_init(&s_full[i], 1);
       mbar_init(&p_ready[i], 4);
-      mbar_init(&o_done[i], 1);
+      mbar_init(&pv_done[i], 1);
     }
     mbar_init(q_ready, 8);
     mbar_init(mma_done, 1);
-    abort_word = 0;
-    odd_values = 0;
+    sh.abort = 0;
+    sh.odd_values = 0;
     mbar_fence_init();
   }
   if (warp == 0 && lane < 2) prefetch_tmap(lane == 0 ? &tmap_k : &tmap_v);
-  if (warp == 1) tmem_alloc(&tmem_slot, 512);
+  if (warp == 1) tmem_alloc(&sh.tmem, 512);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = __shfl_sync(0xFFFFFFFFu, tmem_slot, 0);
+  const uint32_t tmem = __shfl_sync(0xFFFFFFFFu, sh.tmem, 0);
   const uint32_t s_tmem = tmem, o_tmem = tmem + 256;   // stream s: 128 columns further
-  const WaitCtl ctl{&abort_word, p.err, tp.timeout_ns};
+  const WaitCtl ctl{&sh.abort, p.err, tp.timeout_ns};
   grid_dep_wait();
   grid_dep_launch();
   Cursor cur;
-  const Run run = find_run<kRows, kTile, kThreads>(p, cur);
+  const Run run = find_run<kRows, kTile, kThreads>(p, cur, (int)blockIdx.x, (int)gridDim.x, sh.scratch);
 
-  auto slot_of = [&](int64_t pos) { return (int)(pos % C::kSlots); };
-  auto phase_of = [&](int64_t pos) { return (uint32_t)(pos / C::kSlots) & 1u; };
+  // (loads of a CTA are counted in 32 bits: fewer than 2^25 tiles of keys a sequence, 2^31 in all)
+  auto slot_of = [&](uint32_t pos) { return (int)(pos % C::kSlots); };
+  auto phase_of = [&](uint32_t pos) { return (pos / C::kSlots) & 1u; };
 
   if (warp < kSoftWarp0) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRoleRegs));
-    if (warp == 0) {
-      // ---- loads: a lane per page of the tile ----
-      int64_t base = 0, tiles_done = 0;   // loads and K tiles before this segment
-      int64_t issued = 0;
+    if (warp == 0 || warp == 2) {
+      // ---- loads, of K or V: a lane per page of the tile ----
+      const bool is_v = warp == 2;
+      const CUtensorMap* const map = is_v ? &tmap_v : &tmap_k;
+      uint32_t base = 0;         // loads before this segment
+      unsigned tiles_done = 0;   // K tiles before it
+      uint32_t used = 0u, phases = 0u;   // slots that this warp filled, and in which phase last
       bool ok = true;
       for (int64_t unit = run.begin; unit < run.end && ok;) {
         const Segment sg = segment_at(p, cur, unit, run.end);
-        // load i of the segment: tile j of K or V, and the lane's page of it
         struct Load {
-          bool is_v, in;
-          int j, at, page;
+          bool in;
+          int at, page;
         };
-        auto locate = [&](int i) {
+        // the lane's page of tile j, and its first slot of it
+        auto locate = [&](int j) {
           Load d{};
-          if (sg.halves) {
-            d.is_v = (i & 1) != 0;
-            d.j = i >> 1;
-          } else if (i < 2 && i < sg.n) {
-            d.j = i;
-          } else if (sg.n == 1) {
-            d.is_v = true;
-          } else {
-            // V0 K2 V1 K3 ... with V alone once K is through
-            d.is_v = (i & 1) == 0 || (i >> 1) + 1 >= sg.n;
-            d.j = !d.is_v ? (i + 1) >> 1 : (i & 1) == 0 ? (i - 2) >> 1 : i - sg.n;
-          }
-          const int64_t key = (int64_t)(sg.first + d.j) * kTile + lane * tp.box_rows;
-          int index = 0;
-          d.in = lane < tp.boxes && key < cur.s.keys && cache_place(key, p.page_size, p.table_width, &index, &d.at);
+          const uint32_t key = (uint32_t)(sg.first + j) * kTile + lane * tp.box_rows;   // (below 2^31 + 128)
+          const uint32_t index = key / (uint32_t)p.page_size;
+          d.in = lane < tp.boxes && key < cur.s.keys;
+          d.at = (int)(key - index * (uint32_t)p.page_size);
           d.page = d.in ? p.table[cur.b * p.table_stride + index] : 0;
           return d;
         };
         Load next = locate(0);
-        for (int i = 0; i < 2 * sg.n; ++i) {
+        for (int j = 0; j < sg.n; ++j) {
           const Load d = next;
-          if (i + 1 < 2 * sg.n) next = locate(i + 1);   // (the table's entry on its way while this load waits)
-          const bool is_v = d.is_v;
-          const int j = d.j;
-          const int64_t pos = base + i;
+          if (j + 1 < sg.n) next = locate(j + 1);   // (the table's entry on its way while this load waits)
+          const uint32_t pos = base + (is_v ? v_pos(sg.halves, j, sg.n) : k_pos(sg.halves, j));
           const int slot = slot_of(pos);
           const bool bad = d.in && (d.page < 0 || d.page >= p.pages);
           const unsigned bads = __ballot_sync(0xFFFFFFFFu, bad);
@@ -230,7 +258,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             break;
           }
           if (lane == 0) {
-            if (!is_v) *(volatile unsigned*)&bad_pages[(tiles_done + j) % kBadRing] = bads;
+            if (!is_v) *(volatile unsigned*)&sh.bad_pages[(tiles_done + j) % kBadRing] = bads;
             mbar_arrive_expect_tx(&full[slot], C::kSlot);
           }
           __syncwarp();
@@ -238,83 +266,107 @@ __global__ void __launch_bounds__(kThreads, 1)
             uint8_t* const dst = ring + slot * C::kSlot + lane * tp.box_rows * 128;
 #pragma unroll
             for (int c = 0; c < kDC; ++c)
-              tma_load_4d(dst + c * C::kChunk, is_v ? &tmap_v : &tmap_k, smem_u32(&full[slot]), 64 * c, at, cur.h, page);
+              tma_load_4d(dst + c * C::kChunk, map, smem_u32(&full[slot]), 64 * c, at, cur.h, page);
           }
           __syncwarp();
-          ++issued;
+          used |= 1u << slot;
+          phases = (phases & ~(1u << slot)) | (phase_of(pos) << slot);
         }
         base += 2 * sg.n;
         tiles_done += sg.n;
         unit += sg.n;
         if (unit < run.end) skip_segment(p, cur, sg);
       }
-      if (lane == 0) {   // the last copies land before the CTA exits
-        for (int64_t i = issued < C::kSlots ? 0 : issued - C::kSlots; i < issued; ++i) {
-          const uint32_t bar = smem_u32(&full[slot_of(i)]);
-          const uint64_t t0 = global_timer_ns();
-          while (!mbar_try_wait(bar, phase_of(i)))
-            if (global_timer_ns() - t0 > tp.timeout_ns) {
-              atomicExch(p.err, kErrTimeout);
-              break;
-            }
-        }
+      // (The MMAs wait for every load.)  After a wait that gave up, copies in flight land before
+      // the CTA exits, or a limit passes.
+      if (!ok && lane == 0) {
+        const uint64_t t0 = global_timer_ns();
+        for (int i = 0; i < C::kSlots; ++i)
+          while (((used >> i) & 1u) && !mbar_try_wait(smem_u32(&full[i]), (phases >> i) & 1u))
+            if (global_timer_ns() - t0 > tp.timeout_ns) break;
       }
     } else if (warp == 1) {
       // ---- MMAs ----
       const int k_steps = p.head_dim / 16;
       const uint32_t id = kF16 ? idesc_fp16(0) : idesc_bf16(0);
-      const uint32_t id_s = id | ((uint32_t)(kTile >> 3) << 17);
+      const uint32_t id_s = id | ((uint32_t)(kHalf >> 3) << 17);
       const uint32_t id_o = id | ((uint32_t)(p.head_dim >> 3) << 17) | (1u << 16);   // B is MN-major
-      int64_t base = 0;
+      uint32_t base = 0;
       uint32_t q_phase = 0, p_phase[2] = {0u, 0u};
       bool ok = true;
       for (int64_t unit = run.begin; unit < run.end && ok;) {
-        const Segment sg = segment_at(p, cur, unit, run.end);
+        // (what the descriptors depend on goes through a shuffle, so that the compiler knows it to
+        // be the same in all lanes and keeps them in uniform registers, where tcgen05 takes them: an
+        // MMA issued from others cost 70 cycles, more than it runs)
+        Segment sg = segment_at(p, cur, unit, run.end);
+        sg.n = __shfl_sync(0xFFFFFFFFu, sg.n, 0);
+        sg.halves = __shfl_sync(0xFFFFFFFFu, (int)sg.halves, 0) != 0;
         const int n0 = sg.halves ? sg.n : (sg.n + 1) / 2, n1 = sg.halves ? sg.n : sg.n / 2;
         if (!mbar_wait_warp(q_ready, q_phase, ctl)) break;
         q_phase ^= 1u;
         tc_fence_after();
-        auto scores = [&](int s, int j) {
-          const int64_t pos = base + k_pos(sg.halves, sg.halves ? j : 2 * j + s);
-          const int slot = slot_of(pos);
-          if (!mbar_wait_warp(&full[slot], phase_of(pos), ctl)) return false;
-          tc_fence_after();
-          if (elect_one()) {
-            const uint32_t qa = smem_u32(q_smem) + (sg.halves ? s * C::kSlot : 0);
-            const uint32_t ka = smem_u32(ring + slot * C::kSlot);
-            for (int i = 0; i < k_steps; ++i) {
-              const uint32_t o = (uint32_t)(i >> 2) * C::kChunk + (uint32_t)(i & 3) * 32;
-              mma_bf16(s_tmem + 128 * s, sdesc_k128(qa + o), sdesc_k128(ka + o), id_s, i > 0 ? 1u : 0u);
-            }
-            tc_commit(&s_full[s]);
-            if (!sg.halves || s == 1) tc_commit(&empty[slot]);
-          }
-          __syncwarp();
-          return true;
-        };
-        auto product = [&](int s, int j, bool last) {
-          const int64_t pos = base + v_pos(sg.halves, sg.halves ? j : 2 * j + s, sg.n);
-          const int slot = slot_of(pos);
-          if (!mbar_wait_warp(&p_ready[s], p_phase[s], ctl) || !mbar_wait_warp(&full[slot], phase_of(pos), ctl))
-            return false;
-          p_phase[s] ^= 1u;
-          tc_fence_after();
-          if (elect_one()) {
-            const uint32_t va = smem_u32(ring + slot * C::kSlot);
+        // (one elected lane) scores of half hf of the stream's tile in `slot`
+        auto scores = [&](int s, int hf, int slot) {
+          const uint32_t qa = smem_u32(q_smem) + (sg.halves ? s * C::kSlot : 0);
+          const uint32_t ka = smem_u32(ring + slot * C::kSlot) + hf * kHalf * 128;
+          const uint64_t qd = sdesc_k128(qa), kd = sdesc_k128(ka);
 #pragma unroll
-            for (int i = 0; i < kTile / 16; ++i)
-              mma_f16_ts(o_tmem + 128 * s, s_tmem + 128 * s + 8 * i, sdesc_v(va + i * 2048, C::kChunk), id_o,
-                         i > 0 || j > 0 ? 1u : 0u);
-            if (!sg.halves || s == 1) tc_commit(&empty[slot]);
-            if (last) tc_commit(&o_done[s]);
+          for (int i = 0; i < 4 * kDC; ++i) {
+            constexpr uint64_t kStep = 32 >> 4, kNext = C::kChunk >> 4;   // (in the descriptors' units)
+            const uint64_t o = (uint64_t)(i >> 2) * kNext + (uint64_t)(i & 3) * kStep;
+            if (i < k_steps) mma_bf16(s_tmem + 128 * s + kHalf * hf, qd + o, kd + o, id_s, i > 0 ? 1u : 0u);
           }
-          __syncwarp();
+          tc_commit(&s_full[2 * s + hf]);
+          if (hf == 1 && (!sg.halves || s == 1)) tc_commit(&empty[slot]);
+        };
+        auto k_slot = [&](int s, int j, int* slot) {
+          const uint32_t pos = base + k_pos(sg.halves, sg.halves ? j : 2 * j + s);
+          *slot = __shfl_sync(0xFFFFFFFFu, slot_of(pos), 0);
+          const bool there = mbar_wait_warp(&full[*slot], phase_of(pos), ctl);
+          tc_fence_after();
+          return there;
+        };
+        // The products of the stream's tile j, and the scores of its next one: each half's as its P
+        // comes, into the columns that this frees, while the softmax works on the other half.
+        auto tile = [&](int s, int j, bool last) {
+          const uint32_t pos = base + v_pos(sg.halves, sg.halves ? j : 2 * j + s, sg.n);
+          const int slot = __shfl_sync(0xFFFFFFFFu, slot_of(pos), 0);
+          int next = 0;
+          if (!mbar_wait_warp(&full[slot], phase_of(pos), ctl)) return false;
+          const uint64_t vd = sdesc_v(smem_u32(ring + slot * C::kSlot), C::kChunk);
+#pragma unroll
+          for (int hf = 0; hf < 2; ++hf) {
+            if (!mbar_wait_warp(&p_ready[2 * s + hf], p_phase[s], ctl)) return false;
+            tc_fence_after();
+            if (elect_one()) {
+#pragma unroll
+              for (int i = 0; i < kHalf / 16; ++i)
+                mma_f16_ts(o_tmem + 128 * s, s_tmem + 128 * s + kHalf * hf + 8 * i,
+                           vd + (uint64_t)((4 * hf + i) * (2048 >> 4)), id_o, i > 0 || hf > 0 || j > 0 ? 1u : 0u);
+              tc_commit(&pv_done[2 * s + hf]);
+              if (hf == 1 && (!sg.halves || s == 1)) tc_commit(&empty[slot]);
+            }
+            __syncwarp();
+            if (last) continue;
+            if (hf == 0 && !k_slot(s, j + 1, &next)) return false;
+            if (elect_one()) scores(s, hf, next);
+            __syncwarp();
+          }
+          p_phase[s] ^= 1u;
           return true;
         };
-        ok = scores(0, 0) && (n1 == 0 || scores(1, 0));
+        for (int s = 0; s < (n1 > 0 ? 2 : 1) && ok; ++s) {
+          int slot;
+          ok = k_slot(s, 0, &slot);
+          if (ok && elect_one()) {
+            scores(s, 0, slot);
+            scores(s, 1, slot);
+          }
+          __syncwarp();
+        }
         for (int j = 0; j < n0 && ok; ++j) {
-          ok = product(0, j, j + 1 == n0) && (j + 1 >= n0 || scores(0, j + 1));
-          if (ok && j < n1) ok = product(1, j, j + 1 == n1) && (j + 1 >= n1 || scores(1, j + 1));
+          ok = tile(0, j, j + 1 == n0);
+          if (ok && j < n1) ok = tile(1, j, j + 1 == n1);
         }
         base += 2 * sg.n;
         unit += sg.n;
@@ -333,116 +385,156 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
     }
   } else {
-    // ---- softmax: stream s, a thread per row ----
+    // ---- softmax: stream s, row r ----
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
     const int thread = threadIdx.x - kSoftWarp0 * 32;
     const int s = thread >> 7, r = thread & 127;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t my_s = s_tmem + 128 * s + lanes, my_o = o_tmem + 128 * s + lanes;
     bool up = true;   // no wait has failed (after one, the loops run out without waiting)
-    int64_t base = 0, tiles_done = 0;
-    uint32_t s_phase = 0, o_phase = 0;
-    for (int64_t unit = run.begin; unit < run.end;) {
+    uint32_t s_phase = 0;   // of the stream's tiles
+    // Thread 0 walks the run, a segment ahead of the others.
+    int64_t unit = run.begin;
+    uint32_t base = 0;
+    unsigned tiles_done = 0;
+    auto publish = [&](int at) {
+      SoftSegment& g = sh.seg[at];
+      g.n = 0;
+      if (unit >= run.end) return;
       const Segment sg = segment_at(p, cur, unit, run.end);
-      const int rows = (int)min((int64_t)kRows, (int64_t)cur.s.fresh * p.group - (int64_t)cur.rt * kRows);
-      const int my_row = sg.halves ? 128 * s + r : r;
-      const bool row_in = my_row < rows;
-      const int64_t row = (int64_t)cur.rt * kRows + (row_in ? my_row : 0);
-      const int t = (int)(row / p.group);
-      const int64_t token = cur.s.first + t;
-      const int head = cur.h * p.group + (int)(row % p.group);
+      const int64_t item0 = unit - sg.first;
+      g.s = cur.s;
+      g.base = base;
+      g.b = cur.b;
+      g.h = cur.h;
+      g.rt = cur.rt;
+      g.first = sg.first;
+      g.n = sg.n;
+      g.tiles_done = tiles_done;
+      g.halves = sg.halves;
+      g.begun = item0 < run.begin;
+      g.whole = !g.begun && item0 + cur.tiles <= run.end;
+      base += 2 * sg.n;
+      tiles_done += sg.n;
+      unit += sg.n;
+      if (unit < run.end) skip_segment(p, cur, sg);
+    };
+    if (thread == 0) publish(0);
+    softmax_sync();
+    for (int at = 0;; at ^= 1) {
+      const SoftSegment& g = sh.seg[at];
+      const int n = g.n;
+      if (n == 0) break;
+      const bool halves = g.halves;
+      // (tokens and rows below 2^31)
+      const int my_row = halves ? 128 * s + r : r;
+      auto row_in = [&] { return g.rt * kRows + my_row < g.s.fresh * p.group; };
+      auto row_of = [&] { return row_in() ? g.rt * kRows + my_row : 0; };
       // Q into shared memory: rows of 128 swizzled bytes, 64 elements a chunk
-      if (sg.halves || s == 0) {
-        const uint16_t* const q = p.q + token * p.q_token + head * p.q_head;
-        const uint32_t dst = smem_u32(q_smem) + (sg.halves ? s * C::kSlot : 0) + r * 128;
+      if (halves || s == 0) {
+        const int row = row_of();
+        const uint16_t* const q = p.q + (g.s.first + row / p.group) * p.q_token +
+                                  (int64_t)(g.h * p.group + row % p.group) * p.q_head;
+        const uint32_t dst = smem_u32(q_smem) + (halves ? s * C::kSlot : 0) + r * 128;
+        const bool in = row_in();
+        uint4 w[kD / 8];
 #pragma unroll
-        for (int i = 0; i < kD / 8; ++i) {
-          uint4 w = make_uint4(0u, 0u, 0u, 0u);
-          if (row_in && 8 * i < p.head_dim) w = *reinterpret_cast<const uint4*>(q + 8 * i);
-          st_shared_v4(dst + (i >> 3) * C::kChunk + (((i & 7) ^ (r & 7)) << 4), w.x, w.y, w.z, w.w);
+        for (int i = 0; i < kD / 8; ++i) {   // 16-byte pieces
+          w[i] = make_uint4(0u, 0u, 0u, 0u);
+          if (in && 8 * i < p.head_dim) w[i] = *reinterpret_cast<const uint4*>(q + 8 * i);
         }
+#pragma unroll
+        for (int i = 0; i < kD / 8; ++i)
+          st_shared_v4(dst + (i >> 3) * C::kChunk + (((i & 7) ^ (r & 7)) << 4), w[i].x, w[i].y, w[i].z, w[i].w);
         fence_proxy_async_smem();
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(q_ready);
+      if (thread == 0) publish(at ^ 1);
+      __syncwarp();
 
       float m = -INFINITY, l = 0.0f;
-      const int mine = sg.halves ? sg.n : (sg.n + 1 - s) / 2;
-      for (int j = 0; j < mine; ++j) {
-        const int tile = sg.halves ? j : 2 * j + s;
-        const int64_t key0 = (int64_t)(sg.first + tile) * kTile;
-        if (up) up = mbar_wait(&s_full[s], s_phase, ctl);
-        s_phase ^= 1u;
+      const int mine = halves ? n : (n + 1 - s) / 2;
+      const int tail_from = (int)(g.s.cached / kTile - g.first);   // the first tile with new tokens or none
+      for (int j2 = 0; j2 < 2 * mine; ++j2) {
+        const int hf = j2 & 1, tile = halves ? j2 >> 1 : (j2 & ~1) + s;
+        const bool tail = tile >= tail_from;
+        const uint32_t at_s = my_s + kHalf * hf;
+        if (up) up = mbar_wait(&s_full[2 * s + hf], s_phase, ctl);
         __syncwarp();
         tc_fence_after();
-        uint32_t v[4][32];
-#pragma unroll
-        for (int c = 0; c < 4; ++c) tmem_ld32(my_s + 32 * c, v[c]);
+        uint32_t v[2][32];
+        tmem_ld32(at_s, v[0]);
+        tmem_ld32(at_s + 32, v[1]);
+        const unsigned bads = *(volatile unsigned*)&sh.bad_pages[(g.tiles_done + tile) % kBadRing];
         tmem_ld_wait();
-        const unsigned bads = *(volatile unsigned*)&bad_pages[(tiles_done + tile) % kBadRing];
-        const bool tail = key0 + kTile > cur.s.cached;
         if (tail || bads != 0u) {
+          const int row = row_of(), t = row / p.group;
+          const int64_t key = (int64_t)(g.first + tile) * kTile + kHalf * hf;
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            uint32_t bits = tail ? seen_bits(p, cur.s, token, t, key0 + 32 * c) : 0xFFFFFFFFu;
-            if (bads != 0u)
-              for (int i = 0; i < 32; ++i)
-                if ((bads >> ((32 * c + i) / tp.box_rows)) & 1u) bits &= ~(1u << i);
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-              if (!((bits >> i) & 1u)) v[c][i] = 0xFF800000u;   // -infinity
-          }
+          for (int c = 0; c < 2; ++c)
+            hide(tail ? seen_bits(p, g.s, g.s.first + t, t, key + 32 * c) : 0xFFFFFFFFu, bads, 2 * hf + c, tp.box_rows,
+                 v[c]);
         }
-        float top[4];
+        float top[8];
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          top[c] = __uint_as_float(v[c][0]);
+        for (int i = 0; i < 8; ++i) top[i] = __uint_as_float(v[0][i]);
 #pragma unroll
-          for (int i = 1; i < 32; ++i) top[c] = fmaxf(top[c], __uint_as_float(v[c][i]));
-        }
-        const float cand = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * p.scale_log2;
+        for (int i = 8; i < 64; i += 16)
+#pragma unroll
+          for (int k = 0; k < 8; ++k)
+            top[k] = max_nan(top[k], __uint_as_float(v[(i + k) >> 5][(i + k) & 31]),
+                             i + 8 < 64 ? __uint_as_float(v[(i + 8 + k) >> 5][(i + 8 + k) & 31]) : top[k]);
+        const float cand = max_nan(max_nan(top[0], top[1], top[2]), max_nan(top[3], top[4], top[5]),
+                                   max_nan(top[6], top[7], top[7])) *
+                           p.scale_log2;
         const bool rise = cand > m + kSlack || (m == -INFINITY && cand > m);
         if (__any_sync(0xFFFFFFFFu, rise)) {
           const float f = rise ? exp2_fast(m - cand) : 1.0f;
           l *= f;
           if (rise) m = cand;
-          if (j > 0) {   // (the product before is done: the scores came after it)
+          if (j2 > 0) {
+            // the product before this half's has to be done (those before that one are: its
+            // columns hold these scores): the first half's of this tile, the second's of the last
+            if (up) up = mbar_wait(&pv_done[2 * s + (hf ^ 1)], hf ? s_phase : s_phase ^ 1u, ctl);
+            __syncwarp();
+            tc_fence_after();
 #pragma unroll 1
-            for (int c = 0; c < p.head_dim; c += 32) {
-              uint32_t o[32];
-              tmem_ld32(my_o + c, o);
+            for (int c = 0; c < p.head_dim; c += 16) {
+              uint32_t o[16];
+              tmem_ld16(my_o + c, o);
               tmem_ld_wait();
 #pragma unroll
-              for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-              tmem_st32(my_o + c, o);
+              for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+              tmem_st16(my_o + c, o);
             }
           }
         }
         const float2 scale2 = splat(p.scale_log2), base2 = splat(m == -INFINITY ? 0.0f : -m);
-        float2 sum = make_float2(0.0f, 0.0f);
+        // (with a NaN or an infinity among the scores the row is NaN)
+        float2 sum = make_float2(cand < INFINITY ? 0.0f : __uint_as_float(0x7FFFFFFFu), 0.0f);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          uint32_t w[32];
+        for (int c = 0; c < 2; ++c) {
+          uint32_t w[16];
 #pragma unroll
-          for (int i = 0; i < 32; ++i) {
-            const uint32_t* const x = v[2 * h + (i >> 4)];
-            float2 e = fma2(make_float2(__uint_as_float(x[2 * (i & 15)]), __uint_as_float(x[2 * (i & 15) + 1])), scale2,
-                            base2);
+          for (int i = 0; i < 16; ++i) {
+            float2 e = fma2(make_float2(__uint_as_float(v[c][2 * i]), __uint_as_float(v[c][2 * i + 1])), scale2, base2);
             e = make_float2(exp2_fast(e.x), exp2_fast(e.y));
             sum = add2(sum, e);
             w[i] = pack2<kF16>(e.x, e.y);
           }
-          tmem_st32(my_s + 32 * h, w);
+          tmem_st16(at_s + 16 * c, w);
         }
         l += sum.x + sum.y;
         if (tail) {
-          // V's row r of the tile: nothing but finite values may meet a P of zero
-          const int64_t pos = base + v_pos(sg.halves, tile, sg.n);
+          // V's rows of the half, two threads each: nothing but finite values may meet a P of zero
+          const uint32_t pos = g.base + v_pos(halves, tile, n);
           if (up) up = mbar_wait(&full[slot_of(pos)], phase_of(pos), ctl);
-          const uint32_t va = smem_u32(ring + slot_of(pos) * C::kSlot) + r * 128;
-          const bool in = key0 + r < cur.s.keys;
+          const int key_row = kHalf * hf + (r & 63);
+          const uint32_t va = smem_u32(ring + slot_of(pos) * C::kSlot) + key_row * 128;
+          const bool in = (int64_t)(g.first + tile) * kTile + key_row < g.s.keys;
 #pragma unroll 1
-          for (int i = 0; i < kD / 8; ++i) {
+          for (int i = r >> 6; i < kD / 8; i += 2) {
             const uint32_t a = va + (i >> 3) * C::kChunk + (((i & 7) ^ (r & 7)) << 4);
             uint32_t x[4];
             asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
@@ -456,7 +548,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               x[q] = in ? x[q] & ~hit : 0u;
             }
             if (in && odd != 0u) {
-              *(volatile int*)&odd_values = 1;   // before the zeros: who finds them finds this
+              *(volatile int*)&sh.odd_values = 1;   // before the zeros: who finds them finds this
               __threadfence_block();
             }
             if (!in || odd != 0u) st_shared_v4(a, x[0], x[1], x[2], x[3]);
@@ -466,23 +558,21 @@ __global__ void __launch_bounds__(kThreads, 1)
         tmem_st_wait();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&p_ready[s]);
+        if (lane == 0) mbar_arrive(&p_ready[2 * s + hf]);
+        s_phase ^= (uint32_t)hf;
       }
 
       // ---- the segment's end ----
       if (mine > 0) {
-        if (up) up = mbar_wait(&o_done[s], o_phase, ctl);
-        o_phase ^= 1u;
+        if (up) up = mbar_wait(&pv_done[2 * s + 1], s_phase ^ 1u, ctl);
         __syncwarp();
         tc_fence_after();
       }
-      const int64_t item0 = unit - sg.first, item1 = item0 + cur.tiles - 1;
-      const bool whole = item0 >= run.begin && item1 < run.end;
-      const bool join_streams = !sg.halves && sg.n > 1;
+      const bool join_streams = !halves && n > 1;
       // tiles in turn: the odd ones' sums through Q's place
       if (join_streams) {
         if (s == 1) {
-          other_ml[r] = make_float2(m, l);
+          sh.other[r] = make_float2(m, l);
           const uint32_t dst = smem_u32(q_smem) + r * (kD * 4);
 #pragma unroll 1
           for (int c = 0; c < p.head_dim; c += 32) {
@@ -496,19 +586,21 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         softmax_sync();
       }
-      if (sg.halves || s == 0) {
+      if (halves || s == 0) {
         float f0 = 1.0f, f1 = 0.0f;
         if (join_streams) {
-          const float2 b = other_ml[r];
-          const float both = fmaxf(m, b.x), at = both == -INFINITY ? 0.0f : both;
-          f0 = exp2_fast(m - at);
-          f1 = exp2_fast(b.x - at);
+          const float2 b = sh.other[r];
+          const float both = fmaxf(m, b.x), top = both == -INFINITY ? 0.0f : both;
+          f0 = exp2_fast(m - top);
+          f1 = exp2_fast(b.x - top);
           l = fmaf(l, f0, b.y * f1);
           m = both;
         }
-        const int64_t part_row = (int64_t)(2 * blockIdx.x + (item0 < run.begin ? 0 : 1)) * kRows + my_row;
+        const bool in = row_in(), whole = g.whole;
+        const int row = row_of(), t = row / p.group, head = g.h * p.group + row % p.group;
+        const int64_t token = g.s.first + t;
+        const int64_t at_part = (int64_t)(2 * blockIdx.x + (g.begun ? 0 : 1)) * kRows + my_row;
         const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-        const bool odd = *(volatile int*)&odd_values != 0;
         const uint32_t src = smem_u32(q_smem) + r * (kD * 4);
 #pragma unroll 1
         for (int c = 0; c < p.head_dim; c += 32) {
@@ -531,18 +623,18 @@ __global__ void __launch_bounds__(kThreads, 1)
               f[4 * i + 3] = fmaf(b.w, f1, f[4 * i + 3]);
             }
           }
-          if (odd && row_in) {
+          if (*(volatile int*)&sh.odd_values != 0 && in) {
             // values that were zeroed, for the rows that see them: infinities and NaN as they are
-            const int64_t key_end = min(cur.s.keys, (int64_t)(sg.first + sg.n) * kTile);
-            for (int64_t key = max((int64_t)sg.first * kTile, cur.s.cached / kTile * kTile); key < key_end; ++key) {
-              int index, at;
-              if (!(seen_bits(p, cur.s, token, t, key) & 1u) ||
-                  !cache_place(key, p.page_size, p.table_width, &index, &at))
+            const int64_t key_end = min(g.s.keys, (int64_t)(g.first + n) * kTile);
+            for (int64_t key = max((int64_t)g.first * kTile, g.s.cached / kTile * kTile); key < key_end; ++key) {
+              int index, slot;
+              if (!(seen_bits(p, g.s, token, t, key) & 1u) ||
+                  !cache_place(key, p.page_size, p.table_width, &index, &slot))
                 continue;
-              const int page = p.table[cur.b * p.table_stride + index];
+              const int page = p.table[g.b * p.table_stride + index];
               if (page < 0 || page >= p.pages) continue;
               const uint16_t* const x =
-                  reinterpret_cast<const uint16_t*>(p.v + page * p.v_page + at * p.v_slot + cur.h * p.v_head) + c;
+                  reinterpret_cast<const uint16_t*>(p.v + page * p.v_page + slot * p.v_slot + g.h * p.v_head) + c;
 #pragma unroll
               for (int i = 0; i < 32; ++i) {
                 if (c + i >= p.head_dim) break;
@@ -552,7 +644,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               }
             }
           }
-          if (row_in) {
+          if (in) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
               const int d = c + 4 * i;
@@ -561,37 +653,20 @@ __global__ void __launch_bounds__(kThreads, 1)
               if (whole)
                 store_out4(p, token, head, d, make_float4(x.x * inv, x.y * inv, x.z * inv, x.w * inv));
               else
-                *reinterpret_cast<float4*>(p.part + part_row * kD + d) = x;
+                *reinterpret_cast<float4*>(p.part + at_part * kD + d) = x;
             }
           }
         }
-        if (row_in) {
+        if (in) {
           if (!whole)
-            p.part_ml[part_row] = make_float2(m, l);
+            p.part_ml[at_part] = make_float2(m, l);
           else if (p.lse != nullptr)
             p.lse[token * p.lse_token + head] = log_sum(m, l);
         }
       }
-      if (!whole) {
-        const int first = (int)split_owner(item0, run.total, run.ctas), last = (int)split_owner(item1, run.total, run.ctas);
-        __threadfence();
-        softmax_sync();
-        if (thread == 0) {
-          const bool all = atomicAdd(&p.counts[first], 1u) == (unsigned)(last - first);
-          if (all) p.counts[first] = 0u;   // as it was before the call
-          __threadfence();
-          last_flag = all ? 1u : 0u;
-        }
-        softmax_sync();
-        if (last_flag != 0u) join_parts<kRows, kD, 256>(p, cur, first, last, 1.0f, thread);
-      }
       tc_fence_before();
-      softmax_sync();   // Q's place and the flags are free
-      if (thread == 0) odd_values = 0;
-      base += 2 * sg.n;
-      tiles_done += sg.n;
-      unit += sg.n;
-      if (unit < run.end) skip_segment(p, cur, sg);
+      softmax_sync();   // Q's place and the flags are free, the next segment is published
+      if (thread == 0) sh.odd_values = 0;
     }
   }
   __syncwarp();
@@ -601,6 +676,29 @@ __global__ void __launch_bounds__(kThreads, 1)
     tc_fence_after();
     tmem_dealloc(tmem, 512);
   }
+}
+
+// Items that end in other CTAs than they begin in: CTA x joins the one that begins in CTA x of
+// the kernel above, kJoinRows rows of it.
+constexpr int kJoinRows = 32, kJoinThreads = 256;
+template <int kDC>
+__global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const AttnParams p, int ctas) {
+  __shared__ float2 stat[kJoinRows];
+  __shared__ RunScratch scratch;
+  Cursor cur;
+  const int cta = (int)blockIdx.x;
+  // (lengths and counts: as the kernel before found them, which began after they were written)
+  const Run run = find_run<kRows, kTile, kJoinThreads, true>(p, cur, cta, ctas, scratch);
+  grid_dep_wait();
+  grid_dep_launch();
+  if (run.begin >= run.end) return;
+  const int64_t item0 = run.end - 1 - cur.tile, item1 = item0 + cur.tiles - 1;
+  if (item0 < run.begin || item1 < run.end) return;   // begun before, or whole
+  const int all = (int)min((int64_t)kRows, (int64_t)cur.s.fresh * p.group - (int64_t)cur.rt * kRows);
+  const int row0 = (int)blockIdx.y * kJoinRows, rows = min(kJoinRows, all - row0);
+  if (rows <= 0) return;
+  join_parts<kRows, 64 * kDC, kJoinThreads>(p, cur, cta, cta, (int)split_owner(item1, run.total, run.ctas), 1, true, 1.0f,
+                                            row0, rows, (int)threadIdx.x, stat, [] { __syncthreads(); });
 }
 
 template <bool kF16, int kDC>
@@ -618,14 +716,17 @@ cudaError_t launch_cfg(TileParams tp, const CUtensorMap& tk, const CUtensorMap& 
   p.part_ml = reinterpret_cast<float2*>(reinterpret_cast<uint8_t*>(p.counts) + kCountBytes);
   p.part = reinterpret_cast<float*>(p.part_ml + (int64_t)2 * kRows * ctas);
   p.least = 2;
-  return launch_pdl(kern, dim3((unsigned)ctas), kThreads, C::kSmem, s, tk, tv, tp);
+  const cudaError_t st = launch_pdl(kern, dim3((unsigned)ctas), kThreads, C::kSmem, s, tk, tv, tp);
+  if (st != cudaSuccess) return st;
+  return launch_pdl(attn_join_kernel<kDC>, dim3((unsigned)ctas, kRows / kJoinRows), kJoinThreads, 0, s, p, ctas);
 }
 
 }  // namespace
 
 bool attention_tiles_fit(const AttnParams& p) {
   const bool pages = p.page_size % 8 == 0 && (p.page_size >= kTile ? p.page_size % kTile : kTile % p.page_size) == 0;
-  return p.head_dim <= 128 && pages && p.k_slot > 0 && p.k_head > 0 && p.k_page > 0 && p.v_slot > 0 && p.v_head > 0 &&
+  return p.head_dim <= 128 && pages && p.tokens * p.group < (int64_t)1 << 30 &&
+         (int64_t)p.page_size * p.table_width < (int64_t)1 << 31 && p.k_slot > 0 && p.k_head > 0 && p.k_page > 0 && p.v_slot > 0 && p.v_head > 0 &&
          p.v_page > 0;
 }
 

@@ -51,12 +51,16 @@ struct Run {
   int64_t total, begin, end;
   int ctas;
 };
+struct RunScratch {   // in shared memory
+  int64_t warp_sum[32];
+  int64_t found_at;
+  int found_b;
+};
 
-template <int kRows, int kTile, int kThreads>
-__device__ __forceinline__ Run find_run(const AttnParams& p, Cursor& c) {
-  __shared__ int64_t warp_sum[kThreads / 32];
-  __shared__ int64_t found_at;
-  __shared__ int found_b;
+// (kLast: the cursor at its last unit.)
+template <int kRows, int kTile, int kThreads, bool kLast = false>
+__device__ __forceinline__ Run find_run(const AttnParams& p, Cursor& c, int cta, int ctas, RunScratch& scratch) {
+  auto& warp_sum = scratch.warp_sum;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   Run r{0, 0, 0, 1};
   int64_t mine = 0, first = 0;
@@ -68,17 +72,18 @@ __device__ __forceinline__ Run find_run(const AttnParams& p, Cursor& c) {
     if (b < kThreads) first = u;
     mine += u;
   }
-  if (bad && blockIdx.x == 0) atomicExch(p.err, kErrInvalid);
+  if (bad && cta == 0) atomicExch(p.err, kErrInvalid);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xFFFFFFFFu, mine, o);
   if (lane == 0) warp_sum[warp] = mine;
   __syncthreads();
   for (int w = 0; w < kThreads / 32; ++w) r.total += warp_sum[w];
   if (r.total == 0) return r;
-  r.ctas = (int)split_ctas(r.total, gridDim.x, p.least);
-  if ((int)blockIdx.x >= r.ctas) return r;
-  r.begin = split_begin(blockIdx.x, r.total, r.ctas);
-  r.end = split_begin(blockIdx.x + 1, r.total, r.ctas);
+  r.ctas = (int)split_ctas(r.total, ctas, p.least);
+  if (cta >= r.ctas) return r;
+  r.begin = split_begin(cta, r.total, r.ctas);
+  r.end = split_begin(cta + 1, r.total, r.ctas);
+  const int64_t want = kLast ? r.end - 1 : r.begin;
   int64_t run = 0;
   for (int b0 = 0; b0 < p.sequences; b0 += kThreads) {
     const int b = b0 + threadIdx.x;
@@ -98,16 +103,16 @@ __device__ __forceinline__ Run find_run(const AttnParams& p, Cursor& c) {
       if (w < warp) base += warp_sum[w];
       run += warp_sum[w];
     }
-    if (base + incl - u <= r.begin && r.begin < base + incl) {
-      found_b = b;
-      found_at = base + incl - u;
+    if (base + incl - u <= want && want < base + incl) {
+      scratch.found_b = b;
+      scratch.found_at = base + incl - u;
     }
-    if (run > r.begin) break;
+    if (run > want) break;
   }
   __syncthreads();
-  c.b = found_b;
+  c.b = scratch.found_b;
   open_seq<kRows, kTile>(p, c);
-  int64_t at = r.begin - found_at;
+  int64_t at = want - scratch.found_at;
   c.tile = (int)(at % c.tiles);
   at /= c.tiles;
   c.rt = (int)(at % c.row_tiles);
@@ -133,35 +138,76 @@ __device__ __forceinline__ float log_sum(float m, float l) {   // m in powers of
   return l > 0.0f || l != l ? fmaf(m, 0.693147181f, logf(l)) : -INFINITY;
 }
 
-// The rows of an item whose parts CTAs first..last left in the workspace, joined in order.
-template <int kRows, int kD, int kThreads>
-__device__ __forceinline__ void join_parts(const AttnParams& p, const Cursor& c, int first, int last, float v_scale,
-                                           int thread) {
-  const int rows = (int)min((int64_t)kRows, (int64_t)c.s.fresh * p.group - (int64_t)c.rt * kRows);
-  for (int i = thread; i < rows * (p.head_dim / 4); i += kThreads) {
-    const int row = i / (p.head_dim / 4), d = i % (p.head_dim / 4) * 4;
-    float m = -INFINITY;
-    for (int q = first; q <= last; ++q) {
-      const int64_t at = (int64_t)(2 * q + (q == first ? 1 : 0)) * kRows + row;
-      m = fmaxf(m, __ldcg(&p.part_ml[at]).x);
+// An item's parts in the workspace: CTA first's is its second, all others' their first.
+template <int kRows>
+__device__ __forceinline__ int64_t part_row(int cta, int first, int row) {
+  return (int64_t)(2 * cta + (cta == first ? 1 : 0)) * kRows + row;
+}
+
+// Rows row0 .. row0 + rows - 1 of an item, whose parts the CTAs from, from + step, ... to left
+// in the workspace (first: the item's first CTA), joined in the order of the keys: to the
+// output, or to from's part in place.  Called by all of kThreads threads, which `sync` joins;
+// stat: kRows of them in shared memory.
+template <int kRows, int kD, int kThreads, typename Sync>
+__device__ __forceinline__ void join_parts(const AttnParams& p, const Cursor& c, int first, int from, int to, int step,
+                                           bool output, float v_scale, int row0, int rows, int thread, float2* stat,
+                                           Sync&& sync) {
+  for (int i = thread; i < rows; i += kThreads) {
+    float m = -INFINITY, l = 0.0f;
+#pragma unroll 4
+    for (int q = from; q <= to; q += step) {
+      const float2 ml = __ldcg(&p.part_ml[part_row<kRows>(q, first, row0 + i)]);
+      const float now = fmaxf(m, ml.x), base = now == -INFINITY ? 0.0f : now;
+      l = fmaf(l, exp2_fast(m - base), ml.y * exp2_fast(ml.x - base));
+      m = now;
     }
-    const float ms = m == -INFINITY ? 0.0f : m;
-    float l = 0.0f;
-    float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    for (int q = first; q <= last; ++q) {
-      const int64_t at = (int64_t)(2 * q + (q == first ? 1 : 0)) * kRows + row;
-      const float2 ml = __ldcg(&p.part_ml[at]);
-      const float4 v = __ldcg(reinterpret_cast<const float4*>(p.part + at * kD + d));
-      const float f = exp2_fast(ml.x - ms);
-      l = fmaf(ml.y, f, l);
-      o = make_float4(fmaf(v.x, f, o.x), fmaf(v.y, f, o.y), fmaf(v.z, f, o.z), fmaf(v.w, f, o.w));
+    stat[i] = make_float2(m, l);
+  }
+  sync();
+  const int d4s = p.head_dim / 4, items = rows * d4s;
+  constexpr int kAtOnce = 4;
+  for (int i0 = thread; i0 < items; i0 += kThreads * kAtOnce) {
+    float4 o[kAtOnce];
+    float base[kAtOnce];
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
+      const int i = min(i0 + k * kThreads, items - 1);
+      const float m = stat[i / d4s].x;
+      base[k] = m == -INFINITY ? 0.0f : m;
+      o[k] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     }
-    const int64_t r = (int64_t)c.rt * kRows + row;
-    const int64_t token = c.s.first + r / p.group;
-    const int head = c.h * p.group + (int)(r % p.group);
-    const float inv = l == 0.0f ? 0.0f : v_scale / l;
-    store_out4(p, token, head, d, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
-    if (p.lse != nullptr && d == 0) p.lse[token * p.lse_token + head] = log_sum(m, l);
+#pragma unroll 2
+    for (int q = from; q <= to; q += step) {
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k) {
+        const int i = min(i0 + k * kThreads, items - 1);
+        const int64_t at = part_row<kRows>(q, first, row0 + i / d4s);
+        const float f = exp2_fast(__ldcg(&p.part_ml[at].x) - base[k]);
+        const float4 v = __ldcg(reinterpret_cast<const float4*>(p.part + at * kD + i % d4s * 4));
+        o[k] = make_float4(fmaf(v.x, f, o[k].x), fmaf(v.y, f, o[k].y), fmaf(v.z, f, o[k].z), fmaf(v.w, f, o[k].w));
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
+      const int i = i0 + k * kThreads;
+      if (i >= items) break;
+      const int row = i / d4s, d = i % d4s * 4;
+      const float2 ml = stat[row];
+      if (output) {
+        const int64_t r = (int64_t)c.rt * kRows + row0 + row;
+        const int64_t token = c.s.first + r / p.group;
+        const int head = c.h * p.group + (int)(r % p.group);
+        const float inv = ml.y == 0.0f ? 0.0f : v_scale / ml.y;
+        store_out4(p, token, head, d, make_float4(o[k].x * inv, o[k].y * inv, o[k].z * inv, o[k].w * inv));
+        if (p.lse != nullptr && d == 0) p.lse[token * p.lse_token + head] = log_sum(ml.x, ml.y);
+      } else {
+        *reinterpret_cast<float4*>(p.part + part_row<kRows>(from, first, row0 + row) * kD + d) = o[k];
+      }
+    }
+  }
+  if (!output) {
+    sync();   // its maxima and sums have been read
+    for (int i = thread; i < rows; i += kThreads) p.part_ml[part_row<kRows>(from, first, row0 + i)] = stat[i];
   }
 }
 

@@ -334,7 +334,7 @@ def test_bad_tables_and_counts_are_reported_and_touch_nothing():
             assert qlin.qlin_sync_status() == 1
         ws = qlin.alloc_cache_attention_workspace()
         assert torch.equal(qlin.qlin_cache_attention(c, q, 0.125, workspace=ws), good)
-        assert qlin.qlin_sync_status() == 0 and (ws[:4096] == 0).all()
+        assert qlin.qlin_sync_status() == 0 and (ws[:8192] == 0).all()
 
 
 @pytest.mark.parametrize("T,G", [(1, 4), (40, 4)])
