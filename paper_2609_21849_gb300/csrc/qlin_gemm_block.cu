@@ -5,11 +5,15 @@
 // on the way into fp32 registers.  A block is a pipeline stage (128 bytes of K): the MMA
 // issuer writes its four products' sum into one of the tensor-memory buffers in turn, and
 // the epilogue's two warpgroups, which hold the tile's accumulators, take it from there.
-//   pair   256 x 256 tiles on a CTA pair (cta_group::2): a block is 512 cycles of MMAs, in
-//          which a CTA's 128 x 256 sums leave tensor memory (256 cycles of its bandwidth)
-//          and pass 32768 FMAs (256 cycles, two per instruction); 128 accumulators a thread.
+//   shared 128 x 256 tiles, two CTAs of a cluster over the same W: each loads half of its rows
+//          and sends them to both (TMA multicast).  A block is 512 cycles of MMAs, in which 128 x
+//          256 sums leave tensor memory and pass 32768 FMAs (256 cycles, two per instruction).
+//          (As a CTA pair with cta_group::2, every buffer's way to the epilogue and back crossed
+//          the pair: 950 cycles a block.)
 //   single 128 x 128 tiles on one CTA, for fewer rows.
-// Roles: warp 0 loads (TMA), warp 1 issues the MMAs, warps 4-11 hold the accumulators.
+// Roles: warp 0 loads (TMA), warp 1 issues the MMAs, warp 2 multiplies the scales of a block's rows
+// and columns into shared memory (loads of them by the epilogue's own warps cost 20 to 40 of 180
+// us), the warps from 4 on hold the accumulators, 64 columns of a row each.
 #include "qlin_internal.h"
 #include "qlin_tiles.h"
 
@@ -20,24 +24,29 @@ namespace {
 constexpr int kBM = kTileM;
 constexpr int kRowBytes = kStageRowBytes;   // a block of K
 constexpr int kSteps = 4;                   // MMAs of 32 elements of a block
-constexpr int kRoleWarps = 4, kEpiWarps = 8;
-constexpr int kThreads = (kRoleWarps + kEpiWarps) * 32;
-constexpr int kRoleRegs = 56, kHoldRegs = 224, kLaunchRegs = 168;
-static_assert(kRoleWarps * 32 * kRoleRegs + kEpiWarps * 32 * kHoldRegs <= kThreads * kLaunchRegs, "registers");
+constexpr int kRoleWarps = 4, kCols = 64;   // columns of an epilogue thread: inside one 128-row block of W
 
-template <int kBN, bool kPair>
+template <int kBN, bool kShare>
 struct BlockCfg {
-  static constexpr int kCM = kPair ? 2 : 1;
-  static constexpr int kSplit = kPair ? 4 : 2;   // row boxes per operand tile, whose copies overlap
+  static constexpr int kCM = kShare ? 2 : 1;     // CTAs of a cluster
+  static constexpr int kEpiWarps = kBN / kCols * 4;
+  static constexpr int kThreads = (kRoleWarps + kEpiWarps) * 32;
+  static constexpr int kSplit = 2;               // row boxes per load of 128 rows, whose copies overlap
   static constexpr int kABytes = kBM * kRowBytes;
-  static constexpr int kBBytes = kBN / kCM * kRowBytes;
+  static constexpr int kBBytes = kBN * kRowBytes;
   static constexpr int kStageBytes = kABytes + kBBytes;
-  static constexpr int kCols = kBN / 2;          // of an epilogue thread: one 128-row block of W at most
-  static constexpr int kBiasBytes = kEpiWarps * kCols * 4;
-  static constexpr int kStagesRaw = (232448 - 1024 - 512 - kBiasBytes) / kStageBytes;
-  static constexpr int kStages = kStagesRaw > 8 ? 8 : kStagesRaw;
+  static constexpr int kBiasBytes = kEpiWarps * kCols * 2;    // 16-bit, a copy per warp
   static constexpr int kBuffers = 512 / kBN;     // of block sums in tensor memory
-  static constexpr int kSmem = 1024 + kStages * kStageBytes + kBiasBytes + 512;
+  static constexpr int kWBlocks = kBN / 128;
+  static constexpr int kScaleBytes = kBuffers * kWBlocks * kBM * 4;   // of each buffer's block: [W's block][row]
+  static constexpr int kStagesRaw = (232448 - 1024 - 512 - kBiasBytes - kScaleBytes) / kStageBytes;
+  static constexpr int kStages = kStagesRaw > 8 ? 8 : kStagesRaw;
+  static constexpr int kSmem = 1024 + kStages * kStageBytes + kBiasBytes + kScaleBytes + 512;
+  // registers: the roles' warpgroup and those with accumulators
+  static constexpr int kRoleRegs = kThreads == 640 ? 64 : 80, kHoldRegs = kThreads == 640 ? 104 : 128;
+  static constexpr int kLaunchRegs = kThreads == 640 ? 96 : 112;
+  static_assert(kRoleWarps * 32 * kRoleRegs + kEpiWarps * 32 * kHoldRegs <= kThreads * kLaunchRegs, "registers");
+  static_assert(kThreads == 640 || kThreads == 384, "whole warpgroups");
   static_assert(kStages >= 3 && kSmem <= 232448, "shared memory");
 };
 
@@ -65,6 +74,10 @@ __device__ __forceinline__ void drain(uint64_t* bar, uint32_t parity, const Bloc
       return;
     }
   }
+}
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
 
 template <bool kWide>
@@ -96,18 +109,18 @@ __device__ __forceinline__ void store32(uint16_t* p, const uint32_t* v, bool wid
   }
 }
 
-template <int kBN, bool kPair>
-__global__ void __launch_bounds__(kThreads, 1)
+template <int kBN, bool kShare>
+__global__ void __launch_bounds__(BlockCfg<kBN, kShare>::kThreads, 1)
     gemm_block_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ CUtensorMap tmap_b,
                       const BlockParams p) {
-  using C = BlockCfg<kBN, kPair>;
+  using C = BlockCfg<kBN, kShare>;
   constexpr int kCM = C::kCM;
-  constexpr uint16_t kMask = (uint16_t)((1u << kCM) - 1u);
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem =
       reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
-  float* const bias_copies = reinterpret_cast<float*>(smem + C::kStages * C::kStageBytes);
-  uint64_t* full = reinterpret_cast<uint64_t*>(smem + C::kStages * C::kStageBytes + C::kBiasBytes);
+  uint8_t* const bias_copies = smem + C::kStages * C::kStageBytes;
+  float* const scales = reinterpret_cast<float*>(bias_copies + C::kBiasBytes);
+  uint64_t* full = reinterpret_cast<uint64_t*>(bias_copies + C::kBiasBytes + C::kScaleBytes);
   uint64_t* empty = full + C::kStages;
   uint64_t* tmem_full = empty + C::kStages;
   uint64_t* tmem_empty = tmem_full + C::kBuffers;
@@ -117,32 +130,26 @@ __global__ void __launch_bounds__(kThreads, 1)
 
   const int warp = __shfl_sync(0xFFFFFFFFu, (int)(threadIdx.x >> 5), 0);
   const int lane = threadIdx.x & 31;
-  const int rank = kPair ? __shfl_sync(0xFFFFFFFFu, (int)cluster_ctarank(), 0) : 0;
-  const bool leader = rank == 0;
+  const int rank = kShare ? __shfl_sync(0xFFFFFFFFu, (int)cluster_ctarank(), 0) : 0;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < C::kStages; ++s) {
       mbar_init(&full[s], 1);
-      mbar_init(&empty[s], 1);
+      mbar_init(&empty[s], kCM);   // both CTAs' MMAs have read what was sent to both
     }
     for (int a = 0; a < C::kBuffers; ++a) {
-      mbar_init(&tmem_full[a], 1);
-      mbar_init(&tmem_empty[a], kCM * kEpiWarps);
+      mbar_init(&tmem_full[a], 2);   // the block's products, and its scales
+      mbar_init(&tmem_empty[a], C::kEpiWarps);
     }
     mbar_init(mma_done, 1);
     *abort_flag = 0;
     mbar_fence_init();
   }
   if (warp == 0 && lane < 2) prefetch_tmap(lane == 0 ? &tmap_a : &tmap_b);
-  if (warp == 1) {
-    if (kPair)
-      tmem_alloc_pair(tmem_slot, 512);
-    else
-      tmem_alloc(tmem_slot, 512);
-  }
+  if (warp == 1) tmem_alloc(tmem_slot, 512);
   tc_fence_before();
-  if (kPair)
-    cluster_sync();
+  if (kShare)
+    cluster_sync();   // the peer's barriers exist before any copy completes on them
   else
     __syncthreads();
   tc_fence_after();
@@ -156,11 +163,11 @@ __global__ void __launch_bounds__(kThreads, 1)
   grid_dep_wait();
 
   if (warp < kRoleWarps) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRoleRegs));
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kRoleRegs));
     if (warp == 0) {
       // ---- TMA producer ----
-      constexpr int kSplit = C::kSplit, kARows = kBM / kSplit, kWRows = kBN / kCM / kSplit;
-      const uint32_t bar0 = kPair ? __shfl_sync(0xFFFFFFFFu, mapa_shared(full, 0), 0) : smem_u32(full);
+      // (a W load of a cluster: this CTA's half of the rows, to the same place in both CTAs)
+      constexpr int kARows = kBM / C::kSplit, kWRows = kBN / kCM / C::kSplit;
       int stage = 0, issued = 0;
       uint32_t phase = 0;
       bool ok = true;
@@ -174,20 +181,18 @@ __global__ void __launch_bounds__(kThreads, 1)
             break;
           }
           uint8_t* const sA = smem + stage * C::kStageBytes;
-          const uint32_t bar = bar0 + (uint32_t)(stage * 8);
+          uint8_t* const sW = sA + C::kABytes + rank * (C::kBBytes / kCM);
+          const uint32_t bar = smem_u32(&full[stage]);
           if (elect_one()) {
-            if (leader) mbar_arrive_expect_tx(&full[stage], kCM * C::kStageBytes);
+            mbar_arrive_expect_tx(&full[stage], C::kStageBytes);
 #pragma unroll
-            for (int b = 0; b < kSplit; ++b) {
-              if (kPair) {
-                tma_load_4d_pair(sA + b * kARows * kRowBytes, &tmap_a, bar, kb * kRowBytes, a_row + b * kARows, 0, 0);
-                tma_load_4d_pair(sA + C::kABytes + b * kWRows * kRowBytes, &tmap_b, bar, kb * kRowBytes,
-                                 w_row + b * kWRows, 0, 0);
-              } else {
-                tma_load_4d(sA + b * kARows * kRowBytes, &tmap_a, bar, kb * kRowBytes, a_row + b * kARows, 0, 0);
-                tma_load_4d(sA + C::kABytes + b * kWRows * kRowBytes, &tmap_b, bar, kb * kRowBytes,
-                            w_row + b * kWRows, 0, 0);
-              }
+            for (int b = 0; b < C::kSplit; ++b) {
+              tma_load_4d(sA + b * kARows * kRowBytes, &tmap_a, bar, kb * kRowBytes, a_row + b * kARows, 0, 0);
+              if (kShare)
+                tma_load_4d_multicast(sW + b * kWRows * kRowBytes, &tmap_b, bar, kb * kRowBytes, w_row + b * kWRows, 0, 0,
+                                      (uint16_t)3);
+              else
+                tma_load_4d(sW + b * kWRows * kRowBytes, &tmap_b, bar, kb * kRowBytes, w_row + b * kWRows, 0, 0);
             }
           }
           ++issued;
@@ -197,7 +202,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
         }
       }
-      if (leader && lane == 0) {   // the last copies land before the CTA exits
+      if (lane == 0) {   // the last copies land before the CTA exits
         const int n_drain = min(issued, C::kStages);
         for (int i = 0; i < n_drain; ++i) {
           if (--stage < 0) {
@@ -207,9 +212,9 @@ __global__ void __launch_bounds__(kThreads, 1)
           drain(&full[stage], phase, p);
         }
       }
-    } else if (warp == 1 && leader) {
+    } else if (warp == 1) {
       // ---- MMA issuer: a block of K into each tensor-memory buffer in turn ----
-      constexpr uint32_t idesc = idesc_fp8(kBN, kPair ? 256 : 128);
+      constexpr uint32_t idesc = idesc_fp8(kBN, 128);
       const int k_steps = (int)(p.K / 32);
       int stage = 0, buf = 0;
       uint32_t phase = 0, buf_phase = 0;
@@ -228,20 +233,14 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (elect_one()) {
 #pragma unroll
             for (int j = 0; j < kSteps; ++j) {
-              if (j < steps) {   // (32 bytes further per step)
-                if (kPair)
-                  mma_fp8_pair(d, adesc + 2 * j, bdesc + 2 * j, idesc, j > 0 ? 1u : 0u);
-                else
-                  mma_fp8(d, adesc + 2 * j, bdesc + 2 * j, idesc, j > 0 ? 1u : 0u);
-              }
+              // (32 bytes further per step)
+              if (j < steps) mma_fp8(d, adesc + 2 * j, bdesc + 2 * j, idesc, j > 0 ? 1u : 0u);
             }
-            if (kPair) {
-              tc_commit_pair_mc(&empty[stage], kMask);
-              tc_commit_pair_mc(&tmem_full[buf], kMask);
-            } else {
+            if (kShare)
+              tc_commit_mc(&empty[stage], (uint16_t)3);
+            else
               tc_commit(&empty[stage]);
-              tc_commit(&tmem_full[buf]);
-            }
+            tc_commit(&tmem_full[buf]);
           }
           if (++stage == C::kStages) {
             stage = 0;
@@ -265,95 +264,118 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       // Every MMA issued must finish before the tensor memory is released.
       if (elect_one()) {
-        if (kPair)
-          tc_commit_pair_mc(mma_done, 1);
-        else
-          tc_commit(mma_done);
+        tc_commit(mma_done);
         drain(mma_done, 0, p);
       }
-    }
-  } else {
-    // ---- accumulators ----
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kHoldRegs));
-    constexpr int kCols = C::kCols, kChunks = kCols / 32;
-    const int e = warp - kRoleWarps, quarter = warp & 3, half = e >> 2;
-    float* const bias_s = bias_copies + e * kCols;
-    const int64_t w_blocks = (p.N + 127) / 128;
-    int buf = 0;
-    uint32_t buf_phase = 0;
-    bool ok = true;
-    for (int ct = cid; ct < num_ctiles && ok; ct += ncl) {
-      const int64_t row = (int64_t)(ct % groups_m * kCM + rank) * kBM + quarter * 32 + lane;
-      const int64_t col0 = (int64_t)(ct / groups_m) * kBN + half * kCols;
-      const bool row_in = row < p.M;
-      __syncwarp();   // the tile before has read its biases
+    } else if (warp == 2) {
+      // ---- scales: S_A S_W of a block for the tile's rows, a few blocks ahead of their use ----
+      const int64_t w_blocks = (p.N + 127) / 128;
+      int buf = 0;
+      uint32_t buf_phase = 0;
+      bool ok = true;
+      for (int ct = cid; ct < num_ctiles && ok; ct += ncl) {
+        const int64_t row0 = (int64_t)(ct % groups_m * kCM + rank) * kBM + lane;
+        const int64_t wb0 = (int64_t)(ct / groups_m) * C::kWBlocks;
+        constexpr int kAhead = 4;
+        float ra[kAhead][4], rw[kAhead][C::kWBlocks];
+        auto load = [&](int u, int kb) {
+          kb = min(kb, num_kb - 1);
 #pragma unroll
-      for (int c = 0; c < kChunks; ++c) {
-        const int64_t n = col0 + c * 32 + lane;
-        bias_s[c * 32 + lane] = p.bias != nullptr && n < p.N ? bf16_lo(__ldg(p.bias + n)) : 0.0f;
-      }
-      __syncwarp();
-      const float* const sa = p.sa + (row_in ? row : 0);
-      const float* const sw = p.sw + min(col0 >> 7, w_blocks - 1);
-      float2 acc[kChunks][16];
+          for (int i = 0; i < 4; ++i) ra[u][i] = __ldg(p.sa + kb * p.M + min(row0 + 32 * i, p.M - 1));
 #pragma unroll
-      for (int c = 0; c < kChunks; ++c)
+          for (int i = 0; i < C::kWBlocks; ++i) rw[u][i] = __ldg(p.sw + kb * w_blocks + min(wb0 + i, w_blocks - 1));
+        };
 #pragma unroll
-        for (int i = 0; i < 16; ++i) acc[c][i] = make_float2(0.0f, 0.0f);
-      // scales three blocks ahead of their use
-      constexpr int kAhead = 4;
-      float ra[kAhead], rw[kAhead];
+        for (int u = 0; u < kAhead - 1; ++u) load(u, u);
+        for (int kb0 = 0; kb0 < num_kb && ok; kb0 += kAhead) {
 #pragma unroll
-      for (int i = 0; i < kAhead - 1; ++i) {
-        const int kb = min(i, num_kb - 1);
-        ra[i] = __ldg(sa + kb * p.M);
-        rw[i] = __ldg(sw + kb * w_blocks);
-      }
-      for (int kb0 = 0; kb0 < num_kb && ok; kb0 += kAhead) {
+          for (int u = 0; u < kAhead; ++u) {
+            if (kb0 + u < num_kb && ok) {
+              load((u + kAhead - 1) % kAhead, kb0 + u + kAhead - 1);
+              if (!mbar_wait_warp(&tmem_empty[buf], buf_phase ^ 1u, ctl)) {
+                ok = false;
+              } else {
+                float* const s = scales + buf * C::kWBlocks * kBM + lane;
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-          if (kb0 + u < num_kb && ok) {
-            const int next = min(kb0 + u + kAhead - 1, num_kb - 1);
-            ra[(u + kAhead - 1) % kAhead] = __ldg(sa + next * p.M);
-            rw[(u + kAhead - 1) % kAhead] = __ldg(sw + next * w_blocks);
-            if (!mbar_wait_warp(&tmem_full[buf], buf_phase, ctl)) {
-              ok = false;
-            } else {
-              tc_fence_after();
-              const float2 s = splat(__fmul_rn(ra[u], rw[u]));
-              const uint32_t t = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(buf * kBN + half * kCols);
-              uint32_t v[2][32];
-              tmem_ld32(t, v[0]);
-              tmem_ld_wait();
+                for (int w = 0; w < C::kWBlocks; ++w)
 #pragma unroll
-              for (int c = 0; c < kChunks; ++c) {
-                if (c + 1 < kChunks) tmem_ld32(t + 32 * (c + 1), v[(c + 1) & 1]);
-                if (c + 1 == kChunks) {   // the buffer goes back to the MMAs
-                  tc_fence_before();
-                  __syncwarp();
-                  if (lane == 0) {
-                    if (kPair && rank == 1)
-                      mbar_arrive_cluster(mapa_shared(&tmem_empty[buf], 0));
-                    else
-                      mbar_arrive(&tmem_empty[buf]);
-                  }
+                  for (int i = 0; i < 4; ++i) s[w * kBM + 32 * i] = __fmul_rn(ra[u][i], rw[u][w]);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&tmem_full[buf]);
+                if (++buf == C::kBuffers) {
+                  buf = 0;
+                  buf_phase ^= 1u;
                 }
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                  acc[c][i] = fma2(make_float2(__uint_as_float(v[c & 1][2 * i]), __uint_as_float(v[c & 1][2 * i + 1])), s,
-                                   acc[c][i]);
-                if (c + 1 < kChunks) tmem_ld_wait();
-              }
-              if (++buf == C::kBuffers) {
-                buf = 0;
-                buf_phase ^= 1u;
               }
             }
           }
         }
       }
+    }
+  } else {
+    // ---- accumulators ----
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::kHoldRegs));
+    constexpr int kChunks = kCols / 32;
+    const int e = warp - kRoleWarps, quarter = warp & 3, part = e >> 2;   // lanes, columns
+    const uint32_t bias_s = smem_u32(bias_copies) + (uint32_t)(e * kCols * 2);
+    int buf = 0;
+    uint32_t buf_phase = 0;
+    bool ok = true;
+    for (int ct = cid; ct < num_ctiles && ok; ct += ncl) {
+      const int64_t row = (int64_t)(ct % groups_m * kCM + rank) * kBM + quarter * 32 + lane;
+      const int64_t col0 = (int64_t)(ct / groups_m) * kBN + part * kCols;
+      const bool row_in = row < p.M;
+      if (p.bias != nullptr) {   // read at the tile's end
+        __syncwarp();            // (the tile before has read its own)
+        if (8 * lane < kCols && col0 + 8 * lane < p.N) cp_async16(bias_s + 16 * lane, p.bias + col0 + 8 * lane);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+      }
+      float2 acc[kChunks][16];
+#pragma unroll
+      for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[c][i] = make_float2(0.0f, 0.0f);
+      for (int kb = 0; kb < num_kb; ++kb) {
+        if (!mbar_wait_warp(&tmem_full[buf], buf_phase, ctl)) {
+          ok = false;
+          break;
+        }
+        tc_fence_after();
+        const uint32_t t = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(buf * kBN + part * kCols);
+        uint32_t v[32];
+        tmem_ld32(t, v);
+        float scale;
+        asm volatile("ld.shared.f32 %0, [%1];"
+                     : "=f"(scale)
+                     : "r"(smem_u32(scales + (buf * C::kWBlocks + part * kCols / 128) * kBM + quarter * 32 + lane)));
+        const float2 s = splat(scale);
+        tmem_ld_wait();
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            acc[c][i] = fma2(make_float2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])), s, acc[c][i]);
+          if (c + 1 < kChunks) {
+            tmem_ld32(t + 32 * (c + 1), v);
+            tmem_ld_wait();
+          }
+          if (c + 2 == kChunks) {   // the buffer goes back to the MMAs
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&tmem_empty[buf]);
+          }
+        }
+        if (++buf == C::kBuffers) {
+          buf = 0;
+          buf_phase ^= 1u;
+        }
+      }
       if (!ok) break;
       // ---- the tile's end: N % 64 == 0, so 32 columns are wholly inside or outside ----
+      if (p.bias != nullptr) {
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        __syncwarp();
+      }
 #pragma unroll
       for (int c = 0; c < kChunks; ++c) {
         const int64_t n = col0 + c * 32;
@@ -371,10 +393,13 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         if (p.bias != nullptr) {
 #pragma unroll
-          for (int i = 0; i < 16; i += 2) {
-            const float4 b = *reinterpret_cast<const float4*>(bias_s + c * 32 + 2 * i);
-            acc[c][i] = add2(acc[c][i], make_float2(b.x, b.y));
-            acc[c][i + 1] = add2(acc[c][i + 1], make_float2(b.z, b.w));
+          for (int i = 0; i < 16; i += 4) {
+            uint32_t w[4];
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                         : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
+                         : "r"(bias_s + c * 64 + 4 * i));
+#pragma unroll
+            for (int k = 0; k < 4; ++k) acc[c][i + k] = add2(acc[c][i + k], make_float2(bf16_lo(w[k]), bf16_hi(w[k])));
           }
         }
         activate(acc[c], p.act);
@@ -396,25 +421,22 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
   }
 
-  // No CTA of a pair may exit while the peer can still arrive on its barriers.
+  // No CTA of a cluster may exit while the peer can still copy into it or arrive on its barriers.
   __syncwarp();
   tc_fence_before();
-  if (kPair)
+  if (kShare)
     cluster_sync_relaxed();
   else
     __syncthreads();
   if (warp == 1) {
     tc_fence_after();
-    if (kPair)
-      tmem_dealloc_pair(tmem_base, 512);
-    else
-      tmem_dealloc(tmem_base, 512);
+    tmem_dealloc(tmem_base, 512);
   }
 }
 
-template <int kBN, bool kPair>
+template <int kBN, bool kShare>
 cudaError_t launch_cfg(const GemmArgs& a, cudaStream_t s, Device dev, unsigned* err, uint64_t timeout_ns) {
-  using C = BlockCfg<kBN, kPair>;
+  using C = BlockCfg<kBN, kShare>;
   constexpr int kCM = C::kCM;
   CUtensorMap ta, tb;
   if (encode_tensor_map_codes(&ta, a.a_codes, (uint64_t)a.K, (uint64_t)a.M, kBM / C::kSplit) != CUDA_SUCCESS ||
@@ -435,7 +457,7 @@ cudaError_t launch_cfg(const GemmArgs& a, cudaStream_t s, Device dev, unsigned* 
   p.r_v8 = ((reinterpret_cast<uintptr_t>(a.residual) | (uintptr_t)(a.residual_stride * 2)) & 31u) == 0 ? 1 : 0;
   p.err = err;
   p.timeout_ns = timeout_ns;
-  auto kern = gemm_block_kernel<kBN, kPair>;
+  auto kern = gemm_block_kernel<kBN, kShare>;
   cudaLaunchConfig_t cfg{};
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -444,7 +466,7 @@ cudaError_t launch_cfg(const GemmArgs& a, cudaStream_t s, Device dev, unsigned* 
   attr[0].val.clusterDim.z = 1;
   attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[1].val.programmaticStreamSerializationAllowed = 1;
-  cfg.blockDim = dim3(kThreads, 1, 1);
+  cfg.blockDim = dim3(C::kThreads, 1, 1);
   cfg.dynamicSmemBytes = C::kSmem;
   cfg.stream = s;
   cfg.attrs = attr;
