@@ -27,7 +27,6 @@ namespace qlin {
 namespace {
 
 constexpr int kWarps = 4;
-constexpr int kGroup = 16;   // CTAs whose parts are joined at a time
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool in) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(in ? 16 : 0) : "memory");
@@ -101,8 +100,75 @@ struct AttnCfg {
   static_assert(kRow % 64 == 0, "K is read in 64-byte chunks");
 };
 
+// An item that other CTAs share: its rows, and the first and last of its CTAs.
+struct Unfinished {
+  int64_t token0;
+  int row0, head0, rows, first, last;
+};
+
+// The rows of an item (few), whose parts the CTAs from, from + step, ... to left in the workspace
+// (first: the item's first CTA), joined in the order of the keys: to the output, or to from's part
+// in place.  What it costs is waiting for L2: a thread has four elements of 16 parts and their
+// maxima and sums on their way at a time, and meets no other.  stat: kRows of them in shared memory.
+constexpr int kJoin = 16;
+template <int kRows, int kD>
+__device__ __forceinline__ void join_few(const AttnParams& p, const Unfinished& u, int from, int to, int step,
+                                         bool output, float v_scale, float2* stat) {
+  constexpr int kThreads = kWarps * 32;
+  const int d4s = p.head_dim / 4, items = u.rows * d4s, parts = (to - from) / step + 1;
+  for (int i = threadIdx.x; i < items; i += kThreads) {
+    const int row = i / d4s, d = i - row * d4s << 2;
+    float m = -INFINITY, l = 0.0f;
+    float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (int q0 = 0; q0 < parts; q0 += kJoin) {
+      float4 v[kJoin];
+      float2 ml[kJoin];
+      // (past the last part its own again, with a maximum of minus infinity: no branch between the loads)
+#pragma unroll
+      for (int k = 0; k < kJoin; ++k) {
+        const int64_t at = part_row<kRows>(from + min(q0 + k, parts - 1) * step, u.first, row);
+        ml[k] = __ldcg(&p.part_ml[at]);
+        v[k] = __ldcg(reinterpret_cast<const float4*>(p.part + at * kD + d));
+      }
+      float now = m;
+#pragma unroll
+      for (int k = 0; k < kJoin; ++k) {
+        if (q0 + k >= parts) ml[k].x = -INFINITY;
+        now = fmaxf(now, ml[k].x);
+      }
+      const float base = now == -INFINITY ? 0.0f : now, keep = exp2_fast(m - base);
+      l *= keep;
+      o = make_float4(o.x * keep, o.y * keep, o.z * keep, o.w * keep);
+#pragma unroll
+      for (int k = 0; k < kJoin; ++k) {
+        const float w = exp2_fast(ml[k].x - base);
+        if (w != 0.0f) {   // (a weight of 0 takes no part of what lies there)
+          l = fmaf(ml[k].y, w, l);
+          o = make_float4(fmaf(v[k].x, w, o.x), fmaf(v[k].y, w, o.y), fmaf(v[k].z, w, o.z), fmaf(v[k].w, w, o.w));
+        }
+      }
+      m = now;
+    }
+    if (output) {
+      const int r = u.row0 + row;
+      const int64_t token = u.token0 + r / p.group;
+      const int head = u.head0 + r % p.group;
+      const float inv = l == 0.0f ? 0.0f : v_scale / l;
+      store_out4(p, token, head, d, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
+      if (p.lse != nullptr && d == 0) p.lse[token * p.lse_token + head] = log_sum(m, l);
+    } else {
+      *reinterpret_cast<float4*>(p.part + part_row<kRows>(from, u.first, row) * kD + d) = o;
+      if (d == 0) stat[row] = make_float2(m, l);
+    }
+  }
+  if (!output) {
+    __syncthreads();   // the maxima and sums have been read
+    if ((int)threadIdx.x < u.rows) p.part_ml[part_row<kRows>(from, u.first, threadIdx.x)] = stat[threadIdx.x];
+  }
+}
+
 template <CacheKind kKind, int kD, int kM>
-__global__ void __launch_bounds__(kWarps * 32, (AttnCfg<kKind, kD, kM>::kCtas)) attn_kernel(const AttnParams p) {
+__global__ void __launch_bounds__(kWarps * 32, (AttnCfg<kKind, kD, kM>::kCtas)) attn_kernel(const __grid_constant__ AttnParams p) {
   using C = AttnCfg<kKind, kD, kM>;
   constexpr bool kFp8 = kKind == CacheKind::kE4m3, kF16 = kKind != CacheKind::kBf16;
   constexpr int kKeys = C::kKeys, kNT = kKeys / 8, kDT = kD / 8, kRows = C::kRows;
@@ -112,6 +178,7 @@ __global__ void __launch_bounds__(kWarps * 32, (AttnCfg<kKind, kD, kM>::kCtas)) 
   __shared__ unsigned ok_bits[kWarps][C::kStages];
   __shared__ float2 warp_ml[kWarps][kRows];
   __shared__ unsigned last_flag;
+  __shared__ Unfinished unfinished[2];   // the run's first item and its last
   __shared__ RunScratch scratch;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
 
@@ -129,30 +196,32 @@ __global__ void __launch_bounds__(kWarps * 32, (AttnCfg<kKind, kD, kM>::kCtas)) 
   // ---- loads: lane r < kKeys finds the page of the warp's key r, one tile ahead ----
   Cursor ahead = cur;
   int64_t left = run.end - run.begin;   // tiles to fetch
-  int page = -1, page_slot = 0, fetch_h = 0;
-  bool key_in = false;
+  struct Place {
+    bool in;
+    int page, slot, h;
+  };
   auto fetch = [&] {
-    key_in = false;
-    page = -1;
-    if (left <= 0) return;
+    Place f{false, -1, 0, 0};
+    if (left <= 0) return f;
     const int64_t key = (int64_t)ahead.tile * C::kTile + warp * kKeys + lane;
     int index;
-    fetch_h = ahead.h;
-    if (lane < kKeys && key < ahead.s.keys && cache_place(key, p.page_size, p.table_width, &index, &page_slot)) {
-      page = p.table[ahead.b * p.table_stride + index];
-      key_in = true;
+    f.h = ahead.h;
+    if (lane < kKeys && key < ahead.s.keys && cache_place(key, p.page_size, p.table_width, &index, &f.slot)) {
+      f.page = p.table[ahead.b * p.table_stride + index];
+      f.in = true;
     }
     --left;
     if (left > 0) advance<kRows, C::kTile>(p, ahead);
+    return f;
   };
-  auto issue = [&](int stage) {
-    const bool ok = key_in && page >= 0 && page < p.pages;
-    if (key_in && !ok) atomicExch(p.err, kErrInvalid);   // the keys of a bad page are not seen
+  auto issue = [&](int stage, const Place& f) {
+    const bool ok = f.in && f.page >= 0 && f.page < p.pages;
+    if (f.in && !ok) atomicExch(p.err, kErrInvalid);   // the keys of a bad page are not seen
     const unsigned bits = __ballot_sync(0xFFFFFFFFu, ok);
     if (lane == 0) ok_bits[warp][stage] = bits;
     if (bits != 0u) {
-      const int64_t ko = ok ? page * p.k_page + page_slot * p.k_slot + fetch_h * p.k_head : 0;
-      const int64_t vo = ok ? page * p.v_page + page_slot * p.v_slot + fetch_h * p.v_head : 0;
+      const int64_t ko = ok ? f.page * p.k_page + f.slot * p.k_slot + f.h * p.k_head : 0;
+      const int64_t vo = ok ? f.page * p.v_page + f.slot * p.v_slot + f.h * p.v_head : 0;
       const uint32_t kbase = smem_u32(smem + stage * C::kStageBytes + warp * C::kSlot), vbase = kbase + C::kKBytes;
 #pragma unroll
       for (int i = 0; i < kKeys * C::kPieces / 32; ++i) {
@@ -168,6 +237,7 @@ __global__ void __launch_bounds__(kWarps * 32, (AttnCfg<kKind, kD, kM>::kCtas)) 
     cp_async_commit();
   };
 
+  int num_unfinished = 0;
   // ---- one item's state ----
   uint32_t qf[kM][2][kQWords];
   float o[kM][kDT][4], m[kM][2], l[kM][2], mult[kM][2];
@@ -339,7 +409,7 @@ __global__ void __launch_bounds__(kWarps * 32, (AttnCfg<kKind, kD, kM>::kCtas)) 
             odd |= __vcmpgeu2(words[q] & 0x7FFF7FFFu, kF16 ? 0x7C007C00u : 0x7F807F80u) != 0u;
         }
       }
-      if (__any_sync(0xFFFFFFFFu, odd)) {
+      if (__builtin_expect(__any_sync(0xFFFFFFFFu, odd), 0)) {
         // in K's place, or where that is too small in the warp's place for its sums
         constexpr bool kFits = kRows * 4 <= C::kRow;
         static_assert(kFits || C::kOwnMerge, "room for the probabilities");
@@ -430,6 +500,7 @@ __global__ void __launch_bounds__(kWarps * 32, (AttnCfg<kKind, kD, kM>::kCtas)) 
     float* const own = reinterpret_cast<float*>(
         C::kOwnMerge ? smem + C::kStages * C::kStageBytes + warp * C::kMergeBytes
                      : smem + stage * C::kStageBytes + warp * C::kSlot);
+    const int rows = (int)min((int64_t)kRows, (int64_t)cur.s.fresh * p.group - (int64_t)cur.rt * kRows);
     __syncwarp();
 #pragma unroll
     for (int i = 0; i < kM; ++i)
@@ -440,15 +511,25 @@ __global__ void __launch_bounds__(kWarps * 32, (AttnCfg<kKind, kD, kM>::kCtas)) 
         sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 2);
         const int row = i * 16 + r * 8 + g;
         if (t == 0) warp_ml[warp][row] = make_float2(m[i][r], sum);
+        // adjacent elements in one store, the rows' columns permuted over the banks
+        if (row < rows) {
 #pragma unroll
-        for (int j = 0; j < kDT; ++j)
-#pragma unroll
-          for (int k = 0; k < 2; ++k) own[row * kD + column(j, k)] = o[i][j][2 * r + k];
+          for (int j = 0; j < kDT; j += 2) {
+            const float* const x = &o[i][j][2 * r];
+            const float* const y = &o[i][j + 1][2 * r];
+            if constexpr (kFp8) {
+              *reinterpret_cast<float4*>(own + row * kD + (column(j, 0) ^ ((row & 7) * 4))) =
+                  make_float4(x[0], y[0], x[1], y[1]);
+            } else {
+              *reinterpret_cast<float2*>(own + row * kD + (column(j, 0) ^ ((row & 7) * 4))) = make_float2(x[0], x[1]);
+              *reinterpret_cast<float2*>(own + row * kD + (column(j + 1, 0) ^ ((row & 7) * 4))) = make_float2(y[0], y[1]);
+            }
+          }
+        }
       }
     __syncthreads();
     const int64_t item0 = unit - cur.tile, item1 = item0 + cur.tiles - 1;   // the item's first and last unit
     const bool whole = item0 >= run.begin && item1 < run.end;
-    const int rows = (int)min((int64_t)kRows, (int64_t)cur.s.fresh * p.group - (int64_t)cur.rt * kRows);
     const int64_t part_row = (int64_t)(2 * blockIdx.x + (item0 < run.begin ? 0 : 1)) * kRows;
     const uint8_t* const sums = C::kOwnMerge ? smem + C::kStages * C::kStageBytes : smem + stage * C::kStageBytes;
     constexpr int kStep = C::kOwnMerge ? C::kMergeBytes : C::kSlot;
@@ -464,7 +545,7 @@ __global__ void __launch_bounds__(kWarps * 32, (AttnCfg<kKind, kD, kM>::kCtas)) 
       for (int w = 0; w < kWarps; ++w) {
         const float2 ml = warp_ml[w][row];
         const float f = exp2_fast(ml.x - base);
-        const float4 x = *reinterpret_cast<const float4*>(sums + w * kStep + (row * kD + d) * 4);
+        const float4 x = *reinterpret_cast<const float4*>(sums + w * kStep + (row * kD + (d ^ ((row & 7) * 4))) * 4);
         sum = fmaf(ml.y, f, sum);
         v = make_float4(fmaf(x.x, f, v.x), fmaf(x.y, f, v.y), fmaf(x.z, f, v.z), fmaf(x.w, f, v.w));
       }
@@ -481,39 +562,24 @@ __global__ void __launch_bounds__(kWarps * 32, (AttnCfg<kKind, kD, kM>::kCtas)) 
       }
     }
     if (!whole) {
-      const int first = (int)split_owner(item0, run.total, run.ctas), last = (int)split_owner(item1, run.total, run.ctas);
-      // whether this CTA is the last of `parties` to arrive
-      auto arrive = [&](unsigned* count, int parties) {
-        __threadfence();
-        __syncthreads();
-        if (threadIdx.x == 0) {
-          const bool all = atomicAdd(count, 1u) == (unsigned)(parties - 1);
-          if (all) *count = 0u;   // as it was before the call
-          __threadfence();
-          last_flag = all ? 1u : 0u;
-        }
-        __syncthreads();
-        return last_flag != 0u;
-      };
-      auto join = [&](int from, int to, int step, bool output) {
-        join_parts<kRows, kD, kThreads>(p, cur, first, from, to, step, output, v_scale, 0, rows, (int)threadIdx.x,
-                                        warp_ml[0], [] { __syncthreads(); });
-      };
-      const int groups = (last - first) / kGroup + 1, from = first + ((int)blockIdx.x - first) / kGroup * kGroup,
-                to = min(last, from + kGroup - 1);
-      if (arrive(&p.counts[from], to - from + 1)) {
-        join(from, to, 1, groups == 1);
-        if (groups > 1 && arrive(&p.counts[kMostCtas + first], groups)) join(first, last, kGroup, true);
+      if (threadIdx.x == 0) {
+        Unfinished& u = unfinished[num_unfinished];
+        u = {cur.s.first, cur.rt * kRows, cur.h * p.group, rows, (int)split_owner(run.split, item0),
+             (int)split_owner(run.split, item1)};
       }
+      ++num_unfinished;
     }
     __syncthreads();
   };
 
-  fetch();
+  Place next;
+  {
+    Place early[C::kStages - 1];   // (their table entries are on their way together)
 #pragma unroll
-  for (int s = 0; s < C::kStages - 1; ++s) {
-    issue(s);
-    fetch();
+    for (int s = 0; s < C::kStages - 1; ++s) early[s] = fetch();
+#pragma unroll
+    for (int s = 0; s < C::kStages - 1; ++s) issue(s, early[s]);
+    next = fetch();
   }
   bool fresh_item = true;
   int stage = 0;
@@ -521,8 +587,8 @@ __global__ void __launch_bounds__(kWarps * 32, (AttnCfg<kKind, kD, kM>::kCtas)) 
     if (fresh_item) begin_item();
     cp_async_wait<C::kStages - 2>();
     __syncwarp();
-    issue(stage == 0 ? C::kStages - 1 : stage - 1);
-    fetch();
+    issue(stage == 0 ? C::kStages - 1 : stage - 1, next);
+    next = fetch();
     compute(stage);
     const bool done = cur.tile + 1 == cur.tiles;
     if (done || unit + 1 == run.end) end_item(stage, unit);
@@ -532,7 +598,41 @@ __global__ void __launch_bounds__(kWarps * 32, (AttnCfg<kKind, kD, kM>::kCtas)) 
     __syncwarp();
   }
   cp_async_wait<0>();
+  // The unfinished items, now that the registers are free: the last CTA of a group to arrive joins
+  // the group's parts, the last group's the groups'.
+  for (int i = 0; i < num_unfinished; ++i) {
+    const Unfinished u = unfinished[i];
+    // a group: as many parts as a CTA joins in about the time that another level takes
+    const int per4 = u.rows * p.head_dim / (4 * kThreads);
+    const int group = per4 <= 1 ? 64 : per4 <= 4 ? 32 : 16;
+    const int groups = (u.last - u.first) / group + 1;
+    int from = u.first + ((int)blockIdx.x - u.first) / group * group, to = min(u.last, from + group - 1), step = 1;
+    unsigned* count = &p.counts[from];
+    int parties = to - from + 1;
+    for (;;) {
+      __syncthreads();
+      if (threadIdx.x == 0) {
+        __threadfence();   // (the CTA's stores, which the barrier orders before)
+        const bool all = atomicAdd(count, 1u) == (unsigned)(parties - 1);
+        if (all) *count = 0u;   // as it was before the call
+        __threadfence();
+        last_flag = all ? 1u : 0u;
+      }
+      __syncthreads();
+      if (last_flag == 0u) break;
+      const bool output = groups == 1 || step > 1;
+      join_few<kRows, kD>(p, u, from, to, step, output, v_scale, warp_ml[0]);
+      if (output) break;
+      count = &p.counts[kMostCtas + u.first];
+      parties = groups;
+      from = u.first;
+      to = u.last;
+      step = group;
+    }
+    __syncthreads();
+  }
 }
+
 
 template <CacheKind kKind, int kD, int kM>
 cudaError_t launch_attn(AttnParams p, cudaStream_t s, Device dev) {
@@ -556,7 +656,7 @@ cudaError_t launch_attn(AttnParams p, cudaStream_t s, Device dev) {
   const int ctas = (int)std::min<int64_t>((int64_t)setup.ctas * dev.num_sms, most);
   p.part_ml = reinterpret_cast<float2*>(reinterpret_cast<uint8_t*>(p.counts) + kCountBytes);
   p.part = reinterpret_cast<float*>(p.part_ml + (int64_t)2 * C::kRows * ctas);
-  p.least = std::max(1, 256 / C::kTile);
+  p.least = std::max(1, 128 / C::kTile);
   return launch_pdl(attn_kernel<kKind, kD, kM>, dim3((unsigned)ctas), kWarps * 32, C::kSmem, s, p);
 }
 

@@ -697,7 +697,7 @@ __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const AttnParam
   const int all = (int)min((int64_t)kRows, (int64_t)cur.s.fresh * p.group - (int64_t)cur.rt * kRows);
   const int row0 = (int)blockIdx.y * kJoinRows, rows = min(kJoinRows, all - row0);
   if (rows <= 0) return;
-  join_parts<kRows, 64 * kDC, kJoinThreads>(p, cur, cta, cta, (int)split_owner(item1, run.total, run.ctas), 1, true, 1.0f,
+  join_parts<kRows, 64 * kDC, kJoinThreads>(p, cur, cta, cta, (int)split_owner(run.split, item1), 1, true, 1.0f,
                                             row0, rows, (int)threadIdx.x, stat, [] { __syncthreads(); });
 }
 

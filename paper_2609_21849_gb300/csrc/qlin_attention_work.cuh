@@ -20,10 +20,15 @@ __device__ __forceinline__ CacheSeq read_seq(const AttnParams& p, int b) {
 }
 
 template <int kRows, int kTile>
-__device__ __forceinline__ void open_seq(const AttnParams& p, Cursor& c) {
-  c.s = read_seq<kRows, kTile>(p, c.b);
+__device__ __forceinline__ void size_seq(const AttnParams& p, Cursor& c) {
   c.tiles = (int)((c.s.keys + kTile - 1) / kTile);
   c.row_tiles = (int)(((int64_t)c.s.fresh * p.group + kRows - 1) / kRows);
+}
+
+template <int kRows, int kTile>
+__device__ __forceinline__ void open_seq(const AttnParams& p, Cursor& c) {
+  c.s = read_seq<kRows, kTile>(p, c.b);
+  size_seq<kRows, kTile>(p, c);
 }
 
 // The next tile; past the last sequence the cursor stays at its end.
@@ -48,75 +53,105 @@ __device__ __forceinline__ int64_t seq_units(const AttnParams& p, const CacheSeq
 
 // The CTA's run of tiles and the cursor at its begin; the same in all threads.
 struct Run {
-  int64_t total, begin, end;
-  int ctas;
+  int64_t begin, end;
+  Split split;
 };
 struct RunScratch {   // in shared memory
-  int64_t warp_sum[32];
-  int64_t found_at;
-  int found_b;
+  int64_t warp_sum[32], warp_all[32];
+  CacheSeq s;
+  int64_t at;
+  int b;
 };
 
-// (kLast: the cursor at its last unit.)
+// (kLast: the cursor at its last unit.)  Up to kThreads sequences take one pass over the counts
+// and two barriers; more, a second pass.
 template <int kRows, int kTile, int kThreads, bool kLast = false>
 __device__ __forceinline__ Run find_run(const AttnParams& p, Cursor& c, int cta, int ctas, RunScratch& scratch) {
-  auto& warp_sum = scratch.warp_sum;
+  constexpr int kWarps = kThreads / 32;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  Run r{0, 0, 0, 1};
-  int64_t mine = 0, first = 0;
+  Run r{0, 0, {0, 0}};
+  CacheSeq mine{};
+  int64_t first = 0, all = 0;
   bool bad = false;
   for (int b = threadIdx.x; b < p.sequences; b += kThreads) {
     const CacheSeq s = read_seq<kRows, kTile>(p, b);
     bad |= s.bad;
     const int64_t u = seq_units<kRows, kTile>(p, s);
-    if (b < kThreads) first = u;
-    mine += u;
+    if (b < kThreads) {
+      first = u;
+      mine = s;
+    }
+    all += u;
   }
   if (bad && cta == 0) atomicExch(p.err, kErrInvalid);
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xFFFFFFFFu, mine, o);
-  if (lane == 0) warp_sum[warp] = mine;
-  __syncthreads();
-  for (int w = 0; w < kThreads / 32; ++w) r.total += warp_sum[w];
-  if (r.total == 0) return r;
-  r.ctas = (int)split_ctas(r.total, ctas, p.least);
-  if (cta >= r.ctas) return r;
-  r.begin = split_begin(cta, r.total, r.ctas);
-  r.end = split_begin(cta + 1, r.total, r.ctas);
-  const int64_t want = kLast ? r.end - 1 : r.begin;
-  int64_t run = 0;
-  for (int b0 = 0; b0 < p.sequences; b0 += kThreads) {
-    const int b = b0 + threadIdx.x;
-    int64_t u = first;
-    if (b0 > 0) u = b < p.sequences ? seq_units<kRows, kTile>(p, read_seq<kRows, kTile>(p, b)) : 0;
-    int64_t incl = u;
+  // the sequences up to this thread's, and all
+  auto scan = [&](int64_t u) {
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const int64_t n = __shfl_up_sync(0xFFFFFFFFu, incl, o);
-      if (lane >= o) incl += n;
+      const int64_t n = __shfl_up_sync(0xFFFFFFFFu, u, o);
+      if (lane >= o) u += n;
     }
-    __syncthreads();   // warp_sum's last readers
-    if (lane == 31) warp_sum[warp] = incl;
-    __syncthreads();
-    int64_t base = run;
-    for (int w = 0; w < kThreads / 32; ++w) {
-      if (w < warp) base += warp_sum[w];
-      run += warp_sum[w];
-    }
-    if (base + incl - u <= want && want < base + incl) {
-      scratch.found_b = b;
-      scratch.found_at = base + incl - u;
-    }
-    if (run > want) break;
+    return u;
+  };
+  int64_t incl = scan(first);
+  if (lane == 31) scratch.warp_sum[warp] = incl;
+  if (p.sequences > kThreads) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) all += __shfl_xor_sync(0xFFFFFFFFu, all, o);
+    if (lane == 0) scratch.warp_all[warp] = all;
   }
   __syncthreads();
-  c.b = scratch.found_b;
-  open_seq<kRows, kTile>(p, c);
-  int64_t at = want - scratch.found_at;
-  c.tile = (int)(at % c.tiles);
-  at /= c.tiles;
-  c.rt = (int)(at % c.row_tiles);
-  c.h = (int)(at / c.row_tiles);
+  int64_t base = 0, run = 0;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) {
+    if (w < warp) base += scratch.warp_sum[w];
+    run += scratch.warp_sum[w];
+  }
+  int64_t total = run;
+  if (p.sequences > kThreads) {
+    total = 0;
+    for (int w = 0; w < kWarps; ++w) total += scratch.warp_all[w];
+  }
+  if (total == 0) return r;
+  const int64_t working = split_ctas(total, ctas, p.least);
+  if (cta >= working) return r;
+  r.split = split_evenly(total, working);
+  r.begin = split_begin(r.split, cta);
+  r.end = split_begin(r.split, cta + 1);
+  const int64_t want = kLast ? r.end - 1 : r.begin;
+  auto found = [&](int b, const CacheSeq& s, int64_t before) {
+    scratch.b = b;
+    scratch.s = s;
+    scratch.at = want - before;
+  };
+  if (base + incl - first <= want && want < base + incl) found(threadIdx.x, mine, base + incl - first);
+  for (int b0 = kThreads; run <= want; b0 += kThreads) {   // (total above want: some sequence has it)
+    const int b = b0 + threadIdx.x;
+    int64_t u = 0;
+    if (b < p.sequences) {
+      mine = read_seq<kRows, kTile>(p, b);
+      u = seq_units<kRows, kTile>(p, mine);
+    }
+    incl = scan(u);
+    __syncthreads();   // warp_sum's last readers
+    if (lane == 31) scratch.warp_sum[warp] = incl;
+    __syncthreads();
+    base = run;
+    for (int w = 0; w < kWarps; ++w) {
+      if (w < warp) base += scratch.warp_sum[w];
+      run += scratch.warp_sum[w];
+    }
+    if (base + incl - u <= want && want < base + incl) found(b, mine, base + incl - u);
+  }
+  __syncthreads();
+  c.b = scratch.b;
+  c.s = scratch.s;
+  size_seq<kRows, kTile>(p, c);
+  const int64_t at = scratch.at;
+  const int64_t item = div_small(at, c.tiles);
+  c.tile = (int)(at - item * c.tiles);
+  c.h = (int)div_small(item, c.row_tiles);
+  c.rt = (int)(item - (int64_t)c.h * c.row_tiles);
   return r;
 }
 

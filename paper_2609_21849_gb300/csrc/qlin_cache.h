@@ -12,11 +12,16 @@
 
 namespace qlin {
 
+// a / b of what is not negative, in 32 bits where it fits (a tenth of the time on the device).
+QLIN_HD int64_t div_small(int64_t a, int64_t b) {
+  return ((uint64_t)a | (uint64_t)b) >> 32 == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
+}
+
 // Where the cache of one sequence holds its token `at`: its page's number in the table
 // row, and the slot in that page.  False past the table's row.
 QLIN_HD bool cache_place(int64_t at, int page_size, int table_width, int* index, int* slot) {
   if (at < 0 || at >= (int64_t)page_size * table_width) return false;
-  *index = (int)(at / page_size);   // (the product fits 62 bits, the quotient 31)
+  *index = (int)div_small(at, page_size);   // (the product fits 62 bits, the quotient 31)
   *slot = (int)(at - (int64_t)*index * page_size);
   return true;
 }
@@ -48,17 +53,30 @@ QLIN_HD CacheSeq cache_seq(int64_t start, int64_t end, int64_t cached, int64_t t
   return s;
 }
 
-// An even split of `total` units among `ctas`: CTA c takes [begin(c), begin(c + 1)).
-// (total below 2^43, ctas below 2^20)
-QLIN_HD int64_t split_begin(int64_t c, int64_t total, int64_t ctas) { return c * total / ctas; }
-
-// The CTA that takes unit t.
-QLIN_HD int64_t split_owner(int64_t t, int64_t total, int64_t ctas) { return ((t + 1) * ctas - 1) / total; }
+// An even split of `total` units among `ctas`: the first `rest` of them take per + 1, the others
+// per.
+struct Split {
+  int64_t per, rest;
+};
 
 // How many of `ctas` work where each should have `least` units.
 QLIN_HD int64_t split_ctas(int64_t total, int64_t ctas, int64_t least) {
-  const int64_t want = (total + least - 1) / least;
+  const int64_t want = div_small(total + least - 1, least);
   return want < 1 ? 1 : want < ctas ? want : ctas;
+}
+
+QLIN_HD Split split_evenly(int64_t total, int64_t ctas) {
+  const int64_t per = div_small(total, ctas);
+  return {per, total - per * ctas};
+}
+
+// CTA c takes [begin(c), begin(c + 1)).
+QLIN_HD int64_t split_begin(const Split& s, int64_t c) { return c * s.per + (c < s.rest ? c : s.rest); }
+
+// The CTA that takes unit t.
+QLIN_HD int64_t split_owner(const Split& s, int64_t t) {
+  const int64_t longer = s.rest * (s.per + 1);
+  return t < longer ? div_small(t, s.per + 1) : s.rest + div_small(t - longer, s.per);
 }
 
 }  // namespace qlin

@@ -193,11 +193,15 @@ __global__ void __launch_bounds__(kMaxWarps * 32) few_kernel(const FewParams p) 
   float acc[kRowTiles][kTiles][4] = {};
   uint4 va[kUnroll][kRowTiles][2], vb[kUnroll][kTiles];
   uint16_t sa[kUnroll][kRowTiles][2], sb[kUnroll][kTiles];
-  // FP8 block: a chunk's scale of these rows of W, and of the lane's tokens 2 t and 2 t + 1 of each tile
-  float block_w[kUnroll], block_a[kUnroll][kTiles][2];
+  // FP8 block: a pair of chunks' scale of these rows of W, and of the lane's tokens 2 t and 2 t + 1 of
+  // each tile; their products before the scales
+  float block_w[kUnroll / 2], block_a[kUnroll / 2][kTiles][2], part_sum[kBlocks ? kRowTiles : 1][kBlocks ? kTiles : 1][4];
   const int64_t w_blocks = (p.N + 127) / 128;
-  const int first = rank * warps + warp;
-  int left = (chunks - first + stride - 1) / stride;   // chunks to load
+  // (FP8 block: chunks come in pairs, a block of 128 that has one scale, so that a pair's scales are
+  // loaded and applied once)
+  constexpr int kGroup = kBlocks ? 2 : 1;
+  const int first = (rank * warps + warp) * kGroup;
+  int left = (chunks - first + kGroup * stride - 1) / (kGroup * stride) * kGroup;   // chunks to load
   int tail = kFp4 ? (int)(w_row - (int64_t)first * kChunk) - 16 * t : 0;   // bytes of the row from here
   const uint8_t* w = p.w + (n0 + g) * w_row + 16 * t + (int64_t)first * kChunk;
   const uint8_t *a[kTiles], *fa[kTiles], *fw[kRowTiles][2];
@@ -211,11 +215,13 @@ __global__ void __launch_bounds__(kMaxWarps * 32) few_kernel(const FewParams p) 
 #pragma unroll
   for (int h = 0; h < 2 * kRowTiles; ++h)
     fw[h / 2][h % 2] = kFp4 ? p.sfb + scale_offset(n0 + g + 8 * h, 8 * (int64_t)first + 2 * t, p.K) : nullptr;
-  const int step = stride * kChunk, fstep = stride * 1024;
+  const int fstep = stride * 1024;
   int chunk = first;
   auto load = [&](int u) {
-    // NVFP4 rows are multiples of 32 bytes: the last chunk may be half a chunk
-    const bool in = left > 0 && (!kFp4 || tail > 0);
+    // NVFP4 rows are multiples of 32 bytes: the last chunk may be half a chunk; a last block of 128
+    // may be one chunk
+    const bool in = left > 0 && (!kFp4 || tail > 0) && (!kBlocks || chunk < chunks);
+    const int step = kBlocks ? ((u & 1) == 0 ? kChunk : (2 * stride - 1) * kChunk) : stride * kChunk;
 #pragma unroll
     for (int h = 0; h < 2 * kRowTiles; ++h) {
       va[u][h / 2][h % 2] = make_uint4(0u, 0u, 0u, 0u);
@@ -238,16 +244,18 @@ __global__ void __launch_bounds__(kMaxWarps * 32) few_kernel(const FewParams p) 
       }
     }
     if constexpr (kBlocks) {
-      const int64_t kb = chunk >> 1;   // two chunks to a block of 128
-      block_w[u] = in ? __ldg(p.sdec_w + kb * w_blocks + (n0 >> 7)) : 0.0f;
+      if ((u & 1) == 1) {   // (the pair before is done with its own when its second chunk is multiplied)
+        const int64_t kb = chunk >> 1;
+        block_w[u / 2] = left > 0 ? __ldg(p.sdec_w + kb * w_blocks + (n0 >> 7)) : 0.0f;
 #pragma unroll
-      for (int j = 0; j < kTiles; ++j)
+        for (int j = 0; j < kTiles; ++j)
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          const int64_t m = m0 + j * 8 + 2 * t + k;
-          block_a[u][j][k] = in && m < p.M ? __ldg(p.sdec_a + kb * p.M + m) : 0.0f;
-        }
-      chunk += stride;
+          for (int k = 0; k < 2; ++k) {
+            const int64_t m = m0 + j * 8 + 2 * t + k;
+            block_a[u / 2][j][k] = left > 0 && m < p.M ? __ldg(p.sdec_a + kb * p.M + m) : 0.0f;
+          }
+      }
+      chunk += step / kChunk;
     }
     w += step;
     tail -= step;
@@ -297,16 +305,26 @@ __global__ void __launch_bounds__(kMaxWarps * 32) few_kernel(const FewParams p) 
         }
       };
       if constexpr (!kBlocks) products(acc);
-      if constexpr (kBlocks) {   // the chunk's products apart: their scales differ from the next one's
-        float part[kRowTiles][kTiles][4] = {};
-        products(part);
-#pragma unroll
-        for (int j = 0; j < kTiles; ++j) {
-          const float s[2] = {__fmul_rn(block_a[u][j][0], block_w[u]), __fmul_rn(block_a[u][j][1], block_w[u])};
+      if constexpr (kBlocks) {   // a block's products apart: its scales differ from the next one's
+        if ((u & 1) == 0) {
 #pragma unroll
           for (int i = 0; i < kRowTiles; ++i)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) acc[i][j][k] = __fmaf_rn(part[i][j][k], s[k & 1], acc[i][j][k]);
+            for (int j = 0; j < kTiles; ++j)
+#pragma unroll
+              for (int k = 0; k < 4; ++k) part_sum[i][j][k] = 0.0f;
+        }
+        products(part_sum);
+        if ((u & 1) == 1) {
+#pragma unroll
+          for (int j = 0; j < kTiles; ++j) {
+            const float s[2] = {__fmul_rn(block_a[u / 2][j][0], block_w[u / 2]),
+                                __fmul_rn(block_a[u / 2][j][1], block_w[u / 2])};
+#pragma unroll
+            for (int i = 0; i < kRowTiles; ++i)
+#pragma unroll
+              for (int k = 0; k < 4; ++k) acc[i][j][k] = __fmaf_rn(part_sum[i][j][k], s[k & 1], acc[i][j][k]);
+          }
         }
       }
     } else {

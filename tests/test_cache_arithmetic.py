@@ -31,9 +31,10 @@ int main() {
       long long total, ctas, least;
       std::scanf("%lld %lld %lld", &total, &ctas, &least);
       const long long n = split_ctas(total, ctas, least);
+      const Split s = split_evenly(total, n);
       std::printf("%lld", n);
-      for (long long c = 0; c <= n; ++c) std::printf(" %lld", (long long)split_begin(c, total, n));
-      for (long long t = 0; t < total; t += total / 997 + 1) std::printf(" %lld", (long long)split_owner(t, total, n));
+      for (long long c = 0; c <= n; ++c) std::printf(" %lld", (long long)split_begin(s, c));
+      for (long long t = 0; t < total; t += total / 997 + 1) std::printf(" %lld", (long long)split_owner(s, t));
       std::printf("\n");
     }
   }
