@@ -481,7 +481,7 @@ qlin_status qlin_linear_fp8_block(const qlin_fp8_block_t* A, const qlin_fp8_bloc
   Device dev;
   QLIN_TRY(device_state(&status, &dev));
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (a.K <= (int64_t)1 << 28 && few_tokens(false, a.M, a.N, a.K, dev.num_sms))
+  if (a.K <= (int64_t)1 << 28 && few_block_tokens(a.M, a.N, a.K, dev.num_sms))
     QLIN_CUDA(launch_few(a, s, dev));
   else
     QLIN_CUDA(launch_gemm_block(a, s, dev, status, timeout()));

@@ -24,6 +24,7 @@ namespace {
 constexpr int kBM = kTileM;
 constexpr int kRowBytes = kStageRowBytes;   // a block of K
 constexpr int kSteps = 4;                   // MMAs of 32 elements of a block
+constexpr int kRawSlots = 8;   // blocks whose scales are loaded ahead
 constexpr int kRoleWarps = 4, kCols = 64;   // columns of an epilogue thread: inside one 128-row block of W
 
 template <int kBN, bool kShare>
@@ -38,10 +39,12 @@ struct BlockCfg {
   static constexpr int kBiasBytes = kEpiWarps * kCols * 2;    // 16-bit, a copy per warp
   static constexpr int kBuffers = 512 / kBN;     // of block sums in tensor memory
   static constexpr int kWBlocks = kBN / 128;
-  static constexpr int kScaleBytes = kBuffers * kWBlocks * kBM * 4;   // of each buffer's block: [W's block][row]
-  static constexpr int kStagesRaw = (232448 - 1024 - 512 - kBiasBytes - kScaleBytes) / kStageBytes;
+  // scales: of each buffer's block, [W's block][row]; on their way, S_A of the rows and S_W
+  static constexpr int kScaleBytes = kBuffers * kWBlocks * kBM * 4, kRawSlot = kBM + 4;
+  static constexpr int kRawBytes = kRawSlots * kRawSlot * 4;
+  static constexpr int kStagesRaw = (232448 - 1024 - 512 - kBiasBytes - kScaleBytes - kRawBytes) / kStageBytes;
   static constexpr int kStages = kStagesRaw > 8 ? 8 : kStagesRaw;
-  static constexpr int kSmem = 1024 + kStages * kStageBytes + kBiasBytes + kScaleBytes + 512;
+  static constexpr int kSmem = 1024 + kStages * kStageBytes + kBiasBytes + kScaleBytes + kRawBytes + 512;
   // registers: the roles' warpgroup and those with accumulators
   static constexpr int kRoleRegs = kThreads == 640 ? 64 : 80, kHoldRegs = kThreads == 640 ? 104 : 128;
   static constexpr int kLaunchRegs = kThreads == 640 ? 96 : 112;
@@ -60,6 +63,7 @@ struct BlockParams {
   int64_t residual_stride;
   int act;
   int y_v8, r_v8;     // rows start on 32-byte boundaries
+  int split;          // kSplitK: CTAs of a cluster (2, 4 or 8)
   unsigned* err;
   uint64_t timeout_ns;
 };
@@ -76,6 +80,9 @@ __device__ __forceinline__ void drain(uint64_t* bar, uint32_t parity, const Bloc
   }
 }
 
+__device__ __forceinline__ void cp_async4(uint32_t dst, const void* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
@@ -109,7 +116,7 @@ __device__ __forceinline__ void store32(uint16_t* p, const uint32_t* v, bool wid
   }
 }
 
-template <int kBN, bool kShare>
+template <int kBN, bool kShare, bool kSplitK>
 __global__ void __launch_bounds__(BlockCfg<kBN, kShare>::kThreads, 1)
     gemm_block_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ CUtensorMap tmap_b,
                       const BlockParams p) {
@@ -120,7 +127,7 @@ __global__ void __launch_bounds__(BlockCfg<kBN, kShare>::kThreads, 1)
       reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   uint8_t* const bias_copies = smem + C::kStages * C::kStageBytes;
   float* const scales = reinterpret_cast<float*>(bias_copies + C::kBiasBytes);
-  uint64_t* full = reinterpret_cast<uint64_t*>(bias_copies + C::kBiasBytes + C::kScaleBytes);
+  uint64_t* full = reinterpret_cast<uint64_t*>(bias_copies + C::kBiasBytes + C::kScaleBytes + C::kRawBytes);
   uint64_t* empty = full + C::kStages;
   uint64_t* tmem_full = empty + C::kStages;
   uint64_t* tmem_empty = tmem_full + C::kBuffers;
@@ -148,18 +155,23 @@ __global__ void __launch_bounds__(BlockCfg<kBN, kShare>::kThreads, 1)
   if (warp == 0 && lane < 2) prefetch_tmap(lane == 0 ? &tmap_a : &tmap_b);
   if (warp == 1) tmem_alloc(tmem_slot, 512);
   tc_fence_before();
-  if (kShare)
-    cluster_sync();   // the peer's barriers exist before any copy completes on them
+  if (kShare || kSplitK)
+    cluster_sync();   // the peers' barriers exist before any copy completes on them
   else
     __syncthreads();
   tc_fence_after();
   const uint32_t tmem_base = __shfl_sync(0xFFFFFFFFu, *tmem_slot, 0);
   const WaitCtl ctl{abort_flag, p.err, p.timeout_ns};
+  static_assert(!kSplitK || !kShare, "a cluster shares a tile's K, or W");
   const int tiles_m = (int)((p.M + kBM - 1) / kBM), tiles_n = (int)((p.N + kBN - 1) / kBN);
   const int groups_m = (tiles_m + kCM - 1) / kCM;
   const int num_ctiles = groups_m * tiles_n;
-  const int cid = (int)blockIdx.x / kCM, ncl = (int)gridDim.x / kCM;
-  const int num_kb = (int)((p.K + kRowBytes - 1) / kRowBytes);
+  // kSplitK: the CTAs of a cluster take a tile's blocks of K in equal runs (split <= blocks)
+  const int splits = kSplitK ? p.split : 1;
+  const int krank = kSplitK ? __shfl_sync(0xFFFFFFFFu, (int)cluster_ctarank(), 0) : 0;
+  const int cid = (int)blockIdx.x / (kCM * splits), ncl = (int)gridDim.x / (kCM * splits);
+  const int all_kb = (int)((p.K + kRowBytes - 1) / kRowBytes);
+  const int kb0 = krank * all_kb / splits, num_kb = (krank + 1) * all_kb / splits - kb0;
   grid_dep_wait();
 
   if (warp < kRoleWarps) {
@@ -187,12 +199,12 @@ __global__ void __launch_bounds__(BlockCfg<kBN, kShare>::kThreads, 1)
             mbar_arrive_expect_tx(&full[stage], C::kStageBytes);
 #pragma unroll
             for (int b = 0; b < C::kSplit; ++b) {
-              tma_load_4d(sA + b * kARows * kRowBytes, &tmap_a, bar, kb * kRowBytes, a_row + b * kARows, 0, 0);
+              tma_load_4d(sA + b * kARows * kRowBytes, &tmap_a, bar, (kb0 + kb) * kRowBytes, a_row + b * kARows, 0, 0);
               if (kShare)
-                tma_load_4d_multicast(sW + b * kWRows * kRowBytes, &tmap_b, bar, kb * kRowBytes, w_row + b * kWRows, 0, 0,
+                tma_load_4d_multicast(sW + b * kWRows * kRowBytes, &tmap_b, bar, (kb0 + kb) * kRowBytes, w_row + b * kWRows, 0, 0,
                                       (uint16_t)3);
               else
-                tma_load_4d(sW + b * kWRows * kRowBytes, &tmap_b, bar, kb * kRowBytes, w_row + b * kWRows, 0, 0);
+                tma_load_4d(sW + b * kWRows * kRowBytes, &tmap_b, bar, (kb0 + kb) * kRowBytes, w_row + b * kWRows, 0, 0);
             }
           }
           ++issued;
@@ -229,7 +241,7 @@ __global__ void __launch_bounds__(BlockCfg<kBN, kShare>::kThreads, 1)
           const uint32_t sA = smem_u32(smem + stage * C::kStageBytes);
           const uint64_t adesc = sdesc_k128(sA), bdesc = sdesc_k128(sA + C::kABytes);
           const uint32_t d = tmem_base + (uint32_t)(buf * kBN);
-          const int steps = min(kSteps, k_steps - kb * kSteps);
+          const int steps = min(kSteps, k_steps - (kb0 + kb) * kSteps);
           if (elect_one()) {
 #pragma unroll
             for (int j = 0; j < kSteps; ++j) {
@@ -268,49 +280,71 @@ __global__ void __launch_bounds__(BlockCfg<kBN, kShare>::kThreads, 1)
         drain(mma_done, 0, p);
       }
     } else if (warp == 2) {
-      // ---- scales: S_A S_W of a block for the tile's rows, a few blocks ahead of their use ----
+      // ---- scales: S_A S_W of a block for the tile's rows ----
+      // Loaded by cp.async seven blocks ahead, across the tiles.  (Into registers, the loop waited for
+      // the loads it had just issued: 740 cycles a block, and the MMAs with it.)
       const int64_t w_blocks = (p.N + 127) / 128;
-      int buf = 0;
+      const uint32_t raw = smem_u32(scales) + (uint32_t)(C::kScaleBytes + lane * 4);
+      int next_ct = cid, next_kb = 0, next_slot = 0;
+      const float *next_a[4], *next_w = nullptr;
+      auto fetch = [&] {
+        if (next_ct < num_ctiles) {
+          if (next_kb == 0) {
+            const int64_t row0 = (int64_t)(next_ct % groups_m * kCM + rank) * kBM + lane;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) next_a[i] = p.sa + kb0 * p.M + min(row0 + 32 * i, p.M - 1);
+            next_w = p.sw + kb0 * w_blocks + min((int64_t)(next_ct / groups_m) * C::kWBlocks + min(lane, C::kWBlocks - 1), w_blocks - 1);
+          }
+          const uint32_t dst = raw + (uint32_t)(next_slot * C::kRawSlot * 4);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            cp_async4(dst + 128 * i, next_a[i]);
+            next_a[i] += p.M;
+          }
+          if (lane < C::kWBlocks) cp_async4(dst + 4 * kBM, next_w);
+          next_w += w_blocks;
+          if (++next_kb == num_kb) {
+            next_kb = 0;
+            next_ct += ncl;
+          }
+          if (++next_slot == kRawSlots) next_slot = 0;
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+      };
+      for (int i = 0; i < kRawSlots - 1; ++i) fetch();
+      int buf = 0, slot = 0;
       uint32_t buf_phase = 0;
       bool ok = true;
       for (int ct = cid; ct < num_ctiles && ok; ct += ncl) {
-        const int64_t row0 = (int64_t)(ct % groups_m * kCM + rank) * kBM + lane;
-        const int64_t wb0 = (int64_t)(ct / groups_m) * C::kWBlocks;
-        constexpr int kAhead = 4;
-        float ra[kAhead][4], rw[kAhead][C::kWBlocks];
-        auto load = [&](int u, int kb) {
-          kb = min(kb, num_kb - 1);
+        for (int kb = 0; kb < num_kb; ++kb) {
+          asm volatile("cp.async.wait_group %0;" ::"n"(kRawSlots - 2) : "memory");
+          __syncwarp();   // (the others' loads too; and all are done with the slot that the next fills)
+          const float* const from = scales + C::kScaleBytes / 4 + slot * C::kRawSlot;
+          float a[4], w[C::kWBlocks];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) ra[u][i] = __ldg(p.sa + kb * p.M + min(row0 + 32 * i, p.M - 1));
+          for (int i = 0; i < 4; ++i) a[i] = from[lane + 32 * i];
 #pragma unroll
-          for (int i = 0; i < C::kWBlocks; ++i) rw[u][i] = __ldg(p.sw + kb * w_blocks + min(wb0 + i, w_blocks - 1));
-        };
+          for (int i = 0; i < C::kWBlocks; ++i) w[i] = from[kBM + i];
+          if (++slot == kRawSlots) slot = 0;
+          if (!mbar_wait_warp(&tmem_empty[buf], buf_phase ^ 1u, ctl)) {
+            ok = false;
+            break;
+          }
+          float* const to = scales + buf * C::kWBlocks * kBM + lane;
 #pragma unroll
-        for (int u = 0; u < kAhead - 1; ++u) load(u, u);
-        for (int kb0 = 0; kb0 < num_kb && ok; kb0 += kAhead) {
+          for (int k = 0; k < C::kWBlocks; ++k)
 #pragma unroll
-          for (int u = 0; u < kAhead; ++u) {
-            if (kb0 + u < num_kb && ok) {
-              load((u + kAhead - 1) % kAhead, kb0 + u + kAhead - 1);
-              if (!mbar_wait_warp(&tmem_empty[buf], buf_phase ^ 1u, ctl)) {
-                ok = false;
-              } else {
-                float* const s = scales + buf * C::kWBlocks * kBM + lane;
-#pragma unroll
-                for (int w = 0; w < C::kWBlocks; ++w)
-#pragma unroll
-                  for (int i = 0; i < 4; ++i) s[w * kBM + 32 * i] = __fmul_rn(ra[u][i], rw[u][w]);
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&tmem_full[buf]);
-                if (++buf == C::kBuffers) {
-                  buf = 0;
-                  buf_phase ^= 1u;
-                }
-              }
-            }
+            for (int i = 0; i < 4; ++i) to[k * kBM + 32 * i] = __fmul_rn(a[i], w[k]);
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&tmem_full[buf]);
+          fetch();
+          if (++buf == C::kBuffers) {
+            buf = 0;
+            buf_phase ^= 1u;
           }
         }
       }
+      asm volatile("cp.async.wait_group 0;" ::: "memory");
     }
   } else {
     // ---- accumulators ----
@@ -318,6 +352,59 @@ __global__ void __launch_bounds__(BlockCfg<kBN, kShare>::kThreads, 1)
     constexpr int kChunks = kCols / 32;
     const int e = warp - kRoleWarps, quarter = warp & 3, part = e >> 2;   // lanes, columns
     const uint32_t bias_s = smem_u32(bias_copies) + (uint32_t)(e * kCols * 2);
+    // kSplitK: every CTA sends its sums of a column to the CTA that finishes that column, through
+    // shared memory that the stages have left; they are added in the order of K.
+    auto split_end = [&](float2 (&acc)[kChunks][16], int ct) {
+      cluster_sync();   // no MMA reads a stage of any of the CTAs, no copy is on its way
+      const int width = kBN / splits, pitch = (width + 4) * 4;   // columns of a CTA; bytes of a row of them
+      const int my_row = quarter * 32 + lane;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {   // 16 columns
+        const int col = part * kCols + 16 * c, owner = col / width;
+        const uint32_t to = mapa_shared(smem + (krank * kBM + my_row) * pitch + (col - owner * width) * 4, (uint32_t)owner);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float2 a = acc[c >> 1][8 * (c & 1) + 2 * i], b = acc[c >> 1][8 * (c & 1) + 2 * i + 1];
+          asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(to + 16 * i), "f"(a.x), "f"(a.y),
+                       "f"(b.x), "f"(b.y)
+                       : "memory");
+        }
+      }
+      cluster_sync();
+      for (int i = threadIdx.x - kRoleWarps * 32; i < kBM * width / 16; i += C::kEpiWarps * 32) {
+        const int r = i % kBM, group = i / kBM;
+        const int64_t row = (int64_t)(ct % groups_m) * kBM + r;
+        const int64_t n = (int64_t)(ct / groups_m) * kBN + krank * width + 16 * group;
+        if (row >= p.M || n >= p.N) continue;
+        float2 v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = make_float2(0.0f, 0.0f);
+        for (int q = 0; q < splits; ++q) {
+          const float4* const from = reinterpret_cast<const float4*>(smem + (q * kBM + r) * pitch + 64 * group);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const float4 x = from[k];
+            v[2 * k] = add2(v[2 * k], make_float2(x.x, x.y));
+            v[2 * k + 1] = add2(v[2 * k + 1], make_float2(x.z, x.w));
+          }
+        }
+        uint32_t w[8];
+        if (p.bias != nullptr) {
+          load32<false>(p.bias + n, w);
+#pragma unroll
+          for (int k = 0; k < 8; ++k) v[k] = add2(v[k], make_float2(bf16_lo(w[k]), bf16_hi(w[k])));
+        }
+        activate(v, p.act);
+        if (p.residual != nullptr) {
+          load32<false>(p.residual + row * p.residual_stride + n, w);
+#pragma unroll
+          for (int k = 0; k < 8; ++k) v[k] = add2(v[k], make_float2(bf16_lo(w[k]), bf16_hi(w[k])));
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) w[k] = pack_bf16x2(v[k].x, v[k].y);
+        store32(p.y + row * p.N + n, w, p.y_v8 != 0);
+      }
+    };
     int buf = 0;
     uint32_t buf_phase = 0;
     bool ok = true;
@@ -370,6 +457,10 @@ __global__ void __launch_bounds__(BlockCfg<kBN, kShare>::kThreads, 1)
           buf_phase ^= 1u;
         }
       }
+      if constexpr (kSplitK) {   // (one tile)
+        split_end(acc, ct);
+        break;
+      }
       if (!ok) break;
       // ---- the tile's end: N % 64 == 0, so 32 columns are wholly inside or outside ----
       if (p.bias != nullptr) {
@@ -421,10 +512,17 @@ __global__ void __launch_bounds__(BlockCfg<kBN, kShare>::kThreads, 1)
     }
   }
 
+  if constexpr (kSplitK) {
+    if (warp < kRoleWarps) {   // the epilogue's two cluster barriers
+      __syncwarp();
+      cluster_sync();
+      cluster_sync();
+    }
+  }
   // No CTA of a cluster may exit while the peer can still copy into it or arrive on its barriers.
   __syncwarp();
   tc_fence_before();
-  if (kShare)
+  if (kShare || kSplitK)
     cluster_sync_relaxed();
   else
     __syncthreads();
@@ -434,7 +532,7 @@ __global__ void __launch_bounds__(BlockCfg<kBN, kShare>::kThreads, 1)
   }
 }
 
-template <int kBN, bool kShare>
+template <int kBN, bool kShare, bool kSplitK = false>
 cudaError_t launch_cfg(const GemmArgs& a, cudaStream_t s, Device dev, unsigned* err, uint64_t timeout_ns) {
   using C = BlockCfg<kBN, kShare>;
   constexpr int kCM = C::kCM;
@@ -455,9 +553,10 @@ cudaError_t launch_cfg(const GemmArgs& a, cudaStream_t s, Device dev, unsigned* 
   p.act = a.act;
   p.y_v8 = (reinterpret_cast<uintptr_t>(a.y) & 31u) == 0 ? 1 : 0;
   p.r_v8 = ((reinterpret_cast<uintptr_t>(a.residual) | (uintptr_t)(a.residual_stride * 2)) & 31u) == 0 ? 1 : 0;
+  p.split = a.split;
   p.err = err;
   p.timeout_ns = timeout_ns;
-  auto kern = gemm_block_kernel<kBN, kShare>;
+  auto kern = gemm_block_kernel<kBN, kShare, kSplitK>;
   cudaLaunchConfig_t cfg{};
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -490,6 +589,10 @@ cudaError_t launch_cfg(const GemmArgs& a, cudaStream_t s, Device dev, unsigned* 
   if (ctiles > INT32_MAX / 2) return cudaErrorInvalidValue;
   const int clusters = (int)std::min<int64_t>(ctiles, std::min(setup.max_clusters, dev.num_sms / kCM));
   cfg.gridDim = dim3((unsigned)(clusters * kCM), 1, 1);
+  if (kSplitK) {   // a cluster per tile
+    cfg.gridDim.x = (unsigned)(ctiles * a.split);
+    attr[0].val.clusterDim.x = (unsigned)a.split;
+  }
   cfg.numAttrs = 2;
   return cudaLaunchKernelEx(&cfg, kern, ta, tb, p);
 }
@@ -497,9 +600,17 @@ cudaError_t launch_cfg(const GemmArgs& a, cudaStream_t s, Device dev, unsigned* 
 }  // namespace
 
 cudaError_t launch_gemm_block(const GemmArgs& a, cudaStream_t s, Device dev, unsigned* err, uint64_t timeout_ns) {
-  const int64_t tiles_m = (a.M + kBM - 1) / kBM;
-  if (tiles_m * ((a.N + 255) / 256) >= dev.num_sms) return launch_cfg<256, true>(a, s, dev, err, timeout_ns);
-  return launch_cfg<128, false>(a, s, dev, err, timeout_ns);
+  switch (choose_block_tile(a.M, a.N, a.K, dev.num_sms)) {
+    case BlockTile::kShared:
+      return launch_cfg<256, true>(a, s, dev, err, timeout_ns);
+    case BlockTile::kSingle:
+      return launch_cfg<128, false>(a, s, dev, err, timeout_ns);
+    default: {
+      GemmArgs b = a;
+      b.split = choose_block_split(a.M, a.N, a.K, dev.num_sms);
+      return launch_cfg<128, false, true>(b, s, dev, err, timeout_ns);
+    }
+  }
 }
 
 }  // namespace qlin

@@ -160,4 +160,44 @@ inline bool split_over_few(GemmKind kind, int64_t M, int64_t N, int64_t K, int n
          choose_split_k(kind, M, N, K, num_sms) > 1;
 }
 
+// The block-scaled FP8 linear's tiles: 128 x 256 in clusters of two over the same W, 128 x 128,
+// or those with K shared by a cluster.
+enum class BlockTile { kShared, kSingle, kSplit };
+
+// CTAs of a cluster that share a tile's K.  Sending and joining the sums costs about 5 us, a
+// block 0.36 (M x N x K in us, one CTA and split: 600 x 512 x 3072 13.0, 12.1 in four; x 12288 38.5,
+// 18.0; 300 x 2112 x 3072 13.4, 12.4 in two, x 2048 10.5, 10.9; 24 x 5120 x 12288 38.2, 22.8).
+inline int choose_block_split(int64_t M, int64_t N, int64_t K, int num_sms) {
+  const int64_t blocks = (K + 127) / 128, tiles_m = (M + kTileM - 1) / kTileM, tiles_n = (N + 127) / 128;
+  if (tiles_m > num_sms || tiles_n > num_sms) return 1;
+  const int64_t tiles = tiles_m * tiles_n;
+  if (10 * tiles <= num_sms && blocks >= 32) return 8;
+  if (4 * tiles <= num_sms && blocks >= 20) return 4;
+  return 2 * tiles <= num_sms && blocks >= 24 ? 2 : 1;
+}
+
+// Between the unsplit tiles the times of their waves decide, fitted to M 24-4608, N 64-12288, K
+// 256-12288 (in us, 128 x 256 and 128 x 128: 1333 x 2112 x 256 9.0, 8.1; x 1088 12.4, 13.5; 300 x
+// 12288 x 1088 21.6, 13.7; 4608 x 12288 x 3072 198, 248).
+inline BlockTile choose_block_tile(int64_t M, int64_t N, int64_t K, int num_sms) {
+  if (choose_block_split(M, N, K, num_sms) > 1) return BlockTile::kSplit;
+  const int64_t blocks = (K + 127) / 128, tiles_m = (M + kTileM - 1) / kTileM;
+  const TileCost single{1.9, 2.6, 0.36}, shared{1.9, 6.0, 0.43};
+  return shared.us((tiles_m + 1) / 2 * ((N + 255) / 256), num_sms / 2, blocks, 0.0) <
+                 single.us(tiles_m * ((N + 127) / 128), num_sms, blocks, 0.0)
+             ? BlockTile::kShared
+             : BlockTile::kSingle;
+}
+
+// Whether the block-scaled linear takes the few-token kernel: always up to 16 tokens, beyond that as
+// long as its units, 16 rows of W and 16 tokens, are at most 5.2 per SM, or 2.6 over long K.  (Few /
+// the best tiles in us: 24 x 5120 x 3072 9.4 / 11.5 and x 12288 26 / 23 (4.2 units per SM), 300 x 512 x
+// 3072 7.8 / 10.7 and x 12288 17.1 / 16.0 (4.0), 128 x 2112 x 1088 7.2 / 7.5 (7), 64 x 5120 x 1088 11.2 /
+// 7.0 (8.4), 128 x 512 x 12288 12.8 / 12.7 (1.7).)
+inline bool few_block_tokens(int64_t M, int64_t N, int64_t K, int num_sms) {
+  if (M <= 16) return true;
+  const int limit = K <= 4096 ? 52 : 26;
+  return N / 16 <= limit * (int64_t)num_sms && 10 * (N / 16) * ((M + 15) / 16) <= limit * (int64_t)num_sms;
+}
+
 }  // namespace qlin

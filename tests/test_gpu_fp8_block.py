@@ -129,7 +129,7 @@ def _check(y, A, W, bias, act, residual):
 
 
 SHAPES = [(1, 64, 64), (1, 192, 12288), (2, 128, 128), (7, 320, 192), (16, 3072, 1088), (17, 2112, 1088), (33, 64, 4096),
-          (129, 256, 64), (128, 128, 128), (257, 320, 320), (500, 1088, 2112), (1333, 2112, 1088), (2000, 5120, 192),
+          (700, 192, 12288), (700, 1024, 4096), (129, 256, 64), (128, 128, 128), (257, 320, 320), (500, 1088, 2112), (1333, 2112, 1088), (2000, 5120, 192),
           (3000, 3008, 448), (4608, 12288, 256)]
 
 
