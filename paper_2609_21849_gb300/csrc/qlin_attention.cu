@@ -45,8 +45,11 @@ cudaError_t launch_cache_attention(const qlin_cache_t& c, const qlin_cache_atten
   p.counts = static_cast<unsigned*>(workspace);
   p.err = err;
   // more rows per sequence and KV head, on average, than the mma.sync kernel shares a read among
-  if (c.format != QLIN_CACHE_E4M3 && p.tokens * p.group > (int64_t)32 * p.sequences && attention_tiles_fit(p))
-    return launch_attention_tiles(p, c.format == QLIN_CACHE_FP16, timeout_ns, s, dev);
+  const CacheKind kind = c.format == QLIN_CACHE_E4M3   ? CacheKind::kE4m3
+                         : c.format == QLIN_CACHE_FP16 ? CacheKind::kFp16
+                                                       : CacheKind::kBf16;
+  if (p.tokens * p.group > (int64_t)32 * p.sequences && attention_tiles_fit(p))
+    return launch_attention_tiles(p, kind, timeout_ns, s, dev);
   return c.format == QLIN_CACHE_E4M3   ? launch_attention_e4m3(p, s, dev)
          : c.format == QLIN_CACHE_FP16 ? launch_attention_fp16(p, s, dev)
                                        : launch_attention_bf16(p, s, dev);

@@ -45,7 +45,7 @@ constexpr int64_t kWorkspaceBytes = (int64_t)64 << 20;
 
 // Many rows on tcgen05 (qlin_attention_tiles.cu): whether it takes these pages and heads.
 bool attention_tiles_fit(const AttnParams& p);
-cudaError_t launch_attention_tiles(const AttnParams& p, bool fp16, uint64_t timeout_ns, cudaStream_t s, Device dev);
+cudaError_t launch_attention_tiles(const AttnParams& p, CacheKind kind, uint64_t timeout_ns, cudaStream_t s, Device dev);
 cudaError_t launch_attention_bf16(const AttnParams& p, cudaStream_t s, Device dev);
 cudaError_t launch_attention_fp16(const AttnParams& p, cudaStream_t s, Device dev);
 cudaError_t launch_attention_e4m3(const AttnParams& p, cudaStream_t s, Device dev);

@@ -19,16 +19,15 @@
 // (Rows that do see such a value take it at the end.)
 // An item that several CTAs share is joined by a second kernel, many CTAs to an item (by one of
 // these, at one SM's rate of reading, the 16 trees below took 262 us, not 2xx).
+#include <type_traits>
+
 #include "qlin_attention_work.cuh"
 
 namespace qlin {
 
 namespace {
 
-constexpr int kRows = 256, kTile = 128, kHalf = 64;
-constexpr int kSoftWarp0 = 4, kSoftThreads = 256, kThreads = kSoftWarp0 * 32 + kSoftThreads;
-constexpr int kRoleRegs = 104, kSoftRegs = 200, kLaunchRegs = 168;
-static_assert(kSoftWarp0 * 32 * kRoleRegs + kSoftThreads * kSoftRegs <= kThreads * kLaunchRegs, "registers");
+constexpr int kSoftWarp0 = 4, kConvertWarps = 4;
 constexpr float kSlack = 8.0f;   // powers of two that a score may exceed the kept maximum by
 constexpr int kBadRing = 16;     // tiles whose bad pages are remembered
 
@@ -37,13 +36,16 @@ struct Segment {
   int first, n;      // tiles
   bool halves;
 };
+template <typename C>
 __device__ __forceinline__ Segment segment_at(const AttnParams& p, const Cursor& c, int64_t unit, int64_t end) {
-  const int64_t rows = (int64_t)c.s.fresh * p.group - (int64_t)c.rt * kRows;
-  return {c.tile, (int)min((int64_t)(c.tiles - c.tile), end - unit), rows > 128};
+  const int64_t rows = (int64_t)c.s.fresh * p.group - (int64_t)c.rt * C::kRows;
+  // (one stream: its tiles in the order of halves of the rows, of which there is one)
+  return {c.tile, (int)min((int64_t)(c.tiles - c.tile), end - unit), C::kStreams == 1 || rows > 128};
 }
+template <typename C>
 __device__ __forceinline__ void skip_segment(const AttnParams& p, Cursor& c, const Segment& s) {
   c.tile += s.n - 1;
-  advance<kRows, kTile>(p, c);
+  advance<C::kRows, C::kTile>(p, c);
 }
 
 // A segment as the softmax threads need it, in shared memory: their registers hold scores.
@@ -67,15 +69,28 @@ struct TileShared {
   int odd_values;
 };
 
-template <int kDC>   // chunks of 64 elements of a head
+// kDC: chunks of 64 elements of a head.  Heads of up to 128 have two streams; longer ones take all of
+// tensor memory for one stream's sums, 128 rows and tiles of 64 keys.  kCodes: an E4M3 cache.
+template <int kDC, bool kCodes>
 struct TileCfg {
-  static constexpr int kChunk = kTile * 128;          // 64 elements of 128 keys or rows
-  static constexpr int kSlot = kDC * kChunk;          // a tile of K or V, or 128 rows of Q
-  static constexpr int kSlots = kDC == 1 ? 10 : 5;
-  static constexpr int kQBytes = 2 * kSlot;
-  static constexpr int kBarrierBytes = 320;
-  static constexpr int kSmem = kQBytes + kSlots * kSlot + kBarrierBytes + (int)sizeof(TileShared);
-  static_assert((2 * kSlots + 14) * 8 <= kBarrierBytes && kSmem <= 232448, "shared memory");
+  static constexpr int kStreams = kDC <= 2 ? 2 : 1;
+  static constexpr int kRows = 128 * kStreams;
+  static constexpr int kTile = kDC <= 2 ? 128 : 64, kHalf = kTile / 2;   // keys
+  static constexpr int kChunk = kTile * 128, kQChunk = 128 * 128;        // 64 elements of a tile's keys, of 128 rows
+  static constexpr int kSlot = kDC * kChunk;                             // a tile of K or V
+  static constexpr int kQSlot = kDC * kQChunk, kQBytes = kStreams * kQSlot;
+  static constexpr int kRawRow = 64 * kDC, kRawSlot = kCodes ? kTile * kRawRow : 0, kRawSlots = kCodes ? 4 : 0;
+  static constexpr int kBarrierBytes = 384;
+  static constexpr int kOther = kQBytes + kRawSlots * kRawSlot + kBarrierBytes + (int)sizeof(TileShared);
+  static constexpr int kSlotsRaw = (232448 - kOther) / kSlot, kSlots = kSlotsRaw > 10 ? 10 : kSlotsRaw;
+  static constexpr int kSmem = kOther + kSlots * kSlot;
+  static constexpr int kSoftThreads = 128 * kStreams;
+  static constexpr int kThreads = kSoftWarp0 * 32 + kSoftThreads + (kCodes ? kConvertWarps * 32 : 0);
+  // registers: roles (and conversion), softmax
+  static constexpr int kRoleRegs = kThreads == 512 ? 88 : 104, kSoftRegs = kThreads == 512 ? 152 : 200;
+  static constexpr int kLaunchRegs = kThreads == 512 ? 128 : 168;
+  static_assert((kThreads - kSoftThreads) * kRoleRegs + kSoftThreads * kSoftRegs <= kThreads * kLaunchRegs, "registers");
+  static_assert((2 * kSlots + 2 * kRawSlots + 14) * 8 <= kBarrierBytes && kSlots >= 3, "shared memory");
 };
 
 struct TileParams {
@@ -107,7 +122,10 @@ __device__ __forceinline__ uint64_t sdesc_v(uint32_t saddr, uint32_t chunk_bytes
   return d;
 }
 
-__device__ __forceinline__ void softmax_sync() { asm volatile("bar.sync 1, %0;" ::"n"(kSoftThreads) : "memory"); }
+template <int kSoftThreads>
+__device__ __forceinline__ void softmax_sync() {
+  asm volatile("bar.sync 1, %0;" ::"n"(kSoftThreads) : "memory");
+}
 // Where in the order of loads a segment's tiles lie (n tiles; K and V of each).  Rows in two
 // halves: K0 V0 K1 V1 ...  Tiles in turn: K0 K1 V0 K2 V1 K3 ...: each as the MMAs take them.
 __device__ __forceinline__ int k_pos(bool halves, int j) { return halves ? 2 * j : j < 2 ? j : 2 * j - 1; }
@@ -127,6 +145,14 @@ __device__ __forceinline__ uint32_t mask_window(const uint64_t* m, int words, in
 // The first n of 32 (n may be negative or large).
 __device__ __forceinline__ uint32_t first_bits(int64_t n) {
   return n >= 32 ? 0xFFFFFFFFu : n <= 0 ? 0u : (1u << (int)n) - 1u;
+}
+
+// Two E4M3 codes as two halves, exactly.
+__device__ __forceinline__ uint32_t e4m3x2_half2(uint32_t codes) {
+  uint32_t h;
+  const uint16_t c = (uint16_t)codes;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(c));
+  return h;
 }
 
 // Which keys of 32 a row (new token t, number `token` of the call) sees, from key `key` on.
@@ -158,12 +184,13 @@ __device__ __forceinline__ void hide(uint32_t bits, unsigned bads, int c, int bo
     if (!((bits >> i) & 1u)) v[i] = 0xFF800000u;
 }
 
-template <bool kF16, int kDC>
-__global__ void __launch_bounds__(kThreads, 1)
+template <bool kF16, int kDC, bool kCodes>
+__global__ void __launch_bounds__(TileCfg<kDC, kCodes>::kThreads, 1)
     attn_tiles_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v,
                       const TileParams tp) {
-  using C = TileCfg<kDC>;
-  constexpr int kD = 64 * kDC;
+  using C = TileCfg<kDC, kCodes>;
+  constexpr int kD = 64 * kDC, kRows = C::kRows, kTile = C::kTile, kHalf = C::kHalf, kThreads = C::kThreads;
+  static_assert(kF16 || !kCodes, "codes become fp16");
   const AttnParams& p = tp.a;
   extern __shared__ __align__(1024) uint8_t smem[];
   if ((smem_u32(smem) & 1023u) != 0u) {   // (the swizzle's atoms; no other shared memory comes before)
@@ -172,28 +199,35 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
   uint8_t* const q_smem = smem;
   uint8_t* const ring = smem + C::kQBytes;
-  uint64_t* const full = reinterpret_cast<uint64_t*>(ring + C::kSlots * C::kSlot);
+  uint8_t* const raw = ring + C::kSlots * C::kSlot;   // kCodes: tiles of codes as they come
+  uint64_t* const full = reinterpret_cast<uint64_t*>(raw + C::kRawSlots * C::kRawSlot);
   uint64_t* const empty = full + C::kSlots;
   uint64_t* const s_full = empty + C::kSlots;    // per stream and half of a tile: scores are there
   uint64_t* const p_ready = s_full + 4;          // the same: P is there
   uint64_t* const pv_done = p_ready + 4;         // the same: its product is done
   uint64_t* const q_ready = pv_done + 4;
   uint64_t* const mma_done = q_ready + 1;
-  TileShared& sh = *reinterpret_cast<TileShared*>(ring + C::kSlots * C::kSlot + C::kBarrierBytes);
+  uint64_t* const raw_full = mma_done + 1;       // kCodes: codes have landed, and have been converted
+  uint64_t* const raw_empty = raw_full + C::kRawSlots;
+  TileShared& sh = *reinterpret_cast<TileShared*>(raw + C::kRawSlots * C::kRawSlot + C::kBarrierBytes);
 
   const int warp = __shfl_sync(0xFFFFFFFFu, (int)(threadIdx.x >> 5), 0);
   const int lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     for (int i = 0; i < C::kSlots; ++i) {
-      mbar_init(&full[i], 1);
+      mbar_init(&full[i], kCodes ? kConvertWarps : 1);
       mbar_init(&empty[i], 1);
+    }
+    for (int i = 0; i < C::kRawSlots; ++i) {
+      mbar_init(&raw_full[i], 1);
+      mbar_init(&raw_empty[i], kConvertWarps);
     }
     for (int i = 0; i < 4; ++i) {
       mbar_init(&s_full[i], 1);
       mbar_init(&p_ready[i], 4);
       mbar_init(&pv_done[i], 1);
     }
-    mbar_init(q_ready, 8);
+    mbar_init(q_ready, 4 * C::kStreams);
     mbar_init(mma_done, 1);
     sh.abort = 0;
     sh.odd_values = 0;
@@ -215,9 +249,10 @@ __global__ void __launch_bounds__(kThreads, 1)
   // (loads of a CTA are counted in 32 bits: fewer than 2^25 tiles of keys a sequence, 2^31 in all)
   auto slot_of = [&](uint32_t pos) { return (int)(pos % C::kSlots); };
   auto phase_of = [&](uint32_t pos) { return (pos / C::kSlots) & 1u; };
+  constexpr uint32_t kRing = kCodes ? C::kRawSlots : 1;   // of codes
 
   if (warp < kSoftWarp0) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRoleRegs));
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kRoleRegs));
     if (warp == 0 || warp == 2) {
       // ---- loads, of K or V: a lane per page of the tile ----
       const bool is_v = warp == 2;
@@ -227,7 +262,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       uint32_t used = 0u, phases = 0u;   // slots that this warp filled, and in which phase last
       bool ok = true;
       for (int64_t unit = run.begin; unit < run.end && ok;) {
-        const Segment sg = segment_at(p, cur, unit, run.end);
+        const Segment sg = segment_at<C>(p, cur, unit, run.end);
         struct Load {
           bool in;
           int at, page;
@@ -253,36 +288,44 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (bad) atomicExch(p.err, kErrInvalid);
           const int page = !d.in || bad ? p.pages : d.page;   // past the last: zeros
           const int at = !d.in || bad ? 0 : d.at;
-          if (!mbar_wait_warp(&empty[slot], phase_of(pos) ^ 1u, ctl)) {
+          const int rs = (int)(pos % kRing);
+          uint64_t* const there = kCodes ? &raw_full[rs] : &full[slot];
+          if (!(kCodes ? mbar_wait_warp(&raw_empty[rs], ((pos / kRing) & 1u) ^ 1u, ctl)
+                       : mbar_wait_warp(&empty[slot], phase_of(pos) ^ 1u, ctl))) {
             ok = false;
             break;
           }
           if (lane == 0) {
             if (!is_v) *(volatile unsigned*)&sh.bad_pages[(tiles_done + j) % kBadRing] = bads;
-            mbar_arrive_expect_tx(&full[slot], C::kSlot);
+            mbar_arrive_expect_tx(there, kCodes ? C::kRawSlot : C::kSlot);
           }
           __syncwarp();
           if (lane < tp.boxes) {
-            uint8_t* const dst = ring + slot * C::kSlot + lane * tp.box_rows * 128;
+            if (kCodes) {
+              tma_load_4d(raw + rs * C::kRawSlot + lane * tp.box_rows * C::kRawRow, map, smem_u32(there), 0, at, cur.h,
+                          page);
+            } else {
+              uint8_t* const dst = ring + slot * C::kSlot + lane * tp.box_rows * 128;
 #pragma unroll
-            for (int c = 0; c < kDC; ++c)
-              tma_load_4d(dst + c * C::kChunk, map, smem_u32(&full[slot]), 64 * c, at, cur.h, page);
+              for (int c = 0; c < kDC; ++c) tma_load_4d(dst + c * C::kChunk, map, smem_u32(there), 64 * c, at, cur.h, page);
+            }
           }
           __syncwarp();
-          used |= 1u << slot;
-          phases = (phases & ~(1u << slot)) | (phase_of(pos) << slot);
+          const int b = kCodes ? rs : slot;
+          used |= 1u << b;
+          phases = (phases & ~(1u << b)) | ((kCodes ? (pos / kRing) & 1u : phase_of(pos)) << b);
         }
         base += 2 * sg.n;
         tiles_done += sg.n;
         unit += sg.n;
-        if (unit < run.end) skip_segment(p, cur, sg);
+        if (unit < run.end) skip_segment<C>(p, cur, sg);
       }
       // (The MMAs wait for every load.)  After a wait that gave up, copies in flight land before
       // the CTA exits, or a limit passes.
       if (!ok && lane == 0) {
         const uint64_t t0 = global_timer_ns();
-        for (int i = 0; i < C::kSlots; ++i)
-          while (((used >> i) & 1u) && !mbar_try_wait(smem_u32(&full[i]), (phases >> i) & 1u))
+        for (int i = 0; i < (kCodes ? C::kRawSlots : C::kSlots); ++i)
+          while (((used >> i) & 1u) && !mbar_try_wait(smem_u32(kCodes ? &raw_full[i] : &full[i]), (phases >> i) & 1u))
             if (global_timer_ns() - t0 > tp.timeout_ns) break;
       }
     } else if (warp == 1) {
@@ -298,26 +341,27 @@ __global__ void __launch_bounds__(kThreads, 1)
         // (what the descriptors depend on goes through a shuffle, so that the compiler knows it to
         // be the same in all lanes and keeps them in uniform registers, where tcgen05 takes them: an
         // MMA issued from others cost 70 cycles, more than it runs)
-        Segment sg = segment_at(p, cur, unit, run.end);
+        Segment sg = segment_at<C>(p, cur, unit, run.end);
         sg.n = __shfl_sync(0xFFFFFFFFu, sg.n, 0);
         sg.halves = __shfl_sync(0xFFFFFFFFu, (int)sg.halves, 0) != 0;
-        const int n0 = sg.halves ? sg.n : (sg.n + 1) / 2, n1 = sg.halves ? sg.n : sg.n / 2;
+        const int n0 = sg.halves ? sg.n : (sg.n + 1) / 2, n1 = C::kStreams == 1 ? 0 : sg.halves ? sg.n : sg.n / 2;
         if (!mbar_wait_warp(q_ready, q_phase, ctl)) break;
         q_phase ^= 1u;
         tc_fence_after();
         // (one elected lane) scores of half hf of the stream's tile in `slot`
         auto scores = [&](int s, int hf, int slot) {
-          const uint32_t qa = smem_u32(q_smem) + (sg.halves ? s * C::kSlot : 0);
+          const uint32_t qa = smem_u32(q_smem) + (sg.halves ? s * C::kQSlot : 0);
           const uint32_t ka = smem_u32(ring + slot * C::kSlot) + hf * kHalf * 128;
           const uint64_t qd = sdesc_k128(qa), kd = sdesc_k128(ka);
 #pragma unroll
           for (int i = 0; i < 4 * kDC; ++i) {
-            constexpr uint64_t kStep = 32 >> 4, kNext = C::kChunk >> 4;   // (in the descriptors' units)
-            const uint64_t o = (uint64_t)(i >> 2) * kNext + (uint64_t)(i & 3) * kStep;
-            if (i < k_steps) mma_bf16(s_tmem + 128 * s + kHalf * hf, qd + o, kd + o, id_s, i > 0 ? 1u : 0u);
+            constexpr uint64_t kStep = 32 >> 4;   // (in the descriptors' units)
+            const uint64_t q = (uint64_t)(i >> 2) * (C::kQChunk >> 4) + (uint64_t)(i & 3) * kStep;
+            const uint64_t k = (uint64_t)(i >> 2) * (C::kChunk >> 4) + (uint64_t)(i & 3) * kStep;
+            if (i < k_steps) mma_bf16(s_tmem + 128 * s + kHalf * hf, qd + q, kd + k, id_s, i > 0 ? 1u : 0u);
           }
           tc_commit(&s_full[2 * s + hf]);
-          if (hf == 1 && (!sg.halves || s == 1)) tc_commit(&empty[slot]);
+          if (hf == 1 && (C::kStreams == 1 || !sg.halves || s == 1)) tc_commit(&empty[slot]);
         };
         auto k_slot = [&](int s, int j, int* slot) {
           const uint32_t pos = base + k_pos(sg.halves, sg.halves ? j : 2 * j + s);
@@ -342,9 +386,9 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
               for (int i = 0; i < kHalf / 16; ++i)
                 mma_f16_ts(o_tmem + 128 * s, s_tmem + 128 * s + kHalf * hf + 8 * i,
-                           vd + (uint64_t)((4 * hf + i) * (2048 >> 4)), id_o, i > 0 || hf > 0 || j > 0 ? 1u : 0u);
+                           vd + (uint64_t)((kHalf / 16 * hf + i) * (2048 >> 4)), id_o, i > 0 || hf > 0 || j > 0 ? 1u : 0u);
               tc_commit(&pv_done[2 * s + hf]);
-              if (hf == 1 && (!sg.halves || s == 1)) tc_commit(&empty[slot]);
+              if (hf == 1 && (C::kStreams == 1 || !sg.halves || s == 1)) tc_commit(&empty[slot]);
             }
             __syncwarp();
             if (last) continue;
@@ -370,7 +414,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         base += 2 * sg.n;
         unit += sg.n;
-        if (unit < run.end) skip_segment(p, cur, sg);
+        if (unit < run.end) skip_segment<C>(p, cur, sg);
       }
       // every MMA issued finishes before tensor memory is released
       if (elect_one()) {
@@ -384,9 +428,44 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
       }
     }
+  } else if (kCodes && warp >= kSoftWarp0 + C::kSoftThreads / 32) {
+    // ---- codes to fp16 (exactly), from the rows as they came to the MMAs' swizzled tiles ----
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kRoleRegs));
+    const int thread = threadIdx.x - kSoftWarp0 * 32 - C::kSoftThreads;
+    const uint32_t loads = (uint32_t)(2 * (run.end - run.begin));
+    for (uint32_t pos = 0; pos < loads; ++pos) {
+      const int rs = (int)(pos % kRing), slot = slot_of(pos);
+      if (!mbar_wait_warp(&raw_full[rs], (pos / kRing) & 1u, ctl) ||
+          !mbar_wait_warp(&empty[slot], phase_of(pos) ^ 1u, ctl))
+        break;
+      const uint32_t src = smem_u32(raw + rs * C::kRawSlot), dst = smem_u32(ring + slot * C::kSlot);
+#pragma unroll 4
+      for (int i = thread; i < kTile * 4 * kDC; i += kConvertWarps * 32) {   // 16 codes
+        const int key = i / (4 * kDC), at = i % (4 * kDC);
+        uint32_t w[4], h[8];
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                     : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
+                     : "r"(src + key * C::kRawRow + at * 16));
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          h[2 * k] = e4m3x2_half2(w[k]);
+          h[2 * k + 1] = e4m3x2_half2(w[k] >> 16);
+        }
+        const uint32_t to = dst + (at >> 2) * C::kChunk + key * 128;
+        const int piece = 2 * (at & 3);
+        st_shared_v4(to + ((piece ^ (key & 7)) << 4), h[0], h[1], h[2], h[3]);
+        st_shared_v4(to + (((piece + 1) ^ (key & 7)) << 4), h[4], h[5], h[6], h[7]);
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) {
+        mbar_arrive(&full[slot]);
+        mbar_arrive(&raw_empty[rs]);
+      }
+    }
   } else {
     // ---- softmax: stream s, row r ----
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::kSoftRegs));
     const int thread = threadIdx.x - kSoftWarp0 * 32;
     const int s = thread >> 7, r = thread & 127;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
@@ -401,7 +480,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       SoftSegment& g = sh.seg[at];
       g.n = 0;
       if (unit >= run.end) return;
-      const Segment sg = segment_at(p, cur, unit, run.end);
+      const Segment sg = segment_at<C>(p, cur, unit, run.end);
       const int64_t item0 = unit - sg.first;
       g.s = cur.s;
       g.base = base;
@@ -417,10 +496,10 @@ __global__ void __launch_bounds__(kThreads, 1)
       base += 2 * sg.n;
       tiles_done += sg.n;
       unit += sg.n;
-      if (unit < run.end) skip_segment(p, cur, sg);
+      if (unit < run.end) skip_segment<C>(p, cur, sg);
     };
     if (thread == 0) publish(0);
-    softmax_sync();
+    softmax_sync<C::kSoftThreads>();
     for (int at = 0;; at ^= 1) {
       const SoftSegment& g = sh.seg[at];
       const int n = g.n;
@@ -430,22 +509,51 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int my_row = halves ? 128 * s + r : r;
       auto row_in = [&] { return g.rt * kRows + my_row < g.s.fresh * p.group; };
       auto row_of = [&] { return row_in() ? g.rt * kRows + my_row : 0; };
+      float mult = p.scale_log2;   // from scores to powers of two
       // Q into shared memory: rows of 128 swizzled bytes, 64 elements a chunk
-      if (halves || s == 0) {
+      const bool stores_q = halves || s == 0;
+      if (stores_q || kCodes) {
         const int row = row_of();
         const uint16_t* const q = p.q + (g.s.first + row / p.group) * p.q_token +
                                   (int64_t)(g.h * p.group + row % p.group) * p.q_head;
-        const uint32_t dst = smem_u32(q_smem) + (halves ? s * C::kSlot : 0) + r * 128;
+        const uint32_t dst = smem_u32(q_smem) + (halves ? s * C::kQSlot : 0) + r * 128;
         const bool in = row_in();
-        uint4 w[kD / 8];
-#pragma unroll
-        for (int i = 0; i < kD / 8; ++i) {   // 16-byte pieces
-          w[i] = make_uint4(0u, 0u, 0u, 0u);
-          if (in && 8 * i < p.head_dim) w[i] = *reinterpret_cast<const uint4*>(q + 8 * i);
+        auto piece = [&](int i) {   // 16 bytes
+          return in && 8 * i < p.head_dim ? *reinterpret_cast<const uint4*>(q + 8 * i) : make_uint4(0u, 0u, 0u, 0u);
+        };
+        if constexpr (kCodes) {
+          // fp16 after a power of two that brings the row's largest |q| into [1, 2) (a zero, infinite or
+          // NaN row as it is)
+          uint32_t top = 0u;
+#pragma unroll 8
+          for (int i = 0; i < kD / 8; ++i) {
+            const uint4 w = piece(i);
+            top = __vmaxu2(__vmaxu2(__vmaxu2(__vmaxu2(top, w.x & 0x7FFF7FFFu), w.y & 0x7FFF7FFFu), w.z & 0x7FFF7FFFu),
+                           w.w & 0x7FFF7FFFu);
+          }
+          top = max(top & 0xFFFFu, top >> 16);
+          const float big = p.fp16 ? __half2float(__ushort_as_half((unsigned short)top)) : __uint_as_float(top << 16);
+          int e = (int)(__float_as_uint(big) >> 23);   // biased
+          e = e == 0 || e == 255 ? 127 : min(e, 252);
+          const float down = __uint_as_float((uint32_t)(254 - e) << 23);
+          mult = fminf(fmaxf(p.scale_log2 * __uint_as_float((uint32_t)e << 23) * *p.k_scale, FLT_MIN), FLT_MAX);
+          auto scaled = [&](uint32_t w) {
+            const float2 v = p.fp16 ? __half22float2(*reinterpret_cast<const __half2*>(&w)) : make_float2(bf16_lo(w), bf16_hi(w));
+            return pack_f16x2(v.x * down, v.y * down);
+          };
+#pragma unroll 8
+          for (int i = 0; i < (stores_q ? kD / 8 : 0); ++i) {
+            const uint4 w = piece(i);
+            st_shared_v4(dst + (i >> 3) * C::kQChunk + (((i & 7) ^ (r & 7)) << 4), scaled(w.x), scaled(w.y), scaled(w.z),
+                         scaled(w.w));
+          }
+        } else {
+#pragma unroll 16
+          for (int i = 0; i < kD / 8; ++i) {
+            const uint4 w = piece(i);
+            st_shared_v4(dst + (i >> 3) * C::kQChunk + (((i & 7) ^ (r & 7)) << 4), w.x, w.y, w.z, w.w);
+          }
         }
-#pragma unroll
-        for (int i = 0; i < kD / 8; ++i)
-          st_shared_v4(dst + (i >> 3) * C::kChunk + (((i & 7) ^ (r & 7)) << 4), w[i].x, w[i].y, w[i].z, w[i].w);
         fence_proxy_async_smem();
       }
       __syncwarp();
@@ -463,31 +571,32 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (up) up = mbar_wait(&s_full[2 * s + hf], s_phase, ctl);
         __syncwarp();
         tc_fence_after();
-        uint32_t v[2][32];
-        tmem_ld32(at_s, v[0]);
-        tmem_ld32(at_s + 32, v[1]);
+        constexpr int kC = kHalf / 32;
+        uint32_t v[kC][32];
+#pragma unroll
+        for (int c = 0; c < kC; ++c) tmem_ld32(at_s + 32 * c, v[c]);
         const unsigned bads = *(volatile unsigned*)&sh.bad_pages[(g.tiles_done + tile) % kBadRing];
         tmem_ld_wait();
         if (tail || bads != 0u) {
           const int row = row_of(), t = row / p.group;
           const int64_t key = (int64_t)(g.first + tile) * kTile + kHalf * hf;
 #pragma unroll
-          for (int c = 0; c < 2; ++c)
-            hide(tail ? seen_bits(p, g.s, g.s.first + t, t, key + 32 * c) : 0xFFFFFFFFu, bads, 2 * hf + c, tp.box_rows,
+          for (int c = 0; c < kC; ++c)
+            hide(tail ? seen_bits(p, g.s, g.s.first + t, t, key + 32 * c) : 0xFFFFFFFFu, bads, kC * hf + c, tp.box_rows,
                  v[c]);
         }
         float top[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) top[i] = __uint_as_float(v[0][i]);
 #pragma unroll
-        for (int i = 8; i < 64; i += 16)
+        for (int i = 8; i < kHalf; i += 16)
 #pragma unroll
           for (int k = 0; k < 8; ++k)
             top[k] = max_nan(top[k], __uint_as_float(v[(i + k) >> 5][(i + k) & 31]),
-                             i + 8 < 64 ? __uint_as_float(v[(i + 8 + k) >> 5][(i + 8 + k) & 31]) : top[k]);
+                             i + 8 < kHalf ? __uint_as_float(v[(i + 8 + k) >> 5][(i + 8 + k) & 31]) : top[k]);
         const float cand = max_nan(max_nan(top[0], top[1], top[2]), max_nan(top[3], top[4], top[5]),
                                    max_nan(top[6], top[7], top[7])) *
-                           p.scale_log2;
+                           mult;
         const bool rise = cand > m + kSlack || (m == -INFINITY && cand > m);
         if (__any_sync(0xFFFFFFFFu, rise)) {
           const float f = rise ? exp2_fast(m - cand) : 1.0f;
@@ -510,11 +619,11 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
           }
         }
-        const float2 scale2 = splat(p.scale_log2), base2 = splat(m == -INFINITY ? 0.0f : -m);
+        const float2 scale2 = splat(mult), base2 = splat(m == -INFINITY ? 0.0f : -m);
         // (with a NaN or an infinity among the scores the row is NaN)
         float2 sum = make_float2(cand < INFINITY ? 0.0f : __uint_as_float(0x7FFFFFFFu), 0.0f);
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
+        for (int c = 0; c < kC; ++c) {
           uint32_t w[16];
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
@@ -527,14 +636,14 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         l += sum.x + sum.y;
         if (tail) {
-          // V's rows of the half, two threads each: nothing but finite values may meet a P of zero
+          // V's rows of the half, two threads (or four) each: nothing but finite values may meet a P of zero
           const uint32_t pos = g.base + v_pos(halves, tile, n);
           if (up) up = mbar_wait(&full[slot_of(pos)], phase_of(pos), ctl);
-          const int key_row = kHalf * hf + (r & 63);
+          const int key_row = kHalf * hf + (r & (kHalf - 1));
           const uint32_t va = smem_u32(ring + slot_of(pos) * C::kSlot) + key_row * 128;
           const bool in = (int64_t)(g.first + tile) * kTile + key_row < g.s.keys;
 #pragma unroll 1
-          for (int i = r >> 6; i < kD / 8; i += 2) {
+          for (int i = r / kHalf; i < kD / 8; i += 128 / kHalf) {
             const uint32_t a = va + (i >> 3) * C::kChunk + (((i & 7) ^ (r & 7)) << 4);
             uint32_t x[4];
             asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
@@ -584,7 +693,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               st_shared_v4(dst + (((c / 4 + i) ^ (r & 7)) << 4), o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
           }
         }
-        softmax_sync();
+        softmax_sync<C::kSoftThreads>();
       }
       if (halves || s == 0) {
         float f0 = 1.0f, f1 = 0.0f;
@@ -600,7 +709,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int row = row_of(), t = row / p.group, head = g.h * p.group + row % p.group;
         const int64_t token = g.s.first + t;
         const int64_t at_part = (int64_t)(2 * blockIdx.x + (g.begun ? 0 : 1)) * kRows + my_row;
-        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+        const float inv = l == 0.0f ? 0.0f : (kCodes ? *p.v_scale : 1.0f) / l;
         const uint32_t src = smem_u32(q_smem) + r * (kD * 4);
 #pragma unroll 1
         for (int c = 0; c < p.head_dim; c += 32) {
@@ -633,14 +742,17 @@ __global__ void __launch_bounds__(kThreads, 1)
                 continue;
               const int page = p.table[g.b * p.table_stride + index];
               if (page < 0 || page >= p.pages) continue;
-              const uint16_t* const x =
-                  reinterpret_cast<const uint16_t*>(p.v + page * p.v_page + slot * p.v_slot + g.h * p.v_head) + c;
+              const uint8_t* const x = p.v + page * p.v_page + slot * p.v_slot + g.h * p.v_head;
 #pragma unroll
               for (int i = 0; i < 32; ++i) {
                 if (c + i >= p.head_dim) break;
-                const uint32_t w = x[i];
-                if ((w & 0x7FFFu) >= (kF16 ? 0x7C00u : 0x7F80u))
-                  f[i] += kF16 ? __half2float(__ushort_as_half((unsigned short)w)) : __uint_as_float(w << 16);
+                if constexpr (kCodes) {
+                  if ((x[c + i] & 0x7Fu) == 0x7Fu) f[i] = __uint_as_float(0x7FFFFFFFu);
+                } else {
+                  const uint32_t w = reinterpret_cast<const uint16_t*>(x)[c + i];
+                  if ((w & 0x7FFFu) >= (kF16 ? 0x7C00u : 0x7F80u))
+                    f[i] += kF16 ? __half2float(__ushort_as_half((unsigned short)w)) : __uint_as_float(w << 16);
+                }
               }
             }
           }
@@ -665,7 +777,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       }
       tc_fence_before();
-      softmax_sync();   // Q's place and the flags are free, the next segment is published
+      softmax_sync<C::kSoftThreads>();   // Q's place and the flags are free, the next segment is published
       if (thread == 0) sh.odd_values = 0;
     }
   }
@@ -681,7 +793,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 // Items that end in other CTAs than they begin in: CTA x joins the one that begins in CTA x of
 // the kernel above, kJoinRows rows of it.
 constexpr int kJoinRows = 32, kJoinThreads = 256;
-template <int kDC>
+template <int kDC, int kRows, int kTile>
 __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const AttnParams p, int ctas) {
   __shared__ float2 stat[kJoinRows];
   __shared__ RunScratch scratch;
@@ -697,56 +809,69 @@ __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const AttnParam
   const int all = (int)min((int64_t)kRows, (int64_t)cur.s.fresh * p.group - (int64_t)cur.rt * kRows);
   const int row0 = (int)blockIdx.y * kJoinRows, rows = min(kJoinRows, all - row0);
   if (rows <= 0) return;
-  join_parts<kRows, 64 * kDC, kJoinThreads>(p, cur, cta, cta, (int)split_owner(run.split, item1), 1, true, 1.0f,
+  const float v_scale = p.v_scale != nullptr ? *p.v_scale : 1.0f;
+  join_parts<kRows, 64 * kDC, kJoinThreads>(p, cur, cta, cta, (int)split_owner(run.split, item1), 1, true, v_scale,
                                             row0, rows, (int)threadIdx.x, stat, [] { __syncthreads(); });
 }
 
-template <bool kF16, int kDC>
+template <bool kF16, int kDC, bool kCodes>
 cudaError_t launch_cfg(TileParams tp, const CUtensorMap& tk, const CUtensorMap& tv, cudaStream_t s, Device dev) {
-  using C = TileCfg<kDC>;
-  auto kern = attn_tiles_kernel<kF16, kDC>;
+  using C = TileCfg<kDC, kCodes>;
+  auto kern = attn_tiles_kernel<kF16, kDC, kCodes>;
   static PerDevice<cudaError_t> per_device;
   const cudaError_t e = per_device.get(dev.index, [&] {
     return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem);
   });
   if (e != cudaSuccess) return e;
-  constexpr int64_t kPart = 2 * kRows * ((int64_t)64 * kDC * 4 + 8);
+  constexpr int64_t kPart = 2 * C::kRows * ((int64_t)64 * kDC * 4 + 8);
   const int ctas = (int)std::min<int64_t>(dev.num_sms, std::min<int64_t>(kMostCtas, (kWorkspaceBytes - kCountBytes) / kPart));
   AttnParams& p = tp.a;
   p.part_ml = reinterpret_cast<float2*>(reinterpret_cast<uint8_t*>(p.counts) + kCountBytes);
-  p.part = reinterpret_cast<float*>(p.part_ml + (int64_t)2 * kRows * ctas);
+  p.part = reinterpret_cast<float*>(p.part_ml + (int64_t)2 * C::kRows * ctas);
   p.least = 2;
-  const cudaError_t st = launch_pdl(kern, dim3((unsigned)ctas), kThreads, C::kSmem, s, tk, tv, tp);
+  const cudaError_t st = launch_pdl(kern, dim3((unsigned)ctas), C::kThreads, C::kSmem, s, tk, tv, tp);
   if (st != cudaSuccess) return st;
-  return launch_pdl(attn_join_kernel<kDC>, dim3((unsigned)ctas, kRows / kJoinRows), kJoinThreads, 0, s, p, ctas);
+  return launch_pdl(attn_join_kernel<kDC, C::kRows, C::kTile>, dim3((unsigned)ctas, C::kRows / kJoinRows), kJoinThreads, 0, s, p, ctas);
 }
 
 }  // namespace
 
 bool attention_tiles_fit(const AttnParams& p) {
-  const bool pages = p.page_size % 8 == 0 && (p.page_size >= kTile ? p.page_size % kTile : kTile % p.page_size) == 0;
-  return p.head_dim <= 128 && pages && p.tokens * p.group < (int64_t)1 << 30 &&
-         (int64_t)p.page_size * p.table_width < (int64_t)1 << 31 && p.k_slot > 0 && p.k_head > 0 && p.k_page > 0 && p.v_slot > 0 && p.v_head > 0 &&
-         p.v_page > 0;
+  const int tile = p.head_dim <= 128 ? 128 : 64;
+  const bool pages = p.page_size % 8 == 0 && (p.page_size >= tile ? p.page_size % tile : tile % p.page_size) == 0;
+  return pages && p.k_slot > 0 && p.k_head > 0 && p.k_page > 0 && p.v_slot > 0 && p.v_head > 0 && p.v_page > 0 &&
+         p.tokens * p.group < (int64_t)1 << 30 && (int64_t)p.page_size * p.table_width < (int64_t)1 << 31;
 }
 
-cudaError_t launch_attention_tiles(const AttnParams& p, bool fp16, uint64_t timeout_ns, cudaStream_t s, Device dev) {
+cudaError_t launch_attention_tiles(const AttnParams& p, CacheKind kind, uint64_t timeout_ns, cudaStream_t s, Device dev) {
+  const int tile = p.head_dim <= 128 ? 128 : 64, chunks = (p.head_dim + 63) / 64;
+  const bool codes = kind == CacheKind::kE4m3, fp16 = kind == CacheKind::kFp16;
   TileParams tp{};
   tp.a = p;
-  tp.box_rows = std::min(p.page_size, kTile);
-  tp.boxes = kTile / tp.box_rows;
+  tp.box_rows = std::min(p.page_size, tile);
+  tp.boxes = tile / tp.box_rows;
   tp.timeout_ns = timeout_ns;
   CUtensorMap tk, tv;
   const uint64_t dims[4] = {(uint64_t)p.head_dim, (uint64_t)p.page_size, (uint64_t)p.heads, (uint64_t)p.pages};
-  const uint32_t box[4] = {64u, (uint32_t)tp.box_rows, 1u, 1u};
-  if (encode_tensor_map_4d16(&tk, p.k, fp16, dims, {(uint64_t)p.k_slot, (uint64_t)p.k_head, (uint64_t)p.k_page}, box) !=
-          CUDA_SUCCESS ||
-      encode_tensor_map_4d16(&tv, p.v, fp16, dims, {(uint64_t)p.v_slot, (uint64_t)p.v_head, (uint64_t)p.v_page}, box) !=
-          CUDA_SUCCESS)
+  // 16-bit: 64 elements of a box's keys, swizzled; codes: whole rows as they lie
+  const uint32_t box[4] = {codes ? 64u * (uint32_t)chunks : 64u, (uint32_t)tp.box_rows, 1u, 1u};
+  auto encode = [&](CUtensorMap* map, const void* base, int64_t slot, int64_t head, int64_t page) {
+    return encode_tensor_map_4d(map, base, codes ? 1 : fp16 ? 3 : 2, dims, {(uint64_t)slot, (uint64_t)head, (uint64_t)page},
+                                box);
+  };
+  if (encode(&tk, p.k, p.k_slot, p.k_head, p.k_page) != CUDA_SUCCESS ||
+      encode(&tv, p.v, p.v_slot, p.v_head, p.v_page) != CUDA_SUCCESS)
     return cudaErrorInvalidValue;
-  if (p.head_dim <= 64)
-    return fp16 ? launch_cfg<true, 1>(tp, tk, tv, s, dev) : launch_cfg<false, 1>(tp, tk, tv, s, dev);
-  return fp16 ? launch_cfg<true, 2>(tp, tk, tv, s, dev) : launch_cfg<false, 2>(tp, tk, tv, s, dev);
+  auto launch = [&](auto dc) {
+    constexpr int kDC = decltype(dc)::value;
+    return codes  ? launch_cfg<true, kDC, true>(tp, tk, tv, s, dev)
+           : fp16 ? launch_cfg<true, kDC, false>(tp, tk, tv, s, dev)
+                  : launch_cfg<false, kDC, false>(tp, tk, tv, s, dev);
+  };
+  return chunks == 1   ? launch(std::integral_constant<int, 1>{})
+         : chunks == 2 ? launch(std::integral_constant<int, 2>{})
+         : chunks == 3 ? launch(std::integral_constant<int, 3>{})
+                       : launch(std::integral_constant<int, 4>{});
 }
 
 }  // namespace qlin

@@ -1651,12 +1651,15 @@ CUresult encode_tensor_map_out_bf16(CUtensorMap* map, void* base, uint64_t cols,
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
 }
 
-CUresult encode_tensor_map_4d16(CUtensorMap* map, const void* base, bool fp16, const uint64_t (&dims)[4],
-                                const uint64_t (&strides)[3], const uint32_t (&box)[4]) {
+CUresult encode_tensor_map_4d(CUtensorMap* map, const void* base, int kind, const uint64_t (&dims)[4],
+                              const uint64_t (&strides)[3], const uint32_t (&box)[4]) {
   const cuuint64_t d[4] = {dims[0], dims[1], dims[2], dims[3]}, st[3] = {strides[0], strides[1], strides[2]};
   const cuuint32_t b[4] = {box[0], box[1], box[2], box[3]};
-  return encode_4d(map, fp16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, base, d, st, b,
-                   CU_TENSOR_MAP_SWIZZLE_128B);
+  return encode_4d(map,
+                   kind == 1   ? CU_TENSOR_MAP_DATA_TYPE_UINT8
+                   : kind == 3 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16
+                               : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16,
+                   base, d, st, b, kind == 1 ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
 CUresult encode_tensor_map_codes(CUtensorMap* map, const void* base, uint64_t k_bytes, uint64_t rows,

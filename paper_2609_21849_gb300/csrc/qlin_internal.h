@@ -139,9 +139,10 @@ cudaError_t launch_wait_selftest(uint64_t timeout_ns, cudaStream_t s, unsigned* 
 CUresult encode_tensor_map_out_bf16(CUtensorMap* map, void* base, uint64_t cols, uint64_t rows,
                                     bool fp16 = false);
 
-// 16-bit elements, four dimensions (innermost first, strides of the others in bytes), 128-byte swizzle.
-CUresult encode_tensor_map_4d16(CUtensorMap* map, const void* base, bool fp16, const uint64_t (&dims)[4],
-                                const uint64_t (&strides)[3], const uint32_t (&box)[4]);
+// Four dimensions (innermost first, strides of the others in bytes) of bytes (kind 1, not swizzled),
+// bf16 (2) or fp16 (3; 128-byte swizzle).
+CUresult encode_tensor_map_4d(CUtensorMap* map, const void* base, int kind, const uint64_t (&dims)[4],
+                              const uint64_t (&strides)[3], const uint32_t (&box)[4]);
 // FP8 codes [rows, k_bytes]: 128-byte x box_rows boxes, 128-byte swizzle.
 CUresult encode_tensor_map_codes(CUtensorMap* map, const void* base, uint64_t k_bytes, uint64_t rows,
                                  uint32_t box_rows);

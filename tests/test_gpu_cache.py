@@ -196,7 +196,7 @@ def test_many_rows(fmt, dtype):
 
 
 @pytest.mark.parametrize("fmt,dtype", FORMATS)
-@pytest.mark.parametrize("D", [16, 64, 80, 96, 128, 160])
+@pytest.mark.parametrize("D", [16, 64, 80, 96, 128, 160, 192, 256])
 @pytest.mark.parametrize("page", [8, 24, 64, 128, 256])
 def test_many_rows_head_dims_and_pages(page, D, fmt, dtype):
     # one half of the rows and two, tiles that end in a page, sequences without a cache
@@ -204,11 +204,12 @@ def test_many_rows_head_dims_and_pages(page, D, fmt, dtype):
     _attend([128, 64, 383, 0], [64, 128, 1, 33], 1, 4, D, page, fmt, dtype, tree=False)
 
 
-@pytest.mark.parametrize("fmt,dtype", FORMATS[:2])
-@pytest.mark.parametrize("cached", [0, 1, 91, 92, 127, 128, 129, 255, 256, 300, 2000, 40000])
+@pytest.mark.parametrize("fmt,dtype", FORMATS)
+@pytest.mark.parametrize("cached", [0, 1, 63, 64, 91, 92, 127, 128, 129, 255, 256, 300, 2000, 40000])
 def test_many_rows_lengths(cached, fmt, dtype):
     _attend([cached], [36], 1, 3, 64, 16, fmt, dtype)
     _attend([cached, 7 * cached // 8], [130, 70], 1, 2, 128, 64, fmt, dtype)
+    _attend([cached, 7 * cached // 8], [130, 70], 1, 2, 192, 32, fmt, dtype)
     _attend([cached // 2] * 70, [37] * 70, 3, 1, 64, 32, fmt, dtype, tree=False)
 
 
