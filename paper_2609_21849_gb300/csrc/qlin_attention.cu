@@ -44,12 +44,19 @@ cudaError_t launch_cache_attention(const qlin_cache_t& c, const qlin_cache_atten
   p.fp16 = a.dtype == QLIN_FP16 ? 1 : 0;
   p.counts = static_cast<unsigned*>(workspace);
   p.err = err;
-  // more rows per sequence and KV head, on average, than the mma.sync kernel shares a read among
   const CacheKind kind = c.format == QLIN_CACHE_E4M3   ? CacheKind::kE4m3
                          : c.format == QLIN_CACHE_FP16 ? CacheKind::kFp16
                                                        : CacheKind::kBf16;
-  if (p.tokens * p.group > (int64_t)32 * p.sequences && attention_tiles_fit(p))
-    return launch_attention_tiles(p, kind, timeout_ns, s, dev);
+  // The tiles from 17 rows per sequence and KV head on (on average), where the mma.sync kernel would
+  // read the keys again for every 16: in us, 16 sequences of 4096-8192 keys, 8 heads of 128, tiles and
+  // mma.sync, 16 rows 86, 86 (E4M3 97, 62), 20 rows 86, 181 (97, 173), 64 rows 90, 344 (102, 328).  And
+  // for 16-bit heads past 192, whose fragments leave mma.sync one CTA of four warps per SM, over a
+  // table with room for 128 MB of keys and values (one token, heads of 256, 4096 keys: 86, 126; one
+  // sequence of 500 16, 14).
+  const bool many = p.tokens * p.group > (int64_t)16 * p.sequences;
+  const bool wide = kind != CacheKind::kE4m3 && p.head_dim > 192 &&
+                    (int64_t)p.sequences * p.table_width * p.page_size >= ((int64_t)128 << 20) / (4 * p.heads * p.head_dim);
+  if ((many || wide) && attention_tiles_fit(p)) return launch_attention_tiles(p, kind, timeout_ns, s, dev);
   return c.format == QLIN_CACHE_E4M3   ? launch_attention_e4m3(p, s, dev)
          : c.format == QLIN_CACHE_FP16 ? launch_attention_fp16(p, s, dev)
                                        : launch_attention_bf16(p, s, dev);

@@ -660,14 +660,17 @@ cudaError_t launch_attn(AttnParams p, cudaStream_t s, Device dev) {
   return launch_pdl(attn_kernel<kKind, kD, kM>, dim3((unsigned)ctas), kWarps * 32, C::kSmem, s, p);
 }
 
-// Rows per sequence and KV head, on average, say whether 32 rows share a read of the keys.
+// Rows past 16 come here where pages do not fit the tiles.  Heads of up to 64 then take 32 rows to a
+// read of the keys (16 sequences of 4096-8192 keys, 20 rows: 61 us, twice 16 rows 112); longer heads'
+// fragments for 32 rows do not fit the registers (heads of 128: 181 us, twice 16 rows 157).
 template <CacheKind kKind>
 cudaError_t launch_attn_kind(const AttnParams& p, cudaStream_t s, Device dev) {
-  const bool more = p.tokens * p.group > (int64_t)16 * p.sequences;
-  if (p.head_dim <= 64) return more ? launch_attn<kKind, 64, 2>(p, s, dev) : launch_attn<kKind, 64, 1>(p, s, dev);
+  if (p.head_dim <= 64)
+    return p.tokens * p.group > (int64_t)16 * p.sequences ? launch_attn<kKind, 64, 2>(p, s, dev)
+                                                          : launch_attn<kKind, 64, 1>(p, s, dev);
   if constexpr (kKind != CacheKind::kE4m3)
-    if (p.head_dim <= 96) return more ? launch_attn<kKind, 96, 2>(p, s, dev) : launch_attn<kKind, 96, 1>(p, s, dev);
-  if (p.head_dim <= 128) return more ? launch_attn<kKind, 128, 2>(p, s, dev) : launch_attn<kKind, 128, 1>(p, s, dev);
+    if (p.head_dim <= 96) return launch_attn<kKind, 96, 1>(p, s, dev);
+  if (p.head_dim <= 128) return launch_attn<kKind, 128, 1>(p, s, dev);
   if (p.head_dim <= 192) return launch_attn<kKind, 192, 1>(p, s, dev);
   return launch_attn<kKind, 256, 1>(p, s, dev);
 }
