@@ -708,7 +708,7 @@ __global__ void __launch_bounds__(TileCfg<kDC, kCodes>::kThreads, 1)
         const bool in = row_in(), whole = g.whole;
         const int row = row_of(), t = row / p.group, head = g.h * p.group + row % p.group;
         const int64_t token = g.s.first + t;
-        const int64_t at_part = (int64_t)(2 * blockIdx.x + (g.begun ? 0 : 1)) * kRows + my_row;
+        const int64_t at_part = (int64_t)(2 * blockIdx.x + (g.begun ? 0 : 1)) * kRows;
         const float inv = l == 0.0f ? 0.0f : (kCodes ? *p.v_scale : 1.0f) / l;
         const uint32_t src = smem_u32(q_smem) + r * (kD * 4);
 #pragma unroll 1
@@ -762,16 +762,22 @@ __global__ void __launch_bounds__(TileCfg<kDC, kCodes>::kThreads, 1)
               const int d = c + 4 * i;
               if (d >= p.head_dim) break;
               const float4 x = make_float4(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]);
-              if (whole)
-                store_out4(p, token, head, d, make_float4(x.x * inv, x.y * inv, x.z * inv, x.w * inv));
-              else
-                *reinterpret_cast<float4*>(p.part + at_part * kD + d) = x;
+              if (!whole) {
+                *part_sums<kRows, kD>(p, at_part, my_row, d) = x;
+              } else if ((i & 1) == 0) {   // (head_dim % 16 == 0: eight elements at a time)
+                auto pair = [&](float a, float b) {
+                  return p.fp16 ? pack_f16x2(a * inv, b * inv) : pack_bf16x2(a * inv, b * inv);
+                };
+                *reinterpret_cast<uint4*>(p.out + token * p.out_token + (int64_t)head * p.out_head + d) =
+                    make_uint4(pair(x.x, x.y), pair(x.z, x.w), pair(f[4 * i + 4], f[4 * i + 5]),
+                               pair(f[4 * i + 6], f[4 * i + 7]));
+              }
             }
           }
         }
         if (in) {
           if (!whole)
-            p.part_ml[at_part] = make_float2(m, l);
+            p.part_ml[at_part + my_row] = make_float2(m, l);
           else if (p.lse != nullptr)
             p.lse[token * p.lse_token + head] = log_sum(m, l);
         }
@@ -810,8 +816,7 @@ __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const AttnParam
   const int row0 = (int)blockIdx.y * kJoinRows, rows = min(kJoinRows, all - row0);
   if (rows <= 0) return;
   const float v_scale = p.v_scale != nullptr ? *p.v_scale : 1.0f;
-  join_parts<kRows, 64 * kDC, kJoinThreads>(p, cur, cta, cta, (int)split_owner(run.split, item1), 1, true, v_scale,
-                                            row0, rows, (int)threadIdx.x, stat, [] { __syncthreads(); });
+  join_parts<kRows, 64 * kDC, kJoinThreads>(p, cur, cta, (int)split_owner(run.split, item1), v_scale, row0, rows, stat);
 }
 
 template <bool kF16, int kDC, bool kCodes>

@@ -179,18 +179,23 @@ __device__ __forceinline__ int64_t part_row(int cta, int first, int row) {
   return (int64_t)(2 * cta + (cta == first ? 1 : 0)) * kRows + row;
 }
 
-// Rows row0 .. row0 + rows - 1 of an item, whose parts the CTAs from, from + step, ... to left
-// in the workspace (first: the item's first CTA), joined in the order of the keys: to the
-// output, or to from's part in place.  Called by all of kThreads threads, which `sync` joins;
-// stat: kRows of them in shared memory.
-template <int kRows, int kD, int kThreads, typename Sync>
-__device__ __forceinline__ void join_parts(const AttnParams& p, const Cursor& c, int first, int from, int to, int step,
-                                           bool output, float v_scale, int row0, int rows, int thread, float2* stat,
-                                           Sync&& sync) {
+// A part's sums lie [kD / 4][kRows] in fours: threads with a row each write and read whole lines.
+template <int kRows, int kD>
+__device__ __forceinline__ float4* part_sums(const AttnParams& p, int64_t part_row0, int row, int d) {
+  return reinterpret_cast<float4*>(p.part + part_row0 * kD) + (int64_t)(d / 4) * kRows + row;
+}
+
+// Rows row0 .. row0 + rows - 1 of an item, whose parts the CTAs first to last left in the
+// workspace, joined in the order of the keys.  Called by all of kThreads threads of a CTA; stat:
+// `rows` of them in shared memory.
+template <int kRows, int kD, int kThreads>
+__device__ __forceinline__ void join_parts(const AttnParams& p, const Cursor& c, int first, int last, float v_scale,
+                                           int row0, int rows, float2* stat) {
+  const int thread = (int)threadIdx.x;
   for (int i = thread; i < rows; i += kThreads) {
     float m = -INFINITY, l = 0.0f;
 #pragma unroll 4
-    for (int q = from; q <= to; q += step) {
+    for (int q = first; q <= last; ++q) {
       const float2 ml = __ldcg(&p.part_ml[part_row<kRows>(q, first, row0 + i)]);
       const float now = fmaxf(m, ml.x), base = now == -INFINITY ? 0.0f : now;
       l = fmaf(l, exp2_fast(m - base), ml.y * exp2_fast(ml.x - base));
@@ -198,8 +203,8 @@ __device__ __forceinline__ void join_parts(const AttnParams& p, const Cursor& c,
     }
     stat[i] = make_float2(m, l);
   }
-  sync();
-  const int d4s = p.head_dim / 4, items = rows * d4s;
+  __syncthreads();
+  const int items = rows * (p.head_dim / 4);
   constexpr int kAtOnce = 4;
   for (int i0 = thread; i0 < items; i0 += kThreads * kAtOnce) {
     float4 o[kAtOnce];
@@ -207,18 +212,17 @@ __device__ __forceinline__ void join_parts(const AttnParams& p, const Cursor& c,
 #pragma unroll
     for (int k = 0; k < kAtOnce; ++k) {
       const int i = min(i0 + k * kThreads, items - 1);
-      const float m = stat[i / d4s].x;
+      const float m = stat[i % rows].x;
       base[k] = m == -INFINITY ? 0.0f : m;
       o[k] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     }
 #pragma unroll 2
-    for (int q = from; q <= to; q += step) {
+    for (int q = first; q <= last; ++q) {
 #pragma unroll
       for (int k = 0; k < kAtOnce; ++k) {
-        const int i = min(i0 + k * kThreads, items - 1);
-        const int64_t at = part_row<kRows>(q, first, row0 + i / d4s);
-        const float f = exp2_fast(__ldcg(&p.part_ml[at].x) - base[k]);
-        const float4 v = __ldcg(reinterpret_cast<const float4*>(p.part + at * kD + i % d4s * 4));
+        const int i = min(i0 + k * kThreads, items - 1), row = row0 + i % rows;
+        const float f = exp2_fast(__ldcg(&p.part_ml[part_row<kRows>(q, first, row)].x) - base[k]);
+        const float4 v = __ldcg(part_sums<kRows, kD>(p, part_row<kRows>(q, first, 0), row, i / rows * 4));
         o[k] = make_float4(fmaf(v.x, f, o[k].x), fmaf(v.y, f, o[k].y), fmaf(v.z, f, o[k].z), fmaf(v.w, f, o[k].w));
       }
     }
@@ -226,23 +230,15 @@ __device__ __forceinline__ void join_parts(const AttnParams& p, const Cursor& c,
     for (int k = 0; k < kAtOnce; ++k) {
       const int i = i0 + k * kThreads;
       if (i >= items) break;
-      const int row = i / d4s, d = i % d4s * 4;
+      const int row = i % rows, d = i / rows * 4;
       const float2 ml = stat[row];
-      if (output) {
-        const int64_t r = (int64_t)c.rt * kRows + row0 + row;
-        const int64_t token = c.s.first + r / p.group;
-        const int head = c.h * p.group + (int)(r % p.group);
-        const float inv = ml.y == 0.0f ? 0.0f : v_scale / ml.y;
-        store_out4(p, token, head, d, make_float4(o[k].x * inv, o[k].y * inv, o[k].z * inv, o[k].w * inv));
-        if (p.lse != nullptr && d == 0) p.lse[token * p.lse_token + head] = log_sum(ml.x, ml.y);
-      } else {
-        *reinterpret_cast<float4*>(p.part + part_row<kRows>(from, first, row0 + row) * kD + d) = o[k];
-      }
+      const int64_t r = (int64_t)c.rt * kRows + row0 + row;
+      const int64_t token = c.s.first + r / p.group;
+      const int head = c.h * p.group + (int)(r % p.group);
+      const float inv = ml.y == 0.0f ? 0.0f : v_scale / ml.y;
+      store_out4(p, token, head, d, make_float4(o[k].x * inv, o[k].y * inv, o[k].z * inv, o[k].w * inv));
+      if (p.lse != nullptr && d == 0) p.lse[token * p.lse_token + head] = log_sum(ml.x, ml.y);
     }
-  }
-  if (!output) {
-    sync();   // its maxima and sums have been read
-    for (int i = thread; i < rows; i += kThreads) p.part_ml[part_row<kRows>(from, first, row0 + i)] = stat[i];
   }
 }
 
