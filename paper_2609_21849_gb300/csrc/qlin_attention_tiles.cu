@@ -13,12 +13,21 @@
 // stays below 2^8 and the sums in fp32 (both fine in 16 bits: a P's rounding is relative).
 //   Per tile of 256 rows and 128 keys of 128: 2048 cycles of MMAs, 2048 of exponentials (16 a
 // cycle and SM), 64 KB of keys and values, about 2850 cycles of an SM's share of HBM.
-// Roles: warps 0 and 2 load K and V, warp 1 issues MMAs, warps 4-11 and 12-19 are the streams' softmax.
+// Roles: warps 0 and 2 load K and V, warp 1 issues MMAs, warp 3 walks the run for the softmax a
+// segment ahead of it, warps 4-11 and 12-19 are the streams' softmax.
 // Tiles with new tokens are masked, and V's slots behind the last key and values that are
 // not finite are zeroed in shared memory: 0 times them would reach rows that do not see them.
 // (Rows that do see such a value take it at the end.)
-// An item that several CTAs share is joined by a second kernel, many CTAs to an item (by one of
-// these, at one SM's rate of reading, the 16 trees below took 262 us, not 2xx).
+//   Heads above 128 fill tensor memory with one stream's O: tiles of 64 keys, the two halves of a
+// tile's keys taking the streams' turns.  E4M3 codes land in a ring of their own, and four warps
+// convert them to fp16 tiles (every code is an fp16); Q becomes fp16 after a power of two per row.
+// An item that several CTAs share is joined by a second kernel, many CTAs to an item (joined by one
+// of these, at one SM's rate of reading, the trees below took 40 us longer).
+//   Measured, 16 trees of 64 tokens behind 4096-8192 keys, 8 KV heads of 128, 3 query heads each:
+// 220 us (bf16; the keys and values from HBM need 126, the MMAs 106, the exponentials as much), 249
+// from E4M3, 297 at heads of 256.  A segment's end (the last tiles' products, O's way out, the next
+// Q) leaves the tensor cores idle for 5000 to 7000 cycles; the tensor pipe is busy a third of the
+// time, the exponentials and the scores' way through registers bound the rest.
 #include <type_traits>
 
 #include "qlin_attention_work.cuh"
@@ -90,7 +99,7 @@ struct TileCfg {
   static constexpr int kRoleRegs = kThreads == 512 ? 88 : 104, kSoftRegs = kThreads == 512 ? 152 : 200;
   static constexpr int kLaunchRegs = kThreads == 512 ? 128 : 168;
   static_assert((kThreads - kSoftThreads) * kRoleRegs + kSoftThreads * kSoftRegs <= kThreads * kLaunchRegs, "registers");
-  static_assert((2 * kSlots + 2 * kRawSlots + 14) * 8 <= kBarrierBytes && kSlots >= 3, "shared memory");
+  static_assert((2 * kSlots + 2 * kRawSlots + 18) * 8 <= kBarrierBytes && kSlots >= 3, "shared memory");
 };
 
 struct TileParams {
@@ -126,20 +135,39 @@ template <int kSoftThreads>
 __device__ __forceinline__ void softmax_sync() {
   asm volatile("bar.sync 1, %0;" ::"n"(kSoftThreads) : "memory");
 }
+// The same, and whether any thread says so.
+template <int kSoftThreads>
+__device__ __forceinline__ bool softmax_any(bool x) {
+  uint32_t r;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbar.red.or.pred q, 1, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(r)
+      : "r"((uint32_t)x), "n"(kSoftThreads)
+      : "memory");
+  return r != 0u;
+}
+
 // Where in the order of loads a segment's tiles lie (n tiles; K and V of each).  Rows in two
 // halves: K0 V0 K1 V1 ...  Tiles in turn: K0 K1 V0 K2 V1 K3 ...: each as the MMAs take them.
 __device__ __forceinline__ int k_pos(bool halves, int j) { return halves ? 2 * j : j < 2 ? j : 2 * j - 1; }
 __device__ __forceinline__ int v_pos(bool halves, int j, int n) { return halves ? 2 * j + 1 : min(2 * j + 2, n + j); }
 
 // 32 bits of a row's mask from new token i on (negative ones are cached tokens: seen).
-__device__ __forceinline__ uint32_t mask_window(const uint64_t* m, int words, int64_t i) {
+template <typename Words>
+__device__ __forceinline__ uint32_t mask_window(const Words& m, int words, int64_t i) {
   if (i <= -32) return 0xFFFFFFFFu;
   const int n = i < 0 ? (int)-i : 0;
   const int64_t at = i + n;
   const int64_t w = at >> 6;
   const int s = (int)(at & 63);
-  uint64_t v = w < words ? m[w] >> s : 0ull;
-  if (s > 32 && w + 1 < words) v |= m[w + 1] << (64 - s);
+  auto word = [&](int64_t k) -> uint64_t {
+    if constexpr (std::is_array_v<Words>)
+      return k >= words ? 0ull : k == 0 ? m[0] : m[1];   // (in registers: no index)
+    else
+      return k >= words ? 0ull : m[k];
+  };
+  uint64_t v = word(w) >> s;
+  if (s > 32) v |= word(w + 1) << (64 - s);
   return n == 0 ? (uint32_t)v : ((uint32_t)v << n) | ((1u << n) - 1u);
 }
 // The first n of 32 (n may be negative or large).
@@ -155,11 +183,14 @@ __device__ __forceinline__ uint32_t e4m3x2_half2(uint32_t codes) {
   return h;
 }
 
-// Which keys of 32 a row (new token t, number `token` of the call) sees, from key `key` on.
-__device__ __forceinline__ uint32_t seen_bits(const AttnParams& p, const CacheSeq& s, int64_t token, int t, int64_t key) {
+// Which keys of 32 a row (new token t, number `token` of the call) sees, from key `key` on.  early:
+// the row's first two mask words.
+__device__ __forceinline__ uint32_t seen_bits(const AttnParams& p, const CacheSeq& s, int64_t token, int t, int64_t key,
+                                              const uint64_t (&early)[2]) {
   const uint32_t in = first_bits(s.keys - key);
   if (p.mask == nullptr) return in & first_bits(s.cached + t + 1 - key);
-  return in & mask_window(p.mask + token * p.mask_token, p.mask_words, key - s.cached);
+  return in & (p.mask_words <= 2 ? mask_window(early, p.mask_words, key - s.cached)
+                                 : mask_window(p.mask + token * p.mask_token, p.mask_words, key - s.cached));
 }
 
 template <bool kF16>
@@ -207,7 +238,9 @@ __global__ void __launch_bounds__(TileCfg<kDC, kCodes>::kThreads, 1)
   uint64_t* const pv_done = p_ready + 4;         // the same: its product is done
   uint64_t* const q_ready = pv_done + 4;
   uint64_t* const mma_done = q_ready + 1;
-  uint64_t* const raw_full = mma_done + 1;       // kCodes: codes have landed, and have been converted
+  uint64_t* const seg_full = mma_done + 1;       // of two: a segment is published, and has been worked off
+  uint64_t* const seg_free = seg_full + 2;
+  uint64_t* const raw_full = seg_free + 2;       // kCodes: codes have landed, and have been converted
   uint64_t* const raw_empty = raw_full + C::kRawSlots;
   TileShared& sh = *reinterpret_cast<TileShared*>(raw + C::kRawSlots * C::kRawSlot + C::kBarrierBytes);
 
@@ -226,6 +259,10 @@ __global__ void __launch_bounds__(TileCfg<kDC, kCodes>::kThreads, 1)
       mbar_init(&s_full[i], 1);
       mbar_init(&p_ready[i], 4);
       mbar_init(&pv_done[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&seg_full[i], 1);
+      mbar_init(&seg_free[i], 4 * C::kStreams);
     }
     mbar_init(q_ready, 4 * C::kStreams);
     mbar_init(mma_done, 1);
@@ -427,6 +464,42 @@ __global__ void __launch_bounds__(TileCfg<kDC, kCodes>::kThreads, 1)
             break;
           }
       }
+    } else {
+      // ---- the run's segments for the softmax threads, one ahead of them ----
+      if (lane == 0) {
+        uint32_t base = 0;
+        unsigned tiles_done = 0, phase = 0;
+        int64_t unit = run.begin;
+        for (int at = 0;; at ^= 1) {
+          if (!mbar_wait(&seg_free[at], phase ^ 1u, ctl)) break;
+          phase ^= (uint32_t)at;
+          SoftSegment& g = sh.seg[at];
+          g.n = 0;
+          if (unit < run.end) {
+            const Segment sg = segment_at<C>(p, cur, unit, run.end);
+            const int64_t item0 = unit - sg.first;
+            g.s = cur.s;
+            g.base = base;
+            g.b = cur.b;
+            g.h = cur.h;
+            g.rt = cur.rt;
+            g.first = sg.first;
+            g.n = sg.n;
+            g.tiles_done = tiles_done;
+            g.halves = sg.halves;
+            g.begun = item0 < run.begin;
+            g.whole = !g.begun && item0 + cur.tiles <= run.end;
+            base += 2 * sg.n;
+            tiles_done += sg.n;
+            unit += sg.n;
+            mbar_arrive(&seg_full[at]);
+            if (unit < run.end) skip_segment<C>(p, cur, sg);
+          } else {
+            mbar_arrive(&seg_full[at]);
+            break;
+          }
+        }
+      }
     }
   } else if (kCodes && warp >= kSoftWarp0 + C::kSoftThreads / 32) {
     // ---- codes to fp16 (exactly), from the rows as they came to the MMAs' swizzled tiles ----
@@ -472,36 +545,14 @@ __global__ void __launch_bounds__(TileCfg<kDC, kCodes>::kThreads, 1)
     const uint32_t my_s = s_tmem + 128 * s + lanes, my_o = o_tmem + 128 * s + lanes;
     bool up = true;   // no wait has failed (after one, the loops run out without waiting)
     uint32_t s_phase = 0;   // of the stream's tiles
-    // Thread 0 walks the run, a segment ahead of the others.
-    int64_t unit = run.begin;
-    uint32_t base = 0;
-    unsigned tiles_done = 0;
-    auto publish = [&](int at) {
-      SoftSegment& g = sh.seg[at];
-      g.n = 0;
-      if (unit >= run.end) return;
-      const Segment sg = segment_at<C>(p, cur, unit, run.end);
-      const int64_t item0 = unit - sg.first;
-      g.s = cur.s;
-      g.base = base;
-      g.b = cur.b;
-      g.h = cur.h;
-      g.rt = cur.rt;
-      g.first = sg.first;
-      g.n = sg.n;
-      g.tiles_done = tiles_done;
-      g.halves = sg.halves;
-      g.begun = item0 < run.begin;
-      g.whole = !g.begun && item0 + cur.tiles <= run.end;
-      base += 2 * sg.n;
-      tiles_done += sg.n;
-      unit += sg.n;
-      if (unit < run.end) skip_segment<C>(p, cur, sg);
-    };
-    if (thread == 0) publish(0);
-    softmax_sync<C::kSoftThreads>();
+    uint32_t seg_phase = 0;
     for (int at = 0;; at ^= 1) {
       const SoftSegment& g = sh.seg[at];
+      if (up) up = mbar_wait(&seg_full[at], seg_phase, ctl);
+      __syncwarp();
+      seg_phase ^= (uint32_t)at;
+      // (after a wait that gave up, all leave together: no thread waits at a barrier for one that left)
+      if (softmax_any<C::kSoftThreads>(!up)) break;
       const int n = g.n;
       if (n == 0) break;
       const bool halves = g.halves;
@@ -558,9 +609,13 @@ __global__ void __launch_bounds__(TileCfg<kDC, kCodes>::kThreads, 1)
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(q_ready);
-      if (thread == 0) publish(at ^ 1);
-      __syncwarp();
 
+      uint64_t early[2] = {0ull, 0ull};   // the row's mask, on its way before a tile needs it
+      if (p.mask != nullptr && p.mask_words <= 2) {
+        const uint64_t* const words = p.mask + (g.s.first + row_of() / p.group) * p.mask_token;
+        early[0] = words[0];
+        if (p.mask_words == 2) early[1] = words[1];
+      }
       float m = -INFINITY, l = 0.0f;
       const int mine = halves ? n : (n + 1 - s) / 2;
       const int tail_from = (int)(g.s.cached / kTile - g.first);   // the first tile with new tokens or none
@@ -582,7 +637,7 @@ __global__ void __launch_bounds__(TileCfg<kDC, kCodes>::kThreads, 1)
           const int64_t key = (int64_t)(g.first + tile) * kTile + kHalf * hf;
 #pragma unroll
           for (int c = 0; c < kC; ++c)
-            hide(tail ? seen_bits(p, g.s, g.s.first + t, t, key + 32 * c) : 0xFFFFFFFFu, bads, kC * hf + c, tp.box_rows,
+            hide(tail ? seen_bits(p, g.s, g.s.first + t, t, key + 32 * c, early) : 0xFFFFFFFFu, bads, kC * hf + c, tp.box_rows,
                  v[c]);
         }
         float top[8];
@@ -642,7 +697,7 @@ __global__ void __launch_bounds__(TileCfg<kDC, kCodes>::kThreads, 1)
           const int key_row = kHalf * hf + (r & (kHalf - 1));
           const uint32_t va = smem_u32(ring + slot_of(pos) * C::kSlot) + key_row * 128;
           const bool in = (int64_t)(g.first + tile) * kTile + key_row < g.s.keys;
-#pragma unroll 1
+#pragma unroll 4
           for (int i = r / kHalf; i < kD / 8; i += 128 / kHalf) {
             const uint32_t a = va + (i >> 3) * C::kChunk + (((i & 7) ^ (r & 7)) << 4);
             uint32_t x[4];
@@ -737,7 +792,7 @@ __global__ void __launch_bounds__(TileCfg<kDC, kCodes>::kThreads, 1)
             const int64_t key_end = min(g.s.keys, (int64_t)(g.first + n) * kTile);
             for (int64_t key = max((int64_t)g.first * kTile, g.s.cached / kTile * kTile); key < key_end; ++key) {
               int index, slot;
-              if (!(seen_bits(p, g.s, token, t, key) & 1u) ||
+              if (!(seen_bits(p, g.s, token, t, key, early) & 1u) ||
                   !cache_place(key, p.page_size, p.table_width, &index, &slot))
                 continue;
               const int page = p.table[g.b * p.table_stride + index];
@@ -783,8 +838,9 @@ __global__ void __launch_bounds__(TileCfg<kDC, kCodes>::kThreads, 1)
         }
       }
       tc_fence_before();
-      softmax_sync<C::kSoftThreads>();   // Q's place and the flags are free, the next segment is published
+      softmax_sync<C::kSoftThreads>();   // Q's place and the flags are free
       if (thread == 0) sh.odd_values = 0;
+      if (lane == 0) mbar_arrive(&seg_free[at]);
     }
   }
   __syncwarp();
