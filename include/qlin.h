@@ -607,8 +607,9 @@ typedef struct {
  *  positions, turns, magnitude, rot_dim, axes, axis_pairs, layout: as in qlin_rope.
  *         positions NULL: a token's number in its sequence (one axis).  turns NULL: nothing
  *         turns.
- * A 16-bit cache has the type of k and v.  Two tokens that share a slot (a page that two
- * sequences list for new tokens) leave either's values there.
+ * A 16-bit cache has the type of k and v.  Rows that share a slot (a page that two sequences
+ * list for new tokens, strides that overlap, one tensor as the cache's k and v) leave either's
+ * values there.
  * Errors: INVALID_ARG, MISALIGNED, UNSUPPORTED, CUDA.
  */
 typedef struct {
@@ -657,6 +658,7 @@ qlin_status qlin_cache_append(const qlin_cache_t *cache, const qlin_cache_append
  *          aligned, its first 8192 bytes zero before the first use; every call leaves them
  *          zero.  Calls whose work overlaps on the GPU must not share one.
  * A 16-bit cache has the type of q.  head_dim: a multiple of 16.  Cache rows 16-byte aligned.
+ * At most 2^24 tokens, and 2^30 of tokens times q_heads / heads.
  * Sums are joined in the order of the keys, split by all sequences' lengths: equal calls give
  * equal bits, other batches may change the last ones.
  * Errors: INVALID_ARG, MISALIGNED, UNSUPPORTED, WORKSPACE, CUDA.

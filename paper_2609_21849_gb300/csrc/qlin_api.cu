@@ -708,7 +708,8 @@ qlin_status qlin_cache_attention(const qlin_cache_t* c, const qlin_cache_attenti
   if (!apart(a->tokens, a->out_token_stride) || !apart(a->q_heads, a->out_head_stride)) return QLIN_ERR_INVALID_ARG;
   if (c->head_dim % 16 != 0 || (c->format != QLIN_CACHE_E4M3 && c->format != a->dtype)) return QLIN_ERR_UNSUPPORTED;
   // (rows, and the tiles of a call, are counted in 31 and 43 bits)
-  if (a->tokens > 1 << 24 || a->q_heads > 65536) return QLIN_ERR_UNSUPPORTED;
+  if (a->tokens > 1 << 24 || a->q_heads > 65536 || a->tokens * (a->q_heads / c->heads) > (int64_t)1 << 30)
+    return QLIN_ERR_UNSUPPORTED;
   const int64_t per16 = c->format == QLIN_CACHE_E4M3 ? 16 : 8;
   const int64_t strides = c->k_page_stride | c->k_slot_stride | c->k_head_stride | c->v_page_stride |
                           c->v_slot_stride | c->v_head_stride;

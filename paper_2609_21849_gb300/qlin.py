@@ -858,13 +858,12 @@ def _fp8_block_on(q, name, dev) -> bytes:
     """The packed descriptor of a block-scaled FP8 operand whose tensors hold what it says,
     on device `dev`."""
     codes, scales, rows, K, br = q.codes, q.scales, q.rows, q.K, q.block_rows
-    ss = scales.shape
-    if (codes.dtype is not torch.uint8 or codes.shape != (rows, K) or codes.get_device() != dev
+    cs, ss = codes.shape, scales.shape
+    if (codes.dtype is not torch.uint8 or len(cs) != 2 or cs[0] != rows or cs[1] != K or codes.get_device() != dev
             or not codes.is_contiguous()):
         raise ValueError(f"{name}.codes: expected a contiguous uint8 [{rows}, {K}] tensor on cuda:{dev}")
-    if (br != 1 and br != 128) or (scales.dtype is not torch.float32 or len(ss) != 2 or ss[0] != (K + 127) // 128
-                                   or ss[1] != -(-rows // br) or scales.get_device() != dev
-                                   or not scales.is_contiguous()):
+    if ((br != 1 and br != 128) or scales.dtype is not torch.float32 or len(ss) != 2 or ss[0] != (K + 127) // 128
+            or ss[1] != -(-rows // br) or scales.get_device() != dev or not scales.is_contiguous()):
         raise ValueError(f"{name}.scales: expected a contiguous float32 [ceil(K / 128), ceil(rows / block_rows)] "
                          f"tensor on cuda:{dev}, block_rows 1 or 128")
     return _pack_fp8_block(codes.data_ptr(), scales.data_ptr(), rows, K, br)
@@ -934,15 +933,15 @@ def _cache_on(c, dev):
             or v.get_device() != dev or (shape[3] > 1 and (ks[3] != 1 or vs[3] != 1))):
         raise ValueError("cache: expected k and v bf16, fp16 or float8_e4m3fn [pages, page_size, heads, head_dim] "
                          f"on cuda:{dev} with contiguous heads")
-    B, i32 = cached.numel(), torch.int32
-    if cached.dtype is not i32 or cached.dim() != 1 or cached.get_device() != dev or not cached.is_contiguous():
+    cs, qs, ts, tst, i32 = cached.shape, q_start.shape, table.shape, table.stride(), torch.int32
+    if len(cs) != 1 or cached.dtype is not i32 or cached.get_device() != dev or not cached.is_contiguous():
         raise ValueError(f"cache.cached: expected a contiguous int32 vector on cuda:{dev}")
-    if (q_start.dtype is not i32 or q_start.dim() != 1 or q_start.numel() != B + 1 or q_start.get_device() != dev
+    B = cs[0]
+    if (len(qs) != 1 or qs[0] != B + 1 or q_start.dtype is not i32 or q_start.get_device() != dev
             or not q_start.is_contiguous()):
         raise ValueError(f"cache.q_start: expected a contiguous int32 [{B + 1}] tensor on cuda:{dev}")
-    ts = table.shape
-    if (table.dtype is not i32 or len(ts) != 2 or ts[0] != B or table.get_device() != dev
-            or (table.stride(1) != 1 and ts[1] > 1)):
+    if (len(ts) != 2 or ts[0] != B or table.dtype is not i32 or table.get_device() != dev
+            or (tst[1] != 1 and ts[1] > 1)):
         raise ValueError(f"cache.page_table: expected an int32 [{B}, table_width] tensor on cuda:{dev} with "
                          "contiguous rows")
     if fmt == QLIN_CACHE_E4M3:
@@ -952,15 +951,16 @@ def _cache_on(c, dev):
     else:
         sk = sv = 0
     desc = _pack_cache(k.data_ptr(), v.data_ptr(), ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], table.data_ptr(),
-                       table.stride(0) if B > 1 else ts[1], cached.data_ptr(), q_start.data_ptr(), sk, sv, B,
+                       tst[0] if B > 1 else ts[1], cached.data_ptr(), q_start.data_ptr(), sk, sv, B,
                        shape[0], shape[1], ts[1], shape[2], shape[3], fmt)
     return desc, shape[2], shape[3]
 
 
 def _heads16(t, name, dtype, T, H, D, dev):
     """The strides of a 16-bit [tokens, heads, head_dim] tensor with contiguous heads."""
-    s = t.stride()
-    if t.dtype is not dtype or t.shape != (T, H, D) or t.get_device() != dev or (s[2] != 1 and D > 1):
+    s, shape = t.stride(), t.shape
+    if (t.dtype is not dtype or len(shape) != 3 or shape[0] != T or shape[1] != H or shape[2] != D
+            or t.get_device() != dev or (s[2] != 1 and D > 1)):
         raise ValueError(f"{name}: expected a {dtype} [{T}, {H}, {D}] tensor on cuda:{dev} with contiguous heads")
     return s[0], s[1]
 
@@ -1019,6 +1019,13 @@ def qlin_cache_attention_workspace_size() -> int:
     return _library().qlin_cache_attention_workspace_size()
 
 
+def _zero_counters(size, dtype, device):
+    """A workspace for one call: the library wants its first 8192 bytes zero."""
+    t = torch.empty(size, dtype=dtype, device=device)
+    t[:8192].zero_()
+    return t
+
+
 def alloc_cache_attention_workspace(device="cuda") -> torch.Tensor:
     return torch.zeros(qlin_cache_attention_workspace_size(), dtype=torch.uint8, device=device)
 
@@ -1053,7 +1060,7 @@ def qlin_cache_attention(cache: PagedCache, q: torch.Tensor, scale: float, mask:
             raise ValueError(f"lse: expected a contiguous float32 [{T}, {Hq}] tensor on cuda:{dev}")
         lp = lse.data_ptr()
     if workspace is None:
-        workspace = _empty(qlin_cache_attention_workspace_size(), torch.uint8, q.device, stream, torch.zeros)
+        workspace = _empty(qlin_cache_attention_workspace_size(), torch.uint8, q.device, stream, _zero_counters)
     elif workspace.get_device() != dev or not workspace.is_contiguous():
         raise ValueError(f"workspace: expected a contiguous tensor on cuda:{dev}")
     _check(_library().packed.qlin_cache_attention(desc, _pack_attention(
