@@ -10,9 +10,11 @@ scales).
   u   = gelu(c Wup^T + b)                 only its quantized form is written
   y   = u Wdown^T + b + x1
 
-Attention itself is the caller's: ``project`` gives q, k and v, ``finish`` takes what
-attention made of them.  ``forward`` runs both with the values in attention's place (the
-re-quantized value columns feed the out-projection, as in the linear stack).
+Attention is the caller's, or ``attend``, over a paged cache that the new keys and values join
+first: ``project`` gives q, k and v, ``finish`` takes what attention made of them.  ``step`` runs
+the three in a row, as a server does for the tokens of a step; ``forward`` runs project and
+finish with the values in attention's place (the re-quantized value columns feed the
+out-projection, as in the linear stack).
 
 Host-side orchestration only: every step runs in libqlin's kernels, on buffers made once.
 
@@ -51,6 +53,8 @@ class Block:
     x1: torch.Tensor | None = None
     y: torch.Tensor | None = None
     workspace: torch.Tensor | None = None
+    attended: torch.Tensor | None = None               # attend(), on its first call
+    attention_workspace: torch.Tensor | None = None
 
     def _linear(self, A, name, **kw):
         call = qlin.qlin_linear_fp8 if self.fmt == "fp8" else qlin.qlin_linear_nvfp4
@@ -89,6 +93,29 @@ class Block:
                      stream=stream)
         self._linear(self.q["u"], "down", residual=self.x1, y=self.y, stream=stream)
         return self.y
+
+    def attend(self, cache: qlin.PagedCache, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+               mask: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+        """Attention of project()'s q over the cache's keys and the new ones, which are appended
+        first; [M, hidden].  mask as in qlin_cache_attention.  The rows behind the cache's last
+        sequence stay as they were (zeros at first)."""
+        if self.attended is None:
+            if torch.cuda.is_current_stream_capturing():
+                raise RuntimeError("attend: its buffers are made in the first call, which must not be captured")
+            self.attention_workspace = qlin._empty(qlin.qlin_cache_attention_workspace_size(), torch.uint8, q.device,
+                                                   stream, torch.zeros)
+            self.attended = qlin._empty((self.M, self.hidden), torch.bfloat16, q.device, stream, torch.zeros)
+        H, D = self.heads, self.hidden // self.heads
+        qlin.qlin_cache_append(cache, k, v, stream=stream)   # (k has its positions)
+        qlin.qlin_cache_attention(cache, q, D ** -0.5, mask, self.attended.view(self.M, H, D), None,
+                                  self.attention_workspace, stream)
+        return self.attended
+
+    def step(self, x: torch.Tensor, positions: torch.Tensor, cache: qlin.PagedCache,
+             mask: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+        """The whole block for the new tokens x of the cache's sequences."""
+        q, k, v = self.project(x, positions, stream)
+        return self.finish(x, self.attend(cache, q, k, v, mask, stream), stream)
 
     def forward(self, x: torch.Tensor, positions: torch.Tensor, stream=None) -> torch.Tensor:
         self.project(x, positions, stream)

@@ -97,3 +97,56 @@ def test_refusals():
         block.build_block("int8", 4, H, HEADS, F)
     with pytest.raises(ValueError):
         block.build_block("fp8", 4, H, 7, F)
+
+
+def _paged(counts, cached, dtype, page=16):
+    """A cache for sequences of `cached` tokens and `counts` new ones, pages back to front."""
+    D = H // HEADS
+    per = [-(-(c + n) // page) for c, n in zip(cached, counts)]
+    table = torch.zeros(len(per), max(per), dtype=torch.int32, device="cuda")
+    at = sum(per)
+    for b, n in enumerate(per):
+        table[b, :n] = torch.arange(at - 1, at - 1 - n, -1)
+        at -= n
+    g = torch.Generator(device="cuda").manual_seed(5)
+    kv = [torch.randn(sum(per), page, HEADS, D, generator=g, device="cuda").to(dtype) for _ in "kv"]
+    ints = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    scale = torch.full((1,), 4 / 448, device="cuda") if dtype is torch.float8_e4m3fn else None
+    starts = [sum(counts[:i]) for i in range(len(counts) + 1)]
+    return qlin.PagedCache(*kv, table, ints(cached), ints(starts), scale, scale)
+
+
+@pytest.mark.parametrize("fmt,dtype", [("fp8", torch.bfloat16), ("nvfp4", torch.float8_e4m3fn)])
+@pytest.mark.parametrize("counts,cached,M", [([1], [40], 1), ([1, 1, 1], [0, 130, 15], 4), ([70, 0, 25], [33, 5, 0], 100)])
+def test_step_is_its_calls(fmt, dtype, counts, cached, M):
+    b, x, pos = _make(fmt, M)
+    cache, again = (_paged(counts, cached, dtype) for _ in "ab")
+    n = sum(counts)
+    y = b.step(x, pos, cache).clone()
+    attended = b.attended.clone()
+    assert qlin.qlin_sync_status() == 0 and torch.isfinite(y.float()).all()
+    q, k, v = b.project(x, pos)
+    qlin.qlin_cache_append(again, k, v)
+    o = qlin.qlin_cache_attention(again, q, (H // HEADS) ** -0.5)
+    assert torch.equal(cache.k.view(torch.uint8), again.k.view(torch.uint8))
+    assert torch.equal(cache.v.view(torch.uint8), again.v.view(torch.uint8))
+    assert torch.equal(attended[:n], o.view(M, H)[:n]) and not attended[n:].any()
+    assert torch.equal(b.finish(x, attended), y)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        b.step(x, pos, cache)
+    b.y.zero_()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(b.y, y)
+
+
+def test_attend_is_not_captured_first():
+    b, x, pos = _make("fp8", 1)
+    cache = _paged([1], [40], torch.bfloat16)
+    q, k, v = b.project(x, pos)
+    torch.cuda.synchronize()
+    with torch.cuda.graph(torch.cuda.CUDAGraph()):
+        with pytest.raises(RuntimeError, match="captured"):
+            b.attend(cache, q, k, v)
+        b.y.zero_()
