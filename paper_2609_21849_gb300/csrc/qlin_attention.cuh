@@ -613,8 +613,10 @@ __global__ void __launch_bounds__(kWarps * 32, (AttnCfg<kKind, kD, kM>::kCtas)) 
       __syncthreads();
       if (threadIdx.x == 0) {
         __threadfence();   // (the CTA's stores, which the barrier orders before)
-        const bool all = atomicAdd(count, 1u) == (unsigned)(parties - 1);
-        if (all) *count = 0u;   // as it was before the call
+        // (alone it takes no count: an item's last group, of this CTA alone, has the number that the
+        // item which begins here counts with)
+        const bool all = parties == 1 || atomicAdd(count, 1u) == (unsigned)(parties - 1);
+        if (all && parties != 1) *count = 0u;   // as it was before the call
         __threadfence();
         last_flag = all ? 1u : 0u;
       }

@@ -338,6 +338,28 @@ def test_bad_tables_and_counts_are_reported_and_touch_nothing():
         assert qlin.qlin_sync_status() == 0 and (ws[:8192] == 0).all()
 
 
+@pytest.mark.parametrize("fmt,dtype", FORMATS)
+@pytest.mark.parametrize("D,G,parts", [(64, 1, 64), (64, 16, 32), (256, 16, 16)])
+def test_items_that_meet_in_a_cta(D, G, parts, fmt, dtype):
+    """One sequence's last CTA begins the next one, and is alone in its group of `parts` CTAs
+    that join their sums.  (Two tiles each, for the tiles and grids that there may be.)"""
+    ws = qlin.alloc_cache_attention_workspace()
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    for tile in (32, 64, 128):
+        for ctas in (sms, 2 * sms):
+            n = 2 * parts + 1
+            cached = [n * tile - 1, (2 * ctas - n) * tile - 1]
+            c = _make(cached, [1, 1], 1, D, 64, fmt, tile)
+            _fill(c, cached, [1, 1], tile + 1)
+            q = torch.randn(2, G, D, generator=_gen(tile + 2), device="cuda").to(dtype)
+            first = qlin.qlin_cache_attention(c, q, 1 / math.sqrt(D), workspace=ws)
+            assert not ws[:8192].any()
+            _check(c, q, 1 / math.sqrt(D), None, fmt, first, None)
+            for _ in range(5):
+                assert torch.equal(qlin.qlin_cache_attention(c, q, 1 / math.sqrt(D), workspace=ws), first)
+            assert not ws[:8192].any()
+
+
 @pytest.mark.parametrize("T,G", [(1, 4), (40, 4)])
 def test_graph_over_growing_sequences_and_streams(T, G):
     heads, D, B = 2, 128, 3
