@@ -653,7 +653,7 @@ qlin_status qlin_cache_append(const qlin_cache_t *cache, const qlin_cache_append
  *          the two must not overlap.  Rows of tokens of no sequence are left as they were.
  *  lse:    fp32 [tokens, q_heads] or NULL.
  *  mask:   uint64 [tokens, mask_words], rows mask_stride words apart, or NULL.
- *  scale:  normal and > 0.
+ *  scale:  normal, > 0 and < 2^127.
  *  workspace: device memory of >= qlin_cache_attention_workspace_size() bytes, 16-byte
  *          aligned, its first 8192 bytes zero before the first use; every call leaves them
  *          zero.  Calls whose work overlaps on the GPU must not share one.

@@ -697,7 +697,8 @@ qlin_status qlin_cache_attention(const qlin_cache_t* c, const qlin_cache_attenti
   if (a == nullptr || a->q == nullptr || a->out == nullptr || a->tokens < 1 || a->q_heads < 1 ||
       (a->dtype != QLIN_BF16 && a->dtype != QLIN_FP16) || a->q_heads % c->heads != 0)
     return QLIN_ERR_INVALID_ARG;
-  if (!std::isnormal(a->scale) || !(a->scale > 0.0f)) return QLIN_ERR_INVALID_ARG;
+  // (below 2^127: times log2(e) it is finite)
+  if (!std::isnormal(a->scale) || !(a->scale > 0.0f) || a->scale >= 0x1p127f) return QLIN_ERR_INVALID_ARG;
   if (a->mask != nullptr && (a->mask_words < 1 || (a->tokens > 1 && a->mask_stride < 0))) return QLIN_ERR_INVALID_ARG;
   if (a->q == a->out &&
       (a->q_token_stride != a->out_token_stride || a->q_head_stride != a->out_head_stride))

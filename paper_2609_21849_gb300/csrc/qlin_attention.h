@@ -35,6 +35,7 @@ struct AttnParams {
   float2* part_ml;
   float* part;
   int least;                        // tiles that a CTA should have
+  int item_cost;                    // tiles that an item's begin and end take as long as
   unsigned* err;
 };
 

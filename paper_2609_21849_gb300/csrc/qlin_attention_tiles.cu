@@ -14,7 +14,7 @@
 //   Per tile of 256 rows and 128 keys of 128: 2048 cycles of MMAs, 2048 of exponentials (16 a
 // cycle and SM), 64 KB of keys and values, about 2850 cycles of an SM's share of HBM.
 // Roles: warps 0 and 2 load K and V, warp 1 issues MMAs, warp 3 walks the run for the softmax a
-// segment ahead of it, warps 4-11 and 12-19 are the streams' softmax.
+// segment ahead of it (and asks for the segment's Q), warps 4-11 and 12-19 are the streams' softmax.
 // Tiles with new tokens are masked, and V's slots behind the last key and values that are
 // not finite are zeroed in shared memory: 0 times them would reach rows that do not see them.
 // (Rows that do see such a value take it at the end.)
@@ -23,9 +23,9 @@
 // convert them to fp16 tiles (every code is an fp16); Q becomes fp16 after a power of two per row.
 // An item that several CTAs share is joined by a second kernel, many CTAs to an item (joined by one
 // of these, at one SM's rate of reading, the trees below took 40 us longer).
-//   Measured, 16 trees of 64 tokens behind 4096-8192 keys, 8 KV heads of 128, 3 query heads each:
-// 220 us (bf16; the keys and values from HBM need 126, the MMAs 106, the exponentials as much), 249
-// from E4M3, 297 at heads of 256.  A segment's end (the last tiles' products, O's way out, the next
+//   Measured, 16 trees of 64 tokens behind 8192-16384 keys, 8 KV heads of 128, 4 query heads each:
+// 220 us (bf16; the keys and values from HBM need 126, the MMAs 106, the exponentials 87), 249
+// from E4M3; 294 at heads of 256 behind half as many keys.  A segment's end (the last tiles' products, O's way out, the next
 // Q) leaves the tensor cores idle for 5000 to 7000 cycles; the tensor pipe is busy a third of the
 // time, the exponentials and the scores' way through registers bound the rest.
 #include <type_traits>
@@ -55,6 +55,10 @@ template <typename C>
 __device__ __forceinline__ void skip_segment(const AttnParams& p, Cursor& c, const Segment& s) {
   c.tile += s.n - 1;
   advance<C::kRows, C::kTile>(p, c);
+}
+// The unit behind a segment's, c being at its begin.
+__device__ __forceinline__ int64_t unit_after(const Cursor& c, const Segment& s, int64_t unit, int gap) {
+  return unit + s.n + (s.first + s.n == c.tiles ? gap : 0);
 }
 
 // A segment as the softmax threads need it, in shared memory: their registers hold scores.
@@ -354,7 +358,7 @@ __global__ void __launch_bounds__(TileCfg<kDC, kCodes>::kThreads, 1)
         }
         base += 2 * sg.n;
         tiles_done += sg.n;
-        unit += sg.n;
+        unit = unit_after(cur, sg, unit, run.gap);
         if (unit < run.end) skip_segment<C>(p, cur, sg);
       }
       // (The MMAs wait for every load.)  After a wait that gave up, copies in flight land before
@@ -450,7 +454,7 @@ __global__ void __launch_bounds__(TileCfg<kDC, kCodes>::kThreads, 1)
           if (ok && j < n1) ok = tile(1, j, j + 1 == n1);
         }
         base += 2 * sg.n;
-        unit += sg.n;
+        unit = unit_after(cur, sg, unit, run.gap);
         if (unit < run.end) skip_segment<C>(p, cur, sg);
       }
       // every MMA issued finishes before tensor memory is released
@@ -466,75 +470,89 @@ __global__ void __launch_bounds__(TileCfg<kDC, kCodes>::kThreads, 1)
       }
     } else {
       // ---- the run's segments for the softmax threads, one ahead of them ----
-      if (lane == 0) {
-        uint32_t base = 0;
-        unsigned tiles_done = 0, phase = 0;
-        int64_t unit = run.begin;
-        for (int at = 0;; at ^= 1) {
-          if (!mbar_wait(&seg_free[at], phase ^ 1u, ctl)) break;
-          phase ^= (uint32_t)at;
+      uint32_t base = 0;
+      unsigned tiles_done = 0, phase = 0;
+      int64_t unit = run.begin;
+      for (int at = 0;; at ^= 1) {
+        if (!mbar_wait_warp(&seg_free[at], phase ^ 1u, ctl)) break;
+        phase ^= (uint32_t)at;
+        const bool any = unit < run.end;
+        Segment sg{0, 0, false};
+        if (any) sg = segment_at<C>(p, cur, unit, run.end);
+        if (lane == 0) {
           SoftSegment& g = sh.seg[at];
-          g.n = 0;
-          if (unit < run.end) {
-            const Segment sg = segment_at<C>(p, cur, unit, run.end);
-            const int64_t item0 = unit - sg.first;
-            g.s = cur.s;
-            g.base = base;
-            g.b = cur.b;
-            g.h = cur.h;
-            g.rt = cur.rt;
-            g.first = sg.first;
-            g.n = sg.n;
-            g.tiles_done = tiles_done;
-            g.halves = sg.halves;
-            g.begun = item0 < run.begin;
-            g.whole = !g.begun && item0 + cur.tiles <= run.end;
-            base += 2 * sg.n;
-            tiles_done += sg.n;
-            unit += sg.n;
-            mbar_arrive(&seg_full[at]);
-            if (unit < run.end) skip_segment<C>(p, cur, sg);
-          } else {
-            mbar_arrive(&seg_full[at]);
-            break;
-          }
+          const int64_t item0 = unit - sg.first;
+          g.s = cur.s;
+          g.base = base;
+          g.b = cur.b;
+          g.h = cur.h;
+          g.rt = cur.rt;
+          g.first = sg.first;
+          g.n = sg.n;
+          g.tiles_done = tiles_done;
+          g.halves = sg.halves;
+          g.begun = item0 < run.begin;
+          g.whole = !g.begun && item0 + cur.tiles <= run.end;
+          mbar_arrive(&seg_full[at]);
         }
+        __syncwarp();
+        if (!any) break;
+        // its rows of Q towards L2
+        for (int i = lane; i < kRows; i += 32) {
+          const int row = cur.rt * kRows + i;
+          if (row >= cur.s.fresh * p.group) break;
+          const uint16_t* const q = p.q + (cur.s.first + row / p.group) * p.q_token +
+                                    (int64_t)(cur.h * p.group + row % p.group) * p.q_head;
+          for (int d = 0; d < p.head_dim; d += 64) asm volatile("prefetch.global.L2 [%0];" ::"l"(q + d));
+        }
+        base += 2 * sg.n;
+        tiles_done += sg.n;
+        unit = unit_after(cur, sg, unit, run.gap);
+        if (unit < run.end) skip_segment<C>(p, cur, sg);
       }
     }
   } else if (kCodes && warp >= kSoftWarp0 + C::kSoftThreads / 32) {
     // ---- codes to fp16 (exactly), from the rows as they came to the MMAs' swizzled tiles ----
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kRoleRegs));
     const int thread = threadIdx.x - kSoftWarp0 * 32 - C::kSoftThreads;
-    const uint32_t loads = (uint32_t)(2 * (run.end - run.begin));
-    for (uint32_t pos = 0; pos < loads; ++pos) {
-      const int rs = (int)(pos % kRing), slot = slot_of(pos);
-      if (!mbar_wait_warp(&raw_full[rs], (pos / kRing) & 1u, ctl) ||
-          !mbar_wait_warp(&empty[slot], phase_of(pos) ^ 1u, ctl))
-        break;
-      const uint32_t src = smem_u32(raw + rs * C::kRawSlot), dst = smem_u32(ring + slot * C::kSlot);
-#pragma unroll 4
-      for (int i = thread; i < kTile * 4 * kDC; i += kConvertWarps * 32) {   // 16 codes
-        const int key = i / (4 * kDC), at = i % (4 * kDC);
-        uint32_t w[4], h[8];
-        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                     : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
-                     : "r"(src + key * C::kRawRow + at * 16));
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          h[2 * k] = e4m3x2_half2(w[k]);
-          h[2 * k + 1] = e4m3x2_half2(w[k] >> 16);
+    uint32_t pos = 0;
+    bool ok = true;
+    for (int64_t unit = run.begin; unit < run.end && ok;) {
+      const Segment sg = segment_at<C>(p, cur, unit, run.end);
+      for (const uint32_t end = pos + 2 * sg.n; pos < end; ++pos) {
+        const int rs = (int)(pos % kRing), slot = slot_of(pos);
+        if (!mbar_wait_warp(&raw_full[rs], (pos / kRing) & 1u, ctl) ||
+            !mbar_wait_warp(&empty[slot], phase_of(pos) ^ 1u, ctl)) {
+          ok = false;
+          break;
         }
-        const uint32_t to = dst + (at >> 2) * C::kChunk + key * 128;
-        const int piece = 2 * (at & 3);
-        st_shared_v4(to + ((piece ^ (key & 7)) << 4), h[0], h[1], h[2], h[3]);
-        st_shared_v4(to + (((piece + 1) ^ (key & 7)) << 4), h[4], h[5], h[6], h[7]);
+        const uint32_t src = smem_u32(raw + rs * C::kRawSlot), dst = smem_u32(ring + slot * C::kSlot);
+#pragma unroll 4
+        for (int i = thread; i < kTile * 4 * kDC; i += kConvertWarps * 32) {   // 16 codes
+          const int key = i / (4 * kDC), at = i % (4 * kDC);
+          uint32_t w[4], h[8];
+          asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                       : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
+                       : "r"(src + key * C::kRawRow + at * 16));
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            h[2 * k] = e4m3x2_half2(w[k]);
+            h[2 * k + 1] = e4m3x2_half2(w[k] >> 16);
+          }
+          const uint32_t to = dst + (at >> 2) * C::kChunk + key * 128;
+          const int piece = 2 * (at & 3);
+          st_shared_v4(to + ((piece ^ (key & 7)) << 4), h[0], h[1], h[2], h[3]);
+          st_shared_v4(to + (((piece + 1) ^ (key & 7)) << 4), h[4], h[5], h[6], h[7]);
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(&full[slot]);
+          mbar_arrive(&raw_empty[rs]);
+        }
       }
-      fence_proxy_async_smem();
-      __syncwarp();
-      if (lane == 0) {
-        mbar_arrive(&full[slot]);
-        mbar_arrive(&raw_empty[rs]);
-      }
+      unit = unit_after(cur, sg, unit, run.gap);
+      if (unit < run.end) skip_segment<C>(p, cur, sg);
     }
   } else {
     // ---- softmax: stream s, row r ----
@@ -890,6 +908,9 @@ cudaError_t launch_cfg(TileParams tp, const CUtensorMap& tk, const CUtensorMap& 
   p.part_ml = reinterpret_cast<float2*>(reinterpret_cast<uint8_t*>(p.counts) + kCountBytes);
   p.part = reinterpret_cast<float*>(p.part_ml + (int64_t)2 * C::kRows * ctas);
   p.least = 2;
+  // (in us without it, with 6, 8, 11 and 15: the trees above 225, 213, 214, 213, 219; 64 of 500-1000 keys
+  // 152, 135, 131, 132, 135; three of 15000-30000 keys 109, 99, 100, 95, 96)
+  p.item_cost = 8;
   const cudaError_t st = launch_pdl(kern, dim3((unsigned)ctas), C::kThreads, C::kSmem, s, tk, tv, tp);
   if (st != cudaSuccess) return st;
   return launch_pdl(attn_join_kernel<kDC, C::kRows, C::kTile>, dim3((unsigned)ctas, C::kRows / kJoinRows), kJoinThreads, 0, s, p, ctas);

@@ -3,6 +3,12 @@
 //   S = max |x over the block| / 448 (1 for a block of zeros), code = E4M3(x / S as x * (1 / S)).
 // Bound by HBM: 2 bytes in and 1 out per element (and a scale per block), one read of x that
 // stays in registers between a block's maximum and its codes.
+//   rows:  eight lanes hold a block of 128, 16 elements each, so that its maximum is three shuffles;
+//          a warp's four blocks are four rows of one block of K where there are rows enough (their
+//          scales adjacent), else four blocks of a row.
+//   tiles: a CTA of 512 threads holds 128 x 128 values, 32 each, and joins the maxima in shared memory.
+// Measured: 4608 x 12288 27.4 us, 94% of the copy rate; 12288 x 3072 in tiles 20.0, 84% (the codes of
+// a tile wait for its last value); one row of 3072 1.4, a launch.
 #include "qlin_internal.h"
 
 namespace qlin {

@@ -138,7 +138,7 @@ def test_append_cache_refusals(lib):
 @pytest.mark.parametrize("kw,status", [
     (dict(q=None), INVALID), (dict(out=None), INVALID), (dict(tokens=0), INVALID), (dict(q_heads=0), INVALID),
     (dict(q_heads=6), INVALID), (dict(dtype=0), INVALID), (dict(scale=0.0), INVALID), (dict(scale=-1.0), INVALID),
-    (dict(scale=math.inf), INVALID), (dict(scale=math.nan), INVALID), (dict(scale=1e-40), INVALID),
+    (dict(scale=math.inf), INVALID), (dict(scale=math.nan), INVALID), (dict(scale=1e-40), INVALID), (dict(scale=2.0**127), INVALID),
     (dict(mask=A16, mask_words=0), INVALID), (dict(mask=A16, mask_words=1, mask_stride=-1), INVALID),
     (dict(out=A16, out_token_stride=2048), INVALID), (dict(out_head_stride=64), INVALID),
     (dict(out_token_stride=0), INVALID), (dict(dtype=FP16), UNSUPPORTED), (dict(tokens=2**24 + 1), UNSUPPORTED),
