@@ -188,6 +188,13 @@ def test_long_caches_and_uneven_batches(fmt, dtype):
 
 
 @pytest.mark.parametrize("fmt,dtype", FORMATS)
+def test_many_sequences(fmt, dtype):
+    # more than a CTA has threads, some without new tokens; a CTA's run over many items
+    _attend([37 * i % 1500 for i in range(300)], [int(i % 7 > 0) for i in range(300)], 1, 2, 64, 16, fmt, dtype, tree=False)
+    _attend([53 * i % 900 for i in range(700)], [i % 4 * 11 for i in range(700)], 1, 1, 64, 32, fmt, dtype)
+
+
+@pytest.mark.parametrize("fmt,dtype", FORMATS)
 def test_many_rows(fmt, dtype):
     _attend([1500, 700], [64, 33], 2, 4, 128, 128, fmt, dtype)
     _attend([900], [128], 1, 8, 64, 8, fmt, dtype)
