@@ -11,8 +11,9 @@
 //   O += P V      A from tensor memory, V as it lies (keys x elements: an MN-major B)
 // The running maximum moves only when it rises by more than 2^8, so O is rarely rescaled; P
 // stays below 2^8 and the sums in fp32 (both fine in 16 bits: a P's rounding is relative).
-//   Per tile of 256 rows and 128 keys of 128: 2048 cycles of MMAs, 2048 of exponentials (16 a
-// cycle and SM), 64 KB of keys and values, about 2850 cycles of an SM's share of HBM.
+//   Per tile of 256 rows and 128 keys of 128: 2048 cycles of MMAs (2560 where 128 bytes of shared
+// memory a cycle bring a half's scores Q's rows and 64 keys), 1024 of exponentials (four cycles a warp
+// measured), 64 KB of keys and values, about 2850 cycles of an SM's share of HBM.
 // Roles: warps 0 and 2 load K and V, warp 1 issues MMAs, warp 3 walks the run for the softmax a
 // segment ahead of it (and asks for the segment's Q), warps 4-11 and 12-19 are the streams' softmax.
 // Tiles with new tokens are masked, and V's slots behind the last key and values that are
@@ -24,10 +25,11 @@
 // An item that several CTAs share is joined by a second kernel, many CTAs to an item (joined by one
 // of these, at one SM's rate of reading, the trees below took 40 us longer).
 //   Measured, 16 trees of 64 tokens behind 8192-16384 keys, 8 KV heads of 128, 4 query heads each:
-// 220 us (bf16; the keys and values from HBM need 126, the MMAs 106, the exponentials 87), 249
-// from E4M3; 294 at heads of 256 behind half as many keys.  A segment's end (the last tiles' products, O's way out, the next
-// Q) leaves the tensor cores idle for 5000 to 7000 cycles; the tensor pipe is busy a third of the
-// time, the exponentials and the scores' way through registers bound the rest.
+// 214 us (bf16; the keys and values from HBM need 126, the MMAs 106), 240 from E4M3; 291 at heads of
+// 256 behind half as many keys.  About 4800 cycles a tile: the tensor pipe is busy a third of the time
+// and no issue slot is short; what lasts is each stream's chain of scores, maximum, exponentials, P
+// and products, of which two run at a time.  A segment's begin and end (Q's way in, the first scores,
+// the last products, O's way out) leave the tensor cores idle for 5000 to 7000 cycles.
 #include <type_traits>
 
 #include "qlin_attention_work.cuh"

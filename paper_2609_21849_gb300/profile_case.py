@@ -16,6 +16,10 @@ Cases (seeded synthetic inputs, shapes of the paper's workloads):
   linear_up        NVFP4 linear 4608 x 12288 x 3072, bias, tanh GELU, re-quantized
   linear_one       bf16 linear 1 x 12288 x 3072, bias and SiLU
   linear_split     bf16 linear 552 x 832 x 12288 (tiles that share K), bias and SiLU
+  block_linear     block-scaled FP8 linear 4608 x 12288 x 3072, bias and tanh GELU
+  decode_attention one token of each of 64 sequences of 536-2048 E4M3 keys, 64 heads over 8 of 128
+  tree_attention   trees of 64 tokens behind 4 caches of 4096 keys, 32 heads over 8 of 128, bf16
+  cache_append     4608 tokens of 24 heads of 128 into a bf16 cache, q and k rotated
 Prints the mean device time per launch (CUDA events, not for use under a
 profiler).
 """
@@ -31,6 +35,17 @@ from . import build, qlin, synthetic
 
 def _dev(bits):
     return torch.from_numpy(np.ascontiguousarray(bits).view(np.int16)).cuda().view(torch.bfloat16)
+
+
+def _cache(cached, new, heads, page, dtype):
+    per = [-(-(c + new) // page) for c in cached]
+    table = torch.zeros(len(per), max(per), dtype=torch.int32, device="cuda")
+    for b, n in enumerate(per):
+        table[b, :n] = torch.arange(sum(per[:b]), sum(per[:b + 1]))
+    ints = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    kv = [torch.randn(sum(per), page, heads, 128, device="cuda").to(dtype) for _ in "kv"]
+    scale = torch.ones(1, device="cuda") if dtype is torch.float8_e4m3fn else None
+    return qlin.PagedCache(*kv, table, ints(cached), ints([new * b for b in range(len(cached) + 1)]), scale, scale)
 
 
 def make_case(name: str):
@@ -92,6 +107,27 @@ def make_case(name: str):
         w, b = torch.randn(N, K, device="cuda").bfloat16(), torch.zeros(N, dtype=torch.bfloat16, device="cuda")
         y = torch.empty(M, N, dtype=torch.bfloat16, device="cuda")
         return lambda: qlin.qlin_linear_bf16(x, w, b, qlin.QLIN_ACT_SILU, None, y)
+    if name == "block_linear":
+        A = qlin.qlin_quantize_fp8_block(torch.randn(4608, 3072, device="cuda").bfloat16())
+        W = qlin.qlin_quantize_fp8_block(torch.randn(12288, 3072, device="cuda").bfloat16(), 128)
+        b = torch.zeros(12288, dtype=torch.bfloat16, device="cuda")
+        y = torch.empty(4608, 12288, dtype=torch.bfloat16, device="cuda")
+        return lambda: qlin.qlin_linear_fp8_block(A, W, b, qlin.QLIN_ACT_GELU_TANH, None, y)
+    if name == "cache_append":
+        heads = torch.randn(4608, 72, 128, device="cuda").bfloat16()
+        cache = _cache([0], 4608, 24, 64, torch.bfloat16)
+        plan, q_out = qlin.rope_plan(128), torch.empty(4608, 24, 128, dtype=torch.bfloat16, device="cuda")
+        return lambda: qlin.qlin_cache_append(cache, heads[:, 24:48], heads[:, 48:], plan, None, heads[:, :24], q_out)
+    if name in ("decode_attention", "tree_attention"):
+        if name == "decode_attention":
+            cache, q = _cache([2048 - 24 * b for b in range(64)], 1, 8, 32, torch.float8_e4m3fn), (64, 64, 128)
+            mask = None
+        else:
+            cache, q = _cache([4096] * 4, 64, 8, 128, torch.bfloat16), (256, 32, 128)
+            mask = torch.randint(-2**62, 2**62, (256, 1), device="cuda")
+        q = torch.randn(*q, device="cuda").bfloat16()
+        out, ws = torch.empty_like(q), qlin.alloc_cache_attention_workspace()
+        return lambda: qlin.qlin_cache_attention(cache, q, 128**-0.5, mask, out, None, ws)
     raise SystemExit(f"unknown case {name}")
 
 
