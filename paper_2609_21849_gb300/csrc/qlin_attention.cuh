@@ -32,21 +32,6 @@ namespace {
 
 constexpr int kWarps = 4;
 
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool in) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(in ? 16 : 0) : "memory");
-}
-__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void cp_async_wait() {
-  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
-}
-
-__device__ __forceinline__ uint4 lds128(uint32_t a) {
-  uint4 v;
-  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
-  return v;
-}
-
 __device__ __forceinline__ void ldmatrix_trans(uint32_t a, uint32_t (&r)[4]) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
@@ -214,7 +199,7 @@ __global__ void __launch_bounds__(kWarps * 32, (AttnCfg<kKind, kD, kM>::kCtas)) 
       f.page = p.table[ahead.b * p.table_stride + index];
       f.in = true;
     }
-    to_fetch += 1 + (ahead.tile + 1 == ahead.tiles ? run.gap : 0);
+    to_fetch += 1 + (ahead.tile + 1 == ahead.tiles ? p.item_cost : 0);
     if (to_fetch < run.end) {
       advance<kRows, C::kTile>(p, ahead);
       if (ahead.tile == 0 && warp == 0) {   // a new item: its rows of Q towards L2
@@ -607,7 +592,7 @@ __global__ void __launch_bounds__(kWarps * 32, (AttnCfg<kKind, kD, kM>::kCtas)) 
     const bool done = cur.tile + 1 == cur.tiles;
     if (done || unit + 1 == run.end) end_item(stage, unit);
     fresh_item = done;
-    after = unit + 1 + (done ? run.gap : 0);
+    after = unit + 1 + (done ? p.item_cost : 0);
     if (after < run.end) advance<kRows, C::kTile>(p, cur);
     if (++stage == C::kStages) stage = 0;
     __syncwarp();
@@ -677,7 +662,7 @@ cudaError_t launch_attn(AttnParams p, cudaStream_t s, Device dev) {
   p.part = reinterpret_cast<float*>(p.part_ml + (int64_t)2 * C::kRows * ctas);
   p.least = std::max(1, 128 / C::kTile);
   // (in us without it, with 1, 2, 3 and 4: 64 sequences of 2048-8192 E4M3 keys, 8 heads of 128, 144, 141,
-  // 139, 139, 140; of 512-2048 59, 55, 53, 53, 55)
+  // 139, 139, 140; of 512-2048 59, 55, 53, 53, 55; 8 of 512-2048, without and with 2, 20.0, 15.5)
   p.item_cost = 2;
   return launch_pdl(attn_kernel<kKind, kD, kM>, dim3((unsigned)ctas), kWarps * 32, C::kSmem, s, p);
 }

@@ -59,8 +59,8 @@ __device__ __forceinline__ void skip_segment(const AttnParams& p, Cursor& c, con
   advance<C::kRows, C::kTile>(p, c);
 }
 // The unit behind a segment's, c being at its begin.
-__device__ __forceinline__ int64_t unit_after(const Cursor& c, const Segment& s, int64_t unit, int gap) {
-  return unit + s.n + (s.first + s.n == c.tiles ? gap : 0);
+__device__ __forceinline__ int64_t unit_after(const Cursor& c, const Segment& s, int64_t unit, int item_cost) {
+  return unit + s.n + (s.first + s.n == c.tiles ? item_cost : 0);
 }
 
 // A segment as the softmax threads need it, in shared memory: their registers hold scores.
@@ -360,7 +360,7 @@ __global__ void __launch_bounds__(TileCfg<kDC, kCodes>::kThreads, 1)
         }
         base += 2 * sg.n;
         tiles_done += sg.n;
-        unit = unit_after(cur, sg, unit, run.gap);
+        unit = unit_after(cur, sg, unit, p.item_cost);
         if (unit < run.end) skip_segment<C>(p, cur, sg);
       }
       // (The MMAs wait for every load.)  After a wait that gave up, copies in flight land before
@@ -456,7 +456,7 @@ __global__ void __launch_bounds__(TileCfg<kDC, kCodes>::kThreads, 1)
           if (ok && j < n1) ok = tile(1, j, j + 1 == n1);
         }
         base += 2 * sg.n;
-        unit = unit_after(cur, sg, unit, run.gap);
+        unit = unit_after(cur, sg, unit, p.item_cost);
         if (unit < run.end) skip_segment<C>(p, cur, sg);
       }
       // every MMA issued finishes before tensor memory is released
@@ -509,7 +509,7 @@ __global__ void __launch_bounds__(TileCfg<kDC, kCodes>::kThreads, 1)
         }
         base += 2 * sg.n;
         tiles_done += sg.n;
-        unit = unit_after(cur, sg, unit, run.gap);
+        unit = unit_after(cur, sg, unit, p.item_cost);
         if (unit < run.end) skip_segment<C>(p, cur, sg);
       }
     }
@@ -553,7 +553,7 @@ __global__ void __launch_bounds__(TileCfg<kDC, kCodes>::kThreads, 1)
           mbar_arrive(&raw_empty[rs]);
         }
       }
-      unit = unit_after(cur, sg, unit, run.gap);
+      unit = unit_after(cur, sg, unit, p.item_cost);
       if (unit < run.end) skip_segment<C>(p, cur, sg);
     }
   } else {
@@ -581,61 +581,70 @@ __global__ void __launch_bounds__(TileCfg<kDC, kCodes>::kThreads, 1)
       auto row_in = [&] { return g.rt * kRows + my_row < g.s.fresh * p.group; };
       auto row_of = [&] { return row_in() ? g.rt * kRows + my_row : 0; };
       float mult = p.scale_log2;   // from scores to powers of two
-      // Q into shared memory: rows of 128 swizzled bytes, 64 elements a chunk
-      const bool stores_q = halves || s == 0;
-      if (stores_q || kCodes) {
-        const int row = row_of();
-        const uint16_t* const q = p.q + (g.s.first + row / p.group) * p.q_token +
-                                  (int64_t)(g.h * p.group + row % p.group) * p.q_head;
-        const uint32_t dst = smem_u32(q_smem) + (halves ? s * C::kQSlot : 0) + r * 128;
-        const bool in = row_in();
-        auto piece = [&](int i) {   // 16 bytes
-          return in && 8 * i < p.head_dim ? *reinterpret_cast<const uint4*>(q + 8 * i) : make_uint4(0u, 0u, 0u, 0u);
-        };
-        if constexpr (kCodes) {
-          // fp16 after a power of two that brings the row's largest |q| into [1, 2) (a zero, infinite or
-          // NaN row as it is)
-          uint32_t top = 0u;
-#pragma unroll 8
-          for (int i = 0; i < kD / 8; ++i) {
-            const uint4 w = piece(i);
-            top = __vmaxu2(__vmaxu2(__vmaxu2(__vmaxu2(top, w.x & 0x7FFF7FFFu), w.y & 0x7FFF7FFFu), w.z & 0x7FFF7FFFu),
-                           w.w & 0x7FFF7FFFu);
-          }
-          top = max(top & 0xFFFFu, top >> 16);
-          const float big = p.fp16 ? __half2float(__ushort_as_half((unsigned short)top)) : __uint_as_float(top << 16);
-          int e = (int)(__float_as_uint(big) >> 23);   // biased
-          e = e == 0 || e == 255 ? 127 : min(e, 252);
-          const float down = __uint_as_float((uint32_t)(254 - e) << 23);
-          mult = fminf(fmaxf(p.scale_log2 * __uint_as_float((uint32_t)e << 23) * *p.k_scale, FLT_MIN), FLT_MAX);
-          auto scaled = [&](uint32_t w) {
-            const float2 v = p.fp16 ? __half22float2(*reinterpret_cast<const __half2*>(&w)) : make_float2(bf16_lo(w), bf16_hi(w));
-            return pack_f16x2(v.x * down, v.y * down);
-          };
-#pragma unroll 8
-          for (int i = 0; i < (stores_q ? kD / 8 : 0); ++i) {
-            const uint4 w = piece(i);
-            st_shared_v4(dst + (i >> 3) * C::kQChunk + (((i & 7) ^ (r & 7)) << 4), scaled(w.x), scaled(w.y), scaled(w.z),
-                         scaled(w.w));
-          }
-        } else {
-#pragma unroll 16
-          for (int i = 0; i < kD / 8; ++i) {
-            const uint4 w = piece(i);
-            st_shared_v4(dst + (i >> 3) * C::kQChunk + (((i & 7) ^ (r & 7)) << 4), w.x, w.y, w.z, w.w);
-          }
-        }
-        fence_proxy_async_smem();
-      }
-      __syncwarp();
-      if (lane == 0) mbar_arrive(q_ready);
-
       uint64_t early[2] = {0ull, 0ull};   // the row's mask, on its way before a tile needs it
       if (p.mask != nullptr && p.mask_words <= 2) {
         const uint64_t* const words = p.mask + (g.s.first + row_of() / p.group) * p.mask_token;
         early[0] = words[0];
         if (p.mask_words == 2) early[1] = words[1];
       }
+      // Q into shared memory: rows of 128 swizzled bytes, 64 elements a chunk.  Each warp copies its rows,
+      // asynchronously: through registers, with a store behind each load, this took 6000 to 14000 cycles.
+      const bool stores_q = halves || s == 0;
+      const int64_t q_row = row_in() ? (g.s.first + row_of() / p.group) * p.q_token +
+                                           (int64_t)(g.h * p.group + row_of() % p.group) * p.q_head
+                                     : -1;
+      const uint32_t q_dst = smem_u32(q_smem) + (halves ? s * C::kQSlot : 0);
+      if (stores_q) {
+        constexpr int kPieces = kD / 8;   // of 16 bytes
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+          const int at = i * 32 + lane, row = at / kPieces, piece = at % kPieces, to = (r & ~31) + row;
+          const int64_t from = __shfl_sync(0xFFFFFFFFu, q_row, row);
+          const bool in = from >= 0 && 8 * piece < p.head_dim;
+          cp_async16(q_dst + (piece >> 3) * C::kQChunk + to * 128 + (((piece & 7) ^ (to & 7)) << 4),
+                     p.q + (in ? from + 8 * piece : 0), in);
+        }
+        cp_async_commit();
+        cp_async_wait<0>();
+        __syncwarp();
+      }
+      if constexpr (kCodes) {
+        // fp16 after a power of two that brings the row's largest |q| into [1, 2) (a zero, infinite or
+        // NaN row as it is); a stream that did not store reads its rows again
+        const uint32_t dst = q_dst + r * 128;
+        auto place = [&](int i) { return dst + (i >> 3) * C::kQChunk + (((i & 7) ^ (r & 7)) << 4); };
+        auto piece = [&](int i) {
+          if (stores_q) return lds128(place(i));
+          return q_row >= 0 && 8 * i < p.head_dim ? *reinterpret_cast<const uint4*>(p.q + q_row + 8 * i)
+                                                  : make_uint4(0u, 0u, 0u, 0u);
+        };
+        uint32_t top = 0u;
+#pragma unroll 8
+        for (int i = 0; i < kD / 8; ++i) {
+          const uint4 w = piece(i);
+          top = __vmaxu2(__vmaxu2(__vmaxu2(__vmaxu2(top, w.x & 0x7FFF7FFFu), w.y & 0x7FFF7FFFu), w.z & 0x7FFF7FFFu),
+                         w.w & 0x7FFF7FFFu);
+        }
+        top = max(top & 0xFFFFu, top >> 16);
+        const float big = p.fp16 ? __half2float(__ushort_as_half((unsigned short)top)) : __uint_as_float(top << 16);
+        int e = (int)(__float_as_uint(big) >> 23);   // biased
+        e = e == 0 || e == 255 ? 127 : min(e, 252);
+        const float down = __uint_as_float((uint32_t)(254 - e) << 23);
+        mult = fminf(fmaxf(p.scale_log2 * __uint_as_float((uint32_t)e << 23) * *p.k_scale, FLT_MIN), FLT_MAX);
+        auto scaled = [&](uint32_t w) {
+          const float2 v = p.fp16 ? __half22float2(*reinterpret_cast<const __half2*>(&w)) : make_float2(bf16_lo(w), bf16_hi(w));
+          return pack_f16x2(v.x * down, v.y * down);
+        };
+#pragma unroll 8
+        for (int i = 0; i < (stores_q ? kD / 8 : 0); ++i) {
+          const uint4 w = lds128(place(i));
+          st_shared_v4(place(i), scaled(w.x), scaled(w.y), scaled(w.z), scaled(w.w));
+        }
+      }
+      if (stores_q) fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(q_ready);
+
       float m = -INFINITY, l = 0.0f;
       const int mine = halves ? n : (n + 1 - s) / 2;
       const int tail_from = (int)(g.s.cached / kTile - g.first);   // the first tile with new tokens or none
@@ -717,25 +726,31 @@ __global__ void __launch_bounds__(TileCfg<kDC, kCodes>::kThreads, 1)
           const int key_row = kHalf * hf + (r & (kHalf - 1));
           const uint32_t va = smem_u32(ring + slot_of(pos) * C::kSlot) + key_row * 128;
           const bool in = (int64_t)(g.first + tile) * kTile + key_row < g.s.keys;
-#pragma unroll 4
-          for (int i = r / kHalf; i < kD / 8; i += 128 / kHalf) {
-            const uint32_t a = va + (i >> 3) * C::kChunk + (((i & 7) ^ (r & 7)) << 4);
-            uint32_t x[4];
-            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                         : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3])
-                         : "r"(a));
-            uint32_t odd = 0u;
+          constexpr int kStep = 128 / kHalf, kOwn = kD / 8 / kStep, kBatch = kOwn % 4 == 0 ? 4 : 2;
+#pragma unroll 1
+          for (int i0 = r / kHalf; i0 < kD / 8; i0 += kBatch * kStep) {
+            auto place = [&](int k) {
+              const int i = i0 + k * kStep;
+              return va + (i >> 3) * C::kChunk + (((i & 7) ^ (r & 7)) << 4);
+            };
+            uint4 x[kBatch];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              const uint32_t hit = __vcmpgeu2(x[q] & 0x7FFF7FFFu, kF16 ? 0x7C007C00u : 0x7F807F80u);
-              odd |= hit;
-              x[q] = in ? x[q] & ~hit : 0u;
+            for (int k = 0; k < kBatch; ++k) x[k] = lds128(place(k));
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) {
+              uint32_t odd = 0u;
+              auto finite = [&](uint32_t w) {
+                const uint32_t hit = __vcmpgeu2(w & 0x7FFF7FFFu, kF16 ? 0x7C007C00u : 0x7F807F80u);
+                odd |= hit;
+                return in ? w & ~hit : 0u;
+              };
+              const uint4 w = make_uint4(finite(x[k].x), finite(x[k].y), finite(x[k].z), finite(x[k].w));
+              if (in && odd != 0u) {
+                *(volatile int*)&sh.odd_values = 1;   // before the zeros: who finds them finds this
+                __threadfence_block();
+              }
+              if (!in || odd != 0u) st_shared_v4(place(k), w.x, w.y, w.z, w.w);
             }
-            if (in && odd != 0u) {
-              *(volatile int*)&sh.odd_values = 1;   // before the zeros: who finds them finds this
-              __threadfence_block();
-            }
-            if (!in || odd != 0u) st_shared_v4(a, x[0], x[1], x[2], x[3]);
           }
           fence_proxy_async_smem();
         }
@@ -911,7 +926,8 @@ cudaError_t launch_cfg(TileParams tp, const CUtensorMap& tk, const CUtensorMap& 
   p.part = reinterpret_cast<float*>(p.part_ml + (int64_t)2 * C::kRows * ctas);
   p.least = 2;
   // (in us without it, with 6, 8, 11 and 15: the trees above 225, 213, 214, 213, 219; 64 of 500-1000 keys
-  // 152, 135, 131, 132, 135; three of 15000-30000 keys 109, 99, 100, 95, 96)
+  // 152, 135, 131, 132, 135; three of 15000-30000 keys 109, 99, 100, 95, 96; without and with 8: four of
+  // 2048-4096 keys 51.6, 45.0, 16 of 250-500 52.7, 42.6)
   p.item_cost = 8;
   const cudaError_t st = launch_pdl(kern, dim3((unsigned)ctas), C::kThreads, C::kSmem, s, tk, tv, tp);
   if (st != cudaSuccess) return st;

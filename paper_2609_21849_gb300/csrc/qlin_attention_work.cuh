@@ -8,6 +8,21 @@ namespace qlin {
 
 namespace {
 
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool in) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(in ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_async_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
+__device__ __forceinline__ uint4 lds128(uint32_t a) {
+  uint4 v;
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
+  return v;
+}
+
 // A place in the work: tile `tile` of the item (b, h, rt).
 struct Cursor {
   CacheSeq s;
@@ -46,132 +61,115 @@ __device__ __forceinline__ void advance(const AttnParams& p, Cursor& c) {
   }
 }
 
-// The tiles of a sequence, and its items.
-struct Work {
-  int64_t tiles, items;
-};
+// A sequence's units: those of an item are its tiles and behind them item_cost more, which nobody
+// works on, for its begin and end.
 template <int kRows, int kTile>
-__device__ __forceinline__ Work seq_work(const AttnParams& p, const CacheSeq& s) {
+__device__ __forceinline__ int64_t seq_units(const AttnParams& p, const CacheSeq& s) {
   const int64_t tiles = (s.keys + kTile - 1) / kTile;
-  const int64_t items = tiles > 0 ? ((int64_t)s.fresh * p.group + kRows - 1) / kRows * p.heads : 0;
-  return {items * tiles, items};
+  return tiles == 0 ? 0 : ((int64_t)s.fresh * p.group + kRows - 1) / kRows * p.heads * (tiles + p.item_cost);
 }
 
-// The CTA's run of units and the cursor at its begin; the same in all threads.  An item's units are
-// its tiles and behind them `gap` more that nobody works on: what its begin and end cost.
+// The CTA's run of units and the cursor at its begin; the same in all threads.
 struct Run {
   int64_t begin, end;
   Split split;
-  int gap;
 };
 struct RunScratch {   // in shared memory
-  Work warp_sum[32], warp_all[32];
+  int64_t warp_sum[32], warp_all[32];
   CacheSeq s;
   int64_t at;
   int b;
 };
 
-// (kLast: the cursor at its last unit.)  Up to kThreads sequences take one pass over the counts
+// (kLast: the cursor at its last tile.)  Up to kThreads sequences take one pass over the counts
 // and two barriers; more, a second pass.
 template <int kRows, int kTile, int kThreads, bool kLast = false>
 __device__ __forceinline__ Run find_run(const AttnParams& p, Cursor& c, int cta, int ctas, RunScratch& scratch) {
   constexpr int kWarps = kThreads / 32;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  Run r{0, 0, {0, 0}, 0};
+  Run r{0, 0, {0, 0}};
   CacheSeq mine{};
-  Work first{0, 0}, all{0, 0};
+  int64_t first = 0, all = 0;
   bool bad = false;
   for (int b = threadIdx.x; b < p.sequences; b += kThreads) {
     const CacheSeq s = read_seq<kRows, kTile>(p, b);
     bad |= s.bad;
-    const Work u = seq_work<kRows, kTile>(p, s);
+    const int64_t u = seq_units<kRows, kTile>(p, s);
     if (b < kThreads) {
       first = u;
       mine = s;
     }
-    all = {all.tiles + u.tiles, all.items + u.items};
+    all += u;
   }
   if (bad && cta == 0) atomicExch(p.err, kErrInvalid);
   // the sequences up to this thread's, and all
-  auto scan = [&](Work u) {
+  auto scan = [&](int64_t u) {
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const int64_t t = __shfl_up_sync(0xFFFFFFFFu, u.tiles, o), n = __shfl_up_sync(0xFFFFFFFFu, u.items, o);
-      if (lane >= o) u = {u.tiles + t, u.items + n};
+      const int64_t n = __shfl_up_sync(0xFFFFFFFFu, u, o);
+      if (lane >= o) u += n;
     }
     return u;
   };
-  Work incl = scan(first);
+  int64_t incl = scan(first);
   if (lane == 31) scratch.warp_sum[warp] = incl;
   if (p.sequences > kThreads) {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-      all.tiles += __shfl_xor_sync(0xFFFFFFFFu, all.tiles, o);
-      all.items += __shfl_xor_sync(0xFFFFFFFFu, all.items, o);
-    }
+    for (int o = 16; o > 0; o >>= 1) all += __shfl_xor_sync(0xFFFFFFFFu, all, o);
     if (lane == 0) scratch.warp_all[warp] = all;
   }
   __syncthreads();
-  auto plus = [](const Work& a, const Work& b) { return Work{a.tiles + b.tiles, a.items + b.items}; };
-  Work before{0, 0}, run{0, 0};
+  int64_t base = 0, run = 0;
 #pragma unroll
   for (int w = 0; w < kWarps; ++w) {
-    if (w < warp) before = plus(before, scratch.warp_sum[w]);
-    run = plus(run, scratch.warp_sum[w]);
+    if (w < warp) base += scratch.warp_sum[w];
+    run += scratch.warp_sum[w];
   }
-  Work total = run;
+  int64_t total = run;
   if (p.sequences > kThreads) {
-    total = {0, 0};
-    for (int w = 0; w < kWarps; ++w) total = plus(total, scratch.warp_all[w]);
+    total = 0;
+    for (int w = 0; w < kWarps; ++w) total += scratch.warp_all[w];
   }
-  if (total.tiles == 0) return r;
-  // (with fewer tiles per CTA a gap would rather give somebody one more of them)
-  r.gap = total.tiles >= (int64_t)p.item_cost * ctas ? p.item_cost : 0;
-  auto units = [&](const Work& w) { return w.tiles + w.items * r.gap; };
-  const int64_t working = split_ctas(units(total), ctas, p.least);
+  if (total == 0) return r;
+  const int64_t working = split_ctas(total, ctas, p.least);
   if (cta >= working) return r;
-  r.split = split_evenly(units(total), working);
+  r.split = split_evenly(total, working);
   r.begin = split_begin(r.split, cta);
   r.end = split_begin(r.split, cta + 1);
   const int64_t want = kLast ? r.end - 1 : r.begin;
-  // (want: in the thread's own sequence, which ends `incl` behind the units before its warp?)
-  auto look = [&](int b, const Work& own) {
-    const int64_t end = units(plus(before, incl)), begin = end - units(own);
-    if (begin <= want && want < end) {
-      scratch.b = b;
-      scratch.s = mine;
-      scratch.at = want - begin;
-    }
+  auto found = [&](int b, const CacheSeq& s, int64_t before) {
+    scratch.b = b;
+    scratch.s = s;
+    scratch.at = want - before;
   };
-  look(threadIdx.x, first);
-  for (int b0 = kThreads; units(run) <= want; b0 += kThreads) {   // (the total above want: some sequence has it)
+  if (base + incl - first <= want && want < base + incl) found(threadIdx.x, mine, base + incl - first);
+  for (int b0 = kThreads; run <= want; b0 += kThreads) {   // (total above want: some sequence has it)
     const int b = b0 + threadIdx.x;
-    Work u{0, 0};
+    int64_t u = 0;
     if (b < p.sequences) {
       mine = read_seq<kRows, kTile>(p, b);
-      u = seq_work<kRows, kTile>(p, mine);
+      u = seq_units<kRows, kTile>(p, mine);
     }
     incl = scan(u);
     __syncthreads();   // warp_sum's last readers
     if (lane == 31) scratch.warp_sum[warp] = incl;
     __syncthreads();
-    before = run;
+    base = run;
     for (int w = 0; w < kWarps; ++w) {
-      if (w < warp) before = plus(before, scratch.warp_sum[w]);
-      run = plus(run, scratch.warp_sum[w]);
+      if (w < warp) base += scratch.warp_sum[w];
+      run += scratch.warp_sum[w];
     }
-    look(b, u);
+    if (base + incl - u <= want && want < base + incl) found(b, mine, base + incl - u);
   }
   __syncthreads();
   c.b = scratch.b;
   c.s = scratch.s;
   size_seq<kRows, kTile>(p, c);
-  const int64_t at = scratch.at;
-  const int64_t per = c.tiles + r.gap, item = div_small(at, per), tile = at - item * per;
+  const int64_t at = scratch.at, per = c.tiles + p.item_cost, item = div_small(at, per), tile = at - item * per;
   c.tile = (int)min(tile, (int64_t)(c.tiles - 1));
   c.h = (int)div_small(item, c.row_tiles);
   c.rt = (int)(item - (int64_t)c.h * c.row_tiles);
-  // in a gap: on to the next item, or back to the last tile
+  // behind an item's tiles: on to the next item, or back to the last tile
   if (tile >= c.tiles) {
     if (kLast) {
       r.end -= tile - c.tile;
