@@ -596,7 +596,7 @@ __global__ void __launch_bounds__(TileCfg<kDC, kCodes>::kThreads, 1)
       const uint32_t q_dst = smem_u32(q_smem) + (halves ? s * C::kQSlot : 0);
       if (stores_q) {
         constexpr int kPieces = kD / 8;   // of 16 bytes
-#pragma unroll
+#pragma unroll 1
         for (int i = 0; i < kPieces; ++i) {
           const int at = i * 32 + lane, row = at / kPieces, piece = at % kPieces, to = (r & ~31) + row;
           const int64_t from = __shfl_sync(0xFFFFFFFFu, q_row, row);
@@ -619,7 +619,7 @@ __global__ void __launch_bounds__(TileCfg<kDC, kCodes>::kThreads, 1)
                                                   : make_uint4(0u, 0u, 0u, 0u);
         };
         uint32_t top = 0u;
-#pragma unroll 8
+#pragma unroll 2
         for (int i = 0; i < kD / 8; ++i) {
           const uint4 w = piece(i);
           top = __vmaxu2(__vmaxu2(__vmaxu2(__vmaxu2(top, w.x & 0x7FFF7FFFu), w.y & 0x7FFF7FFFu), w.z & 0x7FFF7FFFu),
@@ -635,7 +635,7 @@ __global__ void __launch_bounds__(TileCfg<kDC, kCodes>::kThreads, 1)
           const float2 v = p.fp16 ? __half22float2(*reinterpret_cast<const __half2*>(&w)) : make_float2(bf16_lo(w), bf16_hi(w));
           return pack_f16x2(v.x * down, v.y * down);
         };
-#pragma unroll 8
+#pragma unroll 2
         for (int i = 0; i < (stores_q ? kD / 8 : 0); ++i) {
           const uint4 w = lds128(place(i));
           st_shared_v4(place(i), scaled(w.x), scaled(w.y), scaled(w.z), scaled(w.w));
