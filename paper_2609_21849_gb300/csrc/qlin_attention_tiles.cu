@@ -15,7 +15,8 @@
 // memory a cycle bring a half's scores Q's rows and 64 keys), 1024 of exponentials (four cycles a warp
 // measured), 64 KB of keys and values, about 2850 cycles of an SM's share of HBM.
 // Roles: warps 0 and 2 load K and V, warp 1 issues MMAs, warp 3 walks the run for the softmax a
-// segment ahead of it (and asks for the segment's Q), warps 4-11 and 12-19 are the streams' softmax.
+// segment ahead of it (and asks for the segment's Q), warps 4-7 and 8-11 are the streams' softmax, four
+// more convert codes.
 // Tiles with new tokens are masked, and V's slots behind the last key and values that are
 // not finite are zeroed in shared memory: 0 times them would reach rows that do not see them.
 // (Rows that do see such a value take it at the end.)
@@ -25,11 +26,12 @@
 // An item that several CTAs share is joined by a second kernel, many CTAs to an item (joined by one
 // of these, at one SM's rate of reading, the trees below took 40 us longer).
 //   Measured, 16 trees of 64 tokens behind 8192-16384 keys, 8 KV heads of 128, 4 query heads each:
-// 214 us (bf16; the keys and values from HBM need 126, the MMAs 106), 240 from E4M3; 291 at heads of
-// 256 behind half as many keys.  About 4800 cycles a tile: the tensor pipe is busy a third of the time
+// 210 us (bf16; the keys and values from HBM need 126, the MMAs 106), 232 from E4M3; 290 at heads of
+// 256 behind half as many keys.  About 3600 cycles a tile: the tensor pipe is busy a third of the time
 // and no issue slot is short; what lasts is each stream's chain of scores, maximum, exponentials, P
 // and products, of which two run at a time.  A segment's begin and end (Q's way in, the first scores,
-// the last products, O's way out) leave the tensor cores idle for 5000 to 7000 cycles.
+// the tiles with masks, the last products, O's way out) take 10000 to 20000 cycles, many of them for
+// instructions that no tile before them brought: their loops are not unrolled.
 #include <type_traits>
 
 #include "qlin_attention_work.cuh"
