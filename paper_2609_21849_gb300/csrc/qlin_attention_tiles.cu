@@ -7,7 +7,7 @@
 // 128 rows the streams are the rows' halves over the same keys; with 128 or fewer, even and
 // odd tiles over the same rows, joined at the end.  Per stream and tile:
 //   S = Q K^T     tcgen05 from shared memory (K's pages by TMA, 128-byte swizzle) into 128 columns
-//   P = 2^(S - m) two threads per row, 64 scores in registers each, P as 16-bit over S's columns
+//   P = 2^(S - m) a thread per row, 64 scores in registers at a time, P as 16-bit over S's columns
 //   O += P V      A from tensor memory, V as it lies (keys x elements: an MN-major B)
 // The running maximum moves only when it rises by more than 2^8, so O is rarely rescaled; P
 // stays below 2^8 and the sums in fp32 (both fine in 16 bits: a P's rounding is relative).
