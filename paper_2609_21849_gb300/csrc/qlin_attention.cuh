@@ -20,7 +20,7 @@
 // before that rounding: errors of half a step of P, independent from key to key, average out.
 //   Measured: 64 tokens over 64 caches of 2048-8192 keys in E4M3, 8 KV heads of 128, 8 query heads
 // each, 142 us, 72% of the copy rate (half of an MMA's rows are empty, and the conversion of codes
-// takes more issue slots than the products); one token over 1000 keys 9.9: a launch, six tiles' worth
+// takes more issue slots than the products); one token over 1000 keys 9.8: a launch, six tiles' worth
 // of latency and the join.
 #include <type_traits>
 
@@ -604,10 +604,12 @@ __global__ void __launch_bounds__(kWarps * 32, (AttnCfg<kKind, kD, kM>::kCtas)) 
     // (alone it takes no count: an item's last group, of this CTA alone, has the number that the item
     // which begins here counts with)
     if (parties == 1) return true;
-    __threadfence();   // (the CTA's stores, which the barrier orders before)
-    const bool all = atomicAdd(count, 1u) == (unsigned)(parties - 1);
+    // (releases the CTA's stores, which the barrier orders before, and acquires the other CTAs'; a
+    // relaxed one between two __threadfence() took 0.35 of 10.1 us longer)
+    unsigned before;
+    asm volatile("atom.acq_rel.gpu.global.add.u32 %0, [%1], 1;" : "=r"(before) : "l"(count) : "memory");
+    const bool all = before == (unsigned)(parties - 1);
     if (all) *count = 0u;   // as it was before the call
-    __threadfence();
     return all;
   };
   // a group: as many parts as a CTA joins in about the time that another level takes
