@@ -8,6 +8,12 @@ namespace qlin {
 
 enum class CacheKind { kBf16, kFp16, kE4m3 };
 
+// An item of the tiles' kernel that begins in a CTA and ends in another (rows 0: none does).
+struct JoinItem {
+  int64_t token0;
+  int row0, head0, rows, last;   // last: the CTA that it ends in
+};
+
 struct AttnParams {
   const uint16_t* q;
   int64_t q_token, q_head;        // elements
@@ -32,6 +38,7 @@ struct AttnParams {
   int fp16;                         // q and out are fp16, not bf16
   // workspace: counts (zero between calls), (maximum, sum) and sums of unfinished rows
   unsigned* counts;
+  JoinItem* join;            // of the tiles' kernel
   float2* part_ml;
   float* part;
   int least;                        // tiles that a CTA should have
@@ -39,9 +46,10 @@ struct AttnParams {
   unsigned* err;
 };
 
-// Workspace: two counts per CTA, then two unfinished items per CTA.
+// Workspace: two counts per CTA (mma.sync) and an item to join (tiles), then two unfinished items per CTA.
 constexpr int kMostCtas = 1024;
 constexpr int64_t kCountBytes = 2 * kMostCtas * 4;
+constexpr int64_t kJoinBytes = kMostCtas * sizeof(JoinItem);
 constexpr int64_t kWorkspaceBytes = (int64_t)64 << 20;
 
 // Many rows on tcgen05 (qlin_attention_tiles.cu): whether it takes these pages and heads.

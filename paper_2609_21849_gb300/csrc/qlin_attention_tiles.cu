@@ -234,6 +234,7 @@ __global__ void __launch_bounds__(TileCfg<kDC, kCodes>::kThreads, 1)
   extern __shared__ __align__(1024) uint8_t smem[];
   if ((smem_u32(smem) & 1023u) != 0u) {   // (the swizzle's atoms; no other shared memory comes before)
     atomicExch(p.err, kErrTimeout);
+    if (threadIdx.x == 0) p.join[blockIdx.x].rows = 0;
     return;
   }
   uint8_t* const q_smem = smem;
@@ -477,6 +478,7 @@ __global__ void __launch_bounds__(TileCfg<kDC, kCodes>::kThreads, 1)
       uint32_t base = 0;
       unsigned tiles_done = 0, phase = 0;
       int64_t unit = run.begin;
+      JoinItem mine{0, 0, 0, 0, 0};
       for (int at = 0;; at ^= 1) {
         if (!mbar_wait_warp(&seg_free[at], phase ^ 1u, ctl)) break;
         phase ^= (uint32_t)at;
@@ -501,6 +503,10 @@ __global__ void __launch_bounds__(TileCfg<kDC, kCodes>::kThreads, 1)
         }
         __syncwarp();
         if (!any) break;
+        const int64_t item0 = unit - sg.first, item1 = item0 + cur.tiles - 1;
+        if (item0 >= run.begin && item1 >= run.end)
+          mine = {cur.s.first, cur.rt * kRows, cur.h * p.group, min(kRows, cur.s.fresh * p.group - cur.rt * kRows),
+                  (int)split_owner(run.split, item1)};
         // its rows of Q towards L2
         for (int i = lane; i < kRows; i += 32) {
           const int row = cur.rt * kRows + i;
@@ -514,6 +520,7 @@ __global__ void __launch_bounds__(TileCfg<kDC, kCodes>::kThreads, 1)
         unit = unit_after(cur, sg, unit, p.item_cost);
         if (unit < run.end) skip_segment<C>(p, cur, sg);
       }
+      if (lane == 0) p.join[blockIdx.x] = mine;
     }
   } else if (kCodes && warp >= kSoftWarp0 + C::kSoftThreads / 32) {
     // ---- codes to fp16 (exactly), from the rows as they came to the MMAs' swizzled tiles ----
@@ -889,27 +896,62 @@ __global__ void __launch_bounds__(TileCfg<kDC, kCodes>::kThreads, 1)
   }
 }
 
-// Items that end in other CTAs than they begin in: CTA x joins the one that begins in CTA x of
-// the kernel above, kJoinRows rows of it.
-constexpr int kJoinRows = 32, kJoinThreads = 256;
-template <int kDC, int kRows, int kTile>
-__global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const AttnParams p, int ctas) {
-  __shared__ float2 stat[kJoinRows];
-  __shared__ RunScratch scratch;
-  Cursor cur;
-  const int cta = (int)blockIdx.x;
-  // (lengths and counts: as the kernel before found them, which began after they were written)
-  const Run run = find_run<kRows, kTile, kJoinThreads, true>(p, cur, cta, ctas, scratch);
+// Items that end in other CTAs than they begin in, kJoinRows rows of one a CTA, their parts joined in
+// the order of the keys.  What it costs is waiting for L2: a thread has four elements of kJoin parts
+// and their maxima and sums on their way at a time, and meets no other.  (With the items found anew and
+// the maxima and sums taken first, the trees above took 8 us longer, one short tree 31.6, not 25.7.)
+constexpr int kJoinRows = 16, kJoinThreads = 256, kJoin = 4;
+template <int kDC, int kRows>
+__global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const __grid_constant__ AttnParams p) {
+  constexpr int kD = 64 * kDC;
   grid_dep_wait();
   grid_dep_launch();
-  if (run.begin >= run.end) return;
-  const int64_t item0 = run.end - 1 - cur.tile, item1 = item0 + cur.tiles - 1;
-  if (item0 < run.begin || item1 < run.end) return;   // begun before, or whole
-  const int all = (int)min((int64_t)kRows, (int64_t)cur.s.fresh * p.group - (int64_t)cur.rt * kRows);
-  const int row0 = (int)blockIdx.y * kJoinRows, rows = min(kJoinRows, all - row0);
-  if (rows <= 0) return;
+  const int first = (int)blockIdx.x, row_first = (int)blockIdx.y * kJoinRows;
+  const JoinItem u = p.join[first];
+  const int parts = u.last - first + 1;
   const float v_scale = p.v_scale != nullptr ? *p.v_scale : 1.0f;
-  join_parts<kRows, 64 * kDC, kJoinThreads>(p, cur, cta, (int)split_owner(run.split, item1), v_scale, row0, rows, stat);
+#pragma unroll 1
+  for (int i = threadIdx.x; i < kJoinRows * (p.head_dim / 4); i += kJoinThreads) {
+    const int row = row_first + i % kJoinRows, d = i / kJoinRows * 4;
+    if (row >= u.rows) continue;
+    float m = -INFINITY, l = 0.0f;
+    float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 1
+    for (int q0 = 0; q0 < parts; q0 += kJoin) {
+      float4 v[kJoin];
+      float2 ml[kJoin];
+      // (past the last part its own again, with a maximum of minus infinity: no branch between the loads)
+#pragma unroll
+      for (int k = 0; k < kJoin; ++k) {
+        const int cta = first + min(q0 + k, parts - 1);
+        ml[k] = __ldcg(&p.part_ml[part_row<kRows>(cta, first, row)]);
+        v[k] = __ldcg(part_sums<kRows, kD>(p, part_row<kRows>(cta, first, 0), row, d));
+      }
+      float now = m;
+#pragma unroll
+      for (int k = 0; k < kJoin; ++k) {
+        if (q0 + k >= parts) ml[k].x = -INFINITY;
+        now = fmaxf(now, ml[k].x);
+      }
+      const float base = now == -INFINITY ? 0.0f : now, keep = exp2_fast(m - base);
+      l *= keep;
+      o = make_float4(o.x * keep, o.y * keep, o.z * keep, o.w * keep);
+#pragma unroll
+      for (int k = 0; k < kJoin; ++k) {
+        const float w = exp2_fast(ml[k].x - base);
+        if (w != 0.0f) {   // (a weight of 0 takes no part of what lies there)
+          l = fmaf(ml[k].y, w, l);
+          o = make_float4(fmaf(v[k].x, w, o.x), fmaf(v[k].y, w, o.y), fmaf(v[k].z, w, o.z), fmaf(v[k].w, w, o.w));
+        }
+      }
+      m = now;
+    }
+    const int r = u.row0 + row, head = u.head0 + r % p.group;
+    const int64_t token = u.token0 + r / p.group;
+    const float inv = l == 0.0f ? 0.0f : v_scale / l;
+    store_out4(p, token, head, d, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
+    if (p.lse != nullptr && d == 0) p.lse[token * p.lse_token + head] = log_sum(m, l);
+  }
 }
 
 template <bool kF16, int kDC, bool kCodes>
@@ -922,9 +964,10 @@ cudaError_t launch_cfg(TileParams tp, const CUtensorMap& tk, const CUtensorMap& 
   });
   if (e != cudaSuccess) return e;
   constexpr int64_t kPart = 2 * C::kRows * ((int64_t)64 * kDC * 4 + 8);
-  const int ctas = (int)std::min<int64_t>(dev.num_sms, std::min<int64_t>(kMostCtas, (kWorkspaceBytes - kCountBytes) / kPart));
+  const int ctas = (int)std::min<int64_t>(dev.num_sms, std::min<int64_t>(kMostCtas, (kWorkspaceBytes - kCountBytes - kJoinBytes) / kPart));
   AttnParams& p = tp.a;
-  p.part_ml = reinterpret_cast<float2*>(reinterpret_cast<uint8_t*>(p.counts) + kCountBytes);
+  p.join = reinterpret_cast<JoinItem*>(reinterpret_cast<uint8_t*>(p.counts) + kCountBytes);
+  p.part_ml = reinterpret_cast<float2*>(reinterpret_cast<uint8_t*>(p.join) + kJoinBytes);
   p.part = reinterpret_cast<float*>(p.part_ml + (int64_t)2 * C::kRows * ctas);
   p.least = 2;
   // (in us without it, with 6, 8, 11 and 15: the trees above 225, 213, 214, 213, 219; 64 of 500-1000 keys
@@ -933,7 +976,7 @@ cudaError_t launch_cfg(TileParams tp, const CUtensorMap& tk, const CUtensorMap& 
   p.item_cost = 8;
   const cudaError_t st = launch_pdl(kern, dim3((unsigned)ctas), C::kThreads, C::kSmem, s, tk, tv, tp);
   if (st != cudaSuccess) return st;
-  return launch_pdl(attn_join_kernel<kDC, C::kRows, C::kTile>, dim3((unsigned)ctas, C::kRows / kJoinRows), kJoinThreads, 0, s, p, ctas);
+  return launch_pdl(attn_join_kernel<kDC, C::kRows>, dim3((unsigned)ctas, C::kRows / kJoinRows), kJoinThreads, 0, s, p);
 }
 
 }  // namespace

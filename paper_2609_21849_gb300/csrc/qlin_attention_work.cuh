@@ -81,9 +81,9 @@ struct RunScratch {   // in shared memory
   int b;
 };
 
-// (kLast: the cursor at its last tile.)  Up to kThreads sequences take one pass over the counts
+// Up to kThreads sequences take one pass over the counts
 // and two barriers; more, a second pass.
-template <int kRows, int kTile, int kThreads, bool kLast = false>
+template <int kRows, int kTile, int kThreads>
 __device__ __forceinline__ Run find_run(const AttnParams& p, Cursor& c, int cta, int ctas, RunScratch& scratch) {
   constexpr int kWarps = kThreads / 32;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -136,7 +136,7 @@ __device__ __forceinline__ Run find_run(const AttnParams& p, Cursor& c, int cta,
   r.split = split_evenly(total, working);
   r.begin = split_begin(r.split, cta);
   r.end = split_begin(r.split, cta + 1);
-  const int64_t want = kLast ? r.end - 1 : r.begin;
+  const int64_t want = r.begin;
   auto found = [&](int b, const CacheSeq& s, int64_t before) {
     scratch.b = b;
     scratch.s = s;
@@ -169,14 +169,9 @@ __device__ __forceinline__ Run find_run(const AttnParams& p, Cursor& c, int cta,
   c.tile = (int)min(tile, (int64_t)(c.tiles - 1));
   c.h = (int)div_small(item, c.row_tiles);
   c.rt = (int)(item - (int64_t)c.h * c.row_tiles);
-  // behind an item's tiles: on to the next item, or back to the last tile
-  if (tile >= c.tiles) {
-    if (kLast) {
-      r.end -= tile - c.tile;
-    } else {
-      r.begin += per - tile;
-      if (r.begin < r.end) advance<kRows, kTile>(p, c);
-    }
+  if (tile >= c.tiles) {   // behind an item's tiles: on to the next item
+    r.begin += per - tile;
+    if (r.begin < r.end) advance<kRows, kTile>(p, c);
   }
   return r;
 }
@@ -209,63 +204,6 @@ __device__ __forceinline__ int64_t part_row(int cta, int first, int row) {
 template <int kRows, int kD>
 __device__ __forceinline__ float4* part_sums(const AttnParams& p, int64_t part_row0, int row, int d) {
   return reinterpret_cast<float4*>(p.part + part_row0 * kD) + (int64_t)(d / 4) * kRows + row;
-}
-
-// Rows row0 .. row0 + rows - 1 of an item, whose parts the CTAs first to last left in the
-// workspace, joined in the order of the keys.  Called by all of kThreads threads of a CTA; stat:
-// `rows` of them in shared memory.
-template <int kRows, int kD, int kThreads>
-__device__ __forceinline__ void join_parts(const AttnParams& p, const Cursor& c, int first, int last, float v_scale,
-                                           int row0, int rows, float2* stat) {
-  const int thread = (int)threadIdx.x;
-  for (int i = thread; i < rows; i += kThreads) {
-    float m = -INFINITY, l = 0.0f;
-#pragma unroll 4
-    for (int q = first; q <= last; ++q) {
-      const float2 ml = __ldcg(&p.part_ml[part_row<kRows>(q, first, row0 + i)]);
-      const float now = fmaxf(m, ml.x), base = now == -INFINITY ? 0.0f : now;
-      l = fmaf(l, exp2_fast(m - base), ml.y * exp2_fast(ml.x - base));
-      m = now;
-    }
-    stat[i] = make_float2(m, l);
-  }
-  __syncthreads();
-  const int items = rows * (p.head_dim / 4);
-  constexpr int kAtOnce = 4;
-  for (int i0 = thread; i0 < items; i0 += kThreads * kAtOnce) {
-    float4 o[kAtOnce];
-    float base[kAtOnce];
-#pragma unroll
-    for (int k = 0; k < kAtOnce; ++k) {
-      const int i = min(i0 + k * kThreads, items - 1);
-      const float m = stat[i % rows].x;
-      base[k] = m == -INFINITY ? 0.0f : m;
-      o[k] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    }
-#pragma unroll 2
-    for (int q = first; q <= last; ++q) {
-#pragma unroll
-      for (int k = 0; k < kAtOnce; ++k) {
-        const int i = min(i0 + k * kThreads, items - 1), row = row0 + i % rows;
-        const float f = exp2_fast(__ldcg(&p.part_ml[part_row<kRows>(q, first, row)].x) - base[k]);
-        const float4 v = __ldcg(part_sums<kRows, kD>(p, part_row<kRows>(q, first, 0), row, i / rows * 4));
-        o[k] = make_float4(fmaf(v.x, f, o[k].x), fmaf(v.y, f, o[k].y), fmaf(v.z, f, o[k].z), fmaf(v.w, f, o[k].w));
-      }
-    }
-#pragma unroll
-    for (int k = 0; k < kAtOnce; ++k) {
-      const int i = i0 + k * kThreads;
-      if (i >= items) break;
-      const int row = i % rows, d = i / rows * 4;
-      const float2 ml = stat[row];
-      const int64_t r = (int64_t)c.rt * kRows + row0 + row;
-      const int64_t token = c.s.first + r / p.group;
-      const int head = c.h * p.group + (int)(r % p.group);
-      const float inv = ml.y == 0.0f ? 0.0f : v_scale / ml.y;
-      store_out4(p, token, head, d, make_float4(o[k].x * inv, o[k].y * inv, o[k].z * inv, o[k].w * inv));
-      if (p.lse != nullptr && d == 0) p.lse[token * p.lse_token + head] = log_sum(ml.x, ml.y);
-    }
-  }
 }
 
 }  // namespace
