@@ -31,7 +31,7 @@
 // and no issue slot is short; what lasts is each stream's chain of scores, maximum, exponentials, P
 // and products, of which two run at a time.  A segment's begin and end (Q's way in, the first scores,
 // the tiles with masks, the last products, O's way out) take 10000 to 20000 cycles, many of them for
-// instructions that no tile before them brought: their loops are not unrolled.
+// instructions that no tile before them brought: their loops stay short.
 #include <type_traits>
 
 #include "qlin_attention_work.cuh"
@@ -605,7 +605,7 @@ __global__ void __launch_bounds__(TileCfg<kDC, kCodes>::kThreads, 1)
       const uint32_t q_dst = smem_u32(q_smem) + (halves ? s * C::kQSlot : 0);
       if (stores_q) {
         constexpr int kPieces = kD / 8;   // of 16 bytes
-#pragma unroll 1
+#pragma unroll 4
         for (int i = 0; i < kPieces; ++i) {
           const int at = i * 32 + lane, row = at / kPieces, piece = at % kPieces, to = (r & ~31) + row;
           const int64_t from = __shfl_sync(0xFFFFFFFFu, q_row, row);
@@ -900,7 +900,7 @@ __global__ void __launch_bounds__(TileCfg<kDC, kCodes>::kThreads, 1)
 // the order of the keys.  What it costs is waiting for L2: a thread has four elements of kJoin parts
 // and their maxima and sums on their way at a time, and meets no other.  (With the items found anew and
 // the maxima and sums taken first, the trees above took 8 us longer, one short tree 31.6, not 25.7.)
-constexpr int kJoinRows = 16, kJoinThreads = 256, kJoin = 4;
+constexpr int kJoinRows = 8, kJoinThreads = 256, kJoin = 4;
 template <int kDC, int kRows>
 __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const __grid_constant__ AttnParams p) {
   constexpr int kD = 64 * kDC;
