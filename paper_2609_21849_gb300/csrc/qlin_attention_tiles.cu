@@ -24,9 +24,9 @@
 // tile's keys taking the streams' turns.  E4M3 codes land in a ring of their own, and four warps
 // convert them to fp16 tiles (every code is an fp16); Q becomes fp16 after a power of two per row.
 // An item that several CTAs share is joined by a second kernel, many CTAs to an item (joined by one
-// of these, at one SM's rate of reading, the trees below took 40 us longer).
+// of these, at one SM's rate of reading, the trees below took 40 us longer); it takes 14 of their us.
 //   Measured, 16 trees of 64 tokens behind 8192-16384 keys, 8 KV heads of 128, 4 query heads each:
-// 210 us (bf16; the keys and values from HBM need 126, the MMAs 106), 232 from E4M3; 290 at heads of
+// 199 us (bf16; the keys and values from HBM need 126, the MMAs 106), 221 from E4M3; 288 at heads of
 // 256 behind half as many keys.  About 3600 cycles a tile: the tensor pipe is busy a third of the time
 // and no issue slot is short; what lasts is each stream's chain of scores, maximum, exponentials, P
 // and products, of which two run at a time.  A segment's begin and end (Q's way in, the first scores,
@@ -970,7 +970,7 @@ cudaError_t launch_cfg(TileParams tp, const CUtensorMap& tk, const CUtensorMap& 
   p.part_ml = reinterpret_cast<float2*>(reinterpret_cast<uint8_t*>(p.join) + kJoinBytes);
   p.part = reinterpret_cast<float*>(p.part_ml + (int64_t)2 * C::kRows * ctas);
   p.least = 2;
-  // (in us without it, with 6, 8, 11 and 15: the trees above 225, 213, 214, 213, 219; 64 of 500-1000 keys
+  // (in us without it, with 6, 8, 11 and 15, before the join below its present form: the trees above 225, 213, 214, 213, 219; 64 of 500-1000 keys
   // 152, 135, 131, 132, 135; three of 15000-30000 keys 109, 99, 100, 95, 96; without and with 8: four of
   // 2048-4096 keys 51.6, 45.0, 16 of 250-500 52.7, 42.6)
   p.item_cost = 8;
