@@ -939,7 +939,7 @@ __global__ void __launch_bounds__(kJoinThreads) attn_join_kernel(const __grid_co
 #pragma unroll
       for (int k = 0; k < kJoin; ++k) {
         const float w = exp2_fast(ml[k].x - base);
-        if (w != 0.0f) {   // (a weight of 0 takes no part of what lies there)
+        if (q0 + k < parts) {   // (whatever its weight: a part of NaN scores has a weight of 0 and a NaN sum)
           l = fmaf(ml[k].y, w, l);
           o = make_float4(fmaf(v[k].x, w, o.x), fmaf(v[k].y, w, o.y), fmaf(v[k].z, w, o.z), fmaf(v[k].w, w, o.w));
         }

@@ -1,0 +1,74 @@
+"""Attention over a paged cache where queries, keys, values or scales are NaN or infinite: the
+formula's NaN comes out of every row that they reach, whether its keys lie in one CTA or are split
+among several, and the other rows keep their bits."""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from paper_2609_21849_gb300 import qlin
+from test_gpu_cache import FORMATS, _fill, _gen, _make, _slots
+
+pytestmark = pytest.mark.gpu
+
+HEADS, D = 2, 64
+# new tokens, query heads of a KV head (few rows and many), cached tokens (one CTA's keys and many CTAs')
+FORMS = [(1, 4, 20), (1, 4, 1000), (1, 4, 20000), (40, 4, 20), (40, 4, 3000), (40, 4, 20000)]
+
+
+def _call(c, q, scale=0.125):
+    lse = torch.full(q.shape[:2], 5.0, device="cuda")
+    out = qlin.qlin_cache_attention(c, q, scale, lse=lse)
+    assert qlin.qlin_sync_status() == 0
+    return out, lse
+
+
+def _setup(T, G, have, fmt, dtype):
+    c = _make([have], [T], HEADS, D, 16, fmt)
+    _fill(c, [have], [T])
+    return c, torch.randn(T, HEADS * G, D, generator=_gen(5), device="cuda").to(dtype)
+
+
+@pytest.mark.parametrize("fmt,dtype", FORMATS)
+@pytest.mark.parametrize("T,G,have", FORMS)
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+def test_a_query_that_is_not_finite_gives_nan(bad, T, G, have, fmt, dtype):
+    c, q = _setup(T, G, have, fmt, dtype)
+    good, good_lse = _call(c, q)
+    q[T - 1, 1, 7] = bad   # (an infinity times keys of both signs: scores of both infinities)
+    out, lse = _call(c, q)
+    assert out[T - 1, 1].isnan().all() and lse[T - 1, 1].isnan()
+    rest = torch.ones(T, HEADS * G, dtype=torch.bool, device="cuda")
+    rest[T - 1, 1] = False
+    assert torch.equal(out[rest], good[rest]) and torch.equal(lse[rest], good_lse[rest])
+
+
+@pytest.mark.parametrize("fmt,dtype", FORMATS)
+@pytest.mark.parametrize("T,G,have", [f for f in FORMS if f[2] >= 1000])
+def test_a_nan_among_keys_of_little_weight(T, G, have, fmt, dtype):
+    """The first half's keys are zero, the others' scores lie 300 powers of two above: what is NaN in
+    the first half has a weight that fp32 does not hold, and still reaches every row."""
+    c, q = _setup(T, G, have, fmt, dtype)
+    q.fill_(1.0)
+    where = _slots(c, 0, have + T)
+    c.k[where] = torch.zeros((), device="cuda").to(c.k.dtype)
+    high = tuple(i[have // 2:] for i in where)
+    c.k[high] = torch.full((), 4.0 if c.k_scale is None else 4.0 / c.k_scale.item(), device="cuda").to(c.k.dtype)
+    scale = 300 / (4 * D) * math.log(2)   # (E4M3: 4 / k_scale = 298.7 is 288, 289 powers of two)
+    good, good_lse = _call(c, q, scale)
+    assert good.isfinite().all() and good_lse.isfinite().all()
+    page, slot = (int(i[have // 4]) for i in where)
+    nan = torch.full((), math.nan, device="cuda").to(c.v.dtype)
+    for t in (c.v, c.k):
+        old = t[page, slot, 1].clone()
+        t[page, slot, 1, 3] = nan
+        out, lse = _call(c, q, scale)
+        assert torch.equal(out[:, :G], good[:, :G]) and torch.equal(lse[:, :G], good_lse[:, :G])
+        if t is c.v:
+            assert out[:, G:, 3].isnan().all() and torch.equal(lse, good_lse)
+            others = [d for d in range(D) if d != 3]
+            assert torch.equal(out[..., others], good[..., others])
+        else:
+            assert out[:, G:].isnan().all() and lse[:, G:].isnan().all()
+        t[page, slot, 1] = old
