@@ -419,10 +419,20 @@ __global__ void __launch_bounds__(kWarps * 32, (AttnCfg<kKind, kD, kM>::kCtas)) 
 #pragma unroll
         for (int i = 0; i < kM; ++i)
 #pragma unroll
-          for (int j = 0; j < kNT; ++j)
+          for (int r = 0; r < 2; ++r) {
+            const int64_t row = (int64_t)cur.rt * kRows + i * 16 + r * 8 + g;
+            const int tok = row < (int64_t)cur.s.fresh * p.group ? (int)(row / p.group) : 0;
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-              probs[(i * 16 + (k >> 1) * 8 + g) * kKeys + 8 * j + 2 * t + (k & 1)] = s[i][j][k];
+            for (int j = 0; j < kNT; ++j)
+#pragma unroll
+              for (int k = 0; k < 2; ++k) {
+                // (a key that the row does not see is -1: one that it sees may have a weight of 0 too)
+                const int key = 8 * j + 2 * t + k;
+                const int64_t i_new = key0 + key - cur.s.cached;
+                const bool seen = ((bits >> key) & 1u) != 0u && (i_new < 0 || sees(p, cur.s.first + tok, tok, i_new));
+                probs[(i * 16 + r * 8 + g) * kKeys + key] = seen ? s[i][j][2 * r + k] : -1.0f;
+              }
+          }
         __syncwarp();
         const uint8_t* const vs = smem + stage * C::kStageBytes + warp * C::kSlot + C::kKBytes;
         for (int key = 0; key < kKeys; ++key) {
@@ -444,7 +454,10 @@ __global__ void __launch_bounds__(kWarps * 32, (AttnCfg<kKind, kD, kM>::kCtas)) 
 #pragma unroll
                 for (int r = 0; r < 2; ++r) {
                   const float pr = probs[(i * 16 + r * 8 + g) * kKeys + key];
-                  if (pr != 0.0f) o[i][j][2 * r + k] = fmaf(pr, v, o[i][j][2 * r + k]);
+                  if (!(pr <= 0.0f))
+                    o[i][j][2 * r + k] = fmaf(pr, v, o[i][j][2 * r + k]);
+                  else if (pr == 0.0f && !(fabsf(v) < INFINITY))
+                    o[i][j][2 * r + k] += v;
                 }
             }
         }

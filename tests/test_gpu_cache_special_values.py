@@ -45,7 +45,7 @@ def test_a_query_that_is_not_finite_gives_nan(bad, T, G, have, fmt, dtype):
 
 
 @pytest.mark.parametrize("fmt,dtype", FORMATS)
-@pytest.mark.parametrize("T,G,have", [f for f in FORMS if f[2] >= 1000])
+@pytest.mark.parametrize("T,G,have", FORMS)
 def test_a_nan_among_keys_of_little_weight(T, G, have, fmt, dtype):
     """The first half's keys are zero, the others' scores lie 300 powers of two above: what is NaN in
     the first half has a weight that fp32 does not hold, and still reaches every row."""
@@ -72,3 +72,25 @@ def test_a_nan_among_keys_of_little_weight(T, G, have, fmt, dtype):
         else:
             assert out[:, G:].isnan().all() and lse[:, G:].isnan().all()
         t[page, slot, 1] = old
+
+
+@pytest.mark.parametrize("fmt,dtype", [f for f in FORMATS if f[0] != "e4m3"])
+@pytest.mark.parametrize("T,G", [(3, 4), (40, 4)])
+@pytest.mark.parametrize("bad", [math.inf, -math.inf])
+def test_an_infinite_value_of_little_weight_among_new_tokens(bad, T, G, fmt, dtype):
+    """New token 0's score lies 300 powers of two below the others': its infinite value comes out of the
+    rows that see it, and of no others."""
+    c, q = _setup(T, G, 5, fmt, dtype)
+    q.fill_(1.0)
+    where = _slots(c, 0, 5 + T)
+    c.k[where] = torch.full((), 4.0, device="cuda").to(c.k.dtype)
+    c.k[where[0][5], where[1][5]] = torch.zeros((), device="cuda").to(c.k.dtype)
+    mask = torch.full((T, 1), -1, dtype=torch.int64, device="cuda")
+    mask[1] = -2   # (token 1 does not see it)
+    c.v[where[0][5], where[1][5], 1, 3] = bad
+    out = qlin.qlin_cache_attention(c, q, 300 / (4 * D) * math.log(2), mask)
+    assert qlin.qlin_sync_status() == 0
+    sees = torch.arange(T, device="cuda") != 1
+    assert (out[sees][:, G:, 3] == bad).all()
+    out[:, G:, 3][sees] = 0.0
+    assert out.isfinite().all()
