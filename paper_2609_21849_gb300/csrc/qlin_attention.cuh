@@ -279,8 +279,9 @@ __global__ void __launch_bounds__(kWarps * 32, (AttnCfg<kKind, kD, kM>::kCtas)) 
                                    : __uint_as_float(top << 16);
           int e = (int)(__float_as_uint(big) >> 23);   // biased
           e = e == 0 || e == 255 ? 127 : min(e, 252);
-          const float down = __uint_as_float((uint32_t)(254 - e) << 23);
-          mult[i][r] = fminf(fmaxf(p.scale_log2 * __uint_as_float((uint32_t)e << 23) * k_scale, FLT_MIN), FLT_MAX);
+          const float down = signed_factor(__uint_as_float((uint32_t)(254 - e) << 23), k_scale);
+          mult[i][r] =
+              fminf(fmaxf(p.scale_log2 * __uint_as_float((uint32_t)e << 23) * fabsf(k_scale), FLT_MIN), FLT_MAX);
 #pragma unroll
           for (int k = 0; k < kQWords; ++k) {
             const uint32_t w = qf[i][r][k];

@@ -638,8 +638,8 @@ __global__ void __launch_bounds__(TileCfg<kDC, kCodes>::kThreads, 1)
         const float big = p.fp16 ? __half2float(__ushort_as_half((unsigned short)top)) : __uint_as_float(top << 16);
         int e = (int)(__float_as_uint(big) >> 23);   // biased
         e = e == 0 || e == 255 ? 127 : min(e, 252);
-        const float down = __uint_as_float((uint32_t)(254 - e) << 23);
-        mult = fminf(fmaxf(p.scale_log2 * __uint_as_float((uint32_t)e << 23) * *p.k_scale, FLT_MIN), FLT_MAX);
+        const float k_scale = *p.k_scale, down = signed_factor(__uint_as_float((uint32_t)(254 - e) << 23), k_scale);
+        mult = fminf(fmaxf(p.scale_log2 * __uint_as_float((uint32_t)e << 23) * fabsf(k_scale), FLT_MIN), FLT_MAX);
         auto scaled = [&](uint32_t w) {
           const float2 v = p.fp16 ? __half22float2(*reinterpret_cast<const __half2*>(&w)) : make_float2(bf16_lo(w), bf16_hi(w));
           return pack_f16x2(v.x * down, v.y * down);

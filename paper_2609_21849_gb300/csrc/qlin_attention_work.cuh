@@ -183,6 +183,13 @@ __device__ __forceinline__ bool sees(const AttnParams& p, int64_t token, int t, 
   return w < p.mask_words && ((p.mask[token * p.mask_token + w] >> (i & 63)) & 1u) != 0u;
 }
 
+// What a row of Q is multiplied by where its scores' factor takes the keys' scale without its sign, so
+// that the maximum stays one: the sign is Q's, and a scale of infinity or NaN makes the scores NaN (not
+// those of keys that the row does not see).
+__device__ __forceinline__ float signed_factor(float f, float k_scale) {
+  return fabsf(k_scale) < INFINITY ? copysignf(f, k_scale) : __uint_as_float(0x7FFFFFFFu);
+}
+
 __device__ __forceinline__ void store_out4(const AttnParams& p, int64_t token, int head, int d, float4 v) {
   uint16_t* const y = p.out + token * p.out_token + head * p.out_head + d;
   const uint2 w = p.fp16 ? make_uint2(pack_f16x2(v.x, v.y), pack_f16x2(v.z, v.w))

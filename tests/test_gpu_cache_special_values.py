@@ -8,7 +8,7 @@ import pytest
 torch = pytest.importorskip("torch")
 
 from paper_2609_21849_gb300 import qlin
-from test_gpu_cache import FORMATS, _fill, _gen, _make, _slots
+from test_gpu_cache import FORMATS, _check, _fill, _gen, _make, _slots
 
 pytestmark = pytest.mark.gpu
 
@@ -94,3 +94,42 @@ def test_an_infinite_value_of_little_weight_among_new_tokens(bad, T, G, fmt, dty
     assert (out[sees][:, G:, 3] == bad).all()
     out[:, G:, 3][sees] = 0.0
     assert out.isfinite().all()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("T,G,have", FORMS)
+def test_key_scales_of_any_sign(T, G, have, dtype):
+    c, q = _setup(T, G, have, "e4m3", dtype)
+    c.k_scale.neg_()
+    out, lse = _call(c, q)
+    _check(c, q, 0.125, None, "e4m3", out, lse)
+    # the same values from codes of the other sign
+    other = qlin.PagedCache(**(vars(c) | dict(k=(c.k.view(torch.uint8) ^ 0x80).view(c.k.dtype), k_scale=-c.k_scale)))
+    same, same_lse = _call(other, q)
+    assert torch.equal(out, same) and torch.equal(lse, same_lse)
+    for zero in (0.0, -0.0):
+        c.k_scale.fill_(zero)
+        out, lse = _call(c, q)
+        _check(c, q, 0.125, None, "e4m3", out, lse)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("T,G,have", FORMS)
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+def test_scales_that_are_not_finite_give_nan(bad, T, G, have, dtype):
+    c, q = _setup(T, G, have, "e4m3", dtype)
+    c.k_scale.fill_(bad)
+    out, lse = _call(c, q)
+    assert out.isnan().all() and lse.isnan().all()
+
+
+def test_rows_that_see_nothing_whatever_the_scale_and_the_query():
+    for T, G in ((1, 4), (40, 4)):
+        c, q = _setup(T, G, 0, "e4m3", torch.bfloat16)
+        q[0, 0, 0] = math.nan
+        for scale in (math.nan, math.inf, -1.0, 6 / 448):
+            c.k_scale.fill_(scale)
+            lse = torch.full(q.shape[:2], 5.0, device="cuda")
+            out = qlin.qlin_cache_attention(c, q, 0.125, torch.zeros(T, 1, dtype=torch.int64, device="cuda"), lse=lse)
+            assert (out == 0).all() and (lse == -math.inf).all()
+    assert qlin.qlin_sync_status() == 0
