@@ -572,9 +572,9 @@ typedef enum { QLIN_CACHE_BF16 = 1, QLIN_CACHE_FP16 = 2, QLIN_CACHE_E4M3 = 3 } q
  *              q_start[b] .. q_start[b + 1] - 1 of the call's.  Tokens of the call before the
  *              first or behind the last (a padded batch) are not touched; a sequence may have
  *              none.
- *  k_scale, v_scale: E4M3 only, device fp32 decode scales: value = code * scale, of either sign.
- *              The attention's rows that see a key are NaN with a k_scale that is infinite or
- *              NaN; v_scale multiplies the sum.
+ *  k_scale, v_scale: E4M3 only (not read with other formats), device fp32 decode scales: value =
+ *              code * scale, of either sign.  The attention's rows that see a key are NaN with
+ *              a k_scale that is infinite or NaN; v_scale multiplies the sum.
  * All of this is device data that the host does not see: what it gets wrong (a page that is
  * none of `pages`, a token past the table, counts that are negative or decrease) reads and
  * writes nothing and is reported by qlin_sync_status as QLIN_ERR_INVALID_ARG; such keys are

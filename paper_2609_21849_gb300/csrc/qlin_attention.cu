@@ -30,8 +30,8 @@ cudaError_t launch_cache_attention(const qlin_cache_t& c, const qlin_cache_atten
   p.table_stride = c.table_stride;
   p.cached = c.cached;
   p.q_start = c.q_start;
-  p.k_scale = c.k_scale;
-  p.v_scale = c.v_scale;
+  p.k_scale = c.format == QLIN_CACHE_E4M3 ? c.k_scale : nullptr;   // (16-bit values have none, whatever is set)
+  p.v_scale = c.format == QLIN_CACHE_E4M3 ? c.v_scale : nullptr;
   p.tokens = a.tokens;
   p.sequences = c.sequences;
   p.pages = c.pages;
