@@ -656,7 +656,7 @@ __global__ void __launch_bounds__(TileCfg<kDC, kCodes>::kThreads, 1)
 
       float m = -INFINITY, l = 0.0f;
       const int mine = halves ? n : (n + 1 - s) / 2;
-      const int tail_from = (int)(g.s.cached / kTile - g.first);   // the first tile with new tokens or none
+      const int tail_from = (int)(first_unseen(g.s) / kTile - g.first);   // the first tile with new tokens or none
       for (int j2 = 0; j2 < 2 * mine; ++j2) {
         const int hf = j2 & 1, tile = halves ? j2 >> 1 : (j2 & ~1) + s;
         const bool tail = tile >= tail_from;
@@ -834,7 +834,7 @@ __global__ void __launch_bounds__(TileCfg<kDC, kCodes>::kThreads, 1)
           if (*(volatile int*)&sh.odd_values != 0 && in) {
             // values that were zeroed, for the rows that see them: infinities and NaN as they are
             const int64_t key_end = min(g.s.keys, (int64_t)(g.first + n) * kTile);
-            for (int64_t key = max((int64_t)g.first * kTile, g.s.cached / kTile * kTile); key < key_end; ++key) {
+            for (int64_t key = max((int64_t)g.first * kTile, first_unseen(g.s) / kTile * kTile); key < key_end; ++key) {
               int index, slot;
               if (!(seen_bits(p, g.s, token, t, key, early) & 1u) ||
                   !cache_place(key, p.page_size, p.table_width, &index, &slot))

@@ -176,6 +176,10 @@ __device__ __forceinline__ Run find_run(const AttnParams& p, Cursor& c, int cta,
   return r;
 }
 
+// The first key that not every row sees: the first new one, or where the table ends before it the one
+// behind its last (counts that pass the table's room).
+__device__ __forceinline__ int64_t first_unseen(const CacheSeq& s) { return min(s.cached, s.keys); }
+
 // Whether new token t of a sequence (number `token` of the call) sees new token i.
 __device__ __forceinline__ bool sees(const AttnParams& p, int64_t token, int t, int64_t i) {
   if (p.mask == nullptr) return i <= t;
