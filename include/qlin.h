@@ -688,7 +688,7 @@ qlin_status qlin_cache_attention(const qlin_cache_t *cache, const qlin_cache_att
 /*
  * Waits for `stream`, then returns and clears the device status word:
  * QLIN_ERR_TIMEOUT if a kernel's bounded wait expired since the last call,
- * QLIN_ERR_INVALID_ARG if a cache call found page tables or counts that are wrong,
+ * else QLIN_ERR_INVALID_ARG if a cache call found page tables or counts that are wrong,
  * QLIN_ERR_CUDA if the stream reports an error, else QLIN_OK.
  */
 qlin_status qlin_sync_status(void *stream);

@@ -81,7 +81,7 @@ __device__ __forceinline__ Place find_place(const AppendParams& p, int64_t token
     r.page = p.table[lo * p.table_stride + index];
     r.ok = r.page >= 0 && r.page < p.pages;
   }
-  if (!r.ok && lane == 0) atomicExch(p.err, kErrInvalid);
+  if (!r.ok && lane == 0) report_invalid(p.err);
   return r;
 }
 

@@ -215,7 +215,7 @@ __global__ void __launch_bounds__(kWarps * 32, (AttnCfg<kKind, kD, kM>::kCtas)) 
   };
   auto issue = [&](int stage, const Place& f) {
     const bool ok = f.in && f.page >= 0 && f.page < p.pages;
-    if (f.in && !ok) atomicExch(p.err, kErrInvalid);   // the keys of a bad page are not seen
+    if (f.in && !ok) report_invalid(p.err);   // the keys of a bad page are not seen
     const unsigned bits = __ballot_sync(0xFFFFFFFFu, ok);
     if (lane == 0) ok_bits[warp][stage] = bits;
     if (bits != 0u) {

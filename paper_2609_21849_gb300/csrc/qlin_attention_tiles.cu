@@ -331,7 +331,7 @@ __global__ void __launch_bounds__(TileCfg<kDC, kCodes>::kThreads, 1)
           const int slot = slot_of(pos);
           const bool bad = d.in && (d.page < 0 || d.page >= p.pages);
           const unsigned bads = __ballot_sync(0xFFFFFFFFu, bad);
-          if (bad) atomicExch(p.err, kErrInvalid);
+          if (bad) report_invalid(p.err);
           const int page = !d.in || bad ? p.pages : d.page;   // past the last: zeros
           const int at = !d.in || bad ? 0 : d.at;
           const int rs = (int)(pos % kRing);

@@ -101,7 +101,7 @@ __device__ __forceinline__ Run find_run(const AttnParams& p, Cursor& c, int cta,
     }
     all += u;
   }
-  if (bad && cta == 0) atomicExch(p.err, kErrInvalid);
+  if (bad && cta == 0) report_invalid(p.err);
   // the sequences up to this thread's, and all
   auto scan = [&](int64_t u) {
 #pragma unroll

@@ -18,6 +18,12 @@ namespace qlin {
 constexpr unsigned kErrInvalid = 1u;
 constexpr unsigned kErrTimeout = 5u;
 
+// Wrong tables or counts, into the status word; a time-out that is there stays.
+__device__ __forceinline__ void report_invalid(unsigned* err) {
+  static_assert(kErrInvalid < kErrTimeout, "the larger one stays");
+  atomicMax(err, kErrInvalid);
+}
+
 // ------------------------------------------------------------------ misc ---
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) {
