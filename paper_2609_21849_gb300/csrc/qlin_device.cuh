@@ -206,17 +206,6 @@ __device__ __forceinline__ void tma_load_4d_pair(void* dst, const CUtensorMap* m
       : "memory");
 }
 
-// The same to the same place in every CTA of the cluster named in `mask`, completing on the
-// barrier at the same offset of each (shared::cta address).
-__device__ __forceinline__ void tma_load_4d_multicast(void* dst, const CUtensorMap* map, uint32_t bar, int32_t c0,
-                                                      int32_t c1, int32_t c2, int32_t c3, uint16_t mask) {
-  asm volatile(
-      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.multicast::cluster"
-      " [%0], [%1, {%3, %4, %5, %6}], [%2], %7;" ::"r"(smem_u32(dst)),
-      "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "h"(mask)
-      : "memory");
-}
-
 // Prefetch of a tiled box into L2 (a hint: no data comes back and nothing
 // waits for it).
 __device__ __forceinline__ void l2_prefetch_4d(const CUtensorMap* map, int32_t c0, int32_t c1) {
@@ -315,15 +304,6 @@ __device__ __forceinline__ void tc_commit(uint64_t* bar) {
   asm volatile(
       "tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(
           smem_u32(bar))
-      : "memory");
-}
-
-// The same, arriving on the barrier at the same offset in each CTA named in `mask`.
-__device__ __forceinline__ void tc_commit_mc(uint64_t* bar, uint16_t mask) {
-  asm volatile(
-      "tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(
-          smem_u32(bar)),
-      "h"(mask)
       : "memory");
 }
 

@@ -3,14 +3,15 @@
 // The scales are any fp32 values, so the tensor cores' own block scales (powers of two) do
 // not serve: a block's products leave tensor memory before the next one's are added, scaled
 // on the way into fp32 registers.  A block is a pipeline stage (128 bytes of K): the MMA
-// issuer writes its four products' sum into one of the tensor-memory buffers in turn, and
-// the epilogue's two warpgroups, which hold the tile's accumulators, take it from there.
-//   shared 128 x 256 tiles, two CTAs of a cluster over the same W: each loads half of its rows
-//          and sends them to both (TMA multicast).  A block is 512 cycles of MMAs, in which 128 x
-//          256 sums leave tensor memory and pass 32768 FMAs (256 cycles, two per instruction).
-//          (As a CTA pair with cta_group::2, every buffer's way to the epilogue and back crossed
-//          the pair: 950 cycles a block.)
-//   single 128 x 128 tiles on one CTA, for fewer rows.
+// issuer writes its four products' sum into one of the tensor-memory buffers in turn, and the
+// epilogue's warpgroups (one per 64 columns), which hold the tile's accumulators, take it from there.
+//   wide   128 x 256 tiles.  A block is 512 cycles of MMAs, in which 128 x 256 sums leave tensor memory
+//          and pass 32768 FMAs (256 cycles, two per instruction); 48 KB reach the SM for it, 750 cycles
+//          at 64 bytes each, which is what it takes: 4608 x 12288 x 3072 160 us.  (With W's half sent
+//          by each CTA of two to both it took 160.4: what a copy sent to two CTAs saves is reads of L2, not
+//          what comes into an SM.  As a CTA pair with cta_group::2, every buffer's way to the epilogue
+//          and back crossed the pair: 950 cycles a block.)
+//   single 128 x 128 tiles, for fewer rows, also with K shared by a cluster.
 // Roles: warp 0 loads (TMA), warp 1 issues the MMAs, warp 2 multiplies the scales of a block's rows
 // and columns into shared memory (loads of them by the epilogue's own warps cost 20 to 40 of 180
 // us), the warps from 4 on hold the accumulators, 64 columns of a row each.
@@ -27,9 +28,8 @@ constexpr int kSteps = 4;                   // MMAs of 32 elements of a block
 constexpr int kRawSlots = 8;   // blocks whose scales are loaded ahead
 constexpr int kRoleWarps = 4, kCols = 64;   // columns of an epilogue thread: inside one 128-row block of W
 
-template <int kBN, bool kShare>
+template <int kBN>
 struct BlockCfg {
-  static constexpr int kCM = kShare ? 2 : 1;     // CTAs of a cluster
   static constexpr int kEpiWarps = kBN / kCols * 4;
   static constexpr int kThreads = (kRoleWarps + kEpiWarps) * 32;
   static constexpr int kSplit = 2;               // row boxes per load of 128 rows, whose copies overlap
@@ -116,12 +116,11 @@ __device__ __forceinline__ void store32(uint16_t* p, const uint32_t* v, bool wid
   }
 }
 
-template <int kBN, bool kShare, bool kSplitK>
-__global__ void __launch_bounds__(BlockCfg<kBN, kShare>::kThreads, 1)
+template <int kBN, bool kSplitK>
+__global__ void __launch_bounds__(BlockCfg<kBN>::kThreads, 1)
     gemm_block_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ CUtensorMap tmap_b,
                       const BlockParams p) {
-  using C = BlockCfg<kBN, kShare>;
-  constexpr int kCM = C::kCM;
+  using C = BlockCfg<kBN>;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem =
       reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
@@ -137,12 +136,11 @@ __global__ void __launch_bounds__(BlockCfg<kBN, kShare>::kThreads, 1)
 
   const int warp = __shfl_sync(0xFFFFFFFFu, (int)(threadIdx.x >> 5), 0);
   const int lane = threadIdx.x & 31;
-  const int rank = kShare ? __shfl_sync(0xFFFFFFFFu, (int)cluster_ctarank(), 0) : 0;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < C::kStages; ++s) {
       mbar_init(&full[s], 1);
-      mbar_init(&empty[s], kCM);   // both CTAs' MMAs have read what was sent to both
+      mbar_init(&empty[s], 1);
     }
     for (int a = 0; a < C::kBuffers; ++a) {
       mbar_init(&tmem_full[a], 2);   // the block's products, and its scales
@@ -155,21 +153,19 @@ __global__ void __launch_bounds__(BlockCfg<kBN, kShare>::kThreads, 1)
   if (warp == 0 && lane < 2) prefetch_tmap(lane == 0 ? &tmap_a : &tmap_b);
   if (warp == 1) tmem_alloc(tmem_slot, 512);
   tc_fence_before();
-  if (kShare || kSplitK)
-    cluster_sync();   // the peers' barriers exist before any copy completes on them
+  if (kSplitK)
+    cluster_sync();
   else
     __syncthreads();
   tc_fence_after();
   const uint32_t tmem_base = __shfl_sync(0xFFFFFFFFu, *tmem_slot, 0);
   const WaitCtl ctl{abort_flag, p.err, p.timeout_ns};
-  static_assert(!kSplitK || !kShare, "a cluster shares a tile's K, or W");
   const int tiles_m = (int)((p.M + kBM - 1) / kBM), tiles_n = (int)((p.N + kBN - 1) / kBN);
-  const int groups_m = (tiles_m + kCM - 1) / kCM;
-  const int num_ctiles = groups_m * tiles_n;
+  const int num_tiles = tiles_m * tiles_n;
   // kSplitK: the CTAs of a cluster take a tile's blocks of K in equal runs (split <= blocks)
   const int splits = kSplitK ? p.split : 1;
   const int krank = kSplitK ? __shfl_sync(0xFFFFFFFFu, (int)cluster_ctarank(), 0) : 0;
-  const int cid = (int)blockIdx.x / (kCM * splits), ncl = (int)gridDim.x / (kCM * splits);
+  const int cid = (int)blockIdx.x / splits, ncl = (int)gridDim.x / splits;
   const int all_kb = (int)((p.K + kRowBytes - 1) / kRowBytes);
   const int kb0 = krank * all_kb / splits, num_kb = (krank + 1) * all_kb / splits - kb0;
   grid_dep_wait();
@@ -178,33 +174,27 @@ __global__ void __launch_bounds__(BlockCfg<kBN, kShare>::kThreads, 1)
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kRoleRegs));
     if (warp == 0) {
       // ---- TMA producer ----
-      // (a W load of a cluster: this CTA's half of the rows, to the same place in both CTAs)
-      constexpr int kARows = kBM / C::kSplit, kWRows = kBN / kCM / C::kSplit;
+      constexpr int kARows = kBM / C::kSplit, kWRows = kBN / C::kSplit;
       int stage = 0, issued = 0;
       uint32_t phase = 0;
       bool ok = true;
-      for (int ct = cid; ct < num_ctiles && ok; ct += ncl) {
-        const int a_row = (ct % groups_m * kCM + rank) * kBM;
-        const int w_row = ct / groups_m * kBN + rank * (kBN / kCM);
-        if (ct + ncl >= num_ctiles) grid_dep_launch();
+      for (int ct = cid; ct < num_tiles && ok; ct += ncl) {
+        const int a_row = ct % tiles_m * kBM, w_row = ct / tiles_m * kBN;
+        if (ct + ncl >= num_tiles) grid_dep_launch();
         for (int kb = 0; kb < num_kb; ++kb) {
           if (!mbar_wait_warp(&empty[stage], phase ^ 1u, ctl)) {
             ok = false;
             break;
           }
           uint8_t* const sA = smem + stage * C::kStageBytes;
-          uint8_t* const sW = sA + C::kABytes + rank * (C::kBBytes / kCM);
+          uint8_t* const sW = sA + C::kABytes;
           const uint32_t bar = smem_u32(&full[stage]);
           if (elect_one()) {
             mbar_arrive_expect_tx(&full[stage], C::kStageBytes);
 #pragma unroll
             for (int b = 0; b < C::kSplit; ++b) {
               tma_load_4d(sA + b * kARows * kRowBytes, &tmap_a, bar, (kb0 + kb) * kRowBytes, a_row + b * kARows, 0, 0);
-              if (kShare)
-                tma_load_4d_multicast(sW + b * kWRows * kRowBytes, &tmap_b, bar, (kb0 + kb) * kRowBytes, w_row + b * kWRows, 0, 0,
-                                      (uint16_t)3);
-              else
-                tma_load_4d(sW + b * kWRows * kRowBytes, &tmap_b, bar, (kb0 + kb) * kRowBytes, w_row + b * kWRows, 0, 0);
+              tma_load_4d(sW + b * kWRows * kRowBytes, &tmap_b, bar, (kb0 + kb) * kRowBytes, w_row + b * kWRows, 0, 0);
             }
           }
           ++issued;
@@ -231,7 +221,7 @@ __global__ void __launch_bounds__(BlockCfg<kBN, kShare>::kThreads, 1)
       int stage = 0, buf = 0;
       uint32_t phase = 0, buf_phase = 0;
       bool ok = true;
-      for (int ct = cid; ct < num_ctiles && ok; ct += ncl) {
+      for (int ct = cid; ct < num_tiles && ok; ct += ncl) {
         for (int kb = 0; kb < num_kb; ++kb) {
           if (!mbar_wait_warp(&tmem_empty[buf], buf_phase ^ 1u, ctl) || !mbar_wait_warp(&full[stage], phase, ctl)) {
             ok = false;
@@ -248,10 +238,7 @@ __global__ void __launch_bounds__(BlockCfg<kBN, kShare>::kThreads, 1)
               // (32 bytes further per step)
               if (j < steps) mma_fp8(d, adesc + 2 * j, bdesc + 2 * j, idesc, j > 0 ? 1u : 0u);
             }
-            if (kShare)
-              tc_commit_mc(&empty[stage], (uint16_t)3);
-            else
-              tc_commit(&empty[stage]);
+            tc_commit(&empty[stage]);
             tc_commit(&tmem_full[buf]);
           }
           if (++stage == C::kStages) {
@@ -288,12 +275,12 @@ __global__ void __launch_bounds__(BlockCfg<kBN, kShare>::kThreads, 1)
       int next_ct = cid, next_kb = 0, next_slot = 0;
       const float *next_a[4], *next_w = nullptr;
       auto fetch = [&] {
-        if (next_ct < num_ctiles) {
+        if (next_ct < num_tiles) {
           if (next_kb == 0) {
-            const int64_t row0 = (int64_t)(next_ct % groups_m * kCM + rank) * kBM + lane;
+            const int64_t row0 = (int64_t)(next_ct % tiles_m) * kBM + lane;
 #pragma unroll
             for (int i = 0; i < 4; ++i) next_a[i] = p.sa + kb0 * p.M + min(row0 + 32 * i, p.M - 1);
-            next_w = p.sw + kb0 * w_blocks + min((int64_t)(next_ct / groups_m) * C::kWBlocks + min(lane, C::kWBlocks - 1), w_blocks - 1);
+            next_w = p.sw + kb0 * w_blocks + min((int64_t)(next_ct / tiles_m) * C::kWBlocks + min(lane, C::kWBlocks - 1), w_blocks - 1);
           }
           const uint32_t dst = raw + (uint32_t)(next_slot * C::kRawSlot * 4);
 #pragma unroll
@@ -315,7 +302,7 @@ __global__ void __launch_bounds__(BlockCfg<kBN, kShare>::kThreads, 1)
       int buf = 0, slot = 0;
       uint32_t buf_phase = 0;
       bool ok = true;
-      for (int ct = cid; ct < num_ctiles && ok; ct += ncl) {
+      for (int ct = cid; ct < num_tiles && ok; ct += ncl) {
         for (int kb = 0; kb < num_kb; ++kb) {
           asm volatile("cp.async.wait_group %0;" ::"n"(kRawSlots - 2) : "memory");
           __syncwarp();   // (the others' loads too; and all are done with the slot that the next fills)
@@ -373,8 +360,8 @@ __global__ void __launch_bounds__(BlockCfg<kBN, kShare>::kThreads, 1)
       cluster_sync();
       for (int i = threadIdx.x - kRoleWarps * 32; i < kBM * width / 16; i += C::kEpiWarps * 32) {
         const int r = i % kBM, group = i / kBM;
-        const int64_t row = (int64_t)(ct % groups_m) * kBM + r;
-        const int64_t n = (int64_t)(ct / groups_m) * kBN + krank * width + 16 * group;
+        const int64_t row = (int64_t)(ct % tiles_m) * kBM + r;
+        const int64_t n = (int64_t)(ct / tiles_m) * kBN + krank * width + 16 * group;
         if (row >= p.M || n >= p.N) continue;
         float2 v[8];
 #pragma unroll
@@ -408,9 +395,9 @@ __global__ void __launch_bounds__(BlockCfg<kBN, kShare>::kThreads, 1)
     int buf = 0;
     uint32_t buf_phase = 0;
     bool ok = true;
-    for (int ct = cid; ct < num_ctiles && ok; ct += ncl) {
-      const int64_t row = (int64_t)(ct % groups_m * kCM + rank) * kBM + quarter * 32 + lane;
-      const int64_t col0 = (int64_t)(ct / groups_m) * kBN + part * kCols;
+    for (int ct = cid; ct < num_tiles && ok; ct += ncl) {
+      const int64_t row = (int64_t)(ct % tiles_m) * kBM + quarter * 32 + lane;
+      const int64_t col0 = (int64_t)(ct / tiles_m) * kBN + part * kCols;
       const bool row_in = row < p.M;
       if (p.bias != nullptr) {   // read at the tile's end
         __syncwarp();            // (the tile before has read its own)
@@ -519,10 +506,9 @@ __global__ void __launch_bounds__(BlockCfg<kBN, kShare>::kThreads, 1)
       cluster_sync();
     }
   }
-  // No CTA of a cluster may exit while the peer can still copy into it or arrive on its barriers.
   __syncwarp();
   tc_fence_before();
-  if (kShare || kSplitK)
+  if (kSplitK)
     cluster_sync_relaxed();
   else
     __syncthreads();
@@ -532,13 +518,12 @@ __global__ void __launch_bounds__(BlockCfg<kBN, kShare>::kThreads, 1)
   }
 }
 
-template <int kBN, bool kShare, bool kSplitK = false>
+template <int kBN, bool kSplitK = false>
 cudaError_t launch_cfg(const GemmArgs& a, cudaStream_t s, Device dev, unsigned* err, uint64_t timeout_ns) {
-  using C = BlockCfg<kBN, kShare>;
-  constexpr int kCM = C::kCM;
+  using C = BlockCfg<kBN>;
   CUtensorMap ta, tb;
   if (encode_tensor_map_codes(&ta, a.a_codes, (uint64_t)a.K, (uint64_t)a.M, kBM / C::kSplit) != CUDA_SUCCESS ||
-      encode_tensor_map_codes(&tb, a.w_codes, (uint64_t)a.K, (uint64_t)a.N, kBN / kCM / C::kSplit) != CUDA_SUCCESS)
+      encode_tensor_map_codes(&tb, a.w_codes, (uint64_t)a.K, (uint64_t)a.N, kBN / C::kSplit) != CUDA_SUCCESS)
     return cudaErrorInvalidValue;
   BlockParams p{};
   p.sa = a.sdec_a;
@@ -556,44 +541,27 @@ cudaError_t launch_cfg(const GemmArgs& a, cudaStream_t s, Device dev, unsigned* 
   p.split = a.split;
   p.err = err;
   p.timeout_ns = timeout_ns;
-  auto kern = gemm_block_kernel<kBN, kShare, kSplitK>;
+  auto kern = gemm_block_kernel<kBN, kSplitK>;
+  static PerDevice<cudaError_t> per_device;
+  const cudaError_t e = per_device.get(
+      dev.index, [&] { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem); });
+  if (e != cudaSuccess) return e;
+  const int64_t tiles = ((a.M + kBM - 1) / kBM) * ((a.N + kBN - 1) / kBN);
+  if (tiles > INT32_MAX / 2) return cudaErrorInvalidValue;
   cudaLaunchConfig_t cfg{};
   cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = kCM;
-  attr[0].val.clusterDim.y = 1;
-  attr[0].val.clusterDim.z = 1;
-  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;   // kSplitK: a cluster per tile
+  attr[1].val.clusterDim.x = kSplitK ? (unsigned)a.split : 1u;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
+  cfg.gridDim = dim3((unsigned)(kSplitK ? tiles * a.split : std::min<int64_t>(tiles, dev.num_sms)), 1, 1);
   cfg.blockDim = dim3(C::kThreads, 1, 1);
   cfg.dynamicSmemBytes = C::kSmem;
   cfg.stream = s;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  struct Setup {
-    cudaError_t err;
-    int max_clusters;
-  };
-  static PerDevice<Setup> per_device;
-  const Setup& setup = per_device.get(dev.index, [&] {
-    Setup t{cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem), 0};
-    if (t.err != cudaSuccess) return t;
-    cfg.gridDim = dim3((unsigned)(dev.num_sms / kCM * kCM), 1, 1);
-    t.err = cudaOccupancyMaxActiveClusters(&t.max_clusters, kern, &cfg);
-    if (t.err == cudaSuccess && t.max_clusters < 1) t.err = cudaErrorInvalidConfiguration;
-    return t;
-  });
-  if (setup.err != cudaSuccess) return setup.err;
-  const int64_t tiles_m = (a.M + kBM - 1) / kBM;
-  const int64_t ctiles = ((tiles_m + kCM - 1) / kCM) * ((a.N + kBN - 1) / kBN);
-  if (ctiles > INT32_MAX / 2) return cudaErrorInvalidValue;
-  const int clusters = (int)std::min<int64_t>(ctiles, std::min(setup.max_clusters, dev.num_sms / kCM));
-  cfg.gridDim = dim3((unsigned)(clusters * kCM), 1, 1);
-  if (kSplitK) {   // a cluster per tile
-    cfg.gridDim.x = (unsigned)(ctiles * a.split);
-    attr[0].val.clusterDim.x = (unsigned)a.split;
-  }
-  cfg.numAttrs = 2;
+  cfg.numAttrs = kSplitK ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, kern, ta, tb, p);
 }
 
@@ -601,14 +569,14 @@ cudaError_t launch_cfg(const GemmArgs& a, cudaStream_t s, Device dev, unsigned* 
 
 cudaError_t launch_gemm_block(const GemmArgs& a, cudaStream_t s, Device dev, unsigned* err, uint64_t timeout_ns) {
   switch (choose_block_tile(a.M, a.N, a.K, dev.num_sms)) {
-    case BlockTile::kShared:
-      return launch_cfg<256, true>(a, s, dev, err, timeout_ns);
+    case BlockTile::kWide:
+      return launch_cfg<256>(a, s, dev, err, timeout_ns);
     case BlockTile::kSingle:
-      return launch_cfg<128, false>(a, s, dev, err, timeout_ns);
+      return launch_cfg<128>(a, s, dev, err, timeout_ns);
     default: {
       GemmArgs b = a;
       b.split = choose_block_split(a.M, a.N, a.K, dev.num_sms);
-      return launch_cfg<128, false, true>(b, s, dev, err, timeout_ns);
+      return launch_cfg<128, true>(b, s, dev, err, timeout_ns);
     }
   }
 }

@@ -160,9 +160,8 @@ inline bool split_over_few(GemmKind kind, int64_t M, int64_t N, int64_t K, int n
          choose_split_k(kind, M, N, K, num_sms) > 1;
 }
 
-// The block-scaled FP8 linear's tiles: 128 x 256 in clusters of two over the same W, 128 x 128,
-// or those with K shared by a cluster.
-enum class BlockTile { kShared, kSingle, kSplit };
+// The block-scaled FP8 linear's tiles: 128 x 256, 128 x 128, or those with K shared by a cluster.
+enum class BlockTile { kWide, kSingle, kSplit };
 
 // CTAs of a cluster that share a tile's K.  Sending and joining the sums costs about 5 us, a
 // block 0.36 (M x N x K in us, one CTA and split: 600 x 512 x 3072 13.0, 12.1 in four; x 12288 38.5,
@@ -177,15 +176,16 @@ inline int choose_block_split(int64_t M, int64_t N, int64_t K, int num_sms) {
 }
 
 // Between the unsplit tiles the times of their waves decide, fitted to M 24-4608, N 64-12288, K
-// 256-12288 (in us, 128 x 256 and 128 x 128: 1333 x 2112 x 256 9.0, 8.1; x 1088 12.4, 13.5; 300 x
-// 12288 x 1088 21.6, 13.7; 4608 x 12288 x 3072 198, 248).
+// 256-12288 (in us, 128 x 256 and 128 x 128: 1333 x 2112 x 256 8.8, 7.5; x 1088 12.2, 12.8; 4608 x 12288 x
+// 3072 199, 227).  An odd last row tile of the wide ones counts as two: where a wave has room for it
+// (three row tiles: 300 x 12288 x 1088 12.4, 12.9, x 3072 19.0, 22.6) this gives time away.
 inline BlockTile choose_block_tile(int64_t M, int64_t N, int64_t K, int num_sms) {
   if (choose_block_split(M, N, K, num_sms) > 1) return BlockTile::kSplit;
   const int64_t blocks = (K + 127) / 128, tiles_m = (M + kTileM - 1) / kTileM;
-  const TileCost single{1.9, 2.6, 0.36}, shared{1.9, 6.0, 0.43};
-  return shared.us((tiles_m + 1) / 2 * ((N + 255) / 256), num_sms / 2, blocks, 0.0) <
+  const TileCost single{1.9, 2.6, 0.36}, wide{1.9, 6.0, 0.43};
+  return wide.us((tiles_m + 1) / 2 * ((N + 255) / 256), num_sms / 2, blocks, 0.0) <
                  single.us(tiles_m * ((N + 127) / 128), num_sms, blocks, 0.0)
-             ? BlockTile::kShared
+             ? BlockTile::kWide
              : BlockTile::kSingle;
 }
 
