@@ -649,7 +649,9 @@ qlin_status qlin_cache_append(const qlin_cache_t *cache, const qlin_cache_append
  * sees new token i, itself among them; bits past the words are 0.  mask NULL: those up to
  * itself.  A row that sees nothing gives zeros and lse -infinity.  NaN and infinities in
  * keys and values that a row does not see do not reach it.  Scores, running maximum and sum
- * and the products' sums in fp32; probabilities are rounded to 16 bits for the product with v.
+ * and the products' sums in fp32; probabilities are rounded to the 16 bits of the cache's type
+ * (E4M3: fp16) for the product with v, those in fp16 after a factor that keeps weights from 2^-32
+ * of the row's largest on.
  *  q, out: 16-bit (dtype) [tokens, q_heads, head_dim], head_dim contiguous, strides in
  *          elements, multiples of 8, 16-byte aligned; out may be q with the same strides, else
  *          the two must not overlap.  Rows of tokens of no sequence are left as they were.

@@ -18,6 +18,8 @@
 // below 2^-25 of it), and P is fp16.
 //   P is rounded to the values' 16-bit type for the second product, the row's sum is taken
 // before that rounding: errors of half a step of P, independent from key to key, average out.
+// fp16 has few exponents below 1: there the kept maximum is 2^15 below the row's, and P up to
+// 2^15, so that weights down to 2^-40 of the largest one count (bf16 has those of fp32).
 //   Measured: 64 tokens over 64 caches of 2048-8192 keys in E4M3, 8 KV heads of 128, 8 query heads
 // each, 142 us, 72% of the copy rate (half of an MMA's rows are empty, and the conversion of codes
 // takes more issue slots than the products); one token over 1000 keys 9.8: a launch, six tiles' worth
@@ -31,6 +33,7 @@ namespace qlin {
 namespace {
 
 constexpr int kWarps = 4;
+constexpr float kRaise = 15.0f;   // powers of two above 1 of an fp16 P's maximum
 
 __device__ __forceinline__ void ldmatrix_trans(uint32_t a, uint32_t (&r)[4]) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
@@ -366,7 +369,9 @@ __global__ void __launch_bounds__(kWarps * 32, (AttnCfg<kKind, kD, kM>::kCtas)) 
         for (int j = 1; j < kNT; ++j) mx = fmaxf(mx, fmaxf(s[i][j][2 * r], s[i][j][2 * r + 1]));
         mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 1));
         mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 2));
-        const float now = fmaxf(m[i][r], mx * mult[i][r]);
+        // (fp16: rounded up, so that no P passes 2^15)
+        const float top = kF16 ? __fadd_ru(__fmul_ru(mx, mult[i][r]), -kRaise) : mx * mult[i][r];
+        const float now = fmaxf(m[i][r], top);
         const float base = now == -INFINITY ? 0.0f : now;   // (nothing seen yet)
         keep[i][r] = exp2_fast(m[i][r] - base);
         moved |= now != m[i][r];

@@ -10,7 +10,9 @@
 //   P = 2^(S - m) a thread per row, 64 scores in registers at a time, P as 16-bit over S's columns
 //   O += P V      A from tensor memory, V as it lies (keys x elements: an MN-major B)
 // The running maximum moves only when it rises by more than 2^8, so O is rarely rescaled; P
-// stays below 2^8 and the sums in fp32 (both fine in 16 bits: a P's rounding is relative).
+// stays below 2^8 and the sums in fp32 (both fine in bf16: a P's rounding is relative).  fp16 has
+// few exponents below 1: there the kept maximum is 2^7 below a row's, and P up to 2^15, so that
+// weights down to 2^-32 of the largest one count.
 //   Per tile of 256 rows and 128 keys of 128: 2048 cycles of MMAs (2560 where 128 bytes of shared
 // memory a cycle bring a half's scores Q's rows and 64 keys), 1024 of exponentials (four cycles a warp
 // measured), 64 KB of keys and values, about 2850 cycles of an SM's share of HBM.
@@ -42,6 +44,7 @@ namespace {
 
 constexpr int kSoftWarp0 = 4, kConvertWarps = 4;
 constexpr float kSlack = 8.0f;   // powers of two that a score may exceed the kept maximum by
+constexpr float kRaise = 7.0f;   // powers of two above 1 of an fp16 P's maximum, without these
 constexpr int kBadRing = 16;     // tiles whose bad pages are remembered
 
 // A run's pieces: consecutive tiles of one item.
@@ -687,10 +690,11 @@ __global__ void __launch_bounds__(TileCfg<kDC, kCodes>::kThreads, 1)
           for (int k = 0; k < 8; ++k)
             top[k] = max_nan(top[k], __uint_as_float(v[(i + k) >> 5][(i + k) & 31]),
                              i + 8 < kHalf ? __uint_as_float(v[(i + 8 + k) >> 5][(i + 8 + k) & 31]) : top[k]);
-        const float cand = max_nan(max_nan(top[0], top[1], top[2]), max_nan(top[3], top[4], top[5]),
-                                   max_nan(top[6], top[7], top[7])) *
-                           mult;
-        const bool rise = cand > m + kSlack || (m == -INFINITY && cand > m);
+        const float most = max_nan(max_nan(top[0], top[1], top[2]), max_nan(top[3], top[4], top[5]),
+                                   max_nan(top[6], top[7], top[7]));
+        // (fp16: the candidate rounded up and the limit down, so that no P passes 2^15)
+        const float cand = kF16 ? __fadd_ru(__fmul_ru(most, mult), -kRaise) : most * mult;
+        const bool rise = cand > (kF16 ? __fadd_rd(m, kSlack) : m + kSlack) || (m == -INFINITY && cand > m);
         if (__any_sync(0xFFFFFFFFu, rise)) {
           const float f = rise ? exp2_fast(m - cand) : 1.0f;
           l *= f;

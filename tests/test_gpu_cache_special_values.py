@@ -8,7 +8,7 @@ import pytest
 torch = pytest.importorskip("torch")
 
 from paper_2609_21849_gb300 import qlin
-from test_gpu_cache import FORMATS, _check, _fill, _gen, _make, _slots
+from test_gpu_cache import FORMATS, UNIT, _check, _fill, _gen, _make, _slots
 
 pytestmark = pytest.mark.gpu
 
@@ -22,6 +22,11 @@ def _call(c, q, scale=0.125):
     out = qlin.qlin_cache_attention(c, q, scale, lse=lse)
     assert qlin.qlin_sync_status() == 0
     return out, lse
+
+
+def _largest_value(c, where):
+    v = c.v[where].double().nan_to_num(0)
+    return v.abs().max().item() * (1.0 if c.v_scale is None else c.v_scale.item())
 
 
 def _setup(T, G, have, fmt, dtype):
@@ -68,7 +73,12 @@ def test_a_nan_among_keys_of_little_weight(T, G, have, fmt, dtype):
         if t is c.v:
             assert out[:, G:, 3].isnan().all() and torch.equal(lse, good_lse)
             others = [d for d in range(D) if d != 3]
-            assert torch.equal(out[..., others], good[..., others])
+            off = (out.double() - good.double())[..., others].abs()
+            # Of a tile that holds new tokens the few-row kernel adds the keys one by one, with P as it is in
+            # fp32 where the product takes it in 16 bits: half a step of P times |v|, and the sums' own 2^-20.
+            # Each result is rounded once.
+            least = 0.0 if have >= 1000 else (2.0**-8 if fmt == "bf16" else 2.0**-11) + 2.0**-20 + 2 * UNIT[dtype]
+            assert off.max() <= least * _largest_value(c, where)
         else:
             assert out[:, G:].isnan().all() and lse[:, G:].isnan().all()
         t[page, slot, 1] = old
