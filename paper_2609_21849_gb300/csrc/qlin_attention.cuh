@@ -134,7 +134,8 @@ __device__ __forceinline__ void join_few(const AttnParams& p, const Unfinished& 
 #pragma unroll
       for (int k = 0; k < kJoin; ++k) {
         const float w = exp2_fast(ml[k].x - base);
-        if (q0 + k < parts) {   // (whatever its weight: a part of NaN scores has a weight of 0 and a NaN sum)
+        // (whatever its weight: a part of NaN scores has a weight of 0 and a NaN sum)
+        if (known_here(q0 + k < parts)) {
           l = fmaf(ml[k].y, w, l);
           o = make_float4(fmaf(v[k].x, w, o.x), fmaf(v[k].y, w, o.y), fmaf(v[k].z, w, o.z), fmaf(v[k].w, w, o.w));
         }

@@ -205,6 +205,15 @@ __device__ __forceinline__ float log_sum(float m, float l) {   // m in powers of
   return l > 0.0f || l != l ? fmaf(m, 0.693147181f, logf(l)) : -INFINITY;
 }
 
+// x as a condition that the compiler does not know before this place, so that it guards a few
+// instructions: one that it knows before the loads became a branch for each part of a join (one token
+// over 1000 keys 10.9 us, so 9.8; 64 decodes 144.2, 141.2).
+__device__ __forceinline__ bool known_here(bool x) {
+  uint32_t r = x ? 1u : 0u;
+  asm volatile("" : "+r"(r));
+  return r != 0u;
+}
+
 // An item's parts in the workspace: CTA first's is its second, all others' their first.
 template <int kRows>
 __device__ __forceinline__ int64_t part_row(int cta, int first, int row) {
