@@ -32,7 +32,7 @@ namespace qlin {
 
 namespace {
 
-constexpr int kWarps = 4;
+constexpr int kWarps = kFewWarps;
 constexpr float kRaise = 15.0f;   // powers of two above 1 of an fp16 P's maximum
 
 __device__ __forceinline__ void ldmatrix_trans(uint32_t a, uint32_t (&r)[4]) {
@@ -69,7 +69,7 @@ template <CacheKind kKind, int kD, int kM>
 struct AttnCfg {
   static constexpr int kEs = kKind == CacheKind::kE4m3 ? 1 : 2;
   static constexpr int kRows = 16 * kM;
-  static constexpr int kKeys = kEs == 1 ? 32 : 16 * kM;    // of a warp and tile
+  static constexpr int kKeys = few_warp_keys(kEs, kRows);   // of a warp and tile
   static constexpr int kTile = kWarps * kKeys;
   static constexpr int kRow = kD * kEs;                    // bytes
   static constexpr int kPieces = kRow / 16;
@@ -632,11 +632,7 @@ __global__ void __launch_bounds__(kWarps * 32, (AttnCfg<kKind, kD, kM>::kCtas)) 
     if (all) *count = 0u;   // as it was before the call
     return all;
   };
-  // a group: as many parts as a CTA joins in about the time that another level takes
-  auto group_of = [&](const Unfinished& u) {
-    const int per4 = u.rows * p.head_dim / (4 * kThreads);
-    return per4 <= 1 ? 64 : per4 <= 4 ? 32 : 16;
-  };
+  auto group_of = [&](const Unfinished& u) { return few_join_group(u.rows, p.head_dim); };
   __syncthreads();
   if ((int)threadIdx.x < num_unfinished) {   // (both at a time)
     const Unfinished u = unfinished[threadIdx.x];
@@ -682,10 +678,8 @@ cudaError_t launch_attn(AttnParams p, cudaStream_t s, Device dev) {
   const int ctas = (int)std::min<int64_t>((int64_t)setup.ctas * dev.num_sms, most);
   p.part_ml = reinterpret_cast<float2*>(reinterpret_cast<uint8_t*>(p.counts) + kCountBytes);
   p.part = reinterpret_cast<float*>(p.part_ml + (int64_t)2 * C::kRows * ctas);
-  p.least = std::max(1, 128 / C::kTile);
-  // (in us without it, with 1, 2, 3 and 4: 64 sequences of 2048-8192 E4M3 keys, 8 heads of 128, 144, 141,
-  // 139, 139, 140; of 512-2048 59, 55, 53, 53, 55; 8 of 512-2048, without and with 2, 20.0, 15.5)
-  p.item_cost = 2;
+  p.least = few_least(C::kTile);
+  p.item_cost = kFewItemCost;
   return launch_pdl(attn_kernel<kKind, kD, kM>, dim3((unsigned)ctas), kWarps * 32, C::kSmem, s, p);
 }
 

@@ -79,4 +79,21 @@ QLIN_HD int64_t split_owner(const Split& s, int64_t t) {
   return t < longer ? div_small(t, s.per + 1) : s.rest + div_small(t - longer, s.per);
 }
 
+// The few-row attention's numbers that its split and its joins follow from.
+constexpr int kFewWarps = 4;
+// keys of a warp and tile (rows: 16 or 32)
+QLIN_HD constexpr int few_warp_keys(int element_bytes, int rows) { return element_bytes == 1 ? 32 : rows; }
+// tiles that a CTA should have
+QLIN_HD constexpr int few_least(int tile) { return 128 / tile < 1 ? 1 : 128 / tile; }
+// tiles that an item's begin and end take as long as (in us without it, with 1, 2, 3 and 4: 64 sequences
+// of 2048-8192 E4M3 keys, 8 heads of 128, 144, 141, 139, 139, 140; of 512-2048 59, 55, 53, 53, 55; 8 of
+// 512-2048, without and with 2, 20.0, 15.5)
+constexpr int kFewItemCost = 2;
+// CTAs whose parts of an item are joined by the last of them: as many as a CTA joins in about the time
+// that another level takes
+QLIN_HD int few_join_group(int rows, int head_dim) {
+  const int per4 = rows * head_dim / (4 * 32 * kFewWarps);
+  return per4 <= 1 ? 64 : per4 <= 4 ? 32 : 16;
+}
+
 }  // namespace qlin
