@@ -97,15 +97,17 @@ class Block:
     def attend(self, cache: qlin.PagedCache, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
                mask: torch.Tensor | None = None, stream=None) -> torch.Tensor:
         """Attention of project()'s q over the cache's keys and the new ones, which are appended
-        first; [M, hidden].  mask as in qlin_cache_attention.  The rows behind the cache's last
-        sequence stay as they were (zeros at first)."""
+        first; [M, hidden].  mask as in qlin_cache_attention.  The rows of no sequence (a padded
+        batch) are zeros: what an earlier step left there would take part in the scale that
+        finish() gives all rows."""
         if self.attended is None:
             if torch.cuda.is_current_stream_capturing():
                 raise RuntimeError("attend: its buffers are made in the first call, which must not be captured")
             self.attention_workspace = qlin._empty(qlin.qlin_cache_attention_workspace_size(), torch.uint8, q.device,
                                                    stream, torch.zeros)
-            self.attended = qlin._empty((self.M, self.hidden), torch.bfloat16, q.device, stream, torch.zeros)
+            self.attended = qlin._empty((self.M, self.hidden), torch.bfloat16, q.device, stream)
         H, D = self.heads, self.hidden // self.heads
+        qlin._zero(self.attended, stream)
         qlin.qlin_cache_append(cache, k, v, stream=stream)   # (k has its positions)
         qlin.qlin_cache_attention(cache, q, D ** -0.5, mask, self.attended.view(self.M, H, D), None,
                                   self.attention_workspace, stream)

@@ -528,6 +528,16 @@ def _empty(shape, dtype, device, stream, make=torch.empty):
         return make(shape, dtype=dtype, device=device)
 
 
+def _zero(t, stream):
+    """Zeros in t, in the order of `stream`."""
+    if stream is None:
+        return t.zero_()
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream, device=t.device)
+    with torch.cuda.stream(stream):
+        return t.zero_()
+
+
 # The checks below read each attribute of a tensor once and compare device indices, not
 # device objects: a call's host time is a few microseconds.
 
