@@ -603,8 +603,8 @@ typedef struct {
  * S_enc), S_enc = 1 / scale (FLT_MAX if that overflows).
  *  k, v:  16-bit (dtype) [tokens, heads, head_dim], head_dim contiguous, any strides of
  *         tokens and heads in elements.  q, q_out: [tokens, q_heads, head_dim] likewise (in
- *         q_out, head_dim or more, also negative); q_out may be q itself with the same
- *         strides, else the two must not overlap.  q NULL: none.
+ *         q_out, head_dim or more, also negative, and no row over another); q_out may be q
+ *         itself with the same strides, else the two must not overlap.  q NULL: none.
  *         2-byte aligned; 16-byte aligned rows and pairs in fours take wide accesses.
  *  positions, turns, magnitude, rot_dim, axes, axis_pairs, layout: as in qlin_rope.
  *         positions NULL: a token's number in its sequence (one axis).  turns NULL: nothing
@@ -653,8 +653,9 @@ qlin_status qlin_cache_append(const qlin_cache_t *cache, const qlin_cache_append
  * (E4M3: fp16) for the product with v, those in fp16 after a factor that keeps weights from 2^-32
  * of the row's largest on.
  *  q, out: 16-bit (dtype) [tokens, q_heads, head_dim], head_dim contiguous, strides in
- *          elements, multiples of 8, 16-byte aligned; out may be q with the same strides, else
- *          the two must not overlap.  Rows of tokens of no sequence are left as they were.
+ *          elements, multiples of 8, 16-byte aligned, no row of out over another; out may be
+ *          q with the same strides, else the two must not overlap.  Rows of tokens of no
+ *          sequence are left as they were.
  *  lse:    fp32 [tokens, q_heads] or NULL.
  *  mask:   uint64 [tokens, mask_words], rows mask_stride words apart, or NULL.
  *  scale:  normal, > 0 and < 2^127.

@@ -5,6 +5,7 @@
 #include <cstdio>
 #include <cstring>
 #include <mutex>
+#include <utility>
 
 #include "qlin_attention.h"
 #include "qlin_internal.h"
@@ -619,6 +620,29 @@ qlin_status qlin_quantize_fp8_block(const void* x, int32_t dtype, int64_t x_stri
   return QLIN_OK;
 }
 
+// Whether n0 x n1 rows of `width` elements, s0 and s1 elements apart, lie beside one another.
+static bool rows_beside(int64_t n0, int64_t s0, int64_t n1, int64_t s1, int64_t width) {
+  using Wide = __int128;   // (strides are any 64-bit numbers)
+  Wide outer = s0 < 0 ? -(Wide)s0 : s0, inner = s1 < 0 ? -(Wide)s1 : s1;
+  if (n0 == 1) outer = (Wide)1 << 100;
+  if (n1 == 1) inner = (Wide)1 << 100;
+  if (outer < inner) {
+    std::swap(outer, inner);
+    std::swap(n0, n1);
+  }
+  if (inner < width) return false;
+  if (n0 == 1 || outer >= (n1 - 1) * inner + width) return true;
+  // rows that interleave: the inner one nearest to each outer step (steps past the inner rows' extent meet none)
+  for (Wide i = 1; i < n0 && i * outer < (n1 - 1) * inner + width; ++i) {
+    const Wide j = i * outer / inner;
+    for (Wide k = j; k <= j + 1 && k < n1; ++k) {
+      const Wide d = i * outer - k * inner;
+      if (d < width && d > -(Wide)width) return false;
+    }
+  }
+  return true;
+}
+
 static qlin_status check_cache(const qlin_cache_t* c) {
   if (c == nullptr || c->k == nullptr || c->v == nullptr || c->page_table == nullptr || c->cached == nullptr ||
       c->q_start == nullptr)
@@ -671,14 +695,12 @@ qlin_status qlin_cache_append(const qlin_cache_t* c, const qlin_cache_append_t* 
     if (a->q == a->q_out &&
         (a->q_token_stride != a->q_out_token_stride || a->q_head_stride != a->q_out_head_stride))
       return QLIN_ERR_INVALID_ARG;
-    auto apart = [&](int64_t n, int64_t stride) {
-      return n == 1 || stride >= c->head_dim || stride <= -(int64_t)c->head_dim;
-    };
-    if (!apart(a->tokens, a->q_out_token_stride) || !apart(a->q_heads, a->q_out_head_stride))
+    if (a->tokens > 1 << 28 || a->q_heads > 65536) return QLIN_ERR_UNSUPPORTED;
+    if (!rows_beside(a->tokens, a->q_out_token_stride, a->q_heads, a->q_out_head_stride, c->head_dim))
       return QLIN_ERR_INVALID_ARG;
     if (!aligned(a->q, 2) || !aligned(a->q_out, 2)) return QLIN_ERR_MISALIGNED;
   }
-  if (a->tokens > 1 << 28 || (a->q != nullptr && a->q_heads > 65536)) return QLIN_ERR_UNSUPPORTED;
+  if (a->tokens > 1 << 28) return QLIN_ERR_UNSUPPORTED;
   if (!aligned(a->k, 2) || !aligned(a->v, 2) ||
       (c->format != QLIN_CACHE_E4M3 && (!aligned(c->k, 2) || !aligned(c->v, 2))))
     return QLIN_ERR_MISALIGNED;
@@ -703,10 +725,6 @@ qlin_status qlin_cache_attention(const qlin_cache_t* c, const qlin_cache_attenti
   if (a->q == a->out &&
       (a->q_token_stride != a->out_token_stride || a->q_head_stride != a->out_head_stride))
     return QLIN_ERR_INVALID_ARG;
-  auto apart = [&](int64_t n, int64_t stride) {
-    return n == 1 || stride >= c->head_dim || stride <= -(int64_t)c->head_dim;
-  };
-  if (!apart(a->tokens, a->out_token_stride) || !apart(a->q_heads, a->out_head_stride)) return QLIN_ERR_INVALID_ARG;
   if (c->head_dim % 16 != 0 || (c->format != QLIN_CACHE_E4M3 && c->format != a->dtype)) return QLIN_ERR_UNSUPPORTED;
   // (rows, and the tiles of a call, are counted in 31 and 43 bits)
   if (a->tokens > 1 << 24 || a->q_heads > 65536 || a->tokens * (a->q_heads / c->heads) > (int64_t)1 << 30)
@@ -719,6 +737,8 @@ qlin_status qlin_cache_attention(const qlin_cache_t* c, const qlin_cache_attenti
       ((a->q_token_stride | a->q_head_stride | a->out_token_stride | a->out_head_stride) & 7) != 0 ||
       !aligned(a->lse, 4) || !aligned(a->mask, 8))
     return QLIN_ERR_MISALIGNED;
+  if (!rows_beside(a->tokens, a->out_token_stride, a->q_heads, a->out_head_stride, c->head_dim))
+    return QLIN_ERR_INVALID_ARG;
   if (workspace == nullptr || ws_bytes < qlin_cache_attention_workspace_size()) return QLIN_ERR_WORKSPACE;
   if (!aligned(workspace, 16)) return QLIN_ERR_MISALIGNED;
   unsigned* status;
