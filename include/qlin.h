@@ -647,7 +647,9 @@ qlin_status qlin_cache_append(const qlin_cache_t *cache, const qlin_cache_append
  * Query head h reads KV head h / (q_heads / heads).  Every new token sees all cached ones;
  * of the new ones, mask bit i of token t's words (bit i % 64 of word i / 64) says whether t
  * sees new token i, itself among them; bits past the words are 0.  mask NULL: those up to
- * itself.  A row that sees nothing gives zeros and lse -infinity.  NaN and infinities in
+ * itself.  A row that sees nothing, or only keys of score -infinity, gives zeros and lse
+ * -infinity.  A row that sees a key is NaN with a NaN in its query or in a key that it sees, and
+ * in the elements of NaN in values that it sees, whatever these weigh.  NaN and infinities in
  * keys and values that a row does not see do not reach it.  Scores, running maximum and sum
  * and the products' sums in fp32; probabilities are rounded to the 16 bits of the cache's type
  * (E4M3: fp16) for the product with v, those in fp16 after a factor that keeps weights from 2^-32
@@ -664,6 +666,10 @@ qlin_status qlin_cache_append(const qlin_cache_t *cache, const qlin_cache_append
  *          zero.  Calls whose work overlaps on the GPU must not share one.
  * A 16-bit cache has the type of q.  head_dim: a multiple of 16.  Cache rows 16-byte aligned.
  * At most 2^24 tokens, and 2^30 of tokens times q_heads / heads.
+ * Keys are read once for up to 256 rows (a group's query heads times new tokens; 128 for heads
+ * past 128) where pages are multiples of 8 slots that divide the kernel's tiles of 128 keys (64
+ * for heads past 128) or are multiples of them; with other pages, once for every 16 (head_dim
+ * up to 64: 32), which many new tokens feel.
  * Sums are joined in the order of the keys, split by all sequences' lengths: equal calls give
  * equal bits, other batches may change the last ones.
  * Errors: INVALID_ARG, MISALIGNED, UNSUPPORTED, WORKSPACE, CUDA.

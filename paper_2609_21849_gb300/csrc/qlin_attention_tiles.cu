@@ -29,8 +29,8 @@
 // of these, at one SM's rate of reading, the trees below took 40 us longer); it takes 14 of their us.
 //   Measured, 16 trees of 64 tokens behind 8192-16384 keys, 8 KV heads of 128, 4 query heads each:
 // 199 us (bf16; the keys and values from HBM need 126, the MMAs 106), 221 from E4M3; 288 at heads of
-// 256 behind half as many keys.  About 3600 cycles a tile: the tensor pipe is busy a third of the time
-// and no issue slot is short; what lasts is each stream's chain of scores, maximum, exponentials, P
+// 256 behind half as many keys.  About 3600 cycles a tile, of which the MMAs take 2048 to 2560, and no
+// issue slot is short; what lasts is each stream's chain of scores, maximum, exponentials, P
 // and products, of which two run at a time.  A segment's begin and end (Q's way in, the first scores,
 // the tiles with masks, the last products, O's way out) take 10000 to 20000 cycles, many of them for
 // instructions that no tile before them brought: their loops stay short.

@@ -7,10 +7,10 @@
 // epilogue's warpgroups (one per 64 columns), which hold the tile's accumulators, take it from there.
 //   wide   128 x 256 tiles.  A block is 512 cycles of MMAs, in which 128 x 256 sums leave tensor memory
 //          and pass 32768 FMAs (256 cycles, two per instruction); 48 KB reach the SM for it, 750 cycles
-//          at 64 bytes each, which is what it takes: 4608 x 12288 x 3072 160 us.  (With W's half sent
-//          by each CTA of two to both it took 160.4: what a copy sent to two CTAs saves is reads of L2, not
-//          what comes into an SM.  As a CTA pair with cta_group::2, every buffer's way to the epilogue
-//          and back crossed the pair: 950 cycles a block.)
+//          at 64 bytes each.  It takes 0.43-0.45 us, about 830, a tile's begin and end 6 us: 4608 x 12288
+//          x 3072 160 us.  (With W's half sent by each CTA of two to both it took 160.4: what a copy sent
+//          to two CTAs saves is reads of L2, not what comes into an SM.  As a CTA pair with cta_group::2,
+//          every buffer's way to the epilogue and back crossed the pair: 950 cycles a block.)
 //   single 128 x 128 tiles, for fewer rows, also with K shared by a cluster.
 // Roles: warp 0 loads (TMA), warp 1 issues the MMAs, warp 2 multiplies the scales of a block's rows
 // and columns into shared memory (loads of them by the epilogue's own warps cost 20 to 40 of 180

@@ -143,3 +143,19 @@ def test_rows_that_see_nothing_whatever_the_scale_and_the_query():
             out = qlin.qlin_cache_attention(c, q, 0.125, torch.zeros(T, 1, dtype=torch.int64, device="cuda"), lse=lse)
             assert (out == 0).all() and (lse == -math.inf).all()
     assert qlin.qlin_sync_status() == 0
+
+
+@pytest.mark.parametrize("fmt,dtype", [f for f in FORMATS if f[0] != "e4m3"])
+@pytest.mark.parametrize("T,G,have", FORMS)
+def test_scores_of_minus_infinity(T, G, have, fmt, dtype):
+    """Beside finite scores they weigh nothing; a row that sees no others comes out as one that sees
+    no key."""
+    c, q = _setup(T, G, have, fmt, dtype)
+    q[..., 0] = 1.0
+    where = _slots(c, 0, have + T)
+    c.k[where + (slice(None), 0)] = -math.inf
+    out, lse = _call(c, q)
+    assert (out == 0).all() and (lse == -math.inf).all()
+    c.k[where[0][1:], where[1][1:], :, 0] = 0.0
+    out, lse = _call(c, q)
+    assert out.isfinite().all() and lse.isfinite().all()
